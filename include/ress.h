@@ -9,6 +9,9 @@
  *   ress_sparse_attn exact attention over the kept 64x64 blocks (Sec. 3 step (3))
  *   ress_forward     the three in order on one stream (ress_forward_host: from and to
  *                    host buffers, the output copied back while the attention runs)
+ * What forms Q, K and V out of the residual stream before it: ress_layer_norm, ress_qkv_proj
+ * (projection, per-head norm and rotary positions in one kernel), ress_rope (the latter two on
+ * their own), and the gradients ress_layer_norm_bwd and ress_rope_bwd.
  * Also: the ablation variants of the selection (ress_score_variant, ress_restore_variant),
  * the residual update and token-level drift (ress_out_proj, ress_token_drift), an
  * allocation-free attention entry point, and a bounded-wait self-test of the error path.
@@ -284,6 +287,130 @@ int ress_out_proj(const ress_dims* dims, const uint16_t* O, const uint16_t* W_o,
  * d_model must be a multiple of 64.  Uses the workspace's status word only. */
 int ress_token_drift(const ress_dims* dims, const uint16_t* O_a, const uint16_t* O_b,
                      const uint16_t* W_o, float* drift, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- The input half of the sublayer -----------------------------------------------------
+ * From the residual stream x to Q, K and V: layer norm, projection, a layer norm over each
+ * head's channels of Q and K where the backbone has one, and rotary positions over the axes of
+ * the tokens' positions (row and column of a patch; a time axis as well for video).  The paper
+ * takes Q, K and V as given; these calls have no counterpart in it.  The gradients serve
+ * fine-tuning and the calibration of head budgets from gradients of the projections (Sec. 4.4,
+ * Appendix D).  Sums and statistics are float32; every result is rounded once. */
+typedef enum { RESS_BF16 = 0, RESS_F16 = 1, RESS_F32 = 2 } ress_dtype;
+
+/* Rows for ress_layer_norm and its gradient.  Strides are in elements, from a row to the next;
+ * an input's stride may be any number >= 0 (0: one row for all), an output's at least `width`.
+ * Tensors need the alignment of their elements; 16-byte aligned ones whose strides and width
+ * are multiples of 16 bytes are read and written 16 bytes at a time. */
+#define RESS_MAX_WIDTH 16384
+typedef struct {
+  int64_t rows;       /* >= 0                                                              */
+  int32_t width;      /* channels of a row, 1..RESS_MAX_WIDTH                              */
+  int32_t x_type;     /* ress_dtype of x (and of dx, dres)                                 */
+  int32_t y_type;     /* of y (and dy): x_type, or RESS_BF16 or RESS_F16 with x RESS_F32   */
+  int32_t param_type; /* of weight and bias: any ress_dtype                                */
+  float eps;          /* >= 0                                                              */
+  int64_t x_stride, y_stride; /* of x; of y and dy                                         */
+  int64_t dx_stride, dres_stride; /* of dx and dres (ress_layer_norm_bwd)                  */
+} ress_norm;
+
+/* y = (x - mean) rstd weight + bias with mean = avg(x) and rstd = 1 / sqrt(avg((x - mean)^2) +
+ * eps) over each row.  weight, bias: device [width], NULL for 1 and 0.  mean, rstd: device
+ * float32 [rows] outputs for the gradient, NULL to skip.  y may be x (same type and stride). */
+int ress_layer_norm(const ress_norm* n, const void* x, const void* weight, const void* bias,
+                    void* y, float* mean, float* rstd, void* stream);
+
+/* Gradients of ress_layer_norm: with h = (x - mean) rstd and g = dy weight
+ *   dx = rstd (g - avg(g) - h avg(g h)) + dres,  dweight = sum_rows dy h,  dbias = sum_rows dy.
+ * mean, rstd: as the forward call wrote them.  dres (x's type; NULL: 0) is the gradient of the
+ * residual branch around the norm.  dx may be dy or dres (same type and stride).  dweight,
+ * dbias: device float32 [width] outputs, NULL to skip; their sums over the rows are formed in a
+ * fixed order.  ws: 256-byte aligned, ress_layer_norm_workspace_bytes(n) bytes (unused, and may
+ * be NULL, without dweight and dbias); it needs no initialisation and has no status word. */
+size_t ress_layer_norm_workspace_bytes(const ress_norm* n);
+int ress_layer_norm_bwd(const ress_norm* n, const void* dy, const void* x, const void* weight,
+                        const float* mean, const float* rstd, const void* dres, void* dx,
+                        float* dweight, float* dbias, void* ws, size_t ws_bytes, void* stream);
+
+/* Rotary positions over several axes.  Axis a rotates axis_dims[a] channels of a head (an even
+ * number), as axis_dims[a] / 2 pairs: pair i of axis a turns by the angle pos[token, a] * freq
+ * of that pair, (u, v) -> (u cos - v sin, v cos + u sin).  The pairs of all axes, axis after
+ * axis, are numbered p = 0..n_pairs-1.  Which channels make pair p depends on the layout:
+ *   RESS_ROPE_SECTIONS    each axis has a section of axis_dims[a] consecutive channels, and
+ *                         pairs the first half of it with the second
+ *   RESS_ROPE_HALVES      (p, n_pairs + p)
+ *   RESS_ROPE_INTERLEAVED (2p, 2p + 1)
+ * Channels from 2 n_pairs to head_dim are not rotated.  A plan is plain host data, filled by
+ * ress_rope_plan_init and passed by pointer; it may be copied.  head_dim: even, 2..256.
+ * freq: n_pairs angles in radians per unit position (finite), or NULL for base^(-2i/axis_dims[a])
+ * with i counted within each axis and base > 0.  Angles are exact for every int32 position. */
+typedef enum { RESS_ROPE_SECTIONS = 0, RESS_ROPE_HALVES = 1, RESS_ROPE_INTERLEAVED = 2 } ress_rope_layout;
+#define RESS_ROPE_MAX_AXES 4
+#define RESS_ROPE_MAX_DIM 256
+#define RESS_ROPE_MAX_HEADS 4096
+typedef struct {
+  int32_t head_dim, n_axes;
+  int32_t axis_dims[RESS_ROPE_MAX_AXES];
+  int32_t layout;   /* ress_rope_layout */
+  int32_t n_pairs;  /* sum of axis_dims / 2 */
+  uint64_t turns[RESS_ROPE_MAX_DIM / 2]; /* freq / (2 pi) modulo 1, in units of 2^-64 */
+} ress_rope_plan;
+int ress_rope_plan_init(ress_rope_plan* plan, int32_t head_dim, int32_t n_axes,
+                        const int32_t* axis_dims, int32_t layout, double base, const double* freq);
+
+/* Heads of one tensor [n_tokens, n_heads, head_dim]: strides in elements from a token to the
+ * next and from a head to the next, channels next to each other. */
+typedef struct {
+  void* data;
+  int64_t token_stride, head_stride;
+} ress_heads;
+/* A layer norm over each head's channels, shared by the heads: weight, bias device [head_dim]
+ * (NULL: 1 and 0). */
+typedef struct {
+  int32_t enabled; /* 0: no norm */
+  const void *weight, *bias;
+} ress_head_norm;
+typedef struct {
+  int32_t n_heads;
+  ress_head_norm norm;
+  ress_heads x;  /* the heads before the norm: input (backward: needed with a norm only)    */
+  ress_heads y;  /* forward output; backward input, the gradient of y                       */
+  ress_heads dx; /* backward output, the gradient of x                                      */
+  float *dweight, *dbias; /* backward float32 [head_dim] outputs of a norm, NULL to skip    */
+} ress_rope_heads;
+
+/* y = rotated(norm(x)) for the heads of one or two tensors of the same tokens (q, k; either may
+ * be NULL, their head counts may differ).  pos: device int32 [n_tokens, n_axes].  type:
+ * ress_dtype of x and y; param_type: of the norms' weights and biases; eps as in ress_norm.
+ * n_tokens >= 0.  y may be x with the same strides; otherwise outputs must not overlap inputs.
+ * Input strides may be 0; an output's heads must not overlap. */
+int ress_rope(const ress_rope_plan* plan, int64_t n_tokens, const int32_t* pos, int32_t type,
+              int32_t param_type, float eps, const ress_rope_heads* q, const ress_rope_heads* k,
+              void* stream);
+
+/* Gradients of ress_rope: y is the gradient of its output, dx receives that of x (dx may be y
+ * with the same strides), dweight and dbias those of the norm's parameters, summed over tokens
+ * and heads in a fixed order.  x is read where there is a norm.  ws: 256-byte aligned,
+ * ress_rope_workspace_bytes() bytes (unused, and may be NULL, where no dweight or dbias is
+ * asked for); it needs no initialisation and has no status word. */
+size_t ress_rope_workspace_bytes(const ress_rope_plan* plan, int64_t n_tokens, int32_t q_heads,
+                                 int32_t k_heads);
+int ress_rope_bwd(const ress_rope_plan* plan, int64_t n_tokens, const int32_t* pos, int32_t type,
+                  int32_t param_type, float eps, const ress_rope_heads* q, const ress_rope_heads* k,
+                  void* ws, size_t ws_bytes, void* stream);
+
+/* Q, K and V of a layer: Q = x W_q^T + b_q and so on, then ress_rope's norms and rotation on Q and
+ * K before the result is rounded to bf16.  x: device bf16 [N, d_model] (the norm's output); W_q,
+ * W_k, W_v: device bf16 [H*64, d_model] (Linear weight, out x in; rows of one stacked weight
+ * will do); b_q, b_k, b_v: device bf16 [H*64] or NULL; Q, K, V: device bf16 [N, H, 64], as
+ * ress_forward takes them.  plan (head_dim 64) and pos as in ress_rope, both NULL for no rotation.
+ * q_norm, k_norm: NULL or not enabled for none.  fp32 accumulation on the tensor cores
+ * (tcgen05).  d_model must be a multiple of 64.  Uses the workspace's status word only. */
+int ress_qkv_proj(const ress_dims* dims, const uint16_t* x, const uint16_t* W_q,
+                  const uint16_t* W_k, const uint16_t* W_v, const uint16_t* b_q,
+                  const uint16_t* b_k, const uint16_t* b_v, const ress_rope_plan* plan,
+                  const int32_t* pos, const ress_head_norm* q_norm, const ress_head_norm* k_norm,
+                  int32_t param_type, float eps, uint16_t* Q, uint16_t* K, uint16_t* V, void* ws,
+                  size_t ws_bytes, void* stream);
 
 /* Allocation-free variant of ress_sparse_attn (the paper has no counterpart: this is an
  * interface for callers, not part of the method).  It is for callers that cannot allocate

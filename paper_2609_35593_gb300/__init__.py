@@ -70,6 +70,41 @@ class WsLayout(ctypes.Structure):
                  "cdot", "ny", "nz", "lstat", "kcount", "prow", "ld", "words", "total")]
 
 
+class Norm(ctypes.Structure):
+    """ress_norm: rows for the layer norm and its gradient."""
+    _fields_ = [("rows", ctypes.c_int64), ("width", ctypes.c_int32), ("x_type", ctypes.c_int32),
+                ("y_type", ctypes.c_int32), ("param_type", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("x_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64), ("dx_stride", ctypes.c_int64),
+                ("dres_stride", ctypes.c_int64)]
+
+
+ROPE_MAX_AXES, ROPE_MAX_DIM = 4, 256
+_LAYOUTS = {"sections": 0, "halves": 1, "interleaved": 2}
+
+
+class RopePlan(ctypes.Structure):
+    """ress_rope_plan: which channels of a head rotate with which axis, and how fast."""
+    _fields_ = [("head_dim", ctypes.c_int32), ("n_axes", ctypes.c_int32),
+                ("axis_dims", ctypes.c_int32 * ROPE_MAX_AXES), ("layout", ctypes.c_int32),
+                ("n_pairs", ctypes.c_int32), ("turns", ctypes.c_uint64 * (ROPE_MAX_DIM // 2))]
+
+
+class Heads(ctypes.Structure):
+    """ress_heads: the heads of one tensor, by their strides in elements."""
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class HeadNorm(ctypes.Structure):
+    """ress_head_norm: a layer norm over each head's channels."""
+    _fields_ = [("enabled", ctypes.c_int32), ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p)]
+
+
+class RopeHeads(ctypes.Structure):
+    """ress_rope_heads: one tensor of a ress_rope call."""
+    _fields_ = [("n_heads", ctypes.c_int32), ("norm", HeadNorm), ("x", Heads), ("y", Heads), ("dx", Heads),
+                ("dweight", ctypes.c_void_p), ("dbias", ctypes.c_void_p)]
+
+
 _c = ctypes
 _P = _c.c_void_p
 _SIGS = {
@@ -108,6 +143,20 @@ _SIGS = {
     "ress_token_drift": (_c.c_int, [_c.POINTER(Dims), _P, _P, _P, _P, _P, _c.c_size_t, _P]),
     "ress_sparse_attn_noalloc": (_c.c_int, [_c.POINTER(Dims), _P, _P, _P, _P, _P, _c.c_int64, _P,
                                             _c.c_int32, _P]),
+    "ress_layer_norm": (_c.c_int, [_c.POINTER(Norm), _P, _P, _P, _P, _P, _P, _P]),
+    "ress_layer_norm_workspace_bytes": (_c.c_size_t, [_c.POINTER(Norm)]),
+    "ress_layer_norm_bwd": (_c.c_int, [_c.POINTER(Norm), _P, _P, _P, _P, _P, _P, _P, _P, _P, _P,
+                                       _c.c_size_t, _P]),
+    "ress_rope_plan_init": (_c.c_int, [_c.POINTER(RopePlan), _c.c_int32, _c.c_int32, _P, _c.c_int32,
+                                       _c.c_double, _P]),
+    "ress_rope": (_c.c_int, [_c.POINTER(RopePlan), _c.c_int64, _P, _c.c_int32, _c.c_int32, _c.c_float,
+                             _c.POINTER(RopeHeads), _c.POINTER(RopeHeads), _P]),
+    "ress_rope_workspace_bytes": (_c.c_size_t, [_c.POINTER(RopePlan), _c.c_int64, _c.c_int32, _c.c_int32]),
+    "ress_rope_bwd": (_c.c_int, [_c.POINTER(RopePlan), _c.c_int64, _P, _c.c_int32, _c.c_int32, _c.c_float,
+                                 _c.POINTER(RopeHeads), _c.POINTER(RopeHeads), _P, _c.c_size_t, _P]),
+    "ress_qkv_proj": (_c.c_int, [_c.POINTER(Dims), _P, _P, _P, _P, _P, _P, _P, _c.POINTER(RopePlan), _P,
+                                 _c.POINTER(HeadNorm), _c.POINTER(HeadNorm), _c.c_int32, _c.c_float, _P, _P,
+                                 _P, _P, _c.c_size_t, _P]),
 }
 for _name, (_res, _args) in _SIGS.items():
     _f = getattr(_lib, _name)
@@ -348,6 +397,221 @@ def wait_selftest(ws, limit_us: int = 20000, stream=None):
 def status(ws, stream=None):
     """Synchronise, read and clear the device status word; raise on a device-side error."""
     _check(_lib.ress_status(_dev(ws, None, "ws"), _stream(stream)))
+
+
+# ---- the input half of the sublayer ---------------------------------------------------
+def _dtype_code(t, name):
+    torch = _torch()
+    code = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected bfloat16, float16 or float32")
+    return code
+
+
+def _cuda(t, name, dtype=None):
+    """Device pointer of a CUDA tensor of any layout (None -> NULL)."""
+    if t is None:
+        return None
+    if not isinstance(t, _torch().Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.device.type != "cuda":
+        raise ValueError(f"{name} must live on a CUDA device")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    return t.data_ptr()
+
+
+def _vector(t, n, name, dtype=None):
+    """Device pointer of n contiguous elements (None -> NULL)."""
+    p = _cuda(t, name, dtype)
+    if t is not None and (t.numel() != n or not t.is_contiguous()):
+        raise ValueError(f"{name} must have {n} contiguous elements")
+    return p
+
+
+def _rows(t, name, like=None):
+    """(rows, width, stride) of a tensor [..., width] whose rows are a fixed stride apart."""
+    if t.dim() < 1 or (like is not None and t.shape != like.shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}" + (f", expected {tuple(like.shape)}" if like is not None else ""))
+    width = t.shape[-1]
+    rows = t.numel() // width if width else 0
+    if t.is_contiguous():
+        return rows, width, width
+    if t.dim() != 2 or (width > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be contiguous, or two-dimensional with contiguous rows")
+    return rows, width, t.stride(0)
+
+
+def _param_code(name, *params):
+    """The one dtype of the parameters that are given (float32 if none is)."""
+    codes = {_dtype_code(p, name) for p in params if p is not None}
+    if len(codes) > 1:
+        raise TypeError(f"{name}: weights and biases of different dtypes")
+    return codes.pop() if codes else 2
+
+
+def layer_norm(x, weight, bias, y, eps: float = 1e-5, mean=None, rstd=None, stream=None):
+    """ress_layer_norm over the last dimension of x [..., width] into y of the same shape; weight, bias
+    [width] or None; mean, rstd: float32 outputs, one per row, for layer_norm_bwd, or None."""
+    f32 = _torch().float32
+    px, py = _cuda(x, "x"), _cuda(y, "y")
+    rows, width, sx = _rows(x, "x")
+    n = Norm(rows, width, _dtype_code(x, "x"), _dtype_code(y, "y"), _param_code("layer_norm", weight, bias),
+             eps, sx, _rows(y, "y", x)[2], 0, 0)
+    _check(_lib.ress_layer_norm(n, px, _vector(weight, width, "weight"), _vector(bias, width, "bias"), py,
+                                _vector(mean, rows, "mean", f32), _vector(rstd, rows, "rstd", f32),
+                                _stream(stream)))
+
+
+def layer_norm_workspace_bytes(rows: int, width: int) -> int:
+    """Workspace of layer_norm_bwd on rows of this width."""
+    n = _lib.ress_layer_norm_workspace_bytes(Norm(rows, width, 0, 0, 0, 0.0, width, width, width, width))
+    if n == 0:
+        raise RessError(-1, _lib.ress_last_error().decode())
+    return n
+
+
+def layer_norm_bwd(dy, x, weight, mean, rstd, dx, dweight=None, dbias=None, dres=None, ws=None, stream=None):
+    """ress_layer_norm_bwd: dx (+ dres where given) and the float32 gradients of weight and bias
+    (None to skip; ws is needed for them) from the gradient dy of layer_norm's y."""
+    f32 = _torch().float32
+    pdy, px, pdx, pres = _cuda(dy, "dy"), _cuda(x, "x"), _cuda(dx, "dx", x.dtype), _cuda(dres, "dres", x.dtype)
+    rows, width, sx = _rows(x, "x")
+    n = Norm(rows, width, _dtype_code(x, "x"), _dtype_code(dy, "dy"), _param_code("layer_norm_bwd", weight), 0.0,
+             sx, _rows(dy, "dy", x)[2], _rows(dx, "dx", x)[2], 0 if dres is None else _rows(dres, "dres", x)[2])
+    if mean is None or rstd is None:
+        raise ValueError("mean and rstd are those layer_norm saved")
+    _check(_lib.ress_layer_norm_bwd(n, pdy, px, _vector(weight, width, "weight"), _vector(mean, rows, "mean", f32),
+                                    _vector(rstd, rows, "rstd", f32), pres, pdx,
+                                    _vector(dweight, width, "dweight", f32), _vector(dbias, width, "dbias", f32),
+                                    _dev(ws, None, "ws"), 0 if ws is None else ws.numel() * ws.element_size(),
+                                    _stream(stream)))
+
+
+def rope_plan(axis_dims, head_dim: int = HEAD_DIM, base: float = 100.0, layout: str = "sections",
+              freq=None) -> RopePlan:
+    """ress_rope_plan_init: axis_dims[a] channels of a head rotate with axis a of the positions.
+    layout: sections, halves or interleaved (include/ress.h); freq: radians per unit position of
+    each pair, or None for base^(-2i / axis_dims[a])."""
+    plan = RopePlan()
+    axis_dims = [int(a) for a in axis_dims]
+    arr = None
+    if freq is not None:
+        freq = [float(f) for f in freq]
+        if len(freq) != sum(a // 2 for a in axis_dims):
+            raise ValueError(f"{len(freq)} frequencies for {sum(a // 2 for a in axis_dims)} pairs")
+        arr = (_c.c_double * len(freq))(*freq)
+    _check(_lib.ress_rope_plan_init(plan, int(head_dim), len(axis_dims), (_c.c_int32 * len(axis_dims))(*axis_dims),
+                                    _LAYOUTS[layout], float(base), arr))
+    return plan
+
+
+def _heads(t, plan, tokens, name, dtype, heads=None):
+    """ress_heads of a tensor [tokens, heads, head_dim] with contiguous channels."""
+    p = _cuda(t, name, dtype)
+    if t is None:
+        raise ValueError(f"{name} is missing")
+    if t.dim() != 3 or t.shape[0] != tokens or t.shape[2] != plan.head_dim or (heads is not None and t.shape[1] != heads):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected ({tokens}, {heads or 'heads'}, {plan.head_dim})")
+    if t.stride(2) != 1:
+        raise ValueError(f"{name} must have contiguous channels")
+    return Heads(p, t.stride(0), t.stride(1))
+
+
+def _head_norm(norm, n, name):
+    """ress_head_norm of None or (weight, bias)."""
+    if norm is None:
+        return HeadNorm(0, None, None)
+    weight, bias = norm
+    return HeadNorm(1, _vector(weight, n, name + " weight"), _vector(bias, n, name + " bias"))
+
+
+def _positions(plan, pos):
+    if pos.dim() != 2 or pos.shape[1] != plan.n_axes:
+        raise ValueError(f"pos has shape {tuple(pos.shape)}, expected (tokens, {plan.n_axes})")
+    return _dev(pos, (_torch().int32,), "pos")
+
+
+def _rope_tensor(plan, tokens, name, x, y, dx, norm, grads, dtype):
+    """ress_rope_heads, or None where the tensor is absent."""
+    if y is None:
+        if x is not None or dx is not None or norm is not None or grads is not None:
+            raise ValueError(f"{name}: an input or a norm without its output")
+        return None
+    h = y.shape[1] if y.dim() == 3 else None
+    f32 = _torch().float32
+    none = Heads(None, 0, 0)
+    dweight, dbias = grads if grads is not None else (None, None)
+    return RopeHeads(h or 0, _head_norm(norm, plan.head_dim, name + "_norm"),
+                     none if x is None else _heads(x, plan, tokens, name, dtype, h),
+                     _heads(y, plan, tokens, name + "'s result", dtype, h),
+                     none if dx is None else _heads(dx, plan, tokens, name + "'s gradient", dtype, h),
+                     _vector(dweight, plan.head_dim, name + " dweight", f32),
+                     _vector(dbias, plan.head_dim, name + " dbias", f32))
+
+
+def _norm_params(q_norm, k_norm):
+    return [p for norm in (q_norm, k_norm) if norm is not None for p in norm]
+
+
+def rope(plan: RopePlan, pos, q, q_out, k=None, k_out=None, q_norm=None, k_norm=None, eps: float = 1e-5,
+         stream=None):
+    """ress_rope: q_out, k_out = the heads of q, k [tokens, heads, head_dim] after a layer norm over
+    their channels (q_norm, k_norm: (weight, bias), either may be None; None: no norm) and rotated by
+    pos, int32 [tokens, axes]."""
+    if q is None or q_out is None or (k is None) != (k_out is None):
+        raise ValueError("q and q_out are needed, and k and k_out together")
+    tokens = pos.shape[0]
+    tq = _rope_tensor(plan, tokens, "q", q, q_out, None, q_norm, None, q.dtype)
+    tk = _rope_tensor(plan, tokens, "k", k, k_out, None, k_norm, None, q.dtype)
+    _check(_lib.ress_rope(plan, tokens, _positions(plan, pos), _dtype_code(q, "q"),
+                          _param_code("rope", *_norm_params(q_norm, k_norm)), eps, tq, tk, _stream(stream)))
+
+
+def rope_workspace_bytes(plan: RopePlan, n_tokens: int, q_heads: int, k_heads: int = 0) -> int:
+    """Workspace of rope_bwd with gradients of the norms' parameters."""
+    n = _lib.ress_rope_workspace_bytes(plan, n_tokens, q_heads, k_heads)
+    if n == 0:
+        raise RessError(-1, _lib.ress_last_error().decode())
+    return n
+
+
+def rope_bwd(plan: RopePlan, pos, dq_out, dq, dk_out=None, dk=None, q=None, k=None, q_norm=None, k_norm=None,
+             q_norm_grads=None, k_norm_grads=None, eps: float = 1e-5, ws=None, stream=None):
+    """ress_rope_bwd: the gradients dq, dk of rope's q, k from those of its outputs, and, with norms
+    (which need q, k again), q_norm_grads, k_norm_grads: float32 (dweight, dbias), either or both None."""
+    if dq_out is None or dq is None or (dk_out is None) != (dk is None):
+        raise ValueError("dq_out and dq are needed, and dk_out and dk together")
+    if (q_norm is not None and q is None) or (k_norm is not None and k is None):
+        raise ValueError("a norm's gradient needs the norm's input")
+    tokens = pos.shape[0]
+    tq = _rope_tensor(plan, tokens, "q", q, dq_out, dq, q_norm, q_norm_grads, dq_out.dtype)
+    tk = _rope_tensor(plan, tokens, "k", k, dk_out, dk, k_norm, k_norm_grads, dq_out.dtype)
+    _check(_lib.ress_rope_bwd(plan, tokens, _positions(plan, pos), _dtype_code(dq_out, "dq_out"),
+                              _param_code("rope_bwd", *_norm_params(q_norm, k_norm)), eps, tq, tk,
+                              _dev(ws, None, "ws"), 0 if ws is None else ws.numel() * ws.element_size(),
+                              _stream(stream)))
+
+
+def qkv_proj(d: Dims, x, W_q, W_k, W_v, Q, K, V, ws, b_q=None, b_k=None, b_v=None, plan: RopePlan = None, pos=None,
+             q_norm=None, k_norm=None, eps: float = 1e-5, stream=None):
+    """ress_qkv_proj: Q, K, V [N, H, 64] = x W^T + b with q_norm, k_norm and the rotation by plan and pos
+    as in rope; bf16 tensors."""
+    b, n, out = _bf16(), d.n_tokens, d.n_heads * HEAD_DIM
+    for t, count, name in ((x, n * d.d_model, "x"), (W_q, out * d.d_model, "W_q"), (W_k, out * d.d_model, "W_k"),
+                           (W_v, out * d.d_model, "W_v"), (Q, n * out, "Q"), (K, n * out, "K"), (V, n * out, "V"),
+                           (b_q, out, "b_q"), (b_k, out, "b_k"), (b_v, out, "b_v")):
+        if t is not None and t.numel() != count:
+            raise ValueError(f"{name} has {t.numel()} elements, expected {count}")
+    if plan is not None and (pos is None or pos.shape[0] != n):
+        raise ValueError(f"pos must have the positions of {n} tokens")
+    _check(_lib.ress_qkv_proj(d, _dev(x, b, "x"), _dev(W_q, b, "W_q"), _dev(W_k, b, "W_k"), _dev(W_v, b, "W_v"),
+                              _dev(b_q, b, "b_q"), _dev(b_k, b, "b_k"), _dev(b_v, b, "b_v"), plan,
+                              None if pos is None else _positions(plan, pos) if plan is not None else _dev(pos, None, "pos"),
+                              _head_norm(q_norm, HEAD_DIM, "q_norm"), _head_norm(k_norm, HEAD_DIM, "k_norm"),
+                              _param_code("qkv_proj", *_norm_params(q_norm, k_norm)), eps, _dev(Q, b, "Q"),
+                              _dev(K, b, "K"), _dev(V, b, "V"), _dev(ws, None, "ws"),
+                              ws.numel() * ws.element_size(), _stream(stream)))
 
 
 class Buffers:

@@ -1,6 +1,8 @@
 // C ABI of the ReSS hot path: host-side validation, workspace layout and launch order.
 // Every check happens before the first launch; nothing here allocates device memory.
 
+#include <float.h>
+#include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
 #include <string.h>
@@ -546,11 +548,11 @@ int ress_status(void* ws, void* stream) {
   return fail(RESS_EDEVICE, "device-side argument check failed (code %u)", word);
 }
 
-static int oproj_checks(const ress_dims* d, const void* W_o, void* ws, size_t ws_bytes,
+static int oproj_checks(const ress_dims* d, const void* W, const char* name, void* ws, size_t ws_bytes,
                         ress::Shape* s, ress_ws_layout* L) {
   int e = check_dims(d);
   if (e) return e;
-  if ((e = check_ptr(W_o, 16, "W_o"))) return e;
+  if ((e = check_ptr(W, 16, name))) return e;
   if (d->d_model % 64 != 0)
     return fail(RESS_EUNSUPPORTED, "d_model %d must be a multiple of 64", d->d_model);
   *s = ress::make_shape(*d);
@@ -561,7 +563,7 @@ int ress_out_proj(const ress_dims* d, const uint16_t* O, const uint16_t* W_o, co
                   uint16_t* y, void* ws, size_t ws_bytes, void* stream) {
   ress::Shape s{};
   ress_ws_layout L{};
-  int e = oproj_checks(d, W_o, ws, ws_bytes, &s, &L);
+  int e = oproj_checks(d, W_o, "W_o", ws, ws_bytes, &s, &L);
   if (e) return e;
   if ((e = check_ptr(O, 16, "O")) || (e = check_ptr(y, 16, "y"))) return e;
   if (x && (e = check_ptr(x, 16, "x"))) return e;
@@ -585,7 +587,7 @@ int ress_token_drift(const ress_dims* d, const uint16_t* O_a, const uint16_t* O_
                      const uint16_t* W_o, float* drift, void* ws, size_t ws_bytes, void* stream) {
   ress::Shape s{};
   ress_ws_layout L{};
-  int e = oproj_checks(d, W_o, ws, ws_bytes, &s, &L);
+  int e = oproj_checks(d, W_o, "W_o", ws, ws_bytes, &s, &L);
   if (e) return e;
   if ((e = check_ptr(O_a, 16, "O_a")) || (e = check_ptr(O_b, 16, "O_b")) ||
       (e = check_ptr(drift, 4, "drift")))
@@ -603,6 +605,330 @@ int ress_token_drift(const ress_dims* d, const uint16_t* O_a, const uint16_t* O_
   a.status = reinterpret_cast<uint32_t*>(static_cast<char*>(ws) + L.status);
   cudaError_t ce = ress::launch_token_drift(a, static_cast<cudaStream_t>(stream));
   if (ce != cudaSuccess) return cuda_fail(ce, "ress_token_drift");
+  return ok();
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------------------
+// The input half of the sublayer.
+// ---------------------------------------------------------------------------------------
+namespace {
+
+size_t type_bytes(int t) { return t == RESS_F32 ? 4 : 2; }
+
+int check_type(int t, const char* name) {
+  if (t < RESS_BF16 || t > RESS_F32) return fail(RESS_EUNSUPPORTED, "%s %d is no ress_dtype", name, t);
+  return RESS_OK;
+}
+
+int check_opt_ptr(const void* p, size_t align, const char* name) { return p ? check_ptr(p, align, name) : RESS_OK; }
+
+int check_eps(float eps) {
+  if (!(eps >= 0.0f && eps <= FLT_MAX)) return fail(RESS_EINVAL, "eps %g is not a finite number >= 0", (double)eps);
+  return RESS_OK;
+}
+
+int check_norm(const ress_norm* n) {
+  if (!n) return fail(RESS_EINVAL, "norm is NULL");
+  int e;
+  if (n->rows < 0 || n->rows > INT64_MAX / (8 * RESS_MAX_WIDTH))
+    return fail(RESS_EINVAL, "rows %lld out of range", (long long)n->rows);
+  if (n->width < 1 || n->width > RESS_MAX_WIDTH)
+    return fail(RESS_EUNSUPPORTED, "width %d outside 1..%d", n->width, RESS_MAX_WIDTH);
+  if ((e = check_type(n->x_type, "x_type")) || (e = check_type(n->y_type, "y_type")) ||
+      (e = check_type(n->param_type, "param_type")) || (e = check_eps(n->eps)))
+    return e;
+  if (n->y_type != n->x_type && n->x_type != RESS_F32)
+    return fail(RESS_EUNSUPPORTED, "y_type %d with x_type %d (x_type itself, or a 16-bit type with RESS_F32)",
+                n->y_type, n->x_type);
+  return RESS_OK;
+}
+
+// Strides of rows: any number >= 0 for an input, room for a row for an output.
+int check_stride(const ress_norm* n, int64_t stride, bool output, const char* name) {
+  if (n->rows <= 1) return RESS_OK;
+  const int64_t least = output ? n->width : 0;
+  if (stride < least || stride > INT64_MAX / 8 / n->rows)
+    return fail(RESS_EINVAL, "%s %lld outside %lld..", name, (long long)stride, (long long)least);
+  return RESS_OK;
+}
+
+int check_scratch(const void* ws, size_t ws_bytes, size_t need) {
+  int e = check_ptr(ws, 256, "ws");
+  if (e) return e;
+  if (ws_bytes < need) return fail(RESS_EWORKSPACE, "workspace has %zu bytes, needs %zu", ws_bytes, need);
+  return RESS_OK;
+}
+
+int check_plan(const ress_rope_plan* p) {
+  if (!p) return fail(RESS_EINVAL, "plan is NULL");
+  if (p->head_dim < 2 || p->head_dim > RESS_ROPE_MAX_DIM || p->head_dim % 2)
+    return fail(RESS_EUNSUPPORTED, "head_dim %d is not an even number in 2..%d", p->head_dim, RESS_ROPE_MAX_DIM);
+  if (p->n_axes < 1 || p->n_axes > RESS_ROPE_MAX_AXES)
+    return fail(RESS_EUNSUPPORTED, "n_axes %d outside 1..%d", p->n_axes, RESS_ROPE_MAX_AXES);
+  if (p->layout < RESS_ROPE_SECTIONS || p->layout > RESS_ROPE_INTERLEAVED)
+    return fail(RESS_EINVAL, "rope layout %d unknown", p->layout);
+  int sum = 0;
+  for (int a = 0; a < p->n_axes; ++a) {
+    const int d = p->axis_dims[a];
+    if (d < 2 || d % 2 || d > p->head_dim)
+      return fail(RESS_EINVAL, "axis_dims[%d] = %d is not an even number in 2..head_dim", a, d);
+    sum += d;
+  }
+  if (sum > p->head_dim) return fail(RESS_EINVAL, "the axes have %d channels, a head %d", sum, p->head_dim);
+  if (p->n_pairs != sum / 2) return fail(RESS_EINVAL, "n_pairs %d, the axes have %d", p->n_pairs, sum / 2);
+  return RESS_OK;
+}
+
+int check_head_norm(const ress_head_norm& n, int param_type, const char* name) {
+  if (!n.enabled) return RESS_OK;
+  int e;
+  if ((e = check_opt_ptr(n.weight, type_bytes(param_type), name))) return e;
+  return check_opt_ptr(n.bias, type_bytes(param_type), name);
+}
+
+int check_heads(const ress_rope_heads& t, const ress_heads& h, int64_t tokens, int head_dim, size_t bytes, bool output,
+                const char* name) {
+  int e;
+  if (tokens > 0 && (e = check_ptr(h.data, bytes, name))) return e;
+  const int64_t most = INT64_MAX / 16 / (tokens > 0 ? tokens : 1);
+  if (h.token_stride < 0 || h.token_stride > most || h.head_stride < 0 || h.head_stride > most / t.n_heads)
+    return fail(RESS_EINVAL, "%s: strides %lld, %lld out of range", name, (long long)h.token_stride,
+                (long long)h.head_stride);
+  if (!output) return RESS_OK;
+  // heads of a token, then tokens (or the other way round), each clear of the one before
+  const int64_t ht = t.n_heads > 1 ? (t.n_heads - 1) * h.head_stride : 0, tt = tokens > 1 ? (tokens - 1) * h.token_stride : 0;
+  const bool heads_inside = (t.n_heads == 1 || h.head_stride >= head_dim) && (tokens <= 1 || h.token_stride >= ht + head_dim);
+  const bool tokens_inside = (tokens <= 1 || h.token_stride >= head_dim) && (t.n_heads == 1 || h.head_stride >= tt + head_dim);
+  if (!heads_inside && !tokens_inside)
+    return fail(RESS_EINVAL, "%s: strides %lld, %lld make heads overlap", name, (long long)h.token_stride,
+                (long long)h.head_stride);
+  return RESS_OK;
+}
+
+// The checks that ress_rope and its gradient share; fills a.
+int rope_checks(const ress_rope_plan* plan, int64_t n_tokens, const int32_t* pos, int32_t type, int32_t param_type,
+                float eps, const ress_rope_heads* const (&t)[2], bool bwd, ress::RopeArgs* a) {
+  int e;
+  if ((e = check_plan(plan))) return e;
+  if (n_tokens < 0 || n_tokens > INT64_MAX / 4096 / RESS_ROPE_MAX_DIM)
+    return fail(RESS_EINVAL, "n_tokens %lld out of range", (long long)n_tokens);
+  if (n_tokens > 0 && (e = check_ptr(pos, 4, "pos"))) return e;
+  if ((e = check_type(type, "type")) || (e = check_type(param_type, "param_type")) || (e = check_eps(eps))) return e;
+  if (!t[0] && !t[1]) return fail(RESS_EINVAL, "neither q nor k is given");
+  a->plan = *plan;
+  a->n_tokens = n_tokens;
+  a->pos = pos;
+  a->type = type;
+  a->param_type = param_type;
+  a->eps = eps;
+  a->partial = nullptr;
+  const char* names[2][3] = {{"q.x", "q.y", "q.dx"}, {"k.x", "k.y", "k.dx"}};
+  for (int i = 0; i < 2; ++i) {
+    a->t[i] = ress_rope_heads{};
+    if (!t[i]) continue;
+    const ress_rope_heads& h = *t[i];
+    if (h.n_heads < 1 || h.n_heads > RESS_ROPE_MAX_HEADS)
+      return fail(RESS_EUNSUPPORTED, "n_heads %d outside 1..%d", h.n_heads, RESS_ROPE_MAX_HEADS);
+    const size_t b = type_bytes(type);
+    const int hd = plan->head_dim;
+    if ((e = check_head_norm(h.norm, param_type, i ? "k norm" : "q norm"))) return e;
+    if ((!bwd || h.norm.enabled) && (e = check_heads(h, h.x, n_tokens, hd, b, false, names[i][0]))) return e;
+    if ((e = check_heads(h, h.y, n_tokens, hd, b, !bwd, names[i][1]))) return e;
+    if (bwd && (e = check_heads(h, h.dx, n_tokens, hd, b, true, names[i][2]))) return e;
+    if (bwd && ((e = check_opt_ptr(h.dweight, 4, "dweight")) || (e = check_opt_ptr(h.dbias, 4, "dbias")))) return e;
+    if (bwd && !h.norm.enabled && (h.dweight || h.dbias))
+      return fail(RESS_EINVAL, "dweight or dbias without a norm");
+    a->t[i] = h;
+  }
+  return RESS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int ress_layer_norm(const ress_norm* n, const void* x, const void* weight, const void* bias, void* y, float* mean,
+                    float* rstd, void* stream) {
+  int e;
+  if ((e = check_norm(n)) || (e = check_stride(n, n->x_stride, false, "x_stride")) ||
+      (e = check_stride(n, n->y_stride, true, "y_stride")))
+    return e;
+  if (n->rows > 0 && ((e = check_ptr(x, type_bytes(n->x_type), "x")) || (e = check_ptr(y, type_bytes(n->y_type), "y"))))
+    return e;
+  const size_t pb = type_bytes(n->param_type);
+  if ((e = check_opt_ptr(weight, pb, "weight")) || (e = check_opt_ptr(bias, pb, "bias")) ||
+      (e = check_opt_ptr(mean, 4, "mean")) || (e = check_opt_ptr(rstd, 4, "rstd")))
+    return e;
+  if (n->rows == 0) return ok();
+  ress::NormArgs a{};
+  a.n = *n;
+  a.x = x;
+  a.weight = weight;
+  a.bias = bias;
+  a.out = y;
+  a.mean = mean;
+  a.rstd = rstd;
+  cudaError_t ce = ress::launch_layer_norm(a, static_cast<cudaStream_t>(stream));
+  if (ce != cudaSuccess) return cuda_fail(ce, "ress_layer_norm");
+  return ok();
+}
+
+size_t ress_layer_norm_workspace_bytes(const ress_norm* n) {
+  if (check_norm(n)) return 0;
+  const int64_t parts = n->rows < 1 ? 1 : n->rows < ress::kNormParts ? n->rows : ress::kNormParts;
+  return (size_t)ress::align256(parts * 2 * n->width * 4);
+}
+
+int ress_layer_norm_bwd(const ress_norm* n, const void* dy, const void* x, const void* weight, const float* mean,
+                        const float* rstd, const void* dres, void* dx, float* dweight, float* dbias, void* ws,
+                        size_t ws_bytes, void* stream) {
+  int e;
+  if ((e = check_norm(n)) || (e = check_stride(n, n->x_stride, false, "x_stride")) ||
+      (e = check_stride(n, n->y_stride, false, "y_stride")) || (e = check_stride(n, n->dx_stride, true, "dx_stride")) ||
+      (dres && (e = check_stride(n, n->dres_stride, false, "dres_stride"))))
+    return e;
+  const size_t xb = type_bytes(n->x_type);
+  if (n->rows > 0 &&
+      ((e = check_ptr(dy, type_bytes(n->y_type), "dy")) || (e = check_ptr(x, xb, "x")) ||
+       (e = check_ptr(mean, 4, "mean")) || (e = check_ptr(rstd, 4, "rstd")) || (e = check_ptr(dx, xb, "dx"))))
+    return e;
+  if ((e = check_opt_ptr(dres, xb, "dres")) || (e = check_opt_ptr(weight, type_bytes(n->param_type), "weight")) ||
+      (e = check_opt_ptr(dweight, 4, "dweight")) || (e = check_opt_ptr(dbias, 4, "dbias")))
+    return e;
+  if ((dweight || dbias) && (e = check_scratch(ws, ws_bytes, ress_layer_norm_workspace_bytes(n)))) return e;
+  ress::NormArgs a{};
+  a.n = *n;
+  a.x = x;
+  a.weight = weight;
+  a.dy = dy;
+  a.dres = dres;
+  a.out = dx;
+  a.mean = const_cast<float*>(mean);
+  a.rstd = const_cast<float*>(rstd);
+  a.partial = dweight || dbias ? static_cast<float*>(ws) : nullptr;
+  a.dweight = dweight;
+  a.dbias = dbias;
+  cudaError_t ce = ress::launch_layer_norm_bwd(a, static_cast<cudaStream_t>(stream));
+  if (ce != cudaSuccess) return cuda_fail(ce, "ress_layer_norm_bwd");
+  return ok();
+}
+
+int ress_rope_plan_init(ress_rope_plan* plan, int32_t head_dim, int32_t n_axes, const int32_t* axis_dims,
+                        int32_t layout, double base, const double* freq) {
+  if (!plan) return fail(RESS_EINVAL, "plan is NULL");
+  if (!axis_dims) return fail(RESS_EINVAL, "axis_dims is NULL");
+  ress_rope_plan p{};
+  p.head_dim = head_dim;
+  p.n_axes = n_axes;
+  p.layout = layout;
+  for (int a = 0; a < n_axes && a < RESS_ROPE_MAX_AXES; ++a) {
+    p.axis_dims[a] = axis_dims[a];
+    p.n_pairs += axis_dims[a] / 2;
+  }
+  int e = check_plan(&p);
+  if (e) return e;
+  if (!freq && !(base > 0.0 && base <= DBL_MAX)) return fail(RESS_EINVAL, "base %g is not a positive number", base);
+  int k = 0;
+  for (int a = 0; a < n_axes; ++a)
+    for (int i = 0; i < p.axis_dims[a] / 2; ++i, ++k) {
+      const double f = freq ? freq[k] : pow(base, -2.0 * i / p.axis_dims[a]);
+      if (!(fabs(f) <= DBL_MAX)) return fail(RESS_EINVAL, "frequency %d is not finite", k);
+      // turns per position modulo 1, as a 64-bit fraction: the upper and lower 32 bits in turn
+      // (f / 2 pi is within 2^-53 of itself; what is taken off it below is exact)
+      double t = f / 6.283185307179586476925286766559;
+      t = (t - floor(t)) * 4294967296.0;
+      const double hi = floor(t), lo = floor((t - hi) * 4294967296.0);
+      p.turns[k] = ((uint64_t)hi << 32) + (uint64_t)lo;
+    }
+  *plan = p;
+  return ok();
+}
+
+int ress_rope(const ress_rope_plan* plan, int64_t n_tokens, const int32_t* pos, int32_t type, int32_t param_type,
+              float eps, const ress_rope_heads* q, const ress_rope_heads* k, void* stream) {
+  ress::RopeArgs a;
+  const ress_rope_heads* const t[2] = {q, k};
+  int e = rope_checks(plan, n_tokens, pos, type, param_type, eps, t, false, &a);
+  if (e) return e;
+  cudaError_t ce = ress::launch_rope(a, static_cast<cudaStream_t>(stream));
+  if (ce != cudaSuccess) return cuda_fail(ce, "ress_rope");
+  return ok();
+}
+
+size_t ress_rope_workspace_bytes(const ress_rope_plan* plan, int64_t n_tokens, int32_t q_heads, int32_t k_heads) {
+  if (check_plan(plan)) return 0;
+  if (n_tokens < 0 || q_heads < 0 || k_heads < 0 || q_heads > RESS_ROPE_MAX_HEADS || k_heads > RESS_ROPE_MAX_HEADS) {
+    fail(RESS_EINVAL, "n_tokens %lld, heads %d and %d", (long long)n_tokens, q_heads, k_heads);
+    return 0;
+  }
+  return (size_t)ress::align256((int64_t)ress::kRopeParts * 2 * plan->head_dim * 4);
+}
+
+int ress_rope_bwd(const ress_rope_plan* plan, int64_t n_tokens, const int32_t* pos, int32_t type, int32_t param_type,
+                  float eps, const ress_rope_heads* q, const ress_rope_heads* k, void* ws, size_t ws_bytes,
+                  void* stream) {
+  ress::RopeArgs a;
+  const ress_rope_heads* const t[2] = {q, k};
+  int e = rope_checks(plan, n_tokens, pos, type, param_type, eps, t, true, &a);
+  if (e) return e;
+  if (a.t[0].dweight || a.t[0].dbias || a.t[1].dweight || a.t[1].dbias) {
+    const size_t need = ress_rope_workspace_bytes(plan, n_tokens, a.t[0].n_heads, a.t[1].n_heads);
+    if ((e = check_scratch(ws, ws_bytes, need))) return e;
+    a.partial = static_cast<float*>(ws);
+  }
+  cudaError_t ce = ress::launch_rope_bwd(a, static_cast<cudaStream_t>(stream));
+  if (ce != cudaSuccess) return cuda_fail(ce, "ress_rope_bwd");
+  return ok();
+}
+
+int ress_qkv_proj(const ress_dims* d, const uint16_t* x, const uint16_t* W_q, const uint16_t* W_k,
+                  const uint16_t* W_v, const uint16_t* b_q, const uint16_t* b_k, const uint16_t* b_v,
+                  const ress_rope_plan* plan, const int32_t* pos, const ress_head_norm* q_norm,
+                  const ress_head_norm* k_norm, int32_t param_type, float eps, uint16_t* Q, uint16_t* K, uint16_t* V,
+                  void* ws, size_t ws_bytes, void* stream) {
+  ress::Shape s{};
+  ress_ws_layout L{};
+  int e = oproj_checks(d, W_q, "W_q", ws, ws_bytes, &s, &L);
+  if (e) return e;
+  if ((e = check_ptr(W_k, 16, "W_k")) || (e = check_ptr(W_v, 16, "W_v")) || (e = check_ptr(x, 16, "x")) ||
+      (e = check_ptr(Q, 16, "Q")) || (e = check_ptr(K, 16, "K")) || (e = check_ptr(V, 16, "V")) ||
+      (e = check_opt_ptr(b_q, 2, "b_q")) || (e = check_opt_ptr(b_k, 2, "b_k")) || (e = check_opt_ptr(b_v, 2, "b_v")))
+    return e;
+  if ((plan != nullptr) != (pos != nullptr)) return fail(RESS_EINVAL, "a plan and positions belong together");
+  ress::QkvArgs a{};
+  if (plan) {
+    if ((e = check_plan(plan)) || (e = check_ptr(pos, 4, "pos"))) return e;
+    if (plan->head_dim != RESS_HEAD_DIM)
+      return fail(RESS_EUNSUPPORTED, "the plan's head_dim %d is not %d", plan->head_dim, RESS_HEAD_DIM);
+    a.plan = *plan;
+  }
+  if ((e = check_type(param_type, "param_type")) || (e = check_eps(eps))) return e;
+  const ress_head_norm* const norms[2] = {q_norm, k_norm};
+  for (int i = 0; i < 2; ++i) {
+    if (!norms[i]) continue;
+    if ((e = check_head_norm(*norms[i], param_type, i ? "k_norm" : "q_norm"))) return e;
+    a.norm[i] = *norms[i];
+  }
+  a.N = s.N;
+  a.H = s.H;
+  a.Dm = d->d_model;
+  a.x = x;
+  const uint16_t *const W[3] = {W_q, W_k, W_v}, *const b[3] = {b_q, b_k, b_v};
+  uint16_t* const out[3] = {Q, K, V};
+  for (int i = 0; i < 3; ++i) {
+    a.W[i] = W[i];
+    a.b[i] = b[i];
+    a.out[i] = out[i];
+  }
+  a.rotate = plan != nullptr;
+  a.pos = pos;
+  a.param_type = param_type;
+  a.eps = eps;
+  a.status = reinterpret_cast<uint32_t*>(static_cast<char*>(ws) + L.status);
+  cudaError_t ce = ress::launch_qkv_proj(a, static_cast<cudaStream_t>(stream));
+  if (ce != cudaSuccess) return cuda_fail(ce, "ress_qkv_proj");
   return ok();
 }
 

@@ -280,4 +280,48 @@ struct OProjArgs {
 cudaError_t launch_out_proj(const OProjArgs& a, cudaStream_t st);
 cudaError_t launch_token_drift(const OProjArgs& a, cudaStream_t st);
 
+// Layer norm of rows and its gradients (k_norm.cu).  At most kNormParts CTAs leave partial sums of
+// the weight's and the bias's gradients.
+constexpr int kNormParts = 1024;
+struct NormArgs {
+  ress_norm n;
+  const void *x, *weight, *bias, *dy, *dres;
+  void* out;             // forward y, backward dx
+  float *mean, *rstd;    // forward: outputs or NULL; backward: inputs
+  float* partial;        // [kNormParts, 2, width] scratch of the backward, NULL without dweight and dbias
+  float *dweight, *dbias;
+};
+cudaError_t launch_layer_norm(const NormArgs& a, cudaStream_t st);
+cudaError_t launch_layer_norm_bwd(const NormArgs& a, cudaStream_t st);
+
+// Head norm and rotary positions on the heads of two tensors, and the gradients (k_rope.cu).
+constexpr int kRopeParts = 1024;
+struct RopeArgs {
+  ress_rope_plan plan;
+  int64_t n_tokens;
+  const int32_t* pos;
+  int type, param_type;
+  float eps;
+  ress_rope_heads t[2];  // n_heads 0: absent
+  float* partial;        // [kRopeParts, 2, head_dim] scratch of the backward
+};
+cudaError_t launch_rope(const RopeArgs& a, cudaStream_t st);
+cudaError_t launch_rope_bwd(const RopeArgs& a, cudaStream_t st);
+
+// The projection to Q, K and V with the head norm and the rotation in its epilogue (k_qkv.cu).
+struct QkvArgs {
+  int N, H, Dm;
+  const uint16_t* x;
+  const uint16_t *W[3], *b[3];
+  uint16_t* out[3];
+  bool rotate;
+  ress_rope_plan plan;
+  const int32_t* pos;
+  ress_head_norm norm[2];
+  int param_type;
+  float eps;
+  uint32_t* status;
+};
+cudaError_t launch_qkv_proj(const QkvArgs& a, cudaStream_t st);
+
 }  // namespace ress
