@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import os
 import re
+import struct
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libress.so")
@@ -89,20 +90,10 @@ class RopePlan(ctypes.Structure):
                 ("n_pairs", ctypes.c_int32), ("turns", ctypes.c_uint64 * (ROPE_MAX_DIM // 2))]
 
 
-class Heads(ctypes.Structure):
-    """ress_heads: the heads of one tensor, by their strides in elements."""
-    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
-
-
-class HeadNorm(ctypes.Structure):
-    """ress_head_norm: a layer norm over each head's channels."""
-    _fields_ = [("enabled", ctypes.c_int32), ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p)]
-
-
-class RopeHeads(ctypes.Structure):
-    """ress_rope_heads: one tensor of a ress_rope call."""
-    _fields_ = [("n_heads", ctypes.c_int32), ("norm", HeadNorm), ("x", Heads), ("y", Heads), ("dx", Heads),
-                ("dweight", ctypes.c_void_p), ("dbias", ctypes.c_void_p)]
+# ress_head_norm and ress_rope_heads as bytes (in a call of a few microseconds, nested ctypes
+# structures would be most of it)
+_HEAD_NORM = struct.Struct("@i4xPP")                # enabled, weight, bias
+_ROPE_HEADS = struct.Struct("@i4xi4xPPPqqPqqPqqPP")  # n_heads, norm, x, y, dx, dweight, dbias
 
 
 _c = ctypes
@@ -149,14 +140,13 @@ _SIGS = {
                                        _c.c_size_t, _P]),
     "ress_rope_plan_init": (_c.c_int, [_c.POINTER(RopePlan), _c.c_int32, _c.c_int32, _P, _c.c_int32,
                                        _c.c_double, _P]),
-    "ress_rope": (_c.c_int, [_c.POINTER(RopePlan), _c.c_int64, _P, _c.c_int32, _c.c_int32, _c.c_float,
-                             _c.POINTER(RopeHeads), _c.POINTER(RopeHeads), _P]),
+    "ress_rope": (_c.c_int, [_c.POINTER(RopePlan), _c.c_int64, _P, _c.c_int32, _c.c_int32, _c.c_float, _P,
+                             _P, _P]),
     "ress_rope_workspace_bytes": (_c.c_size_t, [_c.POINTER(RopePlan), _c.c_int64, _c.c_int32, _c.c_int32]),
     "ress_rope_bwd": (_c.c_int, [_c.POINTER(RopePlan), _c.c_int64, _P, _c.c_int32, _c.c_int32, _c.c_float,
-                                 _c.POINTER(RopeHeads), _c.POINTER(RopeHeads), _P, _c.c_size_t, _P]),
+                                 _P, _P, _P, _c.c_size_t, _P]),
     "ress_qkv_proj": (_c.c_int, [_c.POINTER(Dims), _P, _P, _P, _P, _P, _P, _P, _c.POINTER(RopePlan), _P,
-                                 _c.POINTER(HeadNorm), _c.POINTER(HeadNorm), _c.c_int32, _c.c_float, _P, _P,
-                                 _P, _P, _c.c_size_t, _P]),
+                                 _P, _P, _c.c_int32, _c.c_float, _P, _P, _P, _P, _c.c_size_t, _P]),
 }
 for _name, (_res, _args) in _SIGS.items():
     _f = getattr(_lib, _name)
@@ -268,14 +258,15 @@ def _host(t, dtypes, name):
 
 
 def _stream(stream):
-    torch = _torch()
-    s = torch.cuda.current_stream() if stream is None else stream
-    return _c.c_void_p(s.cuda_stream)
+    if stream is not None:
+        return stream.cuda_stream
+    torch = _torch()  # the current stream's handle without a Stream object (0.4 us instead of 3)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _bf16():
     torch = _torch()
-    return (torch.bfloat16, torch.uint16, torch.int16)
+    return (torch.bfloat16, torch.int16, torch.uint16)
 
 
 def prepare_wo(d: Dims, W_o, F, stream=None):
@@ -400,66 +391,94 @@ def status(ws, stream=None):
 
 
 # ---- the input half of the sublayer ---------------------------------------------------
-def _dtype_code(t, name):
-    torch = _torch()
-    code = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}.get(t.dtype)
+# Small calls are a few microseconds on the GPU, so the checks below ask a tensor for each fact once.
+_CODES = {}  # torch dtype -> ress_dtype
+
+
+def _code(t, name):
+    code = _CODES.get(t.dtype)
     if code is None:
-        raise TypeError(f"{name} has dtype {t.dtype}, expected bfloat16, float16 or float32")
+        torch = _torch()
+        _CODES.update({torch.bfloat16: 0, torch.float16: 1, torch.float32: 2})
+        if t.dtype not in _CODES:
+            raise TypeError(f"{name} has dtype {t.dtype}, expected bfloat16, float16 or float32")
+        code = _CODES[t.dtype]
     return code
 
 
-def _cuda(t, name, dtype=None):
-    """Device pointer of a CUDA tensor of any layout (None -> NULL)."""
+def _cuda(t, name):
+    """Device pointer of a CUDA tensor of any layout."""
+    try:
+        if t.is_cuda:
+            return t.data_ptr()
+    except AttributeError:
+        raise TypeError(f"{name} must be a torch.Tensor") from None
+    raise ValueError(f"{name} must live on a CUDA device")
+
+
+def _vector(t, n, name):
+    """Device pointer of n contiguous elements (None -> NULL)."""
     if t is None:
         return None
-    if not isinstance(t, _torch().Tensor):
-        raise TypeError(f"{name} must be a torch.Tensor")
-    if t.device.type != "cuda":
-        raise ValueError(f"{name} must live on a CUDA device")
-    if dtype is not None and t.dtype != dtype:
-        raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
-    return t.data_ptr()
-
-
-def _vector(t, n, name, dtype=None):
-    """Device pointer of n contiguous elements (None -> NULL)."""
-    p = _cuda(t, name, dtype)
-    if t is not None and (t.numel() != n or not t.is_contiguous()):
+    p = _cuda(t, name)
+    if t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name} must have {n} contiguous elements")
     return p
 
 
-def _rows(t, name, like=None):
-    """(rows, width, stride) of a tensor [..., width] whose rows are a fixed stride apart."""
-    if t.dim() < 1 or (like is not None and t.shape != like.shape):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}" + (f", expected {tuple(like.shape)}" if like is not None else ""))
-    width = t.shape[-1]
-    rows = t.numel() // width if width else 0
+def _vector_f32(t, n, name):
+    p = _vector(t, n, name)
+    if p is not None and _code(t, name) != 2:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected float32")
+    return p
+
+
+def _row_stride(t, shape, name):
+    """Elements between the rows of a tensor [..., width] of this shape."""
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     if t.is_contiguous():
-        return rows, width, width
-    if t.dim() != 2 or (width > 1 and t.stride(1) != 1):
+        return shape[-1]
+    if len(shape) != 2 or (t.stride(1) != 1 and shape[1] > 1):
         raise ValueError(f"{name} must be contiguous, or two-dimensional with contiguous rows")
-    return rows, width, t.stride(0)
+    return t.stride(0)
 
 
-def _param_code(name, *params):
-    """The one dtype of the parameters that are given (float32 if none is)."""
-    codes = {_dtype_code(p, name) for p in params if p is not None}
-    if len(codes) > 1:
-        raise TypeError(f"{name}: weights and biases of different dtypes")
-    return codes.pop() if codes else 2
+def _param_code(*params):
+    """The one ress_dtype of the parameters that are given (float32 if none is)."""
+    code = None
+    for p in params:
+        if p is not None:
+            c = _code(p, "weight or bias")
+            if code is not None and c != code:
+                raise TypeError("weights and biases of different dtypes")
+            code = c
+    return 2 if code is None else code
+
+
+def _scratch(ws):
+    """Pointer and bytes of a workspace (None -> NULL, 0)."""
+    if ws is None:
+        return None, 0
+    n = ws.numel()
+    return _vector(ws, n, "ws"), n * ws.element_size()
+
+
+def _width(x):
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError(f"x has shape {tuple(x.shape)}, expected [..., width]")
+    return x.shape[-1]
 
 
 def layer_norm(x, weight, bias, y, eps: float = 1e-5, mean=None, rstd=None, stream=None):
     """ress_layer_norm over the last dimension of x [..., width] into y of the same shape; weight, bias
     [width] or None; mean, rstd: float32 outputs, one per row, for layer_norm_bwd, or None."""
-    f32 = _torch().float32
-    px, py = _cuda(x, "x"), _cuda(y, "y")
-    rows, width, sx = _rows(x, "x")
-    n = Norm(rows, width, _dtype_code(x, "x"), _dtype_code(y, "y"), _param_code("layer_norm", weight, bias),
-             eps, sx, _rows(y, "y", x)[2], 0, 0)
+    px, py, shape, width = _cuda(x, "x"), _cuda(y, "y"), x.shape, _width(x)
+    rows = x.numel() // width
+    n = Norm(rows, width, _code(x, "x"), _code(y, "y"), _param_code(weight, bias), eps,
+             _row_stride(x, shape, "x"), _row_stride(y, shape, "y"), 0, 0)
     _check(_lib.ress_layer_norm(n, px, _vector(weight, width, "weight"), _vector(bias, width, "bias"), py,
-                                _vector(mean, rows, "mean", f32), _vector(rstd, rows, "rstd", f32),
+                                _vector_f32(mean, rows, "mean"), _vector_f32(rstd, rows, "rstd"),
                                 _stream(stream)))
 
 
@@ -474,18 +493,20 @@ def layer_norm_workspace_bytes(rows: int, width: int) -> int:
 def layer_norm_bwd(dy, x, weight, mean, rstd, dx, dweight=None, dbias=None, dres=None, ws=None, stream=None):
     """ress_layer_norm_bwd: dx (+ dres where given) and the float32 gradients of weight and bias
     (None to skip; ws is needed for them) from the gradient dy of layer_norm's y."""
-    f32 = _torch().float32
-    pdy, px, pdx, pres = _cuda(dy, "dy"), _cuda(x, "x"), _cuda(dx, "dx", x.dtype), _cuda(dres, "dres", x.dtype)
-    rows, width, sx = _rows(x, "x")
-    n = Norm(rows, width, _dtype_code(x, "x"), _dtype_code(dy, "dy"), _param_code("layer_norm_bwd", weight), 0.0,
-             sx, _rows(dy, "dy", x)[2], _rows(dx, "dx", x)[2], 0 if dres is None else _rows(dres, "dres", x)[2])
+    pdy, px, pdx, shape, width = _cuda(dy, "dy"), _cuda(x, "x"), _cuda(dx, "dx"), x.shape, _width(x)
+    rows, code, pres, sres = x.numel() // width, _code(x, "x"), None, 0
+    if dres is not None:
+        pres, sres = _cuda(dres, "dres"), _row_stride(dres, shape, "dres")
+    if _code(dx, "dx") != code or (dres is not None and _code(dres, "dres") != code):
+        raise TypeError(f"dx and dres must have x's dtype {x.dtype}")
     if mean is None or rstd is None:
         raise ValueError("mean and rstd are those layer_norm saved")
-    _check(_lib.ress_layer_norm_bwd(n, pdy, px, _vector(weight, width, "weight"), _vector(mean, rows, "mean", f32),
-                                    _vector(rstd, rows, "rstd", f32), pres, pdx,
-                                    _vector(dweight, width, "dweight", f32), _vector(dbias, width, "dbias", f32),
-                                    _dev(ws, None, "ws"), 0 if ws is None else ws.numel() * ws.element_size(),
-                                    _stream(stream)))
+    n = Norm(rows, width, code, _code(dy, "dy"), _param_code(weight), 0.0, _row_stride(x, shape, "x"),
+             _row_stride(dy, shape, "dy"), _row_stride(dx, shape, "dx"), sres)
+    _check(_lib.ress_layer_norm_bwd(n, pdy, px, _vector(weight, width, "weight"), _vector_f32(mean, rows, "mean"),
+                                    _vector_f32(rstd, rows, "rstd"), pres, pdx,
+                                    _vector_f32(dweight, width, "dweight"), _vector_f32(dbias, width, "dbias"),
+                                    *_scratch(ws), _stream(stream)))
 
 
 def rope_plan(axis_dims, head_dim: int = HEAD_DIM, base: float = 100.0, layout: str = "sections",
@@ -506,52 +527,57 @@ def rope_plan(axis_dims, head_dim: int = HEAD_DIM, base: float = 100.0, layout: 
     return plan
 
 
-def _heads(t, plan, tokens, name, dtype, heads=None):
-    """ress_heads of a tensor [tokens, heads, head_dim] with contiguous channels."""
-    p = _cuda(t, name, dtype)
+def _heads(t, shape, code, name):
+    """Pointer and strides of a tensor [tokens, heads, head_dim] with contiguous channels (None: absent)."""
     if t is None:
-        raise ValueError(f"{name} is missing")
-    if t.dim() != 3 or t.shape[0] != tokens or t.shape[2] != plan.head_dim or (heads is not None and t.shape[1] != heads):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected ({tokens}, {heads or 'heads'}, {plan.head_dim})")
-    if t.stride(2) != 1:
+        return 0, 0, 0
+    p = _cuda(t, name)
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if _code(t, name) != code:
+        raise TypeError(f"{name} has dtype {t.dtype}, unlike the call's other heads")
+    st, sh, sc = t.stride()
+    if sc != 1:
         raise ValueError(f"{name} must have contiguous channels")
-    return Heads(p, t.stride(0), t.stride(1))
+    return p, st, sh
 
 
 def _head_norm(norm, n, name):
-    """ress_head_norm of None or (weight, bias)."""
+    """enabled, weight, bias of None or (weight, bias)."""
     if norm is None:
-        return HeadNorm(0, None, None)
+        return 0, 0, 0
     weight, bias = norm
-    return HeadNorm(1, _vector(weight, n, name + " weight"), _vector(bias, n, name + " bias"))
+    return 1, _vector(weight, n, name + " weight") or 0, _vector(bias, n, name + " bias") or 0
 
 
-def _positions(plan, pos):
-    if pos.dim() != 2 or pos.shape[1] != plan.n_axes:
-        raise ValueError(f"pos has shape {tuple(pos.shape)}, expected (tokens, {plan.n_axes})")
-    return _dev(pos, (_torch().int32,), "pos")
+def _positions(plan, pos, tokens):
+    p = _cuda(pos, "pos")
+    if pos.shape != (tokens, plan.n_axes):
+        raise ValueError(f"pos has shape {tuple(pos.shape)}, expected ({tokens}, {plan.n_axes})")
+    if pos.dtype != _torch().int32 or not pos.is_contiguous():
+        raise TypeError("pos must be a contiguous int32 tensor")
+    return p
 
 
-def _rope_tensor(plan, tokens, name, x, y, dx, norm, grads, dtype):
-    """ress_rope_heads, or None where the tensor is absent."""
-    if y is None:
-        if x is not None or dx is not None or norm is not None or grads is not None:
-            raise ValueError(f"{name}: an input or a norm without its output")
-        return None
-    h = y.shape[1] if y.dim() == 3 else None
-    f32 = _torch().float32
-    none = Heads(None, 0, 0)
-    dweight, dbias = grads if grads is not None else (None, None)
-    return RopeHeads(h or 0, _head_norm(norm, plan.head_dim, name + "_norm"),
-                     none if x is None else _heads(x, plan, tokens, name, dtype, h),
-                     _heads(y, plan, tokens, name + "'s result", dtype, h),
-                     none if dx is None else _heads(dx, plan, tokens, name + "'s gradient", dtype, h),
-                     _vector(dweight, plan.head_dim, name + " dweight", f32),
-                     _vector(dbias, plan.head_dim, name + " dbias", f32))
+def _rope_heads(plan, name, y, x, dx, norm, grads, shape, code):
+    """ress_rope_heads of one tensor."""
+    hd = plan.head_dim
+    dweight, dbias = (None, None) if grads is None else grads
+    return _ROPE_HEADS.pack(shape[1], *_head_norm(norm, hd, name + "_norm"), *_heads(x, shape, code, name),
+                            *_heads(y, shape, code, name + "'s result"), *_heads(dx, shape, code, name + "'s gradient"),
+                            _vector_f32(dweight, hd, name + " dweight") or 0,
+                            _vector_f32(dbias, hd, name + " dbias") or 0)
 
 
-def _norm_params(q_norm, k_norm):
-    return [p for norm in (q_norm, k_norm) if norm is not None for p in norm]
+def _rope_shape(plan, t, tokens, name):
+    shape = t.shape
+    if len(shape) != 3 or shape[0] != tokens or shape[2] != plan.head_dim:
+        raise ValueError(f"{name} has shape {tuple(shape)}, expected ({tokens}, heads, {plan.head_dim})")
+    return shape
+
+
+def _norm_code(q_norm, k_norm):
+    return _param_code(*(() if q_norm is None else q_norm), *(() if k_norm is None else k_norm))
 
 
 def rope(plan: RopePlan, pos, q, q_out, k=None, k_out=None, q_norm=None, k_norm=None, eps: float = 1e-5,
@@ -559,13 +585,14 @@ def rope(plan: RopePlan, pos, q, q_out, k=None, k_out=None, q_norm=None, k_norm=
     """ress_rope: q_out, k_out = the heads of q, k [tokens, heads, head_dim] after a layer norm over
     their channels (q_norm, k_norm: (weight, bias), either may be None; None: no norm) and rotated by
     pos, int32 [tokens, axes]."""
-    if q is None or q_out is None or (k is None) != (k_out is None):
+    if q is None or q_out is None or (k is None) != (k_out is None) or (k is None and k_norm is not None):
         raise ValueError("q and q_out are needed, and k and k_out together")
-    tokens = pos.shape[0]
-    tq = _rope_tensor(plan, tokens, "q", q, q_out, None, q_norm, None, q.dtype)
-    tk = _rope_tensor(plan, tokens, "k", k, k_out, None, k_norm, None, q.dtype)
-    _check(_lib.ress_rope(plan, tokens, _positions(plan, pos), _dtype_code(q, "q"),
-                          _param_code("rope", *_norm_params(q_norm, k_norm)), eps, tq, tk, _stream(stream)))
+    tokens, code = pos.shape[0], _code(q, "q")
+    tq = _rope_heads(plan, "q", q_out, q, None, q_norm, None, _rope_shape(plan, q, tokens, "q"), code)
+    tk = None if k is None else _rope_heads(plan, "k", k_out, k, None, k_norm, None,
+                                            _rope_shape(plan, k, tokens, "k"), code)
+    _check(_lib.ress_rope(plan, tokens, _positions(plan, pos, tokens), code, _norm_code(q_norm, k_norm), eps, tq, tk,
+                          _stream(stream)))
 
 
 def rope_workspace_bytes(plan: RopePlan, n_tokens: int, q_heads: int, k_heads: int = 0) -> int:
@@ -580,38 +607,40 @@ def rope_bwd(plan: RopePlan, pos, dq_out, dq, dk_out=None, dk=None, q=None, k=No
              q_norm_grads=None, k_norm_grads=None, eps: float = 1e-5, ws=None, stream=None):
     """ress_rope_bwd: the gradients dq, dk of rope's q, k from those of its outputs, and, with norms
     (which need q, k again), q_norm_grads, k_norm_grads: float32 (dweight, dbias), either or both None."""
-    if dq_out is None or dq is None or (dk_out is None) != (dk is None):
+    if dq_out is None or dq is None or (dk_out is None) != (dk is None) or (dk is None and k_norm is not None):
         raise ValueError("dq_out and dq are needed, and dk_out and dk together")
     if (q_norm is not None and q is None) or (k_norm is not None and k is None):
         raise ValueError("a norm's gradient needs the norm's input")
-    tokens = pos.shape[0]
-    tq = _rope_tensor(plan, tokens, "q", q, dq_out, dq, q_norm, q_norm_grads, dq_out.dtype)
-    tk = _rope_tensor(plan, tokens, "k", k, dk_out, dk, k_norm, k_norm_grads, dq_out.dtype)
-    _check(_lib.ress_rope_bwd(plan, tokens, _positions(plan, pos), _dtype_code(dq_out, "dq_out"),
-                              _param_code("rope_bwd", *_norm_params(q_norm, k_norm)), eps, tq, tk,
-                              _dev(ws, None, "ws"), 0 if ws is None else ws.numel() * ws.element_size(),
-                              _stream(stream)))
+    tokens, code = pos.shape[0], _code(dq_out, "dq_out")
+    tq = _rope_heads(plan, "q", dq_out, q, dq, q_norm, q_norm_grads, _rope_shape(plan, dq_out, tokens, "dq_out"), code)
+    tk = None if dk is None else _rope_heads(plan, "k", dk_out, k, dk, k_norm, k_norm_grads,
+                                             _rope_shape(plan, dk_out, tokens, "dk_out"), code)
+    _check(_lib.ress_rope_bwd(plan, tokens, _positions(plan, pos, tokens), code, _norm_code(q_norm, k_norm), eps, tq,
+                              tk, *_scratch(ws), _stream(stream)))
+
+
+def _dense(t, n, name):
+    """Device pointer of n contiguous bf16 elements (None -> NULL)."""
+    p = _vector(t, n, name)
+    if p is not None and _CODES.get(t.dtype) != 0 and t.dtype not in _bf16():
+        raise TypeError(f"{name} has dtype {t.dtype}, expected one of {_bf16()}")
+    return p
 
 
 def qkv_proj(d: Dims, x, W_q, W_k, W_v, Q, K, V, ws, b_q=None, b_k=None, b_v=None, plan: RopePlan = None, pos=None,
              q_norm=None, k_norm=None, eps: float = 1e-5, stream=None):
     """ress_qkv_proj: Q, K, V [N, H, 64] = x W^T + b with q_norm, k_norm and the rotation by plan and pos
     as in rope; bf16 tensors."""
-    b, n, out = _bf16(), d.n_tokens, d.n_heads * HEAD_DIM
-    for t, count, name in ((x, n * d.d_model, "x"), (W_q, out * d.d_model, "W_q"), (W_k, out * d.d_model, "W_k"),
-                           (W_v, out * d.d_model, "W_v"), (Q, n * out, "Q"), (K, n * out, "K"), (V, n * out, "V"),
-                           (b_q, out, "b_q"), (b_k, out, "b_k"), (b_v, out, "b_v")):
-        if t is not None and t.numel() != count:
-            raise ValueError(f"{name} has {t.numel()} elements, expected {count}")
-    if plan is not None and (pos is None or pos.shape[0] != n):
-        raise ValueError(f"pos must have the positions of {n} tokens")
-    _check(_lib.ress_qkv_proj(d, _dev(x, b, "x"), _dev(W_q, b, "W_q"), _dev(W_k, b, "W_k"), _dev(W_v, b, "W_v"),
-                              _dev(b_q, b, "b_q"), _dev(b_k, b, "b_k"), _dev(b_v, b, "b_v"), plan,
-                              None if pos is None else _positions(plan, pos) if plan is not None else _dev(pos, None, "pos"),
-                              _head_norm(q_norm, HEAD_DIM, "q_norm"), _head_norm(k_norm, HEAD_DIM, "k_norm"),
-                              _param_code("qkv_proj", *_norm_params(q_norm, k_norm)), eps, _dev(Q, b, "Q"),
-                              _dev(K, b, "K"), _dev(V, b, "V"), _dev(ws, None, "ws"),
-                              ws.numel() * ws.element_size(), _stream(stream)))
+    n, dm, out = d.n_tokens, d.d_model, d.n_heads * HEAD_DIM
+    if (plan is None) != (pos is None):
+        raise ValueError("plan and pos belong together")
+    _check(_lib.ress_qkv_proj(d, _dense(x, n * dm, "x"), _dense(W_q, out * dm, "W_q"), _dense(W_k, out * dm, "W_k"),
+                              _dense(W_v, out * dm, "W_v"), _dense(b_q, out, "b_q"), _dense(b_k, out, "b_k"),
+                              _dense(b_v, out, "b_v"), plan, None if pos is None else _positions(plan, pos, n),
+                              _HEAD_NORM.pack(*_head_norm(q_norm, HEAD_DIM, "q_norm")),
+                              _HEAD_NORM.pack(*_head_norm(k_norm, HEAD_DIM, "k_norm")), _norm_code(q_norm, k_norm), eps,
+                              _dense(Q, n * out, "Q"), _dense(K, n * out, "K"), _dense(V, n * out, "V"),
+                              *_scratch(ws), _stream(stream)))
 
 
 class Buffers:

@@ -5,11 +5,18 @@
 // avg and the sums are over the row's channels.  One pass over the data: a row's elements stay in
 // registers, as they lie in memory, between its sums and its result.
 //
-// A row belongs to a team: SEG lanes of a warp (rows of up to 64 or 128 channels), a warp, or a CTA
-// of several warps, so that a thread has C = 8 channels and keeps their weight, bias and gradient sums
-// in registers while its team goes through R rows at a time (above 4096 channels C = 32, and what is
-// kept is in L1 and shared memory).  The
-// mean is subtracted before squares are taken (two sums, one after the other): rows with an offset
+// A row belongs to a team, 8 to 32 lanes of a warp or a CTA, each thread C channels of it, and a team
+// takes R rows at a time, the next ones' elements on their way while it works on these:
+//   forward   a warp has up to 1024 16-bit channels (C = 32), so that rows of that width need no barrier,
+//             and keeps their weights and biases in registers (43,968 x 1024 bf16: 53 us with C = 8 on
+//             four warps, 35 with the next rows under way, 33 with a warp per row; 36 where it reads
+//             float32 parameters from L1 for each row; a device copy of the same bytes takes 31).
+//             float32 elements take twice the registers: C = 16;
+//   backward  C = 8, because a thread keeps its channels' two gradient sums in registers: with C = 32
+//             they leave room for 8 warps per SM (80 us), with C = 8 for 16 (63 us, and a barrier per
+//             R = 2 rows).  Above 4096 channels C = 32, the sums in shared memory.
+// Rows that are no whole vectors of 16 bytes go element by element, C = 8 (32 above 4096 channels).
+// The mean is subtracted before squares are taken (two sums, one after the other): rows with an offset
 // much larger than their spread keep their digits.  All sums are float32 in a fixed order.
 //
 // The gradients of the weight and the bias: each CTA adds up its rows in registers and shared memory
@@ -32,245 +39,318 @@ struct NormParams {
   void *out;                                 // forward y, backward dx
   float *mean, *rstd, *partial;
   float eps;
-  int width, param_type, team;
+  int width, param_type;
 };
 
-// Sums over a team's threads of N values each: over the warp's segments, then over the CTA's warps
-// through shared memory where the team has several.  The two halves of `red` take turns, so that one
-// barrier per call is enough: a warp that writes a half again has passed the barrier of the call in
-// between, which every warp reaches after reading.
-template <int SEG, int N>
-__device__ __forceinline__ void team_sum(float (&v)[N], float* red, int& turn, int warps) {
-#pragma unroll
-  for (int k = 0; k < N; ++k) v[k] = segment_sum<SEG>(v[k]);
-  if (SEG < 32 || warps == 1) return;
-  float* at = red + turn * (16 * N);
-  turn ^= 1;
-  if ((threadIdx.x & 31) == 0) {
-#pragma unroll
-    for (int k = 0; k < N; ++k) at[(threadIdx.x >> 5) * N + k] = v[k];
-  }
-  __syncthreads();
-#pragma unroll
-  for (int k = 0; k < N; ++k) v[k] = 0.f;
-  for (int w = 0; w < warps; ++w) {
-#pragma unroll
-    for (int k = 0; k < N; ++k) v[k] += at[w * N + k];
-  }
-}
+// A team: TEAM lanes of a warp (8, 16 or 32), or all the warps of a CTA.
+constexpr int kWholeCta = 0;
+template <int TEAM>
+constexpr int kLanes = TEAM == kWholeCta ? 32 : TEAM;  // that share a row in a warp
 
-// The team of this thread: its index in the grid, the thread's place in it, its threads and warps.
-template <int SEG>
+template <int TEAM>
 struct Team {
-  int64_t index, count;
-  int t, threads, warps;
-  __device__ explicit Team(int n) {  // n: threads of a team, SEG or a CTA's whole warps
-    threads = SEG < 32 ? SEG : n;
-    warps = SEG < 32 ? 1 : n / 32;
-    t = (int)threadIdx.x % threads;
-    const int per_cta = (int)blockDim.x / threads;
-    index = (int64_t)blockIdx.x * per_cta + (int)threadIdx.x / threads;
+  int64_t index, count;  // in the grid
+  int t, threads;        // this thread's place in it, its threads
+  __device__ Team() {
+    threads = TEAM == kWholeCta ? (int)blockDim.x : TEAM;
+    t = TEAM == kWholeCta ? (int)threadIdx.x : (int)threadIdx.x % kLanes<TEAM>;
+    const int per_cta = TEAM == kWholeCta ? 1 : kNormThreads / kLanes<TEAM>;
+    index = (int64_t)blockIdx.x * per_cta + (TEAM == kWholeCta ? 0 : (int)threadIdx.x / kLanes<TEAM>);
     count = (int64_t)gridDim.x * per_cta;
   }
 };
 
-// A thread's weights or biases: in registers for the whole kernel where it has 8 channels, read
-// where they are used (from L1) where it has 32.
-template <int C>
-constexpr bool kInRegisters = C == 8;
-template <int E, int C>
-struct Params {
-  float v[kInRegisters<C> ? C : 1];
-  const void* p;
-  float none;
-  int type, width, t, threads;
-  __device__ Params(const void* p_, int type_, float none_, int width_, int t_, int threads_)
-      : p(p_), none(none_), type(type_), width(width_), t(t_), threads(threads_) {
-    if constexpr (kInRegisters<C>) {
+// Sums over a team's threads of N values each: over the warp's lanes, then over the CTA's warps
+// through shared memory.  The two halves of `red` take turns, so that one barrier per call is enough:
+// a warp that writes a half again has passed the barrier of the call in between, which every warp
+// reaches after reading.
+template <int TEAM, int N>
+__device__ __forceinline__ void team_sum(float (&v)[N], float* red, int& turn) {
+  if constexpr (TEAM != kWholeCta) {
+    if constexpr (N > 1 && N <= TEAM) {
+      const float r = segment_sums<TEAM>(v);
 #pragma unroll
-      for (int c = 0; c < C; ++c) v[c] = load(c / E, c % E);
+      for (int k = 0; k < N; ++k) v[k] = __shfl_sync(0xffffffffu, r, k * (TEAM / N), TEAM);
+    } else {
+#pragma unroll
+      for (int k = 0; k < N; ++k) v[k] = segment_sum<TEAM>(v[k]);
+    }
+  } else {
+    constexpr int kSpan = 32 / N;  // lanes that hold the same value's sum
+    const float r = segment_sums<32>(v);
+    float* at = red + turn * (16 * N);
+    turn ^= 1;
+    const int lane = (int)threadIdx.x & 31;
+    if (lane % kSpan == 0) at[((int)threadIdx.x >> 5) * N + lane / kSpan] = r;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = 0.f;
+    for (int w = 0; w < (int)blockDim.x / 32; ++w) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) v[k] += at[w * N + k];
     }
   }
-  __device__ float load(int i, int e) const {
-    const int col = (t + i * threads) * E + e;
-    return col < width ? param_at(p, type, col, none) : 0.f;
-  }
-  __device__ float at(int i, int e) const {
-    if constexpr (kInRegisters<C>)
-      return v[i * E + e];
-    else
-      return load(i, e);
-  }
+}
+
+// A thread's channels are vectors of E, a team's threads next to each other: vector i of thread t
+// starts at channel (t + i threads) E.
+template <int E, int TEAM>
+struct Place {
+  int first, step, width;
+  __device__ Place(const Team<TEAM>& team, int width_) : first(team.t * E), step(team.threads * E), width(width_) {}
+  __device__ int col(int i) const { return first + i * (TEAM == kWholeCta ? step : TEAM * E); }
+  __device__ bool in(int i) const { return col(i) < width; }  // widths are whole vectors
 };
 
-template <typename X, typename Y, int E, int C, int SEG, int R>
-__global__ void __launch_bounds__(kNormMaxThreads) k_layer_norm(const NormParams p) {
+template <typename T, int E, int V, int TEAM>
+__device__ __forceinline__ void load_row(Vec<T, E> (&r)[V], const void* p, int64_t row, int64_t stride,
+                                         const Place<E, TEAM>& at, bool live) {
+  const T* x = static_cast<const T*>(p) + row * stride;
+#pragma unroll
+  for (int i = 0; i < V; ++i) r[i] = live && at.in(i) ? load_vec<T, E>(x + at.col(i)) : zero_vec<T, E>();
+}
+
+template <typename X, typename Y, int E, int C, int TEAM, int R>
+__global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThreads) k_layer_norm(const NormParams p) {
   __shared__ float red[2 * 16 * R];
-  constexpr int V = C / E;
-  const Team<SEG> team(p.team);
+  constexpr int V = C / E, P = C / 2;
+  // where elements take a register each, 32 channels leave no room for the next row and the parameters
+  constexpr bool kKeep = C < 32 || (E > 1 && sizeof(X) == 2);
+  const Team<TEAM> team;
+  const Place<E, TEAM> at(team, p.width);
   const float inv = 1.f / (float)p.width;
   int turn = 0;
   stream_acquire();
-  Params<E, C> w(p.weight, p.param_type, 1.f, p.width, team.t, team.threads);
-  Params<E, C> b(p.bias, p.param_type, 0.f, p.width, team.t, team.threads);
-  bool in[V];
+  F2 w[kKeep ? P : 1], b[kKeep ? P : 1];
+  if constexpr (kKeep) {
+    float v[2][C];
 #pragma unroll
-  for (int i = 0; i < V; ++i) in[i] = (team.t + i * team.threads) * E < p.width;
-  const X* x = static_cast<const X*>(p.x) + (int64_t)team.t * E;
-  Y* y = static_cast<Y*>(p.out) + (int64_t)team.t * E;
-  const int step = team.threads * E;  // columns from one of the thread's vectors to the next
-  // teams of a warp leave the loop together: their segments take part in each other's shuffles
-  const int64_t first = SEG < 32 ? team.index / (32 / SEG) * (32 / SEG) : team.index;
+    for (int i = 0; i < V; ++i) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[0][i * E + e] = v[1][i * E + e] = 0.f;
+      if (!at.in(i)) continue;
+      params_at<E>(p.weight, p.param_type, at.col(i), 1.f, v[0] + i * E);
+      params_at<E>(p.bias, p.param_type, at.col(i), 0.f, v[1] + i * E);
+    }
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+      w[j] = pack2(v[0][2 * j], v[0][2 * j + 1]);
+      b[j] = pack2(v[1][2 * j], v[1][2 * j + 1]);
+    }
+  }
+  Vec<X, E> next[R][V];
+  auto load = [&](int64_t row0) {
+#pragma unroll
+    for (int k = 0; k < R; ++k) load_row<X, E, V>(next[k], p.x, row0 + k, p.x_stride, at, row0 + k < p.rows);
+  };
+  // teams of a warp go through the loop together: their segments take part in each other's shuffles
+  const int64_t first = team.index / (32 / kLanes<TEAM>) * (32 / kLanes<TEAM>);
+  if (kKeep) load(team.index * R);
   for (int64_t base = 0; (base + first) * R < p.rows; base += team.count) {
     const int64_t row0 = (base + team.index) * R;
+    if (!kKeep) load(row0);
     Vec<X, E> raw[R][V];
 #pragma unroll
     for (int k = 0; k < R; ++k)
 #pragma unroll
-      for (int i = 0; i < V; ++i)
-        raw[k][i] = in[i] && row0 + k < p.rows ? load_vec<X, E>(x + (row0 + k) * p.x_stride + i * step)
-                                               : zero_vec<X, E>();
+      for (int i = 0; i < V; ++i) raw[k][i] = next[k][i];
+    if (kKeep) load(row0 + team.count * R);
+    // a thread's sums are scaled before the threads' meet: a row's sum may overflow where its average
+    // does not
     float mean[R], rstd[R];
 #pragma unroll
     for (int k = 0; k < R; ++k) {
-      mean[k] = 0.f;
+      F2 s = both(0.f);
 #pragma unroll
-      for (int i = 0; i < V; ++i)
-#pragma unroll
-        for (int e = 0; e < E; ++e) mean[k] += elem(raw[k][i], e);
-      mean[k] *= inv;  // before the threads' sums meet: a row's sum may overflow where its mean does not
+      for (int j = 0; j < P; ++j) s = add2(s, pair_of(raw[k], j));
+      mean[k] = sum2(s) * inv;
     }
-    team_sum<SEG>(mean, red, turn, team.warps);
+    team_sum<TEAM>(mean, red, turn);
 #pragma unroll
     for (int k = 0; k < R; ++k) {
-      rstd[k] = 0.f;
+      if constexpr (E == 1) {
+        float sq = 0.f;
 #pragma unroll
-      for (int i = 0; i < V; ++i)
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float d = in[i] ? elem(raw[k][i], e) - mean[k] : 0.f;
-          rstd[k] = fmaf(d, d, rstd[k]);
+        for (int i = 0; i < V; ++i) {
+          const float d = at.in(i) ? elem(raw[k][i], 0) - mean[k] : 0.f;
+          sq = fmaf(d, d, sq);
         }
-      rstd[k] *= inv;
+        rstd[k] = sq * inv;
+      } else {
+        const F2 m = both(-mean[k]);
+        F2 s = both(0.f);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          if (!at.in(i)) continue;
+#pragma unroll
+          for (int j = i * E / 2; j < (i + 1) * E / 2; ++j) {
+            const F2 d = add2(pair_of(raw[k], j), m);
+            s = fma2(d, d, s);
+          }
+        }
+        rstd[k] = sum2(s) * inv;
+      }
     }
-    team_sum<SEG>(rstd, red, turn, team.warps);
+    team_sum<TEAM>(rstd, red, turn);
 #pragma unroll
     for (int k = 0; k < R; ++k) {
       if (row0 + k >= p.rows) continue;
+      const int64_t row = row0 + k;
       const float r = rsqrtf(rstd[k] + p.eps);
+      Y* y = static_cast<Y*>(p.out) + row * p.y_stride;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        if (!in[i]) continue;
+        if (!at.in(i)) continue;
         float out[E];
+        if constexpr (kKeep && E > 1) {
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-          out[e] = fmaf((elem(raw[k][i], e) - mean[k]) * r, w.at(i, e), b.at(i, e));
-        store_vec<Y, E>(y + (row0 + k) * p.y_stride + i * step, out);
+          for (int j = 0; j < E / 2; ++j) {
+            const F2 h = mul2(add2(pair_of(raw[k], i * E / 2 + j), both(-mean[k])), both(r));
+            unpack2(fma2(h, w[i * E / 2 + j], b[i * E / 2 + j]), out[2 * j], out[2 * j + 1]);
+          }
+        } else {
+          float v[2][E];
+          if constexpr (kKeep) {  // E = 1
+            float a, c;
+            unpack2(w[i / 2], a, c);
+            v[0][0] = i % 2 ? c : a;
+            unpack2(b[i / 2], a, c);
+            v[1][0] = i % 2 ? c : a;
+          } else {
+            params_at<E>(p.weight, p.param_type, at.col(i), 1.f, v[0]);
+            params_at<E>(p.bias, p.param_type, at.col(i), 0.f, v[1]);
+          }
+#pragma unroll
+          for (int e = 0; e < E; ++e) out[e] = fmaf((elem(raw[k][i], e) - mean[k]) * r, v[0][e], v[1][e]);
+        }
+        store_vec<Y, E>(y + at.col(i), out);
       }
       if (team.t == 0) {
-        if (p.mean) p.mean[row0 + k] = mean[k];
-        if (p.rstd) p.rstd[row0 + k] = r;
+        if (p.mean) p.mean[row] = mean[k];
+        if (p.rstd) p.rstd[row] = r;
       }
     }
   }
   stream_release();
 }
 
-template <typename X, typename Y, int E, int C, int SEG, int R>
-__global__ void __launch_bounds__(kNormMaxThreads) k_layer_norm_bwd(const NormParams p) {
+template <typename X, typename Y, int E, int C, int TEAM, int R>
+__global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThreads, TEAM == kWholeCta ? 1 : 4)
+    k_layer_norm_bwd(const NormParams p) {
   __shared__ float red[2 * 16 * 2 * R];
-  constexpr int V = C / E;
-  const Team<SEG> team(p.team);
+  extern __shared__ float wide[];  // C = 32: the threads' gradient sums, each at its own places
+  constexpr int V = C / E, P = C / 2;
+  constexpr bool kKeep = C == 8;
+  const Team<TEAM> team;
+  const Place<E, TEAM> at(team, p.width);
   const float inv = 1.f / (float)p.width;
   int turn = 0;
   stream_acquire();
-  Params<E, C> w(p.weight, p.param_type, 1.f, p.width, team.t, team.threads);
-  // The thread's gradient sums: registers, or (C = 32) its own places in shared memory.
-  extern __shared__ float wide[];
-  float dw[kInRegisters<C> ? C : 1], db[kInRegisters<C> ? C : 1];
-  bool in[V];
+  // Channels past the row's end have a weight, a dy and so every sum of 0.
+  float w[C];
+  F2 dw[kKeep ? P : 1], db[kKeep ? P : 1];
+  auto weights = [&](int i) {
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    in[i] = (team.t + i * team.threads) * E < p.width;
+    for (int e = 0; e < E; ++e) w[i * E + e] = 0.f;
+    if (at.in(i)) params_at<E>(p.weight, p.param_type, at.col(i), 1.f, w + i * E);
+  };
+  if (kKeep) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      if constexpr (kInRegisters<C>) {
-        dw[i * E + e] = 0.f;
-        db[i * E + e] = 0.f;
-      } else if (in[i]) {
-        wide[(i * E + e) * team.threads + team.t] = 0.f;
-        wide[(C + i * E + e) * team.threads + team.t] = 0.f;
-      }
-    }
+    for (int i = 0; i < V; ++i) weights(i);
+#pragma unroll
+    for (int j = 0; j < (kKeep ? P : 1); ++j) dw[j] = db[j] = both(0.f);
+  } else {
+#pragma unroll
+    for (int c = 0; c < 2 * C; ++c) wide[c * team.threads + team.t] = 0.f;
   }
-  const X* x = static_cast<const X*>(p.x) + (int64_t)team.t * E;
-  const Y* dy = static_cast<const Y*>(p.y) + (int64_t)team.t * E;
-  const X* dres = static_cast<const X*>(p.dres) + (p.dres ? (int64_t)team.t * E : 0);
-  X* dx = static_cast<X*>(p.out) + (int64_t)team.t * E;
-  const int step = team.threads * E;
-  const int64_t first = SEG < 32 ? team.index / (32 / SEG) * (32 / SEG) : team.index;
-  for (int64_t base = 0; (base + first) * R < p.rows; base += team.count) {
-    const int64_t row0 = (base + team.index) * R;
-    Vec<X, E> rx[R][V], rres[R][V];
-    Vec<Y, E> rdy[R][V];
-    float mean[R], rstd[R];
+  constexpr bool kAhead = kKeep;  // the next rows fit in the registers too
+  Vec<X, E> next_x[R][V], next_res[R][V];
+  Vec<Y, E> next_dy[R][V];
+  float next_mean[R], next_rstd[R];
+  auto load = [&](int64_t row0) {
 #pragma unroll
     for (int k = 0; k < R; ++k) {
-      const bool live = row0 + k < p.rows;
+      const int64_t row = row0 + k;
+      const bool live = row < p.rows;
+      load_row<X, E, V>(next_x[k], p.x, row, p.x_stride, at, live);
+      load_row<Y, E, V>(next_dy[k], p.y, row, p.y_stride, at, live);
+      if (p.dres) load_row<X, E, V>(next_res[k], p.dres, row, p.dres_stride, at, live);
+      next_mean[k] = live ? p.mean[row] : 0.f;
+      next_rstd[k] = live ? p.rstd[row] : 0.f;
+    }
+  };
+  const int64_t first = team.index / (32 / kLanes<TEAM>) * (32 / kLanes<TEAM>);
+  if (kAhead) load(team.index * R);
+  for (int64_t base = 0; (base + first) * R < p.rows; base += team.count) {
+    const int64_t row0 = (base + team.index) * R;
+    if (!kAhead) load(row0);
+    Vec<X, E> x[R][V], res[R][V];
+    Vec<Y, E> dy[R][V];
+    float r[R], mr[R];  // h = x r + mr
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const int64_t row = row0 + k;
-        rx[k][i] = in[i] && live ? load_vec<X, E>(x + row * p.x_stride + i * step) : zero_vec<X, E>();
-        rdy[k][i] = in[i] && live ? load_vec<Y, E>(dy + row * p.y_stride + i * step) : zero_vec<Y, E>();
-        rres[k][i] =
-            p.dres && in[i] && live ? load_vec<X, E>(dres + row * p.dres_stride + i * step) : zero_vec<X, E>();
+        x[k][i] = next_x[k][i];
+        dy[k][i] = next_dy[k][i];
+        res[k][i] = next_res[k][i];
       }
-      mean[k] = live ? p.mean[row0 + k] : 0.f;
-      rstd[k] = live ? p.rstd[row0 + k] : 0.f;
+      mr[k] = next_mean[k];
+      r[k] = next_rstd[k];
     }
+    if (kAhead) load(row0 + team.count * R);
+    // h = (x - mean) r, in this order: the difference keeps the digits of rows far from 0
+    auto h_of = [&](int k, int j) { return mul2(add2(pair_of(x[k], j), both(-mr[k])), both(r[k])); };
     float sums[2 * R];
 #pragma unroll
     for (int k = 0; k < R; ++k) {
-      float sg = 0.f, sgh = 0.f;
-      if (row0 + k < p.rows) {
+      F2 sg = both(0.f), sgh = both(0.f);
 #pragma unroll
-        for (int i = 0; i < V; ++i)
+      for (int j = 0; j < P; ++j) {
+        if (!kKeep && 2 * j % E == 0) weights(2 * j / E);
+        if (!kKeep && E == 1) weights(2 * j + 1);
+        const F2 d = pair_of(dy[k], j), h = h_of(k, j), g = mul2(d, pack2(w[2 * j], w[2 * j + 1]));
+        sg = add2(sg, g);
+        sgh = fma2(g, h, sgh);
+        if constexpr (kKeep) {
+          dw[j] = fma2(d, h, dw[j]);
+          db[j] = add2(db[j], d);
+        } else {
+          float v[4];
+          unpack2(mul2(d, h), v[0], v[1]);
+          unpack2(d, v[2], v[3]);
 #pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const int c = i * E + e;
-            const float d = elem(rdy[k][i], e), h = in[i] ? (elem(rx[k][i], e) - mean[k]) * rstd[k] : 0.f;
-            const float g = d * w.at(i, e);
-            sg += g;
-            sgh = fmaf(g, h, sgh);
-            if constexpr (kInRegisters<C>) {
-              dw[c] = fmaf(d, h, dw[c]);
-              db[c] += d;
-            } else if (in[i]) {
-              wide[c * team.threads + team.t] += d * h;
-              wide[(C + c) * team.threads + team.t] += d;
-            }
-          }
+          for (int q = 0; q < 4; ++q) wide[(C * (q / 2) + 2 * j + q % 2) * team.threads + team.t] += v[q];
+        }
       }
-      sums[2 * k] = sg;
-      sums[2 * k + 1] = sgh;
+      sums[2 * k] = sum2(sg) * inv;
+      sums[2 * k + 1] = sum2(sgh) * inv;
     }
-    team_sum<SEG>(sums, red, turn, team.warps);
+    team_sum<TEAM>(sums, red, turn);
 #pragma unroll
     for (int k = 0; k < R; ++k) {
       if (row0 + k >= p.rows) continue;
-      const float ag = sums[2 * k] * inv, agh = sums[2 * k + 1] * inv;
+      const F2 ag = both(-sums[2 * k]), agh = both(-sums[2 * k + 1]), r2 = both(r[k]);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        if (!in[i]) continue;
+        if (!at.in(i)) continue;
         float out[E];
+        if constexpr (E > 1) {
+          if (!kKeep) weights(i);
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float h = (elem(rx[k][i], e) - mean[k]) * rstd[k];
-          const float g = elem(rdy[k][i], e) * w.at(i, e);
-          out[e] = rstd[k] * (g - ag - h * agh);
-          if (p.dres) out[e] += elem(rres[k][i], e);
+          for (int j = i * E / 2; j < (i + 1) * E / 2; ++j) {
+            const F2 g = fma2(pair_of(dy[k], j), pack2(w[2 * j], w[2 * j + 1]), ag);
+            F2 d = mul2(fma2(h_of(k, j), agh, g), r2);
+            if (p.dres) d = add2(d, pair_of(res[k], j));
+            unpack2(d, out[2 * j - i * E], out[2 * j + 1 - i * E]);
+          }
+        } else {
+          if (!kKeep) weights(i);
+          const float h = (elem(x[k][i], 0) - mr[k]) * r[k], g = elem(dy[k][i], 0) * w[i];
+          out[0] = r[k] * (g - sums[2 * k] - h * sums[2 * k + 1]);
+          if (p.dres) out[0] += elem(res[k][i], 0);
         }
-        store_vec<X, E>(dx + (row0 + k) * p.dx_stride + i * step, out);
+        store_vec<X, E>(static_cast<X*>(p.out) + (row0 + k) * p.dx_stride + at.col(i), out);
       }
     }
   }
@@ -278,44 +358,46 @@ __global__ void __launch_bounds__(kNormMaxThreads) k_layer_norm_bwd(const NormPa
   if (!p.partial) return;
   // the CTA's partial rows: segments of a warp, then (teams of up to a warp) the CTA's warps in order
   float* out = p.partial + (int64_t)blockIdx.x * 2 * p.width;
-  if (SEG == 32 && team.warps > 1) {
+  if constexpr (TEAM == kWholeCta) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      if (!in[i]) continue;
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const int col = (team.t + i * team.threads) * E + e;
-        const int c = i * E + e;
-        out[col] = kInRegisters<C> ? dw[kInRegisters<C> ? c : 0] : wide[c * team.threads + team.t];
-        out[p.width + col] = kInRegisters<C> ? db[kInRegisters<C> ? c : 0] : wide[(C + c) * team.threads + team.t];
+    for (int c = 0; c < C; ++c) {
+      const int col = at.col(c / E) + c % E;
+      if (col >= p.width) continue;
+      float v[2];
+      if constexpr (kKeep) {
+        float a, b;
+        unpack2(dw[c / 2], a, b);
+        v[0] = c % 2 ? b : a;
+        unpack2(db[c / 2], a, b);
+        v[1] = c % 2 ? b : a;
+      } else {
+        v[0] = wide[c * team.threads + team.t];
+        v[1] = wide[(C + c) * team.threads + team.t];
       }
+      out[col] = v[0];
+      out[p.width + col] = v[1];
     }
-    return;
-  }
-  // teams of up to a warp have at most 32 C = 256 channels
-  __shared__ float part[kNormThreads / 32][2][32 * 8];
-  if constexpr (kInRegisters<C>) {
+  } else {  // at most 32 lanes of 8 channels
+    static_assert(C == 8, "8 channels per lane");
+    __shared__ float part[kNormThreads / 32][2][32 * C];
     const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
 #pragma unroll
-    for (int c = 0; c < C; ++c)
+    for (int c = 0; c < C; ++c) {
+      float a, b, v[2];
+      unpack2(dw[c / 2], a, b);
+      v[0] = c % 2 ? b : a;
+      unpack2(db[c / 2], a, b);
+      v[1] = c % 2 ? b : a;
 #pragma unroll
-      for (int o = SEG; o < 32; o <<= 1) {
-        dw[c] += __shfl_xor_sync(0xffffffffu, dw[c], o);
-        db[c] += __shfl_xor_sync(0xffffffffu, db[c], o);
+      for (int q = 0; q < 2; ++q) {
+#pragma unroll
+        for (int o = TEAM; o < 32; o <<= 1) v[q] += __shfl_xor_sync(0xffffffffu, v[q], o);
+        if (lane < TEAM) part[warp][q][at.col(c / E) + c % E] = v[q];
       }
-    if (lane < SEG) {
-#pragma unroll
-      for (int i = 0; i < V; ++i)
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const int col = (team.t + i * team.threads) * E + e;
-          part[warp][0][col] = dw[i * E + e];
-          part[warp][1][col] = db[i * E + e];
-        }
     }
     __syncthreads();
     for (int k = (int)threadIdx.x; k < 2 * p.width; k += kNormThreads) {
-      const int a = k / p.width, col = k - a * p.width;
+      const int a = k >= p.width, col = k - a * p.width;
       float v = 0.f;
 #pragma unroll
       for (int q = 0; q < kNormThreads / 32; ++q) v += part[q][a][col];
@@ -366,24 +448,24 @@ int norm_ctas(K kern, int threads, size_t smem, int teams_per_cta, int64_t batch
   return (int)((ctas + steps - 1) / steps);
 }
 
-template <bool BWD, typename X, typename Y, int E, int C, int SEG>
-cudaError_t launch_norm_as(const NormArgs& a, NormParams p, cudaStream_t st) {
-  constexpr int R = C == 32 ? 1 : BWD ? (sizeof(X) == 2 && E > 1 ? 2 : 1) : (sizeof(X) == 2 && E > 1 ? 4 : 2);
-  p.team = SEG < 32 ? SEG : ((p.width + C - 1) / C + 31) / 32 * 32;
-  const int threads = p.team <= 32 ? kNormThreads : p.team;
-  const int per_cta = threads / p.team;
-  const int64_t batches = (p.rows + R - 1) / R;
+template <bool BWD, typename X, typename Y, int E, int C, int TEAM>
+cudaError_t launch_norm_as(const NormArgs& a, const NormParams& p, cudaStream_t st) {
+  constexpr bool wide = sizeof(X) == 4 || E == 1;  // elements that take a register each as they lie
+  const int threads = TEAM == kWholeCta ? ((p.width + C - 1) / C + 31) / 32 * 32 : kNormThreads;
+  const int per_cta = TEAM == kWholeCta ? 1 : kNormThreads / kLanes<TEAM>;
   if constexpr (!BWD) {
-    auto kern = k_layer_norm<X, Y, E, C, SEG, R>;
-    const int ctas = norm_ctas(kern, threads, 0, per_cta, batches, INT32_MAX);
+    constexpr int R = C == 32 ? 1 : wide ? 16 / C : 32 / C;
+    auto kern = k_layer_norm<X, Y, E, C, TEAM, R>;
+    const int ctas = norm_ctas(kern, threads, 0, per_cta, (p.rows + R - 1) / R, INT32_MAX);
     return launch_pdl(kern, ctas, threads, 0, st, true, p);
   } else {
-    auto kern = k_layer_norm_bwd<X, Y, E, C, SEG, R>;
-    const size_t smem = kInRegisters<C> ? 0 : 2 * C * sizeof(float) * threads;
+    constexpr int R = C == 32 || wide ? 1 : 2;
+    auto kern = k_layer_norm_bwd<X, Y, E, C, TEAM, R>;
+    const size_t smem = C == 8 ? 0 : 2 * C * sizeof(float) * threads;
     cudaError_t e = cudaSuccess;
     if (smem > 0) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    const int ctas = norm_ctas(kern, threads, smem, per_cta, batches, kNormParts);
+    const int ctas = norm_ctas(kern, threads, smem, per_cta, (p.rows + R - 1) / R, kNormParts);
     e = launch_pdl(kern, ctas, threads, smem, st, true, p);
     if (e != cudaSuccess || !p.partial) return e;
     return launch_pdl(k_fold_parts, (2 * p.width + 31) / 32, 32 * kFoldWarps, 0, st, true, p.partial, ctas,
@@ -394,11 +476,26 @@ cudaError_t launch_norm_as(const NormArgs& a, NormParams p, cudaStream_t st) {
 template <bool BWD, typename X, typename Y>
 cudaError_t launch_norm_typed(const NormArgs& a, const NormParams& p, bool vec, cudaStream_t st) {
   constexpr int E = 16 / (int)sizeof(X);
-  if (vec && p.width <= 64) return launch_norm_as<BWD, X, Y, E, 8, 8>(a, p, st);
-  if (vec && p.width <= 128) return launch_norm_as<BWD, X, Y, E, 8, 16>(a, p, st);
-  if (p.width <= 8 * kNormMaxThreads)
-    return vec ? launch_norm_as<BWD, X, Y, E, 8, 32>(a, p, st) : launch_norm_as<BWD, X, Y, 1, 8, 32>(a, p, st);
-  return vec ? launch_norm_as<BWD, X, Y, E, 32, 32>(a, p, st) : launch_norm_as<BWD, X, Y, 1, 32, 32>(a, p, st);
+  const int D = p.width;
+  if (!vec) {
+    if (D <= 256) return launch_norm_as<BWD, X, Y, 1, 8, 32>(a, p, st);
+    if (D <= 8 * kNormMaxThreads) return launch_norm_as<BWD, X, Y, 1, 8, kWholeCta>(a, p, st);
+    return launch_norm_as<BWD, X, Y, 1, 32, kWholeCta>(a, p, st);
+  }
+  if (D <= 64) return launch_norm_as<BWD, X, Y, E, 8, 8>(a, p, st);
+  if (D <= 128) return launch_norm_as<BWD, X, Y, E, 8, 16>(a, p, st);
+  if (D <= 256) return launch_norm_as<BWD, X, Y, E, 8, 32>(a, p, st);
+  if constexpr (BWD) {
+    if (D <= 8 * kNormMaxThreads) return launch_norm_as<BWD, X, Y, E, 8, kWholeCta>(a, p, st);
+  } else {
+    if (D <= 512) return launch_norm_as<BWD, X, Y, E, 16, 32>(a, p, st);
+    if constexpr (sizeof(X) == 2) {
+      if (D <= 1024) return launch_norm_as<BWD, X, Y, E, 32, 32>(a, p, st);
+    } else {
+      if (D <= 16 * kNormMaxThreads) return launch_norm_as<BWD, X, Y, E, 16, kWholeCta>(a, p, st);
+    }
+  }
+  return launch_norm_as<BWD, X, Y, E, 32, kWholeCta>(a, p, st);
 }
 
 template <bool BWD>
@@ -432,7 +529,8 @@ cudaError_t launch_norm(const NormArgs& a, cudaStream_t st) {
   auto fits = [&](const void* q, int64_t stride, int bytes) {
     return !q || (reinterpret_cast<uintptr_t>(q) % (E * bytes) == 0 && (p.rows == 1 || stride % E == 0));
   };
-  const bool vec = p.width % E == 0 && fits(a.x, p.x_stride, xb) && fits(a.dy, p.y_stride, yb) &&
+  auto fits_params = [&](const void* q) { return reinterpret_cast<uintptr_t>(q) % 16 == 0; };
+  const bool vec = p.width % E == 0 && fits_params(a.weight) && fits_params(a.bias) && fits(a.x, p.x_stride, xb) && fits(a.dy, p.y_stride, yb) &&
                    fits(a.dres, p.dres_stride, xb) &&
                    fits(a.out, BWD ? p.dx_stride : p.y_stride, BWD ? xb : yb);
   switch (a.n.x_type * 4 + a.n.y_type) {

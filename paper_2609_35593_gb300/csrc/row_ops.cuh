@@ -132,12 +132,121 @@ __device__ __forceinline__ float param_at(const void* p, int type, int64_t i, fl
   return to_f32(static_cast<const f16*>(p)[i]);
 }
 
+// E consecutive parameters, col a multiple of E, aligned to 16 bytes (E = 4 of 16 bits: 8) where E > 1.
+template <int E>
+__device__ __forceinline__ void params_at(const void* p, int type, int64_t col, float none, float* out) {
+  if constexpr (E == 1) {
+    out[0] = param_at(p, type, col, none);
+  } else if (!p) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) out[e] = none;
+  } else if (type == RESS_F32) {
+#pragma unroll
+    for (int k = 0; k < E / 4; ++k) {
+      const float4 v = reinterpret_cast<const float4*>(static_cast<const float*>(p) + col)[k];
+      out[4 * k] = v.x, out[4 * k + 1] = v.y, out[4 * k + 2] = v.z, out[4 * k + 3] = v.w;
+    }
+  } else {
+    uint32_t w[E / 2];
+    const uint16_t* at = static_cast<const uint16_t*>(p) + col;
+    if constexpr (E == 8) {
+      const uint4 v = *reinterpret_cast<const uint4*>(at);
+      w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+    } else {
+      static_assert(E == 4, "1, 4 or 8 parameters");
+      const uint2 v = *reinterpret_cast<const uint2*>(at);
+      w[0] = v.x, w[1] = v.y;
+    }
+    if (type == RESS_BF16) {
+#pragma unroll
+      for (int k = 0; k < E / 2; ++k) out[2 * k] = bf16_lo(w[k]), out[2 * k + 1] = bf16_hi(w[k]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < E / 2; ++k) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
+        out[2 * k] = f.x, out[2 * k + 1] = f.y;
+      }
+    }
+  }
+}
+
+// Two floats for the packed float32 instructions, which do two operations per lane and issue: these
+// kernels have enough arithmetic per byte for it to show (layer norm's gradient, 43,968 x 1024 bf16
+// with a residual: 63 us packed, 80 one by one).
+struct F2 {
+  uint64_t v;
+};
+__device__ __forceinline__ F2 pack2(float a, float b) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ F2 both(float a) { return pack2(a, a); }
+__device__ __forceinline__ void unpack2(F2 x, float& a, float& b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x.v));
+}
+__device__ __forceinline__ float sum2(F2 x) {
+  float a, b;
+  unpack2(x, a, b);
+  return a + b;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return d;
+}
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+  F2 d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v));
+  return d;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+  F2 d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v));
+  return d;
+}
+
+// Elements 2j and 2j + 1 of a thread's vectors.
+template <typename T, int E, int V>
+__device__ __forceinline__ F2 pair_of(const Vec<T, E> (&v)[V], int j) {
+  if constexpr (E > 1 && __is_same(T, f16)) {
+    const uint32_t w = v[2 * j / E].w[j % (E / 2)];
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+    return pack2(f.x, f.y);
+  } else {
+    return pack2(elem(v[2 * j / E], 2 * j % E), elem(v[(2 * j + 1) / E], (2 * j + 1) % E));
+  }
+}
+
 // The sum of v over aligned segments of SEG lanes, in every lane of the segment.
 template <int SEG>
 __device__ __forceinline__ float segment_sum(float v) {
 #pragma unroll
   for (int o = SEG / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
+}
+
+// Sums of N values over aligned segments of SEG lanes, N a power of two of at most SEG, by halves:
+// each step sends one half of the values to the other half of the lanes, so that N values take
+// N - 1 + log2(SEG / N) exchanges instead of N log2(SEG).  Lane l of a segment holds the sum of value
+// l / (SEG / N).
+template <int SEG, int N>
+__device__ __forceinline__ float segment_sums(float (&v)[N]) {
+  const int lane = (int)threadIdx.x & 31;
+  int o = SEG / 2;
+#pragma unroll
+  for (int n = N; n > 1; n /= 2, o /= 2) {
+    const bool up = (lane & o) != 0;
+#pragma unroll
+    for (int k = 0; k < n / 2; ++k) {
+      const float send = up ? v[k] : v[k + n / 2], keep = up ? v[k + n / 2] : v[k];
+      v[k] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+    }
+  }
+  float r = v[0];
+#pragma unroll
+  for (int q = SEG / N / 2; q > 0; q /= 2) r += __shfl_xor_sync(0xffffffffu, r, q);
+  return r;
 }
 
 // cos and sin of a position's angle.  The plan holds each frequency in turns per unit position as
