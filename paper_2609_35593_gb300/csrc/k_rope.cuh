@@ -1,0 +1,512 @@
+// Rotary positions over several axes on the heads of Q and K, after a layer norm over each head's
+// channels where there is one, and the gradients of both.
+//   forward   u = (x - m) r w + b over the head's channels (or u = x), then for each pair (i, j) of
+//             channels with its angle t:  y_i = u_i cos t - u_j sin t,  y_j = u_j cos t + u_i sin t
+//   backward  du = the same of dy with -t;  dx = du, or with h = (x - m) r and g = du w:
+//             dx = r (g - avg(g) - h avg(g h)),  dw = sum over tokens and heads of du h,  db = of du
+// Memory-bound in bytes, but every element takes part in two sums and a rotation: with 248
+// instructions per row of 4 heads of 64 the instructions took 111 us of the 53 that the bytes need
+// (43,968 tokens, 16 + 16 heads, bf16), so the kernel is laid out for few of them.
+//
+// A lane holds 4 slots, each the two channels of a pair (or two channels without a pair), so that a
+// rotation needs no other lane, and a head has G lanes.  Where the plan's pairs are 4 and 4
+// neighbouring channels (kChunks) or 8 neighbours (kNeighbours) they are read and written as
+// vectors, else one by one (kGather).  A warp goes through rows of 32 / G heads, the next D rows on
+// their way.  An item is a token's rows of one tensor (or one of them, where tokens are few): a CTA
+// stays with Q or K (shares of the grid by their heads), and its lanes keep the norm's parameters
+// and their gradients' sums in registers.  The token's cosines and sines are formed once per item,
+// one pair per lane, and handed out through shared memory.  Sums are float32 in a fixed order; the
+// gradients of the parameters are summed per CTA and then over CTAs by a second kernel.
+#pragma once
+
+#include "row_ops.cuh"
+
+namespace ress {
+using namespace rows;
+
+namespace {
+
+constexpr int kRopeWarps = 4;
+constexpr int kRopeThreads = 32 * kRopeWarps;
+
+enum { kChunks = 0, kNeighbours = 1, kGather = 2 };
+
+struct RopeTensor {
+  int heads;
+  const void *weight, *bias;
+  const void *x, *y;  // y: backward dy
+  void* out;          // forward y, backward dx
+  int64_t x_token, x_head, y_token, y_head, out_token, out_head;  // strides in elements
+};
+
+struct RopeParams {
+  ress_rope_plan plan;
+  RopeTensor t[2];
+  int64_t tokens;
+  const int32_t* pos;
+  float* partial;
+  float eps;
+  int first_ctas;  // CTAs of t[0]; the others have t[1]
+  int item_rows;   // rows of an item
+  int param_type;
+  bool all;        // every channel has a pair
+};
+
+// The channels of a slot.  Slots past the pairs have channels without one, if any are left: two
+// neighbours, or (kChunks) those of 4 slots as 4 and 4 neighbours.
+__device__ __forceinline__ void slot_channels(const ress_rope_plan& p, int mode, int slot, int& a, int& b) {
+  if (slot >= p.n_pairs) {
+    const int i = slot - p.n_pairs;
+    a = mode == kChunks ? 2 * p.n_pairs + i / 4 * 8 + i % 4 : 2 * p.n_pairs + 2 * i;
+    b = mode == kChunks ? a + 4 : a + 1;
+    return;
+  }
+  if (p.layout == RESS_ROPE_INTERLEAVED) {
+    a = 2 * slot, b = 2 * slot + 1;
+  } else if (p.layout == RESS_ROPE_HALVES) {
+    a = slot, b = slot + p.n_pairs;
+  } else {
+    const int axis = rope_axis(p, slot);
+    int start = 0;
+    for (int i = 0; i < axis; ++i) start += p.axis_dims[i];
+    a = start + slot - start / 2;
+    b = a + p.axis_dims[axis] / 2;
+  }
+}
+
+// A lane's 8 elements: the first channels of its slots in words of their own, then the second ones
+// (kNeighbours: as they lie).
+template <typename T, int MODE>
+struct Slots {
+  const int *a, *b;  // kGather: the slots' channels
+  bool in[4];        // the slots that exist
+  bool any;          // (not kGather: all or none)
+  int first, next;   // kChunks, kNeighbours: the lane's two vectors of 4 channels
+
+  __device__ Vec<T, 8> load(const T* p, bool live) const {
+    Vec<T, 8> r = zero_vec<T, 8>();
+    if (!live || !any) return r;
+    if constexpr (MODE == kNeighbours) {
+      r = load_vec<T, 8>(p + first);
+    } else if constexpr (MODE == kChunks) {
+      const Vec<T, 4> u = load_vec<T, 4>(p + first), v = load_vec<T, 4>(p + next);
+      constexpr int W = Vec<T, 4>::kWords;
+#pragma unroll
+      for (int k = 0; k < W; ++k) r.w[k] = u.w[k], r.w[W + k] = v.w[k];
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (in[j]) {
+          put(r, j, p[a[j]]);
+          put(r, 4 + j, p[b[j]]);
+        }
+    }
+    return r;
+  }
+  __device__ static void put(Vec<T, 8>& r, int j, T v) {
+    if constexpr (sizeof(T) == 4)
+      r.w[j] = __float_as_uint(v);
+    else
+      r.w[j / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(&v) << (16 * (j & 1));
+  }
+  // Slots 2 q and 2 q + 1: their first (side 0) or second channels.
+  __device__ static F2 get(const Vec<T, 8>& r, int side, int q) {
+    if constexpr (MODE == kNeighbours)
+      return pack2(elem(r, 4 * q + side), elem(r, 4 * q + 2 + side));
+    const Vec<T, 8> one[1] = {r};
+    return pair_of(one, 2 * side + q);
+  }
+  __device__ void store(T* p, const F2 (&u)[2][2], bool live) const {
+    if (!live || !any) return;
+    float v[2][4];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      unpack2(u[s][0], v[s][0], v[s][1]);
+      unpack2(u[s][1], v[s][2], v[s][3]);
+    }
+    if constexpr (MODE == kNeighbours) {
+      float o[8];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[2 * j] = v[0][j], o[2 * j + 1] = v[1][j];
+      store_vec<T, 8>(p + first, o);
+    } else if constexpr (MODE == kChunks) {
+      store_vec<T, 4>(p + first, v[0]);
+      store_vec<T, 4>(p + next, v[1]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (in[j]) {
+          p[a[j]] = from_f32<T>(v[0][j]);
+          p[b[j]] = from_f32<T>(v[1][j]);
+        }
+    }
+  }
+};
+
+template <typename T, int G, int MODE, bool NORM, bool BWD, int D>
+__global__ void __launch_bounds__(kRopeThreads, NORM && BWD ? 4 : 5) k_rope(const __grid_constant__ RopeParams p) {
+  constexpr int kHeads = 32 / G;              // heads of a warp's row
+  constexpr int kPairs = G <= 8 ? 1 : G / 8;  // pairs per lane: 4 G pairs at most
+  constexpr bool kReadX = !BWD || NORM;
+  __shared__ __align__(16) float cosines[kRopeWarps][32 * kPairs], sines[kRopeWarps][32 * kPairs];
+  const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
+  const bool second = (int)blockIdx.x >= p.first_ctas;
+  const RopeTensor& t = p.t[second];
+  const int hd = p.plan.head_dim, heads = t.heads;
+  const int group = lane / G, slot = lane % G * 4;
+  const float inv = 1.f / (float)hd;
+
+  int a[4], b[4];
+  Slots<T, MODE> at_slots;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    at_slots.in[j] = 2 * (slot + j) < hd;
+    slot_channels(p.plan, MODE, min(slot + j, hd / 2 - 1), a[j], b[j]);
+  }
+  at_slots.a = a;
+  at_slots.b = b;
+  at_slots.any = at_slots.in[0];
+  at_slots.first = a[0];
+  at_slots.next = b[0];
+  const bool turns = slot < p.plan.n_pairs;  // kGather: slots turn one by one
+  // The pairs whose angles this lane forms.
+  uint64_t freq[kPairs];
+  int axis[kPairs];
+#pragma unroll
+  for (int q = 0; q < kPairs; ++q) {
+    const int k = min(lane + 32 * q, p.plan.n_pairs - 1);
+    freq[q] = p.plan.turns[k];
+    axis[q] = rope_axis(p.plan, k);
+  }
+
+  stream_acquire();
+  // [side][slots 0 and 1, slots 2 and 3]
+  F2 w[2][2], shift[2][2], dw[2][2], db[2][2];
+#pragma unroll
+  for (int s = 0; s < 2; ++s)
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      float v[2][2] = {};
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int j = 2 * q + e, c = s ? b[j] : a[j];
+        if (NORM && at_slots.in[j]) {
+          v[0][e] = param_at(t.weight, p.param_type, c, 1.f);
+          if (!BWD) v[1][e] = param_at(t.bias, p.param_type, c, 0.f);
+        }
+      }
+      w[s][q] = pack2(v[0][0], v[0][1]);
+      shift[s][q] = pack2(v[1][0], v[1][1]);
+      dw[s][q] = db[s][q] = both(0.f);
+    }
+
+  // Rows of the warp, item after item.
+  const int token_rows = (heads + kHeads - 1) / kHeads, chunks = (token_rows + p.item_rows - 1) / p.item_rows;
+  const int64_t warps = (int64_t)(second ? gridDim.x - p.first_ctas : p.first_ctas) * kRopeWarps;
+  const int64_t w0 = (int64_t)(blockIdx.x - (second ? p.first_ctas : 0)) * kRopeWarps + warp;
+  const int64_t step = warps / chunks;
+  const int step_rest = (int)(warps - step * chunks);
+  const int64_t x_row = t.x_head * kHeads, y_row = t.y_head * kHeads, out_row = t.out_head * kHeads;
+  int64_t token = w0 / chunks;
+  int chunk = (int)(w0 - token * chunks);
+  // the rows under way: of the item at (ahead, ahead_chunk), rows up to `end`
+  Vec<T, 8> queue_x[kReadX ? D : 1], queue_y[BWD ? D : 1];
+  int64_t ahead = token;
+  int ahead_chunk = chunk, row = 0, end = 0;
+  const T *px = nullptr, *py = nullptr;
+  auto open = [&]() {
+    row = ahead_chunk * p.item_rows;
+    end = ahead < p.tokens ? min(token_rows, row + p.item_rows) : INT32_MAX;  // no rows any more
+    const int h = row * kHeads + group;
+    if constexpr (kReadX) px = static_cast<const T*>(t.x) + ahead * t.x_token + h * t.x_head;
+    if constexpr (BWD) py = static_cast<const T*>(t.y) + ahead * t.y_token + h * t.y_head;
+  };
+  auto load = [&](int d) {
+    const bool live = end != INT32_MAX && row * kHeads + group < heads;
+    if constexpr (kReadX) {
+      queue_x[d] = at_slots.load(px, live);
+      px += x_row;
+    }
+    if constexpr (BWD) {
+      queue_y[d] = at_slots.load(py, live);
+      py += y_row;
+    }
+    if (++row == end) {
+      ahead += step;
+      ahead_chunk += step_rest;
+      if (ahead_chunk >= chunks) {
+        ahead_chunk -= chunks;
+        ++ahead;
+      }
+      open();
+    }
+  };
+  int32_t pos[kPairs];
+  auto load_pos = [&](int64_t at) {
+#pragma unroll
+    for (int q = 0; q < kPairs; ++q) pos[q] = at < p.tokens ? p.pos[at * p.plan.n_axes + axis[q]] : 0;
+  };
+  load_pos(token);
+  open();
+#pragma unroll
+  for (int d = 0; d < D; ++d) load(d);
+#pragma unroll 1
+  while (token < p.tokens) {
+    // the item's angles; the next one's positions are on their way meanwhile
+    float2 cs[kPairs];
+#pragma unroll
+    for (int q = 0; q < kPairs; ++q) cs[q] = rope_cos_sin(pos[q], freq[q]);
+    int64_t next_token = token + step;
+    int next_chunk = chunk + step_rest;
+    if (next_chunk >= chunks) {
+      next_chunk -= chunks;
+      ++next_token;
+    }
+    load_pos(next_token);
+    __syncwarp();  // the last item's are read
+#pragma unroll
+    for (int q = 0; q < kPairs; ++q) {
+      cosines[warp][lane + 32 * q] = cs[q].x;
+      sines[warp][lane + 32 * q] = BWD ? -cs[q].y : cs[q].y;
+    }
+    __syncwarp();
+    const float4 c4 = *reinterpret_cast<const float4*>(&cosines[warp][slot]);
+    const float4 s4 = *reinterpret_cast<const float4*>(&sines[warp][slot]);
+    const F2 co[2] = {pack2(c4.x, c4.y), pack2(c4.z, c4.w)}, si[2] = {pack2(s4.x, s4.y), pack2(s4.z, s4.w)};
+    const F2 neg[2] = {pack2(-s4.x, -s4.y), pack2(-s4.z, -s4.w)};
+    int head = chunk * p.item_rows * kHeads + group;
+    const int last = min(heads, (chunk * p.item_rows + p.item_rows) * kHeads);
+    T* out = static_cast<T*>(t.out) + token * t.out_token + head * t.out_head;
+#pragma unroll 1
+    for (; head - group < last; head += kHeads, out += out_row) {
+      Vec<T, 8> x, y;
+      if constexpr (kReadX) {
+        x = queue_x[0];
+#pragma unroll
+        for (int d = 1; d < D; ++d) queue_x[d - 1] = queue_x[d];
+      }
+      if constexpr (BWD) {
+        y = queue_y[0];
+#pragma unroll
+        for (int d = 1; d < D; ++d) queue_y[d - 1] = queue_y[d];
+      }
+      load(D - 1);
+      F2 h[2][2], u[2][2];
+      float rstd = 1.f;
+      if constexpr (NORM) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int q = 0; q < 2; ++q) h[s][q] = Slots<T, MODE>::get(x, s, q);
+        // a lane's sum is scaled before the lanes' meet: the sum may overflow where its average does not
+        const F2 m = both(-segment_sum<G>(sum2(add2(add2(h[0][0], h[0][1]), add2(h[1][0], h[1][1]))) * inv));
+        F2 sq = both(0.f);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            h[s][q] = add2(h[s][q], m);
+            if constexpr (MODE == kGather) {  // slots that do not exist
+              float e0, e1;
+              unpack2(h[s][q], e0, e1);
+              h[s][q] = pack2(at_slots.in[2 * q] ? e0 : 0.f, at_slots.in[2 * q + 1] ? e1 : 0.f);
+            }
+            sq = fma2(h[s][q], h[s][q], sq);
+          }
+        rstd = rsqrtf(segment_sum<G>(at_slots.any ? sum2(sq) * inv : 0.f) + p.eps);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            h[s][q] = mul2(h[s][q], both(rstd));
+            if (!BWD) u[s][q] = fma2(h[s][q], w[s][q], shift[s][q]);
+          }
+      }
+      if constexpr (BWD || !NORM) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int q = 0; q < 2; ++q) u[s][q] = Slots<T, MODE>::get(BWD ? y : x, s, q);
+      }
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        F2 r0 = fma2(u[0][q], co[q], mul2(u[1][q], neg[q])), r1 = fma2(u[1][q], co[q], mul2(u[0][q], si[q]));
+        if (!p.all) {  // channels without a pair keep their bits
+          if constexpr (MODE == kGather) {
+            float v[4], k[4];
+            unpack2(r0, v[0], v[1]);
+            unpack2(r1, v[2], v[3]);
+            unpack2(u[0][q], k[0], k[1]);
+            unpack2(u[1][q], k[2], k[3]);
+            const bool t0 = slot + 2 * q < p.plan.n_pairs, t1 = slot + 2 * q + 1 < p.plan.n_pairs;
+            r0 = pack2(t0 ? v[0] : k[0], t1 ? v[1] : k[1]);
+            r1 = pack2(t0 ? v[2] : k[2], t1 ? v[3] : k[3]);
+          } else if (!turns) {
+            r0 = u[0][q], r1 = u[1][q];
+          }
+        }
+        u[0][q] = r0, u[1][q] = r1;
+      }
+      if constexpr (NORM && BWD) {
+        // rows past the last head and slots that do not exist have dy = 0 and add nothing, but h may
+        // be anything where x is not read
+        F2 sg = both(0.f), sgh = both(0.f);
+        const bool live = head < heads;
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            if (live) {
+              dw[s][q] = fma2(u[s][q], h[s][q], dw[s][q]);
+              db[s][q] = add2(db[s][q], u[s][q]);
+            }
+            u[s][q] = mul2(u[s][q], w[s][q]);
+            sg = add2(sg, u[s][q]);
+            sgh = fma2(u[s][q], h[s][q], sgh);
+          }
+        const F2 ag = both(-segment_sum<G>(sum2(sg) * inv)), agh = both(-segment_sum<G>(sum2(sgh) * inv));
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int q = 0; q < 2; ++q) u[s][q] = mul2(fma2(h[s][q], agh, add2(u[s][q], ag)), both(rstd));
+      }
+      at_slots.store(out, u, head < heads);
+    }
+    token = next_token;
+    chunk = next_chunk;
+  }
+  stream_release();
+  if constexpr (NORM && BWD) {
+    if (!p.partial) return;
+    // the CTA's sums: a warp's groups, then its warps in order
+    __shared__ float part[kRopeWarps][2][G * 8];
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        float v[2][2];
+        unpack2(dw[s][q], v[0][0], v[0][1]);
+        unpack2(db[s][q], v[1][0], v[1][1]);
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+#pragma unroll
+            for (int o = G; o < 32; o <<= 1) v[k][e] += __shfl_xor_sync(0xffffffffu, v[k][e], o);
+            if (lane < G && at_slots.in[2 * q + e]) part[warp][k][s ? b[2 * q + e] : a[2 * q + e]] = v[k][e];
+          }
+      }
+    __syncthreads();
+    for (int k = (int)threadIdx.x; k < 2 * hd; k += kRopeThreads) {
+      const int which = k >= hd, c = k - which * hd;
+      float v = 0.f;
+#pragma unroll
+      for (int q = 0; q < kRopeWarps; ++q) v += part[q][which][c];
+      p.partial[((int64_t)blockIdx.x * 2 + which) * hd + c] = v;
+    }
+  }
+}
+
+// CTAs of the two tensors of a launch; the forward's launch has no sums to fold.
+template <typename T, int G, int MODE, bool NORM, bool BWD>
+cudaError_t launch_rope_as(RopeParams& p, int (&ctas)[2], cudaStream_t st) {
+  constexpr int D = 2;
+  auto kern = k_rope<T, G, MODE, NORM, BWD, D>;
+  int resident = 1;
+  if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kern, kRopeThreads, 0) != cudaSuccess || resident < 1)
+    resident = 1;
+  const int64_t fit = min((int64_t)resident * sm_count(), (int64_t)kRopeParts - 1);
+  // Items: whole tokens, which form their angles once, if there is work for every warp; else single rows.
+  p.item_rows = 2 * p.tokens >= fit * kRopeWarps ? INT32_MAX / 64 : 1;
+  int64_t need[2], all = 0;  // CTAs at one item per warp
+  for (int i = 0; i < 2; ++i) {
+    const int rows = (p.t[i].heads + 32 / G - 1) / (32 / G);
+    need[i] = (p.tokens * (p.item_rows == 1 ? rows : min(rows, 1)) + kRopeWarps - 1) / kRopeWarps;
+    all += need[i];
+  }
+  // shares of what fits at once by the tensors' heads, with the same number of items for each warp
+  for (int i = 0; i < 2; ++i) {
+    const int64_t heads = p.t[0].heads + p.t[1].heads;
+    const int64_t share = all <= fit ? need[i] : max(fit * p.t[i].heads / heads, (int64_t)1);
+    const int64_t steps = need[i] == 0 ? 1 : (need[i] + share - 1) / share;
+    ctas[i] = (int)((need[i] + steps - 1) / steps);
+  }
+  p.first_ctas = ctas[0];
+  if (ctas[0] + ctas[1] == 0) return cudaSuccess;
+  return launch_pdl(kern, ctas[0] + ctas[1], kRopeThreads, 0, st, true, p);
+}
+
+template <typename T, bool NORM, bool BWD>
+cudaError_t launch_rope_typed(RopeParams& p, int mode, int (&ctas)[2], cudaStream_t st) {
+  const int hd = p.plan.head_dim;
+  if (mode == kGather)
+    return hd <= 64 ? launch_rope_as<T, 8, kGather, NORM, BWD>(p, ctas, st)
+                    : launch_rope_as<T, 32, kGather, NORM, BWD>(p, ctas, st);
+  if (mode == kNeighbours) {
+    if (hd <= 32) return launch_rope_as<T, 4, kNeighbours, NORM, BWD>(p, ctas, st);
+    if (hd <= 64) return launch_rope_as<T, 8, kNeighbours, NORM, BWD>(p, ctas, st);
+    if (hd <= 128) return launch_rope_as<T, 16, kNeighbours, NORM, BWD>(p, ctas, st);
+    return launch_rope_as<T, 32, kNeighbours, NORM, BWD>(p, ctas, st);
+  }
+  if (hd <= 32) return launch_rope_as<T, 4, kChunks, NORM, BWD>(p, ctas, st);
+  if (hd <= 64) return launch_rope_as<T, 8, kChunks, NORM, BWD>(p, ctas, st);
+  if (hd <= 128) return launch_rope_as<T, 16, kChunks, NORM, BWD>(p, ctas, st);
+  return launch_rope_as<T, 32, kChunks, NORM, BWD>(p, ctas, st);
+}
+
+// How a lane's channels lie: see the top.  vector: elements that the tensors are aligned to.
+inline int rope_mode(const ress_rope_plan& plan, int vector) {
+  if (plan.head_dim % 8 != 0 || plan.n_pairs % 4 != 0) return kGather;
+  if (plan.layout == RESS_ROPE_INTERLEAVED) return vector % 8 == 0 ? kNeighbours : kGather;
+  if (plan.layout == RESS_ROPE_SECTIONS)
+    for (int a = 0; a < plan.n_axes; ++a)
+      if (plan.axis_dims[a] % 8 != 0) return kGather;
+  return vector % 4 == 0 ? kChunks : kGather;
+}
+
+// The launch of the tensors whose norm is enabled, or of those where it is not; the others' head count
+// is 0 in it.  ctas: of each tensor; any: whether there are such tensors.
+template <bool NORM, bool BWD>
+cudaError_t launch_rope_part(const RopeArgs& a, int (&ctas)[2], cudaStream_t st) {
+  RopeParams p;
+  p.plan = a.plan;
+  p.tokens = a.n_tokens;
+  p.pos = a.pos;
+  p.eps = a.eps;
+  p.param_type = a.param_type;
+  p.all = 2 * a.plan.n_pairs == a.plan.head_dim;
+  p.partial = NORM && BWD ? a.partial : nullptr;
+  ctas[0] = ctas[1] = 0;
+  const int bytes = a.type == RESS_F32 ? 4 : 2;
+  int vector = 8;  // 8, 4 or 1 elements
+  bool any = false;
+  for (int i = 0; i < 2; ++i) {
+    const ress_rope_heads& t = a.t[i];
+    p.t[i] = RopeTensor{};
+    if (t.n_heads == 0 || (t.norm.enabled != 0) != NORM) continue;
+    any = true;
+    const ress_heads& out = BWD ? t.dx : t.y;
+    p.t[i] = RopeTensor{t.n_heads,        t.norm.weight,   t.norm.bias,    t.x.data,         t.y.data,
+                        out.data,         t.x.token_stride, t.x.head_stride, t.y.token_stride, t.y.head_stride,
+                        out.token_stride, out.head_stride};
+    auto fits = [&](const ress_heads& h) {
+      for (; vector > 1; vector = vector == 8 ? 4 : 1) {
+        const int align = min(vector * bytes, 16);
+        if (reinterpret_cast<uintptr_t>(h.data) % align == 0 &&
+            (a.n_tokens == 1 || h.token_stride * bytes % align == 0) && (t.n_heads == 1 || h.head_stride * bytes % align == 0))
+          return;
+      }
+    };
+    if (!BWD || NORM) fits(t.x);
+    fits(t.y);
+    if (BWD) fits(t.dx);
+  }
+  if (!any || p.tokens == 0) return cudaSuccess;
+  const int mode = rope_mode(a.plan, vector);
+  if (a.type == RESS_BF16) return launch_rope_typed<bf16, NORM, BWD>(p, mode, ctas, st);
+  if (a.type == RESS_F16) return launch_rope_typed<f16, NORM, BWD>(p, mode, ctas, st);
+  return launch_rope_typed<float, NORM, BWD>(p, mode, ctas, st);
+}
+
+}  // namespace
+}  // namespace ress
