@@ -11,8 +11,8 @@
 // A lane holds 4 slots, each the two channels of a pair (or two channels without a pair), so that a
 // rotation needs no other lane, and a head has G lanes.  Where the plan's pairs are 4 and 4
 // neighbouring channels (kChunks) or 8 neighbours (kNeighbours) they are read and written as
-// vectors, else one by one (kGather).  A warp goes through rows of 32 / G heads, the next D rows on
-// their way.  An item is a token's rows of one tensor (or one of them, where tokens are few): a CTA
+// vectors, else one by one (kGather).  An item is one token and up to K rows of 32 / G of its heads
+// of one tensor, and a warp has the next item's elements on their way while it works on one.  A CTA
 // stays with Q or K (shares of the grid by their heads), and its lanes keep the norm's parameters
 // and their gradients' sums in registers.  The token's cosines and sines are formed once per item,
 // one pair per lane, and handed out through shared memory.  Sums are float32 in a fixed order; the
@@ -47,7 +47,6 @@ struct RopeParams {
   float* partial;
   float eps;
   int first_ctas;  // CTAs of t[0]; the others have t[1]
-  int item_rows;   // rows of an item
   int param_type;
   bool all;        // every channel has a pair
 };
@@ -143,7 +142,7 @@ struct Slots {
   }
 };
 
-template <typename T, int G, int MODE, bool NORM, bool BWD, int D>
+template <typename T, int G, int MODE, bool NORM, bool BWD, int K>
 __global__ void __launch_bounds__(kRopeThreads, NORM && BWD ? 4 : 5) k_rope(const __grid_constant__ RopeParams p) {
   constexpr int kHeads = 32 / G;              // heads of a warp's row
   constexpr int kPairs = G <= 8 ? 1 : G / 8;  // pairs per lane: 4 G pairs at most
@@ -151,23 +150,36 @@ __global__ void __launch_bounds__(kRopeThreads, NORM && BWD ? 4 : 5) k_rope(cons
   __shared__ __align__(16) float cosines[kRopeWarps][32 * kPairs], sines[kRopeWarps][32 * kPairs];
   const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
   const bool second = (int)blockIdx.x >= p.first_ctas;
-  const RopeTensor& t = p.t[second];
+  // (one field at a time: an index into the parameters would be looked up at each use)
+  RopeTensor t;
+  t.heads = second ? p.t[1].heads : p.t[0].heads;
+  t.weight = second ? p.t[1].weight : p.t[0].weight;
+  t.bias = second ? p.t[1].bias : p.t[0].bias;
+  t.x = second ? p.t[1].x : p.t[0].x;
+  t.y = second ? p.t[1].y : p.t[0].y;
+  t.out = second ? p.t[1].out : p.t[0].out;
+  t.x_token = second ? p.t[1].x_token : p.t[0].x_token;
+  t.x_head = second ? p.t[1].x_head : p.t[0].x_head;
+  t.y_token = second ? p.t[1].y_token : p.t[0].y_token;
+  t.y_head = second ? p.t[1].y_head : p.t[0].y_head;
+  t.out_token = second ? p.t[1].out_token : p.t[0].out_token;
+  t.out_head = second ? p.t[1].out_head : p.t[0].out_head;
   const int hd = p.plan.head_dim, heads = t.heads;
   const int group = lane / G, slot = lane % G * 4;
   const float inv = 1.f / (float)hd;
 
   int a[4], b[4];
-  Slots<T, MODE> at_slots;
+  Slots<T, MODE> slots;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    at_slots.in[j] = 2 * (slot + j) < hd;
+    slots.in[j] = 2 * (slot + j) < hd;
     slot_channels(p.plan, MODE, min(slot + j, hd / 2 - 1), a[j], b[j]);
   }
-  at_slots.a = a;
-  at_slots.b = b;
-  at_slots.any = at_slots.in[0];
-  at_slots.first = a[0];
-  at_slots.next = b[0];
+  slots.a = a;
+  slots.b = b;
+  slots.any = slots.in[0];
+  slots.first = a[0];
+  slots.next = b[0];
   const bool turns = slot < p.plan.n_pairs;  // kGather: slots turn one by one
   // The pairs whose angles this lane forms.
   uint64_t freq[kPairs];
@@ -190,7 +202,7 @@ __global__ void __launch_bounds__(kRopeThreads, NORM && BWD ? 4 : 5) k_rope(cons
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int j = 2 * q + e, c = s ? b[j] : a[j];
-        if (NORM && at_slots.in[j]) {
+        if (NORM && slots.in[j]) {
           v[0][e] = param_at(t.weight, p.param_type, c, 1.f);
           if (!BWD) v[1][e] = param_at(t.bias, p.param_type, c, 0.f);
         }
@@ -200,69 +212,52 @@ __global__ void __launch_bounds__(kRopeThreads, NORM && BWD ? 4 : 5) k_rope(cons
       dw[s][q] = db[s][q] = both(0.f);
     }
 
-  // Rows of the warp, item after item.
-  const int token_rows = (heads + kHeads - 1) / kHeads, chunks = (token_rows + p.item_rows - 1) / p.item_rows;
+  const int chunks = (heads + K * kHeads - 1) / (K * kHeads);  // items of a token
   const int64_t warps = (int64_t)(second ? gridDim.x - p.first_ctas : p.first_ctas) * kRopeWarps;
   const int64_t w0 = (int64_t)(blockIdx.x - (second ? p.first_ctas : 0)) * kRopeWarps + warp;
   const int64_t step = warps / chunks;
   const int step_rest = (int)(warps - step * chunks);
-  const int64_t x_row = t.x_head * kHeads, y_row = t.y_head * kHeads, out_row = t.out_head * kHeads;
   int64_t token = w0 / chunks;
   int chunk = (int)(w0 - token * chunks);
-  // the rows under way: of the item at (ahead, ahead_chunk), rows up to `end`
-  Vec<T, 8> queue_x[kReadX ? D : 1], queue_y[BWD ? D : 1];
-  int64_t ahead = token;
-  int ahead_chunk = chunk, row = 0, end = 0;
-  const T *px = nullptr, *py = nullptr;
-  auto open = [&]() {
-    row = ahead_chunk * p.item_rows;
-    end = ahead < p.tokens ? min(token_rows, row + p.item_rows) : INT32_MAX;  // no rows any more
-    const int h = row * kHeads + group;
-    if constexpr (kReadX) px = static_cast<const T*>(t.x) + ahead * t.x_token + h * t.x_head;
-    if constexpr (BWD) py = static_cast<const T*>(t.y) + ahead * t.y_token + h * t.y_head;
-  };
-  auto load = [&](int d) {
-    const bool live = end != INT32_MAX && row * kHeads + group < heads;
-    if constexpr (kReadX) {
-      queue_x[d] = at_slots.load(px, live);
-      px += x_row;
-    }
-    if constexpr (BWD) {
-      queue_y[d] = at_slots.load(py, live);
-      py += y_row;
-    }
-    if (++row == end) {
-      ahead += step;
-      ahead_chunk += step_rest;
-      if (ahead_chunk >= chunks) {
-        ahead_chunk -= chunks;
-        ++ahead;
-      }
-      open();
-    }
-  };
+  // the next item's rows and positions are on their way while this one is worked on
+  Vec<T, 8> next_x[kReadX ? K : 1], next_y[BWD ? K : 1];
   int32_t pos[kPairs];
-  auto load_pos = [&](int64_t at) {
+  auto load = [&]() {
+    const bool live = token < p.tokens;
+    const int h0 = chunk * K * kHeads + group;
+    const T *px = nullptr, *py = nullptr;
+    if constexpr (kReadX) px = static_cast<const T*>(t.x) + token * t.x_token + h0 * t.x_head;
+    if constexpr (BWD) py = static_cast<const T*>(t.y) + token * t.y_token + h0 * t.y_head;
 #pragma unroll
-    for (int q = 0; q < kPairs; ++q) pos[q] = at < p.tokens ? p.pos[at * p.plan.n_axes + axis[q]] : 0;
+    for (int k = 0; k < K; ++k) {
+      const bool row = live && h0 + k * kHeads < heads;
+      if constexpr (kReadX) next_x[k] = slots.load(px + k * kHeads * t.x_head, row);
+      if constexpr (BWD) next_y[k] = slots.load(py + k * kHeads * t.y_head, row);
+    }
+#pragma unroll
+    for (int q = 0; q < kPairs; ++q) pos[q] = live ? p.pos[token * p.plan.n_axes + axis[q]] : 0;
   };
-  load_pos(token);
-  open();
-#pragma unroll
-  for (int d = 0; d < D; ++d) load(d);
+  load();
 #pragma unroll 1
   while (token < p.tokens) {
-    // the item's angles; the next one's positions are on their way meanwhile
+    Vec<T, 8> x[kReadX ? K : 1], y[BWD ? K : 1];
     float2 cs[kPairs];
 #pragma unroll
-    for (int q = 0; q < kPairs; ++q) cs[q] = rope_cos_sin(pos[q], freq[q]);
-    int64_t next_token = token + step;
-    int next_chunk = chunk + step_rest;
-    if (next_chunk >= chunks) {
-      next_chunk -= chunks;
-      ++next_token;
+    for (int k = 0; k < K; ++k) {
+      if constexpr (kReadX) x[k] = next_x[k];
+      if constexpr (BWD) y[k] = next_y[k];
     }
-    load_pos(next_token);
+#pragma unroll
+    for (int q = 0; q < kPairs; ++q) cs[q] = rope_cos_sin(pos[q], freq[q]);
+    const int head0 = chunk * K * kHeads + group;
+    T* const out = static_cast<T*>(t.out) + token * t.out_token + head0 * t.out_head;
+    token += step;
+    chunk += step_rest;
+    if (chunk >= chunks) {
+      chunk -= chunks;
+      ++token;
+    }
+    load();
     __syncwarp();  // the last item's are read
 #pragma unroll
     for (int q = 0; q < kPairs; ++q) {
@@ -274,30 +269,17 @@ __global__ void __launch_bounds__(kRopeThreads, NORM && BWD ? 4 : 5) k_rope(cons
     const float4 s4 = *reinterpret_cast<const float4*>(&sines[warp][slot]);
     const F2 co[2] = {pack2(c4.x, c4.y), pack2(c4.z, c4.w)}, si[2] = {pack2(s4.x, s4.y), pack2(s4.z, s4.w)};
     const F2 neg[2] = {pack2(-s4.x, -s4.y), pack2(-s4.z, -s4.w)};
-    int head = chunk * p.item_rows * kHeads + group;
-    const int last = min(heads, (chunk * p.item_rows + p.item_rows) * kHeads);
-    T* out = static_cast<T*>(t.out) + token * t.out_token + head * t.out_head;
-#pragma unroll 1
-    for (; head - group < last; head += kHeads, out += out_row) {
-      Vec<T, 8> x, y;
-      if constexpr (kReadX) {
-        x = queue_x[0];
 #pragma unroll
-        for (int d = 1; d < D; ++d) queue_x[d - 1] = queue_x[d];
-      }
-      if constexpr (BWD) {
-        y = queue_y[0];
-#pragma unroll
-        for (int d = 1; d < D; ++d) queue_y[d - 1] = queue_y[d];
-      }
-      load(D - 1);
+    for (int k = 0; k < K; ++k) {
+      const int head = head0 + k * kHeads;
+      if (head - group >= heads) break;  // no head of this row
       F2 h[2][2], u[2][2];
       float rstd = 1.f;
       if constexpr (NORM) {
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int q = 0; q < 2; ++q) h[s][q] = Slots<T, MODE>::get(x, s, q);
+          for (int q = 0; q < 2; ++q) h[s][q] = Slots<T, MODE>::get(x[k], s, q);
         // a lane's sum is scaled before the lanes' meet: the sum may overflow where its average does not
         const F2 m = both(-segment_sum<G>(sum2(add2(add2(h[0][0], h[0][1]), add2(h[1][0], h[1][1]))) * inv));
         F2 sq = both(0.f);
@@ -309,11 +291,11 @@ __global__ void __launch_bounds__(kRopeThreads, NORM && BWD ? 4 : 5) k_rope(cons
             if constexpr (MODE == kGather) {  // slots that do not exist
               float e0, e1;
               unpack2(h[s][q], e0, e1);
-              h[s][q] = pack2(at_slots.in[2 * q] ? e0 : 0.f, at_slots.in[2 * q + 1] ? e1 : 0.f);
+              h[s][q] = pack2(slots.in[2 * q] ? e0 : 0.f, slots.in[2 * q + 1] ? e1 : 0.f);
             }
             sq = fma2(h[s][q], h[s][q], sq);
           }
-        rstd = rsqrtf(segment_sum<G>(at_slots.any ? sum2(sq) * inv : 0.f) + p.eps);
+        rstd = rsqrtf(segment_sum<G>(slots.any ? sum2(sq) * inv : 0.f) + p.eps);
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -326,7 +308,7 @@ __global__ void __launch_bounds__(kRopeThreads, NORM && BWD ? 4 : 5) k_rope(cons
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int q = 0; q < 2; ++q) u[s][q] = Slots<T, MODE>::get(BWD ? y : x, s, q);
+          for (int q = 0; q < 2; ++q) u[s][q] = Slots<T, MODE>::get(BWD ? y[k] : x[k], s, q);
       }
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
@@ -370,10 +352,8 @@ __global__ void __launch_bounds__(kRopeThreads, NORM && BWD ? 4 : 5) k_rope(cons
 #pragma unroll
           for (int q = 0; q < 2; ++q) u[s][q] = mul2(fma2(h[s][q], agh, add2(u[s][q], ag)), both(rstd));
       }
-      at_slots.store(out, u, head < heads);
+      slots.store(out + k * kHeads * t.out_head, u, head < heads);
     }
-    token = next_token;
-    chunk = next_chunk;
   }
   stream_release();
   if constexpr (NORM && BWD) {
@@ -393,7 +373,7 @@ __global__ void __launch_bounds__(kRopeThreads, NORM && BWD ? 4 : 5) k_rope(cons
           for (int e = 0; e < 2; ++e) {
 #pragma unroll
             for (int o = G; o < 32; o <<= 1) v[k][e] += __shfl_xor_sync(0xffffffffu, v[k][e], o);
-            if (lane < G && at_slots.in[2 * q + e]) part[warp][k][s ? b[2 * q + e] : a[2 * q + e]] = v[k][e];
+            if (lane < G && slots.in[2 * q + e]) part[warp][k][s ? b[2 * q + e] : a[2 * q + e]] = v[k][e];
           }
       }
     __syncthreads();
@@ -410,18 +390,17 @@ __global__ void __launch_bounds__(kRopeThreads, NORM && BWD ? 4 : 5) k_rope(cons
 // CTAs of the two tensors of a launch; the forward's launch has no sums to fold.
 template <typename T, int G, int MODE, bool NORM, bool BWD>
 cudaError_t launch_rope_as(RopeParams& p, int (&ctas)[2], cudaStream_t st) {
-  constexpr int D = 2;
-  auto kern = k_rope<T, G, MODE, NORM, BWD, D>;
+  // rows of an item: what fits in the registers twice
+  constexpr int K = sizeof(T) == 2 ? (BWD && NORM ? 2 : 4) : (BWD && NORM ? 1 : 2);
+  auto kern = k_rope<T, G, MODE, NORM, BWD, K>;
   int resident = 1;
   if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kern, kRopeThreads, 0) != cudaSuccess || resident < 1)
     resident = 1;
   const int64_t fit = min((int64_t)resident * sm_count(), (int64_t)kRopeParts - 1);
-  // Items: whole tokens, which form their angles once, if there is work for every warp; else single rows.
-  p.item_rows = 2 * p.tokens >= fit * kRopeWarps ? INT32_MAX / 64 : 1;
   int64_t need[2], all = 0;  // CTAs at one item per warp
   for (int i = 0; i < 2; ++i) {
-    const int rows = (p.t[i].heads + 32 / G - 1) / (32 / G);
-    need[i] = (p.tokens * (p.item_rows == 1 ? rows : min(rows, 1)) + kRopeWarps - 1) / kRopeWarps;
+    const int chunks = (p.t[i].heads + K * (32 / G) - 1) / (K * (32 / G));
+    need[i] = (p.tokens * chunks + kRopeWarps - 1) / kRopeWarps;
     all += need[i];
   }
   // shares of what fits at once by the tensors' heads, with the same number of items for each warp
