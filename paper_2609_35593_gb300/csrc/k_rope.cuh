@@ -48,7 +48,8 @@ struct RopeParams {
   float eps;
   int first_ctas;  // CTAs of t[0]; the others have t[1]
   int param_type;
-  bool all;        // every channel has a pair
+  bool whole_tokens;  // a warp takes all of a token's items
+  bool all;           // every channel has a pair
 };
 
 // The channels of a slot.  Slots past the pairs have channels without one, if any are left: two
@@ -143,7 +144,7 @@ struct Slots {
 };
 
 template <typename T, int G, int MODE, bool NORM, bool BWD, int K>
-__global__ void __launch_bounds__(kRopeThreads, NORM && BWD ? 4 : 5) k_rope(const __grid_constant__ RopeParams p) {
+__global__ void __launch_bounds__(kRopeThreads, !NORM ? 6 : BWD ? 3 : 4) k_rope(const __grid_constant__ RopeParams p) {
   constexpr int kHeads = 32 / G;              // heads of a warp's row
   constexpr int kPairs = G <= 8 ? 1 : G / 8;  // pairs per lane: 4 G pairs at most
   constexpr bool kReadX = !BWD || NORM;
@@ -212,13 +213,15 @@ __global__ void __launch_bounds__(kRopeThreads, NORM && BWD ? 4 : 5) k_rope(cons
       dw[s][q] = db[s][q] = both(0.f);
     }
 
+  // A token's items one after the other, so that they share its angles, or (few tokens) each by itself.
   const int chunks = (heads + K * kHeads - 1) / (K * kHeads);  // items of a token
+  const int span = p.whole_tokens ? chunks : 1, spans = chunks / span;
   const int64_t warps = (int64_t)(second ? gridDim.x - p.first_ctas : p.first_ctas) * kRopeWarps;
   const int64_t w0 = (int64_t)(blockIdx.x - (second ? p.first_ctas : 0)) * kRopeWarps + warp;
-  const int64_t step = warps / chunks;
-  const int step_rest = (int)(warps - step * chunks);
-  int64_t token = w0 / chunks;
-  int chunk = (int)(w0 - token * chunks);
+  const int64_t step = warps / spans;
+  const int step_rest = (int)(warps - step * spans);
+  int64_t token = w0 / spans;
+  int chunk = (int)(w0 - token * spans) * span, left = span;  // left: items of the span from this one on
   // the next item's rows and positions are on their way while this one is worked on
   Vec<T, 8> next_x[kReadX ? K : 1], next_y[BWD ? K : 1];
   int32_t pos[kPairs];
@@ -247,24 +250,30 @@ __global__ void __launch_bounds__(kRopeThreads, NORM && BWD ? 4 : 5) k_rope(cons
       if constexpr (kReadX) x[k] = next_x[k];
       if constexpr (BWD) y[k] = next_y[k];
     }
+    if (left == span) {  // the token's angles
 #pragma unroll
-    for (int q = 0; q < kPairs; ++q) cs[q] = rope_cos_sin(pos[q], freq[q]);
+      for (int q = 0; q < kPairs; ++q) cs[q] = rope_cos_sin(pos[q], freq[q]);
+      __syncwarp();  // the last token's are read
+#pragma unroll
+      for (int q = 0; q < kPairs; ++q) {
+        cosines[warp][lane + 32 * q] = cs[q].x;
+        sines[warp][lane + 32 * q] = BWD ? -cs[q].y : cs[q].y;
+      }
+      __syncwarp();
+    }
     const int head0 = chunk * K * kHeads + group;
     T* const out = static_cast<T*>(t.out) + token * t.out_token + head0 * t.out_head;
-    token += step;
-    chunk += step_rest;
-    if (chunk >= chunks) {
-      chunk -= chunks;
-      ++token;
+    ++chunk;
+    if (--left == 0) {
+      left = span;
+      chunk += step_rest * span - span;
+      token += step;
+      if (chunk >= chunks) {
+        chunk -= chunks;
+        ++token;
+      }
     }
     load();
-    __syncwarp();  // the last item's are read
-#pragma unroll
-    for (int q = 0; q < kPairs; ++q) {
-      cosines[warp][lane + 32 * q] = cs[q].x;
-      sines[warp][lane + 32 * q] = BWD ? -cs[q].y : cs[q].y;
-    }
-    __syncwarp();
     const float4 c4 = *reinterpret_cast<const float4*>(&cosines[warp][slot]);
     const float4 s4 = *reinterpret_cast<const float4*>(&sines[warp][slot]);
     const F2 co[2] = {pack2(c4.x, c4.y), pack2(c4.z, c4.w)}, si[2] = {pack2(s4.x, s4.y), pack2(s4.z, s4.w)};
@@ -390,17 +399,20 @@ __global__ void __launch_bounds__(kRopeThreads, NORM && BWD ? 4 : 5) k_rope(cons
 // CTAs of the two tensors of a launch; the forward's launch has no sums to fold.
 template <typename T, int G, int MODE, bool NORM, bool BWD>
 cudaError_t launch_rope_as(RopeParams& p, int (&ctas)[2], cudaStream_t st) {
-  // rows of an item: what fits in the registers twice
-  constexpr int K = sizeof(T) == 2 ? (BWD && NORM ? 2 : 4) : (BWD && NORM ? 1 : 2);
+  // Rows of an item, their elements in registers twice (43,968 tokens, 16 + 16 heads of 64, bf16, with a
+  // norm: 66 us with K = 4, 73 with 2; without one, 20,011 tokens, 12 + 4 heads: 22 and 20.5; gradient with
+  // a norm, 10,992 tokens: 36 with K = 2 or 4, 45 with 1).
+  constexpr int K = sizeof(T) == 2 ? (NORM && !BWD ? 4 : 2) : (NORM && BWD ? 1 : 2);
   auto kern = k_rope<T, G, MODE, NORM, BWD, K>;
   int resident = 1;
   if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kern, kRopeThreads, 0) != cudaSuccess || resident < 1)
     resident = 1;
   const int64_t fit = min((int64_t)resident * sm_count(), (int64_t)kRopeParts - 1);
-  int64_t need[2], all = 0;  // CTAs at one item per warp
+  p.whole_tokens = p.tokens * ((p.t[0].heads > 0) + (p.t[1].heads > 0)) >= fit * kRopeWarps;
+  int64_t need[2], all = 0;  // CTAs at one visit per warp
   for (int i = 0; i < 2; ++i) {
     const int chunks = (p.t[i].heads + K * (32 / G) - 1) / (K * (32 / G));
-    need[i] = (p.tokens * chunks + kRopeWarps - 1) / kRopeWarps;
+    need[i] = (p.tokens * (p.whole_tokens ? min(chunks, 1) : chunks) + kRopeWarps - 1) / kRopeWarps;
     all += need[i];
   }
   // shares of what fits at once by the tensors' heads, with the same number of items for each warp
