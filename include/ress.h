@@ -402,7 +402,7 @@ int ress_rope_bwd(const ress_rope_plan* plan, int64_t n_tokens, const int32_t* p
  * K before the result is rounded to bf16.  x: device bf16 [N, d_model] (the norm's output); W_q,
  * W_k, W_v: device bf16 [H*64, d_model] (Linear weight, out x in; rows of one stacked weight
  * will do); b_q, b_k, b_v: device bf16 [H*64] or NULL; Q, K, V: device bf16 [N, H, 64], as
- * ress_forward takes them.  plan (head_dim 64) and pos as in ress_rope, both NULL for no rotation.
+ * ress_forward takes them (all of these 16-byte aligned).  plan (head_dim 64) and pos as in ress_rope, both NULL for no rotation.
  * q_norm, k_norm: NULL or not enabled for none.  fp32 accumulation on the tensor cores
  * (tcgen05).  d_model must be a multiple of 64.  Uses the workspace's status word only. */
 int ress_qkv_proj(const ress_dims* dims, const uint16_t* x, const uint16_t* W_q,

@@ -12,10 +12,15 @@
 //   warp 0     TMA of its half of the x and W slices;
 //   warp 1     TMEM owner; in the rank-0 CTA one elected lane issues the pair's MMAs;
 //   warps 2-9  epilogue in two groups of four warps that take the tile's heads in turn, one thread
-//              per token: a head's 64 channels are 64 columns of the thread's TMEM lane, so the norm's
-//              two sums need no other thread, and the two channels of a pair, wherever the plan has
-//              them, are columns of the same lane, read 8 at a time.  The cosines and sines of the
-//              CTA's 128 tokens are formed in shared memory while the tile's MMAs run.
+//              per token: a head's 64 channels are 64 columns of the thread's TMEM lane, all of them in
+//              its registers, so that neither the norm's sums nor the rotation need another thread.
+//              Plans that pair channel c with c xor h and turn all of them (h = 1, 16, 32: neighbours,
+//              two sections of 32, halves) are unrolled; any other plan's pairs are read from TMEM
+//              once more, one by one, over the head without rotation.  The cosines and sines of the
+//              CTA's 128 tokens are formed in shared memory while the tile's MMAs run.  The epilogue
+//              has to stay below the MMAs' 8,270 cycles per tile (D = 1024): read and worked on 8
+//              channels at a time, with every parameter looked up on its own, it took 19,000 (243 us
+//              for 43,968 tokens, 16 heads, D = 1024).
 // Waits are bounded as in k_oproj.cu.
 
 #include <cudaTypedefs.h>
@@ -24,6 +29,7 @@
 
 namespace ress {
 using namespace ptx;
+using rows::F2;
 
 PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder();
 
@@ -42,25 +48,26 @@ constexpr uint64_t kQWaitNs = 2000000000ull;
 constexpr uint64_t kQDrainNs = 200000000ull;
 
 constexpr uint32_t kQOffOut = kQStages * kQStage;          // two boxes per epilogue group
-constexpr uint32_t kQOffTurn = kQOffOut + 4 * kQBox;       // float2 [32 pairs][128 tokens]
+constexpr uint32_t kQOffTurn = kQOffOut + 4 * kQBox;       // float4 [16][128 tokens]: of pairs 2q and
+                                                           // 2q + 1 both cosines, both sines
 constexpr uint32_t kQOffCtl = kQOffTurn + 32 * kQM * 8;
 
 struct QCtl {
-  uint16_t bias[kQHeads * 64];
-  float weight[2][64], shift[2][64];  // the norms of Q and K
+  __align__(16) float gain[2][64], shift[2][64];  // the norms of Q and K
   uint64_t full[kQStages], empty[kQStages], acc_full[2], acc_empty[2];
   uint32_t tmem_base;
   int abort;
 };
 
-// How the epilogue walks a head's channels.
-enum { kPlain = 0, kBlocks = 1, kNeighbours = 2, kSingle = 3 };
+// Which of a plan's rotations are unrolled: by the distance h of pairs (c, c xor h); the others pair
+// by pair.
+enum { kNoTurn = 0, kByPairs = -1 };
 
 struct QParams {
   int N, K, H, mtiles;
   int tiles_of;            // tiles of one of Q, K, V: ceil(H / 4)
   int whole, parts;        // the first `whole` tiles run whole, the others as `parts` units each
-  int walk, pairs, axes;
+  int turn, pairs, axes;   // turn: h, kNoTurn or kByPairs
   uint8_t lo[32], hi[32];  // channels of each pair
   uint8_t axis[32];
   uint64_t turns[32];
@@ -107,32 +114,15 @@ __device__ __forceinline__ void q_group_sync(int group) {
   asm volatile("barrier.cta.sync %0, 128;" ::"r"(3 + group) : "memory");
 }
 
-// 8 (or 1) columns at each of two places, or 8 at one, of this warp's lanes, waited for in the same asm
-// block so that no register is read before it is valid.
-#define RESS_TMEM_LD8_TWICE(at0, a, at1, b)                                                          \
-  asm volatile(                                                                                      \
-      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%16];\n\t"                  \
-      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%8,%9,%10,%11,%12,%13,%14,%15}, [%17];\n\t"            \
-      "tcgen05.wait::ld.sync.aligned;"                                                               \
-      : "=&r"(a[0]), "=&r"(a[1]), "=&r"(a[2]), "=&r"(a[3]), "=&r"(a[4]), "=&r"(a[5]), "=&r"(a[6]),   \
-        "=&r"(a[7]), "=&r"(b[0]), "=&r"(b[1]), "=&r"(b[2]), "=&r"(b[3]), "=&r"(b[4]), "=&r"(b[5]),   \
-        "=&r"(b[6]), "=&r"(b[7])                                                                     \
-      : "r"(at0), "r"(at1)                                                                           \
-      : "memory")
-#define RESS_TMEM_LD8(at, a)                                                                         \
-  asm volatile(                                                                                      \
-      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n\t"                   \
-      "tcgen05.wait::ld.sync.aligned;"                                                               \
-      : "=r"(a[0]), "=r"(a[1]), "=r"(a[2]), "=r"(a[3]), "=r"(a[4]), "=r"(a[5]), "=r"(a[6]), "=r"(a[7]) \
-      : "r"(at)                                                                                      \
-      : "memory")
-#define RESS_TMEM_LD1_TWICE(at0, a, at1, b)                                                          \
-  asm volatile(                                                                                      \
-      "tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%2];\n\t"                                        \
-      "tcgen05.ld.sync.aligned.32x32b.x1.b32 {%1}, [%3];\n\t"                                        \
-      "tcgen05.wait::ld.sync.aligned;"                                                               \
-      : "=&r"(a), "=&r"(b)                                                                           \
-      : "r"(at0), "r"(at1)                                                                           \
+// One column at each of two places of this warp's lanes, waited for in the same asm block so that no
+// register is read before it is valid.
+#define RESS_TMEM_LD1_TWICE(at0, a, at1, b)                 \
+  asm volatile(                                             \
+      "tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%2];\n\t" \
+      "tcgen05.ld.sync.aligned.32x32b.x1.b32 {%1}, [%3];\n\t" \
+      "tcgen05.wait::ld.sync.aligned;"                      \
+      : "=&r"(a), "=&r"(b)                                  \
+      : "r"(at0), "r"(at1)                                  \
       : "memory")
 
 // One unit of work of a pair: token stripe mt, `heads` heads from `head` on of Q, K or V (which).
@@ -159,6 +149,97 @@ __device__ __forceinline__ QUnit q_unit(const QParams& p, int k) {
   t.head = kQHeads * (j % p.tiles_of) + heads * part;
   t.heads = max(0, min(heads, p.H - t.head));  // a part past the last head has none
   return t;
+}
+
+// One head of one token: 64 columns of this thread's TMEM lane, to its row of an output box.
+struct QHead {
+  const uint16_t* bias;         // of the head, or NULL
+  const float *gain, *shift;    // of the norm, or NULL
+  float eps;
+  const float4* turn;           // the token's entry of the cosines and sines
+};
+
+// The accumulators plus the bias; with a norm, their mean and 1 / standard deviation (else 0 and 1).
+__device__ __forceinline__ void q_add_bias(const uint16_t* bias, F2 (&u)[32]) {
+  if (!bias) return;
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    const uint4 v = reinterpret_cast<const uint4*>(bias)[c];
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) u[4 * c + j] = rows::add2(u[4 * c + j], rows::pack2(bf16_lo(w[j]), bf16_hi(w[j])));
+  }
+}
+
+template <int H>
+__device__ __forceinline__ void q_head(uint32_t acc, const QHead& a, uint8_t* row, int r, float& mean, float& rstd) {
+  using rows::add2;
+  using rows::both;
+  using rows::fma2;
+  using rows::mul2;
+  using rows::pack2;
+  F2 u[32];  // channels 2j and 2j + 1
+  {
+    uint32_t v[64];
+    __syncwarp();
+    RESS_TMEM_LD64(acc, v);
+#pragma unroll
+    for (int j = 0; j < 32; ++j) u[j] = pack2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
+  }
+  q_add_bias(a.bias, u);
+  mean = 0.f;
+  rstd = 1.f;
+  if (a.gain) {
+    F2 s[2] = {both(0.f), both(0.f)};
+#pragma unroll
+    for (int j = 0; j < 32; ++j) s[j & 1] = add2(s[j & 1], u[j]);
+    mean = rows::sum2(add2(s[0], s[1])) * (1.f / 64.f);
+    const F2 m = both(-mean);
+    s[0] = s[1] = both(0.f);
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+      u[j] = add2(u[j], m);
+      s[j & 1] = fma2(u[j], u[j], s[j & 1]);
+    }
+    rstd = rsqrtf(fmaf(rows::sum2(add2(s[0], s[1])), 1.f / 64.f, a.eps));
+#pragma unroll
+    for (int c = 0; c < 16; ++c) {
+      const float4 g = reinterpret_cast<const float4*>(a.gain)[c], b = reinterpret_cast<const float4*>(a.shift)[c];
+      u[2 * c] = fma2(mul2(u[2 * c], both(rstd)), pack2(g.x, g.y), pack2(b.x, b.y));
+      u[2 * c + 1] = fma2(mul2(u[2 * c + 1], both(rstd)), pack2(g.z, g.w), pack2(b.z, b.w));
+    }
+  }
+  if constexpr (H > 0) {
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {  // pairs 2q and 2q + 1
+      const float4 t = a.turn[q * kQM];
+      if constexpr (H == 1) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float c = e ? t.y : t.x, s = e ? t.w : t.z;
+          float x, y;
+          rows::unpack2(u[2 * q + e], x, y);
+          u[2 * q + e] = pack2(fmaf(x, c, -y * s), fmaf(y, c, x * s));
+        }
+      } else {
+        const int lo = (2 * q / H * 2 * H + 2 * q % H) / 2, hi = lo + H / 2;
+        const F2 c = pack2(t.x, t.y), s = pack2(t.z, t.w), x = u[lo], y = u[hi];
+        u[lo] = fma2(x, c, mul2(y, pack2(-t.z, -t.w)));
+        u[hi] = fma2(y, c, mul2(x, s));
+      }
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float x, y;
+      rows::unpack2(u[4 * c + j], x, y);
+      w[j] = cvt_bf16x2(x, y);
+    }
+    *reinterpret_cast<uint4*>(row + ((c ^ (r & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
 }
 
 __global__ void __launch_bounds__(kQThreads, 1)
@@ -298,12 +379,11 @@ __global__ void __launch_bounds__(kQThreads, 1)
     const int et = (int)threadIdx.x - 64;
     const bool leader = (warp - 2) % 4 == 0 && lane == 0;
     uint8_t* out = base + kQOffOut + 2 * group * kQBox;
-    float2* turn = reinterpret_cast<float2*>(base + kQOffTurn);
+    float4* turn = reinterpret_cast<float4*>(base + kQOffTurn);
     if (et < 64) {
       for (int i = 0; i < 2; ++i) {
-        const ress_head_norm& m = p.norm[i];
-        C.weight[i][et] = m.enabled ? rows::param_at(m.weight, p.param_type, et, 1.f) : 1.f;
-        C.shift[i][et] = m.enabled ? rows::param_at(m.bias, p.param_type, et, 0.f) : 0.f;
+        C.gain[i][et] = rows::param_at(p.norm[i].weight, p.param_type, et, 1.f);
+        C.shift[i][et] = rows::param_at(p.norm[i].bias, p.param_type, et, 0.f);
       }
     }
     int n = 0, boxes = 0, table = -1;  // units done; boxes this group has stored; the table's stripe
@@ -312,16 +392,20 @@ __global__ void __launch_bounds__(kQThreads, 1)
       if (t.heads == 0) continue;
       const int b = n & 1, use = n >> 1;
       ++n;
-      const int row0 = kQM * (2 * t.mt + rank), which = t.which;
-      // the unit's bias and the stripe's cosines and sines, while its MMAs run
-      q_epi_sync();  // nobody reads the last unit's any more
-      if (et < 64 * t.heads)
-        C.bias[et] = p.bias[which] ? p.bias[which][64 * t.head + et] : (uint16_t)0;
-      if (which < 2 && p.walk != kPlain && table != t.mt) {
+      const int row0 = kQM * (2 * t.mt + rank), which = t.which, mode = which < 2 ? p.turn : kNoTurn;
+      if (mode != kNoTurn && table != t.mt) {  // the stripe's cosines and sines, while the unit's MMAs run
         table = t.mt;
+        q_epi_sync();  // nobody reads the last stripe's any more
         const int64_t token = min(row0 + r, p.N - 1);
-        for (int q = group; q < p.pairs; q += 2)
-          turn[q * kQM + r] = rows::rope_cos_sin(p.pos[token * p.axes + p.axis[q]], p.turns[q]);
+        for (int q = group; 2 * q < p.pairs; q += 2) {
+          float2 cs[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int pair = min(2 * q + e, p.pairs - 1);
+            cs[e] = rows::rope_cos_sin(p.pos[token * p.axes + p.axis[pair]], p.turns[pair]);
+          }
+          turn[q * kQM + r] = make_float4(cs[0].x, cs[1].x, cs[0].y, cs[1].y);
+        }
       }
       const bool ok = q_wait(&C.acc_full[b], use & 1, abort);
       if (!q_epi_sync_and(ok)) {  // all leave together
@@ -329,114 +413,49 @@ __global__ void __launch_bounds__(kQThreads, 1)
         break;
       }
       tc_fence_after();
+      QHead a;
+      const bool norm = which < 2 && p.norm[which & 1].enabled;
+      a.gain = norm ? C.gain[which & 1] : nullptr;
+      a.shift = C.shift[which & 1];
+      a.eps = p.eps;
+      a.turn = turn + r;
       for (int h = group; h < t.heads; h += 2) {
         const uint32_t acc = tmem + ((uint32_t)(32 * quarter) << 16) + 256u * b + 64 * h;
-        const uint16_t* bias_bits = C.bias + 64 * h;
-        auto bias = [&](int c) { return __uint_as_float((uint32_t)bias_bits[c] << 16); };
-        const int side = which & 1;
-        float mean = 0.f, rstd = 1.f;
-        if (which < 2 && p.norm[side].enabled) {
-          uint32_t v[64];
-          __syncwarp();
-          RESS_TMEM_LD64(acc, v);
-          float sum = 0.f;
-#pragma unroll
-          for (int c = 0; c < 64; ++c) {
-            const float u = __uint_as_float(v[c]) + bias(c);
-            v[c] = __float_as_uint(u);
-            sum += u;
-          }
-          mean = sum * (1.f / 64.f);
-          float sq = 0.f;
-#pragma unroll
-          for (int c = 0; c < 64; ++c) {
-            const float u = __uint_as_float(v[c]) - mean;
-            sq = fmaf(u, u, sq);
-          }
-          rstd = rsqrtf(fmaf(sq, 1.f / 64.f, p.eps));
-        }
+        a.bias = p.bias[which] ? p.bias[which] + 64 * (t.head + h) : nullptr;
         // the box is free when the store before the last has read it
         uint8_t* box = out + (boxes & 1) * kQBox;
         ++boxes;
         if (leader) bulk_wait_read_but1();
         q_group_sync(group);
         uint8_t* row = box + r * 128;
-        const float* gain = C.weight[side];
-        const float* shift = C.shift[side];
-        // a channel's value from its accumulator: bias, norm
-        auto value = [&](uint32_t bits, int c) {
-          const float u = __uint_as_float(bits) + bias(c);
-          return which < 2 ? fmaf((u - mean) * rstd, gain[c], shift[c]) : u;
-        };
-        auto chunk = [&](int c) { return reinterpret_cast<uint4*>(row + (((c >> 3) ^ (r & 7)) << 4)); };
-        const int walk = which < 2 ? p.walk : kPlain;
-        int done = 0;  // channels below this one are written
-        if (walk == kBlocks) {
-#pragma unroll 1
-          for (int q = 0; q < p.pairs; q += 8) {
-            const int lo = p.lo[q], hi = p.hi[q];
-            uint32_t a[8], c[8];
-            float ya[8], yc[8];
-            __syncwarp();
-            RESS_TMEM_LD8_TWICE(acc + lo, a, acc + hi, c);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const float2 cs = turn[(q + j) * kQM + r];
-              const float ua = value(a[j], lo + j), uc = value(c[j], hi + j);
-              ya[j] = fmaf(ua, cs.x, -uc * cs.y);
-              yc[j] = fmaf(uc, cs.x, ua * cs.y);
-            }
-            *chunk(lo) = make_uint4(cvt_bf16x2(ya[0], ya[1]), cvt_bf16x2(ya[2], ya[3]),
-                                    cvt_bf16x2(ya[4], ya[5]), cvt_bf16x2(ya[6], ya[7]));
-            *chunk(hi) = make_uint4(cvt_bf16x2(yc[0], yc[1]), cvt_bf16x2(yc[2], yc[3]),
-                                    cvt_bf16x2(yc[4], yc[5]), cvt_bf16x2(yc[6], yc[7]));
-          }
-          done = 2 * p.pairs;
-        } else if (walk == kNeighbours) {
-          // 8 channels at a time; a last block may have fewer than 4 pairs
-#pragma unroll 1
-          for (int q = 0; q < p.pairs; q += 4) {
-            uint32_t a[8];
-            float y[8];
-            __syncwarp();
-            RESS_TMEM_LD8(acc + 2 * q, a);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float u = value(a[2 * j], 2 * (q + j)), v = value(a[2 * j + 1], 2 * (q + j) + 1);
-              const float2 cs = q + j < p.pairs ? turn[(q + j) * kQM + r] : make_float2(1.f, 0.f);
-              y[2 * j] = q + j < p.pairs ? fmaf(u, cs.x, -v * cs.y) : u;
-              y[2 * j + 1] = q + j < p.pairs ? fmaf(v, cs.x, u * cs.y) : v;
-            }
-            *chunk(2 * q) = make_uint4(cvt_bf16x2(y[0], y[1]), cvt_bf16x2(y[2], y[3]), cvt_bf16x2(y[4], y[5]),
-                                       cvt_bf16x2(y[6], y[7]));
-          }
-          done = (2 * p.pairs + 7) & ~7;
-        } else if (walk == kSingle) {
-          // the whole head without rotation first (below), then the pairs one by one over it
-          done = 0;
-        }
-#pragma unroll 1
-        for (; done < 64; done += 8) {
-          uint32_t a[8];
-          float y[8];
-          __syncwarp();
-          RESS_TMEM_LD8(acc + done, a);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) y[j] = value(a[j], done + j);
-          *chunk(done) = make_uint4(cvt_bf16x2(y[0], y[1]), cvt_bf16x2(y[2], y[3]), cvt_bf16x2(y[4], y[5]),
-                                    cvt_bf16x2(y[6], y[7]));
-        }
-        if (walk == kSingle) {
+        float mean, rstd;
+        if (mode == 16)
+          q_head<16>(acc, a, row, r, mean, rstd);
+        else if (mode == 32)
+          q_head<32>(acc, a, row, r, mean, rstd);
+        else if (mode == 1)
+          q_head<1>(acc, a, row, r, mean, rstd);
+        else
+          q_head<0>(acc, a, row, r, mean, rstd);
+        if (mode == kByPairs) {
 #pragma unroll 1
           for (int q = 0; q < p.pairs; ++q) {
-            const int lo = p.lo[q], hi = p.hi[q];
-            uint32_t a, c;
+            const int c[2] = {p.lo[q], p.hi[q]};
+            uint32_t v[2];
             __syncwarp();
-            RESS_TMEM_LD1_TWICE(acc + lo, a, acc + hi, c);
-            const float2 cs = turn[q * kQM + r];
-            const float ua = value(a, lo), uc = value(c, hi);
-            reinterpret_cast<uint16_t*>(chunk(lo))[lo & 7] = cvt_bf16(fmaf(ua, cs.x, -uc * cs.y));
-            reinterpret_cast<uint16_t*>(chunk(hi))[hi & 7] = cvt_bf16(fmaf(uc, cs.x, ua * cs.y));
+            RESS_TMEM_LD1_TWICE(acc + c[0], v[0], acc + c[1], v[1]);
+            const float4 t4 = a.turn[q / 2 * kQM];
+            const float cs = q % 2 ? t4.y : t4.x, sn = q % 2 ? t4.w : t4.z;
+            float u[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              u[e] = __uint_as_float(v[e]) + (a.bias ? __uint_as_float((uint32_t)a.bias[c[e]] << 16) : 0.f);
+              if (norm) u[e] = fmaf((u[e] - mean) * rstd, a.gain[c[e]], a.shift[c[e]]);
+            }
+            const float y[2] = {fmaf(u[0], cs, -u[1] * sn), fmaf(u[1], cs, u[0] * sn)};
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+              reinterpret_cast<uint16_t*>(row + (((c[e] >> 3) ^ (r & 7)) << 4))[c[e] & 7] = cvt_bf16(y[e]);
           }
         }
         fence_proxy_async_smem();
@@ -491,24 +510,30 @@ cudaError_t launch_qkv_proj(const QkvArgs& a, cudaStream_t st) {
   p.H = a.H;
   p.mtiles = (a.N + 2 * kQM - 1) / (2 * kQM);
   p.tiles_of = (a.H + kQHeads - 1) / kQHeads;
-  p.walk = kPlain;
+  p.turn = kNoTurn;
   if (a.rotate) {
     const ress_rope_plan& plan = a.plan;
     p.pairs = plan.n_pairs;
     p.axes = plan.n_axes;
-    bool blocks = plan.layout != RESS_ROPE_INTERLEAVED;  // whole blocks of 8 pairs
-    for (int c = 0; c < 2 * plan.n_pairs; ++c) {
-      const rows::RopeChannel r = rows::rope_channel(plan, c);
-      (r.second ? p.hi : p.lo)[r.pair] = (uint8_t)c;
+    int first = 0, k = 0;  // of the axis: its first channel, its first pair
+    for (int t = 0; t < plan.n_axes; ++t) {
+      const int half = plan.axis_dims[t] / 2;
+      for (int i = 0; i < half; ++i, ++k) {
+        p.axis[k] = (uint8_t)t;
+        p.turns[k] = plan.turns[k];
+        p.lo[k] = (uint8_t)(plan.layout == RESS_ROPE_SECTIONS ? first + i : plan.layout == RESS_ROPE_HALVES ? k : 2 * k);
+        p.hi[k] = (uint8_t)(p.lo[k] + (plan.layout == RESS_ROPE_SECTIONS ? half
+                                       : plan.layout == RESS_ROPE_HALVES ? plan.n_pairs : 1));
+      }
+      first += 2 * half;
     }
-    for (int q = 0; q < plan.n_pairs; ++q) {
-      p.axis[q] = (uint8_t)rows::rope_axis(plan, q);
-      p.turns[q] = plan.turns[q];
+    // all channels turn, pair k at distance h where an unrolled rotation has it
+    p.turn = kByPairs;
+    for (int h : {1, 16, 32}) {
+      bool fits = p.pairs == 32;
+      for (k = 0; fits && k < p.pairs; ++k) fits = p.lo[k] == k / h * 2 * h + k % h && p.hi[k] == p.lo[k] + h;
+      if (fits) p.turn = h;
     }
-    blocks = blocks && plan.n_pairs % 8 == 0;
-    for (int q = 0; blocks && q < plan.n_pairs; q += 8)
-      blocks = p.lo[q] % 8 == 0 && p.hi[q] % 8 == 0 && p.lo[q + 7] == p.lo[q] + 7 && p.hi[q + 7] == p.hi[q] + 7;
-    p.walk = plan.layout == RESS_ROPE_INTERLEAVED ? kNeighbours : blocks ? kBlocks : kSingle;
   }
   p.pos = a.pos;
   for (int i = 0; i < 3; ++i) p.bias[i] = a.b[i];

@@ -894,7 +894,7 @@ int ress_qkv_proj(const ress_dims* d, const uint16_t* x, const uint16_t* W_q, co
   if (e) return e;
   if ((e = check_ptr(W_k, 16, "W_k")) || (e = check_ptr(W_v, 16, "W_v")) || (e = check_ptr(x, 16, "x")) ||
       (e = check_ptr(Q, 16, "Q")) || (e = check_ptr(K, 16, "K")) || (e = check_ptr(V, 16, "V")) ||
-      (e = check_opt_ptr(b_q, 2, "b_q")) || (e = check_opt_ptr(b_k, 2, "b_k")) || (e = check_opt_ptr(b_v, 2, "b_v")))
+      (e = check_opt_ptr(b_q, 16, "b_q")) || (e = check_opt_ptr(b_k, 16, "b_k")) || (e = check_opt_ptr(b_v, 16, "b_v")))
     return e;
   if ((plan != nullptr) != (pos != nullptr)) return fail(RESS_EINVAL, "a plan and positions belong together");
   ress::QkvArgs a{};
