@@ -71,14 +71,6 @@ class WsLayout(ctypes.Structure):
                  "cdot", "ny", "nz", "lstat", "kcount", "prow", "ld", "words", "total")]
 
 
-class Norm(ctypes.Structure):
-    """ress_norm: rows for the layer norm and its gradient."""
-    _fields_ = [("rows", ctypes.c_int64), ("width", ctypes.c_int32), ("x_type", ctypes.c_int32),
-                ("y_type", ctypes.c_int32), ("param_type", ctypes.c_int32), ("eps", ctypes.c_float),
-                ("x_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64), ("dx_stride", ctypes.c_int64),
-                ("dres_stride", ctypes.c_int64)]
-
-
 ROPE_MAX_AXES, ROPE_MAX_DIM = 4, 256
 _LAYOUTS = {"sections": 0, "halves": 1, "interleaved": 2}
 
@@ -90,8 +82,9 @@ class RopePlan(ctypes.Structure):
                 ("n_pairs", ctypes.c_int32), ("turns", ctypes.c_uint64 * (ROPE_MAX_DIM // 2))]
 
 
-# ress_head_norm and ress_rope_heads as bytes (in a call of a few microseconds, nested ctypes
-# structures would be most of it)
+# ress_norm, ress_head_norm and ress_rope_heads as bytes (in a call of a few microseconds, nested
+# ctypes structures would be most of it)
+_NORM = struct.Struct("@qiiiif4xqqqq")              # rows, width, types, eps, strides
 _HEAD_NORM = struct.Struct("@i4xPP")                # enabled, weight, bias
 _ROPE_HEADS = struct.Struct("@i4xi4xPPPqqPqqPqqPP")  # n_heads, norm, x, y, dx, dweight, dbias
 
@@ -134,9 +127,9 @@ _SIGS = {
     "ress_token_drift": (_c.c_int, [_c.POINTER(Dims), _P, _P, _P, _P, _P, _c.c_size_t, _P]),
     "ress_sparse_attn_noalloc": (_c.c_int, [_c.POINTER(Dims), _P, _P, _P, _P, _P, _c.c_int64, _P,
                                             _c.c_int32, _P]),
-    "ress_layer_norm": (_c.c_int, [_c.POINTER(Norm), _P, _P, _P, _P, _P, _P, _P]),
-    "ress_layer_norm_workspace_bytes": (_c.c_size_t, [_c.POINTER(Norm)]),
-    "ress_layer_norm_bwd": (_c.c_int, [_c.POINTER(Norm), _P, _P, _P, _P, _P, _P, _P, _P, _P, _P,
+    "ress_layer_norm": (_c.c_int, [_P, _P, _P, _P, _P, _P, _P, _P]),
+    "ress_layer_norm_workspace_bytes": (_c.c_size_t, [_P]),
+    "ress_layer_norm_bwd": (_c.c_int, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P,
                                        _c.c_size_t, _P]),
     "ress_rope_plan_init": (_c.c_int, [_c.POINTER(RopePlan), _c.c_int32, _c.c_int32, _P, _c.c_int32,
                                        _c.c_double, _P]),
@@ -260,8 +253,8 @@ def _host(t, dtypes, name):
 def _stream(stream):
     if stream is not None:
         return stream.cuda_stream
-    torch = _torch()  # the current stream's handle without a Stream object (0.4 us instead of 3)
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    # the current device's current stream without a Stream object (0.2 us instead of 3)
+    return _torch()._C._cuda_getCurrentRawStream(-1)
 
 
 def _bf16():
@@ -391,57 +384,74 @@ def status(ws, stream=None):
 
 
 # ---- the input half of the sublayer ---------------------------------------------------
-# Small calls are a few microseconds on the GPU, so the checks below ask a tensor for each fact once.
+# Small calls take a few microseconds on the GPU, so a tensor that is as it should be is asked for each
+# fact once, and why another one is not is found out afterwards.
 _CODES = {}  # torch dtype -> ress_dtype
 
 
-def _code(t, name):
-    code = _CODES.get(t.dtype)
-    if code is None:
+def _types():
+    if not _CODES:
         torch = _torch()
         _CODES.update({torch.bfloat16: 0, torch.float16: 1, torch.float32: 2})
-        if t.dtype not in _CODES:
-            raise TypeError(f"{name} has dtype {t.dtype}, expected bfloat16, float16 or float32")
-        code = _CODES[t.dtype]
+    return _CODES
+
+
+def _code(t, name):
+    code = (_CODES or _types()).get(getattr(t, "dtype", None))
+    if code is None:
+        _refuse(t, name, dtypes=tuple(_types()))
     return code
 
 
-def _cuda(t, name):
-    """Device pointer of a CUDA tensor of any layout."""
-    try:
-        if t.is_cuda:
-            return t.data_ptr()
-    except AttributeError:
-        raise TypeError(f"{name} must be a torch.Tensor") from None
-    raise ValueError(f"{name} must live on a CUDA device")
+def _refuse(t, name, dtypes=None, shape=None, numel=None):
+    """Raises for a tensor that is not on a CUDA device, or not of this kind; else for its layout."""
+    if not isinstance(t, _torch().Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live on a CUDA device")
+    if dtypes is not None and t.dtype not in dtypes:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected one of {dtypes}")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if numel is not None and t.numel() != numel:
+        raise ValueError(f"{name} has {t.numel()} elements, expected {numel}")
+    raise ValueError(f"{name} must be contiguous, or have contiguous rows a fixed stride apart")
 
 
 def _vector(t, n, name):
-    """Device pointer of n contiguous elements (None -> NULL)."""
+    """Device pointer of n contiguous elements of one of the types (None -> NULL)."""
     if t is None:
-        return None
-    p = _cuda(t, name)
-    if t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"{name} must have {n} contiguous elements")
-    return p
+        return 0
+    try:
+        if t.is_cuda and t.numel() == n and t.is_contiguous() and t.dtype in (_CODES or _types()):
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _refuse(t, name, tuple(_types()), numel=n)
 
 
 def _vector_f32(t, n, name):
-    p = _vector(t, n, name)
-    if p is not None and _code(t, name) != 2:
-        raise TypeError(f"{name} has dtype {t.dtype}, expected float32")
-    return p
+    if t is None:
+        return 0
+    try:
+        if t.is_cuda and t.numel() == n and t.is_contiguous() and (_CODES or _types()).get(t.dtype) == 2:
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _refuse(t, name, (_torch().float32,), numel=n)
 
 
-def _row_stride(t, shape, name):
-    """Elements between the rows of a tensor [..., width] of this shape."""
-    if t.shape != shape:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.is_contiguous():
-        return shape[-1]
-    if len(shape) != 2 or (t.stride(1) != 1 and shape[1] > 1):
-        raise ValueError(f"{name} must be contiguous, or two-dimensional with contiguous rows")
-    return t.stride(0)
+def _rows(t, shape, name):
+    """Device pointer and elements between the rows of a tensor [..., width] of this shape."""
+    try:
+        if t.is_cuda and t.shape == shape:
+            if t.is_contiguous():
+                return t.data_ptr(), shape[-1]
+            if len(shape) == 2 and (t.stride(1) == 1 or shape[1] == 1):
+                return t.data_ptr(), t.stride(0)
+    except AttributeError:
+        pass
+    _refuse(t, name, shape=shape)
 
 
 def _param_code(*params):
@@ -459,24 +469,31 @@ def _param_code(*params):
 def _scratch(ws):
     """Pointer and bytes of a workspace (None -> NULL, 0)."""
     if ws is None:
-        return None, 0
-    n = ws.numel()
-    return _vector(ws, n, "ws"), n * ws.element_size()
+        return 0, 0
+    try:
+        if ws.is_cuda and ws.is_contiguous():
+            return ws.data_ptr(), ws.numel() * ws.element_size()
+    except AttributeError:
+        pass
+    _refuse(ws, "ws")
 
 
-def _width(x):
-    if x.dim() < 1 or x.shape[-1] < 1:
-        raise ValueError(f"x has shape {tuple(x.shape)}, expected [..., width]")
-    return x.shape[-1]
+def _row_shape(x):
+    shape = getattr(x, "shape", None)
+    if shape is None:
+        _refuse(x, "x")
+    if len(shape) < 1 or shape[-1] < 1:
+        raise ValueError(f"x has shape {tuple(shape)}, expected [..., width]")
+    return shape
 
 
 def layer_norm(x, weight, bias, y, eps: float = 1e-5, mean=None, rstd=None, stream=None):
     """ress_layer_norm over the last dimension of x [..., width] into y of the same shape; weight, bias
     [width] or None; mean, rstd: float32 outputs, one per row, for layer_norm_bwd, or None."""
-    px, py, shape, width = _cuda(x, "x"), _cuda(y, "y"), x.shape, _width(x)
+    shape = _row_shape(x)
+    (px, sx), (py, sy), width = _rows(x, shape, "x"), _rows(y, shape, "y"), shape[-1]
     rows = x.numel() // width
-    n = Norm(rows, width, _code(x, "x"), _code(y, "y"), _param_code(weight, bias), eps,
-             _row_stride(x, shape, "x"), _row_stride(y, shape, "y"), 0, 0)
+    n = _NORM.pack(rows, width, _code(x, "x"), _code(y, "y"), _param_code(weight, bias), eps, sx, sy, 0, 0)
     _check(_lib.ress_layer_norm(n, px, _vector(weight, width, "weight"), _vector(bias, width, "bias"), py,
                                 _vector_f32(mean, rows, "mean"), _vector_f32(rstd, rows, "rstd"),
                                 _stream(stream)))
@@ -484,7 +501,7 @@ def layer_norm(x, weight, bias, y, eps: float = 1e-5, mean=None, rstd=None, stre
 
 def layer_norm_workspace_bytes(rows: int, width: int) -> int:
     """Workspace of layer_norm_bwd on rows of this width."""
-    n = _lib.ress_layer_norm_workspace_bytes(Norm(rows, width, 0, 0, 0, 0.0, width, width, width, width))
+    n = _lib.ress_layer_norm_workspace_bytes(_NORM.pack(rows, width, 0, 0, 0, 0.0, width, width, width, width))
     if n == 0:
         raise RessError(-1, _lib.ress_last_error().decode())
     return n
@@ -493,16 +510,16 @@ def layer_norm_workspace_bytes(rows: int, width: int) -> int:
 def layer_norm_bwd(dy, x, weight, mean, rstd, dx, dweight=None, dbias=None, dres=None, ws=None, stream=None):
     """ress_layer_norm_bwd: dx (+ dres where given) and the float32 gradients of weight and bias
     (None to skip; ws is needed for them) from the gradient dy of layer_norm's y."""
-    pdy, px, pdx, shape, width = _cuda(dy, "dy"), _cuda(x, "x"), _cuda(dx, "dx"), x.shape, _width(x)
-    rows, code, pres, sres = x.numel() // width, _code(x, "x"), None, 0
-    if dres is not None:
-        pres, sres = _cuda(dres, "dres"), _row_stride(dres, shape, "dres")
-    if _code(dx, "dx") != code or (dres is not None and _code(dres, "dres") != code):
+    shape = _row_shape(x)
+    (pdy, sdy), (px, sx), (pdx, sdx) = _rows(dy, shape, "dy"), _rows(x, shape, "x"), _rows(dx, shape, "dx")
+    pres, sres = (0, 0) if dres is None else _rows(dres, shape, "dres")
+    width, code = shape[-1], _code(x, "x")
+    rows = x.numel() // width
+    if dx.dtype != x.dtype or (dres is not None and dres.dtype != x.dtype):
         raise TypeError(f"dx and dres must have x's dtype {x.dtype}")
     if mean is None or rstd is None:
         raise ValueError("mean and rstd are those layer_norm saved")
-    n = Norm(rows, width, code, _code(dy, "dy"), _param_code(weight), 0.0, _row_stride(x, shape, "x"),
-             _row_stride(dy, shape, "dy"), _row_stride(dx, shape, "dx"), sres)
+    n = _NORM.pack(rows, width, code, _code(dy, "dy"), _param_code(weight), 0.0, sx, sdy, sdx, sres)
     _check(_lib.ress_layer_norm_bwd(n, pdy, px, _vector(weight, width, "weight"), _vector_f32(mean, rows, "mean"),
                                     _vector_f32(rstd, rows, "rstd"), pres, pdx,
                                     _vector_f32(dweight, width, "dweight"), _vector_f32(dbias, width, "dbias"),
@@ -527,19 +544,18 @@ def rope_plan(axis_dims, head_dim: int = HEAD_DIM, base: float = 100.0, layout: 
     return plan
 
 
-def _heads(t, shape, code, name):
+def _heads(t, shape, dtype, name):
     """Pointer and strides of a tensor [tokens, heads, head_dim] with contiguous channels (None: absent)."""
     if t is None:
         return 0, 0, 0
-    p = _cuda(t, name)
-    if t.shape != shape:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if _code(t, name) != code:
-        raise TypeError(f"{name} has dtype {t.dtype}, unlike the call's other heads")
-    st, sh, sc = t.stride()
-    if sc != 1:
-        raise ValueError(f"{name} must have contiguous channels")
-    return p, st, sh
+    try:
+        if t.is_cuda and t.shape == shape and t.dtype == dtype:
+            st, sh, sc = t.stride()
+            if sc == 1:
+                return t.data_ptr(), st, sh
+    except AttributeError:
+        pass
+    _refuse(t, name, (dtype,), shape)
 
 
 def _head_norm(norm, n, name):
@@ -547,26 +563,25 @@ def _head_norm(norm, n, name):
     if norm is None:
         return 0, 0, 0
     weight, bias = norm
-    return 1, _vector(weight, n, name + " weight") or 0, _vector(bias, n, name + " bias") or 0
+    return 1, _vector(weight, n, name), _vector(bias, n, name)
 
 
 def _positions(plan, pos, tokens):
-    p = _cuda(pos, "pos")
-    if pos.shape != (tokens, plan.n_axes):
-        raise ValueError(f"pos has shape {tuple(pos.shape)}, expected ({tokens}, {plan.n_axes})")
-    if pos.dtype != _torch().int32 or not pos.is_contiguous():
-        raise TypeError("pos must be a contiguous int32 tensor")
-    return p
+    try:
+        if pos.is_cuda and pos.shape == (tokens, plan.n_axes) and pos.dtype == _torch().int32 and pos.is_contiguous():
+            return pos.data_ptr()
+    except AttributeError:
+        pass
+    _refuse(pos, "pos", (_torch().int32,), (tokens, plan.n_axes))
 
 
-def _rope_heads(plan, name, y, x, dx, norm, grads, shape, code):
+def _rope_heads(plan, name, y, x, dx, norm, grads, shape, dtype):
     """ress_rope_heads of one tensor."""
     hd = plan.head_dim
     dweight, dbias = (None, None) if grads is None else grads
-    return _ROPE_HEADS.pack(shape[1], *_head_norm(norm, hd, name + "_norm"), *_heads(x, shape, code, name),
-                            *_heads(y, shape, code, name + "'s result"), *_heads(dx, shape, code, name + "'s gradient"),
-                            _vector_f32(dweight, hd, name + " dweight") or 0,
-                            _vector_f32(dbias, hd, name + " dbias") or 0)
+    return _ROPE_HEADS.pack(shape[1], *_head_norm(norm, hd, name), *_heads(x, shape, dtype, name),
+                            *_heads(y, shape, dtype, name), *_heads(dx, shape, dtype, name),
+                            _vector_f32(dweight, hd, name), _vector_f32(dbias, hd, name))
 
 
 def _rope_shape(plan, t, tokens, name):
@@ -587,10 +602,10 @@ def rope(plan: RopePlan, pos, q, q_out, k=None, k_out=None, q_norm=None, k_norm=
     pos, int32 [tokens, axes]."""
     if q is None or q_out is None or (k is None) != (k_out is None) or (k is None and k_norm is not None):
         raise ValueError("q and q_out are needed, and k and k_out together")
-    tokens, code = pos.shape[0], _code(q, "q")
-    tq = _rope_heads(plan, "q", q_out, q, None, q_norm, None, _rope_shape(plan, q, tokens, "q"), code)
-    tk = None if k is None else _rope_heads(plan, "k", k_out, k, None, k_norm, None,
-                                            _rope_shape(plan, k, tokens, "k"), code)
+    tokens, code, dtype = pos.shape[0], _code(q, "q"), q.dtype
+    tq = _rope_heads(plan, "q, q_out or q_norm", q_out, q, None, q_norm, None, _rope_shape(plan, q, tokens, "q"), dtype)
+    tk = None if k is None else _rope_heads(plan, "k, k_out or k_norm", k_out, k, None, k_norm, None,
+                                            _rope_shape(plan, k, tokens, "k"), dtype)
     _check(_lib.ress_rope(plan, tokens, _positions(plan, pos, tokens), code, _norm_code(q_norm, k_norm), eps, tq, tk,
                           _stream(stream)))
 
@@ -611,20 +626,25 @@ def rope_bwd(plan: RopePlan, pos, dq_out, dq, dk_out=None, dk=None, q=None, k=No
         raise ValueError("dq_out and dq are needed, and dk_out and dk together")
     if (q_norm is not None and q is None) or (k_norm is not None and k is None):
         raise ValueError("a norm's gradient needs the norm's input")
-    tokens, code = pos.shape[0], _code(dq_out, "dq_out")
-    tq = _rope_heads(plan, "q", dq_out, q, dq, q_norm, q_norm_grads, _rope_shape(plan, dq_out, tokens, "dq_out"), code)
-    tk = None if dk is None else _rope_heads(plan, "k", dk_out, k, dk, k_norm, k_norm_grads,
-                                             _rope_shape(plan, dk_out, tokens, "dk_out"), code)
+    tokens, code, dtype = pos.shape[0], _code(dq_out, "dq_out"), dq_out.dtype
+    tq = _rope_heads(plan, "q, dq, dq_out, q_norm or its gradients", dq_out, q, dq, q_norm, q_norm_grads,
+                     _rope_shape(plan, dq_out, tokens, "dq_out"), dtype)
+    tk = None if dk is None else _rope_heads(plan, "k, dk, dk_out, k_norm or its gradients", dk_out, k, dk, k_norm,
+                                             k_norm_grads, _rope_shape(plan, dk_out, tokens, "dk_out"), dtype)
     _check(_lib.ress_rope_bwd(plan, tokens, _positions(plan, pos, tokens), code, _norm_code(q_norm, k_norm), eps, tq,
                               tk, *_scratch(ws), _stream(stream)))
 
 
 def _dense(t, n, name):
     """Device pointer of n contiguous bf16 elements (None -> NULL)."""
-    p = _vector(t, n, name)
-    if p is not None and _CODES.get(t.dtype) != 0 and t.dtype not in _bf16():
-        raise TypeError(f"{name} has dtype {t.dtype}, expected one of {_bf16()}")
-    return p
+    if t is None:
+        return 0
+    try:
+        if t.is_cuda and t.numel() == n and t.is_contiguous() and ((_CODES or _types()).get(t.dtype) == 0 or t.dtype in _bf16()):
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _refuse(t, name, _bf16(), numel=n)
 
 
 def qkv_proj(d: Dims, x, W_q, W_k, W_v, Q, K, V, ws, b_q=None, b_k=None, b_v=None, plan: RopePlan = None, pos=None,

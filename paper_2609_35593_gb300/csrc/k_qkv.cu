@@ -36,6 +36,7 @@ PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder();
 namespace {
 
 constexpr int kQThreads = 320;
+constexpr int kQEpilogue = 256;                  // threads of the epilogue: two groups of four warps
 constexpr int kQM = 128;                         // tokens per tile and CTA
 constexpr int kQHeads = 4;                       // heads per tile
 constexpr int kQStages = 4;
@@ -48,7 +49,7 @@ constexpr uint64_t kQWaitNs = 2000000000ull;
 constexpr uint64_t kQDrainNs = 200000000ull;
 
 constexpr uint32_t kQOffOut = kQStages * kQStage;          // two boxes per epilogue group
-constexpr uint32_t kQOffTurn = kQOffOut + 4 * kQBox;       // float4 [16][128 tokens]: of pairs 2q and
+constexpr uint32_t kQOffTurn = kQOffOut + kQHeads * kQBox;  // float4 [16][128 tokens]: of pairs 2q and
                                                            // 2q + 1 both cosines, both sines
 constexpr uint32_t kQOffCtl = kQOffTurn + 32 * kQM * 8;
 
@@ -64,9 +65,8 @@ struct QCtl {
 enum { kNoTurn = 0, kByPairs = -1 };
 
 struct QParams {
-  int N, K, H, mtiles;
-  int tiles_of;            // tiles of one of Q, K, V: ceil(H / 4)
-  int whole, parts;        // the first `whole` tiles run whole, the others as `parts` units each
+  int N, K, H;
+  int work;                // heads of all stripes
   int turn, pairs, axes;   // turn: h, kNoTurn or kByPairs
   uint8_t lo[32], hi[32];  // channels of each pair
   uint8_t axis[32];
@@ -97,16 +97,16 @@ __device__ __forceinline__ void q_give_up(QCtl& C, uint32_t* status) {
   *reinterpret_cast<volatile int*>(&C.abort) = 1;
 }
 
-// Barriers of the eight epilogue warps (the second also ANDs a flag across them) and of one group of
+// Barriers of all epilogue warps (the second also ANDs a flag across them) and of one group of
 // four, in the form that does not ask for a converged warp.
-__device__ __forceinline__ void q_epi_sync() { asm volatile("barrier.cta.sync 1, 256;" ::: "memory"); }
+__device__ __forceinline__ void q_epi_sync() { asm volatile("barrier.cta.sync 1, %0;" ::"n"(kQEpilogue) : "memory"); }
 __device__ __forceinline__ bool q_epi_sync_and(bool v) {
   uint32_t r;
   asm volatile(
       "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
-      "barrier.cta.red.and.pred q, 2, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+      "barrier.cta.red.and.pred q, 2, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
       : "=r"(r)
-      : "r"(v ? 1u : 0u)
+      : "r"(v ? 1u : 0u), "n"(kQEpilogue)
       : "memory");
   return r != 0;
 }
@@ -125,31 +125,33 @@ __device__ __forceinline__ void q_group_sync(int group) {
       : "r"(at0), "r"(at1)                                  \
       : "memory")
 
-// One unit of work of a pair: token stripe mt, `heads` heads from `head` on of Q, K or V (which).
+// The work is the heads of all stripes in a row (stripe, then Q, K, V, then head), and a pair's share
+// is a range of them, so that shares differ by one head at most, a call on few tokens has single heads
+// on many SMs, and a pair goes through its stripes' tiles one after the other (their x slices come from
+// L2 and their cosines and sines are formed once).  A unit is up to 4 heads of a range from `head` on,
+// to the next multiple of 4: one tile.
 struct QUnit {
   int mt, which, head, heads;
 };
-__device__ __forceinline__ int q_units(const QParams& p) {
-  const int units = p.whole + (p.mtiles * 3 * p.tiles_of - p.whole) * p.parts;
-  return (units - 1 - (int)(blockIdx.x >> 1)) / (int)(gridDim.x >> 1) + 1;
-}
-__device__ __forceinline__ QUnit q_unit(const QParams& p, int k) {
-  const int u = (int)(blockIdx.x >> 1) + k * (int)(gridDim.x >> 1);
-  int tile = u, part = 0, parts = 1;
-  if (u >= p.whole) {
-    parts = p.parts;
-    tile = p.whole + (u - p.whole) / parts;
-    part = (u - p.whole) % parts;
+struct QCursor {
+  int at, end;
+  __device__ explicit QCursor(const QParams& p) {
+    const int pairs = (int)gridDim.x >> 1, i = (int)blockIdx.x >> 1, rest = p.work % pairs;
+    at = p.work / pairs * i + min(i, rest);
+    end = at + p.work / pairs + (i < rest);
   }
-  // consecutive tiles share their token stripe, so x slices are re-read from L2
-  const int per = 3 * p.tiles_of, j = tile % per, heads = kQHeads / parts;
-  QUnit t;
-  t.mt = tile / per;
-  t.which = j / p.tiles_of;
-  t.head = kQHeads * (j % p.tiles_of) + heads * part;
-  t.heads = max(0, min(heads, p.H - t.head));  // a part past the last head has none
-  return t;
-}
+  __device__ bool more() const { return at < end; }
+  __device__ QUnit unit(const QParams& p) const {
+    const int in_stripe = at % (3 * p.H);
+    QUnit t;
+    t.mt = at / (3 * p.H);
+    t.which = in_stripe / p.H;
+    t.head = in_stripe % p.H;
+    t.heads = min(min(kQHeads - t.head % kQHeads, p.H - t.head), end - at);
+    return t;
+  }
+  __device__ void next(const QUnit& t) { at += t.heads; }
+};
 
 // One head of one token: 64 columns of this thread's TMEM lane, to its row of an output box.
 struct QHead {
@@ -250,7 +252,7 @@ __global__ void __launch_bounds__(kQThreads, 1)
   QCtl& C = *reinterpret_cast<QCtl*>(base + kQOffCtl);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   volatile int* abort = &C.abort;
-  const int ksteps = p.K / 64, nunits = q_units(p);
+  const int ksteps = p.K / 64;
   const int rank = (int)cluster_rank() & 1, lead = (int)cluster_rank() & ~1;
   const uint32_t both = 3u << lead;
   auto A = [&](int s) { return base + s * kQStage; };
@@ -263,7 +265,7 @@ __global__ void __launch_bounds__(kQThreads, 1)
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(&C.acc_full[b], 1);
-      mbar_init(&C.acc_empty[b], 16);  // the epilogue warps of both CTAs
+      mbar_init(&C.acc_empty[b], 2 * kQEpilogue / 32);  // the epilogue warps of both CTAs
     }
     C.abort = 0;
     fence_barrier_init();
@@ -285,9 +287,10 @@ __global__ void __launch_bounds__(kQThreads, 1)
     // ================================ loads ==========================================
     int it = 0;
     bool failed = false;
-    for (int k = 0; k < nunits && !failed; ++k) {
-      const QUnit t = q_unit(p, k);
-      if (t.heads == 0) continue;
+    for (QCursor c(p); c.more() && !failed;) {
+      const QUnit t = c.unit(p);
+      c.next(t);
+      const bool ahead = c.more() && c.unit(p).mt != t.mt;  // the next stripe into L2 meanwhile
       for (int ks = 0; ks < ksteps; ++ks, ++it) {
         const int s = it % kQStages, u = it / kQStages;
         if (u > 0 && !q_wait(&C.empty[s], (u - 1) & 1, abort)) {
@@ -305,6 +308,7 @@ __global__ void __launch_bounds__(kQThreads, 1)
             for (int h = 0; h < t.heads; ++h)
               tma_load_3d_pair(B(s) + h * 32 * 128, &maps.w_part[t.which], full, 64 * ks, row + 32 * h, 0);
           }
+          if (ahead) tma_prefetch_3d(&maps.x, 64 * ks, kQM * (2 * t.mt + 2 + rank), 0);
         }
         __syncwarp();
       }
@@ -332,9 +336,9 @@ __global__ void __launch_bounds__(kQThreads, 1)
       }
       failed = true;
     }
-    for (int k = 0; k < nunits && !failed; ++k) {
-      const QUnit t = q_unit(p, k);
-      if (t.heads == 0) continue;
+    for (QCursor c(p); c.more() && !failed;) {
+      const QUnit t = c.unit(p);
+      c.next(t);
       const uint32_t idesc = idesc_bf16_f32(2 * kQM, 64 * t.heads, false);
       const int b = n & 1, use = n >> 1;  // the accumulator, its earlier uses
       ++n;
@@ -387,9 +391,9 @@ __global__ void __launch_bounds__(kQThreads, 1)
       }
     }
     int n = 0, boxes = 0, table = -1;  // units done; boxes this group has stored; the table's stripe
-    for (int k = 0; k < nunits; ++k) {
-      const QUnit t = q_unit(p, k);
-      if (t.heads == 0) continue;
+    for (QCursor c(p); c.more();) {
+      const QUnit t = c.unit(p);
+      c.next(t);
       const int b = n & 1, use = n >> 1;
       ++n;
       const int row0 = kQM * (2 * t.mt + rank), which = t.which, mode = which < 2 ? p.turn : kNoTurn;
@@ -508,8 +512,7 @@ cudaError_t launch_qkv_proj(const QkvArgs& a, cudaStream_t st) {
   p.N = a.N;
   p.K = a.Dm;
   p.H = a.H;
-  p.mtiles = (a.N + 2 * kQM - 1) / (2 * kQM);
-  p.tiles_of = (a.H + kQHeads - 1) / kQHeads;
+  p.work = (a.N + 2 * kQM - 1) / (2 * kQM) * 3 * a.H;
   p.turn = kNoTurn;
   if (a.rotate) {
     const ress_rope_plan& plan = a.plan;
@@ -545,17 +548,7 @@ cudaError_t launch_qkv_proj(const QkvArgs& a, cudaStream_t st) {
   static_assert(kQOffCtl + sizeof(QCtl) + 1024 <= 227 * 1024, "shared memory of a CTA");
   cudaError_t e = cudaFuncSetAttribute(k_qkv, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
-  const int tiles = p.mtiles * 3 * p.tiles_of, slots = max(1, rows::sm_count() / 2);
-  // tiles past the last whole wave of pairs run as 2 or 4 units of fewer heads where those fit into one
-  p.whole = tiles;
-  p.parts = 1;
-  const int left = tiles % slots;
-  if (left > 0 && 2 * left <= slots) {
-    p.whole = tiles - left;
-    p.parts = 4 * left <= slots ? 4 : 2;
-  }
-  const int units = p.whole + (tiles - p.whole) * p.parts;
-  return launch_with(k_qkv, 2 * min(units, slots), kQThreads, smem, st, true, 2, m, p);
+  return launch_with(k_qkv, 2 * min(p.work, max(1, rows::sm_count() / 2)), kQThreads, smem, st, true, 2, m, p);
 }
 
 }  // namespace ress
