@@ -23,6 +23,8 @@
 // and leaves one partial row of each in the workspace, and a second kernel adds the partial rows up
 // in order, so that the result does not depend on the order in which CTAs finish.
 
+#include <atomic>
+
 #include "row_ops.cuh"
 
 namespace ress {
@@ -435,17 +437,28 @@ __global__ void __launch_bounds__(32 * kFoldWarps)
   }
 }
 
-// Teams of the launch: a multiple of a CTA's, as many as fit on the GPU at once at most, all with
-// the same number of steps but for the last ones.
-template <typename K>
-int norm_ctas(K kern, int threads, size_t smem, int teams_per_cta, int64_t batches, int most) {
-  int resident = 1;
-  if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kern, threads, smem) != cudaSuccess || resident < 1)
-    resident = 1;
+// CTAs of the launch: as many as fit on the GPU at once at most, all with the same number of steps but
+// for the last ones.  (A team of a CTA has the threads its rows' width asks for: `resident` is for the
+// threads at hand.)
+int norm_ctas(int resident, int teams_per_cta, int64_t batches, int most) {
   const int64_t ctas = (batches + teams_per_cta - 1) / teams_per_cta;
   const int64_t fit = min((int64_t)resident * sm_count(), (int64_t)most);
   const int64_t steps = (ctas + fit - 1) / fit;
   return (int)((ctas + steps - 1) / steps);
+}
+
+// CTAs of a kernel that fit on an SM, for each number of warps, asked for once.
+template <auto kKernel>
+int norm_resident(int threads, size_t smem) {
+  static std::atomic<int> known[kNormMaxThreads / 32 + 1];
+  std::atomic<int>& at = known[threads / 32];
+  int n = at.load(std::memory_order_relaxed);
+  if (n == 0) {
+    const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kKernel, threads, smem);
+    if (e != cudaSuccess || n < 1) n = 1;
+    at.store(n, std::memory_order_relaxed);
+  }
+  return n;
 }
 
 template <bool BWD, typename X, typename Y, int E, int C, int TEAM>
@@ -455,17 +468,17 @@ cudaError_t launch_norm_as(const NormArgs& a, const NormParams& p, cudaStream_t 
   const int per_cta = TEAM == kWholeCta ? 1 : kNormThreads / kLanes<TEAM>;
   if constexpr (!BWD) {
     constexpr int R = C == 32 ? 1 : wide ? 16 / C : 32 / C;
-    auto kern = k_layer_norm<X, Y, E, C, TEAM, R>;
-    const int ctas = norm_ctas(kern, threads, 0, per_cta, (p.rows + R - 1) / R, INT32_MAX);
+    constexpr auto kern = k_layer_norm<X, Y, E, C, TEAM, R>;
+    const int ctas = norm_ctas(norm_resident<kern>(threads, 0), per_cta, (p.rows + R - 1) / R, INT32_MAX);
     return launch_pdl(kern, ctas, threads, 0, st, true, p);
   } else {
     constexpr int R = C == 32 || wide ? 1 : 2;
-    auto kern = k_layer_norm_bwd<X, Y, E, C, TEAM, R>;
+    constexpr auto kern = k_layer_norm_bwd<X, Y, E, C, TEAM, R>;
     const size_t smem = C == 8 ? 0 : 2 * C * sizeof(float) * threads;
     cudaError_t e = cudaSuccess;
     if (smem > 0) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    const int ctas = norm_ctas(kern, threads, smem, per_cta, (p.rows + R - 1) / R, kNormParts);
+    const int ctas = norm_ctas(norm_resident<kern>(threads, smem), per_cta, (p.rows + R - 1) / R, kNormParts);
     e = launch_pdl(kern, ctas, threads, smem, st, true, p);
     if (e != cudaSuccess || !p.partial) return e;
     return launch_pdl(k_fold_parts, (2 * p.width + 31) / 32, 32 * kFoldWarps, 0, st, true, p.partial, ctas,

@@ -403,10 +403,8 @@ cudaError_t launch_rope_as(RopeParams& p, int (&ctas)[2], cudaStream_t st) {
   // norm: 66 us with K = 4, 73 with 2; without one, 20,011 tokens, 12 + 4 heads: 22 and 20.5; gradient with
   // a norm, 10,992 tokens: 36 with K = 2 or 4, 45 with 1).
   constexpr int K = sizeof(T) == 2 ? (NORM && !BWD ? 4 : 2) : (NORM && BWD ? 1 : 2);
-  auto kern = k_rope<T, G, MODE, NORM, BWD, K>;
-  int resident = 1;
-  if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kern, kRopeThreads, 0) != cudaSuccess || resident < 1)
-    resident = 1;
+  constexpr auto kern = k_rope<T, G, MODE, NORM, BWD, K>;
+  const int resident = resident_ctas<kern>(kRopeThreads, 0);
   const int64_t fit = min((int64_t)resident * sm_count(), (int64_t)kRopeParts - 1);
   p.whole_tokens = p.tokens * ((p.t[0].heads > 0) + (p.t[1].heads > 0)) >= fit * kRopeWarps;
   int64_t need[2], all = 0;  // CTAs at one visit per warp

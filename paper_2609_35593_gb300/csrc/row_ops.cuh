@@ -285,6 +285,17 @@ __host__ __device__ inline int rope_axis(const ress_rope_plan& plan, int pair) {
   return a;
 }
 
+// CTAs of a kernel that fit on an SM (asked for once: the question takes about as long as a launch).
+template <auto kKernel>
+int resident_ctas(int threads, size_t smem) {
+  static const int n = [&] {
+    int r = 0;
+    const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&r, kKernel, threads, smem);
+    return e == cudaSuccess && r > 0 ? r : 1;
+  }();
+  return n;
+}
+
 inline int sm_count() {
   int dev = 0, n = 0;
   cudaGetDevice(&dev);
