@@ -8,9 +8,9 @@
 // instructions per row of 4 heads of 64 the instructions took 111 us of the 53 that the bytes need
 // (43,968 tokens, 16 + 16 heads, bf16), so the kernel is laid out for few of them.
 //
-// A lane holds 4 slots, each the two channels of a pair (or two channels without a pair), so that a
-// rotation needs no other lane, and a head has G lanes.  Where the plan's pairs are 4 and 4
-// neighbouring channels (kChunks) or 8 neighbours (kNeighbours) they are read and written as
+// A lane holds S = 4 or 8 slots, each the two channels of a pair (or two channels without a pair), so
+// that a rotation needs no other lane, and a head has G lanes.  Where the plan's pairs are S and S
+// neighbouring channels (kChunks) or 2 S neighbours (kNeighbours) they are read and written as
 // vectors, else one by one (kGather).  An item is one token and up to K rows of 32 / G of its heads
 // of one tensor, and a warp has the next item's elements on their way while it works on one.  A CTA
 // stays with Q or K (shares of the grid by their heads), and its lanes keep the norm's parameters
@@ -53,12 +53,13 @@ struct RopeParams {
 };
 
 // The channels of a slot.  Slots past the pairs have channels without one, if any are left: two
-// neighbours, or (kChunks) those of 4 slots as 4 and 4 neighbours.
-__device__ __forceinline__ void slot_channels(const ress_rope_plan& p, int mode, int slot, int& a, int& b) {
+// neighbours, or (kChunks) those of a lane's S slots as S and S neighbours.
+template <int MODE, int S>
+__device__ __forceinline__ void slot_channels(const ress_rope_plan& p, int slot, int& a, int& b) {
   if (slot >= p.n_pairs) {
     const int i = slot - p.n_pairs;
-    a = mode == kChunks ? 2 * p.n_pairs + i / 4 * 8 + i % 4 : 2 * p.n_pairs + 2 * i;
-    b = mode == kChunks ? a + 4 : a + 1;
+    a = MODE == kChunks ? 2 * p.n_pairs + i / S * 2 * S + i % S : 2 * p.n_pairs + 2 * i;
+    b = MODE == kChunks ? a + S : a + 1;
     return;
   }
   if (p.layout == RESS_ROPE_INTERLEAVED) {
@@ -74,67 +75,65 @@ __device__ __forceinline__ void slot_channels(const ress_rope_plan& p, int mode,
   }
 }
 
-// A lane's 8 elements: the first channels of its slots in words of their own, then the second ones
-// (kNeighbours: as they lie).
-template <typename T, int MODE>
+// A lane's 2 S elements: the first channels of its slots, then the second ones (kNeighbours: as they
+// lie).
+template <typename T, int MODE, int S>
 struct Slots {
   const int *a, *b;  // kGather: the slots' channels
-  bool in[4];        // the slots that exist
+  bool in[S];        // the slots that exist
   bool any;          // (not kGather: all or none)
-  int first, next;   // kChunks, kNeighbours: the lane's two vectors of 4 channels
+  int first, next;   // kChunks, kNeighbours: the lane's vectors
 
-  __device__ Vec<T, 8> load(const T* p, bool live) const {
-    Vec<T, 8> r = zero_vec<T, 8>();
+  __device__ Vec<T, 2 * S> load(const T* p, bool live) const {
+    Vec<T, 2 * S> r = zero_vec<T, 2 * S>();
     if (!live || !any) return r;
     if constexpr (MODE == kNeighbours) {
-      r = load_vec<T, 8>(p + first);
+      r = load_vec<T, 2 * S>(p + first);
     } else if constexpr (MODE == kChunks) {
-      const Vec<T, 4> u = load_vec<T, 4>(p + first), v = load_vec<T, 4>(p + next);
-      constexpr int W = Vec<T, 4>::kWords;
+      const Vec<T, S> u = load_vec<T, S>(p + first), v = load_vec<T, S>(p + next);
+      constexpr int W = Vec<T, S>::kWords;
 #pragma unroll
       for (int k = 0; k < W; ++k) r.w[k] = u.w[k], r.w[W + k] = v.w[k];
     } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < S; ++j)
         if (in[j]) {
           put(r, j, p[a[j]]);
-          put(r, 4 + j, p[b[j]]);
+          put(r, S + j, p[b[j]]);
         }
     }
     return r;
   }
-  __device__ static void put(Vec<T, 8>& r, int j, T v) {
+  __device__ static void put(Vec<T, 2 * S>& r, int j, T v) {
     if constexpr (sizeof(T) == 4)
       r.w[j] = __float_as_uint(v);
     else
       r.w[j / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(&v) << (16 * (j & 1));
   }
   // Slots 2 q and 2 q + 1: their first (side 0) or second channels.
-  __device__ static F2 get(const Vec<T, 8>& r, int side, int q) {
-    if constexpr (MODE == kNeighbours)
-      return pack2(elem(r, 4 * q + side), elem(r, 4 * q + 2 + side));
-    const Vec<T, 8> one[1] = {r};
-    return pair_of(one, 2 * side + q);
+  __device__ static F2 get(const Vec<T, 2 * S>& r, int side, int q) {
+    if constexpr (MODE == kNeighbours) return pack2(elem(r, 4 * q + side), elem(r, 4 * q + 2 + side));
+    const Vec<T, 2 * S> one[1] = {r};
+    return pair_of(one, side * (S / 2) + q);
   }
-  __device__ void store(T* p, const F2 (&u)[2][2], bool live) const {
+  __device__ void store(T* p, const F2 (&u)[2][S / 2], bool live) const {
     if (!live || !any) return;
-    float v[2][4];
+    float v[2][S];
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      unpack2(u[s][0], v[s][0], v[s][1]);
-      unpack2(u[s][1], v[s][2], v[s][3]);
-    }
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int q = 0; q < S / 2; ++q) unpack2(u[s][q], v[s][2 * q], v[s][2 * q + 1]);
     if constexpr (MODE == kNeighbours) {
-      float o[8];
+      float o[2 * S];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) o[2 * j] = v[0][j], o[2 * j + 1] = v[1][j];
-      store_vec<T, 8>(p + first, o);
+      for (int j = 0; j < S; ++j) o[2 * j] = v[0][j], o[2 * j + 1] = v[1][j];
+      store_vec<T, 2 * S>(p + first, o);
     } else if constexpr (MODE == kChunks) {
-      store_vec<T, 4>(p + first, v[0]);
-      store_vec<T, 4>(p + next, v[1]);
+      store_vec<T, S>(p + first, v[0]);
+      store_vec<T, S>(p + next, v[1]);
     } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < S; ++j)
         if (in[j]) {
           p[a[j]] = from_f32<T>(v[0][j]);
           p[b[j]] = from_f32<T>(v[1][j]);
@@ -143,10 +142,11 @@ struct Slots {
   }
 };
 
-template <typename T, int G, int MODE, bool NORM, bool BWD, int K>
-__global__ void __launch_bounds__(kRopeThreads, !NORM ? 6 : BWD ? 3 : 4) k_rope(const __grid_constant__ RopeParams p) {
+template <typename T, int G, int MODE, int S, bool NORM, bool BWD, int K>
+__global__ void __launch_bounds__(kRopeThreads, (!NORM ? 6 : BWD ? 3 : 4) - (S == 8 ? 1 : 0)) k_rope(const __grid_constant__ RopeParams p) {
   constexpr int kHeads = 32 / G;              // heads of a warp's row
-  constexpr int kPairs = G <= 8 ? 1 : G / 8;  // pairs per lane: 4 G pairs at most
+  constexpr int kPairs = G * S <= 32 ? 1 : G * S / 32;  // pairs per lane: G S pairs at most
+  constexpr int Q = S / 2;
   constexpr bool kReadX = !BWD || NORM;
   __shared__ __align__(16) float cosines[kRopeWarps][32 * kPairs], sines[kRopeWarps][32 * kPairs];
   const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
@@ -166,15 +166,15 @@ __global__ void __launch_bounds__(kRopeThreads, !NORM ? 6 : BWD ? 3 : 4) k_rope(
   t.out_token = second ? p.t[1].out_token : p.t[0].out_token;
   t.out_head = second ? p.t[1].out_head : p.t[0].out_head;
   const int hd = p.plan.head_dim, heads = t.heads;
-  const int group = lane / G, slot = lane % G * 4;
+  const int group = lane / G, slot = lane % G * S;
   const float inv = 1.f / (float)hd;
 
-  int a[4], b[4];
-  Slots<T, MODE> slots;
+  int a[S], b[S];
+  Slots<T, MODE, S> slots;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
+  for (int j = 0; j < S; ++j) {
     slots.in[j] = 2 * (slot + j) < hd;
-    slot_channels(p.plan, MODE, min(slot + j, hd / 2 - 1), a[j], b[j]);
+    slot_channels<MODE, S>(p.plan, min(slot + j, hd / 2 - 1), a[j], b[j]);
   }
   slots.a = a;
   slots.b = b;
@@ -193,12 +193,12 @@ __global__ void __launch_bounds__(kRopeThreads, !NORM ? 6 : BWD ? 3 : 4) k_rope(
   }
 
   stream_acquire();
-  // [side][slots 0 and 1, slots 2 and 3]
-  F2 w[2][2], shift[2][2], dw[2][2], db[2][2];
+  // [side][slots 2q and 2q + 1]
+  F2 w[2][Q], shift[2][Q], dw[2][Q], db[2][Q];
 #pragma unroll
   for (int s = 0; s < 2; ++s)
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
+    for (int q = 0; q < Q; ++q) {
       float v[2][2] = {};
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
@@ -223,7 +223,7 @@ __global__ void __launch_bounds__(kRopeThreads, !NORM ? 6 : BWD ? 3 : 4) k_rope(
   int64_t token = w0 / spans;
   int chunk = (int)(w0 - token * spans) * span, left = span;  // left: items of the span from this one on
   // the next item's rows and positions are on their way while this one is worked on
-  Vec<T, 8> next_x[kReadX ? K : 1], next_y[BWD ? K : 1];
+  Vec<T, 2 * S> next_x[kReadX ? K : 1], next_y[BWD ? K : 1];
   int32_t pos[kPairs];
   auto load = [&]() {
     const bool live = token < p.tokens;
@@ -243,7 +243,7 @@ __global__ void __launch_bounds__(kRopeThreads, !NORM ? 6 : BWD ? 3 : 4) k_rope(
   load();
 #pragma unroll 1
   while (token < p.tokens) {
-    Vec<T, 8> x[kReadX ? K : 1], y[BWD ? K : 1];
+    Vec<T, 2 * S> x[kReadX ? K : 1], y[BWD ? K : 1];
     float2 cs[kPairs];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -274,28 +274,36 @@ __global__ void __launch_bounds__(kRopeThreads, !NORM ? 6 : BWD ? 3 : 4) k_rope(
       }
     }
     load();
-    const float4 c4 = *reinterpret_cast<const float4*>(&cosines[warp][slot]);
-    const float4 s4 = *reinterpret_cast<const float4*>(&sines[warp][slot]);
-    const F2 co[2] = {pack2(c4.x, c4.y), pack2(c4.z, c4.w)}, si[2] = {pack2(s4.x, s4.y), pack2(s4.z, s4.w)};
-    const F2 neg[2] = {pack2(-s4.x, -s4.y), pack2(-s4.z, -s4.w)};
+    F2 co[Q], si[Q], neg[Q];
+#pragma unroll
+    for (int q = 0; q < Q; q += 2) {
+      const float4 c = *reinterpret_cast<const float4*>(&cosines[warp][slot + 2 * q]);
+      const float4 z = *reinterpret_cast<const float4*>(&sines[warp][slot + 2 * q]);
+      co[q] = pack2(c.x, c.y), co[q + 1] = pack2(c.z, c.w);
+      si[q] = pack2(z.x, z.y), si[q + 1] = pack2(z.z, z.w);
+      neg[q] = pack2(-z.x, -z.y), neg[q + 1] = pack2(-z.z, -z.w);
+    }
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int head = head0 + k * kHeads;
       if (head - group >= heads) break;  // no head of this row
-      F2 h[2][2], u[2][2];
+      F2 h[2][Q], u[2][Q];
       float rstd = 1.f;
       if constexpr (NORM) {
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int q = 0; q < 2; ++q) h[s][q] = Slots<T, MODE>::get(x[k], s, q);
+          for (int q = 0; q < Q; ++q) h[s][q] = Slots<T, MODE, S>::get(x[k], s, q);
         // a lane's sum is scaled before the lanes' meet: the sum may overflow where its average does not
-        const F2 m = both(-segment_sum<G>(sum2(add2(add2(h[0][0], h[0][1]), add2(h[1][0], h[1][1]))) * inv));
+        F2 sum[2] = {h[0][0], h[1][0]};
+#pragma unroll
+        for (int q = 1; q < Q; ++q) sum[0] = add2(sum[0], h[0][q]), sum[1] = add2(sum[1], h[1][q]);
+        const F2 m = both(-segment_sum<G>(sum2(add2(sum[0], sum[1])) * inv));
         F2 sq = both(0.f);
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int q = 0; q < 2; ++q) {
+          for (int q = 0; q < Q; ++q) {
             h[s][q] = add2(h[s][q], m);
             if constexpr (MODE == kGather) {  // slots that do not exist
               float e0, e1;
@@ -308,7 +316,7 @@ __global__ void __launch_bounds__(kRopeThreads, !NORM ? 6 : BWD ? 3 : 4) k_rope(
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int q = 0; q < 2; ++q) {
+          for (int q = 0; q < Q; ++q) {
             h[s][q] = mul2(h[s][q], both(rstd));
             if (!BWD) u[s][q] = fma2(h[s][q], w[s][q], shift[s][q]);
           }
@@ -317,10 +325,10 @@ __global__ void __launch_bounds__(kRopeThreads, !NORM ? 6 : BWD ? 3 : 4) k_rope(
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int q = 0; q < 2; ++q) u[s][q] = Slots<T, MODE>::get(BWD ? y[k] : x[k], s, q);
+          for (int q = 0; q < Q; ++q) u[s][q] = Slots<T, MODE, S>::get(BWD ? y[k] : x[k], s, q);
       }
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
+      for (int q = 0; q < Q; ++q) {
         F2 r0 = fma2(u[0][q], co[q], mul2(u[1][q], neg[q])), r1 = fma2(u[1][q], co[q], mul2(u[0][q], si[q]));
         if (!p.all) {  // channels without a pair keep their bits
           if constexpr (MODE == kGather) {
@@ -346,7 +354,7 @@ __global__ void __launch_bounds__(kRopeThreads, !NORM ? 6 : BWD ? 3 : 4) k_rope(
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int q = 0; q < 2; ++q) {
+          for (int q = 0; q < Q; ++q) {
             if (live) {
               dw[s][q] = fma2(u[s][q], h[s][q], dw[s][q]);
               db[s][q] = add2(db[s][q], u[s][q]);
@@ -359,7 +367,7 @@ __global__ void __launch_bounds__(kRopeThreads, !NORM ? 6 : BWD ? 3 : 4) k_rope(
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int q = 0; q < 2; ++q) u[s][q] = mul2(fma2(h[s][q], agh, add2(u[s][q], ag)), both(rstd));
+          for (int q = 0; q < Q; ++q) u[s][q] = mul2(fma2(h[s][q], agh, add2(u[s][q], ag)), both(rstd));
       }
       slots.store(out + k * kHeads * t.out_head, u, head < heads);
     }
@@ -368,11 +376,11 @@ __global__ void __launch_bounds__(kRopeThreads, !NORM ? 6 : BWD ? 3 : 4) k_rope(
   if constexpr (NORM && BWD) {
     if (!p.partial) return;
     // the CTA's sums: a warp's groups, then its warps in order
-    __shared__ float part[kRopeWarps][2][G * 8];
+    __shared__ float part[kRopeWarps][2][G * 2 * S];
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
+      for (int q = 0; q < Q; ++q) {
         float v[2][2];
         unpack2(dw[s][q], v[0][0], v[0][1]);
         unpack2(db[s][q], v[1][0], v[1][1]);
@@ -397,13 +405,14 @@ __global__ void __launch_bounds__(kRopeThreads, !NORM ? 6 : BWD ? 3 : 4) k_rope(
 }
 
 // CTAs of the two tensors of a launch; the forward's launch has no sums to fold.
-template <typename T, int G, int MODE, bool NORM, bool BWD>
+template <typename T, int G, int MODE, int S, bool NORM, bool BWD>
 cudaError_t launch_rope_as(RopeParams& p, int (&ctas)[2], cudaStream_t st) {
   // Rows of an item, their elements in registers twice (43,968 tokens, 16 + 16 heads of 64, bf16, with a
-  // norm: 66 us with K = 4, 73 with 2; without one, 20,011 tokens, 12 + 4 heads: 22 and 20.5; gradient with
-  // a norm, 10,992 tokens: 36 with K = 2 or 4, 45 with 1).
-  constexpr int K = sizeof(T) == 2 ? (NORM && !BWD ? 4 : 2) : (NORM && BWD ? 1 : 2);
-  constexpr auto kern = k_rope<T, G, MODE, NORM, BWD, K>;
+  // norm: S = 4 and K = 4 67 us, K = 2 73; S = 8 and K = 2 66, K = 1 76; without one, 20,011 tokens,
+  // 12 + 4 heads, S = 4: K = 4 22, K = 2 20.5; gradient with a norm, 10,992 tokens, both launches: S = 4 and
+  // K = 2 36.5, K = 1 45; S = 8 and K = 2 33, K = 1 40).
+  constexpr int K = S == 8 ? 2 : sizeof(T) == 2 ? (NORM && !BWD ? 4 : 2) : (NORM && BWD ? 1 : 2);
+  constexpr auto kern = k_rope<T, G, MODE, S, NORM, BWD, K>;
   const int resident = resident_ctas<kern>(kRopeThreads, 0);
   const int64_t fit = min((int64_t)resident * sm_count(), (int64_t)kRopeParts - 1);
   p.whole_tokens = p.tokens * ((p.t[0].heads > 0) + (p.t[1].heads > 0)) >= fit * kRopeWarps;
@@ -425,32 +434,44 @@ cudaError_t launch_rope_as(RopeParams& p, int (&ctas)[2], cudaStream_t st) {
   return launch_pdl(kern, ctas[0] + ctas[1], kRopeThreads, 0, st, true, p);
 }
 
-template <typename T, bool NORM, bool BWD>
-cudaError_t launch_rope_typed(RopeParams& p, int mode, int (&ctas)[2], cudaStream_t st) {
-  const int hd = p.plan.head_dim;
-  if (mode == kGather)
-    return hd <= 64 ? launch_rope_as<T, 8, kGather, NORM, BWD>(p, ctas, st)
-                    : launch_rope_as<T, 32, kGather, NORM, BWD>(p, ctas, st);
-  if (mode == kNeighbours) {
-    if (hd <= 32) return launch_rope_as<T, 4, kNeighbours, NORM, BWD>(p, ctas, st);
-    if (hd <= 64) return launch_rope_as<T, 8, kNeighbours, NORM, BWD>(p, ctas, st);
-    if (hd <= 128) return launch_rope_as<T, 16, kNeighbours, NORM, BWD>(p, ctas, st);
-    return launch_rope_as<T, 32, kNeighbours, NORM, BWD>(p, ctas, st);
-  }
-  if (hd <= 32) return launch_rope_as<T, 4, kChunks, NORM, BWD>(p, ctas, st);
-  if (hd <= 64) return launch_rope_as<T, 8, kChunks, NORM, BWD>(p, ctas, st);
-  if (hd <= 128) return launch_rope_as<T, 16, kChunks, NORM, BWD>(p, ctas, st);
-  return launch_rope_as<T, 32, kChunks, NORM, BWD>(p, ctas, st);
+template <typename T, int MODE, int S, bool NORM, bool BWD>
+cudaError_t launch_rope_wide(RopeParams& p, int (&ctas)[2], cudaStream_t st) {
+  const int lanes = (p.plan.head_dim + 2 * S - 1) / (2 * S);
+  if constexpr (S == 8)
+    if (lanes <= 2) return launch_rope_as<T, 2, MODE, S, NORM, BWD>(p, ctas, st);
+  if (lanes <= 4) return launch_rope_as<T, 4, MODE, S, NORM, BWD>(p, ctas, st);
+  if (lanes <= 8) return launch_rope_as<T, 8, MODE, S, NORM, BWD>(p, ctas, st);
+  if constexpr (S == 4)
+    if (lanes > 16) return launch_rope_as<T, 32, MODE, S, NORM, BWD>(p, ctas, st);
+  return launch_rope_as<T, 16, MODE, S, NORM, BWD>(p, ctas, st);
 }
 
-// How a lane's channels lie: see the top.  vector: elements that the tensors are aligned to.
-inline int rope_mode(const ress_rope_plan& plan, int vector) {
-  if (plan.head_dim % 8 != 0 || plan.n_pairs % 4 != 0) return kGather;
-  if (plan.layout == RESS_ROPE_INTERLEAVED) return vector % 8 == 0 ? kNeighbours : kGather;
-  if (plan.layout == RESS_ROPE_SECTIONS)
+// How a lane's channels lie (see the top) and how many slots it has, given the elements that the
+// tensors are aligned to.  8 slots want 16-bit elements, vectors of 8, and heads that fill a warp's
+// rows.
+template <typename T, bool NORM, bool BWD>
+cudaError_t launch_rope_typed(RopeParams& p, int vector, int (&ctas)[2], cudaStream_t st) {
+  const ress_rope_plan& plan = p.plan;
+  int run = vector;  // pairs of neighbouring channels that a lane can take as vectors
+  if (plan.layout == RESS_ROPE_INTERLEAVED)
+    run = vector % 8 == 0 ? 8 : 1;
+  else if (plan.layout == RESS_ROPE_SECTIONS)
     for (int a = 0; a < plan.n_axes; ++a)
-      if (plan.axis_dims[a] % 8 != 0) return kGather;
-  return vector % 4 == 0 ? kChunks : kGather;
+      while (run > 1 && plan.axis_dims[a] % (2 * run) != 0) run = run == 8 ? 4 : 1;
+  while (run > 1 && (plan.head_dim % (2 * run) != 0 || plan.n_pairs % run != 0)) run = run == 8 ? 4 : 1;
+  if constexpr (sizeof(T) == 2) {
+    int lanes = 2;
+    while (16 * lanes < plan.head_dim) lanes *= 2;
+    const int heads = 32 / lanes;
+    if (run == 8 && p.t[0].heads % heads == 0 && p.t[1].heads % heads == 0)
+      return plan.layout == RESS_ROPE_INTERLEAVED ? launch_rope_wide<T, kNeighbours, 8, NORM, BWD>(p, ctas, st)
+                                                  : launch_rope_wide<T, kChunks, 8, NORM, BWD>(p, ctas, st);
+  }
+  if (run > 1)
+    return plan.layout == RESS_ROPE_INTERLEAVED ? launch_rope_wide<T, kNeighbours, 4, NORM, BWD>(p, ctas, st)
+                                                : launch_rope_wide<T, kChunks, 4, NORM, BWD>(p, ctas, st);
+  return plan.head_dim <= 64 ? launch_rope_as<T, 8, kGather, 4, NORM, BWD>(p, ctas, st)
+                             : launch_rope_as<T, 32, kGather, 4, NORM, BWD>(p, ctas, st);
 }
 
 // The launch of the tensors whose norm is enabled, or of those where it is not; the others' head count
@@ -491,10 +512,9 @@ cudaError_t launch_rope_part(const RopeArgs& a, int (&ctas)[2], cudaStream_t st)
     if (BWD) fits(t.dx);
   }
   if (!any || p.tokens == 0) return cudaSuccess;
-  const int mode = rope_mode(a.plan, vector);
-  if (a.type == RESS_BF16) return launch_rope_typed<bf16, NORM, BWD>(p, mode, ctas, st);
-  if (a.type == RESS_F16) return launch_rope_typed<f16, NORM, BWD>(p, mode, ctas, st);
-  return launch_rope_typed<float, NORM, BWD>(p, mode, ctas, st);
+  if (a.type == RESS_BF16) return launch_rope_typed<bf16, NORM, BWD>(p, vector, ctas, st);
+  if (a.type == RESS_F16) return launch_rope_typed<f16, NORM, BWD>(p, vector, ctas, st);
+  return launch_rope_typed<float, NORM, BWD>(p, vector, ctas, st);
 }
 
 }  // namespace

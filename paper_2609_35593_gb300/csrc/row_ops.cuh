@@ -65,9 +65,9 @@ __device__ __forceinline__ Vec<T, E> load_vec(const T* p) {
     const uint4 v = ld_stream(reinterpret_cast<const uint4*>(p));
     r.w[0] = v.x, r.w[1] = v.y, r.w[2] = v.z, r.w[3] = v.w;
   } else {
-    static_assert(kBytes == 32, "vectors of 8, 16 or 32 bytes");
+    static_assert(kBytes % 16 == 0, "vectors of 8 bytes or whole 16");
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
+    for (int k = 0; k < kBytes / 16; ++k) {
       const uint4 v = reinterpret_cast<const uint4*>(p)[k];
       r.w[4 * k] = v.x, r.w[4 * k + 1] = v.y, r.w[4 * k + 2] = v.z, r.w[4 * k + 3] = v.w;
     }
