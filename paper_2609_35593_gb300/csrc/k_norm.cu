@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThr
   __shared__ float red[2 * 16 * R];
   constexpr int V = C / E, P = C / 2;
   // where elements take a register each, 32 channels leave no room for the next row and the parameters
-  constexpr bool kKeep = C < 32 || (E > 1 && sizeof(X) == 2);
+  constexpr bool kKeep = C < 32 || (E > 1 && sizeof(X) == 2), kAhead = kKeep || E > 1;
   const Team<TEAM> team;
   const Place<E, TEAM> at(team, p.width);
   const float inv = 1.f / (float)p.width;
@@ -147,16 +147,16 @@ __global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThr
   };
   // teams of a warp go through the loop together: their segments take part in each other's shuffles
   const int64_t first = team.index / (32 / kLanes<TEAM>) * (32 / kLanes<TEAM>);
-  if (kKeep) load(team.index * R);
+  if (kAhead) load(team.index * R);
   for (int64_t base = 0; (base + first) * R < p.rows; base += team.count) {
     const int64_t row0 = (base + team.index) * R;
-    if (!kKeep) load(row0);
+    if (!kAhead) load(row0);
     Vec<X, E> raw[R][V];
 #pragma unroll
     for (int k = 0; k < R; ++k)
 #pragma unroll
       for (int i = 0; i < V; ++i) raw[k][i] = next[k][i];
-    if (kKeep) load(row0 + team.count * R);
+    if (kAhead) load(row0 + team.count * R);
     // a thread's sums are scaled before the threads' meet: a row's sum may overflow where its average
     // does not
     float mean[R], rstd[R];
@@ -242,7 +242,7 @@ __global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThr
   __shared__ float red[2 * 16 * 2 * R];
   extern __shared__ float wide[];  // C = 32: the threads' gradient sums, each at its own places
   constexpr int V = C / E, P = C / 2;
-  constexpr bool kKeep = C == 8;
+  constexpr bool kKeep = C <= 16;
   const Team<TEAM> team;
   const Place<E, TEAM> at(team, p.width);
   const float inv = 1.f / (float)p.width;
@@ -379,8 +379,8 @@ __global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThr
       out[col] = v[0];
       out[p.width + col] = v[1];
     }
-  } else {  // at most 32 lanes of 8 channels
-    static_assert(C == 8, "8 channels per lane");
+  } else {
+    static_assert(kKeep, "a lane's sums are in registers");
     __shared__ float part[kNormThreads / 32][2][32 * C];
     const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
 #pragma unroll
@@ -461,20 +461,20 @@ int norm_resident(int threads, size_t smem) {
   return n;
 }
 
-template <bool BWD, typename X, typename Y, int E, int C, int TEAM>
+template <bool BWD, typename X, typename Y, int E, int C, int TEAM, bool ONE = false>
 cudaError_t launch_norm_as(const NormArgs& a, const NormParams& p, cudaStream_t st) {
   constexpr bool wide = sizeof(X) == 4 || E == 1;  // elements that take a register each as they lie
   const int threads = TEAM == kWholeCta ? ((p.width + C - 1) / C + 31) / 32 * 32 : kNormThreads;
   const int per_cta = TEAM == kWholeCta ? 1 : kNormThreads / kLanes<TEAM>;
   if constexpr (!BWD) {
-    constexpr int R = C == 32 ? 1 : wide ? 16 / C : 32 / C;
+    constexpr int R = C == 32 || ONE ? 1 : wide ? 16 / C : 32 / C;
     constexpr auto kern = k_layer_norm<X, Y, E, C, TEAM, R>;
     const int ctas = norm_ctas(norm_resident<kern>(threads, 0), per_cta, (p.rows + R - 1) / R, INT32_MAX);
     return launch_pdl(kern, ctas, threads, 0, st, true, p);
   } else {
-    constexpr int R = C == 32 || wide ? 1 : 2;
+    constexpr int R = C > 8 || wide ? 1 : 2;
     constexpr auto kern = k_layer_norm_bwd<X, Y, E, C, TEAM, R>;
-    const size_t smem = C == 8 ? 0 : 2 * C * sizeof(float) * threads;
+    const size_t smem = C <= 16 ? 0 : 2 * C * sizeof(float) * threads;
     cudaError_t e = cudaSuccess;
     if (smem > 0) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
@@ -491,8 +491,15 @@ cudaError_t launch_norm_typed(const NormArgs& a, const NormParams& p, bool vec, 
   constexpr int E = 16 / (int)sizeof(X);
   const int D = p.width;
   if (!vec) {
+    if (D <= 64) return launch_norm_as<BWD, X, Y, 1, 8, 8>(a, p, st);
+    if (D <= 128) return launch_norm_as<BWD, X, Y, 1, 8, 16>(a, p, st);
     if (D <= 256) return launch_norm_as<BWD, X, Y, 1, 8, 32>(a, p, st);
-    if (D <= 8 * kNormMaxThreads) return launch_norm_as<BWD, X, Y, 1, 8, kWholeCta>(a, p, st);
+    // one row at a time where the CTAs get large: rows of 2 leave one CTA of 9 warps per SM (21,961 x 2049
+    // bf16: 141 us and 117 one at a time; 44,955 x 1001: 82 and 96)
+    if (D <= 4 * kNormMaxThreads || (BWD && D <= 8 * kNormMaxThreads))
+      return launch_norm_as<BWD, X, Y, 1, 8, kWholeCta>(a, p, st);
+    if constexpr (!BWD)
+      if (D <= 8 * kNormMaxThreads) return launch_norm_as<BWD, X, Y, 1, 8, kWholeCta, true>(a, p, st);
     return launch_norm_as<BWD, X, Y, 1, 32, kWholeCta>(a, p, st);
   }
   if (D <= 64) return launch_norm_as<BWD, X, Y, E, 8, 8>(a, p, st);
@@ -500,13 +507,12 @@ cudaError_t launch_norm_typed(const NormArgs& a, const NormParams& p, bool vec, 
   if (D <= 256) return launch_norm_as<BWD, X, Y, E, 8, 32>(a, p, st);
   if constexpr (BWD) {
     if (D <= 8 * kNormMaxThreads) return launch_norm_as<BWD, X, Y, E, 8, kWholeCta>(a, p, st);
+    if (D <= 16 * kNormMaxThreads) return launch_norm_as<BWD, X, Y, E, 16, kWholeCta>(a, p, st);
   } else {
     if (D <= 512) return launch_norm_as<BWD, X, Y, E, 16, 32>(a, p, st);
-    if constexpr (sizeof(X) == 2) {
-      if (D <= 1024) return launch_norm_as<BWD, X, Y, E, 32, 32>(a, p, st);
-    } else {
+    if (D <= 1024) return launch_norm_as<BWD, X, Y, E, 32, 32>(a, p, st);
+    if constexpr (sizeof(X) == 4)
       if (D <= 16 * kNormMaxThreads) return launch_norm_as<BWD, X, Y, E, 16, kWholeCta>(a, p, st);
-    }
   }
   return launch_norm_as<BWD, X, Y, E, 32, kWholeCta>(a, p, st);
 }

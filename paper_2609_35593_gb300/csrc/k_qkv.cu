@@ -66,7 +66,7 @@ enum { kNoTurn = 0, kByPairs = -1 };
 
 struct QParams {
   int N, K, H;
-  int work;                // heads of all stripes
+  int step, units;         // heads of a unit, units
   int turn, pairs, axes;   // turn: h, kNoTurn or kByPairs
   uint8_t lo[32], hi[32];  // channels of each pair
   uint8_t axis[32];
@@ -125,32 +125,32 @@ __device__ __forceinline__ void q_group_sync(int group) {
       : "r"(at0), "r"(at1)                                  \
       : "memory")
 
-// The work is the heads of all stripes in a row (stripe, then Q, K, V, then head), and a pair's share
-// is a range of them, so that shares differ by one head at most, a call on few tokens has single heads
-// on many SMs, and a pair goes through its stripes' tiles one after the other (their x slices come from
-// L2 and their cosines and sines are formed once).  A unit is up to 4 heads of a range from `head` on,
-// to the next multiple of 4: one tile.
+// A unit is up to `step` heads of one of Q, K, V of one token stripe: one tile.  The units of all
+// stripes stand in a row (stripe, then Q, K, V, then head), and a pair's share is a range of them, so that
+// a pair goes through its stripes' tiles one after the other: their x slices come from L2 and their
+// cosines and sines are formed once.  step is 4, or fewer where each pair then still has one unit at
+// most: a call on few tokens has single heads on many SMs.
 struct QUnit {
   int mt, which, head, heads;
 };
 struct QCursor {
   int at, end;
   __device__ explicit QCursor(const QParams& p) {
-    const int pairs = (int)gridDim.x >> 1, i = (int)blockIdx.x >> 1, rest = p.work % pairs;
-    at = p.work / pairs * i + min(i, rest);
-    end = at + p.work / pairs + (i < rest);
+    const int pairs = (int)gridDim.x >> 1, i = (int)blockIdx.x >> 1, rest = p.units % pairs;
+    at = p.units / pairs * i + min(i, rest);
+    end = at + p.units / pairs + (i < rest);
   }
   __device__ bool more() const { return at < end; }
   __device__ QUnit unit(const QParams& p) const {
-    const int in_stripe = at % (3 * p.H);
+    const int per = (p.H + p.step - 1) / p.step, in_stripe = at % (3 * per);
     QUnit t;
-    t.mt = at / (3 * p.H);
-    t.which = in_stripe / p.H;
-    t.head = in_stripe % p.H;
-    t.heads = min(min(kQHeads - t.head % kQHeads, p.H - t.head), end - at);
+    t.mt = at / (3 * per);
+    t.which = in_stripe / per;
+    t.head = in_stripe % per * p.step;
+    t.heads = min(p.step, p.H - t.head);
     return t;
   }
-  __device__ void next(const QUnit& t) { at += t.heads; }
+  __device__ void next() { ++at; }
 };
 
 // One head of one token: 64 columns of this thread's TMEM lane, to its row of an output box.
@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(kQThreads, 1)
     bool failed = false;
     for (QCursor c(p); c.more() && !failed;) {
       const QUnit t = c.unit(p);
-      c.next(t);
+      c.next();
       const bool ahead = c.more() && c.unit(p).mt != t.mt;  // the next stripe into L2 meanwhile
       for (int ks = 0; ks < ksteps; ++ks, ++it) {
         const int s = it % kQStages, u = it / kQStages;
@@ -338,7 +338,7 @@ __global__ void __launch_bounds__(kQThreads, 1)
     }
     for (QCursor c(p); c.more() && !failed;) {
       const QUnit t = c.unit(p);
-      c.next(t);
+      c.next();
       const uint32_t idesc = idesc_bf16_f32(2 * kQM, 64 * t.heads, false);
       const int b = n & 1, use = n >> 1;  // the accumulator, its earlier uses
       ++n;
@@ -393,7 +393,7 @@ __global__ void __launch_bounds__(kQThreads, 1)
     int n = 0, boxes = 0, table = -1;  // units done; boxes this group has stored; the table's stripe
     for (QCursor c(p); c.more();) {
       const QUnit t = c.unit(p);
-      c.next(t);
+      c.next();
       const int b = n & 1, use = n >> 1;
       ++n;
       const int row0 = kQM * (2 * t.mt + rank), which = t.which, mode = which < 2 ? p.turn : kNoTurn;
@@ -512,7 +512,11 @@ cudaError_t launch_qkv_proj(const QkvArgs& a, cudaStream_t st) {
   p.N = a.N;
   p.K = a.Dm;
   p.H = a.H;
-  p.work = (a.N + 2 * kQM - 1) / (2 * kQM) * 3 * a.H;
+  const int pairs = max(1, rows::sm_count() / 2);
+  for (p.step = 1; p.step <= kQHeads; p.step *= 2) {
+    p.units = (a.N + 2 * kQM - 1) / (2 * kQM) * 3 * ((a.H + p.step - 1) / p.step);
+    if (p.step == kQHeads || p.units <= pairs) break;
+  }
   p.turn = kNoTurn;
   if (a.rotate) {
     const ress_rope_plan& plan = a.plan;
@@ -548,7 +552,7 @@ cudaError_t launch_qkv_proj(const QkvArgs& a, cudaStream_t st) {
   static_assert(kQOffCtl + sizeof(QCtl) + 1024 <= 227 * 1024, "shared memory of a CTA");
   cudaError_t e = cudaFuncSetAttribute(k_qkv, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
-  return launch_with(k_qkv, 2 * min(p.work, max(1, rows::sm_count() / 2)), kQThreads, smem, st, true, 2, m, p);
+  return launch_with(k_qkv, 2 * min(p.units, pairs), kQThreads, smem, st, true, 2, m, p);
 }
 
 }  // namespace ress

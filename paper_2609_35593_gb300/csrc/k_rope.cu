@@ -5,9 +5,8 @@
 namespace ress {
 
 cudaError_t launch_rope(const RopeArgs& a, cudaStream_t st) {
-  int ctas[2];
-  const cudaError_t e = launch_rope_part<true, false>(a, ctas, st);
-  return e != cudaSuccess ? e : launch_rope_part<false, false>(a, ctas, st);
+  int first[3];
+  return launch_rope_all<false>(a, first, st);
 }
 
 }  // namespace ress

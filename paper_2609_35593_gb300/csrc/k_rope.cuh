@@ -13,8 +13,10 @@
 // neighbouring channels (kChunks) or 2 S neighbours (kNeighbours) they are read and written as
 // vectors, else one by one (kGather).  An item is one token and up to K rows of 32 / G of its heads
 // of one tensor, and a warp has the next item's elements on their way while it works on one.  A CTA
-// stays with Q or K (shares of the grid by their heads), and its lanes keep the norm's parameters
-// and their gradients' sums in registers.  The token's cosines and sines are formed once per item,
+// stays with Q or K (shares of the grid by their cost), and its lanes keep the norm's parameters
+// and their gradients' sums in registers.  Where the heads fit into one row (FEW), a row has as
+// many tokens as it has room for, and an item K such rows (1 head of 32 channels, a row of 8 for each: 13
+// times the bytes' time).  The token's cosines and sines are formed once per item,
 // one pair per lane, and handed out through shared memory.  Sums are float32 in a fixed order; the
 // gradients of the parameters are summed per CTA and then over CTAs by a second kernel.
 #pragma once
@@ -23,11 +25,6 @@
 
 namespace ress {
 using namespace rows;
-
-namespace {
-
-constexpr int kRopeWarps = 4;
-constexpr int kRopeThreads = 32 * kRopeWarps;
 
 enum { kChunks = 0, kNeighbours = 1, kGather = 2 };
 
@@ -46,11 +43,30 @@ struct RopeParams {
   const int32_t* pos;
   float* partial;
   float eps;
-  int first_ctas;  // CTAs of t[0]; the others have t[1]
+  int most;           // CTAs at most
+  int first_ctas;     // CTAs of t[0]; the others have t[1]
   int param_type;
   bool whole_tokens;  // a warp takes all of a token's items
   bool all;           // every channel has a pair
 };
+
+// Which kernel a tensor gets; tensors of one kind share a launch.
+struct RopeKind {
+  bool norm, few;   // few: several tokens per item
+  int mode, slots;  // S
+  int tokens;       // that fit into a row
+  bool operator==(const RopeKind& k) const {
+    return norm == k.norm && few == k.few && mode == k.mode && slots == k.slots;
+  }
+};
+
+// The launches of tensors of one kind (p.t with 0 heads: absent); ctas: of each.  Few: k_rope_few.cu.
+cudaError_t launch_rope_few(bool bwd, const RopeKind& kind, int type, RopeParams& p, int (&ctas)[2], cudaStream_t st);
+
+namespace {
+
+constexpr int kRopeWarps = 4;
+constexpr int kRopeThreads = 32 * kRopeWarps;
 
 // The channels of a slot.  Slots past the pairs have channels without one, if any are left: two
 // neighbours, or (kChunks) those of a lane's S slots as S and S neighbours.
@@ -142,13 +158,14 @@ struct Slots {
   }
 };
 
-template <typename T, int G, int MODE, int S, bool NORM, bool BWD, int K>
+template <typename T, int G, int MODE, int S, bool NORM, bool BWD, bool FEW, int K>
 __global__ void __launch_bounds__(kRopeThreads, (!NORM ? 6 : BWD ? 3 : 4) - (S == 8 ? 1 : 0)) k_rope(const __grid_constant__ RopeParams p) {
   constexpr int kHeads = 32 / G;              // heads of a warp's row
   constexpr int kPairs = G * S <= 32 ? 1 : G * S / 32;  // pairs per lane: G S pairs at most
   constexpr int Q = S / 2;
   constexpr bool kReadX = !BWD || NORM;
-  __shared__ __align__(16) float cosines[kRopeWarps][32 * kPairs], sines[kRopeWarps][32 * kPairs];
+  constexpr int kMostTokens = FEW ? K * kHeads : 1;  // tokens of an item
+  __shared__ __align__(16) float cosines[kRopeWarps][kMostTokens][G * S], sines[kRopeWarps][kMostTokens][G * S];
   const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
   const bool second = (int)blockIdx.x >= p.first_ctas;
   // (one field at a time: an index into the parameters would be looked up at each use)
@@ -182,14 +199,36 @@ __global__ void __launch_bounds__(kRopeThreads, (!NORM ? 6 : BWD ? 3 : 4) - (S =
   slots.first = a[0];
   slots.next = b[0];
   const bool turns = slot < p.plan.n_pairs;  // kGather: slots turn one by one
-  // The pairs whose angles this lane forms.
+  // FEW: a row has row_tokens tokens, this lane's group the head my_head of the one of number my_token,
+  // and an item has K such rows.
+  const int row_tokens = FEW ? kHeads / heads : 1, item_tokens = FEW ? K * row_tokens : 1;
+  const int my_token = FEW ? group / heads : 0, my_head = FEW ? group % heads : group;
+  // The pairs whose angles this lane forms: of one token at a time, or (fewer than 32 pairs) of several.
+  int span_pairs = 32;
+  while (FEW && span_pairs / 2 >= p.plan.n_pairs) span_pairs /= 2;
+  const int first_pair = lane % span_pairs;
   uint64_t freq[kPairs];
   int axis[kPairs];
 #pragma unroll
   for (int q = 0; q < kPairs; ++q) {
-    const int k = min(lane + 32 * q, p.plan.n_pairs - 1);
+    const int k = min(first_pair + 32 * q, p.plan.n_pairs - 1);
     freq[q] = p.plan.turns[k];
     axis[q] = rope_axis(p.plan, k);
+  }
+  auto angle = [&](int token, int q, int32_t at) {  // of a token of the item
+    const float2 cs = rope_cos_sin(at, freq[q]);
+    if (first_pair + 32 * q < p.plan.n_pairs) {
+      cosines[warp][token][first_pair + 32 * q] = cs.x;
+      sines[warp][token][first_pair + 32 * q] = BWD ? -cs.y : cs.y;
+    }
+  };
+
+  // Slots without a pair, and lanes without channels, turn by nothing: their sums stay what they are.
+  if (p.plan.n_pairs < G * S) {
+    for (int i = lane; i < kMostTokens * G * S; i += 32) {
+      cosines[warp][0][i] = 1.f;
+      sines[warp][0][i] = 0.f;
+    }
   }
 
   stream_acquire();
@@ -218,51 +257,83 @@ __global__ void __launch_bounds__(kRopeThreads, (!NORM ? 6 : BWD ? 3 : 4) - (S =
   const int span = p.whole_tokens ? chunks : 1, spans = chunks / span;
   const int64_t warps = (int64_t)(second ? gridDim.x - p.first_ctas : p.first_ctas) * kRopeWarps;
   const int64_t w0 = (int64_t)(blockIdx.x - (second ? p.first_ctas : 0)) * kRopeWarps + warp;
-  const int64_t step = warps / spans;
-  const int step_rest = (int)(warps - step * spans);
-  int64_t token = w0 / spans;
-  int chunk = (int)(w0 - token * spans) * span, left = span;  // left: items of the span from this one on
-  // the next item's rows and positions are on their way while this one is worked on
+  const int64_t step = warps / spans * item_tokens;
+  const int step_rest = (int)(warps % spans);
+  int64_t token = w0 / spans * item_tokens;
+  int chunk = (int)(w0 % spans) * span, left = span;  // left: items of the span from this one on
+  // from row to row of an item, and to this lane's place in the first
+  auto row_step = [&](int64_t token_stride, int64_t head_stride) {
+    return FEW ? row_tokens * token_stride : kHeads * head_stride;
+  };
+  auto place = [&](int64_t token_stride, int64_t head_stride) {
+    return (token + my_token) * token_stride + (chunk * K * kHeads + my_head) * head_stride;
+  };
+  // whether this lane's head of row k exists
+  auto lives = [&](int64_t at, int ch, int k) {
+    if (FEW) return my_token < row_tokens && at + k * row_tokens + my_token < p.tokens;
+    return at < p.tokens && (ch * K + k) * kHeads + group < heads;
+  };
+  const int64_t x_step = row_step(t.x_token, t.x_head), y_step = row_step(t.y_token, t.y_head);
+  const int64_t out_step = row_step(t.out_token, t.out_head);
+  // the next item's rows (and, a token by itself, its positions) are on their way while this one is
+  // worked on
   Vec<T, 2 * S> next_x[kReadX ? K : 1], next_y[BWD ? K : 1];
-  int32_t pos[kPairs];
+  constexpr int kAhead = FEW && kPairs == 1 ? K : kPairs;
+  int32_t pos[kAhead];
+  const int sweep = FEW ? 32 / span_pairs : 1, sweep_token = FEW ? lane / span_pairs : 0;  // tokens per sweep of the lanes
+  auto position = [&](int64_t item, int i, int q) {  // of this lane's token of sweep i
+    const int64_t at = item + i * sweep + sweep_token;
+    return at < p.tokens ? p.pos[at * p.plan.n_axes + axis[q]] : 0;
+  };
   auto load = [&]() {
-    const bool live = token < p.tokens;
-    const int h0 = chunk * K * kHeads + group;
     const T *px = nullptr, *py = nullptr;
-    if constexpr (kReadX) px = static_cast<const T*>(t.x) + token * t.x_token + h0 * t.x_head;
-    if constexpr (BWD) py = static_cast<const T*>(t.y) + token * t.y_token + h0 * t.y_head;
+    if constexpr (kReadX) px = static_cast<const T*>(t.x) + place(t.x_token, t.x_head);
+    if constexpr (BWD) py = static_cast<const T*>(t.y) + place(t.y_token, t.y_head);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const bool row = live && h0 + k * kHeads < heads;
-      if constexpr (kReadX) next_x[k] = slots.load(px + k * kHeads * t.x_head, row);
-      if constexpr (BWD) next_y[k] = slots.load(py + k * kHeads * t.y_head, row);
+      const bool live = lives(token, chunk, k);
+      if constexpr (kReadX) next_x[k] = slots.load(px + k * x_step, live);
+      if constexpr (BWD) next_y[k] = slots.load(py + k * y_step, live);
     }
+    if constexpr (kPairs == 1) {
 #pragma unroll
-    for (int q = 0; q < kPairs; ++q) pos[q] = live ? p.pos[token * p.plan.n_axes + axis[q]] : 0;
+      for (int i = 0; i < kAhead; ++i)
+        if (i == 0 || i * sweep < item_tokens) pos[i] = position(token, i, 0);
+    } else {
+#pragma unroll
+      for (int q = 0; q < kPairs; ++q) pos[q] = position(token, 0, q);
+    }
   };
   load();
 #pragma unroll 1
   while (token < p.tokens) {
     Vec<T, 2 * S> x[kReadX ? K : 1], y[BWD ? K : 1];
-    float2 cs[kPairs];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       if constexpr (kReadX) x[k] = next_x[k];
       if constexpr (BWD) y[k] = next_y[k];
     }
-    if (left == span) {  // the token's angles
+    if (left == span) {  // the angles of the item's tokens, once the last one's are read
+      __syncwarp();
+      if constexpr (kPairs == 1) {
 #pragma unroll
-      for (int q = 0; q < kPairs; ++q) cs[q] = rope_cos_sin(pos[q], freq[q]);
-      __syncwarp();  // the last token's are read
+        for (int i = 0; i < kAhead; ++i)
+          if (i * sweep + sweep_token < item_tokens) angle(i * sweep + sweep_token, 0, pos[i]);
+        for (int i = kAhead; i * sweep < item_tokens; ++i)
+          if (i * sweep + sweep_token < item_tokens) angle(i * sweep + sweep_token, 0, position(token, i, 0));
+      } else {
 #pragma unroll
-      for (int q = 0; q < kPairs; ++q) {
-        cosines[warp][lane + 32 * q] = cs[q].x;
-        sines[warp][lane + 32 * q] = BWD ? -cs[q].y : cs[q].y;
+        for (int q = 0; q < kPairs; ++q) angle(0, q, pos[q]);
+        for (int i = 1; i < item_tokens; ++i) {
+#pragma unroll
+          for (int q = 0; q < kPairs; ++q) angle(i, q, position(token, i, q));
+        }
       }
       __syncwarp();
     }
-    const int head0 = chunk * K * kHeads + group;
-    T* const out = static_cast<T*>(t.out) + token * t.out_token + head0 * t.out_head;
+    const int64_t token0 = token;
+    const int chunk0 = chunk;
+    T* const out = static_cast<T*>(t.out) + place(t.out_token, t.out_head);
     ++chunk;
     if (--left == 0) {
       left = span;
@@ -270,23 +341,27 @@ __global__ void __launch_bounds__(kRopeThreads, (!NORM ? 6 : BWD ? 3 : 4) - (S =
       token += step;
       if (chunk >= chunks) {
         chunk -= chunks;
-        ++token;
+        token += item_tokens;
       }
     }
     load();
     F2 co[Q], si[Q], neg[Q];
 #pragma unroll
-    for (int q = 0; q < Q; q += 2) {
-      const float4 c = *reinterpret_cast<const float4*>(&cosines[warp][slot + 2 * q]);
-      const float4 z = *reinterpret_cast<const float4*>(&sines[warp][slot + 2 * q]);
-      co[q] = pack2(c.x, c.y), co[q + 1] = pack2(c.z, c.w);
-      si[q] = pack2(z.x, z.y), si[q + 1] = pack2(z.z, z.w);
-      neg[q] = pack2(-z.x, -z.y), neg[q + 1] = pack2(-z.z, -z.w);
-    }
-#pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int head = head0 + k * kHeads;
-      if (head - group >= heads) break;  // no head of this row
+      // no head of this row
+      if (FEW ? token0 + k * row_tokens >= p.tokens : (chunk0 * K + k) * kHeads >= heads) break;
+      if (FEW || k == 0) {
+        const int at = FEW ? k * row_tokens + min(my_token, row_tokens - 1) : 0;
+#pragma unroll
+        for (int q = 0; q < Q; q += 2) {
+          const float4 c = *reinterpret_cast<const float4*>(&cosines[warp][at][slot + 2 * q]);
+          const float4 z = *reinterpret_cast<const float4*>(&sines[warp][at][slot + 2 * q]);
+          co[q] = pack2(c.x, c.y), co[q + 1] = pack2(c.z, c.w);
+          si[q] = pack2(z.x, z.y), si[q + 1] = pack2(z.z, z.w);
+          neg[q] = pack2(-z.x, -z.y), neg[q + 1] = pack2(-z.z, -z.w);
+        }
+      }
+      const bool live = lives(token0, chunk0, k);
       F2 h[2][Q], u[2][Q];
       float rstd = 1.f;
       if constexpr (NORM) {
@@ -350,7 +425,6 @@ __global__ void __launch_bounds__(kRopeThreads, (!NORM ? 6 : BWD ? 3 : 4) - (S =
         // rows past the last head and slots that do not exist have dy = 0 and add nothing, but h may
         // be anything where x is not read
         F2 sg = both(0.f), sgh = both(0.f);
-        const bool live = head < heads;
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -369,7 +443,7 @@ __global__ void __launch_bounds__(kRopeThreads, (!NORM ? 6 : BWD ? 3 : 4) - (S =
 #pragma unroll
           for (int q = 0; q < Q; ++q) u[s][q] = mul2(fma2(h[s][q], agh, add2(u[s][q], ag)), both(rstd));
       }
-      slots.store(out + k * kHeads * t.out_head, u, head < heads);
+      slots.store(out + k * out_step, u, live);
     }
   }
   stream_release();
@@ -404,28 +478,40 @@ __global__ void __launch_bounds__(kRopeThreads, (!NORM ? 6 : BWD ? 3 : 4) - (S =
   }
 }
 
-// CTAs of the two tensors of a launch; the forward's launch has no sums to fold.
-template <typename T, int G, int MODE, int S, bool NORM, bool BWD>
+template <typename T, int G, int MODE, int S, bool NORM, bool BWD, bool FEW>
 cudaError_t launch_rope_as(RopeParams& p, int (&ctas)[2], cudaStream_t st) {
   // Rows of an item, their elements in registers twice (43,968 tokens, 16 + 16 heads of 64, bf16, with a
   // norm: S = 4 and K = 4 67 us, K = 2 73; S = 8 and K = 2 66, K = 1 76; without one, 20,011 tokens,
   // 12 + 4 heads, S = 4: K = 4 22, K = 2 20.5; gradient with a norm, 10,992 tokens, both launches: S = 4 and
   // K = 2 36.5, K = 1 45; S = 8 and K = 2 33, K = 1 40).
   constexpr int K = S == 8 ? 2 : sizeof(T) == 2 ? (NORM && !BWD ? 4 : 2) : (NORM && BWD ? 1 : 2);
-  constexpr auto kern = k_rope<T, G, MODE, S, NORM, BWD, K>;
-  const int resident = resident_ctas<kern>(kRopeThreads, 0);
-  const int64_t fit = min((int64_t)resident * sm_count(), (int64_t)kRopeParts - 1);
+  constexpr int kHeads = 32 / G;
+  constexpr auto kern = k_rope<T, G, MODE, S, NORM, BWD, FEW, K>;
+  const int64_t fit = min((int64_t)resident_ctas<kern>(kRopeThreads, 0) * sm_count(), (int64_t)p.most);
   p.whole_tokens = p.tokens * ((p.t[0].heads > 0) + (p.t[1].heads > 0)) >= fit * kRopeWarps;
-  int64_t need[2], all = 0;  // CTAs at one visit per warp
+  // CTAs at one visit (a token's items, or an item) per warp, and what a visit costs: an item about a row,
+  // a lane's angle about half of one
+  int64_t need[2], all = 0;
+  double cost[2];
   for (int i = 0; i < 2; ++i) {
-    const int chunks = (p.t[i].heads + K * (32 / G) - 1) / (K * (32 / G));
-    need[i] = (p.tokens * (p.whole_tokens ? min(chunks, 1) : chunks) + kRopeWarps - 1) / kRopeWarps;
+    const int heads = p.t[i].heads, rows = (heads + kHeads - 1) / kHeads, chunks = (rows + K - 1) / K;
+    int64_t visits = 0;
+    cost[i] = 0.0;
+    if (heads > 0 && FEW) {
+      const int tokens = K * (kHeads / heads);
+      visits = (p.tokens + tokens - 1) / tokens;
+      cost[i] = 1.0 + K + tokens * p.plan.n_pairs / 64.0;
+    } else if (heads > 0) {
+      visits = p.tokens * (p.whole_tokens ? 1 : chunks);
+      cost[i] = p.whole_tokens ? chunks + rows + 0.5 : 1.5 + min(rows, K);
+    }
+    cost[i] *= visits;
+    need[i] = (visits + kRopeWarps - 1) / kRopeWarps;
     all += need[i];
   }
-  // shares of what fits at once by the tensors' heads, with the same number of items for each warp
+  // shares of what fits at once by the tensors' costs, with the same number of visits for each warp of one
   for (int i = 0; i < 2; ++i) {
-    const int64_t heads = p.t[0].heads + p.t[1].heads;
-    const int64_t share = all <= fit ? need[i] : max(fit * p.t[i].heads / heads, (int64_t)1);
+    const int64_t share = all <= fit ? need[i] : max((int64_t)(fit * (cost[i] / (cost[0] + cost[1]))), (int64_t)1);
     const int64_t steps = need[i] == 0 ? 1 : (need[i] + share - 1) / share;
     ctas[i] = (int)((need[i] + steps - 1) / steps);
   }
@@ -434,50 +520,83 @@ cudaError_t launch_rope_as(RopeParams& p, int (&ctas)[2], cudaStream_t st) {
   return launch_pdl(kern, ctas[0] + ctas[1], kRopeThreads, 0, st, true, p);
 }
 
-template <typename T, int MODE, int S, bool NORM, bool BWD>
+template <typename T, int MODE, int S, bool NORM, bool BWD, bool FEW>
 cudaError_t launch_rope_wide(RopeParams& p, int (&ctas)[2], cudaStream_t st) {
   const int lanes = (p.plan.head_dim + 2 * S - 1) / (2 * S);
   if constexpr (S == 8)
-    if (lanes <= 2) return launch_rope_as<T, 2, MODE, S, NORM, BWD>(p, ctas, st);
-  if (lanes <= 4) return launch_rope_as<T, 4, MODE, S, NORM, BWD>(p, ctas, st);
-  if (lanes <= 8) return launch_rope_as<T, 8, MODE, S, NORM, BWD>(p, ctas, st);
-  if constexpr (S == 4)
-    if (lanes > 16) return launch_rope_as<T, 32, MODE, S, NORM, BWD>(p, ctas, st);
-  return launch_rope_as<T, 16, MODE, S, NORM, BWD>(p, ctas, st);
+    if (lanes <= 2) return launch_rope_as<T, 2, MODE, S, NORM, BWD, FEW>(p, ctas, st);
+  if (lanes <= 4) return launch_rope_as<T, 4, MODE, S, NORM, BWD, FEW>(p, ctas, st);
+  if (lanes <= 8) return launch_rope_as<T, 8, MODE, S, NORM, BWD, FEW>(p, ctas, st);
+  if constexpr (S == 4 && !FEW)
+    if (lanes > 16) return launch_rope_as<T, 32, MODE, S, NORM, BWD, FEW>(p, ctas, st);
+  return launch_rope_as<T, 16, MODE, S, NORM, BWD, FEW>(p, ctas, st);
 }
 
-// How a lane's channels lie (see the top) and how many slots it has, given the elements that the
-// tensors are aligned to.  8 slots want 16-bit elements, vectors of 8, and heads that fill a warp's
-// rows.
-template <typename T, bool NORM, bool BWD>
-cudaError_t launch_rope_typed(RopeParams& p, int vector, int (&ctas)[2], cudaStream_t st) {
-  const ress_rope_plan& plan = p.plan;
-  int run = vector;  // pairs of neighbouring channels that a lane can take as vectors
-  if (plan.layout == RESS_ROPE_INTERLEAVED)
-    run = vector % 8 == 0 ? 8 : 1;
-  else if (plan.layout == RESS_ROPE_SECTIONS)
-    for (int a = 0; a < plan.n_axes; ++a)
-      while (run > 1 && plan.axis_dims[a] % (2 * run) != 0) run = run == 8 ? 4 : 1;
-  while (run > 1 && (plan.head_dim % (2 * run) != 0 || plan.n_pairs % run != 0)) run = run == 8 ? 4 : 1;
-  if constexpr (sizeof(T) == 2) {
-    int lanes = 2;
-    while (16 * lanes < plan.head_dim) lanes *= 2;
-    const int heads = 32 / lanes;
-    if (run == 8 && p.t[0].heads % heads == 0 && p.t[1].heads % heads == 0)
-      return plan.layout == RESS_ROPE_INTERLEAVED ? launch_rope_wide<T, kNeighbours, 8, NORM, BWD>(p, ctas, st)
-                                                  : launch_rope_wide<T, kChunks, 8, NORM, BWD>(p, ctas, st);
+template <typename T, bool NORM, bool BWD, bool FEW>
+cudaError_t launch_rope_mode(const RopeKind& kind, RopeParams& p, int (&ctas)[2], cudaStream_t st) {
+  if constexpr (sizeof(T) == 2 && !FEW)
+    if (kind.slots == 8)
+      return kind.mode == kNeighbours ? launch_rope_wide<T, kNeighbours, 8, NORM, BWD, FEW>(p, ctas, st)
+                                      : launch_rope_wide<T, kChunks, 8, NORM, BWD, FEW>(p, ctas, st);
+  if constexpr (!FEW)
+    if (kind.mode == kGather) return launch_rope_wide<T, kGather, 4, NORM, BWD, FEW>(p, ctas, st);
+  return kind.mode == kNeighbours ? launch_rope_wide<T, kNeighbours, 4, NORM, BWD, FEW>(p, ctas, st)
+                                  : launch_rope_wide<T, kChunks, 4, NORM, BWD, FEW>(p, ctas, st);
+}
+
+template <bool BWD, bool FEW>
+cudaError_t launch_rope_kind(const RopeKind& kind, int type, RopeParams& p, int (&ctas)[2], cudaStream_t st) {
+  auto typed = [&](auto t) {
+    using T = decltype(t);
+    return kind.norm ? launch_rope_mode<T, true, BWD, FEW>(kind, p, ctas, st)
+                     : launch_rope_mode<T, false, BWD, FEW>(kind, p, ctas, st);
+  };
+  return type == RESS_BF16 ? typed(bf16()) : type == RESS_F16 ? typed(f16()) : typed(0.f);
+}
+
+// How a tensor's channels lie on the lanes (see the top): 8 slots want 16-bit elements, vectors of 8, and
+// heads that fill a warp's rows.
+inline RopeKind rope_kind(const RopeArgs& a, const ress_rope_heads& t, bool bwd) {
+  const ress_rope_plan& plan = a.plan;
+  const int bytes = a.type == RESS_F32 ? 4 : 2;
+  int run = 8;  // pairs of neighbouring channels that a lane can take as vectors: 8, 4 or 1
+  auto fits = [&](const ress_heads& h) {
+    const int align = min(run * bytes, 16);
+    return reinterpret_cast<uintptr_t>(h.data) % align == 0 &&
+           (a.n_tokens == 1 || h.token_stride * bytes % align == 0) &&
+           (t.n_heads == 1 || h.head_stride * bytes % align == 0);
+  };
+  auto possible = [&] {
+    if (plan.head_dim % (2 * run) != 0 || plan.n_pairs % run != 0) return false;
+    if (plan.layout == RESS_ROPE_SECTIONS)
+      for (int i = 0; i < plan.n_axes; ++i)
+        if (plan.axis_dims[i] % (2 * run) != 0) return false;
+    return ((bwd && !t.norm.enabled) || fits(t.x)) && fits(t.y) && (!bwd || fits(t.dx));
+  };
+  if (plan.layout == RESS_ROPE_INTERLEAVED) {  // a lane's vectors are as long as 8 channels all the same
+    const bool aligned = ((bwd && !t.norm.enabled) || fits(t.x)) && fits(t.y) && (!bwd || fits(t.dx));
+    while (run > 1 && (plan.head_dim % (2 * run) != 0 || plan.n_pairs % run != 0)) run = run == 8 ? 4 : 1;
+    if (!aligned) run = 1;
+  } else {
+    while (run > 1 && !possible()) run = run == 8 ? 4 : 1;
   }
-  if (run > 1)
-    return plan.layout == RESS_ROPE_INTERLEAVED ? launch_rope_wide<T, kNeighbours, 4, NORM, BWD>(p, ctas, st)
-                                                : launch_rope_wide<T, kChunks, 4, NORM, BWD>(p, ctas, st);
-  return plan.head_dim <= 64 ? launch_rope_as<T, 8, kGather, 4, NORM, BWD>(p, ctas, st)
-                             : launch_rope_as<T, 32, kGather, 4, NORM, BWD>(p, ctas, st);
+  RopeKind k;
+  k.norm = t.norm.enabled != 0;
+  k.mode = run == 1 ? kGather : plan.layout == RESS_ROPE_INTERLEAVED ? kNeighbours : kChunks;
+  int lanes = 2;  // of 8 slots
+  while (16 * lanes < plan.head_dim) lanes *= 2;
+  k.slots = run == 8 && bytes == 2 && t.n_heads % (32 / lanes) == 0 ? 8 : 4;
+  int row = 8;  // heads of a row, of lanes of 4 slots
+  while (row > 1 && plan.head_dim > 256 / row) row /= 2;
+  k.tokens = row / t.n_heads;
+  k.few = k.slots == 4 && k.mode != kGather && row > 1 && k.tokens > 0;
+  return k;
 }
 
-// The launch of the tensors whose norm is enabled, or of those where it is not; the others' head count
-// is 0 in it.  ctas: of each tensor; any: whether there are such tensors.
-template <bool NORM, bool BWD>
-cudaError_t launch_rope_part(const RopeArgs& a, int (&ctas)[2], cudaStream_t st) {
+// All launches; first[i]..first[i + 1]: the CTAs of tensor i that leave partial sums of its norm's
+// gradients.
+template <bool BWD>
+cudaError_t launch_rope_all(const RopeArgs& a, int (&first)[3], cudaStream_t st) {
   RopeParams p;
   p.plan = a.plan;
   p.tokens = a.n_tokens;
@@ -485,36 +604,45 @@ cudaError_t launch_rope_part(const RopeArgs& a, int (&ctas)[2], cudaStream_t st)
   p.eps = a.eps;
   p.param_type = a.param_type;
   p.all = 2 * a.plan.n_pairs == a.plan.head_dim;
-  p.partial = NORM && BWD ? a.partial : nullptr;
-  ctas[0] = ctas[1] = 0;
-  const int bytes = a.type == RESS_F32 ? 4 : 2;
-  int vector = 8;  // 8, 4 or 1 elements
-  bool any = false;
+  RopeTensor tensors[2];
+  RopeKind kinds[2];
   for (int i = 0; i < 2; ++i) {
     const ress_rope_heads& t = a.t[i];
-    p.t[i] = RopeTensor{};
-    if (t.n_heads == 0 || (t.norm.enabled != 0) != NORM) continue;
-    any = true;
     const ress_heads& out = BWD ? t.dx : t.y;
-    p.t[i] = RopeTensor{t.n_heads,        t.norm.weight,   t.norm.bias,    t.x.data,         t.y.data,
-                        out.data,         t.x.token_stride, t.x.head_stride, t.y.token_stride, t.y.head_stride,
-                        out.token_stride, out.head_stride};
-    auto fits = [&](const ress_heads& h) {
-      for (; vector > 1; vector = vector == 8 ? 4 : 1) {
-        const int align = min(vector * bytes, 16);
-        if (reinterpret_cast<uintptr_t>(h.data) % align == 0 &&
-            (a.n_tokens == 1 || h.token_stride * bytes % align == 0) && (t.n_heads == 1 || h.head_stride * bytes % align == 0))
-          return;
-      }
-    };
-    if (!BWD || NORM) fits(t.x);
-    fits(t.y);
-    if (BWD) fits(t.dx);
+    tensors[i] = RopeTensor{t.n_heads,        t.norm.weight,    t.norm.bias,     t.x.data,         t.y.data,
+                            out.data,         t.x.token_stride, t.x.head_stride, t.y.token_stride, t.y.head_stride,
+                            out.token_stride, out.head_stride};
+    if (t.n_heads > 0) kinds[i] = rope_kind(a, t, BWD);
   }
-  if (!any || p.tokens == 0) return cudaSuccess;
-  if (a.type == RESS_BF16) return launch_rope_typed<bf16, NORM, BWD>(p, vector, ctas, st);
-  if (a.type == RESS_F16) return launch_rope_typed<f16, NORM, BWD>(p, vector, ctas, st);
-  return launch_rope_typed<float, NORM, BWD>(p, vector, ctas, st);
+  first[0] = first[1] = first[2] = 0;
+  if (p.tokens == 0) return cudaSuccess;
+  // One launch is worth more than several tokens per item with a token per row (20,011 tokens, 12 + 4 heads:
+  // 22 us together, 31 apart).
+  if (a.t[0].n_heads > 0 && a.t[1].n_heads > 0 && kinds[0].few != kinds[1].few) {
+    RopeKind& few = kinds[kinds[0].few ? 0 : 1];
+    if (few.tokens == 1) few.few = false;
+  }
+  const bool together = a.t[0].n_heads > 0 && a.t[1].n_heads > 0 && kinds[0] == kinds[1];
+  p.most = together ? kRopeParts - 1 : kRopeParts / 2 - 1;
+  for (int i = 0; i < 2; ++i) {
+    first[i + 1] = max(first[i], first[i + 1]);
+    if (a.t[i].n_heads == 0 || (together && i == 1)) continue;
+    p.t[i] = tensors[i];
+    p.t[1 - i] = together ? tensors[1 - i] : RopeTensor{};
+    p.partial = BWD && kinds[i].norm && a.partial ? a.partial + (int64_t)first[i] * 2 * p.plan.head_dim : nullptr;
+    int ctas[2] = {0, 0};
+    const cudaError_t e = kinds[i].few ? launch_rope_few(BWD, kinds[i], a.type, p, ctas, st)
+                                       : launch_rope_kind<BWD, false>(kinds[i], a.type, p, ctas, st);
+    if (e != cudaSuccess) return e;
+    if (!p.partial) continue;
+    if (together) {
+      first[1] = ctas[0];
+      first[2] = ctas[0] + ctas[1];
+    } else {
+      first[i + 1] = first[i] + ctas[i];
+    }
+  }
+  return cudaSuccess;
 }
 
 }  // namespace

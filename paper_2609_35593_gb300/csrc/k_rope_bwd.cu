@@ -40,20 +40,15 @@ __global__ void __launch_bounds__(32 * kRopeFoldWarps) k_rope_fold(const RopeFol
 }  // namespace
 
 cudaError_t launch_rope_bwd(const RopeArgs& a, cudaStream_t st) {
-  int ctas[2], none[2];
-  cudaError_t e = launch_rope_part<false, true>(a, none, st);
-  if (e == cudaSuccess) e = launch_rope_part<true, true>(a, ctas, st);
-  if (e != cudaSuccess || !a.partial) return e;
   RopeFoldParams f;
+  const cudaError_t e = launch_rope_all<true>(a, f.first, st);
+  if (e != cudaSuccess || !a.partial) return e;
   f.partial = a.partial;
   for (int i = 0; i < 2; ++i) {
     const bool norm = a.t[i].n_heads > 0 && a.t[i].norm.enabled;
     f.out[2 * i] = norm ? a.t[i].dweight : nullptr;
     f.out[2 * i + 1] = norm ? a.t[i].dbias : nullptr;
   }
-  f.first[0] = 0;
-  f.first[1] = ctas[0];
-  f.first[2] = ctas[0] + ctas[1];
   f.hd = a.plan.head_dim;
   return launch_pdl(k_rope_fold, dim3((f.hd + 31) / 32, 4), 32 * kRopeFoldWarps, 0, st, true, f);
 }

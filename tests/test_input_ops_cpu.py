@@ -193,7 +193,7 @@ def test_binding_refuses():
 
 # ---- sources ---------------------------------------------------------------------------------
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2609_35593_gb300", "csrc")
-FILES = ["k_norm.cu", "k_rope.cuh", "k_rope.cu", "k_rope_bwd.cu", "k_qkv.cu", "row_ops.cuh"]
+FILES = ["k_norm.cu", "k_rope.cuh", "k_rope.cu", "k_rope_bwd.cu", "k_rope_few.cu", "k_qkv.cu", "row_ops.cuh"]
 
 
 def code(name):
