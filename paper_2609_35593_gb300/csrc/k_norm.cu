@@ -60,6 +60,12 @@ struct Team {
     index = (int64_t)blockIdx.x * per_cta + (TEAM == kWholeCta ? 0 : (int)threadIdx.x / kLanes<TEAM>);
     count = (int64_t)gridDim.x * per_cta;
   }
+  // The row that the first team of this warp is at: teams of a warp go through their loop together,
+  // because their lanes take part in each other's shuffles.
+  __device__ int64_t lead(int64_t row, int rows) const {
+    if constexpr (kLanes<TEAM> == 32) return row;
+    return row - (int)(threadIdx.x % 32) / kLanes<TEAM> * rows;
+  }
 };
 
 // Sums over a team's threads of N values each: over the warp's lanes, then over the CTA's warps
@@ -113,7 +119,8 @@ __device__ __forceinline__ void load_row(Vec<T, E> (&r)[V], const void* p, int64
 }
 
 template <typename X, typename Y, int E, int C, int TEAM, int R>
-__global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThreads) k_layer_norm(const NormParams p) {
+__global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThreads, TEAM == kWholeCta ? 1 : 4)
+    k_layer_norm(const NormParams p) {
   __shared__ float red[2 * 16 * R];
   constexpr int V = C / E, P = C / 2;
   // where elements take a register each, 32 channels leave no room for the next row and the parameters
@@ -145,11 +152,8 @@ __global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThr
 #pragma unroll
     for (int k = 0; k < R; ++k) load_row<X, E, V>(next[k], p.x, row0 + k, p.x_stride, at, row0 + k < p.rows);
   };
-  // teams of a warp go through the loop together: their segments take part in each other's shuffles
-  const int64_t first = team.index / (32 / kLanes<TEAM>) * (32 / kLanes<TEAM>);
   if (kAhead) load(team.index * R);
-  for (int64_t base = 0; (base + first) * R < p.rows; base += team.count) {
-    const int64_t row0 = (base + team.index) * R;
+  for (int64_t row0 = team.index * R; team.lead(row0, R) < p.rows; row0 += team.count * R) {
     if (!kAhead) load(row0);
     Vec<X, E> raw[R][V];
 #pragma unroll
@@ -281,10 +285,8 @@ __global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThr
       next_rstd[k] = live ? p.rstd[row] : 0.f;
     }
   };
-  const int64_t first = team.index / (32 / kLanes<TEAM>) * (32 / kLanes<TEAM>);
   if (kAhead) load(team.index * R);
-  for (int64_t base = 0; (base + first) * R < p.rows; base += team.count) {
-    const int64_t row0 = (base + team.index) * R;
+  for (int64_t row0 = team.index * R; team.lead(row0, R) < p.rows; row0 += team.count * R) {
     if (!kAhead) load(row0);
     Vec<X, E> x[R][V], res[R][V];
     Vec<Y, E> dy[R][V];
