@@ -501,13 +501,6 @@ bool make_map(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int 
 }  // namespace
 
 cudaError_t launch_qkv_proj(const QkvArgs& a, cudaStream_t st) {
-  QMaps m;
-  const int64_t out = (int64_t)a.H * 64;
-  if (!make_map(&m.x, a.x, a.N, a.Dm, kQM)) return cudaErrorInvalidValue;
-  for (int i = 0; i < 3; ++i)
-    if (!make_map(&m.w[i], a.W[i], out, a.Dm, 32 * kQHeads) || !make_map(&m.w_part[i], a.W[i], out, a.Dm, 32) ||
-        !make_map(&m.out[i], a.out[i], a.N, out, kQM))
-      return cudaErrorInvalidValue;
   QParams p{};
   p.N = a.N;
   p.K = a.Dm;
@@ -517,6 +510,19 @@ cudaError_t launch_qkv_proj(const QkvArgs& a, cudaStream_t st) {
     p.units = (a.N + 2 * kQM - 1) / (2 * kQM) * 3 * ((a.H + p.step - 1) / p.step);
     if (p.step == kQHeads || p.units <= pairs) break;
   }
+  // a map takes the host a good part of what the GPU needs for a few tokens: those that the units use
+  QMaps m;
+  const int64_t out = (int64_t)a.H * 64;
+  const bool whole = p.step == kQHeads && a.H >= kQHeads, part = p.step < kQHeads || a.H % kQHeads != 0;
+  bool made = make_map(&m.x, a.x, a.N, a.Dm, kQM);
+  for (int i = 0; i < 3; ++i) {
+    if (whole) made = made && make_map(&m.w[i], a.W[i], out, a.Dm, 32 * kQHeads);
+    if (part) made = made && make_map(&m.w_part[i], a.W[i], out, a.Dm, 32);
+    if (!whole) m.w[i] = m.w_part[i];
+    if (!part) m.w_part[i] = m.w[i];
+    made = made && make_map(&m.out[i], a.out[i], a.N, out, kQM);
+  }
+  if (!made) return cudaErrorInvalidValue;
   p.turn = kNoTurn;
   if (a.rotate) {
     const ress_rope_plan& plan = a.plan;
