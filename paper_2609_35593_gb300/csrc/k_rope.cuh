@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(kRopeThreads, (!NORM ? 6 : BWD ? 3 : 4) - (S =
   const int my_token = FEW ? group / heads : 0, my_head = FEW ? group % heads : group;
   // The pairs whose angles this lane forms: of one token at a time, or (fewer than 32 pairs) of several.
   int span_pairs = 32;
-  while (FEW && span_pairs / 2 >= p.plan.n_pairs) span_pairs /= 2;
+  while (FEW && kPairs == 1 && span_pairs / 2 >= p.plan.n_pairs) span_pairs /= 2;
   const int first_pair = lane % span_pairs;
   uint64_t freq[kPairs];
   int axis[kPairs];

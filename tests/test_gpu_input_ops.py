@@ -336,6 +336,59 @@ def test_rope_and_gradient(ress, hd, axes, layout, kind):
                     within(dx[n], d, rounded(d, kind) + derr, "d" + n)
 
 
+@pytest.mark.parametrize("hd,axes,layout", [
+    (128, (32,), "halves"), (128, (16, 8, 8), "sections"), (80, (8, 12, 12), "interleaved"), (80, (16, 16), "halves"),
+    (64, (16, 16), "sections"), (64, (64,), "sections"), (32, (8, 8), "interleaved"), (32, (32,), "halves"),
+    (96, (96,), "halves"), (24, (8, 8), "sections")])
+@pytest.mark.parametrize("kind", [BF16, F32])
+def test_rope_with_few_heads(ress, hd, axes, layout, kind):
+    """Heads that leave room for several tokens in a row of a warp, beside heads that do not; gradients
+    against those of 16 copies of each head, which fill their rows."""
+    plan = ress.rope_plan(axes, head_dim=hd, base=50.0, layout=layout)
+    for tokens, hq, hk in ((1, 1, 1), (2, 2, 1), (203, 16, 1), (90, 1, 3), (57, 3, 2), (1500, 4, 1)):
+        g = gen(tokens + hd)
+        pos = torch.randint(-50, 150, (tokens, len(axes)), generator=g, device="cuda", dtype=torch.int32)
+        x = {"q": normal(g, tokens, hq, hd).to(kind), "k": normal(g, tokens, hk, hd).to(kind)}
+        dy = {n: (0.2 * normal(g, *t.shape)).to(kind) for n, t in x.items()}
+        w, b = 1 + 0.3 * normal(g, hd), 0.2 * normal(g, hd)
+        for norm in (None, (w, b)):
+            out, dx = ({n: torch.full_like(t, float("nan")) for n, t in x.items()} for _ in range(2))
+            grads = torch.full((4, hd), float("nan"), device="cuda")
+            ws = torch.empty(ress.rope_workspace_bytes(plan, tokens, hq, hk), dtype=torch.uint8, device="cuda")
+            ress.rope(plan, pos, x["q"], out["q"], x["k"], out["k"], q_norm=norm, k_norm=norm)
+            kw = {}
+            if norm:
+                kw = dict(q=x["q"], k=x["k"], q_norm=norm, k_norm=norm, q_norm_grads=(grads[0], grads[1]),
+                          k_norm_grads=(grads[2], grads[3]), ws=ws)
+            ress.rope_bwd(plan, pos, dy["q"], dx["q"], dy["k"], dx["k"], **kw)
+            for i, n in enumerate("qk"):
+                u, mag = x[n].double(), 0
+                if norm:
+                    h, _, rstd, u = norm64(x[n].double(), w.double(), b.double(), 1e-5)
+                    spread = norm_bound(x[n].double(), h, w.double(), b.double(), rstd)
+                else:
+                    spread = torch.zeros_like(u)
+                want, mag = rotate64(u, pos, axes, layout, 50.0)
+                within(out[n], want, rounded(want, kind) + TURN * mag + rotate_bound(spread, axes, layout), n)
+                d, mag = rotate64(dy[n].double(), pos, axes, layout, 50.0, sign=-1.0)
+                if not norm:
+                    within(dx[n], d, rounded(d, kind) + TURN * mag, "d" + n)
+                    continue
+                # 16 heads fill their rows: each head beside 15 copies of itself, token by token
+                wide, dwide = (t.repeat_interleave(16, 1).contiguous() for t in (x[n], dy[n]))
+                dwide_x = torch.empty_like(wide)
+                ress.rope_bwd(plan, pos, dwide, dwide_x, q=wide, q_norm=norm)
+                ref = dwide_x.view(tokens, -1, 16, hd)[:, :, 0].double()
+                # the two may add a row's channels in another order
+                size = dx[n].double().abs().mean(-1, keepdim=True) + ref.abs()
+                within(dx[n], ref, 2 * rounded(ref, kind) + 8 * E * (size + rstd * (d * w.double()).abs()), "d" + n)
+                hw = norm_bound(x[n].double(), h, torch.ones_like(w.double()), torch.zeros_like(b.double()), rstd)
+                depth = (tokens * x[n].shape[1] / 16 + 256) * U32
+                flat = lambda v: v.flatten(0, 1).sum(0)
+                within(grads[2 * i], flat(d * h), flat(depth * (d * h).abs() + TURN * mag * h.abs() + d.abs() * hw) + 1e-30, "dw")
+                within(grads[2 * i + 1], flat(d), flat(depth * d.abs() + TURN * mag) + 1e-30, "db")
+
+
 def rotate_bound(e, axes, layout):
     """Errors of the channels after a rotation of channels with errors e."""
     out = e.clone()
