@@ -3,8 +3,8 @@
 Argument marshalling only: every function here checks the tensors it is given (device,
 dtype, contiguity), passes raw pointers and the current CUDA stream to the function of the
 same name in include/ress.h, and turns a negative return code into RessError.  All
-arithmetic runs in the library's CUDA kernels; if libress.so is missing the import fails
-(build it with `python -m paper_2609_35593_gb300.build` or __graft_entry__.build()).
+arithmetic runs in the library's CUDA kernels (the newer operators' questions about tensors
+are asked in C++, by _tensors.so); if libress.so is missing the import fails (build it with `python -m paper_2609_35593_gb300.build` or __graft_entry__.build()).
 """
 from __future__ import annotations
 
@@ -384,22 +384,31 @@ def status(ws, stream=None):
 
 
 # ---- the input half of the sublayer ---------------------------------------------------
-# Small calls take a few microseconds on the GPU, so a tensor that is as it should be is asked for each
-# fact once, and why another one is not is found out afterwards.
-_CODES = {}  # torch dtype -> ress_dtype
+# Small calls take a few microseconds on the GPU, so csrc/tensors.cpp asks a tensor all that matters in one
+# call, and why one is not as it should be is found out afterwards.
+class _Tensors:
+    """Stands in for the module _tensors until its first use: the rest of the binding needs no torch."""
+
+    def __getattr__(self, name):
+        _torch()
+        from . import _tensors
+        globals()["_t"] = _tensors
+        return getattr(_tensors, name)
+
+
+_t = _Tensors()
+_ANY, _F32, _BF16 = 0b0111, 0b0100, 0b1001  # bits of ress_dtype; bit 3: 16-bit integers
 
 
 def _types():
-    if not _CODES:
-        torch = _torch()
-        _CODES.update({torch.bfloat16: 0, torch.float16: 1, torch.float32: 2})
-    return _CODES
+    torch = _torch()
+    return (torch.bfloat16, torch.float16, torch.float32)
 
 
 def _code(t, name):
-    code = (_CODES or _types()).get(getattr(t, "dtype", None))
+    code = None if t is None else _t.code(t)
     if code is None:
-        _refuse(t, name, dtypes=tuple(_types()))
+        _refuse(t, name, dtypes=_types())
     return code
 
 
@@ -420,80 +429,63 @@ def _refuse(t, name, dtypes=None, shape=None, numel=None):
 
 def _vector(t, n, name):
     """Device pointer of n contiguous elements of one of the types (None -> NULL)."""
-    if t is None:
-        return 0
-    try:
-        if t.is_cuda and t.numel() == n and t.is_contiguous() and t.dtype in (_CODES or _types()):
-            return t.data_ptr()
-    except AttributeError:
-        pass
-    _refuse(t, name, tuple(_types()), numel=n)
+    p = _t.vector(t, n, _ANY)
+    if p is None:
+        _refuse(t, name, _types(), numel=n)
+    return p
 
 
 def _vector_f32(t, n, name):
-    if t is None:
-        return 0
-    try:
-        if t.is_cuda and t.numel() == n and t.is_contiguous() and (_CODES or _types()).get(t.dtype) == 2:
-            return t.data_ptr()
-    except AttributeError:
-        pass
-    _refuse(t, name, (_torch().float32,), numel=n)
+    p = _t.vector(t, n, _F32)
+    if p is None:
+        _refuse(t, name, _types()[2:], numel=n)
+    return p
 
 
-def _rows(t, shape, name):
-    """Device pointer and elements between the rows of a tensor [..., width] of this shape."""
-    try:
-        if t.is_cuda and t.shape == shape:
-            if t.is_contiguous():
-                return t.data_ptr(), shape[-1]
-            if len(shape) == 2 and (t.stride(1) == 1 or shape[1] == 1):
-                return t.data_ptr(), t.stride(0)
-    except AttributeError:
-        pass
-    _refuse(t, name, shape=shape)
+def _rows(t, like, name):
+    """Device pointer and elements between the rows of a tensor [..., width] of like's shape."""
+    r = _t.rows(t, like)
+    if r is None:
+        _refuse(t, name, shape=like.shape)
+    return r
 
 
 def _param_code(*params):
     """The one ress_dtype of the parameters that are given (float32 if none is)."""
-    code = None
-    for p in params:
-        if p is not None:
-            c = _code(p, "weight or bias")
-            if code is not None and c != code:
-                raise TypeError("weights and biases of different dtypes")
-            code = c
-    return 2 if code is None else code
+    code = _t.code(*params)
+    if code is None:
+        for p in params:
+            if p is not None:
+                _code(p, "weight or bias")
+        raise TypeError("weights and biases of different dtypes")
+    return code
 
 
 def _scratch(ws):
     """Pointer and bytes of a workspace (None -> NULL, 0)."""
-    if ws is None:
-        return 0, 0
-    try:
-        if ws.is_cuda and ws.is_contiguous():
-            return ws.data_ptr(), ws.numel() * ws.element_size()
-    except AttributeError:
-        pass
-    _refuse(ws, "ws")
+    s = _t.scratch(ws)
+    if s is None:
+        _refuse(ws, "ws")
+    return s
 
 
 def _row_shape(x):
-    shape = getattr(x, "shape", None)
-    if shape is None:
-        _refuse(x, "x")
-    if len(shape) < 1 or shape[-1] < 1:
-        raise ValueError(f"x has shape {tuple(shape)}, expected [..., width]")
-    return shape
+    """Rows, width and ress_dtype of x [..., width]."""
+    s = _t.shape(x)
+    if s is None:
+        shape = getattr(x, "shape", (1,))
+        if len(shape) < 1 or shape[-1] < 1:
+            raise ValueError(f"x has shape {tuple(shape)}, expected [..., width]")
+        _refuse(x, "x", _types())
+    return s
 
 
 def layer_norm(x, weight, bias, y, eps: float = 1e-5, mean=None, rstd=None, stream=None):
     """ress_layer_norm over the last dimension of x [..., width] into y of the same shape; weight, bias
     [width] or None; mean, rstd: float32 outputs, one per row, for layer_norm_bwd, or None."""
-    shape = _row_shape(x)
-    (px, sx), (py, sy), width = _rows(x, shape, "x"), _rows(y, shape, "y"), shape[-1]
-    rows = x.numel() // width
-    n = _NORM.pack(rows, width, _code(x, "x"), _code(y, "y"), _param_code(weight, bias), eps, sx, sy, 0, 0)
+    rows, width, code = _row_shape(x)
+    (px, sx), (py, sy) = _rows(x, x, "x"), _rows(y, x, "y")
+    n = _NORM.pack(rows, width, code, _code(y, "y"), _param_code(weight, bias), eps, sx, sy, 0, 0)
     _check(_lib.ress_layer_norm(n, px, _vector(weight, width, "weight"), _vector(bias, width, "bias"), py,
                                 _vector_f32(mean, rows, "mean"), _vector_f32(rstd, rows, "rstd"),
                                 _stream(stream)))
@@ -510,11 +502,9 @@ def layer_norm_workspace_bytes(rows: int, width: int) -> int:
 def layer_norm_bwd(dy, x, weight, mean, rstd, dx, dweight=None, dbias=None, dres=None, ws=None, stream=None):
     """ress_layer_norm_bwd: dx (+ dres where given) and the float32 gradients of weight and bias
     (None to skip; ws is needed for them) from the gradient dy of layer_norm's y."""
-    shape = _row_shape(x)
-    (pdy, sdy), (px, sx), (pdx, sdx) = _rows(dy, shape, "dy"), _rows(x, shape, "x"), _rows(dx, shape, "dx")
-    pres, sres = (0, 0) if dres is None else _rows(dres, shape, "dres")
-    width, code = shape[-1], _code(x, "x")
-    rows = x.numel() // width
+    rows, width, code = _row_shape(x)
+    (pdy, sdy), (px, sx), (pdx, sdx) = _rows(dy, x, "dy"), _rows(x, x, "x"), _rows(dx, x, "dx")
+    pres, sres = (0, 0) if dres is None else _rows(dres, x, "dres")
     if dx.dtype != x.dtype or (dres is not None and dres.dtype != x.dtype):
         raise TypeError(f"dx and dres must have x's dtype {x.dtype}")
     if mean is None or rstd is None:
@@ -544,20 +534,6 @@ def rope_plan(axis_dims, head_dim: int = HEAD_DIM, base: float = 100.0, layout: 
     return plan
 
 
-def _heads(t, shape, dtype, name):
-    """Pointer and strides of a tensor [tokens, heads, head_dim] with contiguous channels (None: absent)."""
-    if t is None:
-        return 0, 0, 0
-    try:
-        if t.is_cuda and t.shape == shape and t.dtype == dtype:
-            st, sh, sc = t.stride()
-            if sc == 1:
-                return t.data_ptr(), st, sh
-    except AttributeError:
-        pass
-    _refuse(t, name, (dtype,), shape)
-
-
 def _head_norm(norm, n, name):
     """enabled, weight, bias of None or (weight, bias)."""
     if norm is None:
@@ -567,32 +543,36 @@ def _head_norm(norm, n, name):
 
 
 def _positions(plan, pos, tokens):
-    try:
-        if pos.is_cuda and pos.shape == (tokens, plan.n_axes) and pos.dtype == _torch().int32 and pos.is_contiguous():
-            return pos.data_ptr()
-    except AttributeError:
-        pass
-    _refuse(pos, "pos", (_torch().int32,), (tokens, plan.n_axes))
+    p = _t.positions(pos, tokens, plan.n_axes)
+    if p is None:
+        _refuse(pos, "pos", (_torch().int32,), (tokens, plan.n_axes))
+    return p
 
 
-def _rope_heads(plan, name, y, x, dx, norm, grads, shape, dtype):
-    """ress_rope_heads of one tensor."""
-    hd = plan.head_dim
+def _rope_heads(plan, name, like, y, x, dx, norm, grads, tokens, code):
+    """ress_rope_heads of one tensor [tokens, heads, head_dim] of the type of this code, as like is."""
+    h = _t.rope_heads(y, x, dx, norm, grads, tokens, plan.head_dim, code)
+    if h is None:
+        _refuse_heads(plan, name, like, (x, y, dx), norm, grads, tokens, code)
+    return h
+
+
+def _refuse_heads(plan, name, like, tensors, norm, grads, tokens, code):
+    hd, shape = plan.head_dim, like.shape
+    if len(shape) != 3 or shape[0] != tokens or shape[2] != hd:
+        raise ValueError(f"{name}: shape {tuple(shape)}, expected ({tokens}, heads, {hd})")
+    for t in tensors:
+        if t is not None and (getattr(t, "shape", None) != shape
+                              or _t.rope_heads(t, None, None, None, None, tokens, hd, code) is None):
+            _refuse(t, name, _types()[code:code + 1], shape)
+    _head_norm(norm, hd, name)
     dweight, dbias = (None, None) if grads is None else grads
-    return _ROPE_HEADS.pack(shape[1], *_head_norm(norm, hd, name), *_heads(x, shape, dtype, name),
-                            *_heads(y, shape, dtype, name), *_heads(dx, shape, dtype, name),
-                            _vector_f32(dweight, hd, name), _vector_f32(dbias, hd, name))
-
-
-def _rope_shape(plan, t, tokens, name):
-    shape = t.shape
-    if len(shape) != 3 or shape[0] != tokens or shape[2] != plan.head_dim:
-        raise ValueError(f"{name} has shape {tuple(shape)}, expected ({tokens}, heads, {plan.head_dim})")
-    return shape
+    _vector_f32(dweight, hd, name), _vector_f32(dbias, hd, name)
+    raise ValueError(f"{name}: norms and their gradients are tuples of two")
 
 
 def _norm_code(q_norm, k_norm):
-    return _param_code(*(() if q_norm is None else q_norm), *(() if k_norm is None else k_norm))
+    return _param_code(*(q_norm or ()), *(k_norm or ()))
 
 
 def rope(plan: RopePlan, pos, q, q_out, k=None, k_out=None, q_norm=None, k_norm=None, eps: float = 1e-5,
@@ -602,10 +582,9 @@ def rope(plan: RopePlan, pos, q, q_out, k=None, k_out=None, q_norm=None, k_norm=
     pos, int32 [tokens, axes]."""
     if q is None or q_out is None or (k is None) != (k_out is None) or (k is None and k_norm is not None):
         raise ValueError("q and q_out are needed, and k and k_out together")
-    tokens, code, dtype = pos.shape[0], _code(q, "q"), q.dtype
-    tq = _rope_heads(plan, "q, q_out or q_norm", q_out, q, None, q_norm, None, _rope_shape(plan, q, tokens, "q"), dtype)
-    tk = None if k is None else _rope_heads(plan, "k, k_out or k_norm", k_out, k, None, k_norm, None,
-                                            _rope_shape(plan, k, tokens, "k"), dtype)
+    tokens, code = pos.size(0), _code(q, "q")
+    tq = _rope_heads(plan, "q, q_out or q_norm", q, q_out, q, None, q_norm, None, tokens, code)
+    tk = None if k is None else _rope_heads(plan, "k, k_out or k_norm", k, k_out, k, None, k_norm, None, tokens, code)
     _check(_lib.ress_rope(plan, tokens, _positions(plan, pos, tokens), code, _norm_code(q_norm, k_norm), eps, tq, tk,
                           _stream(stream)))
 
@@ -626,25 +605,21 @@ def rope_bwd(plan: RopePlan, pos, dq_out, dq, dk_out=None, dk=None, q=None, k=No
         raise ValueError("dq_out and dq are needed, and dk_out and dk together")
     if (q_norm is not None and q is None) or (k_norm is not None and k is None):
         raise ValueError("a norm's gradient needs the norm's input")
-    tokens, code, dtype = pos.shape[0], _code(dq_out, "dq_out"), dq_out.dtype
-    tq = _rope_heads(plan, "q, dq, dq_out, q_norm or its gradients", dq_out, q, dq, q_norm, q_norm_grads,
-                     _rope_shape(plan, dq_out, tokens, "dq_out"), dtype)
-    tk = None if dk is None else _rope_heads(plan, "k, dk, dk_out, k_norm or its gradients", dk_out, k, dk, k_norm,
-                                             k_norm_grads, _rope_shape(plan, dk_out, tokens, "dk_out"), dtype)
+    tokens, code = pos.size(0), _code(dq_out, "dq_out")
+    tq = _rope_heads(plan, "q, dq, dq_out, q_norm or its gradients", dq_out, dq_out, q, dq, q_norm, q_norm_grads, tokens,
+                     code)
+    tk = None if dk is None else _rope_heads(plan, "k, dk, dk_out, k_norm or its gradients", dk_out, dk_out, k, dk,
+                                             k_norm, k_norm_grads, tokens, code)
     _check(_lib.ress_rope_bwd(plan, tokens, _positions(plan, pos, tokens), code, _norm_code(q_norm, k_norm), eps, tq,
                               tk, *_scratch(ws), _stream(stream)))
 
 
 def _dense(t, n, name):
     """Device pointer of n contiguous bf16 elements (None -> NULL)."""
-    if t is None:
-        return 0
-    try:
-        if t.is_cuda and t.numel() == n and t.is_contiguous() and ((_CODES or _types()).get(t.dtype) == 0 or t.dtype in _bf16()):
-            return t.data_ptr()
-    except AttributeError:
-        pass
-    _refuse(t, name, _bf16(), numel=n)
+    p = _t.vector(t, n, _BF16)
+    if p is None:
+        _refuse(t, name, _bf16(), numel=n)
+    return p
 
 
 def qkv_proj(d: Dims, x, W_q, W_k, W_v, Q, K, V, ws, b_q=None, b_k=None, b_v=None, plan: RopePlan = None, pos=None,

@@ -1,4 +1,5 @@
-"""Builds libress.so (the C-ABI library) in-tree with nvcc for sm_103a.
+"""Builds libress.so (the C-ABI library) in-tree with nvcc for sm_103a, and _tensors.so, the
+binding's questions about tensors, with the host compiler.
 
 Translation units are compiled in parallel into _build/ and linked into
 paper_2609_35593_gb300/libress.so.  A unit is recompiled when it or any header it may
@@ -7,10 +8,12 @@ include is newer than its object file.
 from __future__ import annotations
 
 import glob
+import importlib.util
 import os
 import platform
 import shutil
 import subprocess
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -19,6 +22,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 OBJDIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libress.so")
+TENSORS = os.path.join(HERE, "_tensors.so")
 SOURCES = ["ress_abi.cu", "k_select.cu", "k_attn.cu", "k_dot.cu", "k_yagg.cu", "k_oproj.cu",
            "k_norm.cu", "k_rope.cu", "k_rope_bwd.cu", "k_rope_few.cu",
            "k_qkv.cu"]
@@ -32,6 +36,16 @@ def nvcc() -> str:
     if not os.path.exists(exe):
         raise RuntimeError("nvcc not found: the CUDA toolkit is required to build libress.so")
     return exe
+
+
+def _tensors_command(src: str) -> list[str]:
+    """Compiles the one unit that knows torch's tensors (and Python); libress.so knows neither."""
+    torch = os.path.dirname(importlib.util.find_spec("torch").origin)
+    inc, lib = os.path.join(torch, "include"), os.path.join(torch, "lib")
+    includes = ["-I", INCLUDE, "-I", sysconfig.get_paths()["include"], "-isystem", inc, "-isystem",
+                os.path.join(inc, "torch", "csrc", "api", "include")]
+    return [shutil.which("g++") or "c++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", *includes, src, "-o", TENSORS,
+            "-L", lib, "-Wl,-rpath," + lib, "-ltorch_python", "-ltorch_cpu", "-lc10"]
 
 
 def _headers_mtime() -> float:
@@ -54,20 +68,24 @@ def build(force: bool = False, verbose: bool = False, extra_flags: list[str] | N
         o = os.path.join(OBJDIR, src.replace(".cu", ".o"))
         if force or not os.path.exists(o) or os.path.getmtime(o) < max(os.path.getmtime(s), hdr):
             jobs.append([nvcc(), *ARCH, *flags, "-c", s, "-o", o])
+    units = len(jobs)
+    s = os.path.join(CSRC, "tensors.cpp")
+    if force or not os.path.exists(TENSORS) or os.path.getmtime(TENSORS) < max(os.path.getmtime(s), hdr):
+        jobs.append(_tensors_command(s))
 
     def run(cmd):
         if verbose:
             print(" ".join(cmd), flush=True)
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
-            raise RuntimeError(f"nvcc failed:\n{' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
+            raise RuntimeError(f"build failed:\n{' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
         if verbose and (r.stdout or r.stderr):
             print(r.stdout, r.stderr, flush=True)
 
-    with ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+    with ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
         list(ex.map(run, jobs))
     objs = [os.path.join(OBJDIR, s.replace(".cu", ".o")) for s in SOURCES]
-    if jobs or not os.path.exists(LIB) or os.path.getmtime(LIB) < max(map(os.path.getmtime, objs)):
+    if units or not os.path.exists(LIB) or os.path.getmtime(LIB) < max(map(os.path.getmtime, objs)):
         run([nvcc(), *ARCH, "-shared", "-o", LIB, *objs])
     with open(stamp, "w") as f:
         f.write(machine)

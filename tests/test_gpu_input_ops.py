@@ -644,3 +644,70 @@ def test_results_do_not_depend_on_the_run(ress):
     for n in o:
         assert torch.equal(first[n], again[n]) and torch.equal(first[n], replayed[n]) and torch.equal(fresh[n], direct[n]), n
         assert not torch.equal(first[n], fresh[n]) and bool(first[n].isfinite().all()), n
+
+
+def test_binding_refuses_tensors(ress):
+    """What the binding finds wrong with tensors on the device, and that it says what."""
+    z = lambda *shape, dtype=F32: torch.zeros(*shape, device="cuda", dtype=dtype)
+    x, w, row = z(4, 64), z(64), z(4)
+    ws = torch.empty(ress.layer_norm_workspace_bytes(4, 64), dtype=torch.uint8, device="cuda")
+    ln, lb = ress.layer_norm, ress.layer_norm_bwd
+    for error, text, call in (
+            (TypeError, "x has dtype", lambda: ln(x.double(), None, None, x)),
+            (ValueError, "y must live", lambda: ln(x, None, None, x.cpu())),
+            (ValueError, "y has shape", lambda: ln(x, None, None, z(4, 63))),
+            (ValueError, "y must be contiguous", lambda: ln(x, None, None, z(64, 4).t())),
+            (ValueError, "x has shape", lambda: ln(z(4, 0), None, None, z(4, 0))),
+            (ValueError, "x has shape", lambda: ln(z(1)[0], None, None, x)),
+            (TypeError, "y must be a torch.Tensor", lambda: ln(x, None, None, None)),
+            (TypeError, "weight or bias has dtype", lambda: ln(x, w.double(), None, z(4, 64))),
+            (ValueError, "weight has 63", lambda: ln(x, z(63), None, z(4, 64))),
+            (ValueError, "bias must be contiguous", lambda: ln(x, w, z(128)[::2], z(4, 64))),
+            (TypeError, "different dtypes", lambda: ln(x, w, w.half(), z(4, 64))),
+            (TypeError, "mean has dtype", lambda: ln(x, w, w, z(4, 64), mean=row.half())),
+            (ValueError, "rstd has 3", lambda: ln(x, w, w, z(4, 64), rstd=z(3))),
+            (TypeError, "dx and dres", lambda: lb(x, x, w, row, row, x.half())),
+            (TypeError, "dx and dres", lambda: lb(x, x, w, row, row, z(4, 64), dres=x.half())),
+            (ValueError, "dres has shape", lambda: lb(x, x, w, row, row, z(4, 64), dres=z(3, 64))),
+            (ValueError, "mean and rstd", lambda: lb(x, x, w, None, row, z(4, 64))),
+            (ValueError, "ws must be contiguous", lambda: lb(x, x, w, row, row, z(4, 64), dweight=z(64), ws=ws[::2])),
+            (ress.RessError, "EWORKSPACE", lambda: lb(x, x, w, row, row, z(4, 64), dweight=z(64), ws=ws[:256]))):
+        with pytest.raises(error, match=text):
+            call()
+
+    plan, pos, q, p = ress.rope_plan((32, 32)), z(4, 2, dtype=torch.int32), z(4, 2, 64), z(64)
+    rope, rb = ress.rope, ress.rope_bwd
+    for error, text, call in (
+            (TypeError, "q has dtype", lambda: rope(plan, pos, q.double(), q.double())),
+            (TypeError, "has dtype", lambda: rope(plan, pos, q, q.half())),
+            (ValueError, "shape", lambda: rope(plan, pos, z(5, 2, 64), z(5, 2, 64))),
+            (ValueError, "shape", lambda: rope(plan, pos, z(4, 2, 32), z(4, 2, 32))),
+            (ValueError, "shape", lambda: rope(plan, pos, q, z(4, 3, 64))),
+            (ValueError, "contiguous", lambda: rope(plan, pos, q, z(4, 64, 2).transpose(1, 2))),
+            (ValueError, "must live", lambda: rope(plan, pos, q, q.cpu())),
+            (TypeError, "torch.Tensor", lambda: rope(plan, pos, q, [0.0])),
+            (TypeError, "pos has dtype", lambda: rope(plan, pos.long(), q, z(4, 2, 64))),
+            (ValueError, "pos has shape", lambda: rope(plan, z(4, 3, dtype=torch.int32), q, z(4, 2, 64))),
+            (ValueError, "pos must be contiguous", lambda: rope(plan, z(2, 4, dtype=torch.int32).t(), q, z(4, 2, 64))),
+            (ValueError, "has 63", lambda: rope(plan, pos, q, z(4, 2, 64), q_norm=(z(63), None))),
+            (TypeError, "has dtype", lambda: rope(plan, pos, q, z(4, 2, 64), q_norm=(p, p.double()))),
+            (TypeError, "different dtypes", lambda: rope(plan, pos, q, z(4, 2, 64), q_norm=(p, p.half()))),
+            (ValueError, "too many values", lambda: rope(plan, pos, q, z(4, 2, 64), q_norm=(p, p, p))),
+            (TypeError, "has dtype", lambda: rb(plan, pos, q, z(4, 2, 64), q=q, q_norm=(p, p), q_norm_grads=(p.half(), None))),
+            (ValueError, "has 65", lambda: rb(plan, pos, q, z(4, 2, 64), q=q, q_norm=(p, p), q_norm_grads=(None, z(65)))),
+            (ress.RessError, "ws is NULL", lambda: rb(plan, pos, q, z(4, 2, 64), q=q, q_norm=(p, p), q_norm_grads=(z(64), z(64))))):
+        with pytest.raises(error, match=text):
+            call()
+
+    d = ress.dims(100, 2, 0, 128)
+    t = z(100, 128, dtype=BF16)
+    wt, o, space = z(128, 128, dtype=BF16), z(100, 2, 64, dtype=BF16), torch.empty(ress.workspace_bytes(d), dtype=torch.uint8, device="cuda")
+    for error, text, call in (
+            (TypeError, "x has dtype", lambda: ress.qkv_proj(d, t.half(), wt, wt, wt, o, o.clone(), o.clone(), space)),
+            (ValueError, "W_v has", lambda: ress.qkv_proj(d, t, wt, wt, wt[:64], o, o.clone(), o.clone(), space)),
+            (ValueError, "K must be contiguous",
+             lambda: ress.qkv_proj(d, t, wt, wt, wt, o, z(2, 100, 64, dtype=BF16).transpose(0, 1), o.clone(), space)),
+            (ValueError, "ws must live", lambda: ress.qkv_proj(d, t, wt, wt, wt, o, o.clone(), o.clone(), space.cpu()))):
+        with pytest.raises(error, match=text):
+            call()
+    torch.cuda.synchronize()
