@@ -15,7 +15,12 @@
 //   backward  C = 8, because a thread keeps its channels' two gradient sums in registers: with C = 32
 //             they leave room for 8 warps per SM (80 us), with C = 8 for 16 (63 us, and a barrier per
 //             R = 2 rows).  Above 4096 channels C = 32, the sums in shared memory.
-// Rows that are no whole vectors of 16 bytes go element by element, C = 8 (32 above 4096 channels).
+// Rows that are no whole vectors of 16 bytes, or not aligned to them, are taken as the aligned vectors that they
+// have and the elements at their two edges, one to a thread (EDGES: 20,000 x 1021 bf16 22.5 us, and 37 element by
+// element; 3000 x 8191 28 and 123; 5003 x 1021 float32 to bf16 7.5 and 12.2; the gradient of the first 41 and 57;
+// rows of whole vectors take 16, 21, 7 and 30).  A team's rows are then a whole number of vectors apart, so that
+// its channels' parameters stay in registers all the same.  Up to 256 channels, for few rows, and where the tensors'
+// rows start at different places of a vector they go element by element, C = 8 (32 above 4096 channels).
 // The mean is subtracted before squares are taken (two sums, one after the other): rows with an offset
 // much larger than their spread keep their digits.  All sums are float32 in a fixed order.
 //
@@ -102,23 +107,62 @@ __device__ __forceinline__ void team_sum(float (&v)[N], float* red, int& turn) {
 
 // A thread's channels are vectors of E, a team's threads next to each other: vector i of thread t
 // starts at channel (t + i threads) E.
-template <int E, int TEAM>
+// EDGES: rows that start between vectors and need not be whole ones.  The channels before the row's first
+// aligned vector and after its last one, at most E - 1 each, go one to a thread beside its vectors.
+template <int E, int TEAM, bool EDGES>
 struct Place {
-  int first, step, width;
-  __device__ Place(const Team<TEAM>& team, int width_) : first(team.t * E), step(team.threads * E), width(width_) {}
+  int first, step, end;  // of the vectors
+  int edge;              // this thread's channel at an edge, or -1
+  __device__ Place(const Team<TEAM>& team, int width, int head) : first(team.t * E), step(team.threads * E), end(width), edge(-1) {
+    if (EDGES) {
+      const int tail = (width - head) % E, k = team.t - 8;
+      first += head;
+      end -= tail;
+      edge = team.t < head ? team.t : k >= 0 && k < tail ? end + k : -1;
+    }
+  }
   __device__ int col(int i) const { return first + i * (TEAM == kWholeCta ? step : TEAM * E); }
-  __device__ bool in(int i) const { return col(i) < width; }  // widths are whole vectors
+  __device__ bool in(int i) const { return col(i) < end; }
 };
 
-template <typename T, int E, int V, int TEAM>
-__device__ __forceinline__ void load_row(Vec<T, E> (&r)[V], const void* p, int64_t row, int64_t stride,
-                                         const Place<E, TEAM>& at, bool live) {
+// Elements before the first aligned vector of a row, the same for all rows of a team: they are team.count rows
+// apart, whole vectors.
+template <typename X, int E>
+__device__ __forceinline__ int head_of(const void* x, int64_t row, int64_t stride) {
+  return (int)(-(reinterpret_cast<uintptr_t>(x) / sizeof(X) + (uint64_t)(row * stride)) % E);
+}
+
+template <typename T, int E, int V, int TEAM, bool EDGES>
+__device__ __forceinline__ void load_row(Vec<T, E> (&r)[V], Vec<T, 1>& edge, const void* p, int64_t row, int64_t stride,
+                                         const Place<E, TEAM, EDGES>& at, bool live) {
   const T* x = static_cast<const T*>(p) + row * stride;
 #pragma unroll
   for (int i = 0; i < V; ++i) r[i] = live && at.in(i) ? load_vec<T, E>(x + at.col(i)) : zero_vec<T, E>();
+  if (EDGES) edge = live && at.edge >= 0 ? load_vec<T, 1>(x + at.edge) : zero_vec<T, 1>();
 }
 
-template <typename X, typename Y, int E, int C, int TEAM, int R>
+// E parameters at a channel that need not be a vector's.
+template <typename T, int E>
+__device__ __forceinline__ void params_each(const void* p, int col, float* out) {
+  T v[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) v[e] = static_cast<const T*>(p)[col + e];
+#pragma unroll
+  for (int e = 0; e < E; ++e) out[e] = to_f32(v[e]);
+}
+template <int E, bool EDGES>
+__device__ __forceinline__ void row_params(const void* p, int type, int col, float none, float* out) {
+  if (!EDGES || !p)
+    params_at<E>(p, type, col, none, out);
+  else if (type == RESS_F32)
+    params_each<float, E>(p, col, out);
+  else if (type == RESS_BF16)
+    params_each<bf16, E>(p, col, out);
+  else
+    params_each<f16, E>(p, col, out);
+}
+
+template <typename X, typename Y, int E, int C, int TEAM, int R, bool EDGES>
 __global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThreads, TEAM == kWholeCta ? 1 : 4)
     k_layer_norm(const NormParams p) {
   __shared__ float red[2 * 16 * R];
@@ -126,7 +170,9 @@ __global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThr
   // where elements take a register each, 32 channels leave no room for the next row and the parameters
   constexpr bool kKeep = C < 32 || (E > 1 && sizeof(X) == 2), kAhead = kKeep || E > 1;
   const Team<TEAM> team;
-  const Place<E, TEAM> at(team, p.width);
+  // a team's R rows are next to each other or (EDGES) as far apart as its visits
+  const int64_t start = EDGES ? team.index : team.index * R, gap = EDGES ? team.count : 1;
+  const Place<E, TEAM, EDGES> at(team, p.width, EDGES ? head_of<X, E>(p.x, team.index, p.x_stride) : 0);
   const float inv = 1.f / (float)p.width;
   int turn = 0;
   stream_acquire();
@@ -138,8 +184,8 @@ __global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThr
 #pragma unroll
       for (int e = 0; e < E; ++e) v[0][i * E + e] = v[1][i * E + e] = 0.f;
       if (!at.in(i)) continue;
-      params_at<E>(p.weight, p.param_type, at.col(i), 1.f, v[0] + i * E);
-      params_at<E>(p.bias, p.param_type, at.col(i), 0.f, v[1] + i * E);
+      row_params<E, EDGES>(p.weight, p.param_type, at.col(i), 1.f, v[0] + i * E);
+      row_params<E, EDGES>(p.bias, p.param_type, at.col(i), 0.f, v[1] + i * E);
     }
 #pragma unroll
     for (int j = 0; j < P; ++j) {
@@ -147,19 +193,29 @@ __global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThr
       b[j] = pack2(v[1][2 * j], v[1][2 * j + 1]);
     }
   }
+  float edge_w = 0.f, edge_b = 0.f;
+  if (EDGES && at.edge >= 0) {
+    edge_w = param_at(p.weight, p.param_type, at.edge, 1.f);
+    edge_b = param_at(p.bias, p.param_type, at.edge, 0.f);
+  }
   Vec<X, E> next[R][V];
+  Vec<X, 1> next_edge[R];
   auto load = [&](int64_t row0) {
 #pragma unroll
-    for (int k = 0; k < R; ++k) load_row<X, E, V>(next[k], p.x, row0 + k, p.x_stride, at, row0 + k < p.rows);
+    for (int k = 0; k < R; ++k)
+      load_row<X, E, V>(next[k], next_edge[k], p.x, row0 + k * gap, p.x_stride, at, row0 + k * gap < p.rows);
   };
-  if (kAhead) load(team.index * R);
-  for (int64_t row0 = team.index * R; team.lead(row0, R) < p.rows; row0 += team.count * R) {
+  if (kAhead) load(start);
+  for (int64_t row0 = start; team.lead(row0, EDGES ? 1 : R) < p.rows; row0 += team.count * R) {
     if (!kAhead) load(row0);
     Vec<X, E> raw[R][V];
+    float edge[R];
 #pragma unroll
-    for (int k = 0; k < R; ++k)
+    for (int k = 0; k < R; ++k) {
 #pragma unroll
       for (int i = 0; i < V; ++i) raw[k][i] = next[k][i];
+      if (EDGES) edge[k] = elem(next_edge[k], 0);
+    }
     if (kAhead) load(row0 + team.count * R);
     // a thread's sums are scaled before the threads' meet: a row's sum may overflow where its average
     // does not
@@ -169,7 +225,7 @@ __global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThr
       F2 s = both(0.f);
 #pragma unroll
       for (int j = 0; j < P; ++j) s = add2(s, pair_of(raw[k], j));
-      mean[k] = sum2(s) * inv;
+      mean[k] = (EDGES ? sum2(s) + edge[k] : sum2(s)) * inv;
     }
     team_sum<TEAM>(mean, red, turn);
 #pragma unroll
@@ -194,14 +250,15 @@ __global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThr
             s = fma2(d, d, s);
           }
         }
-        rstd[k] = sum2(s) * inv;
+        const float d = EDGES && at.edge >= 0 ? edge[k] - mean[k] : 0.f;
+        rstd[k] = fmaf(d, d, sum2(s)) * inv;
       }
     }
     team_sum<TEAM>(rstd, red, turn);
 #pragma unroll
     for (int k = 0; k < R; ++k) {
-      if (row0 + k >= p.rows) continue;
-      const int64_t row = row0 + k;
+      const int64_t row = row0 + k * gap;
+      if (row >= p.rows) continue;
       const float r = rsqrtf(rstd[k] + p.eps);
       Y* y = static_cast<Y*>(p.out) + row * p.y_stride;
 #pragma unroll
@@ -223,14 +280,15 @@ __global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThr
             unpack2(b[i / 2], a, c);
             v[1][0] = i % 2 ? c : a;
           } else {
-            params_at<E>(p.weight, p.param_type, at.col(i), 1.f, v[0]);
-            params_at<E>(p.bias, p.param_type, at.col(i), 0.f, v[1]);
+            row_params<E, EDGES>(p.weight, p.param_type, at.col(i), 1.f, v[0]);
+            row_params<E, EDGES>(p.bias, p.param_type, at.col(i), 0.f, v[1]);
           }
 #pragma unroll
           for (int e = 0; e < E; ++e) out[e] = fmaf((elem(raw[k][i], e) - mean[k]) * r, v[0][e], v[1][e]);
         }
         store_vec<Y, E>(y + at.col(i), out);
       }
+      if (EDGES && at.edge >= 0) y[at.edge] = from_f32<Y>(fmaf((edge[k] - mean[k]) * r, edge_w, edge_b));
       if (team.t == 0) {
         if (p.mean) p.mean[row] = mean[k];
         if (p.rstd) p.rstd[row] = r;
@@ -240,7 +298,7 @@ __global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThr
   stream_release();
 }
 
-template <typename X, typename Y, int E, int C, int TEAM, int R>
+template <typename X, typename Y, int E, int C, int TEAM, int R, bool EDGES>
 __global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThreads, TEAM == kWholeCta ? 1 : 4)
     k_layer_norm_bwd(const NormParams p) {
   __shared__ float red[2 * 16 * 2 * R];
@@ -248,7 +306,9 @@ __global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThr
   constexpr int V = C / E, P = C / 2;
   constexpr bool kKeep = C <= 16;
   const Team<TEAM> team;
-  const Place<E, TEAM> at(team, p.width);
+  // a team's R rows are next to each other or (EDGES) as far apart as its visits
+  const int64_t start = EDGES ? team.index : team.index * R, gap = EDGES ? team.count : 1;
+  const Place<E, TEAM, EDGES> at(team, p.width, EDGES ? head_of<X, E>(p.x, team.index, p.x_stride) : 0);
   const float inv = 1.f / (float)p.width;
   int turn = 0;
   stream_acquire();
@@ -258,8 +318,10 @@ __global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThr
   auto weights = [&](int i) {
 #pragma unroll
     for (int e = 0; e < E; ++e) w[i * E + e] = 0.f;
-    if (at.in(i)) params_at<E>(p.weight, p.param_type, at.col(i), 1.f, w + i * E);
+    if (at.in(i)) row_params<E, EDGES>(p.weight, p.param_type, at.col(i), 1.f, w + i * E);
   };
+  const float edge_w = EDGES && at.edge >= 0 ? param_at(p.weight, p.param_type, at.edge, 1.f) : 0.f;
+  float edge_dw = 0.f, edge_db = 0.f;
   if (kKeep) {
 #pragma unroll
     for (int i = 0; i < V; ++i) weights(i);
@@ -272,25 +334,28 @@ __global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThr
   constexpr bool kAhead = kKeep;  // the next rows fit in the registers too
   Vec<X, E> next_x[R][V], next_res[R][V];
   Vec<Y, E> next_dy[R][V];
+  Vec<X, 1> next_edge_x[R], next_edge_res[R];
+  Vec<Y, 1> next_edge_dy[R];
   float next_mean[R], next_rstd[R];
   auto load = [&](int64_t row0) {
 #pragma unroll
     for (int k = 0; k < R; ++k) {
-      const int64_t row = row0 + k;
+      const int64_t row = row0 + k * gap;
       const bool live = row < p.rows;
-      load_row<X, E, V>(next_x[k], p.x, row, p.x_stride, at, live);
-      load_row<Y, E, V>(next_dy[k], p.y, row, p.y_stride, at, live);
-      if (p.dres) load_row<X, E, V>(next_res[k], p.dres, row, p.dres_stride, at, live);
+      load_row<X, E, V>(next_x[k], next_edge_x[k], p.x, row, p.x_stride, at, live);
+      load_row<Y, E, V>(next_dy[k], next_edge_dy[k], p.y, row, p.y_stride, at, live);
+      if (p.dres) load_row<X, E, V>(next_res[k], next_edge_res[k], p.dres, row, p.dres_stride, at, live);
       next_mean[k] = live ? p.mean[row] : 0.f;
       next_rstd[k] = live ? p.rstd[row] : 0.f;
     }
   };
-  if (kAhead) load(team.index * R);
-  for (int64_t row0 = team.index * R; team.lead(row0, R) < p.rows; row0 += team.count * R) {
+  if (kAhead) load(start);
+  for (int64_t row0 = start; team.lead(row0, EDGES ? 1 : R) < p.rows; row0 += team.count * R) {
     if (!kAhead) load(row0);
     Vec<X, E> x[R][V], res[R][V];
     Vec<Y, E> dy[R][V];
     float r[R], mr[R];  // h = x r + mr
+    float edge_x[R], edge_res[R], edge_dy[R];
 #pragma unroll
     for (int k = 0; k < R; ++k) {
 #pragma unroll
@@ -301,6 +366,11 @@ __global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThr
       }
       mr[k] = next_mean[k];
       r[k] = next_rstd[k];
+      if (EDGES) {
+        edge_x[k] = elem(next_edge_x[k], 0);
+        edge_dy[k] = elem(next_edge_dy[k], 0);
+        edge_res[k] = p.dres ? elem(next_edge_res[k], 0) : 0.f;
+      }
     }
     if (kAhead) load(row0 + team.count * R);
     // h = (x - mean) r, in this order: the difference keeps the digits of rows far from 0
@@ -327,13 +397,22 @@ __global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThr
           for (int q = 0; q < 4; ++q) wide[(C * (q / 2) + 2 * j + q % 2) * team.threads + team.t] += v[q];
         }
       }
-      sums[2 * k] = sum2(sg) * inv;
-      sums[2 * k + 1] = sum2(sgh) * inv;
+      float g = sum2(sg), gh = sum2(sgh);
+      if (EDGES && at.edge >= 0) {
+        const float h = (edge_x[k] - mr[k]) * r[k], ge = edge_dy[k] * edge_w;
+        g += ge;
+        gh = fmaf(ge, h, gh);
+        edge_dw = fmaf(edge_dy[k], h, edge_dw);
+        edge_db += edge_dy[k];
+      }
+      sums[2 * k] = g * inv;
+      sums[2 * k + 1] = gh * inv;
     }
     team_sum<TEAM>(sums, red, turn);
 #pragma unroll
     for (int k = 0; k < R; ++k) {
-      if (row0 + k >= p.rows) continue;
+      const int64_t row = row0 + k * gap;
+      if (row >= p.rows) continue;
       const F2 ag = both(-sums[2 * k]), agh = both(-sums[2 * k + 1]), r2 = both(r[k]);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
@@ -354,7 +433,12 @@ __global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThr
           out[0] = r[k] * (g - sums[2 * k] - h * sums[2 * k + 1]);
           if (p.dres) out[0] += elem(res[k][i], 0);
         }
-        store_vec<X, E>(static_cast<X*>(p.out) + (row0 + k) * p.dx_stride + at.col(i), out);
+        store_vec<X, E>(static_cast<X*>(p.out) + row * p.dx_stride + at.col(i), out);
+      }
+      if (EDGES && at.edge >= 0) {
+        const float h = (edge_x[k] - mr[k]) * r[k], g = edge_dy[k] * edge_w;
+        const float d = r[k] * (g - sums[2 * k] - h * sums[2 * k + 1]);
+        static_cast<X*>(p.out)[row * p.dx_stride + at.edge] = from_f32<X>(p.dres ? d + edge_res[k] : d);
       }
     }
   }
@@ -363,10 +447,14 @@ __global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThr
   // the CTA's partial rows: segments of a warp, then (teams of up to a warp) the CTA's warps in order
   float* out = p.partial + (int64_t)blockIdx.x * 2 * p.width;
   if constexpr (TEAM == kWholeCta) {
+    if (EDGES && at.edge >= 0) {
+      out[at.edge] = edge_dw;
+      out[p.width + at.edge] = edge_db;
+    }
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const int col = at.col(c / E) + c % E;
-      if (col >= p.width) continue;
+      if (col >= at.end) continue;
       float v[2];
       if constexpr (kKeep) {
         float a, b;
@@ -382,7 +470,7 @@ __global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThr
       out[p.width + col] = v[1];
     }
   } else {
-    static_assert(kKeep, "a lane's sums are in registers");
+    static_assert(kKeep && !EDGES, "a lane's sums are in registers, of the same channels in every team");
     __shared__ float part[kNormThreads / 32][2][32 * C];
     const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
 #pragma unroll
@@ -449,6 +537,11 @@ int norm_ctas(int resident, int teams_per_cta, int64_t batches, int most) {
   return (int)((ctas + steps - 1) / steps);
 }
 
+// EDGES: a team's rows start at the same place of a vector if their distance, the teams of the grid, is a
+// multiple of its elements, `of` CTAs'.  kEdgeRows make at least that many.
+constexpr int kEdgeRows = 64;
+int same_heads(int ctas, int of) { return of <= 1 ? ctas : ctas / of * of; }
+
 // CTAs of a kernel that fit on an SM, for each number of warps, asked for once.
 template <auto kKernel>
 int norm_resident(int threads, size_t smem) {
@@ -463,24 +556,26 @@ int norm_resident(int threads, size_t smem) {
   return n;
 }
 
-template <bool BWD, typename X, typename Y, int E, int C, int TEAM, bool ONE = false>
+template <bool BWD, typename X, typename Y, int E, int C, int TEAM, bool ONE = false, bool EDGES = false>
 cudaError_t launch_norm_as(const NormArgs& a, const NormParams& p, cudaStream_t st) {
   constexpr bool wide = sizeof(X) == 4 || E == 1;  // elements that take a register each as they lie
   const int threads = TEAM == kWholeCta ? ((p.width + C - 1) / C + 31) / 32 * 32 : kNormThreads;
   const int per_cta = TEAM == kWholeCta ? 1 : kNormThreads / kLanes<TEAM>;
   if constexpr (!BWD) {
     constexpr int R = C == 32 || ONE ? 1 : wide ? 16 / C : 32 / C;
-    constexpr auto kern = k_layer_norm<X, Y, E, C, TEAM, R>;
-    const int ctas = norm_ctas(norm_resident<kern>(threads, 0), per_cta, (p.rows + R - 1) / R, INT32_MAX);
+    constexpr auto kern = k_layer_norm<X, Y, E, C, TEAM, R, EDGES>;
+    int ctas = norm_ctas(norm_resident<kern>(threads, 0), per_cta, (p.rows + R - 1) / R, INT32_MAX);
+    if (EDGES) ctas = same_heads(ctas, E / per_cta);
     return launch_pdl(kern, ctas, threads, 0, st, true, p);
   } else {
     constexpr int R = C > 8 || wide ? 1 : 2;
-    constexpr auto kern = k_layer_norm_bwd<X, Y, E, C, TEAM, R>;
+    constexpr auto kern = k_layer_norm_bwd<X, Y, E, C, TEAM, R, EDGES>;
     const size_t smem = C <= 16 ? 0 : 2 * C * sizeof(float) * threads;
     cudaError_t e = cudaSuccess;
     if (smem > 0) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    const int ctas = norm_ctas(norm_resident<kern>(threads, smem), per_cta, (p.rows + R - 1) / R, kNormParts);
+    int ctas = norm_ctas(norm_resident<kern>(threads, smem), per_cta, (p.rows + R - 1) / R, kNormParts);
+    if (EDGES) ctas = same_heads(ctas, E / per_cta);
     e = launch_pdl(kern, ctas, threads, smem, st, true, p);
     if (e != cudaSuccess || !p.partial) return e;
     return launch_pdl(k_fold_parts, (2 * p.width + 31) / 32, 32 * kFoldWarps, 0, st, true, p.partial, ctas,
@@ -489,9 +584,23 @@ cudaError_t launch_norm_as(const NormArgs& a, const NormParams& p, cudaStream_t 
 }
 
 template <bool BWD, typename X, typename Y>
-cudaError_t launch_norm_typed(const NormArgs& a, const NormParams& p, bool vec, cudaStream_t st) {
+cudaError_t launch_norm_typed(const NormArgs& a, const NormParams& p, bool vec, bool edges, cudaStream_t st) {
   constexpr int E = 16 / (int)sizeof(X);
   const int D = p.width;
+  if (!vec && edges && D > 256 && p.rows >= kEdgeRows) {
+    if constexpr (BWD) {
+      if (D <= 8 * kNormMaxThreads) return launch_norm_as<BWD, X, Y, E, 8, kWholeCta, false, true>(a, p, st);
+      if (D <= 16 * kNormMaxThreads) return launch_norm_as<BWD, X, Y, E, 16, kWholeCta, false, true>(a, p, st);
+    } else {
+      if (D <= 512) return launch_norm_as<BWD, X, Y, E, 16, 32, false, true>(a, p, st);
+      if constexpr (sizeof(X) == 4) {
+        if (D <= 16 * kNormMaxThreads) return launch_norm_as<BWD, X, Y, E, 16, kWholeCta, false, true>(a, p, st);
+      } else {
+        if (D <= 1024) return launch_norm_as<BWD, X, Y, E, 32, 32, false, true>(a, p, st);
+      }
+    }
+    return launch_norm_as<BWD, X, Y, E, 32, kWholeCta, false, true>(a, p, st);
+  }
   if (!vec) {
     if (D <= 64) return launch_norm_as<BWD, X, Y, 1, 8, 8>(a, p, st);
     if (D <= 128) return launch_norm_as<BWD, X, Y, 1, 8, 16>(a, p, st);
@@ -554,12 +663,19 @@ cudaError_t launch_norm(const NormArgs& a, cudaStream_t st) {
   const bool vec = p.width % E == 0 && fits_params(a.weight) && fits_params(a.bias) && fits(a.x, p.x_stride, xb) && fits(a.dy, p.y_stride, yb) &&
                    fits(a.dres, p.dres_stride, xb) &&
                    fits(a.out, BWD ? p.dx_stride : p.y_stride, BWD ? xb : yb);
+  // rows that start at any element, but all tensors' at the same one of a vector
+  const uintptr_t place = reinterpret_cast<uintptr_t>(a.x) / xb % E;
+  auto same = [&](const void* q, int64_t stride, int bytes) {
+    return !q || (reinterpret_cast<uintptr_t>(q) / bytes % E == place && (stride - p.x_stride) % E == 0);
+  };
+  const bool edges = same(a.dy, p.y_stride, yb) && same(a.dres, p.dres_stride, xb) &&
+                     same(a.out, BWD ? p.dx_stride : p.y_stride, BWD ? xb : yb);
   switch (a.n.x_type * 4 + a.n.y_type) {
-    case RESS_BF16 * 4 + RESS_BF16: return launch_norm_typed<BWD, bf16, bf16>(a, p, vec, st);
-    case RESS_F16 * 4 + RESS_F16: return launch_norm_typed<BWD, f16, f16>(a, p, vec, st);
-    case RESS_F32 * 4 + RESS_BF16: return launch_norm_typed<BWD, float, bf16>(a, p, vec, st);
-    case RESS_F32 * 4 + RESS_F16: return launch_norm_typed<BWD, float, f16>(a, p, vec, st);
-    default: return launch_norm_typed<BWD, float, float>(a, p, vec, st);
+    case RESS_BF16 * 4 + RESS_BF16: return launch_norm_typed<BWD, bf16, bf16>(a, p, vec, edges, st);
+    case RESS_F16 * 4 + RESS_F16: return launch_norm_typed<BWD, f16, f16>(a, p, vec, edges, st);
+    case RESS_F32 * 4 + RESS_BF16: return launch_norm_typed<BWD, float, bf16>(a, p, vec, edges, st);
+    case RESS_F32 * 4 + RESS_F16: return launch_norm_typed<BWD, float, f16>(a, p, vec, edges, st);
+    default: return launch_norm_typed<BWD, float, float>(a, p, vec, edges, st);
   }
 }
 

@@ -159,6 +159,54 @@ def test_layer_norm_strides_and_alignment(ress, x_type):
             assert bool((out == 7.0).all())  # nothing written beside the rows
 
 
+@pytest.mark.parametrize("width", [257, 263, 511, 1023, 1025, 2049, 4095, 4097, 8191, 8193, 16383])
+@pytest.mark.parametrize("x_type,y_type", [(BF16, BF16), (F32, F32), (F32, F16)])
+def test_layer_norm_rows_between_vectors(ress, width, x_type, y_type):
+    """Rows that start at any element of a vector, from the number of rows that they are worth it on: all
+    tensors at the same one, and not; a row that is not finite, and what lies beside the rows."""
+    eps = 1e-5
+    for rows, off, pitch, apart in ((63, 0, width, 0), (64, 0, width, 0), (330, 3, width + 6, 0), (330, 1, width, 1)):
+        g = gen(rows * 1000003 + width)
+        like = lambda kind, o, fill: torch.full((rows * pitch + 16,), fill, device="cuda", dtype=kind)[o:].as_strided(
+            (rows, width), (pitch, 1))
+        x, y = like(x_type, off, 9.0), like(y_type, off + apart, 9.0)
+        x.copy_(normal(g, rows, width) + 2.0)
+        x[5, width // 2] = float("nan")
+        w, b = 1 + 0.3 * normal(g, width), 0.2 * normal(g, width)
+        mean, rstd = torch.full((2, rows), float("nan"), device="cuda").unbind()
+        ress.layer_norm(x, w, b, y, eps=eps, mean=mean, rstd=rstd)
+        keep = [i for i in range(rows) if i != 5]
+        x64, w64, b64 = x.double(), w.double(), b.double()
+        h, m64, r64, y64 = norm64(x64, w64, b64, eps)
+        within(y[keep], y64[keep], (rounded(y64, y_type) + norm_bound(x64, h, w64, b64, r64))[keep], "y")
+        assert bool(y[5].isnan().all())
+        y[5] = 0.0
+        beside = torch.ones(rows, pitch, device="cuda", dtype=torch.bool)
+        beside[:, :width] = False
+        assert bool((y.as_strided((rows, pitch), (pitch, 1))[:-1][beside[:-1]] == 9.0).all())
+
+        x[5] = 1.0 + x[4]  # the gradient, of finite rows
+        ress.layer_norm(x, w, b, y, eps=eps, mean=mean, rstd=rstd)
+        x64, dy, dres, dx = x.double(), like(y_type, off, 9.0), like(x_type, off, 9.0), like(x_type, off + apart, 9.0)
+        dy.copy_(0.3 * normal(g, rows, width))
+        dres.copy_(normal(g, rows, width))
+        m, r = mean.double()[:, None], rstd.double()[:, None]
+        h, gr = (x64 - m) * r, dy.double() * w64
+        ag, agh = gr.mean(-1, keepdim=True), (gr * h).mean(-1, keepdim=True)
+        core = r * (gr - ag - h * agh)
+        err = r * (E * (gr.abs().mean(-1, keepdim=True) + h.abs() * (gr * h).abs().mean(-1, keepdim=True))
+                   + 8 * U32 * (gr.abs() + ag.abs() + (h * agh).abs()))
+        ws = torch.empty(ress.layer_norm_workspace_bytes(rows, width), dtype=torch.uint8, device="cuda")
+        dw, db = torch.full((2, width), float("nan"), device="cuda").unbind()
+        ress.layer_norm_bwd(dy, x, w, mean, rstd, dx, dweight=dw, dbias=db, dres=dres, ws=ws)
+        want = core + dres.double()
+        within(dx, want, rounded(want, x_type) + err + U32 * dres.double().abs(), "dx")
+        assert bool((dx.as_strided((rows, pitch), (pitch, 1))[:-1][beside[:-1]] == 9.0).all())
+        depth = (rows + 128 + 64) * U32
+        within(dw, (dy.double() * h).sum(0), depth * (dy.double() * h).abs().sum(0) + 1e-30, "dweight")
+        within(db, dy.double().sum(0), depth * dy.double().abs().sum(0) + 1e-30, "dbias")
+
+
 def test_layer_norm_extreme_rows(ress):
     """Constant rows, a row of zeros, offsets a thousand times the spread, rows with inf and NaN: the
     last only concern themselves."""
