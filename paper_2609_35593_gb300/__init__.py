@@ -250,11 +250,17 @@ def _host(t, dtypes, name):
     return _c.c_void_p(t.data_ptr())
 
 
+_current_stream = None
+
+
 def _stream(stream):
     if stream is not None:
         return stream.cuda_stream
-    # the current device's current stream without a Stream object (0.2 us instead of 3)
-    return _torch()._C._cuda_getCurrentRawStream(-1)
+    # the current device's current stream without a Stream object (0.1 us instead of 3)
+    global _current_stream
+    if _current_stream is None:
+        _current_stream = _torch()._C._cuda_getCurrentRawStream
+    return _current_stream(-1)
 
 
 def _bf16():

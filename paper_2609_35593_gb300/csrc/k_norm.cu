@@ -11,10 +11,11 @@
 //             and keeps their weights and biases in registers (43,968 x 1024 bf16: 53 us with C = 8 on
 //             four warps, 35 with the next rows under way, 33 with a warp per row; 36 where it reads
 //             float32 parameters from L1 for each row; a device copy of the same bytes takes 31).
-//             float32 elements take twice the registers: C = 16;
+//             float32 elements take twice the registers: above 896 channels
+//             C = 16;
 //   backward  C = 8, because a thread keeps its channels' two gradient sums in registers: with C = 32
 //             they leave room for 8 warps per SM (80 us), with C = 8 for 16 (63 us, and a barrier per
-//             R = 2 rows).  Above 4096 channels C = 32, the sums in shared memory.
+//             R = 2 rows).  Above 4096 channels C = 16, above 8192 C = 32 and the sums in shared memory.
 // Rows that are no whole vectors of 16 bytes, or not aligned to them, are taken as the aligned vectors that they
 // have and the elements at their two edges, one to a thread (EDGES: 20,000 x 1021 bf16 22.5 us, and 37 element by
 // element; 3000 x 8191 28 and 123; 5003 x 1021 float32 to bf16 7.5 and 12.2; the gradient of the first 41 and 57;
@@ -621,9 +622,14 @@ cudaError_t launch_norm_typed(const NormArgs& a, const NormParams& p, bool vec, 
     if (D <= 16 * kNormMaxThreads) return launch_norm_as<BWD, X, Y, E, 16, kWholeCta>(a, p, st);
   } else {
     if (D <= 512) return launch_norm_as<BWD, X, Y, E, 16, 32>(a, p, st);
-    if (D <= 1024) return launch_norm_as<BWD, X, Y, E, 32, 32>(a, p, st);
-    if constexpr (sizeof(X) == 4)
+    if constexpr (sizeof(X) == 4) {
+      // a warp per row reads its parameters anew for each (20,000 x 1024 to bf16: 25.8 us, two warps per row that
+      // keep them 23.8; x 640, where the second warp is mostly idle: 17.5 and 18.7)
+      if (D <= 896) return launch_norm_as<BWD, X, Y, E, 32, 32>(a, p, st);
       if (D <= 16 * kNormMaxThreads) return launch_norm_as<BWD, X, Y, E, 16, kWholeCta>(a, p, st);
+    } else if (D <= 1024) {
+      return launch_norm_as<BWD, X, Y, E, 32, 32>(a, p, st);
+    }
   }
   return launch_norm_as<BWD, X, Y, E, 32, kWholeCta>(a, p, st);
 }
