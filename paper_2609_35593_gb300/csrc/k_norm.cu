@@ -571,9 +571,12 @@ cudaError_t launch_norm_as(const NormArgs& a, const NormParams& p, cudaStream_t 
   } else {
     constexpr int R = C > 8 || wide ? 1 : 2;
     constexpr auto kern = k_layer_norm_bwd<X, Y, E, C, TEAM, R, EDGES>;
-    const size_t smem = C <= 16 ? 0 : 2 * C * sizeof(float) * threads;
+    // what the kernel may have is set for its largest CTA, the same by every call: the setting is the kernel's,
+    // and calls of other widths on other host threads set it between this call's setting and its launch
+    constexpr size_t kThreadSmem = C <= 16 ? 0 : 2 * C * sizeof(float), kMostSmem = kThreadSmem * kNormMaxThreads;
+    const size_t smem = kThreadSmem * threads;
     cudaError_t e = cudaSuccess;
-    if (smem > 0) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (kMostSmem > 0) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem);
     if (e != cudaSuccess) return e;
     int ctas = norm_ctas(norm_resident<kern>(threads, smem), per_cta, (p.rows + R - 1) / R, kNormParts);
     if (EDGES) ctas = same_heads(ctas, E / per_cta);
