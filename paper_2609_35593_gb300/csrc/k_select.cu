@@ -1779,6 +1779,16 @@ static Budgets budgets_of(const SelectArgs& a) {
   return b;
 }
 
+// Shared memory that the kernels may have: of the largest scene, the same by every call.  The setting is the
+// kernel's, and calls on scenes of other sizes on other host threads set it between this call's setting and
+// its launch.
+constexpr int kMostWords = RESS_MAX_BLOCKS / 32;
+constexpr int kMostRowSmem =
+    (int)(kRowWarps * warp_scratch_words(RESS_MAX_BLOCKS, score_mask_words(kMostWords, true)) * 4);
+static_assert(score_mask_words(kMostWords, true) >= 3 * kMostWords, "the rounds' masks fit too");
+constexpr size_t pair_smem(int words) { return (size_t)kPairWindow * ((((words + 1) >> 1) | 1) * 8); }
+constexpr int kMostPairSmem = (int)pair_smem(kMostWords);
+
 cudaError_t launch_score(const SelectArgs& a, cudaStream_t st) {
   const Shape& s = a.s;
   SelPtrs p = sel_ptrs(s, a.ws, a.L);
@@ -1809,7 +1819,7 @@ cudaError_t launch_score(const SelectArgs& a, cudaStream_t st) {
   auto kern = a.v.key == 0   ? (large ? k_score_rows<0, true> : k_score_rows<0, false>)
               : a.v.key == 1 ? (large ? k_score_rows<1, true> : k_score_rows<1, false>)
                              : (large ? k_score_rows<2, true> : k_score_rows<2, false>);
-  e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)rsmem);
+  e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostRowSmem);
   if (e != cudaSuccess) return e;
   return launch_pdl(kern, dim3((s.nqc + kRowWarps - 1) / kRowWarps, s.H), 32 * kRowWarps, rsmem, st,
                     true, p, budgets_of(a), a.v);
@@ -1827,7 +1837,7 @@ cudaError_t launch_round(const SelectArgs& a, int round, float rho, cudaStream_t
   const bool large = mmax > 20;
   auto kern = a.v.direction != 0 ? (large ? k_round_rows<1, true> : k_round_rows<1, false>)
                                  : (large ? k_round_rows<0, true> : k_round_rows<0, false>);
-  e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)rsmem);
+  e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostRowSmem);
   if (e != cudaSuccess) return e;
   return launch_pdl(kern, dim3((s.nqc + kRowWarps - 1) / kRowWarps, s.H), 32 * kRowWarps, rsmem, st,
                     true, p, budgets_of(a), round, rho);
@@ -1875,8 +1885,8 @@ cudaError_t launch_pairing(const SelectArgs& a, int32_t* prow, cudaStream_t st) 
   const Shape& s = a.s;
   const int npaired = paired_items(s);
   const int windows = (2 * npaired + kPairWindow - 1) / kPairWindow;
-  const size_t smem = (size_t)kPairWindow * ((((s.words + 1) >> 1) | 1) * 8);
-  cudaError_t e = cudaFuncSetAttribute(k_pairing, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  const size_t smem = pair_smem(s.words);
+  cudaError_t e = cudaFuncSetAttribute(k_pairing, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostPairSmem);
   if (e != cudaSuccess) return e;
   return launch_pdl(k_pairing, dim3(windows, s.H), 512, smem, st, true,
                     (const uint32_t*)(a.ws + a.L.bmask), s.nq, s.words, s.ncand, npaired,

@@ -63,3 +63,36 @@ def test_layer_norm_gradients_of_two_widths(ress, widths):
     assert together(layers, 3000) == []
     for layer, expected in zip(layers, want):
         assert all(torch.equal(a, b) for a, b in zip(layer.out, expected))
+
+
+class Selection:
+    """Scoring and restoration of one scene."""
+
+    def __init__(self, ress, views):
+        g = torch.Generator(device="cuda").manual_seed(views)
+        normal = lambda *s: torch.randn(*s, generator=g, device="cuda", dtype=torch.float32).bfloat16()
+        N, H, dm = views * 1374, 1, 64
+        self.ress, self.d, self.c = ress, ress.dims(N, H, views * 5, dm), [20] * H
+        self.Q, self.K, self.V = (normal(N, H, 64) for _ in range(3))
+        self.buf = ress.Buffers(self.d, self.c)
+        ress.prepare_wo(self.d, 0.1 * normal(dm, dm), self.buf.F)
+        self.out = [self.buf.J_best, self.buf.row_ptr, self.buf.col_idx]
+
+    def __call__(self, stream=None):
+        b = self.buf
+        self.ress.score(self.d, self.Q, self.K, self.V, b.F, self.c, b.ws, stream=stream)
+        self.ress.restore(self.d, self.c, 3, 0.5, b.ws, b.row_ptr, b.col_idx, b.J_best, stream=stream)
+
+
+def test_selections_of_two_scenes(ress):
+    """Above 2,700 blocks a selection kernel's shared memory needs more than the 48 KB that any launch may have."""
+    scenes = [Selection(ress, 2), Selection(ress, 180)]
+    want = []
+    for s in scenes:
+        s()
+        want.append([t.clone() for t in s.out])
+        [t.fill_(-1) for t in s.out]
+    assert together(scenes, 600) == []
+    for s, expected in zip(scenes, want):
+        ress.status(s.buf.ws)
+        assert all(torch.equal(a, b) for a, b in zip(s.out, expected))
