@@ -29,8 +29,6 @@
 // and leaves one partial row of each in the workspace, and a second kernel adds the partial rows up
 // in order, so that the result does not depend on the order in which CTAs finish.
 
-#include <atomic>
-
 #include "row_ops.cuh"
 
 namespace ress {
@@ -543,20 +541,6 @@ int norm_ctas(int resident, int teams_per_cta, int64_t batches, int most) {
 constexpr int kEdgeRows = 64;
 int same_heads(int ctas, int of) { return of <= 1 ? ctas : ctas / of * of; }
 
-// CTAs of a kernel that fit on an SM, for each number of warps, asked for once.
-template <auto kKernel>
-int norm_resident(int threads, size_t smem) {
-  static std::atomic<int> known[kNormMaxThreads / 32 + 1];
-  std::atomic<int>& at = known[threads / 32];
-  int n = at.load(std::memory_order_relaxed);
-  if (n == 0) {
-    const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kKernel, threads, smem);
-    if (e != cudaSuccess || n < 1) n = 1;
-    at.store(n, std::memory_order_relaxed);
-  }
-  return n;
-}
-
 template <bool BWD, typename X, typename Y, int E, int C, int TEAM, bool ONE = false, bool EDGES = false>
 cudaError_t launch_norm_as(const NormArgs& a, const NormParams& p, cudaStream_t st) {
   constexpr bool wide = sizeof(X) == 4 || E == 1;  // elements that take a register each as they lie
@@ -565,7 +549,10 @@ cudaError_t launch_norm_as(const NormArgs& a, const NormParams& p, cudaStream_t 
   if constexpr (!BWD) {
     constexpr int R = C == 32 || ONE ? 1 : wide ? 16 / C : 32 / C;
     constexpr auto kern = k_layer_norm<X, Y, E, C, TEAM, R, EDGES>;
-    int ctas = norm_ctas(norm_resident<kern>(threads, 0), per_cta, (p.rows + R - 1) / R, INT32_MAX);
+    int fit = 0;
+    const cudaError_t e = resident_ctas<kern>(threads, 0, fit);
+    if (e != cudaSuccess) return e;
+    int ctas = norm_ctas(fit, per_cta, (p.rows + R - 1) / R, INT32_MAX);
     if (EDGES) ctas = same_heads(ctas, E / per_cta);
     return launch_pdl(kern, ctas, threads, 0, st, true, p);
   } else {
@@ -577,8 +564,10 @@ cudaError_t launch_norm_as(const NormArgs& a, const NormParams& p, cudaStream_t 
     const size_t smem = kThreadSmem * threads;
     cudaError_t e = cudaSuccess;
     if (kMostSmem > 0) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem);
+    int fit = 0;
+    if (e == cudaSuccess) e = resident_ctas<kern>(threads, smem, fit);
     if (e != cudaSuccess) return e;
-    int ctas = norm_ctas(norm_resident<kern>(threads, smem), per_cta, (p.rows + R - 1) / R, kNormParts);
+    int ctas = norm_ctas(fit, per_cta, (p.rows + R - 1) / R, kNormParts);
     if (EDGES) ctas = same_heads(ctas, E / per_cta);
     e = launch_pdl(kern, ctas, threads, smem, st, true, p);
     if (e != cudaSuccess || !p.partial) return e;

@@ -487,7 +487,10 @@ cudaError_t launch_rope_as(RopeParams& p, int (&ctas)[2], cudaStream_t st) {
   constexpr int K = S == 8 ? 2 : sizeof(T) == 2 ? (NORM && !BWD ? 4 : 2) : (NORM && BWD ? 1 : 2);
   constexpr int kHeads = 32 / G;
   constexpr auto kern = k_rope<T, G, MODE, S, NORM, BWD, FEW, K>;
-  const int64_t fit = min((int64_t)resident_ctas<kern>(kRopeThreads, 0) * sm_count(), (int64_t)p.most);
+  int resident = 0;
+  const cudaError_t e = resident_ctas<kern>(kRopeThreads, 0, resident);
+  if (e != cudaSuccess) return e;
+  const int64_t fit = min((int64_t)resident * sm_count(), (int64_t)p.most);
   p.whole_tokens = p.tokens * ((p.t[0].heads > 0) + (p.t[1].heads > 0)) >= fit * kRopeWarps;
   // CTAs at one visit (a token's items, or an item) per warp, and what a visit costs: an item about a row,
   // a lane's angle about half of one

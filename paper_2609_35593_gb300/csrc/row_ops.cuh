@@ -6,6 +6,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <atomic>
+
 #include "ress_internal.cuh"
 #include "sm100_ptx.cuh"
 
@@ -285,15 +287,19 @@ __host__ __device__ inline int rope_axis(const ress_rope_plan& plan, int pair) {
   return a;
 }
 
-// CTAs of a kernel that fit on an SM (asked for once: the question takes about as long as a launch).
+// CTAs of a kernel that fit on an SM, for each number of warps.  Asked for once (the question takes about as long
+// as a launch), and again after an answer that failed.
 template <auto kKernel>
-int resident_ctas(int threads, size_t smem) {
-  static const int n = [&] {
-    int r = 0;
-    const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&r, kKernel, threads, smem);
-    return e == cudaSuccess && r > 0 ? r : 1;
-  }();
-  return n;
+cudaError_t resident_ctas(int threads, size_t smem, int& ctas) {
+  static std::atomic<int> known[1024 / 32 + 1];
+  std::atomic<int>& at = known[threads / 32];
+  ctas = at.load(std::memory_order_relaxed);
+  if (ctas > 0) return cudaSuccess;
+  const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&ctas, kKernel, threads, smem);
+  if (e != cudaSuccess) return e;
+  if (ctas < 1) return cudaErrorLaunchOutOfResources;
+  at.store(ctas, std::memory_order_relaxed);
+  return cudaSuccess;
 }
 
 inline int sm_count() {
