@@ -311,7 +311,7 @@ __global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThr
   const float inv = 1.f / (float)p.width;
   int turn = 0;
   stream_acquire();
-  // Channels past the row's end have a weight, a dy and so every sum of 0.
+  // Channels past the row's end have a weight, a dy and so every sum of the row of 0.
   float w[C];
   F2 dw[kKeep ? P : 1], db[kKeep ? P : 1];
   auto weights = [&](int i) {
@@ -353,7 +353,7 @@ __global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThr
     if (!kAhead) load(row0);
     Vec<X, E> x[R][V], res[R][V];
     Vec<Y, E> dy[R][V];
-    float r[R], mr[R];  // h = x r + mr
+    float r[R], mr[R];  // 1 / standard deviation, mean
     float edge_x[R], edge_res[R], edge_dy[R];
 #pragma unroll
     for (int k = 0; k < R; ++k) {
@@ -373,18 +373,21 @@ __global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThr
     }
     if (kAhead) load(row0 + team.count * R);
     // h = (x - mean) r, in this order: the difference keeps the digits of rows far from 0
-    auto h_of = [&](int k, int j) { return mul2(add2(pair_of(x[k], j), both(-mr[k])), both(r[k])); };
+    auto centred = [&](int k, int j) { return add2(pair_of(x[k], j), both(-mr[k])); };
+    auto h_of = [&](int k, int j) { return mul2(centred(k, j), both(r[k])); };
     float sums[2 * R];
 #pragma unroll
     for (int k = 0; k < R; ++k) {
-      F2 sg = both(0.f), sgh = both(0.f);
+      // sum of g h as r times that of g (x - mean): past the row's end x, dy and g are 0, and (0 - mean) r may be
+      // infinite, but mean is not
+      F2 sg = both(0.f), sgc = both(0.f);
 #pragma unroll
       for (int j = 0; j < P; ++j) {
         if (!kKeep && 2 * j % E == 0) weights(2 * j / E);
         if (!kKeep && E == 1) weights(2 * j + 1);
-        const F2 d = pair_of(dy[k], j), h = h_of(k, j), g = mul2(d, pack2(w[2 * j], w[2 * j + 1]));
+        const F2 d = pair_of(dy[k], j), c = centred(k, j), h = mul2(c, both(r[k])), g = mul2(d, pack2(w[2 * j], w[2 * j + 1]));
         sg = add2(sg, g);
-        sgh = fma2(g, h, sgh);
+        sgc = fma2(g, c, sgc);
         if constexpr (kKeep) {
           dw[j] = fma2(d, h, dw[j]);
           db[j] = add2(db[j], d);
@@ -396,18 +399,20 @@ __global__ void __launch_bounds__(TEAM == kWholeCta ? kNormMaxThreads : kNormThr
           for (int q = 0; q < 4; ++q) wide[(C * (q / 2) + 2 * j + q % 2) * team.threads + team.t] += v[q];
         }
       }
-      float g = sum2(sg), gh = sum2(sgh);
+      float g = sum2(sg), gc = sum2(sgc);
       if (EDGES && at.edge >= 0) {
-        const float h = (edge_x[k] - mr[k]) * r[k], ge = edge_dy[k] * edge_w;
+        const float c = edge_x[k] - mr[k], ge = edge_dy[k] * edge_w;
         g += ge;
-        gh = fmaf(ge, h, gh);
-        edge_dw = fmaf(edge_dy[k], h, edge_dw);
+        gc = fmaf(ge, c, gc);
+        edge_dw = fmaf(edge_dy[k], c * r[k], edge_dw);
         edge_db += edge_dy[k];
       }
       sums[2 * k] = g * inv;
-      sums[2 * k + 1] = gh * inv;
+      sums[2 * k + 1] = gc * inv;
     }
     team_sum<TEAM>(sums, red, turn);
+#pragma unroll
+    for (int k = 0; k < R; ++k) sums[2 * k + 1] *= r[k];
 #pragma unroll
     for (int k = 0; k < R; ++k) {
       const int64_t row = row0 + k * gap;

@@ -1,0 +1,49 @@
+"""Layer norm and rotary positions where lanes without channels, or the ends of the ranges, must not show."""
+from fractions import Fraction
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+DEPTH, U32 = 64, 2.0 ** -24  # of the float32 sums, and of one rounding
+ROUND = {BF16: 2.0 ** -8, F32: 2.0 ** -24}
+BIG, EPS = 2.0 ** 120, 1e-5  # BIG / sqrt(EPS) is past the largest float32
+
+
+@pytest.fixture(scope="module")
+def ress():
+    import paper_2609_35593_gb300 as r
+    return r
+
+
+def normal(seed, *shape):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randn(*shape, generator=g, device="cuda", dtype=torch.float32)
+
+
+def centred_bound(g, r, want, kind):
+    """Error of r (g - avg g) in float32 and of its rounding: the mean's, and five roundings on the way."""
+    return r * (DEPTH * U32 * g.abs().mean(-1, keepdim=True) + 8 * U32 * (g.abs() + g.mean(-1, keepdim=True).abs())) + \
+        1.01 * ROUND[kind] * want.abs()
+
+
+@pytest.mark.parametrize("width", [24, 33, 72, 136, 264, 1021, 1032, 2049, 4104, 5000, 9001, 16000])
+@pytest.mark.parametrize("kind", [BF16, F32])
+def test_layer_norm_gradient_of_huge_constant_rows(ress, kind, width):
+    """Every h = (x - mean) rstd is 0, and dx = rstd (g - avg g) is finite, although mean rstd is not."""
+    for rows in (3, 70):
+        x = torch.full((rows, width), BIG, device="cuda", dtype=kind)
+        dy, w = normal(width, rows, width).to(kind), 1 + 0.3 * normal(width + 1, width)
+        mean = torch.full((rows,), BIG, device="cuda")
+        rstd = torch.full((rows,), EPS ** -0.5, device="cuda")
+        dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty_like(w)
+        ws = torch.empty(ress.layer_norm_workspace_bytes(rows, width), dtype=torch.uint8, device="cuda")
+        ress.layer_norm_bwd(dy, x, w, mean, rstd, dx, dweight=dw, dbias=db, ws=ws)
+        g, r = dy.double() * w.double(), rstd.double()[:, None]
+        want = r * (g - g.mean(-1, keepdim=True))
+        assert bool(((dx.double() - want).abs() <= centred_bound(g, r, want, kind)).all()), rows
+        assert not dw.any()
+        assert bool(((db.double() - dy.double().sum(0)).abs() <= (rows + 192) * U32 * dy.double().abs().sum(0)).all())
