@@ -373,7 +373,10 @@ __global__ void __launch_bounds__(kRopeThreads, (!NORM ? 6 : BWD ? 3 : 4) - (S =
         F2 sum[2] = {h[0][0], h[1][0]};
 #pragma unroll
         for (int q = 1; q < Q; ++q) sum[0] = add2(sum[0], h[0][q]), sum[1] = add2(sum[1], h[1][q]);
-        const F2 m = both(-segment_sum<G>(sum2(add2(sum[0], sum[1])) * inv));
+        const float mean = segment_sum<G>(sum2(add2(sum[0], sum[1])) * inv);
+        // lanes without channels have h = 0: (0 - mean) rstd may be infinite, and times u = 0 it would enter the
+        // gradient's sums
+        const F2 m = both(slots.any ? -mean : 0.f);
         F2 sq = both(0.f);
 #pragma unroll
         for (int s = 0; s < 2; ++s)
@@ -387,7 +390,7 @@ __global__ void __launch_bounds__(kRopeThreads, (!NORM ? 6 : BWD ? 3 : 4) - (S =
             }
             sq = fma2(h[s][q], h[s][q], sq);
           }
-        rstd = rsqrtf(segment_sum<G>(slots.any ? sum2(sq) * inv : 0.f) + p.eps);
+        rstd = rsqrtf(segment_sum<G>(sum2(sq) * inv) + p.eps);
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll

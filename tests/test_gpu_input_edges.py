@@ -47,3 +47,24 @@ def test_layer_norm_gradient_of_huge_constant_rows(ress, kind, width):
         assert bool(((dx.double() - want).abs() <= centred_bound(g, r, want, kind)).all()), rows
         assert not dw.any()
         assert bool(((db.double() - dy.double().sum(0)).abs() <= (rows + 192) * U32 * dy.double().abs().sum(0)).all())
+
+
+@pytest.mark.parametrize("hd,heads", [(24, 1), (24, 3), (24, 11), (48, 8), (96, 1), (96, 2), (96, 3), (96, 4)])
+@pytest.mark.parametrize("layout", ["halves", "interleaved"])
+@pytest.mark.parametrize("kind", [BF16, F32])
+def test_head_norm_gradient_of_huge_constant_heads(ress, kind, layout, hd, heads):
+    """Heads that leave lanes without channels.  (A head's mean is exact: 24, 48 and 96 are 3 times a power of two,
+    and 3 times 1/3 in float32 rounds to 1.)"""
+    tokens, plan = 50, ress.rope_plan((hd,), head_dim=hd, layout=layout)
+    pos = torch.zeros(tokens, 1, dtype=torch.int32, device="cuda")
+    x = torch.full((tokens, heads, hd), BIG, device="cuda", dtype=kind)
+    dy, w, b = normal(hd + heads, tokens, heads, hd).to(kind), 1 + 0.3 * normal(5, hd), normal(6, hd)
+    dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty_like(w)
+    ws = torch.empty(ress.rope_workspace_bytes(plan, tokens, heads), dtype=torch.uint8, device="cuda")
+    ress.rope_bwd(plan, pos, dy, dx, q=x, q_norm=(w, b), q_norm_grads=(dw, db), eps=EPS, ws=ws)
+    g, r = dy.double() * w.double(), EPS ** -0.5
+    want = r * (g - g.mean(-1, keepdim=True))
+    assert bool(((dx.double() - want).abs() <= centred_bound(g, r, want, kind)).all())
+    assert not dw.any()
+    total = dy.double().sum((0, 1))
+    assert bool(((db.double() - total).abs() <= (tokens * heads + 192) * U32 * dy.double().abs().sum((0, 1))).all())
