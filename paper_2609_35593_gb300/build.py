@@ -3,7 +3,7 @@ binding's questions about tensors, with the host compiler.
 
 Translation units are compiled in parallel into _build/ and linked into
 paper_2609_35593_gb300/libress.so.  A unit is recompiled when it or any header it may
-include is newer than its object file.
+include is newer than its object file, and _tensors.so for another Python or torch as well.
 """
 from __future__ import annotations
 
@@ -38,9 +38,20 @@ def nvcc() -> str:
     return exe
 
 
+def _torch_dir() -> str:
+    return os.path.dirname(importlib.util.find_spec("torch").origin)
+
+
+def _tensors_abi() -> str:
+    """The Python and the torch that _tensors.so is compiled against and linked to: it holds their layouts."""
+    torch = _torch_dir()
+    with open(os.path.join(torch, "version.py")) as f:
+        return f"{sysconfig.get_config_var('SOABI')}\n{torch}\n{f.read()}"
+
+
 def _tensors_command(src: str) -> list[str]:
     """Compiles the one unit that knows torch's tensors (and Python); libress.so knows neither."""
-    torch = os.path.dirname(importlib.util.find_spec("torch").origin)
+    torch = _torch_dir()
     inc, lib = os.path.join(torch, "include"), os.path.join(torch, "lib")
     includes = ["-I", INCLUDE, "-I", sysconfig.get_paths()["include"], "-isystem", inc, "-isystem",
                 os.path.join(inc, "torch", "csrc", "api", "include")]
@@ -70,7 +81,9 @@ def build(force: bool = False, verbose: bool = False, extra_flags: list[str] | N
             jobs.append([nvcc(), *ARCH, *flags, "-c", s, "-o", o])
     units = len(jobs)
     s = os.path.join(CSRC, "tensors.cpp")
-    if force or not os.path.exists(TENSORS) or os.path.getmtime(TENSORS) < max(os.path.getmtime(s), hdr):
+    abi, abi_stamp = _tensors_abi(), os.path.join(OBJDIR, "tensors_abi")
+    if (force or not os.path.exists(TENSORS) or os.path.getmtime(TENSORS) < max(os.path.getmtime(s), hdr)
+            or not os.path.exists(abi_stamp) or open(abi_stamp).read() != abi):
         jobs.append(_tensors_command(s))
 
     def run(cmd):
@@ -87,8 +100,9 @@ def build(force: bool = False, verbose: bool = False, extra_flags: list[str] | N
     objs = [os.path.join(OBJDIR, s.replace(".cu", ".o")) for s in SOURCES]
     if units or not os.path.exists(LIB) or os.path.getmtime(LIB) < max(map(os.path.getmtime, objs)):
         run([nvcc(), *ARCH, "-shared", "-o", LIB, *objs])
-    with open(stamp, "w") as f:
-        f.write(machine)
+    for path, text in ((stamp, machine), (abi_stamp, abi)):
+        with open(path, "w") as f:
+            f.write(text)
     return LIB
 
 
