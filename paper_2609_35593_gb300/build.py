@@ -38,20 +38,19 @@ def nvcc() -> str:
     return exe
 
 
-def _torch_dir() -> str:
-    return os.path.dirname(importlib.util.find_spec("torch").origin)
+def _torch_dir() -> str | None:
+    spec = importlib.util.find_spec("torch")
+    return os.path.dirname(spec.origin) if spec is not None and spec.origin else None
 
 
-def _tensors_abi() -> str:
+def _tensors_abi(torch: str) -> str:
     """The Python and the torch that _tensors.so is compiled against and linked to: it holds their layouts."""
-    torch = _torch_dir()
     with open(os.path.join(torch, "version.py")) as f:
         return f"{sysconfig.get_config_var('SOABI')}\n{torch}\n{f.read()}"
 
 
-def _tensors_command(src: str) -> list[str]:
+def _tensors_command(src: str, torch: str) -> list[str]:
     """Compiles the one unit that knows torch's tensors (and Python); libress.so knows neither."""
-    torch = _torch_dir()
     inc, lib = os.path.join(torch, "include"), os.path.join(torch, "lib")
     includes = ["-I", INCLUDE, "-I", sysconfig.get_paths()["include"], "-isystem", inc, "-isystem",
                 os.path.join(inc, "torch", "csrc", "api", "include")]
@@ -80,11 +79,18 @@ def build(force: bool = False, verbose: bool = False, extra_flags: list[str] | N
         if force or not os.path.exists(o) or os.path.getmtime(o) < max(os.path.getmtime(s), hdr):
             jobs.append([nvcc(), *ARCH, *flags, "-c", s, "-o", o])
     units = len(jobs)
-    s = os.path.join(CSRC, "tensors.cpp")
-    abi, abi_stamp = _tensors_abi(), os.path.join(OBJDIR, "tensors_abi")
-    if (force or not os.path.exists(TENSORS) or os.path.getmtime(TENSORS) < max(os.path.getmtime(s), hdr)
-            or not os.path.exists(abi_stamp) or open(abi_stamp).read() != abi):
-        jobs.append(_tensors_command(s))
+    stamps = {stamp: machine}
+    torch = _torch_dir()
+    if torch is None:
+        print("torch is not installed: libress.so is built without _tensors.so, which binds torch's tensors to it",
+              flush=True)
+    else:
+        s = os.path.join(CSRC, "tensors.cpp")
+        abi, abi_stamp = _tensors_abi(torch), os.path.join(OBJDIR, "tensors_abi")
+        if (force or not os.path.exists(TENSORS) or os.path.getmtime(TENSORS) < max(os.path.getmtime(s), hdr)
+                or not os.path.exists(abi_stamp) or open(abi_stamp).read() != abi):
+            jobs.append(_tensors_command(s, torch))
+        stamps[abi_stamp] = abi
 
     def run(cmd):
         if verbose:
@@ -100,7 +106,7 @@ def build(force: bool = False, verbose: bool = False, extra_flags: list[str] | N
     objs = [os.path.join(OBJDIR, s.replace(".cu", ".o")) for s in SOURCES]
     if units or not os.path.exists(LIB) or os.path.getmtime(LIB) < max(map(os.path.getmtime, objs)):
         run([nvcc(), *ARCH, "-shared", "-o", LIB, *objs])
-    for path, text in ((stamp, machine), (abi_stamp, abi)):
+    for path, text in stamps.items():
         with open(path, "w") as f:
             f.write(text)
     return LIB

@@ -58,3 +58,20 @@ def test_tensors_are_compiled_again_for_another_torch_or_python(build, monkeypat
     monkeypatch.setattr(build.sysconfig, "get_config_var", lambda n: "cpython-399" if n == "SOABI" else variables(n))
     assert build.outputs() == ["_tensors.so"]
     assert build.outputs() == []
+
+
+def test_library_is_built_without_torch(build, monkeypatch, capsys):
+    """libress.so and the calls on raw pointers need no torch."""
+    monkeypatch.setattr(build.importlib.util, "find_spec", lambda name: None)
+    want = sorted([os.path.basename(build.LIB)] + [s.replace(".cu", ".o") for s in build.SOURCES])
+    assert build.outputs() == want
+    assert "torch" in capsys.readouterr().out
+    assert build.outputs() == []
+
+
+def test_tensors_follow_once_torch_is_there(build, monkeypatch, tmp_path):
+    monkeypatch.setattr(build.importlib.util, "find_spec", lambda name: None)
+    build.outputs()
+    spec = torch_at(str(tmp_path / "torch"), "2.11.0")
+    monkeypatch.setattr(build.importlib.util, "find_spec", lambda name: spec)
+    assert build.outputs() == ["_tensors.so"]
