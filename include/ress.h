@@ -342,7 +342,10 @@ int ress_layer_norm_bwd(const ress_norm* n, const void* dy, const void* x, const
  * Channels from 2 n_pairs to head_dim are not rotated.  A plan is plain host data, filled by
  * ress_rope_plan_init and passed by pointer; it may be copied.  head_dim: even, 2..256.
  * freq: n_pairs angles in radians per unit position (finite), or NULL for base^(-2i/axis_dims[a])
- * with i counted within each axis and base > 0.  Angles are exact for every int32 position. */
+ * with i counted within each axis and base > 0.  The plan keeps each frequency's turns per position
+ * modulo 1 to 64 bits (for |freq| below 2^40; 2^-104 of itself above), so the angle at any int32
+ * position is off by at most the position times 2^-65 turns; of it the kernels take the upper 32 bits
+ * (2^-32 turns) and round them to float32. */
 typedef enum { RESS_ROPE_SECTIONS = 0, RESS_ROPE_HALVES = 1, RESS_ROPE_INTERLEAVED = 2 } ress_rope_layout;
 #define RESS_ROPE_MAX_AXES 4
 #define RESS_ROPE_MAX_DIM 256

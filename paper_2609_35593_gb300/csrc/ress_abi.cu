@@ -707,6 +707,21 @@ int check_heads(const ress_rope_heads& t, const ress_heads& h, int64_t tokens, i
   return RESS_OK;
 }
 
+// f / 2 pi modulo 1, rounded to a fraction of 64 bits.  The product with 1 / 2 pi in two doubles is good to 2^-104
+// of itself; taking whole turns off it, scaling and splitting it are exact.  |f| throughout, so that a small
+// negative f keeps its digits; the fraction of -f is what wraps around.
+uint64_t turns_of(double f) {
+  constexpr double kInv = 0x1.45f306dc9c883p-3, kInvRest = -0x1.6b01ec5417056p-57;
+  const double a = fabs(f);
+  double hi = a * kInv, lo = fma(a, kInvRest, fma(a, kInv, -hi));
+  hi = (hi - floor(hi)) * 0x1p64;
+  lo = (lo - rint(lo)) * 0x1p64;
+  const uint64_t whole = (uint64_t)hi;
+  const double rest = rint((hi - (double)whole) + lo);  // in +-2^63
+  const uint64_t turns = whole + (rest < 0 ? 0 - (uint64_t)-rest : (uint64_t)rest);
+  return f < 0 ? 0 - turns : turns;
+}
+
 // The checks that ress_rope and its gradient share; fills a.
 int rope_checks(const ress_rope_plan* plan, int64_t n_tokens, const int32_t* pos, int32_t type, int32_t param_type,
                 float eps, const ress_rope_heads* const (&t)[2], bool bwd, ress::RopeArgs* a) {
@@ -835,12 +850,7 @@ int ress_rope_plan_init(ress_rope_plan* plan, int32_t head_dim, int32_t n_axes, 
     for (int i = 0; i < p.axis_dims[a] / 2; ++i, ++k) {
       const double f = freq ? freq[k] : pow(base, -2.0 * i / p.axis_dims[a]);
       if (!(fabs(f) <= DBL_MAX)) return fail(RESS_EINVAL, "frequency %d is not finite", k);
-      // turns per position modulo 1, as a 64-bit fraction: the upper and lower 32 bits in turn
-      // (f / 2 pi is within 2^-53 of itself; what is taken off it below is exact)
-      double t = f / 6.283185307179586476925286766559;
-      t = (t - floor(t)) * 4294967296.0;
-      const double hi = floor(t), lo = floor((t - hi) * 4294967296.0);
-      p.turns[k] = ((uint64_t)hi << 32) + (uint64_t)lo;
+      p.turns[k] = turns_of(f);
     }
   *plan = p;
   return ok();

@@ -252,10 +252,10 @@ __device__ __forceinline__ float segment_sums(float (&v)[N]) {
 }
 
 // cos and sin of a position's angle.  The plan holds each frequency in turns per unit position as
-// a 64-bit fixed-point fraction, so that the product with an integer position, taken modulo whole
-// turns, is exact: the 64-bit product's wrap-around is the reduction.  Its upper 32 bits are the
-// angle in units of 2^-31 half turns, and float rounds that to 2^-24 of itself, at any position
-// (a product in float is off by the position times 2^-24 turns).
+// a 64-bit fixed-point fraction, so that the product with an integer position is taken modulo whole
+// turns without a further error: the 64-bit product's wrap-around is the reduction.  Its upper 32 bits are the
+// angle in units of 2^-31 half turns (what is dropped is less than 2^-32 turns), and float rounds that to 2^-24 of
+// itself (a product in float is off by the position times 2^-24 turns).
 __device__ __forceinline__ float2 rope_cos_sin(int32_t pos, uint64_t turns) {
   const uint64_t phase = (uint64_t)(int64_t)pos * turns;
   const float half_turns = (float)(int32_t)(phase >> 32) * 0x1p-31f;

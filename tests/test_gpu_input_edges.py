@@ -68,3 +68,24 @@ def test_head_norm_gradient_of_huge_constant_heads(ress, kind, layout, hd, heads
     assert not dw.any()
     total = dy.double().sum((0, 1))
     assert bool(((db.double() - total).abs() <= (tokens * heads + 192) * U32 * dy.double().abs().sum((0, 1))).all())
+
+
+def test_rope_of_given_frequencies_at_the_ends_of_int32(ress):
+    """The angle is position times frequency: its turns are good to the position times 2^-64, the kernel takes the
+    upper 32 bits, rounds them to float32, and cos and sin are good to two units in the last place."""
+    freq = [100.0, 1000.0, -1e-4, -1.0, 1e-9, 0.7, 12345.678, -3e5]
+    where = [-2 ** 31, 2 ** 31 - 1, 2 ** 30 + 12345, -77777777, 1, -1, 43968, 0]
+    plan = ress.rope_plan((16,), head_dim=16, layout="interleaved", freq=freq)
+    pos = torch.tensor(where, device="cuda", dtype=torch.int32)[:, None].contiguous()
+    x = torch.zeros(len(where), 1, 16, device="cuda")
+    x[..., 0::2] = 1.0
+    y = torch.empty_like(x)
+    ress.rope(plan, pos, x, y)
+    two_pi = Fraction("6.28318530717958647692528676655900576839433879875021164194988918461563281257")
+    for i, p in enumerate(where):
+        for k, f in enumerate(freq):
+            angle = torch.tensor(float(p * Fraction(f) % two_pi), dtype=torch.float64)
+            # half turns in [-1, 1], rounded: 2^-25 of them, so pi 2^-25; 2^-32 turns; 2^-32 of them in 2^-64 p
+            bound = 3.2 * 2.0 ** -25 + 2 * 6.3 * 2.0 ** -32 + 2 * 2.0 ** -24
+            assert abs(float(y[i, 0, 2 * k]) - float(torch.cos(angle))) <= bound, (p, f)
+            assert abs(float(y[i, 0, 2 * k + 1]) - float(torch.sin(angle))) <= bound, (p, f)
