@@ -609,6 +609,8 @@ def rope_bwd(plan: RopePlan, pos, dq_out, dq, dk_out=None, dk=None, q=None, k=No
     (which need q, k again), q_norm_grads, k_norm_grads: float32 (dweight, dbias), either or both None."""
     if dq_out is None or dq is None or (dk_out is None) != (dk is None) or (dk is None and k_norm is not None):
         raise ValueError("dq_out and dq are needed, and dk_out and dk together")
+    if dk is None and k_norm_grads is not None:
+        raise ValueError("k_norm_grads are written together with dk")
     if (q_norm is not None and q is None) or (k_norm is not None and k is None):
         raise ValueError("a norm's gradient needs the norm's input")
     tokens, code = pos.size(0), _code(dq_out, "dq_out")
