@@ -59,9 +59,9 @@ class Sublayer:
         self.mean, self.rstd = empty(self.N, dtype=torch.float32), empty(self.N, dtype=torch.float32)
         self.buf = None
 
-    def inputs(self, x):
-        """Q, K and V of the residual stream x [N, d_model]."""
-        W, b, ws = self.W, self.b, self._buffers([self.candidates] * self.H).ws
+    def inputs(self, x, ws):
+        """Q, K and V of the residual stream x [N, d_model]; ws holds the projection's status afterwards."""
+        W, b = self.W, self.b
         ress.layer_norm(x, *self.norm, self.h, eps=self.eps, mean=self.mean, rstd=self.rstd)
         ress.qkv_proj(self.d, self.h, W["q"], W["k"], W["v"], self.Q, self.K, self.V, ws, b_q=b["q"], b_k=b["k"],
                       b_v=b["v"], plan=self.plan, pos=self.pos, q_norm=self.head_norm["q"],
@@ -70,7 +70,7 @@ class Sublayer:
     def forward(self, x, c_h, rounds=3):
         """y = x + attention(x) with head budgets c_h (candidate key blocks kept per row)."""
         buf = self._buffers(c_h)
-        self.inputs(x)
+        self.inputs(x, buf.ws)
         ress.forward(self.d, self.Q, self.K, self.V, buf.F, list(c_h), rounds, 0.5, buf.ws, buf.row_ptr, buf.col_idx,
                      buf.O, buf.J_best)
         ress.out_proj(self.d, buf.O, self.W_o, x, self.y, buf.ws)
@@ -87,7 +87,7 @@ class Sublayer:
         """Gradients of sum(dy y) for dense attention: of the residual stream, of the norms' parameters
         and of the outputs of the three projections."""
         W, ws = self.W, self._buffers([self.candidates] * self.H).ws
-        self.inputs(x)
+        self.inputs(x, ws)
         # the projections' outputs before norm and rotation, which the head norm's gradient reads
         ress.qkv_proj(self.d, self.h, W["q"], W["k"], W["v"], self.raw["q"], self.raw["k"], self.raw["v"], ws,
                       b_q=self.b["q"], b_k=self.b["k"], b_v=self.b["v"])
