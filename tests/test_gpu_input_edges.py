@@ -19,6 +19,15 @@ def ress():
     return r
 
 
+@pytest.fixture(autouse=True)
+def float32_by_default():
+    """Tensors made without a dtype here are float32, whatever other files left as the default."""
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(before)
+
+
 def normal(seed, *shape):
     g = torch.Generator(device="cuda").manual_seed(seed)
     return torch.randn(*shape, generator=g, device="cuda", dtype=torch.float32)
@@ -89,3 +98,14 @@ def test_rope_of_given_frequencies_at_the_ends_of_int32(ress):
             bound = 3.2 * 2.0 ** -25 + 2 * 6.3 * 2.0 ** -32 + 2 * 2.0 ** -24
             assert abs(float(y[i, 0, 2 * k]) - float(torch.cos(angle))) <= bound, (p, f)
             assert abs(float(y[i, 0, 2 * k + 1]) - float(torch.sin(angle))) <= bound, (p, f)
+
+
+def test_heads_as_the_library_takes_them(ress):
+    """The bytes that the binding makes of tensors are those of the struct that callers with raw pointers pack."""
+    x = torch.zeros(7, 10, 64, device="cuda")[:, 1:4]
+    y, dx = torch.zeros(7, 3, 64, device="cuda"), torch.zeros(3, 7, 64, device="cuda").transpose(0, 1)
+    w, b, dw, db = torch.zeros(4, 64, device="cuda").unbind()
+    got = ress._t.rope_heads(y, x, dx, (w, b), (dw, db), 7, 64, 2)
+    assert len(got) == ress._ROPE_HEADS.size
+    assert ress._ROPE_HEADS.unpack(got) == (3, 1, w.data_ptr(), b.data_ptr(), x.data_ptr(), 640, 64, y.data_ptr(), 192, 64,
+                                            dx.data_ptr(), 64, 448, dw.data_ptr(), db.data_ptr())
