@@ -86,7 +86,8 @@ class RopePlan(ctypes.Structure):
 # ctypes structures would be most of it)
 _NORM = struct.Struct("@qiiiif4xqqqq")              # rows, width, types, eps, strides
 _HEAD_NORM = struct.Struct("@i4xPP")                # enabled, weight, bias
-_ROPE_HEADS = struct.Struct("@i4xi4xPPPqqPqqPqqPP")  # n_heads, norm, x, y, dx, dweight, dbias
+_ROPE_HEADS = struct.Struct("@i4xi4xPPPqqPqqPqqPP")  # n_heads, norm, x, y, dx, dweight, dbias; for callers with
+#                                                       raw pointers (tensors.cpp fills it from tensors)
 
 
 _c = ctypes

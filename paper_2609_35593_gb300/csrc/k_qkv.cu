@@ -161,7 +161,7 @@ struct QHead {
   const float4* turn;           // the token's entry of the cosines and sines
 };
 
-// The accumulators plus the bias; with a norm, their mean and 1 / standard deviation (else 0 and 1).
+// The accumulators plus the bias.
 __device__ __forceinline__ void q_add_bias(const uint16_t* bias, F2 (&u)[32]) {
   if (!bias) return;
 #pragma unroll
@@ -173,6 +173,8 @@ __device__ __forceinline__ void q_add_bias(const uint16_t* bias, F2 (&u)[32]) {
   }
 }
 
+// The head's row: bias, norm and the unrolled rotation of pairs H apart (H = 0: none).  With a norm, mean and rstd
+// are left for the pairs that are turned one by one afterwards (else 0 and 1).
 template <int H>
 __device__ __forceinline__ void q_head(uint32_t acc, const QHead& a, uint8_t* row, int r, float& mean, float& rstd) {
   using rows::add2;

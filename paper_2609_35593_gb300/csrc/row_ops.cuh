@@ -264,23 +264,7 @@ __device__ __forceinline__ float2 rope_cos_sin(int32_t pos, uint64_t turns) {
   return r;
 }
 
-// Where channel c stands in the rotation: its pair (-1: not rotated), whether it is the pair's second
-// channel, and the other one.
-struct RopeChannel {
-  int pair, second, partner;
-};
-__host__ __device__ inline RopeChannel rope_channel(const ress_rope_plan& plan, int c) {
-  if (c >= 2 * plan.n_pairs) return {-1, 0, c};
-  if (plan.layout == RESS_ROPE_INTERLEAVED) return {c >> 1, c & 1, c ^ 1};
-  int start = 0, half = plan.n_pairs;  // channels before this section, pairs in it
-  if (plan.layout == RESS_ROPE_SECTIONS) {
-    int a = 0;
-    while (c >= start + plan.axis_dims[a]) start += plan.axis_dims[a++];
-    half = plan.axis_dims[a] / 2;
-  }
-  const int i = c - start, second = i >= half;
-  return {start / 2 + i - second * half, second, second ? c - half : c + half};
-}
+// The axis of a pair.
 __host__ __device__ inline int rope_axis(const ress_rope_plan& plan, int pair) {
   int a = 0, end = plan.axis_dims[0] / 2;
   while (pair >= end) end += plan.axis_dims[++a] / 2;
