@@ -12,6 +12,8 @@
  * What forms Q, K and V out of the residual stream before it: ress_layer_norm, ress_qkv_proj
  * (projection, per-head norm and rotary positions in one kernel), ress_rope (the latter two on
  * their own), and the gradients ress_layer_norm_bwd and ress_rope_bwd.
+ * Dense attention over packed sequences and its gradient (ress_attn, ress_attn_bwd), over a paged
+ * cache (ress_paged_attn), and the cache itself (ress_cache_tables, ress_cache_write).
  * Also: the ablation variants of the selection (ress_score_variant, ress_restore_variant),
  * the residual update and token-level drift (ress_out_proj, ress_token_drift), an
  * allocation-free attention entry point, and a bounded-wait self-test of the error path.
@@ -414,6 +416,105 @@ int ress_qkv_proj(const ress_dims* dims, const uint16_t* x, const uint16_t* W_q,
                   const int32_t* pos, const ress_head_norm* q_norm, const ress_head_norm* k_norm,
                   int32_t param_type, float eps, uint16_t* Q, uint16_t* K, uint16_t* V, void* ws,
                   size_t ws_bytes, void* stream);
+
+/* ---- Dense attention, packed or paged -----------------------------------------------------
+ * Exact attention of sequences on their own keys: the frame attention between the layers that
+ * this library sparsifies, dense reference layers, packed batches of any lengths, and views or
+ * tokens that arrive one after another and see a paged cache of what came before.  With
+ * scores x = q.k / 8 of a row on a key
+ *   s = cap tanh(x / cap) - slope[head] |distance|,   lse = log sum exp(s),   o = sum exp(s - lse) v
+ * over the keys that the row sees, distance = its position - the key's.  The last row and the last
+ * key of a sequence stand at the same position: row i of a sequence of n_q rows and n_k keys at
+ * n_k - n_q + i.  causal: a row sees the keys up to its own position, and the first prefix[b]
+ * of its sequence whatever its position; otherwise all of them.  A row that sees no key gets o = 0,
+ * lse = -infinity.  Keys outside a sequence and pages' unused rows change nothing, whatever they
+ * hold; K and V of a sequence's own keys should be finite (a masked key's infinity in V still
+ * reaches rows by 0 x infinity).  Products are exact and summed in float32; the exponentials are
+ * rounded to the tensors' type for their product with V, their sums are not.
+ *
+ * Heads are [tokens, heads, 64] with strides in elements, multiples of 8 above 0 (any stride where
+ * there is one head or one token), data 16-byte aligned.  Heads h g .. h g + g - 1 of Q use head h
+ * of K and V, g = q_heads / kv_heads at most RESS_MAX_GROUP.  The starts of the sequences are device
+ * data, so that a captured graph serves other lengths: q_start[n_seqs + 1] ascending, rows behind the last
+ * sequence are neither read nor written (a tile's other rows may be read).  A start or a length
+ * outside its tensor is recorded in the status word (RESS_EDEVICE); that sequence then has no rows
+ * (or keys).  ws: 256-byte aligned, ress_attn_workspace_bytes(rows, q_heads, backward) bytes, a status
+ * word first (zero before the first call, read by ress_status); the rest needs no initialisation.
+ * Calls on one workspace must not overlap. */
+#define RESS_MAX_GROUP 64
+#define RESS_MAX_SEQS 8192 /* of ress_cache_tables */
+typedef struct {
+  int32_t type;     /* RESS_BF16 or RESS_F16: of all heads                                    */
+  int32_t n_seqs;   /* >= 0                                                                   */
+  int32_t q_heads, kv_heads;
+  int32_t causal;   /* 0 or 1                                                                 */
+  float cap;        /* > 0, or 0 for none                                                     */
+  int64_t rows;     /* of q, o (and their gradients), lse: below 2^31                         */
+  int64_t keys;     /* of k, v (and their gradients); not for paged calls                     */
+  const int32_t* q_start; /* device int32 [n_seqs + 1]; NULL: one sequence of all rows        */
+  const int32_t* k_start; /* device int32 [n_seqs + 1]; NULL: one sequence of all keys        */
+  const int32_t* prefix;  /* device int32 [n_seqs], only with causal; NULL: none              */
+  const float* slopes;    /* device float32 [q_heads]; NULL: none                             */
+  ress_heads q, k, v, o;
+  float* lse;             /* device float32 [q_heads, rows]; output, NULL to skip             */
+} ress_attn_args;
+size_t ress_attn_workspace_bytes(int64_t rows, int32_t q_heads, int32_t backward);
+int ress_attn(const ress_attn_args* a, void* ws, size_t ws_bytes, void* stream);
+
+/* Gradients of ress_attn with respect to q, k and v from that of o (d_o): a->o and a->lse as the call
+ * wrote them (lse is needed here).  The gradients of heads of K and V that several heads of Q use are
+ * added up in float32, in a fixed order.  p and the gradients of the scores are rounded to the
+ * tensors' type for their products (in f16 after scaling by a power of two).  dq, dk, dv are written for
+ * the rows and keys of every sequence, and must not overlap inputs.  ws: the workspace of backward = 1. */
+typedef struct {
+  ress_heads d_o, dq; /* as q */
+  ress_heads dk, dv;  /* as k */
+} ress_attn_grads;
+int ress_attn_bwd(const ress_attn_args* a, const ress_attn_grads* g, void* ws, size_t ws_bytes,
+                  void* stream);
+
+/* The same over a paged cache that holds the sequences' keys, those of the rows themselves
+ * included: sequence b has lens[b] of them, key j in row j mod page of page
+ * table[b, j / page].  a->k and a->v: heads of the pages' rows, [n_pages, page, kv_heads, 64] with
+ * k_page_stride and v_page_stride elements between pages; a->keys and a->k_start are not used.  page: a
+ * multiple of 8.  An entry that is needed and is no page is recorded in the status word, and its
+ * keys count as zeros.  (ress_cache_tables makes table, lens and q_start.) */
+typedef struct {
+  const int32_t* table;   /* device int32 [n_seqs, table_cols]                                */
+  const int32_t* lens;    /* device int32 [n_seqs]                                            */
+  int64_t table_stride;   /* elements between rows of the table                               */
+  int32_t table_cols, page;
+  int64_t n_pages;        /* n_pages * page below 2^31                                        */
+  int64_t k_page_stride, v_page_stride;
+} ress_pages;
+int ress_paged_attn(const ress_attn_args* a, const ress_pages* pages, void* ws, size_t ws_bytes,
+                    void* stream);
+
+/* Pages and slots for the next add[b] tokens of every sequence, which has have[b] of them: entries of
+ * the table that begin with these tokens are filled from free[taken[0]..] in order of the sequences.
+ * Outputs: lens[b] = have[b] + add[b]; q_start [n_seqs + 1], where the sequences' new tokens begin
+ * among all of them; slots, pos [n_slots]: each new token's row in the cache (page x page size +
+ * row) and its position in its sequence, -1 behind the last token; taken_out[0], the free pages used
+ * so far.  Where pages, table columns or slots do not suffice, or a length is negative, the status word says so,
+ * and tokens without a place get slot -1.  All device int32; outputs must not be inputs, but for
+ * the table.  ws: 256 bytes, a status word as above. */
+typedef struct {
+  int32_t n_seqs;  /* 0..RESS_MAX_SEQS                  */
+  int32_t page;    /* tokens of a page, >= 1            */
+  int32_t table_cols;
+  int64_t table_stride, n_free, n_slots; /* below 2^31  */
+  const int32_t *have, *add, *free, *taken;
+  int32_t *table, *lens, *q_start, *slots, *pos, *taken_out;
+} ress_tables;
+int ress_cache_tables(const ress_tables* t, void* ws, size_t ws_bytes, void* stream);
+
+/* Writes K and V of `tokens` tokens (heads as in ress_attn, any 16-bit type) to rows slots[i] of the
+ * pages (kc, vc: as k and v of ress_paged_attn); a slot of -1 is passed over, another one outside the
+ * pages is recorded in the status word.  Slots must differ.  ws: 256 bytes, a status word as above. */
+int ress_cache_write(int64_t tokens, int32_t kv_heads, const ress_heads* k, const ress_heads* v,
+                     const int32_t* slots, const ress_heads* kc, const ress_heads* vc,
+                     int64_t k_page_stride, int64_t v_page_stride, int32_t page, int64_t n_pages,
+                     void* ws, size_t ws_bytes, void* stream);
 
 /* Allocation-free variant of ress_sparse_attn (the paper has no counterpart: this is an
  * interface for callers, not part of the method).  It is for callers that cannot allocate

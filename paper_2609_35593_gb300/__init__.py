@@ -141,6 +141,13 @@ _SIGS = {
                                  _P, _P, _P, _c.c_size_t, _P]),
     "ress_qkv_proj": (_c.c_int, [_c.POINTER(Dims), _P, _P, _P, _P, _P, _P, _P, _c.POINTER(RopePlan), _P,
                                  _P, _P, _c.c_int32, _c.c_float, _P, _P, _P, _P, _c.c_size_t, _P]),
+    "ress_attn_workspace_bytes": (_c.c_size_t, [_c.c_int64, _c.c_int32, _c.c_int32]),
+    "ress_attn": (_c.c_int, [_P, _P, _c.c_size_t, _P]),
+    "ress_attn_bwd": (_c.c_int, [_P, _P, _P, _c.c_size_t, _P]),
+    "ress_paged_attn": (_c.c_int, [_P, _P, _P, _c.c_size_t, _P]),
+    "ress_cache_tables": (_c.c_int, [_P, _P, _c.c_size_t, _P]),
+    "ress_cache_write": (_c.c_int, [_c.c_int64, _c.c_int32, _P, _P, _P, _P, _P, _c.c_int64, _c.c_int64, _c.c_int32,
+                                    _c.c_int64, _P, _c.c_size_t, _P]),
 }
 for _name, (_res, _args) in _SIGS.items():
     _f = getattr(_lib, _name)
@@ -645,6 +652,155 @@ def qkv_proj(d: Dims, x, W_q, W_k, W_v, Q, K, V, ws, b_q=None, b_k=None, b_v=Non
                               _HEAD_NORM.pack(*_head_norm(k_norm, HEAD_DIM, "k_norm")), _norm_code(q_norm, k_norm), eps,
                               _dense(Q, n * out, "Q"), _dense(K, n * out, "K"), _dense(V, n * out, "V"),
                               *_scratch(ws), _stream(stream)))
+
+
+# ---- dense attention, packed or paged -------------------------------------------------
+def attn_workspace_bytes(rows: int, q_heads: int, backward: bool = False) -> int:
+    """Workspace of attn and paged_attn (backward: attn_bwd) on tensors of this many rows; its first word is a
+    status word, zero before the first call."""
+    n = _lib.ress_attn_workspace_bytes(rows, q_heads, 1 if backward else 0)
+    if n == 0:
+        raise RessError(-1, _lib.ress_last_error().decode())
+    return n
+
+
+def _on_current_device(t):
+    """The kernels run where the current stream is."""
+    if t.get_device() != _torch()._C._cuda_getDevice():
+        raise ValueError(f"tensors on {t.device}, which is not the current CUDA device")
+
+
+def _attn_args(q, k, v, o, lse, q_start, k_start, prefix, slopes, causal, cap, paged):
+    args = _t.attn_args(q, k, v, o, lse, q_start, k_start, prefix, slopes, bool(causal), cap, paged)
+    if args is None:
+        _refuse_attn(q, k, v, o, lse, q_start, k_start, prefix, slopes, paged)
+    _on_current_device(q)
+    return args
+
+
+def _refuse_tiles(t, name, like, shape=None, pages=False):
+    """Raises unless t is [tokens, heads, 64] (pages: [pages, page, heads, 64]) as the dense attention takes it."""
+    types = _types()[:2] if like is None else (like.dtype,)
+    dims = 4 if pages else 3
+    if (isinstance(t, _torch().Tensor) and t.is_cuda and t.dtype in types and t.dim() == dims and t.shape[-1] == HEAD_DIM
+            and t.stride(-1) == 1 and (like is None or t.device == like.device) and shape in (None, tuple(t.shape))):
+        return
+    if isinstance(t, _torch().Tensor) and t.is_cuda and t.dtype in types:
+        if t.dim() != dims or t.shape[-1] != HEAD_DIM or shape not in (None, tuple(t.shape)):
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected "
+                             f"{shape or ('[pages, page, heads, 64]' if pages else '[tokens, heads, 64]')}")
+        if like is not None and t.device != like.device:
+            raise ValueError(f"{name} is on {t.device}, q on {like.device}")
+        raise ValueError(f"{name}: the channels of a head must be next to each other")
+    _refuse(t, name, types)
+
+
+def _refuse_numbers(t, name, like, n=None, dtype=None):
+    """Raises unless t is None or n contiguous numbers on like's device."""
+    dtype = dtype or _torch().int32
+    if t is None or (isinstance(t, _torch().Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous()
+                     and t.device == like.device and n in (None, t.numel())):
+        return
+    _refuse(t, name, (dtype,), numel=n)
+
+
+def _refuse_attn(q, k, v, o, lse, q_start, k_start, prefix, slopes, paged):
+    _refuse_tiles(q, "q", None)
+    _refuse_tiles(k, "k_pages" if paged else "k", q, pages=paged)
+    _refuse_tiles(v, "v_pages" if paged else "v", q, tuple(k.shape), paged)
+    _refuse_tiles(o, "o", q, tuple(q.shape))
+    if not paged and (q_start is None) != (k_start is None):
+        raise ValueError("q_start and k_start belong together")
+    _refuse_numbers(q_start, "q_start", q)
+    if q_start is not None and q_start.numel() == 0:
+        raise ValueError("q_start has no elements, expected one more than sequences")
+    seqs = 1 if q_start is None else q_start.numel() - 1
+    _refuse_numbers(k_start, "k_start", q, seqs + 1)
+    _refuse_numbers(prefix, "prefix", q, seqs)
+    _refuse_numbers(slopes, "slopes", q, q.shape[1], _torch().float32)
+    _refuse_numbers(lse, "lse", q, q.shape[0] * q.shape[1], _torch().float32)
+    raise ValueError("tensors are too large")
+
+
+def attn(q, k, v, o, ws, q_start=None, k_start=None, lse=None, causal: bool = False, prefix=None, cap: float = 0.0,
+         slopes=None, stream=None):
+    """ress_attn: o [rows, q_heads, 64] = softmax attention of q on k, v [keys, kv_heads, 64], bf16 or f16, each
+    sequence on its own keys: rows q_start[b]..q_start[b + 1], keys k_start[b]..k_start[b + 1] (int32; None: one
+    sequence).  causal, prefix (int32 per sequence), cap, slopes (float32 per head of q): see include/ress.h.
+    lse: float32 [q_heads, rows] output, or None."""
+    a = _attn_args(q, k, v, o, lse, q_start, k_start, prefix, slopes, causal, cap, False)
+    _check(_lib.ress_attn(a, *_scratch(ws), _stream(stream)))
+
+
+def attn_bwd(do, q, k, v, o, lse, dq, dk, dv, ws, q_start=None, k_start=None, causal: bool = False, prefix=None,
+             cap: float = 0.0, slopes=None, stream=None):
+    """ress_attn_bwd: dq, dk, dv from the gradient do of attn's o; o and lse as attn wrote them, the other
+    arguments as it took them."""
+    if lse is None:
+        raise ValueError("lse is the one attn wrote")
+    a = _attn_args(q, k, v, o, lse, q_start, k_start, prefix, slopes, causal, cap, False)
+    g = _t.attn_grads(do, dq, dk, dv, q, k)
+    if g is None:
+        for t, name, like in ((do, "do", q), (dq, "dq", q), (dk, "dk", k), (dv, "dv", k)):
+            _refuse_tiles(t, name, q, tuple(like.shape))
+    _check(_lib.ress_attn_bwd(a, g, *_scratch(ws), _stream(stream)))
+
+
+def paged_attn(q, k_pages, v_pages, table, lens, o, ws, q_start=None, lse=None, causal: bool = False, prefix=None,
+               cap: float = 0.0, slopes=None, stream=None):
+    """ress_paged_attn: as attn, with the keys of sequence b in pages table[b] of k_pages, v_pages [pages, page,
+    kv_heads, 64], lens[b] of them (int32), the new rows' own included."""
+    a = _attn_args(q, k_pages, v_pages, o, lse, q_start, None, prefix, slopes, causal, cap, True)
+    seqs = 1 if q_start is None else q_start.numel() - 1
+    p = _t.pages(k_pages, v_pages, table, lens, seqs)
+    if p is None:
+        _refuse_numbers(lens, "lens", q, seqs)
+        _refuse_table(table, seqs)
+        raise ValueError("lens and table are needed, on q's device")
+    _check(_lib.ress_paged_attn(a, p, *_scratch(ws), _stream(stream)))
+
+
+def _refuse_table(table, seqs=None):
+    if not isinstance(table, _torch().Tensor) or not table.is_cuda or table.dtype != _torch().int32:
+        _refuse(table, "table", (_torch().int32,))
+    if table.dim() != 2 or seqs not in (None, table.shape[0]):
+        raise ValueError(f"table has shape {tuple(table.shape)}, expected [{'sequences' if seqs is None else seqs}, columns]")
+    if table.shape[1] > 1 and table.stride(1) != 1:
+        raise ValueError("table must have contiguous rows")
+
+
+def cache_tables(have, add, free, taken, table, page: int, lens, q_start, slots, pos, taken_out, ws, stream=None):
+    """ress_cache_tables: the next add[b] tokens of sequences that have have[b] get pages free[taken[0]..] where
+    they begin one (entered into table [sequences, columns]), and outputs lens, q_start [sequences + 1], slots and
+    pos (one per token; -1 behind the last), taken_out [1]; all int32."""
+    a = _t.tables(have, add, free, taken, table, page, lens, q_start, slots, pos, taken_out)
+    if a is None:
+        _refuse_table(table)
+        n = table.shape[0]
+        for t, name, size in ((have, "have", n), (add, "add", n), (free, "free", None), (taken, "taken", 1), (lens, "lens", n),
+                              (q_start, "q_start", n + 1), (slots, "slots", None), (pos, "pos", None),
+                              (taken_out, "taken_out", 1)):
+            if t is None:
+                raise TypeError(f"{name} must be a torch.Tensor")
+            _refuse_numbers(t, name, table, size)
+        raise ValueError(f"page {page} out of range, or slots and pos of different sizes")
+    _on_current_device(table)
+    _check(_lib.ress_cache_tables(a, *_scratch(ws), _stream(stream)))
+
+
+def cache_write(k, v, slots, k_pages, v_pages, ws, stream=None):
+    """ress_cache_write: k, v [tokens, kv_heads, 64] into rows slots (int32, -1: none) of k_pages, v_pages [pages, page,
+    kv_heads, 64]."""
+    a = _t.cache_rows(k, v, slots, k_pages, v_pages)
+    if a is None:
+        _refuse_tiles(k, "k", None)
+        _refuse_tiles(v, "v", k, tuple(k.shape))
+        _refuse_tiles(k_pages, "k_pages", k, pages=True)
+        _refuse_tiles(v_pages, "v_pages", k, tuple(k_pages.shape), True)
+        _refuse_numbers(slots, "slots", k, k.shape[0])
+        raise ValueError(f"k has {k.shape[1]} heads, the pages {k_pages.shape[2]}, or slots are missing")
+    _on_current_device(k)
+    _check(_lib.ress_cache_write(*a, *_scratch(ws), _stream(stream)))
 
 
 class Buffers:

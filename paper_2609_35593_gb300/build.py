@@ -25,7 +25,7 @@ LIB = os.path.join(HERE, "libress.so")
 TENSORS = os.path.join(HERE, "_tensors.so")
 SOURCES = ["ress_abi.cu", "k_select.cu", "k_attn.cu", "k_dot.cu", "k_yagg.cu", "k_oproj.cu",
            "k_norm.cu", "k_rope.cu", "k_rope_bwd.cu", "k_rope_few.cu",
-           "k_qkv.cu"]
+           "k_qkv.cu", "k_flash.cu", "k_flash_bwd.cu", "k_cache.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall",
          "--expt-relaxed-constexpr", "-I", INCLUDE, "-I", CSRC]

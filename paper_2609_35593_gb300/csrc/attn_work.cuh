@@ -1,0 +1,269 @@
+// What dense attention over packed or paged sequences (k_flash.cu) and its gradient (k_flash_bwd.cu) share:
+// the sequences, the equal shares of their work that the CTAs take, and the rules of the masks.
+//
+// Work.  An item is what stays on chip while tiles stream past it: a range of query rows of one head of K
+// (of all the heads of Q that share it), or in the gradient of K and V a range of keys.  Lengths are device
+// data, so the host knows only the totals: every CTA adds up all sequences' work itself (a few hundred
+// instructions, sequences over its threads) and takes share c of C of it, wherever that begins and ends.
+// An item that several CTAs have shares of leaves partial results in the workspace, two slots per CTA, which
+// a second kernel adds up in the order of the shares: no atomics, the same bits for the same inputs.
+// With whole items instead, 176 items of 172 tiles on 152 SMs (one image over the keys of 32) would take two
+// rounds where 1.16 do.
+//
+// An item's work is kOver + mul x its length, a length being the keys (or rows) that it sees, in closed form
+// over the items of a sequence: a constant up to some item, then linear (causal), the last one on its own.
+#pragma once
+
+#include "row_ops.cuh"
+#include "sm100_ptx.cuh"
+
+namespace ress {
+namespace work {
+using namespace ptx;
+
+constexpr int kMaxCtas = 192;            // most CTAs that share a call's work (one per SM)
+constexpr int kTile = 64;                // columns of a tile
+constexpr int64_t kOver = 8 * 2 * kTile; // an item's loads and epilogue, as work: two tiles
+constexpr int64_t kLeast = 8 * 4 * kTile;  // least share of a CTA: four tiles
+constexpr uint64_t kWaitNs = 2000000000ull;  // 2 s per wait
+constexpr uint64_t kDrainNs = 200000000ull;  // 0.2 s to drain after an abort
+
+// One sequence: rows [q0, q0 + nq) of Q, keys [k0, k0 + nk) (paged: positions 0..nk-1 of its table row).
+// Row t stands at position d + t; with a causal mask it sees the keys below max(p, d + t + 1).
+struct Seq {
+  int q0, nq, k0, nk, d, p;
+};
+
+__device__ __forceinline__ Seq load_seq(const DenseArgs& a, int b, uint32_t* status) {
+  Seq s;
+  int64_t q0 = 0, q1 = a.rows, k0 = 0, k1 = a.keys;
+  if (a.q_start) q0 = a.q_start[b], q1 = a.q_start[b + 1];
+  if (a.table)
+    k1 = a.lens[b];
+  else if (a.k_start)
+    k0 = a.k_start[b], k1 = a.k_start[b + 1];
+  const int64_t most = a.table ? (int64_t)a.table_cols * a.page : a.keys;
+  if (q0 < 0 || q1 < q0 || q1 > a.rows) {  // such a sequence has no rows
+    if (status) flag_status(status, kStatusBadRow);
+    q0 = q1 = 0;
+  }
+  if (k0 < 0 || k1 < k0 || k1 > most) {  // or no keys
+    if (status) flag_status(status, kStatusBadRow);
+    k0 = k1 = 0;
+  }
+  s.q0 = (int)q0, s.nq = (int)(q1 - q0), s.k0 = (int)k0, s.nk = (int)(k1 - k0);
+  s.d = s.nk - s.nq;
+  s.p = 0;
+  if (a.causal && a.prefix) s.p = max(0, min(a.prefix[b], s.nk));
+  return s;
+}
+
+// Keys that the row at position `pos` of a sequence sees: those below this.
+__device__ __forceinline__ int row_limit(const DenseArgs& a, const Seq& s, int pos) {
+  return a.causal ? min(s.nk, max(s.p, pos + 1)) : s.nk;
+}
+
+// Items 0..n-1 of one head of a sequence: lengths and work.
+struct Line {
+  int n, cnt;          // items; those of the constant length
+  int64_t a, b, step;  // length of items below cnt; b + step j of the others
+  int64_t last, last_mul;
+  __device__ int64_t length(int j) const { return j == n - 1 ? last : j < cnt ? a : b + step * j; }
+  __device__ int64_t before(int j) const {  // work of items 0..j-1
+    if (n == 0) return 0;
+    const int64_t m = min(j, n - 1), c = min((int64_t)cnt, m);
+    int64_t w = m * kOver + 8 * (c * a + (m - c) * b + step * ((m * (m - 1) - c * (c - 1)) / 2));
+    if (j == n) w += kOver + last_mul * last;
+    return w;
+  }
+};
+
+// Query rows as items of `per` tokens; one that fills less than half of its rows takes 5/8 of the time.
+__device__ __forceinline__ Line row_line(const DenseArgs& a, const Seq& s, int per, int half) {
+  Line l;
+  l.n = (s.nq + per - 1) / per;
+  l.cnt = l.n, l.a = s.nk, l.b = l.step = 0;
+  if (a.causal && l.n > 0) {
+    l.cnt = s.p - s.d >= per ? min(l.n, (s.p - s.d) / per) : 0;
+    l.a = s.p, l.b = (int64_t)s.d + per, l.step = per;
+  }
+  l.last = s.nk;
+  l.last_mul = s.nq - (l.n - 1) * per > half ? 8 : 5;
+  return l;
+}
+
+// Keys as items of `per`; their lengths are the rows (tokens of all heads) that see any of them.
+__device__ __forceinline__ int first_row(const DenseArgs& a, const Seq& s, int key) {
+  return a.causal && key >= s.p ? max(0, min(s.nq, key - s.d)) : 0;
+}
+__device__ __forceinline__ Line key_line(const DenseArgs& a, const Seq& s, int per) {
+  Line l;
+  l.n = (s.nk + per - 1) / per;
+  l.cnt = l.n, l.a = (int64_t)s.nq * a.group, l.b = l.step = 0;
+  if (a.causal && l.n > 0) {
+    const int top = max(s.d, s.p - 1);  // items that start here or before are seen by every row
+    l.cnt = top >= 0 ? min(l.n, top / per + 1) : 0;
+    l.b = (int64_t)s.nk * a.group, l.step = -per * a.group;
+  }
+  l.last = l.n > 0 ? (int64_t)(s.nq - first_row(a, s, (l.n - 1) * per)) * a.group : 0;
+  l.last_mul = 8;
+  return l;
+}
+
+// Share [x0, x1) of all work: sequence b0 holds x0 and begins at `base`.
+struct Range {
+  int64_t total, x0, x1, base;
+  int b0, active;
+};
+__device__ __forceinline__ int active_ctas(int64_t total, int ctas) {
+  return (int)max((int64_t)1, min((int64_t)ctas, total / kLeast));
+}
+__device__ __forceinline__ int64_t bound(int64_t total, int active, int c) { return total / active * c + total % active * c / active; }
+
+// All threads of the CTA: share `cta` of `ctas`.  scratch: 34 words of shared memory; status: NULL, or where
+// sequences outside their tensors are told.
+template <class LineOf>
+__device__ __forceinline__ Range find_range(const DenseArgs& a, LineOf line_of, int ctas, int cta, int64_t* scratch,
+                                            uint32_t* status) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
+  const int per = (a.n_seqs + (int)blockDim.x - 1) / (int)blockDim.x;
+  const int lo = min(a.n_seqs, tid * per), hi = min(a.n_seqs, lo + per);
+  int64_t sum = 0;
+  for (int b = lo; b < hi; ++b) {
+    const Line l = line_of(load_seq(a, b, status));
+    sum += a.kv_heads * l.before(l.n);
+  }
+  int64_t inc = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t v = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += v;
+  }
+  if (lane == 31) scratch[warp] = inc;
+  __syncthreads();
+  int64_t before = inc - sum, total = 0;
+  for (int w = 0; w < warps; ++w) {
+    if (w < warp) before += scratch[w];
+    total += scratch[w];
+  }
+  Range r;
+  r.total = total;
+  r.active = active_ctas(total, ctas);
+  r.x0 = cta < r.active ? bound(total, r.active, cta) : total;
+  r.x1 = cta < r.active ? bound(total, r.active, cta + 1) : total;
+  if (r.x0 >= before && r.x0 < before + sum) {
+    int64_t at = before;
+    for (int b = lo; b < hi; ++b) {
+      const Line l = line_of(load_seq(a, b, nullptr));
+      const int64_t w = a.kv_heads * l.before(l.n);
+      if (r.x0 < at + w) {
+        scratch[32] = at;
+        scratch[33] = b;
+        break;
+      }
+      at += w;
+    }
+  }
+  __syncthreads();
+  r.base = scratch[32];
+  r.b0 = (int)scratch[33];
+  return r;
+}
+
+// The items that a share touches, one after another.
+struct Cursor {
+  Seq s;
+  Line l;
+  int b, h, j;
+  int64_t start, weight;  // of the item, in all work
+};
+template <class LineOf>
+__device__ __forceinline__ void seek(const DenseArgs& a, LineOf line_of, int64_t x, int b, int64_t base, Cursor& c) {
+  c.b = b;
+  c.s = load_seq(a, b, nullptr);
+  c.l = line_of(c.s);
+  const int64_t one = c.l.before(c.l.n), rem = x - base;
+  c.h = (int)(rem / one);
+  const int64_t r = rem % one;
+  int lo = 0, hi = c.l.n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (c.l.before(mid) <= r)
+      lo = mid;
+    else
+      hi = mid - 1;
+  }
+  c.j = lo;
+  c.start = base + c.h * one + c.l.before(lo);
+  c.weight = c.l.before(lo + 1) - c.l.before(lo);
+}
+// The next item (false: there is none).
+template <class LineOf>
+__device__ __forceinline__ bool next(const DenseArgs& a, LineOf line_of, Cursor& c) {
+  c.start += c.weight;
+  if (++c.j == c.l.n) {
+    c.j = 0;
+    if (++c.h == a.kv_heads) {
+      c.h = 0;
+      do {
+        if (++c.b == a.n_seqs) return false;
+        c.s = load_seq(a, c.b, nullptr);
+        c.l = line_of(c.s);
+      } while (c.l.n == 0);
+    }
+  }
+  c.weight = c.l.before(c.j + 1) - c.l.before(c.j);
+  return true;
+}
+// Tiles [t0, t1) of an item's n that share [x0, x1) has.
+__device__ __forceinline__ void tiles_of(const Cursor& c, int64_t x0, int64_t x1, int n, int& t0, int& t1) {
+  const int64_t lo = max(x0 - c.start, (int64_t)0), hi = min(x1 - c.start, c.weight);
+  t0 = (int)(lo * n / c.weight);
+  t1 = (int)(hi * n / c.weight);
+}
+
+// Bounded wait for a whole warp: every lane tests the barrier, else lane 0 polls and tells the others, so that
+// no lane leaves code its neighbours stay in.
+__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile int* abort) {
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  int ok = 1;
+  if ((threadIdx.x & 31) == 0) ok = mbar_wait(bar, parity, abort, kWaitNs) ? 1 : 0;
+  ok = __shfl_sync(0xffffffffu, ok, 0);
+  __syncwarp();
+  return ok != 0;
+}
+
+template <bool kF16>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  uint32_t r;
+  if (kF16)
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  else
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+template <bool kF16>
+__host__ __device__ constexpr uint32_t idesc16(int M, int N, bool b_mn_major) {
+  return kF16 ? idesc_bf16_f32(M, N, b_mn_major) & ~((1u << 7) | (1u << 10)) : idesc_bf16_f32(M, N, b_mn_major);
+}
+
+// 64 bytes of a 128-byte row of a swizzled 64-row tile become 0; thread i of 128 takes half of row i / 2.
+__device__ __forceinline__ void zero_rows(uint8_t* tile, int from, int i) {
+  if (i / 2 >= from) {
+    uint4* p = reinterpret_cast<uint4*>(tile + (i / 2) * 128 + (i & 1) * 64);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) p[k] = make_uint4(0u, 0u, 0u, 0u);
+  }
+}
+
+// tanh.  Near 0, where 1 - 2 / (e^2u + 1) cancels, its series (to u^7: off by 2^-21 of itself at |u| = 1/4,
+// where the other form's rounding is 2^-22).
+__device__ __forceinline__ float tanh_of(float u) {
+  const float e = ex2(u * 2.8853900817779268f), u2 = u * u;
+  const float far = 1.0f - __fdividef(2.0f, e + 1.0f);
+  const float near = u * fmaf(u2, fmaf(u2, fmaf(u2, -17.0f / 315.0f, 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
+  return fabsf(u) < 0.25f ? near : far;
+}
+
+}  // namespace work
+}  // namespace ress

@@ -945,6 +945,214 @@ int ress_qkv_proj(const ress_dims* d, const uint16_t* x, const uint16_t* W_q, co
 }  // extern "C"
 
 // ---------------------------------------------------------------------------------------
+// Dense attention, packed or paged, and the cache.
+// ---------------------------------------------------------------------------------------
+namespace {
+
+// Heads that TMA reads or 16-byte accesses touch: [n tokens, heads, 64] (paged: a page's rows).
+int check_tiles(const ress_heads& h, int64_t tokens, int heads, bool output, const char* name) {
+  int e = check_ptr(h.data, 16, name);
+  if (e) return e;
+  const struct { int64_t n, stride; const char* what; } dims[2] = {{heads, h.head_stride, "head"},
+                                                                   {tokens, h.token_stride, "token"}};
+  for (const auto& d : dims)
+    if (d.n > 1 && (d.stride < 8 || d.stride % 8 || d.stride > (INT64_C(1) << 38) || d.stride > INT64_MAX / 16 / d.n))
+      return fail(RESS_EINVAL, "%s: %s stride %lld is not a multiple of 8 in range", name, d.what, (long long)d.stride);
+  if (!output) return RESS_OK;
+  // heads of a token, then tokens (or the other way round), each clear of the one before
+  const int64_t hs = heads > 1 ? h.head_stride : INT64_MAX / 8, ts = tokens > 1 ? h.token_stride : INT64_MAX / 8;
+  const int64_t ht = heads > 1 ? (heads - 1) * hs : 0, tt = tokens > 1 ? (tokens - 1) * ts : 0;
+  if (!(hs >= 64 && ts >= ht + 64) && !(ts >= 64 && hs >= tt + 64))
+    return fail(RESS_EINVAL, "%s: strides %lld, %lld make heads overlap", name, (long long)h.token_stride,
+                (long long)h.head_stride);
+  return RESS_OK;
+}
+
+size_t attn_bytes(int64_t rows, int32_t q_heads, int32_t backward) {
+  const int64_t parts = 256 + ress::align256((int64_t)ress::dense_part_bytes());
+  return (size_t)(backward ? parts + ress::align256(rows * q_heads * 8) + ress::kBigParts * 4 : parts);
+}
+
+int check_rows(int64_t rows, int32_t q_heads) {
+  if (rows < 0 || rows > INT32_MAX) return fail(RESS_EINVAL, "rows %lld outside 0..2^31-1", (long long)rows);
+  if (q_heads < 1 || q_heads > RESS_ROPE_MAX_HEADS)
+    return fail(RESS_EUNSUPPORTED, "q_heads %d outside 1..%d", q_heads, RESS_ROPE_MAX_HEADS);
+  return RESS_OK;
+}
+
+// The checks that the dense attention calls share; fills out.
+int attn_checks(const ress_attn_args* a, const ress_pages* pg, bool backward, void* ws, size_t ws_bytes,
+                ress::DenseArgs* out) {
+  if (!a) return fail(RESS_EINVAL, "args is NULL");
+  int e;
+  if (a->type != RESS_BF16 && a->type != RESS_F16) return fail(RESS_EUNSUPPORTED, "type %d is neither bf16 nor f16", a->type);
+  if ((e = check_rows(a->rows, a->q_heads))) return e;
+  if (a->kv_heads < 1 || a->q_heads % a->kv_heads || a->q_heads / a->kv_heads > RESS_MAX_GROUP)
+    return fail(RESS_EUNSUPPORTED, "%d heads of Q over %d of K (a multiple, at most %d times)", a->q_heads, a->kv_heads,
+                RESS_MAX_GROUP);
+  if (a->n_seqs < 0 || a->n_seqs > INT32_MAX / 2) return fail(RESS_EINVAL, "n_seqs %d out of range", a->n_seqs);
+  if (a->causal != 0 && a->causal != 1) return fail(RESS_EINVAL, "causal is %d, not 0 or 1", a->causal);
+  if (!(a->cap >= 0.0f && a->cap <= FLT_MAX) || (a->cap > 0.0f && a->cap < 1e-30f))
+    return fail(RESS_EINVAL, "cap %g is neither 0 nor a number in 1e-30..", (double)a->cap);
+  if (a->prefix && !a->causal) return fail(RESS_EINVAL, "a prefix without causal (every row sees every key)");
+  if ((e = check_opt_ptr(a->q_start, 4, "q_start")) || (e = check_opt_ptr(a->k_start, 4, "k_start")) ||
+      (e = check_opt_ptr(a->prefix, 4, "prefix")) || (e = check_opt_ptr(a->slopes, 4, "slopes")) ||
+      (e = check_opt_ptr(a->lse, 4, "lse")))
+    return e;
+  if (a->n_seqs != 1 && (!a->q_start || (!pg && !a->k_start)))
+    return fail(RESS_EINVAL, "%d sequences without their starts", a->n_seqs);
+  if ((e = check_scratch(ws, ws_bytes, attn_bytes(a->rows, a->q_heads, backward)))) return e;
+  *out = ress::DenseArgs{};
+  if (a->rows > 0 && ((e = check_tiles(a->q, a->rows, a->q_heads, false, "q")) ||
+                      (e = check_tiles(a->o, a->rows, a->q_heads, !backward, "o"))))
+    return e;
+  if (pg) {
+    if (pg->page < 8 || pg->page % 8) return fail(RESS_EUNSUPPORTED, "page %d is not a multiple of 8", pg->page);
+    if (pg->n_pages < 0 || pg->n_pages > INT32_MAX / pg->page)
+      return fail(RESS_EINVAL, "%lld pages of %d outside 0..2^31-1 rows", (long long)pg->n_pages, pg->page);
+    if (pg->table_cols < 0 || pg->table_cols > INT32_MAX / pg->page ||
+        (a->n_seqs > 1 && (pg->table_stride < 0 || pg->table_stride > INT64_MAX / 8 / a->n_seqs)))
+      return fail(RESS_EINVAL, "table of %d columns, %lld apart", pg->table_cols, (long long)pg->table_stride);
+    if (a->n_seqs > 0 && a->rows > 0) {
+      if ((e = check_ptr(pg->lens, 4, "lens")) || (e = check_ptr(pg->table, 4, "table")) ||
+          (e = check_tiles(a->k, pg->page, a->kv_heads, false, "k")) ||
+          (e = check_tiles(a->v, pg->page, a->kv_heads, false, "v")))
+        return e;
+      if (pg->n_pages < 1) return fail(RESS_EINVAL, "a cache without pages");
+      for (int64_t s : {pg->k_page_stride, pg->v_page_stride})
+        if (pg->n_pages > 1 && (s < 8 || s % 8 || s > (INT64_C(1) << 38) || s > INT64_MAX / 16 / pg->n_pages))
+          return fail(RESS_EINVAL, "page stride %lld is not a multiple of 8 in range", (long long)s);
+    }
+    out->table = pg->table, out->lens = pg->lens, out->table_stride = pg->table_stride, out->n_pages = pg->n_pages;
+    out->table_cols = pg->table_cols, out->page = pg->page;
+    out->k_page_stride = pg->k_page_stride, out->v_page_stride = pg->v_page_stride;
+  } else {
+    if (a->keys < 0 || a->keys > INT32_MAX) return fail(RESS_EINVAL, "keys %lld outside 0..2^31-1", (long long)a->keys);
+    if (a->keys > 0 && ((e = check_tiles(a->k, a->keys, a->kv_heads, false, "k")) ||
+                        (e = check_tiles(a->v, a->keys, a->kv_heads, false, "v"))))
+      return e;
+    out->keys = a->keys;
+    out->k_start = a->k_start;
+  }
+  out->type = a->type, out->n_seqs = a->n_seqs, out->kv_heads = a->kv_heads, out->group = a->q_heads / a->kv_heads;
+  out->causal = a->causal, out->cap = a->cap, out->rows = a->rows;
+  out->q_start = a->q_start, out->prefix = a->prefix, out->slopes = a->slopes;
+  out->q = a->q, out->k = a->k, out->v = a->v, out->o = a->o, out->lse = a->lse;
+  out->status = static_cast<uint32_t*>(ws);
+  char* w = static_cast<char*>(ws) + 256;
+  out->part = reinterpret_cast<float*>(w);
+  out->stat = reinterpret_cast<float2*>(w += ress::align256((int64_t)ress::dense_part_bytes()));
+  out->big = reinterpret_cast<float*>(w + ress::align256(a->rows * a->q_heads * 8));
+  return RESS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ress_attn_workspace_bytes(int64_t rows, int32_t q_heads, int32_t backward) {
+  return check_rows(rows, q_heads) ? 0 : attn_bytes(rows, q_heads, backward);
+}
+
+int ress_attn(const ress_attn_args* args, void* ws, size_t ws_bytes, void* stream) {
+  ress::DenseArgs a;
+  int e = attn_checks(args, nullptr, false, ws, ws_bytes, &a);
+  if (e) return e;
+  if (a.rows == 0 || a.n_seqs == 0) return ok();
+  cudaError_t ce = ress::launch_flash(a, static_cast<cudaStream_t>(stream));
+  if (ce != cudaSuccess) return cuda_fail(ce, "ress_attn");
+  return ok();
+}
+
+int ress_attn_bwd(const ress_attn_args* args, const ress_attn_grads* g, void* ws, size_t ws_bytes, void* stream) {
+  if (!g) return fail(RESS_EINVAL, "grads is NULL");
+  ress::DenseArgs a;
+  int e = attn_checks(args, nullptr, true, ws, ws_bytes, &a);
+  if (e) return e;
+  if (a.rows > 0 && ((e = check_ptr(a.lse, 4, "lse")) || (e = check_tiles(g->d_o, a.rows, args->q_heads, false, "d_o")) ||
+                     (e = check_tiles(g->dq, a.rows, args->q_heads, true, "dq"))))
+    return e;
+  if (a.keys > 0 && ((e = check_tiles(g->dk, a.keys, a.kv_heads, true, "dk")) ||
+                     (e = check_tiles(g->dv, a.keys, a.kv_heads, true, "dv"))))
+    return e;
+  if ((a.rows == 0 && a.keys == 0) || a.n_seqs == 0) return ok();
+  a.d_o = g->d_o, a.dq = g->dq, a.dk = g->dk, a.dv = g->dv;
+  cudaError_t ce = ress::launch_flash_bwd(a, static_cast<cudaStream_t>(stream));
+  if (ce != cudaSuccess) return cuda_fail(ce, "ress_attn_bwd");
+  return ok();
+}
+
+int ress_paged_attn(const ress_attn_args* args, const ress_pages* pages, void* ws, size_t ws_bytes, void* stream) {
+  if (!pages) return fail(RESS_EINVAL, "pages is NULL");
+  ress::DenseArgs a;
+  int e = attn_checks(args, pages, false, ws, ws_bytes, &a);
+  if (e) return e;
+  if (a.rows == 0 || a.n_seqs == 0) return ok();
+  cudaError_t ce = ress::launch_flash(a, static_cast<cudaStream_t>(stream));
+  if (ce != cudaSuccess) return cuda_fail(ce, "ress_paged_attn");
+  return ok();
+}
+
+int ress_cache_tables(const ress_tables* t, void* ws, size_t ws_bytes, void* stream) {
+  if (!t) return fail(RESS_EINVAL, "tables is NULL");
+  int e;
+  if (t->n_seqs < 0 || t->n_seqs > RESS_MAX_SEQS)
+    return fail(RESS_EUNSUPPORTED, "n_seqs %d outside 0..%d", t->n_seqs, RESS_MAX_SEQS);
+  if (t->page < 1 || t->page > INT32_MAX / 2) return fail(RESS_EINVAL, "page %d out of range", t->page);
+  if (t->table_cols < 0 || (t->n_seqs > 1 && (t->table_stride < t->table_cols || t->table_stride > INT32_MAX)) ||
+      t->n_free < 0 || t->n_free > INT32_MAX || t->n_slots < 0 || t->n_slots > INT32_MAX)
+    return fail(RESS_EINVAL, "table of %d columns, %lld apart, %lld free pages, %lld slots: out of range", t->table_cols,
+                (long long)t->table_stride, (long long)t->n_free, (long long)t->n_slots);
+  const struct { const int32_t* p; bool needed; const char* name; } ins[] = {
+      {t->have, t->n_seqs > 0, "have"}, {t->add, t->n_seqs > 0, "add"}, {t->free, t->n_free > 0, "free"}, {t->taken, true, "taken"}},
+      outs[] = {{t->table, t->n_seqs > 0 && t->table_cols > 0, "table"}, {t->lens, t->n_seqs > 0, "lens"},
+                {t->q_start, true, "q_start"}, {t->slots, t->n_slots > 0, "slots"}, {t->pos, t->n_slots > 0, "pos"},
+                {t->taken_out, true, "taken_out"}};
+  for (const auto& i : ins)
+    if (i.needed && (e = check_ptr(i.p, 4, i.name))) return e;
+  for (const auto& o : outs) {
+    if (o.needed && (e = check_ptr(o.p, 4, o.name))) return e;
+    for (const auto& i : ins)
+      if (o.needed && i.needed && o.p == i.p) return fail(RESS_EINVAL, "%s must not be %s", o.name, i.name);
+  }
+  if ((e = check_scratch(ws, ws_bytes, 256))) return e;
+  ress::CacheTablesArgs a{t->n_seqs, t->page, t->table_cols, t->n_free, t->n_slots, t->table_stride, t->have, t->add,
+                          t->free, t->taken, t->table, t->lens, t->q_start, t->slots, t->pos, t->taken_out,
+                          static_cast<uint32_t*>(ws)};
+  cudaError_t ce = ress::launch_cache_tables(a, static_cast<cudaStream_t>(stream));
+  if (ce != cudaSuccess) return cuda_fail(ce, "ress_cache_tables");
+  return ok();
+}
+
+int ress_cache_write(int64_t tokens, int32_t kv_heads, const ress_heads* k, const ress_heads* v, const int32_t* slots,
+                     const ress_heads* kc, const ress_heads* vc, int64_t k_page_stride, int64_t v_page_stride,
+                     int32_t page, int64_t n_pages, void* ws, size_t ws_bytes, void* stream) {
+  int e;
+  if (!k || !v || !kc || !vc) return fail(RESS_EINVAL, "k, v, kc or vc is NULL");
+  if (tokens < 0 || tokens > INT32_MAX) return fail(RESS_EINVAL, "tokens %lld outside 0..2^31-1", (long long)tokens);
+  if (kv_heads < 1 || kv_heads > RESS_ROPE_MAX_HEADS)
+    return fail(RESS_EUNSUPPORTED, "kv_heads %d outside 1..%d", kv_heads, RESS_ROPE_MAX_HEADS);
+  if (page < 1 || n_pages < 0 || n_pages > INT32_MAX / page)
+    return fail(RESS_EINVAL, "%lld pages of %d outside 0..2^31-1 rows", (long long)n_pages, page);
+  if ((e = check_scratch(ws, ws_bytes, 256))) return e;
+  if (tokens == 0) return ok();
+  if ((e = check_ptr(slots, 4, "slots")) || (e = check_tiles(*k, tokens, kv_heads, false, "k")) ||
+      (e = check_tiles(*v, tokens, kv_heads, false, "v")) || (e = check_tiles(*kc, page, kv_heads, true, "kc")) ||
+      (e = check_tiles(*vc, page, kv_heads, true, "vc")))
+    return e;
+  for (int64_t s : {k_page_stride, v_page_stride})
+    if (n_pages > 1 && (s < 64 || s % 8 || s > INT64_MAX / 16 / n_pages))
+      return fail(RESS_EINVAL, "page stride %lld is not a multiple of 8 in range", (long long)s);
+  ress::CacheWriteArgs a{tokens, n_pages, kv_heads, page, *k, *v, *kc, *vc, k_page_stride, v_page_stride, slots,
+                         static_cast<uint32_t*>(ws)};
+  cudaError_t ce = ress::launch_cache_write(a, static_cast<cudaStream_t>(stream));
+  if (ce != cudaSuccess) return cuda_fail(ce, "ress_cache_write");
+  return ok();
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------------------
 // Allocation-free attention entry point.
 //
 // Some callers cannot allocate device memory when they call into this library: a host

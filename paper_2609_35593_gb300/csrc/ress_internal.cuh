@@ -324,4 +324,55 @@ struct QkvArgs {
 };
 cudaError_t launch_qkv_proj(const QkvArgs& a, cudaStream_t st);
 
+// Dense attention over packed or paged sequences, its gradient, and the cache (k_flash.cu, k_flash_bwd.cu,
+// k_cache.cu).  rows and keys are below 2^31.
+struct DenseArgs {
+  int type, n_seqs, kv_heads, group;  // group: heads of Q per head of K and V
+  int causal;
+  float cap;
+  int64_t rows, keys;
+  const int32_t *q_start, *k_start, *prefix;
+  const float* slopes;
+  // paged: K and V in pages
+  const int32_t *table, *lens;
+  int64_t table_stride, n_pages;
+  int table_cols, page;
+  ress_heads q, k, v, o, d_o, dq, dk, dv;
+  int64_t k_page_stride, v_page_stride;
+  float* lse;
+  uint32_t* status;
+  float* part;   // partial results of items that several CTAs share
+  float2* stat;  // gradient: per row of each head of K, log2 of its sum and o . do
+  float* big;    // gradient in f16: largest |do| of each of n_big parts of the rows
+  int n_big;
+};
+size_t dense_part_bytes();
+constexpr int kBigParts = 1024;
+cudaError_t launch_flash(const DenseArgs& a, cudaStream_t st);
+cudaError_t launch_flash_bwd(const DenseArgs& a, cudaStream_t st);
+// Tensor maps of the dense attention: heads of Q of one head of K, `tokens` tokens of them per box; and heads
+// of K or V, `box` tokens of a page per box (packed tensors are one page).
+bool make_row_map(void* map, const ress_heads& h, int type, int64_t rows, int kv_heads, int group, int tokens);
+bool make_key_map(void* map, const ress_heads& h, int type, int64_t keys, int64_t pages, int64_t page_stride,
+                  int kv_heads, int box);
+int dense_ctas();
+
+struct CacheTablesArgs {
+  int n_seqs, page, table_cols;
+  int64_t n_free, n_slots, table_stride;
+  const int32_t *have, *add, *free, *taken;
+  int32_t *table, *lens, *q_start, *slots, *pos, *taken_out;
+  uint32_t* status;
+};
+cudaError_t launch_cache_tables(const CacheTablesArgs& a, cudaStream_t st);
+struct CacheWriteArgs {
+  int64_t tokens, n_pages;
+  int kv_heads, page;
+  ress_heads k, v, kc, vc;
+  int64_t k_page_stride, v_page_stride;
+  const int32_t* slots;
+  uint32_t* status;
+};
+cudaError_t launch_cache_write(const CacheWriteArgs& a, cudaStream_t st);
+
 }  // namespace ress

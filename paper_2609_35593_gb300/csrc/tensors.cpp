@@ -8,6 +8,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <exception>
+#include <type_traits>
 
 #include "ress.h"
 
@@ -165,6 +166,139 @@ PyObject* code(PyObject* const* args, Py_ssize_t n) {
   return PyLong_FromLong(c < 0 ? 2 : c);
 }
 
+// [tokens, heads, 64] of a type, channels next to each other, on a device (pages: the rows of one more, outer
+// dimension, which is left to the caller).
+bool tiles_at(const at::Tensor* t, int dims, int code, const at::Tensor& like, ress_heads& h) {
+  if (!t || t->dim() != dims || t->size(dims - 1) != RESS_HEAD_DIM || t->stride(dims - 1) != 1 || code_of(*t) != code ||
+      t->device() != like.device())
+    return false;
+  h.data = t->data_ptr();
+  h.token_stride = t->stride(dims - 3);
+  h.head_stride = t->stride(dims - 2);
+  return true;
+}
+
+// Contiguous int32 (or float32) numbers on like's device; n < 0: any number, which it becomes (None: null).
+template <typename T>
+bool numbers_at(PyObject* o, long long& n, const at::Tensor& like, T*& p) {
+  p = nullptr;
+  if (o == Py_None) return true;
+  const at::Tensor* t = cuda_tensor(o);
+  if (!t || t->scalar_type() != (std::is_same<std::remove_const_t<T>, float>::value ? at::kFloat : at::kInt) ||
+      !t->is_contiguous() || t->device() != like.device() || (n >= 0 && t->numel() != n))
+    return false;
+  n = t->numel();
+  p = static_cast<T*>(t->data_ptr());
+  return true;
+}
+
+// attn_args(q, k, v, o, lse, q_start, k_start, prefix, slopes, causal, cap, paged): the bytes of a ress_attn_args.
+PyObject* attn_args(PyObject* const* args) {
+  long long v[1];
+  if (!integers(args + 9, v)) return nullptr;
+  const double cap = PyFloat_AsDouble(args[10]);
+  if (cap == -1.0 && PyErr_Occurred()) return nullptr;
+  const bool paged = args[11] == Py_True;
+  const int kd = paged ? 4 : 3;
+  const at::Tensor *q = cuda_tensor(args[0]), *k = cuda_tensor(args[1]), *w = cuda_tensor(args[2]), *o = cuda_tensor(args[3]);
+  ress_attn_args a = {};
+  if (!q || !k || !o || code_of(*q) > 1) return none();
+  a.type = code_of(*q);
+  if (!tiles_at(q, 3, a.type, *q, a.q) || !tiles_at(k, kd, a.type, *q, a.k) || !tiles_at(w, kd, a.type, *q, a.v) ||
+      !tiles_at(o, 3, a.type, *q, a.o) || o->sizes() != q->sizes() || w->sizes() != k->sizes())
+    return none();
+  a.rows = q->size(0), a.keys = paged ? 0 : k->size(0);
+  if (q->size(1) > INT32_MAX || k->size(kd - 2) > INT32_MAX) return none();
+  a.q_heads = static_cast<int32_t>(q->size(1)), a.kv_heads = static_cast<int32_t>(k->size(kd - 2));
+  long long n = -1, all = a.rows * a.q_heads, heads = a.q_heads;
+  if (!numbers_at(args[5], n, *q, a.q_start) || !numbers_at(args[6], n, *q, a.k_start) ||
+      (!paged && (args[5] == Py_None) != (args[6] == Py_None)) || n == 0 || n > INT32_MAX)
+    return none();
+  a.n_seqs = n < 0 ? 1 : static_cast<int32_t>(n - 1);
+  long long seqs = a.n_seqs;
+  if (!numbers_at(args[7], seqs, *q, a.prefix) || !numbers_at(args[8], heads, *q, a.slopes) ||
+      !numbers_at(args[4], all, *q, a.lse))
+    return none();
+  a.causal = v[0] != 0;
+  a.cap = static_cast<float>(cap);
+  return PyBytes_FromStringAndSize(reinterpret_cast<const char*>(&a), sizeof a);
+}
+
+// attn_grads(d_o, dq, dk, dv, q, k): the bytes of a ress_attn_grads.
+PyObject* attn_grads(PyObject* const* args) {
+  const at::Tensor *q = cuda_tensor(args[4]), *k = cuda_tensor(args[5]);
+  ress_attn_grads g = {};
+  ress_heads* to[4] = {&g.d_o, &g.dq, &g.dk, &g.dv};
+  if (!q || !k) return none();
+  for (int i = 0; i < 4; i++) {
+    const at::Tensor* t = cuda_tensor(args[i]);
+    if (!tiles_at(t, 3, code_of(*q), *q, *to[i]) || t->sizes() != (i < 2 ? q : k)->sizes()) return none();
+  }
+  return PyBytes_FromStringAndSize(reinterpret_cast<const char*>(&g), sizeof g);
+}
+
+// pages(k_pages, v_pages, table, lens, n_seqs): the bytes of a ress_pages.
+PyObject* pages(PyObject* const* args) {
+  long long v[1];
+  if (!integers(args + 4, v)) return nullptr;
+  const at::Tensor *k = cuda_tensor(args[0]), *w = cuda_tensor(args[1]), *t = cuda_tensor(args[2]);
+  ress_pages p = {};
+  if (!k || !w || k->dim() != 4 || w->dim() != 4 || !t || t->dim() != 2 || t->size(0) != v[0] || t->scalar_type() != at::kInt ||
+      (t->size(1) > 1 && t->stride(1) != 1) || t->device() != k->device() || t->size(1) > INT32_MAX || k->size(1) > INT32_MAX ||
+      args[3] == Py_None || !numbers_at(args[3], v[0], *k, p.lens))
+    return none();
+  p.table = static_cast<const int32_t*>(t->data_ptr());
+  p.table_stride = t->stride(0), p.table_cols = static_cast<int32_t>(t->size(1));
+  p.page = static_cast<int32_t>(k->size(1)), p.n_pages = k->size(0);
+  p.k_page_stride = k->stride(0), p.v_page_stride = w->stride(0);
+  return PyBytes_FromStringAndSize(reinterpret_cast<const char*>(&p), sizeof p);
+}
+
+// tables(have, add, free, taken, table, page, lens, q_start, slots, pos, taken_out): the bytes of a ress_tables.
+PyObject* tables(PyObject* const* args) {
+  long long v[1];
+  if (!integers(args + 5, v)) return nullptr;
+  const at::Tensor* t = cuda_tensor(args[4]);
+  ress_tables r = {};
+  if (!t || t->dim() != 2 || t->scalar_type() != at::kInt || (t->size(1) > 1 && t->stride(1) != 1) || t->size(0) > INT32_MAX ||
+      t->size(1) > INT32_MAX || v[0] < 1 || v[0] > INT32_MAX)
+    return none();
+  for (int i = 0; i < 11; i++)
+    if (i != 5 && args[i] == Py_None) return none();
+  long long seqs = t->size(0), starts = seqs + 1, one = 1, more = 1, any = -1, slots = -1;
+  if (!numbers_at(args[0], seqs, *t, r.have) || !numbers_at(args[1], seqs, *t, r.add) || !numbers_at(args[2], any, *t, r.free) ||
+      !numbers_at(args[3], one, *t, r.taken) || !numbers_at(args[6], seqs, *t, r.lens) ||
+      !numbers_at(args[7], starts, *t, r.q_start) || !numbers_at(args[8], slots, *t, r.slots) ||
+      !numbers_at(args[9], slots, *t, r.pos) || !numbers_at(args[10], more, *t, r.taken_out))
+    return none();
+  r.table = static_cast<int32_t*>(t->data_ptr());
+  r.n_seqs = static_cast<int32_t>(seqs), r.page = static_cast<int32_t>(v[0]);
+  r.table_cols = static_cast<int32_t>(t->size(1)), r.table_stride = t->stride(0);
+  r.n_free = any, r.n_slots = slots;
+  return PyBytes_FromStringAndSize(reinterpret_cast<const char*>(&r), sizeof r);
+}
+
+// cache_rows(k, v, slots, k_pages, v_pages): what ress_cache_write takes but the workspace, as a tuple with the bytes of
+// the four ress_heads.
+PyObject* cache_rows(PyObject* const* args) {
+  const at::Tensor *k = cuda_tensor(args[0]), *w = cuda_tensor(args[1]), *kp = cuda_tensor(args[3]), *vp = cuda_tensor(args[4]);
+  ress_heads h[4];
+  const int32_t* slots;
+  if (!k || !w || !kp || !vp || code_of(*k) > 1 || args[2] == Py_None) return none();
+  const int code = code_of(*k);
+  if (!tiles_at(k, 3, code, *k, h[0]) || !tiles_at(w, 3, code, *k, h[1]) || !tiles_at(kp, 4, code, *k, h[2]) ||
+      !tiles_at(vp, 4, code, *k, h[3]) || w->sizes() != k->sizes() || vp->sizes() != kp->sizes() || kp->size(2) != k->size(1) ||
+      k->size(1) > INT32_MAX || kp->size(1) > INT32_MAX)
+    return none();
+  long long tokens = k->size(0);
+  if (!numbers_at(args[2], tokens, *k, slots)) return none();
+  const auto bytes = [&](int i) { return PyBytes_FromStringAndSize(reinterpret_cast<const char*>(&h[i]), sizeof h[i]); };
+  return Py_BuildValue("LiNNNNNLLiL", tokens, static_cast<int>(k->size(1)), bytes(0), bytes(1),
+                       PyLong_FromVoidPtr(const_cast<int32_t*>(slots)), bytes(2), bytes(3),
+                       static_cast<long long>(kp->stride(0)), static_cast<long long>(vp->stride(0)),
+                       static_cast<int>(kp->size(1)), static_cast<long long>(kp->size(0)));
+}
+
 // Torch's C++ exceptions (a tensor without storage) end here.
 template <typename F>
 PyObject* guarded(F&& ask) {
@@ -196,6 +330,8 @@ PyMethodDef method(const char* name) {
 
 PyMethodDef methods[] = {method<vector, 3>("vector"), method<shape, 1>("shape"), method<rows, 2>("rows"),
                          method<rope_heads, 8>("rope_heads"), method<positions, 3>("positions"), method<scratch, 1>("scratch"),
+                         method<attn_args, 12>("attn_args"), method<attn_grads, 6>("attn_grads"), method<pages, 5>("pages"), method<tables, 11>("tables"),
+                         method<cache_rows, 5>("cache_rows"),
                          {"code", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry_code)), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 
