@@ -233,6 +233,21 @@ __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile in
   return ok != 0;
 }
 
+// Registers of this warp's group of four (all four warps come here): fewer, or more of those that others gave up.
+template <int N>
+__device__ __forceinline__ void regs_dec() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void regs_inc() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+
+// Whether the phase is complete now, for the whole warp.
+__device__ __forceinline__ bool mbar_ready(uint64_t* bar, uint32_t parity) {
+  return __all_sync(0xffffffffu, mbar_try_wait(bar, parity));
+}
+
 template <bool kF16>
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   uint32_t r;

@@ -5,14 +5,15 @@
 // floor(128 / group) tokens, each with its `group` heads of Q, make 128 rows, so that heads which share K read it
 // once and single tokens still fill rows.  The two halves ("slots") share the 64-key tiles that TMA brings
 // in, which halves what comes from L2: at the tensor cores' peak a tile of 16 KB per 128 rows would need 64 bytes
-// per cycle and SM.  Warp roles (320 threads):
-//   warp 0      item and tile producer: TMA of Q, K and V (128-byte swizzle), 10 stages of 16 KB, so that single
-//               tokens, which only stream the cache, keep 160 KB per SM in flight
-//   warp 1      TMEM owner and MMA issuer, per tile and slot: S = Q K^T (M128 N64 K64, Q copied to TMEM) and,
-//               one tile later, O += P V (P from TMEM, V MN-major); S is double-buffered
-//   warps 2-5, 6-9  one row of slot 0, 1 per thread: online softmax in the exp2 domain.  The reference maximum is only
+// per cycle and SM.  An item with rows for one slot only (single tokens, a sequence's end) gives its tiles to the
+// slots in turn, which join their sums on chip.  Warp roles (384 threads):
+//   warps 0-3, 4-7  one row of slot 0, 1 per thread: online softmax in the exp2 domain.  The reference maximum is only
 //               raised when a tile exceeds it by 2^8 (what P's 16 bits and O's 32 hold easily), so O in TMEM is
 //               rescaled seldom; sums are float32, of the exponentials before they are rounded to 16 bits.
+//   warp 8      item and tile producer: TMA of Q, K and V (128-byte swizzle), 9 stages of 16 KB, so that single
+//               tokens, which only stream the cache, keep 144 KB per SM in flight
+//   warps 9, 10 MMA issuers of slot 0, 1, per tile: S = Q K^T (M128 N64 K64, Q copied to TMEM) and, one tile later,
+//               O += P V (P from TMEM, V MN-major); S is double-buffered
 // Rows of V behind a sequence's last key are zeroed in shared memory (0 x NaN of a cache page never written
 // would be NaN); keys there and masked ones are -inf by selection, whatever their scores are.
 // Every mbarrier wait is bounded; one that gives up records RESS_ETIMEOUT and the CTA leaves, see k_attn.cu.
@@ -26,10 +27,12 @@ using namespace work;
 
 namespace {
 
-constexpr int kThreads = 320, kStages = 10, kSlots = 2, kItems = 4;
+constexpr int kThreads = 384, kStages = 9, kSlots = 2, kItems = 4;
+constexpr int kProducer = 8, kIssuer = 9;  // warps 0-7: softmax; issuers of slot 0, 1: 9, 10
 constexpr uint32_t kTileBytes = kTile * 128;
 constexpr uint32_t kColSlot = 256, kColO = 128, kColQ = 192;  // TMEM: per slot S x 2, O, Q
-constexpr int kFirst = 1, kTerm = 2, kHas = 4;
+// flags of a tile: the item's first; no more; Q of slot 0 for both; (per slot) it has the tile; its last of the item
+constexpr int kFirst = 1, kTerm = 2, kNarrow = 4, kHas = 8, kEnd = 32;
 constexpr float kLazy = 8.0f;  // log2 units
 // Lowest reference maximum: finite, so that rows that have seen no key yet give exponentials of 0.
 constexpr float kMinRef = -2147483648.0f;
@@ -37,10 +40,11 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int64_t kPartFloats = 256 * 66;  // a slot of partial results: 256 rows of 64, maxima, sums
 
 struct Item {
-  int q0, nq, nk, d, p;      // the sequence
-  int h, tok;                // head of K, first token (of the sequence)
+  int q0, nq, k0, nk, d, p, b;  // the sequence
+  int h, tok;                   // head of K (-1: no more items), first token of the sequence
   int t0, t1, g0;            // tiles; number of the first among all of the CTA's
   int n[kSlots];             // tiles of each slot's keys
+  int narrow;                // rows of slot 0 only: the slots take every other tile
   int part;                  // slot of partial results, or -1: whole
 };
 
@@ -49,11 +53,14 @@ struct __align__(1024) Smem {
   uint8_t K[kStages][kTileBytes];
   uint8_t V[kStages][kTileBytes];
   uint64_t kv_full[kStages], kv_empty[kStages];
-  uint64_t q_full, q_empty, drain;
+  float other[66][128];  // narrow items: slot 1's O, maxima and sums
+  uint64_t q_full, q_empty, drain[kSlots];
+  uint64_t other_full[4], other_empty[4];
   uint64_t s_full[kSlots][2], p_full[kSlots][2], o_full[kSlots][2];
   uint64_t it_full[kItems], it_empty[kItems];
   int64_t scratch[34];
-  Item item[kItems];
+  Item item[kItems], next;
+  Cursor cursor;
   int flags[kStages];
   uint32_t tmem_base;
   int abort;
@@ -104,12 +111,16 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
       mbar_init(&S.kv_full[s], 1);
-      mbar_init(&S.kv_empty[s], 1);
+      mbar_init(&S.kv_empty[s], kSlots);
     }
     mbar_init(&S.q_full, 1);
-    mbar_init(&S.q_empty, 1);
-    mbar_init(&S.drain, 1);
+    mbar_init(&S.q_empty, kSlots);
+    for (int q = 0; q < 4; ++q) {
+      mbar_init(&S.other_full[q], 1);
+      mbar_init(&S.other_empty[q], 1);
+    }
     for (int s = 0; s < kSlots; ++s) {
+      mbar_init(&S.drain[s], 1);
       for (int b = 0; b < 2; ++b) {
         mbar_init(&S.s_full[s][b], 1);
         mbar_init(&S.p_full[s][b], 4);
@@ -126,7 +137,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     prefetch_tensormap(&tmK);
     prefetch_tensormap(&tmV);
   }
-  if (warp == 1) tmem_alloc(&S.tmem_base, 512);
+  if (warp == kIssuer) tmem_alloc(&S.tmem_base, 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -135,210 +146,252 @@ __global__ void __launch_bounds__(kThreads, 1)
   auto line_of = [&](const Seq& s) { return row_line(a, s, kSlots * T, T); };
   const Range range = find_range(a, line_of, gridDim.x, blockIdx.x, S.scratch, blockIdx.x == 0 ? a.status : nullptr);
 
-  if (warp == 0) {
-    // =============================== producer ====================================
-    int g = 0, it = 0, pub = 0;
-    bool failed = false, q_loaded = false;
-    const int box = a.table ? min(kTile, a.page & -a.page) : kTile;  // the page's power of two
-    const int boxes = kTile / box;
-    auto publish = [&](const Item* item) -> bool {
-      const int i = pub % kItems, u = pub / kItems;
-      if (u > 0 && !wait(&S.it_empty[i], (u - 1) & 1, abort)) return false;
-      if (lane == 0) {
-        if (item)
-          S.item[i] = *item;
-        else
-          S.item[i].h = -1;
-        mbar_arrive(&S.it_full[i]);
-      }
-      __syncwarp();
-      ++pub;
-      return true;
-    };
-    if (range.x0 < range.x1) {
-      Cursor c;
-      seek(a, line_of, range.x0, range.b0, range.base, c);
-      do {
-        Item item;
-        item.q0 = c.s.q0, item.nq = c.s.nq, item.nk = c.s.nk, item.d = c.s.d, item.p = c.s.p;
-        item.h = c.h, item.tok = c.j * kSlots * T;
-        int n = 0;
-#pragma unroll
-        for (int s = 0; s < kSlots; ++s) n = max(n, item.n[s] = slot_tiles(a, c.s, item.tok, s, T));
-        tiles_of(c, range.x0, range.x1, n, item.t0, item.t1);
-        item.g0 = g;
-        item.part = item.t0 == 0 && item.t1 == n ? -1 : 2 * (int)blockIdx.x + (c.start >= range.x0 ? 1 : 0);
-        if (item.t0 == item.t1 && (n > 0 || c.start < range.x0)) continue;
-        if (!publish(&item)) {
-          failed = true;
-          break;
-        }
-        if (n == 0) continue;
-        if (it > 0 && !wait(&S.q_empty, (it - 1) & 1, abort)) {
-          failed = true;
-          break;
-        }
+  // 384 threads start with 168 registers each; the softmax warps, which hold a row's scores, get 208 of them
+  // (2 x 128 x 208 + 128 x 80 <= 384 x 168).  A spilled register would go to L2: shared memory leaves next to no L1.
+  if (warp >= kProducer) {
+    regs_dec<80>();
+    if (warp == kProducer) {
+      // =============================== producer ====================================
+      int g = 0, it = 0, pub = 0;
+      bool failed = false, q_loaded = false;
+      const int box = a.table ? min(kTile, a.page & -a.page) : kTile;  // the page's power of two
+      const int boxes = kTile / box;
+      // The next item that this share has tiles of, to S.next (h -1: none left).  One lane looks for it, in shared
+      // memory: the sequences' arithmetic in 64 bits would otherwise take the registers of the tile loop.
+      auto advance = [&](bool first) {
+        __syncwarp();
         if (lane == 0) {
-          const bool two = item.n[1] > item.t0, one = item.n[0] > item.t0;
-          mbar_arrive_expect_tx(&S.q_full, T * G * 128 * ((one ? 1 : 0) + (two ? 1 : 0)));
-          if (one) tma_load_4d(S.Q[0], &tmQ, &S.q_full, 0, 0, c.h, item.q0 + item.tok);
-          if (two) tma_load_4d(S.Q[1], &tmQ, &S.q_full, 0, 0, c.h, item.q0 + item.tok + T);
+          Cursor& c = S.cursor;
+          Item& item = S.next;
+          item.h = -1;
+          if (first) seek(a, line_of, range.x0, range.b0, range.base, c);
+          while (first || (next(a, line_of, c) && c.start < range.x1)) {
+            first = false;
+            const int tok = c.j * kSlots * T, n0 = slot_tiles(a, c.s, tok, 0, T), n1 = slot_tiles(a, c.s, tok, 1, T);
+            const int n = max(n0, n1);
+            int t0, t1;
+            tiles_of(c, range.x0, range.x1, n, t0, t1);
+            if (t0 == t1 && (n > 0 || c.start < range.x0)) continue;
+            item.q0 = c.s.q0, item.nq = c.s.nq, item.k0 = c.s.k0, item.nk = c.s.nk, item.d = c.s.d, item.p = c.s.p;
+            item.h = c.h, item.b = c.b, item.tok = tok;
+            item.t0 = t0, item.t1 = t1, item.n[0] = n0, item.n[1] = n1;
+            item.narrow = slot_tokens(c.s.nq, tok, 1, T) == 0;
+            item.part = t0 == 0 && t1 == n ? -1 : 2 * (int)blockIdx.x + (c.start >= range.x0 ? 1 : 0);
+            break;
+          }
         }
         __syncwarp();
-        q_loaded = true;
-        // where this lane's box of a tile is: lanes 0..boxes-1 load K, the next ones V
-        const bool mine = lane < 2 * boxes;
-        const int at = (lane < boxes ? lane : lane - boxes) * box;  // its first key in the tile
-        auto place = [&](int t, int& row, int& page) {
-          row = c.s.k0 + t * kTile + at, page = 0;
-          if (!a.table) return;
-          const int key = t * kTile + at;
-          row = key % a.page, page = (int)a.n_pages;  // no such page: TMA fills in zeros
-          if (mine && key < item.nk) {
-            const int id = a.table[c.b * a.table_stride + key / a.page];
-            if (id >= 0 && id < a.n_pages)
-              page = id;
-            else
-              flag_status(a.status, kStatusBadIndex);
-          }
-        };
-        int row, page;
-        place(item.t0, row, page);
-        for (int t = item.t0; t < item.t1; ++t) {
-          const int s = g % kStages, u = g / kStages;
-          int next_row = 0, next_page = 0;
-          if (t + 1 < item.t1) place(t + 1, next_row, next_page);
-          if (u > 0 && !wait(&S.kv_empty[s], (u - 1) & 1, abort)) {
+      };
+      auto publish = [&]() -> bool {
+        const int i = pub % kItems, u = pub / kItems;
+        if (u > 0 && !wait(&S.it_empty[i], (u - 1) & 1, abort)) return false;
+        if (lane == 0) {
+          S.next.g0 = g;
+          S.item[i] = S.next;
+          mbar_arrive(&S.it_full[i]);
+        }
+        __syncwarp();
+        ++pub;
+        return true;
+      };
+      if (range.x0 < range.x1) {
+        for (advance(true); S.next.h >= 0; advance(false)) {
+          if (!publish()) {
             failed = true;
             break;
           }
+          const Item& item = S.next;
+          if (item.t0 == item.t1) continue;  // rows without keys
+          if (it > 0 && !wait(&S.q_empty, (it - 1) & 1, abort)) {
+            failed = true;
+            break;
+          }
+          const int h = item.h, nk = item.nk, t0 = item.t0, t1 = item.t1, n0 = item.n[0], n1 = item.n[1], k0 = item.k0;
+          const bool narrow = item.narrow;
+          const int32_t* table = a.table ? a.table + item.b * a.table_stride : nullptr;
           if (lane == 0) {
-            S.flags[s] = (t == item.t0 ? kFirst : 0) | (t < item.n[0] ? kHas : 0) | (t < item.n[1] ? 2 * kHas : 0);
-            mbar_arrive_expect_tx(&S.kv_full[s], 2 * kTileBytes);
+            const bool two = !narrow && n1 > t0, one = n0 > t0;
+            mbar_arrive_expect_tx(&S.q_full, T * G * 128 * ((one ? 1 : 0) + (two ? 1 : 0)));
+            if (one) tma_load_4d(S.Q[0], &tmQ, &S.q_full, 0, 0, h, item.q0 + item.tok);
+            if (two) tma_load_4d(S.Q[1], &tmQ, &S.q_full, 0, 0, h, item.q0 + item.tok + T);
           }
           __syncwarp();
-          if (mine)
-            tma_load_4d((lane < boxes ? S.K[s] : S.V[s]) + at * 128, lane < boxes ? &tmK : &tmV, &S.kv_full[s], 0,
-                        c.h, row, page);
-          __syncwarp();
-          row = next_row, page = next_page;
-          ++g;
+          q_loaded = true;
+          // where this lane's box of a tile is: lanes 0..boxes-1 load K, the next ones V
+          const bool mine = lane < 2 * boxes;
+          const int at = (lane < boxes ? lane : lane - boxes) * box;  // its first key in the tile
+          auto place = [&](int t, int& row, int& page) {
+            const int key = t * kTile + at;
+            row = k0 + key, page = 0;
+            if (!table) return;
+            row = key % a.page, page = (int)a.n_pages;  // no such page: TMA fills in zeros
+            if (mine && key < nk) {
+              const int id = table[key / a.page];
+              if (id >= 0 && id < a.n_pages)
+                page = id;
+              else
+                flag_status(a.status, kStatusBadIndex);
+            }
+          };
+          int row, page;
+          place(t0, row, page);
+          for (int t = t0; t < t1; ++t) {
+            const int s = g % kStages, u = g / kStages;
+            int next_row = 0, next_page = 0;
+            if (t + 1 < t1) place(t + 1, next_row, next_page);
+            if (u > 0 && !wait(&S.kv_empty[s], (u - 1) & 1, abort)) {
+              failed = true;
+              break;
+            }
+            if (lane == 0) {
+              int flags = t == t0 ? kFirst : 0;
+              if (narrow) {
+                flags |= kNarrow | kHas << ((t - t0) & 1);
+                if (t + 2 >= t1) flags |= kEnd << ((t - t0) & 1);
+              } else {
+                flags |= (t < n0 ? kHas : 0) | (t + 1 == min(t1, n0) ? kEnd : 0);
+                flags |= (t < n1 ? 2 * kHas : 0) | (t + 1 == min(t1, n1) ? 2 * kEnd : 0);
+              }
+              S.flags[s] = flags;
+              mbar_arrive_expect_tx(&S.kv_full[s], 2 * kTileBytes);
+            }
+            __syncwarp();
+            if (mine)
+              tma_load_4d((lane < boxes ? S.K[s] : S.V[s]) + at * 128, lane < boxes ? &tmK : &tmV, &S.kv_full[s], 0, h, row,
+                          page);
+            __syncwarp();
+            row = next_row, page = next_page;
+            ++g;
+          }
+          if (failed) break;
+          ++it;
+          q_loaded = false;
         }
-        if (failed) break;
-        ++it;
-        q_loaded = false;
-      } while (next(a, line_of, c) && c.start < range.x1);
-    }
-    rows::stream_release();
-    if (!failed) {
-      const int s = g % kStages, u = g / kStages;
-      if (u > 0 && !wait(&S.kv_empty[s], (u - 1) & 1, abort)) {
-        failed = true;
-      } else if (lane == 0) {
-        S.flags[s] = kTerm;
-        mbar_arrive(&S.kv_full[s]);
       }
-      if (!failed && !publish(nullptr)) failed = true;
-    }
-    if (failed && lane == 0) {
-      give_up(S, a.status);
-      // let every copy already issued land before the CTA's shared memory goes away
-      volatile int no_abort = 0;
-      for (int back = 1; back <= kStages && g - back >= 0; ++back)
-        mbar_wait(&S.kv_full[(g - back) % kStages], ((g - back) / kStages) & 1, &no_abort, kDrainNs);
-      if (q_loaded) mbar_wait(&S.q_full, it & 1, &no_abort, kDrainNs);
-    }
-  } else if (warp == 1) {
-    // ================================ MMA issuer ===================================
-    const bool leader = elect_one();
-    bool failed = false;
-    constexpr uint32_t kQk = idesc16<kF16>(128, kTile, false), kPv = idesc16<kF16>(128, 64, true);
-    constexpr uint64_t kStageUnits = kTileBytes >> 4;
-    const uint64_t kd0 = sdesc_sw128(smem_u32(S.K[0])), vd0 = sdesc_sw128(smem_u32(S.V[0]));
-    int it = 0, ns[kSlots] = {0, 0}, np[kSlots] = {0, 0};  // S and P V of each slot so far
-    auto fetch = [&](int t, int& flags) -> bool {
-      if (!wait(&S.kv_full[t % kStages], (t / kStages) & 1, abort)) return false;
-      flags = S.flags[t % kStages];
-      return true;
-    };
-    auto issue_pv = [&](int t, int flags) -> bool {
-      const int st = t % kStages;
-      const uint64_t vd = vd0 + (uint64_t)st * kStageUnits;
-#pragma unroll
-      for (int s = 0; s < kSlots; ++s) {
-        if (!(flags & (kHas << s))) continue;
-        const int b = np[s] & 1;
-        if (!wait(&S.p_full[s][b], (np[s] >> 1) & 1, abort)) return false;
+      rows::stream_release();
+      if (!failed) {
+        const int s = g % kStages, u = g / kStages;
+        if (u > 0 && !wait(&S.kv_empty[s], (u - 1) & 1, abort)) {
+          failed = true;
+        } else if (lane == 0) {
+          S.flags[s] = kTerm;
+          mbar_arrive(&S.kv_full[s]);
+        }
+        __syncwarp();
+        if (lane == 0) S.next.h = -1;
+        if (!failed && !publish()) failed = true;
+      }
+      if (failed && lane == 0) {
+        give_up(S, a.status);
+        // let every copy already issued land before the CTA's shared memory goes away
+        volatile int no_abort = 0;
+        for (int back = 1; back <= kStages && g - back >= 0; ++back)
+          mbar_wait(&S.kv_full[(g - back) % kStages], ((g - back) / kStages) & 1, &no_abort, kDrainNs);
+        if (q_loaded) mbar_wait(&S.q_full, it & 1, &no_abort, kDrainNs);
+      }
+    } else if (warp < kProducer + 1 + kSlots) {
+      // ================================ MMA issuers ==================================
+      const int slot = warp - kIssuer;
+      const int has = kHas << slot, end = kEnd << slot;
+      const uint32_t tm = tmem + slot * kColSlot;
+      const bool leader = elect_one();
+      bool failed = false;
+      constexpr uint32_t kQk = idesc16<kF16>(128, kTile, false), kPv = idesc16<kF16>(128, 64, true);
+      constexpr uint64_t kStageUnits = kTileBytes >> 4;
+      const uint64_t kd0 = sdesc_sw128(smem_u32(S.K[0])), vd0 = sdesc_sw128(smem_u32(S.V[0]));
+      int it = 0, ns = 0, np = 0;     // items; S and P V so far
+      int held = -1, held_flags = 0;  // tile whose P V is to come
+      bool begins = false;            // the next P V is the slot's first of its item
+      auto fetch = [&](int t, int& flags) -> bool {
+        if (!wait(&S.kv_full[t % kStages], (t / kStages) & 1, abort)) return false;
+        flags = S.flags[t % kStages];
+        return true;
+      };
+      auto issue_pv = [&]() -> bool {
+        const int st = held % kStages, b = np & 1;
+        const uint64_t vd = vd0 + (uint64_t)st * kStageUnits;
+        if (!wait(&S.p_full[slot][b], (np >> 1) & 1, abort)) return false;
         tc_fence_after();
         if (leader) {
 #pragma unroll
           for (int k = 0; k < 4; ++k)
-            mma_bf16_ts(tmem + s * kColSlot + kColO, tmem + s * kColSlot + 64 * b + 8 * k, vd + 128 * k, kPv,
-                        (k > 0 || !(flags & kFirst)) ? 1u : 0u);
-          mma_commit(&S.o_full[s][b]);
+            mma_bf16_ts(tm + kColO, tm + 64 * b + 8 * k, vd + 128 * k, kPv, (k > 0 || !begins) ? 1u : 0u);
+          mma_commit(&S.o_full[slot][b]);
+          mma_commit(&S.kv_empty[st]);
         }
         __syncwarp();
-        ++np[s];
-      }
-      if (leader) mma_commit(&S.kv_empty[st]);
-      __syncwarp();
-      return true;
-    };
-    int flags = kTerm, prev = 0;
-    if (!fetch(0, flags)) failed = true;
-    for (int g = 0; !failed && !(flags & kTerm); ++g) {
-      if (flags & kFirst) {
-        if (!wait(&S.q_full, it & 1, abort)) {
+        begins = (held_flags & end) != 0;
+        ++np;
+        held = -1;
+        return true;
+      };
+      // Per tile: S, then P V of the tile before it.  The last P V of an item does not wait for a tile to come:
+      // the producer may be waiting for the softmax warps to end the item.
+      begins = true;
+      int flags = kTerm;
+      if (!fetch(0, flags)) failed = true;
+      for (int g = 0; !failed && !(flags & kTerm); ++g) {
+        const int st = g % kStages;
+        if (flags & kFirst) {
+          if (!wait(&S.q_full, it & 1, abort)) {
+            failed = true;
+            break;
+          }
+          tc_fence_after();
+          // every slot with tiles in the item copies its Q
+          if (leader) {
+            const uint32_t q = smem_u32(S.Q[flags & kNarrow ? 0 : slot]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) tmem_cp_128x256b(tm + kColQ + 8 * k, sdesc_sw128(q + 32 * k));
+            mma_commit(&S.q_empty);
+          }
+          __syncwarp();
+          ++it;
+        }
+        if (flags & has) {
+          const uint64_t kd = kd0 + (uint64_t)st * kStageUnits;
+          const int b = ns & 1;
+          if (leader) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              mma_bf16_ts(tm + 64 * b, tm + kColQ + 8 * k, kd + 2 * k, kQk, k > 0 ? 1u : 0u);
+            mma_commit(&S.s_full[slot][b]);
+          }
+          __syncwarp();
+          ++ns;
+          if (held >= 0 && !issue_pv()) {
+            failed = true;
+            break;
+          }
+          held = g, held_flags = flags;
+        } else if (lane == 0) {
+          mbar_arrive(&S.kv_empty[st]);
+        }
+        __syncwarp();
+        if (held >= 0 && (held_flags & end) && !mbar_ready(&S.kv_full[(g + 1) % kStages], ((g + 1) / kStages) & 1) &&
+            !issue_pv()) {
           failed = true;
           break;
         }
-        tc_fence_after();
-        if (leader) {
-#pragma unroll
-          for (int s = 0; s < kSlots; ++s)
-            if (flags & (kHas << s))
-#pragma unroll
-              for (int k = 0; k < 4; ++k)
-                tmem_cp_128x256b(tmem + s * kColSlot + kColQ + 8 * k, sdesc_sw128(smem_u32(S.Q[s]) + 32 * k));
-          mma_commit(&S.q_empty);
+        if (!fetch(g + 1, flags) || ((flags & kTerm) && held >= 0 && !issue_pv())) {
+          failed = true;
+          break;
         }
-        __syncwarp();
-        ++it;
       }
-      const uint64_t kd = kd0 + (uint64_t)(g % kStages) * kStageUnits;
-#pragma unroll
-      for (int s = 0; s < kSlots; ++s) {
-        if (!(flags & (kHas << s))) continue;
-        const int b = ns[s] & 1;
-        if (leader) {
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            mma_bf16_ts(tmem + s * kColSlot + 64 * b, tmem + s * kColSlot + kColQ + 8 * k, kd + 2 * k, kQk, k > 0 ? 1u : 0u);
-          mma_commit(&S.s_full[s][b]);
-        }
-        __syncwarp();
-        ++ns[s];
+      if (failed && lane == 0) give_up(S, a.status);
+      // wait for every MMA issued so far before TMEM is released
+      if (leader) {
+        mma_commit(&S.drain[slot]);
+        volatile int no_abort = 0;
+        mbar_wait(&S.drain[slot], 0, &no_abort, kDrainNs);
       }
-      const int cur = flags;
-      if (!fetch(g + 1, flags) || (g > 0 && !issue_pv(g - 1, prev)) || ((flags & kTerm) && !issue_pv(g, cur))) {
-        failed = true;
-        break;
-      }
-      prev = cur;
+      __syncwarp();
     }
-    if (failed && lane == 0) give_up(S, a.status);
-    // wait for every MMA issued so far before TMEM is released
-    if (leader) {
-      mma_commit(&S.drain);
-      volatile int no_abort = 0;
-      mbar_wait(&S.drain, 0, &no_abort, kDrainNs);
-    }
-    __syncwarp();
   } else {
+    regs_inc<208>();
     // ================================ softmax =====================================
-    const int slot = (warp - 2) >> 2, quarter = warp & 3;
+    const int slot = warp >> 2, quarter = warp & 3;
     const int r = quarter * 32 + lane;             // row within the slot
-    const int tid = (warp - 2 - 4 * slot) * 32 + lane;  // 0..127, for the zeroing of V
     const uint32_t tm = tmem + slot * kColSlot + ((uint32_t)(quarter * 32) << 16);
     const float kScale = kGen ? 1.0f : kLog2e * 0.125f;
     const float cap = a.cap, in = a.cap > 0.f ? 0.125f / a.cap : 0.125f * kLog2e, out = a.cap * kLog2e;
@@ -370,7 +423,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       m2[7] = m1[21];
       return fmax3(fmax3(m2[0], m2[1], m2[2]), fmax3(m2[3], m2[4], m2[5]), fmaxf(m2[6], m2[7]));
     };
-    int c = 0;  // tiles of this slot so far
+    int c = 0, joins = 0;  // tiles of this slot, and narrow items, so far
     bool stop = false;
     for (int pub = 0; !stop; ++pub) {
       const int i = pub % kItems;
@@ -378,13 +431,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         give_up(S, a.status);
         break;
       }
-      const Item item = S.item[i];
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&S.it_empty[i]);
+      const Item& item = S.item[i];
       if (item.h < 0) break;
-      const int ntok = slot_tokens(item.nq, item.tok, slot, T);
-      const int tiles = max(0, min(item.t1, item.n[slot]) - item.t0);
-      const int tok = item.tok + slot * T + r / G;  // of the sequence
+      const int part = item.narrow ? 0 : slot;  // which of the item's rows
+      const int ntok = slot_tokens(item.nq, item.tok, part, T);
+      const int step = item.narrow ? 2 : 1, from = item.narrow ? item.t0 + slot : item.t0;
+      const int tiles = max(0, min(item.t1, item.n[part]) - from + step - 1) / step;
+      const int tok = item.tok + part * T + r / G;  // of the sequence
       const bool exists = r / G < ntok;
       const int pos = item.d + tok;
       const int lim = !exists ? 0 : a.causal ? min(item.nk, max(item.p, pos + 1)) : item.nk;
@@ -396,7 +449,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (kGen && a.slopes && exists) slope = a.slopes[head] * kLog2e;
       float m = -INFINITY, l = 0.f;  // reference maximum (log2 units), sum of the exponentials against it
       for (int k = 0; k < tiles; ++k, ++c) {
-        const int b = c & 1, key = (item.t0 + k) * kTile;
+        const int b = c & 1, t = from + k * step, key = t * kTile;
         if (!wait(&S.s_full[slot][b], (c >> 1) & 1, abort)) {
           give_up(S, a.status);
           stop = true;
@@ -473,13 +526,13 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
         if (key + kTile > item.nk) {  // V's rows behind the last key
-          const int st = (item.g0 + k) % kStages;
-          if (!wait(&S.kv_full[st], ((item.g0 + k) / kStages) & 1, abort)) {
+          const int g = item.g0 + t - item.t0, st = g % kStages;
+          if (!wait(&S.kv_full[st], (g / kStages) & 1, abort)) {
             give_up(S, a.status);
             stop = true;
             break;
           }
-          zero_rows(S.V[st], item.nk - key, tid);
+          zero_rows(S.V[st], item.nk - key, r);
           fence_proxy_async_smem();
         }
         tc_fence_before();
@@ -503,30 +556,68 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int e = 0; e < 32; ++e) o[0][e] = o[1][e] = 0u;
       }
-      if (!exists) continue;
-      if (item.part >= 0) {
-        float* part = a.part + item.part * kPartFloats;
-        const int row = slot * 128 + r;
-        float4* dst = reinterpret_cast<float4*>(part + row * 64);
+      if (item.narrow) {  // slot 1 hands its half to slot 0
+        const uint32_t turn = joins++ & 1;
+        if (slot == 1) {
+          if (!wait(&S.other_empty[quarter], turn ^ 1, abort)) {
+            give_up(S, a.status);
+            break;
+          }
+          if (exists) {
+#pragma unroll
+            for (int e = 0; e < 64; ++e) S.other[e][r] = __uint_as_float(o[e >> 5][e & 31]);
+            S.other[64][r] = l == 0.f ? -INFINITY : m;
+            S.other[65][r] = l;
+          }
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(&S.other_full[quarter]);
+            mbar_arrive(&S.it_empty[i]);
+          }
+          continue;
+        }
+        if (!wait(&S.other_full[quarter], turn, abort)) {
+          give_up(S, a.status);
+          break;
+        }
+        if (exists && S.other[65][r] != 0.f) {
+          const float m1 = S.other[64][r], top = l == 0.f ? m1 : fmaxf(m, m1);
+          const float w0 = l == 0.f ? 0.f : ex2(m - top), w1 = ex2(m1 - top);
+          l = fmaf(l, w0, S.other[65][r] * w1);
+          m = top;
+#pragma unroll
+          for (int e = 0; e < 64; ++e)
+            o[e >> 5][e & 31] = __float_as_uint(fmaf(__uint_as_float(o[e >> 5][e & 31]), w0, S.other[e][r] * w1));
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&S.other_empty[quarter]);
+      }
+      if (!exists) {
+      } else if (item.part >= 0) {
+        float* parts = a.part + item.part * kPartFloats;
+        const int row = part * 128 + r;
+        float4* dst = reinterpret_cast<float4*>(parts + row * 64);
 #pragma unroll
         for (int e = 0; e < 16; ++e)
           dst[e] = make_float4(__uint_as_float(o[e >> 3][(4 * e) & 31]), __uint_as_float(o[e >> 3][(4 * e + 1) & 31]),
                                __uint_as_float(o[e >> 3][(4 * e + 2) & 31]), __uint_as_float(o[e >> 3][(4 * e + 3) & 31]));
-        part[256 * 64 + row] = l == 0.f ? -INFINITY : m;
-        part[256 * 65 + row] = l;
+        parts[256 * 64 + row] = l == 0.f ? -INFINITY : m;
+        parts[256 * 65 + row] = l;
       } else {
         const int64_t q = (int64_t)item.q0 + tok;
         store_row<kF16>(static_cast<uint16_t*>(a.o.data) + q * a.o.token_stride + head * a.o.head_stride, o,
                         l == 0.f ? 0.f : 1.0f / l);
         if (a.lse) a.lse[head * a.rows + q] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&S.it_empty[i]);
     }
   }
 
   __syncwarp();
   tc_fence_before();
   __syncthreads();
-  if (warp == 1) {
+  if (warp == kIssuer) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }

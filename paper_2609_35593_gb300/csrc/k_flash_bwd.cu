@@ -401,7 +401,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
       return true;
     };
-    int flags = kTerm, prev = 0;
+    // Per tile: S and dP, then the sums over the tile before it.  The last sums of an item do not wait for a tile
+    // to come: the producer may be waiting for the element-wise warps to end the item.
+    int flags = kTerm, held = -1, held_flags = 0;
     if (!fetch(0, flags)) failed = true;
     for (int g = 0; !failed && !(flags & kTerm); ++g) {
       if (flags & kFirst) {
@@ -433,12 +435,22 @@ __global__ void __launch_bounds__(kThreads, 1)
         mma_commit(&S.s_full[b]);
       }
       __syncwarp();
-      const int cur = flags;
-      if (!fetch(g + 1, flags) || (g > 0 && !issue_sums(g - 1, prev)) || ((flags & kTerm) && !issue_sums(g, cur))) {
+      if (held >= 0 && !issue_sums(held, held_flags)) {
         failed = true;
         break;
       }
-      prev = cur;
+      held = g, held_flags = flags;
+      if ((flags & kLast) && !mbar_ready(&S.kv_full[(g + 1) % kStages], ((g + 1) / kStages) & 1)) {
+        if (!issue_sums(held, held_flags)) {
+          failed = true;
+          break;
+        }
+        held = -1;
+      }
+      if (!fetch(g + 1, flags) || ((flags & kTerm) && held >= 0 && !issue_sums(held, held_flags))) {
+        failed = true;
+        break;
+      }
     }
     if (failed && lane == 0) give_up(S, a.status);
     // wait for every MMA issued so far before TMEM is released

@@ -133,6 +133,17 @@ def test_large_scores():
     check(q, k, v, [200], [1000], run(q, k, v, [200], [1000]))
 
 
+def test_many_sequences_without_keys():
+    """Between others: items without tiles end while the last tiles before them are worked on."""
+    lens = ([70, 300] + [3] * 3000 + [130], [70, 300] + [0] * 3000 + [130])
+    q, k, v = problem(*lens, 2, 2)
+    o, lse = run(q, k, v, *lens)
+    for a, b, n in ((0, 0, 70), (70, 70, 300), (9370, 370, 130)):
+        part = slice(b, b + n)
+        check(q[a:a + n], k[part], v[part], [n], [n], (o[a:a + n], lse[:, a:a + n]))
+    assert (o[370:9370] == 0).all() and (lse[:, 370:9370] == -math.inf).all()
+
+
 def test_same_bits_again():
     lens = ([300, 1000], [9000, 1000])
     q, k, v = problem(*lens, 4, 2)
