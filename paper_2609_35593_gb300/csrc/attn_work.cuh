@@ -78,8 +78,9 @@ struct Line {
   }
 };
 
-// Query rows as items of `per` tokens; one that fills less than half of its rows takes 5/8 of the time.
-__device__ __forceinline__ Line row_line(const DenseArgs& a, const Seq& s, int per, int half) {
+// Query rows as items of `per` tokens.  The last one's time per key: `eighths`(its tokens) / 8 of a full one's.
+template <class F>
+__device__ __forceinline__ Line row_line(const DenseArgs& a, const Seq& s, int per, F eighths) {
   Line l;
   l.n = (s.nq + per - 1) / per;
   l.cnt = l.n, l.a = s.nk, l.b = l.step = 0;
@@ -88,7 +89,7 @@ __device__ __forceinline__ Line row_line(const DenseArgs& a, const Seq& s, int p
     l.a = s.p, l.b = (int64_t)s.d + per, l.step = per;
   }
   l.last = s.nk;
-  l.last_mul = s.nq - (l.n - 1) * per > half ? 8 : 5;
+  l.last_mul = eighths(s.nq - (l.n - 1) * per);
   return l;
 }
 
@@ -258,6 +259,15 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   return r;
 }
 template <bool kF16>
+__device__ __forceinline__ float2 unpack2(uint32_t v) {
+  if (!kF16) return make_float2(bf16_lo(v), bf16_hi(v));
+  float2 r;
+  asm("{\n\t.reg .f16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, h;\n\t}"
+      : "=f"(r.x), "=f"(r.y)
+      : "r"(v));
+  return r;
+}
+template <bool kF16>
 __host__ __device__ constexpr uint32_t idesc16(int M, int N, bool b_mn_major) {
   return kF16 ? idesc_bf16_f32(M, N, b_mn_major) & ~((1u << 7) | (1u << 10)) : idesc_bf16_f32(M, N, b_mn_major);
 }
@@ -268,6 +278,15 @@ __device__ __forceinline__ void zero_rows(uint8_t* tile, int from, int i) {
     uint4* p = reinterpret_cast<uint4*>(tile + (i / 2) * 128 + (i & 1) * 64);
 #pragma unroll
     for (int k = 0; k < 4; ++k) p[k] = make_uint4(0u, 0u, 0u, 0u);
+  }
+}
+
+// The 128 bytes of row i.
+__device__ __forceinline__ void zero_row(uint8_t* tile, int from, int i) {
+  if (i >= from) {
+    uint4* p = reinterpret_cast<uint4*>(tile + i * 128);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) p[k] = make_uint4(0u, 0u, 0u, 0u);
   }
 }
 

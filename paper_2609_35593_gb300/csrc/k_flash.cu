@@ -1,19 +1,22 @@
 // Dense attention over packed sequences or a paged cache: O = softmax(s) V for the keys that each row sees,
 // with s = cap tanh(q.k / 8 / cap) - slope |distance|, and log sum exp(s) of each row.
 //
-// One CTA per SM walks its share of the work (attn_work.cuh).  An item is 2 x 128 rows of one head of K and V:
+// One CTA per SM walks its share of the work (attn_work.cuh).  An item is 4 x 128 rows of one head of K and V:
 // floor(128 / group) tokens, each with its `group` heads of Q, make 128 rows, so that heads which share K read it
-// once and single tokens still fill rows.  The two halves ("slots") share the 64-key tiles that TMA brings
-// in, which halves what comes from L2: at the tensor cores' peak a tile of 16 KB per 128 rows would need 64 bytes
-// per cycle and SM.  An item with rows for one slot only (single tokens, a sequence's end) gives its tiles to the
-// slots in turn, which join their sums on chip.  Warp roles (384 threads):
-//   warps 0-3, 4-7  one row of slot 0, 1 per thread: online softmax in the exp2 domain.  The reference maximum is only
-//               raised when a tile exceeds it by 2^8 (what P's 16 bits and O's 32 hold easily), so O in TMEM is
-//               rescaled seldom; sums are float32, of the exponentials before they are rounded to 16 bits.
-//   warp 8      item and tile producer: TMA of Q, K and V (128-byte swizzle), 9 stages of 16 KB, so that single
-//               tokens, which only stream the cache, keep 144 KB per SM in flight
-//   warps 9, 10 MMA issuers of slot 0, 1, per tile: S = Q K^T (M128 N64 K64, Q copied to TMEM) and, one tile later,
-//               O += P V (P from TMEM, V MN-major); S is double-buffered
+// once and single tokens still fill rows.  Its four parts ("slots") share the 64-key tiles that TMA brings in, a
+// quarter of what 128 rows at a time would take from L2.  An item with rows for one slot (single tokens) or two gives
+// its tiles to the slots in turn, which join their sums on chip.  Warp roles (640 threads):
+//   warps 0-15  one row of a slot per thread: online softmax in the exp2 domain.  The reference maximum is that of
+//               an item's first tile, and only raised where 64 exponentials against it add up to more than 2^13
+//               (what P's 16 bits and O's 32 hold easily): O in TMEM is rescaled seldom, and no maximum is formed
+//               otherwise.  Sums are float32, of the exponentials before they are rounded to 16 bits.
+//   warp 16     item and tile producer: TMA of Q, K and V (128-byte swizzle), 9 stages of 16 KB, so that single
+//               tokens, which only stream the cache, keep about 100 KB per SM in flight
+//   warps 17, 18  MMA issuers of two slots each, per tile and slot: O += P V of the tile before (M128 N64 K64, P from
+//               TMEM, V MN-major), then S = Q K^T (M128 N64 K64, both from shared memory) over P's columns
+// Four slots because the softmax warps' chain (scores from TMEM, exponentials, P to TMEM, hand-over) is latency:
+// with two, S double-buffered or in columns of its own, a sub-partition's two warps kept its SFU busy a third of the time
+// (8 images at once 636 and 618 us).
 // Rows of V behind a sequence's last key are zeroed in shared memory (0 x NaN of a cache page never written
 // would be NaN); keys there and masked ones are -inf by selection, whatever their scores are.
 // Every mbarrier wait is bounded; one that gives up records RESS_ETIMEOUT and the CTA leaves, see k_attn.cu.
@@ -27,24 +30,27 @@ using namespace work;
 
 namespace {
 
-constexpr int kThreads = 384, kStages = 9, kSlots = 2, kItems = 4;
-constexpr int kProducer = 8, kIssuer = 9;  // warps 0-7: softmax; issuers of slot 0, 1: 9, 10
+constexpr int kThreads = 640, kStages = 9, kSlots = 4, kItems = 4;
+constexpr int kProducer = 16, kIssuer = 17;  // warps 0-15: softmax; issuers of slots 0, 1 and 2, 3: 17, 18
 constexpr uint32_t kTileBytes = kTile * 128;
-constexpr uint32_t kColSlot = 256, kColO = 128, kColQ = 192;  // TMEM: per slot S x 2, O, Q
-// flags of a tile: the item's first; no more; Q of slot 0 for both; (per slot) it has the tile; its last of the item
-constexpr int kFirst = 1, kTerm = 2, kNarrow = 4, kHas = 8, kEnd = 32;
-constexpr float kLazy = 8.0f;  // log2 units
+constexpr uint32_t kColSlot = 128, kColO = 64;  // TMEM: per slot S (and P), O
+// flags of a tile: no more; (per slot) it has the tile; it is its first, its last of the item
+// tiles go to the slots in turn
+constexpr int kTerm = 1, kTurns = 1 << 16, kHas = 2, kBegin = kHas << kSlots, kEnd = kBegin << kSlots;
+constexpr float kMost = 8192.0f;  // sum of 64 exponentials above which the reference is raised
 // Lowest reference maximum: finite, so that rows that have seen no key yet give exponentials of 0.
 constexpr float kMinRef = -2147483648.0f;
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int64_t kPartFloats = 256 * 66;  // a slot of partial results: 256 rows of 64, maxima, sums
+constexpr int kRows = kSlots * 128;
+constexpr int64_t kPartFloats = kRows * 66;  // a slot of partial results: rows of 64, maxima, sums
 
 struct Item {
   int q0, nq, k0, nk, d, p, b;  // the sequence
   int h, tok;                   // head of K (-1: no more items), first token of the sequence
   int t0, t1, g0;            // tiles; number of the first among all of the CTA's
-  int n[kSlots];             // tiles of each slot's keys
-  int narrow;                // rows of slot 0 only: the slots take every other tile
+  int n[kSlots];             // tiles of each 128 rows' keys
+  int parts;                 // 128 rows that the item has, 1..4: slot s takes part s mod `parts` (3: slot 3 idles) and,
+  int ways;                  // of that, every `ways`th tile
   int part;                  // slot of partial results, or -1: whole
 };
 
@@ -53,10 +59,10 @@ struct __align__(1024) Smem {
   uint8_t K[kStages][kTileBytes];
   uint8_t V[kStages][kTileBytes];
   uint64_t kv_full[kStages], kv_empty[kStages];
-  float other[66][128];  // narrow items: slot 1's O, maxima and sums
-  uint64_t q_full, q_empty, drain[kSlots];
-  uint64_t other_full[4], other_empty[4];
-  uint64_t s_full[kSlots][2], p_full[kSlots][2], o_full[kSlots][2];
+  float other[kSlots][2][128];  // maxima and sums of slots that share rows
+  uint64_t other_full[kSlots][4], other_empty[kSlots][4];  // (and their quarters)
+  uint64_t q_full[kSlots], q_empty[kSlots], drain[2];
+  uint64_t s_full[kSlots], p_full[kSlots], o_full[kSlots];
   uint64_t it_full[kItems], it_empty[kItems];
   int64_t scratch[34];
   Item item[kItems], next;
@@ -72,28 +78,20 @@ __device__ __forceinline__ void give_up(Smem& S, uint32_t* status) {
   *reinterpret_cast<volatile int*>(&S.abort) = 1;
 }
 
-// Tokens of slot s of an item, and the tiles of the keys that any of them sees.
-__device__ __forceinline__ int slot_tokens(int nq, int tok, int s, int T) { return max(0, min(T, nq - tok - s * T)); }
-__device__ __forceinline__ int slot_tiles(const DenseArgs& a, const Seq& q, int tok, int s, int T) {
-  const int n = slot_tokens(q.nq, tok, s, T);
+// Tokens of 128 rows of an item, and the tiles of the keys that any of them sees.
+__device__ __forceinline__ int part_tokens(int nq, int tok, int s, int T) { return max(0, min(T, nq - tok - s * T)); }
+__device__ __forceinline__ int part_tiles(const DenseArgs& a, const Seq& q, int tok, int s, int T) {
+  const int n = part_tokens(q.nq, tok, s, T);
   if (n == 0) return 0;
   return (max(0, row_limit(a, q, q.d + tok + s * T + n - 1)) + kTile - 1) / kTile;
 }
-
-template <bool kF16>
-__device__ __forceinline__ void store_row(void* dst, const uint32_t (&o)[2][32], float by) {
-  uint4* p = static_cast<uint4*>(dst);
+__device__ __forceinline__ int item_tiles(const DenseArgs& a, const Seq& q, int tok, int T) {
+  int n = 0;
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    uint32_t w[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int c = 8 * k + 2 * e;
-      w[e] = pack2<kF16>(__uint_as_float(o[c >> 5][c & 31]) * by, __uint_as_float(o[c >> 5][(c & 31) + 1]) * by);
-    }
-    p[k] = make_uint4(w[0], w[1], w[2], w[3]);
-  }
+  for (int s = 0; s < kSlots; ++s) n = max(n, part_tiles(a, q, tok, s, T));
+  return n;
 }
+__device__ __forceinline__ int ways_of(int parts) { return parts == 1 ? 4 : parts == 2 ? 2 : 1; }
 
 }  // namespace
 
@@ -113,23 +111,21 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&S.kv_full[s], 1);
       mbar_init(&S.kv_empty[s], kSlots);
     }
-    mbar_init(&S.q_full, 1);
-    mbar_init(&S.q_empty, kSlots);
-    for (int q = 0; q < 4; ++q) {
-      mbar_init(&S.other_full[q], 1);
-      mbar_init(&S.other_empty[q], 1);
-    }
     for (int s = 0; s < kSlots; ++s) {
-      mbar_init(&S.drain[s], 1);
-      for (int b = 0; b < 2; ++b) {
-        mbar_init(&S.s_full[s][b], 1);
-        mbar_init(&S.p_full[s][b], 4);
-        mbar_init(&S.o_full[s][b], 1);
+      mbar_init(&S.q_full[s], 1);
+      mbar_init(&S.q_empty[s], 1);
+      mbar_init(&S.s_full[s], 1);
+      mbar_init(&S.p_full[s], 4);
+      mbar_init(&S.o_full[s], 1);
+      for (int q = 0; q < 4; ++q) {
+        mbar_init(&S.other_full[s][q], 1);
+        mbar_init(&S.other_empty[s][q], 1);
       }
     }
+    for (int p = 0; p < 2; ++p) mbar_init(&S.drain[p], 1);
     for (int i = 0; i < kItems; ++i) {
       mbar_init(&S.it_full[i], 1);
-      mbar_init(&S.it_empty[i], 8);
+      mbar_init(&S.it_empty[i], 4 * kSlots);
     }
     S.abort = 0;
     fence_barrier_init();
@@ -143,20 +139,21 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = S.tmem_base;
   rows::stream_acquire();
-  auto line_of = [&](const Seq& s) { return row_line(a, s, kSlots * T, T); };
+  auto line_of = [&](const Seq& s) { return row_line(a, s, kSlots * T, [&](int n) { return n > 3 * T ? 8 : n > 2 * T ? 6 : n > T ? 5 : 3; }); };
   const Range range = find_range(a, line_of, gridDim.x, blockIdx.x, S.scratch, blockIdx.x == 0 ? a.status : nullptr);
 
-  // 384 threads start with 168 registers each; the softmax warps, which hold a row's scores, get 208 of them
-  // (2 x 128 x 208 + 128 x 80 <= 384 x 168).  A spilled register would go to L2: shared memory leaves next to no L1.
+  // 640 threads start with 96 registers each; the softmax warps, which hold a row's scores, get 104 of them
+  // (512 x 104 + 128 x 64 <= 640 x 96).  A spilled register would go to L2: shared memory leaves next to no L1.
   if (warp >= kProducer) {
-    regs_dec<80>();
+    regs_dec<64>();
     if (warp == kProducer) {
       // =============================== producer ====================================
-      int g = 0, it = 0, pub = 0;
-      bool failed = false, q_loaded = false;
+      int g = 0, pub = 0;
+      uint32_t loads = 0;  // times that each slot's Q was loaded, a byte per slot
+      bool failed = false;
       const int box = a.table ? min(kTile, a.page & -a.page) : kTile;  // the page's power of two
       const int boxes = kTile / box;
-      // The next item that this share has tiles of, to S.next (h -1: none left).  One lane looks for it, in shared
+        // The next item that this share has tiles of, to S.next (h -1: none left).  One lane looks for it, in shared
       // memory: the sequences' arithmetic in 64 bits would otherwise take the registers of the tile loop.
       auto advance = [&](bool first) {
         __syncwarp();
@@ -167,15 +164,15 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (first) seek(a, line_of, range.x0, range.b0, range.base, c);
           while (first || (next(a, line_of, c) && c.start < range.x1)) {
             first = false;
-            const int tok = c.j * kSlots * T, n0 = slot_tiles(a, c.s, tok, 0, T), n1 = slot_tiles(a, c.s, tok, 1, T);
-            const int n = max(n0, n1);
+            const int tok = c.j * kSlots * T, n = item_tiles(a, c.s, tok, T);
             int t0, t1;
             tiles_of(c, range.x0, range.x1, n, t0, t1);
             if (t0 == t1 && (n > 0 || c.start < range.x0)) continue;
             item.q0 = c.s.q0, item.nq = c.s.nq, item.k0 = c.s.k0, item.nk = c.s.nk, item.d = c.s.d, item.p = c.s.p;
-            item.h = c.h, item.b = c.b, item.tok = tok;
-            item.t0 = t0, item.t1 = t1, item.n[0] = n0, item.n[1] = n1;
-            item.narrow = slot_tokens(c.s.nq, tok, 1, T) == 0;
+            item.h = c.h, item.b = c.b, item.tok = tok, item.t0 = t0, item.t1 = t1;
+            for (int s = 0; s < kSlots; ++s) item.n[s] = part_tiles(a, c.s, tok, s, T);
+            item.parts = min(kSlots, (c.s.nq - tok + T - 1) / T);
+            item.ways = ways_of(item.parts);
             item.part = t0 == 0 && t1 == n ? -1 : 2 * (int)blockIdx.x + (c.start >= range.x0 ? 1 : 0);
             break;
           }
@@ -195,28 +192,35 @@ __global__ void __launch_bounds__(kThreads, 1)
         return true;
       };
       if (range.x0 < range.x1) {
-        for (advance(true); S.next.h >= 0; advance(false)) {
+        for (advance(true); S.next.h >= 0 && !failed; advance(false)) {
           if (!publish()) {
             failed = true;
             break;
           }
           const Item& item = S.next;
           if (item.t0 == item.t1) continue;  // rows without keys
-          if (it > 0 && !wait(&S.q_empty, (it - 1) & 1, abort)) {
-            failed = true;
-            break;
-          }
-          const int h = item.h, nk = item.nk, t0 = item.t0, t1 = item.t1, n0 = item.n[0], n1 = item.n[1], k0 = item.k0;
-          const bool narrow = item.narrow;
+          const int h = item.h, nk = item.nk, t0 = item.t0, t1 = item.t1, k0 = item.k0;
           const int32_t* table = a.table ? a.table + item.b * a.table_stride : nullptr;
-          if (lane == 0) {
-            const bool two = !narrow && n1 > t0, one = n0 > t0;
-            mbar_arrive_expect_tx(&S.q_full, T * G * 128 * ((one ? 1 : 0) + (two ? 1 : 0)));
-            if (one) tma_load_4d(S.Q[0], &tmQ, &S.q_full, 0, 0, h, item.q0 + item.tok);
-            if (two) tma_load_4d(S.Q[1], &tmQ, &S.q_full, 0, 0, h, item.q0 + item.tok + T);
+          // lanes 0..3: what slot `lane` takes of the item
+          const int parts = item.parts, ways = item.ways, mine_part = lane % parts, way = lane / parts;
+          const int last = lane < kSlots && way < ways ? min(t1, item.n[mine_part]) : 0;
+          const uint32_t some = __ballot_sync(0xffffffffu, t0 + way < last);
+          for (int s = 0; s < kSlots; ++s) {
+            if (!(some >> s & 1)) continue;
+            const uint32_t times = loads >> (8 * s) & 0xff;
+            if (times > 0 && !wait(&S.q_empty[s], (times - 1) & 1, abort)) {
+              failed = true;
+              break;
+            }
+            if (lane == 0) {
+              mbar_arrive_expect_tx(&S.q_full[s], T * G * 128);
+              tma_load_4d(S.Q[s], &tmQ, &S.q_full[s], 0, 0, h, item.q0 + item.tok + s % parts * T);
+            }
+            __syncwarp();
+            // counts to 255 and goes on at 128 + (same parity)
+            loads = (loads & ~(0xffu << (8 * s))) | ((times == 255 ? 128 : times + 1) << (8 * s));
           }
-          __syncwarp();
-          q_loaded = true;
+          if (failed) break;
           // where this lane's box of a tile is: lanes 0..boxes-1 load K, the next ones V
           const bool mine = lane < 2 * boxes;
           const int at = (lane < boxes ? lane : lane - boxes) * box;  // its first key in the tile
@@ -239,33 +243,29 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int s = g % kStages, u = g / kStages;
             int next_row = 0, next_page = 0;
             if (t + 1 < t1) place(t + 1, next_row, next_page);
+            int flags = 0;
+            if (t < last && (t - t0) % ways == way) {
+              flags = kHas << lane | (ways > 1 ? kTurns : 0);
+              if (t == t0 + way) flags |= kBegin << lane;
+              if (t + ways >= last) flags |= kEnd << lane;
+            }
+            flags = __reduce_or_sync(0xffffffffu, flags);
             if (u > 0 && !wait(&S.kv_empty[s], (u - 1) & 1, abort)) {
               failed = true;
               break;
             }
             if (lane == 0) {
-              int flags = t == t0 ? kFirst : 0;
-              if (narrow) {
-                flags |= kNarrow | kHas << ((t - t0) & 1);
-                if (t + 2 >= t1) flags |= kEnd << ((t - t0) & 1);
-              } else {
-                flags |= (t < n0 ? kHas : 0) | (t + 1 == min(t1, n0) ? kEnd : 0);
-                flags |= (t < n1 ? 2 * kHas : 0) | (t + 1 == min(t1, n1) ? 2 * kEnd : 0);
-              }
               S.flags[s] = flags;
               mbar_arrive_expect_tx(&S.kv_full[s], 2 * kTileBytes);
             }
             __syncwarp();
             if (mine)
-              tma_load_4d((lane < boxes ? S.K[s] : S.V[s]) + at * 128, lane < boxes ? &tmK : &tmV, &S.kv_full[s], 0, h, row,
-                          page);
+              tma_load_4d((lane < boxes ? S.K[s] : S.V[s]) + at * 128, lane < boxes ? &tmK : &tmV, &S.kv_full[s], 0, h,
+                          row, page);
             __syncwarp();
             row = next_row, page = next_page;
             ++g;
           }
-          if (failed) break;
-          ++it;
-          q_loaded = false;
         }
       }
       rows::stream_release();
@@ -287,143 +287,107 @@ __global__ void __launch_bounds__(kThreads, 1)
         volatile int no_abort = 0;
         for (int back = 1; back <= kStages && g - back >= 0; ++back)
           mbar_wait(&S.kv_full[(g - back) % kStages], ((g - back) / kStages) & 1, &no_abort, kDrainNs);
-        if (q_loaded) mbar_wait(&S.q_full, it & 1, &no_abort, kDrainNs);
+        for (int s = 0; s < kSlots; ++s)
+          if (loads >> (8 * s) & 0xff) mbar_wait(&S.q_full[s], ((loads >> (8 * s) & 0xff) - 1) & 1, &no_abort, kDrainNs);
       }
-    } else if (warp < kProducer + 1 + kSlots) {
+    } else if (warp < kIssuer + 2) {
       // ================================ MMA issuers ==================================
-      const int slot = warp - kIssuer;
-      const int has = kHas << slot, end = kEnd << slot;
-      const uint32_t tm = tmem + slot * kColSlot;
+      const int pair = warp - kIssuer;
       const bool leader = elect_one();
       bool failed = false;
       constexpr uint32_t kQk = idesc16<kF16>(128, kTile, false), kPv = idesc16<kF16>(128, 64, true);
-      constexpr uint64_t kStageUnits = kTileBytes >> 4;
+      constexpr uint64_t kStageUnits = kTileBytes >> 4, kQUnits = (128 * 128) >> 4;
       const uint64_t kd0 = sdesc_sw128(smem_u32(S.K[0])), vd0 = sdesc_sw128(smem_u32(S.V[0]));
-      int it = 0, ns = 0, np = 0;     // items; S and P V so far
-      int held = -1, held_flags = 0;  // tile whose P V is to come
-      bool begins = false;            // the next P V is the slot's first of its item
-      auto fetch = [&](int t, int& flags) -> bool {
-        if (!wait(&S.kv_full[t % kStages], (t / kStages) & 1, abort)) return false;
-        flags = S.flags[t % kStages];
-        return true;
-      };
-      auto issue_pv = [&]() -> bool {
-        const int st = held % kStages, b = np & 1;
-        const uint64_t vd = vd0 + (uint64_t)st * kStageUnits;
-        if (!wait(&S.p_full[slot][b], (np >> 1) & 1, abort)) return false;
+      const uint64_t qd0 = sdesc_sw128(smem_u32(S.Q[2 * pair]));
+      int st = 0;
+      uint32_t phase = 0;
+      // of each of the two slots: tiles' P and items' Q so far (parity); stage of the tile whose P V is to come (or -1);
+      // whether that is its item's last, its item's first
+      uint32_t p_phase[2] = {0, 0}, q_phase[2] = {0, 0};
+      int held[2] = {-1, -1};
+      bool ends[2] = {false, false}, begins[2] = {false, false};
+      auto issue_pv = [&](int j) -> bool {
+        const int slot = 2 * pair + j;
+        if (!wait(&S.p_full[slot], p_phase[j], abort)) return false;
         tc_fence_after();
         if (leader) {
+          const uint32_t tm = tmem + slot * kColSlot;
+          const uint64_t vd = vd0 + (uint64_t)held[j] * kStageUnits;
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            mma_bf16_ts(tm + kColO, tm + 64 * b + 8 * k, vd + 128 * k, kPv, (k > 0 || !begins) ? 1u : 0u);
-          mma_commit(&S.o_full[slot][b]);
-          mma_commit(&S.kv_empty[st]);
+          for (int k = 0; k < 4; ++k) mma_bf16_ts(tm + kColO, tm + 8 * k, vd + 128 * k, kPv, (k > 0 || !begins[j]) ? 1u : 0u);
+          mma_commit(&S.kv_empty[held[j]]);
+          if (ends[j]) mma_commit(&S.o_full[slot]);
         }
         __syncwarp();
-        begins = (held_flags & end) != 0;
-        ++np;
-        held = -1;
+        p_phase[j] ^= 1;
+        held[j] = -1;
         return true;
       };
-      // Per tile: S, then P V of the tile before it.  The last P V of an item does not wait for a tile to come:
-      // the producer may be waiting for the softmax warps to end the item.
-      begins = true;
-      int flags = kTerm;
-      if (!fetch(0, flags)) failed = true;
-      for (int g = 0; !failed && !(flags & kTerm); ++g) {
-        const int st = g % kStages;
-        if (flags & kFirst) {
-          if (!wait(&S.q_full, it & 1, abort)) {
-            failed = true;
-            break;
-          }
-          tc_fence_after();
-          // every slot with tiles in the item copies its Q
-          if (leader) {
-            const uint32_t q = smem_u32(S.Q[flags & kNarrow ? 0 : slot]);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) tmem_cp_128x256b(tm + kColQ + 8 * k, sdesc_sw128(q + 32 * k));
-            mma_commit(&S.q_empty);
-          }
-          __syncwarp();
-          ++it;
-        }
-        if (flags & has) {
-          const uint64_t kd = kd0 + (uint64_t)st * kStageUnits;
-          const int b = ns & 1;
-          if (leader) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              mma_bf16_ts(tm + 64 * b, tm + kColQ + 8 * k, kd + 2 * k, kQk, k > 0 ? 1u : 0u);
-            mma_commit(&S.s_full[slot][b]);
-          }
-          __syncwarp();
-          ++ns;
-          if (held >= 0 && !issue_pv()) {
-            failed = true;
-            break;
-          }
-          held = g, held_flags = flags;
-        } else if (lane == 0) {
-          mbar_arrive(&S.kv_empty[st]);
-        }
-        __syncwarp();
-        if (held >= 0 && (held_flags & end) && !mbar_ready(&S.kv_full[(g + 1) % kStages], ((g + 1) / kStages) & 1) &&
-            !issue_pv()) {
+      // Per tile and slot: P V of the slot's tile before, then S.  The last P V of an item does not wait for a tile to
+      // come: the producer may be waiting for the softmax warps to end the item.
+      while (!failed) {
+        if (!wait(&S.kv_full[st], phase, abort)) {
           failed = true;
           break;
         }
-        if (!fetch(g + 1, flags) || ((flags & kTerm) && held >= 0 && !issue_pv())) {
-          failed = true;
-          break;
+        const int flags = S.flags[st];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int slot = 2 * pair + j;
+          const bool has = flags >> slot & kHas;
+          if (failed) continue;
+          if (has && (flags >> slot & kBegin)) {
+            if (!wait(&S.q_full[slot], q_phase[j], abort)) failed = true;
+            q_phase[j] ^= 1;
+          }
+          if (!failed && held[j] >= 0 && (has || ends[j] || (flags & kTerm) ||
+                                           ((flags & kTurns) && mbar_ready(&S.p_full[slot], p_phase[j]))) &&
+              !issue_pv(j))
+            failed = true;
+          if (failed || (flags & kTerm)) continue;
+          if (has) {
+            tc_fence_after();
+            if (leader) {
+              const uint64_t kd = kd0 + (uint64_t)st * kStageUnits, qd = qd0 + j * kQUnits;
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                mma_bf16_ss(tmem + slot * kColSlot, qd + 2 * k, kd + 2 * k, kQk, k > 0 ? 1u : 0u);
+              mma_commit(&S.s_full[slot]);
+              if (flags >> slot & kEnd) mma_commit(&S.q_empty[slot]);
+            }
+            held[j] = st, ends[j] = flags >> slot & kEnd, begins[j] = flags >> slot & kBegin;
+          } else if (lane == 0) {
+            mbar_arrive(&S.kv_empty[st]);
+          }
+          __syncwarp();
+        }
+        if (flags & kTerm) break;
+        if (++st == kStages) st = 0, phase ^= 1;
+        if (!failed && ((held[0] >= 0 && ends[0]) || (held[1] >= 0 && ends[1])) && !mbar_ready(&S.kv_full[st], phase)) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+            if (!failed && held[j] >= 0 && ends[j] && !issue_pv(j)) failed = true;
         }
       }
       if (failed && lane == 0) give_up(S, a.status);
       // wait for every MMA issued so far before TMEM is released
       if (leader) {
-        mma_commit(&S.drain[slot]);
+        mma_commit(&S.drain[pair]);
         volatile int no_abort = 0;
-        mbar_wait(&S.drain[slot], 0, &no_abort, kDrainNs);
+        mbar_wait(&S.drain[pair], 0, &no_abort, kDrainNs);
       }
       __syncwarp();
     }
   } else {
-    regs_inc<208>();
+    regs_inc<104>();
     // ================================ softmax =====================================
     const int slot = warp >> 2, quarter = warp & 3;
     const int r = quarter * 32 + lane;             // row within the slot
     const uint32_t tm = tmem + slot * kColSlot + ((uint32_t)(quarter * 32) << 16);
     const float kScale = kGen ? 1.0f : kLog2e * 0.125f;
     const float cap = a.cap, in = a.cap > 0.f ? 0.125f / a.cap : 0.125f * kLog2e, out = a.cap * kLog2e;
-    // p = 2^(x kScale - m) of this row's 64 columns, packed; returns their sum
-    auto exps = [&](const float (&x)[64], float m, uint32_t (&w)[32]) -> float {
-      const float nm = -m;
-      float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
-#pragma unroll
-      for (int e = 0; e < 32; ++e) {
-        float t0, t1;
-        fma2(t0, t1, x[2 * e], x[2 * e + 1], kScale, kScale, nm, nm);
-        t0 = ex2(t0), t1 = ex2(t1);
-        w[e] = pack2<kF16>(t0, t1);
-        if (e & 1)
-          add2(s2, s3, s2, s3, t0, t1);
-        else
-          add2(s0, s1, s0, s1, t0, t1);
-      }
-      return (s0 + s2) + (s1 + s3);
-    };
-    auto row_max = [&](const float (&x)[64]) -> float {
-      float m1[22];
-#pragma unroll
-      for (int k = 0; k < 21; ++k) m1[k] = fmax3(x[3 * k], x[3 * k + 1], x[3 * k + 2]);
-      m1[21] = x[63];
-      float m2[8];
-#pragma unroll
-      for (int k = 0; k < 7; ++k) m2[k] = fmax3(m1[3 * k], m1[3 * k + 1], m1[3 * k + 2]);
-      m2[7] = m1[21];
-      return fmax3(fmax3(m2[0], m2[1], m2[2]), fmax3(m2[3], m2[4], m2[5]), fmaxf(m2[6], m2[7]));
-    };
-    int c = 0, joins = 0;  // tiles of this slot, and narrow items, so far
+    uint32_t c = 0, ended = 0;        // tiles of this slot, and items with any, so far
+    uint32_t turn1 = 0, turn23 = 0;   // items in which slot 1, slots 2 and 3 help another one, so far
     bool stop = false;
     for (int pub = 0; !stop; ++pub) {
       const int i = pub % kItems;
@@ -433,10 +397,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       const Item& item = S.item[i];
       if (item.h < 0) break;
-      const int part = item.narrow ? 0 : slot;  // which of the item's rows
-      const int ntok = slot_tokens(item.nq, item.tok, part, T);
-      const int step = item.narrow ? 2 : 1, from = item.narrow ? item.t0 + slot : item.t0;
-      const int tiles = max(0, min(item.t1, item.n[part]) - from + step - 1) / step;
+      const int parts = item.parts, ways = item.ways, part = slot % parts, way = slot / parts;
+      const int ntok = way < ways ? part_tokens(item.nq, item.tok, part, T) : 0;
+      const int from = item.t0 + way, tiles = way < ways ? max(0, min(item.t1, item.n[part]) - from + ways - 1) / ways : 0;
       const int tok = item.tok + part * T + r / G;  // of the sequence
       const bool exists = r / G < ntok;
       const int pos = item.d + tok;
@@ -449,72 +412,78 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (kGen && a.slopes && exists) slope = a.slopes[head] * kLog2e;
       float m = -INFINITY, l = 0.f;  // reference maximum (log2 units), sum of the exponentials against it
       for (int k = 0; k < tiles; ++k, ++c) {
-        const int b = c & 1, t = from + k * step, key = t * kTile;
-        if (!wait(&S.s_full[slot][b], (c >> 1) & 1, abort)) {
+        const int t = from + k * ways, key = t * kTile;
+        if (!wait(&S.s_full[slot], c & 1, abort)) {
           give_up(S, a.status);
           stop = true;
           break;
         }
         tc_fence_after();
         if (any) {  // rows of a warp without any are garbage that nothing reads
-          const uint32_t tS = tm + 64 * b;
-          float x[64];
-          {
-            uint32_t v[64];
-            RESS_TMEM_LD64(tS, v);
-#pragma unroll
-            for (int e = 0; e < 64; ++e) x[e] = __uint_as_float(v[e]);
-          }
-          if (kGen) {
-            if (cap > 0.f) {
-#pragma unroll
-              for (int e = 0; e < 64; ++e) x[e] = out * tanh_of(x[e] * in);
-            } else {
-#pragma unroll
-              for (int e = 0; e < 64; ++e) x[e] *= in;
-            }
-            if (a.slopes) {
-              const float dist = (float)(pos - key);
-#pragma unroll
-              for (int e = 0; e < 64; ++e) x[e] = fmaf(-slope, fabsf(dist - (float)e), x[e]);
-            }
-          }
-          if (key + kTile > least) {
-#pragma unroll
-            for (int e = 0; e < 64; ++e) x[e] = key + e < lim ? x[e] : -INFINITY;
-          }
+          float alpha = 1.f, sum;
           uint32_t w[32];
-          float alpha = 1.f;
-          bool rescale = false;
-          if (k == 0) {
-            m = fmaxf(row_max(x) * kScale, kMinRef);
-            l = exps(x, m, w);
-          } else {
-            // against the reference so far, while the tile's maximum is formed; redone in the rare case that
-            // this grew too far past it
-            float sum = exps(x, m, w);
-            const float mt = row_max(x) * kScale;
-            const bool grow = mt > m + kLazy;
-            if (__any_sync(0xffffffffu, grow)) {
-              if (grow) {
-                alpha = ex2(m - mt);
-                m = mt;
-                rescale = true;
+          // Against the reference so far: a sum below kMost says that no exponential is above it, so the maximum is
+          // looked for only in an item's first tile and where that fails.
+          bool looked = k == 0;
+#pragma unroll 1
+          for (;;) {
+            float x[64];
+            {
+              uint32_t v[64];
+              RESS_TMEM_LD64(tm, v);
+#pragma unroll
+              for (int e = 0; e < 64; ++e) x[e] = __uint_as_float(v[e]);
+            }
+            if (kGen) {
+              if (cap > 0.f) {
+#pragma unroll
+                for (int e = 0; e < 64; ++e) x[e] = out * tanh_of(x[e] * in);
+              } else {
+#pragma unroll
+                for (int e = 0; e < 64; ++e) x[e] *= in;
               }
-              __syncwarp();
-              sum = exps(x, m, w);
+              if (a.slopes) {
+                const float dist = (float)(pos - key);
+#pragma unroll
+                for (int e = 0; e < 64; ++e) x[e] = fmaf(-slope, fabsf(dist - (float)e), x[e]);
+              }
             }
-            l = fmaf(l, alpha, sum);
+            if (key + kTile > least) {
+#pragma unroll
+              for (int e = 0; e < 64; ++e) x[e] = key + e < lim ? x[e] : -INFINITY;
+            }
+            if (looked) {
+              float top = x[0];
+#pragma unroll
+              for (int e = 1; e < 63; e += 2) top = fmax3(top, x[e], x[e + 1]);
+              top = fmaxf(top, x[63]) * kScale;
+              if (k == 0) {
+                m = fmaxf(top, kMinRef);
+              } else if (top > m) {
+                alpha = ex2(m - top);
+                m = top;
+              }
+            }
+            const float nm = -m;
+            float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              float t0, t1;
+              fma2(t0, t1, x[2 * e], x[2 * e + 1], kScale, kScale, nm, nm);
+              t0 = ex2(t0), t1 = ex2(t1);
+              w[e] = pack2<kF16>(t0, t1);
+              if (e & 1)
+                add2(s2, s3, s2, s3, t0, t1);
+              else
+                add2(s0, s1, s0, s1, t0, t1);
+            }
+            sum = (s0 + s2) + (s1 + s3);
+            if (looked || !__any_sync(0xffffffffu, sum > kMost)) break;
+            looked = true;
           }
-          RESS_TMEM_ST32(tS, w);
-          if (__any_sync(0xffffffffu, rescale)) {
-            // the P V before this one (the one before that is done: S of this tile was issued after it)
-            if (!wait(&S.o_full[slot][b ^ 1], ((c - 1) >> 1) & 1, abort)) {
-              give_up(S, a.status);
-              stop = true;
-              break;
-            }
-            tc_fence_after();
+          l = fmaf(l, alpha, sum);
+          RESS_TMEM_ST32(tm, w);
+          if (looked && k > 0) {  // the P V before this one is done: S of this tile was issued after it
 #pragma unroll
             for (int hc = 0; hc < 2; ++hc) {
               uint32_t v[32];
@@ -537,80 +506,123 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&S.p_full[slot][b]);
+        if (lane == 0) mbar_arrive(&S.p_full[slot]);
       }
       if (stop) break;
-      uint32_t o[2][32];
       if (tiles > 0) {
-        if (!wait(&S.o_full[slot][(c - 1) & 1], ((c - 1) >> 1) & 1, abort)) {
+        if (!wait(&S.o_full[slot], ended & 1, abort)) {
           give_up(S, a.status);
           break;
         }
+        ++ended;
         tc_fence_after();
-        if (any) {
-          RESS_TMEM_LD32(tm + kColO, o[0]);
-          RESS_TMEM_LD32(tm + kColO + 32, o[1]);
-        }
-        tc_fence_before();
-      } else {
-#pragma unroll
-        for (int e = 0; e < 32; ++e) o[0][e] = o[1][e] = 0u;
       }
-      if (item.narrow) {  // slot 1 hands its half to slot 0
-        const uint32_t turn = joins++ & 1;
-        if (slot == 1) {
-          if (!wait(&S.other_empty[quarter], turn ^ 1, abort)) {
+      // Slots with the same rows: the first of them adds the others' O, which it reads where they are, to its own:
+      // O = sum_s 2^(m_s - m) O_s.
+      const uint32_t turn = (slot == 1 ? turn1 : turn23) & 1;
+      if (way > 0 && way < ways) {
+        S.other[slot][0][r] = l == 0.f ? -INFINITY : m;
+        S.other[slot][1][r] = l;
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(&S.other_full[slot][quarter]);
+          mbar_arrive(&S.it_empty[i]);
+        }
+        if (!wait(&S.other_empty[slot][quarter], turn, abort)) {
+          give_up(S, a.status);
+          break;
+        }
+      } else {
+        float by[kSlots] = {1.f, 0.f, 0.f, 0.f};  // weights of this slot and the others
+        if (ways > 1) {
+          float ms[kSlots];
+          ms[0] = l == 0.f ? -INFINITY : m;
+#pragma unroll
+          for (int j = 1; j < kSlots; ++j) {
+            ms[j] = -INFINITY;
+            if (j < ways) {
+              const int s = slot + j * parts;
+              if (!wait(&S.other_full[s][quarter], (s == 1 ? turn1 : turn23) & 1, abort)) stop = true;
+              ms[j] = S.other[s][0][r];
+            }
+          }
+          if (stop) {
             give_up(S, a.status);
             break;
           }
-          if (exists) {
+          tc_fence_after();
+          const float top = fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3]));
+          by[0] = ms[0] == -INFINITY ? 0.f : ex2(ms[0] - top);
+          l *= by[0];
 #pragma unroll
-            for (int e = 0; e < 64; ++e) S.other[e][r] = __uint_as_float(o[e >> 5][e & 31]);
-            S.other[64][r] = l == 0.f ? -INFINITY : m;
-            S.other[65][r] = l;
-          }
-          __syncwarp();
-          if (lane == 0) {
-            mbar_arrive(&S.other_full[quarter]);
-            mbar_arrive(&S.it_empty[i]);
-          }
-          continue;
+          for (int j = 1; j < kSlots; ++j)
+            if (ms[j] != -INFINITY) {
+              by[j] = ex2(ms[j] - top);
+              l = fmaf(by[j], S.other[slot + j * parts][1][r], l);
+            }
+          if (top != -INFINITY) m = top;
         }
-        if (!wait(&S.other_full[quarter], turn, abort)) {
-          give_up(S, a.status);
-          break;
-        }
-        if (exists && S.other[65][r] != 0.f) {
-          const float m1 = S.other[64][r], top = l == 0.f ? m1 : fmaxf(m, m1);
-          const float w0 = l == 0.f ? 0.f : ex2(m - top), w1 = ex2(m1 - top);
-          l = fmaf(l, w0, S.other[65][r] * w1);
-          m = top;
-#pragma unroll
-          for (int e = 0; e < 64; ++e)
-            o[e >> 5][e & 31] = __float_as_uint(fmaf(__uint_as_float(o[e >> 5][e & 31]), w0, S.other[e][r] * w1));
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&S.other_empty[quarter]);
-      }
-      if (!exists) {
-      } else if (item.part >= 0) {
-        float* parts = a.part + item.part * kPartFloats;
-        const int row = part * 128 + r;
-        float4* dst = reinterpret_cast<float4*>(parts + row * 64);
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          dst[e] = make_float4(__uint_as_float(o[e >> 3][(4 * e) & 31]), __uint_as_float(o[e >> 3][(4 * e + 1) & 31]),
-                               __uint_as_float(o[e >> 3][(4 * e + 2) & 31]), __uint_as_float(o[e >> 3][(4 * e + 3) & 31]));
-        parts[256 * 64 + row] = l == 0.f ? -INFINITY : m;
-        parts[256 * 65 + row] = l;
-      } else {
+        const float inv = l == 0.f ? 0.f : 1.0f / l;
         const int64_t q = (int64_t)item.q0 + tok;
-        store_row<kF16>(static_cast<uint16_t*>(a.o.data) + q * a.o.token_stride + head * a.o.head_stride, o,
-                        l == 0.f ? 0.f : 1.0f / l);
-        if (a.lse) a.lse[head * a.rows + q] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+#pragma unroll 1
+        for (int hc = 0; hc < 2 && any; ++hc) {
+          uint32_t o[32];
+          if (tiles > 0) {
+            RESS_TMEM_LD32(tm + kColO + 32 * hc, o);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = 0u;
+          }
+          if (ways > 1) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * by[0]);
+#pragma unroll
+            for (int j = 1; j < kSlots; ++j)
+              if (j < ways && from + j < min(item.t1, item.n[part])) {
+                uint32_t v[32];
+                RESS_TMEM_LD32(tm + j * parts * kColSlot + kColO + 32 * hc, v);
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                  o[e] = __float_as_uint(fmaf(__uint_as_float(v[e]), by[j], __uint_as_float(o[e])));
+              }
+          }
+          if (!exists) continue;
+          if (item.part >= 0) {
+            float4* dst = reinterpret_cast<float4*>(a.part + item.part * kPartFloats + (part * 128 + r) * 64 + 32 * hc);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              dst[e] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]),
+                                   __uint_as_float(o[4 * e + 3]));
+          } else {
+            uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.o.data) + q * a.o.token_stride +
+                                                  head * a.o.head_stride + 32 * hc);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              uint32_t w[4];
+#pragma unroll
+              for (int f = 0; f < 4; ++f)
+                w[f] = pack2<kF16>(__uint_as_float(o[8 * e + 2 * f]) * inv, __uint_as_float(o[8 * e + 2 * f + 1]) * inv);
+              dst[e] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+          }
+        }
+        if (exists && item.part >= 0) {
+          float* rest = a.part + item.part * kPartFloats + kRows * 64 + part * 128 + r;
+          rest[0] = l == 0.f ? -INFINITY : m;
+          rest[kRows] = l;
+        } else if (exists && a.lse) {
+          a.lse[head * a.rows + q] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          for (int j = 1; j < ways; ++j) mbar_arrive(&S.other_empty[slot + j * parts][quarter]);
+          mbar_arrive(&S.it_empty[i]);
+        }
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&S.it_empty[i]);
+      turn1 += parts == 1;
+      turn23 += parts <= 2;
     }
   }
 
@@ -633,7 +645,7 @@ __global__ void __launch_bounds__(256) k_flash_join(const __grid_constant__ Dens
   __shared__ int64_t scratch[34];
   rows::stream_acquire();
   const int G = a.group, T = 128 / G;
-  auto line_of = [&](const Seq& s) { return row_line(a, s, kSlots * T, T); };
+  auto line_of = [&](const Seq& s) { return row_line(a, s, kSlots * T, [&](int n) { return n > 3 * T ? 8 : n > 2 * T ? 6 : n > T ? 5 : 3; }); };
   const int first = blockIdx.x;
   const Range r = find_range(a, line_of, ctas, first + 1, scratch, nullptr);
   if (first + 1 >= r.active || r.total == 0) return;
@@ -642,9 +654,7 @@ __global__ void __launch_bounds__(256) k_flash_join(const __grid_constant__ Dens
   const int64_t end = c.start + c.weight;
   if (c.start == r.x0 || (first > 0 && bound(r.total, r.active, first) > c.start)) return;
   const int tok0 = c.j * kSlots * T;
-  int n = 0;
-#pragma unroll
-  for (int s = 0; s < kSlots; ++s) n = max(n, slot_tiles(a, c.s, tok0, s, T));
+  const int n = item_tiles(a, c.s, tok0, T);
   if (n == 0) return;
   int parts = 1;  // shares first .. first + parts - 1 touch the item
   while (first + parts < r.active && bound(r.total, r.active, first + parts) < end) ++parts;
@@ -662,7 +672,7 @@ __global__ void __launch_bounds__(256) k_flash_join(const __grid_constant__ Dens
   const int half = threadIdx.x >> 4, sub = threadIdx.x & 15;
   for (int i = half; i < 32; i += 16) {
     const int row = blockIdx.y * 32 + i, slot = row >> 7, rr = row & 127;
-    if (rr / G >= slot_tokens(c.s.nq, tok0, slot, T)) continue;
+    if (rr / G >= part_tokens(c.s.nq, tok0, slot, T)) continue;
     float m = -INFINITY, l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int k = 0; k < parts; ++k) {
@@ -670,10 +680,10 @@ __global__ void __launch_bounds__(256) k_flash_join(const __grid_constant__ Dens
       share(k, t0, t1);
       if (t0 == t1) continue;
       const float* p = slot_of(k);
-      const float mk = p[256 * 64 + row];
+      const float mk = p[kRows * 64 + row];
       if (mk == -INFINITY) continue;
       const float4 v = reinterpret_cast<const float4*>(p + row * 64)[sub];
-      const float lk = p[256 * 65 + row], top = fmaxf(m, mk);
+      const float lk = p[kRows * 65 + row], top = fmaxf(m, mk);
       const float wa = m == -INFINITY ? 0.f : ex2(m - top), wb = ex2(mk - top);
       m = top;
       l = fmaf(l, wa, lk * wb);
@@ -759,7 +769,7 @@ cudaError_t launch_flash(const DenseArgs& a, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   if ((e = launch_pdl(kern, ctas, kThreads, smem, st, true, tq, tk, tv, a)) != cudaSuccess) return e;
   if (ctas == 1) return e;
-  return launch_pdl(f16 ? k_flash_join<true> : k_flash_join<false>, dim3(ctas - 1, 8), 256, 0, st, true, a, ctas);
+  return launch_pdl(f16 ? k_flash_join<true> : k_flash_join<false>, dim3(ctas - 1, kRows / 32), 256, 0, st, true, a, ctas);
 }
 
 }  // namespace ress

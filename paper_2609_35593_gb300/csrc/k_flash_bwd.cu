@@ -95,7 +95,7 @@ template <bool kKeys>
 struct Lines {
   const DenseArgs& a;
   int T;  // tokens of an item of rows
-  __device__ Line operator()(const Seq& s) const { return kKeys ? key_line(a, s, 128) : row_line(a, s, T, -1); }
+  __device__ Line operator()(const Seq& s) const { return kKeys ? key_line(a, s, 128) : row_line(a, s, T, [](int) { return 8; }); }
 };
 template <bool kKeys>
 __device__ __forceinline__ int item_tiles(const DenseArgs& a, const Seq& s, int at, int T, int& from) {
@@ -120,16 +120,6 @@ __device__ __forceinline__ void store_row(void* dst, const uint32_t (&o)[N], flo
       w[e] = pack2<kF16>(__uint_as_float(o[8 * k + 2 * e]) * by, __uint_as_float(o[8 * k + 2 * e + 1]) * by);
     p[k] = make_uint4(w[0], w[1], w[2], w[3]);
   }
-}
-
-template <bool kF16>
-__device__ __forceinline__ float2 unpack2(uint32_t v) {
-  if (!kF16) return make_float2(bf16_lo(v), bf16_hi(v));
-  float2 r;
-  asm("{\n\t.reg .f16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, h;\n\t}"
-      : "=f"(r.x), "=f"(r.y)
-      : "r"(v));
-  return r;
 }
 
 }  // namespace
