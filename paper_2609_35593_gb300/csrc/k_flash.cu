@@ -1,22 +1,26 @@
 // Dense attention over packed sequences or a paged cache: O = softmax(s) V for the keys that each row sees,
 // with s = cap tanh(q.k / 8 / cap) - slope |distance|, and log sum exp(s) of each row.
 //
-// One CTA per SM walks its share of the work (attn_work.cuh).  An item is 4 x 128 rows of one head of K and V:
+// One CTA per SM walks its share of the work (attn_work.cuh).  An item is 2 x 128 rows of one head of K and V:
 // floor(128 / group) tokens, each with its `group` heads of Q, make 128 rows, so that heads which share K read it
-// once and single tokens still fill rows.  Its four parts ("slots") share the 64-key tiles that TMA brings in, a
-// quarter of what 128 rows at a time would take from L2.  An item with rows for one slot (single tokens) or two gives
-// its tiles to the slots in turn, which join their sums on chip.  Warp roles (640 threads):
-//   warps 0-15  one row of a slot per thread: online softmax in the exp2 domain.  The reference maximum is that of
-//               an item's first tile, and only raised where 64 exponentials against it add up to more than 2^13
-//               (what P's 16 bits and O's 32 hold easily): O in TMEM is rescaled seldom, and no maximum is formed
-//               otherwise.  Sums are float32, of the exponentials before they are rounded to 16 bits.
-//   warp 16     item and tile producer: TMA of Q, K and V (128-byte swizzle), 9 stages of 16 KB, so that single
-//               tokens, which only stream the cache, keep about 100 KB per SM in flight
-//   warps 17, 18  MMA issuers of two slots each, per tile and slot: O += P V of the tile before (M128 N64 K64, P from
-//               TMEM, V MN-major), then S = Q K^T (M128 N64 K64, both from shared memory) over P's columns
-// Four slots because the softmax warps' chain (scores from TMEM, exponentials, P to TMEM, hand-over) is latency:
-// with two, S double-buffered or in columns of its own, a sub-partition's two warps kept its SFU busy a third of the time
-// (8 images at once 636 and 618 us).
+// once and single tokens still fill rows.  Its halves ("slots") share the 128-key tiles that TMA brings in, half of
+// what 128 rows at a time would take from L2.  An item with rows for one slot (single tokens) gives its tiles to the
+// slots in turn, which join their sums on chip.  Warp roles (640 threads):
+//   warps 4-19  16 rows of a slot each, a row on four lanes: online softmax in the exp2 domain.  The reference maximum is
+//               that of an item's first columns, and only raised where a lane's 16 exponentials against it add up to more
+//               than 2^13 (what P's 16 bits and O's 32 hold easily): O in TMEM is rescaled seldom, and no maximum is
+//               formed otherwise.  Sums are float32, of the exponentials before they are rounded to 16 bits, one for
+//               each lane until the item ends.
+//   warp 0      item and tile producer: TMA of Q, K and V (128-byte swizzle), 5 stages of 32 KB, so that single
+//               tokens, which only stream the cache, keep over 100 KB per SM in flight
+//   warp 1      issuer of S = Q K^T (M128 N128 K64, both from shared memory)
+//   warps 2, 3  issuers of O += P V (M128 N64 K128, P from TMEM, V MN-major), a slot each.  S and P have columns of their
+//               own: S of the next tile runs while the exponentials of this one are formed.
+// What bounds it is the chain of a slot's tile: scores from TMEM, exponentials, P to TMEM and the hand-overs between
+// warps take some 1,200 cycles whatever they compute, so the tiles are as large as TMEM allows, and the 16 warps of
+// softmax (four to a sub-partition) work while others wait.  Measured on 8 images at once, all with the same
+// results: a row per thread and 8 warps, S of 64 keys double-buffered under P 636 us, 128 keys with S and P apart 618;
+// 12 warps, three slots of 64 keys 586; 16 warps, four slots of 64 keys and two issuers 553.
 // Rows of V behind a sequence's last key are zeroed in shared memory (0 x NaN of a cache page never written
 // would be NaN); keys there and masked ones are -inf by selection, whatever their scores are.
 // Every mbarrier wait is bounded; one that gives up records RESS_ETIMEOUT and the CTA leaves, see k_attn.cu.
@@ -30,14 +34,13 @@ using namespace work;
 
 namespace {
 
-constexpr int kThreads = 640, kStages = 9, kSlots = 4, kItems = 4;
-constexpr int kProducer = 16, kIssuer = 17;  // warps 0-15: softmax; issuers of slots 0, 1 and 2, 3: 17, 18
-constexpr uint32_t kTileBytes = kTile * 128;
-constexpr uint32_t kColSlot = 128, kColO = 64;  // TMEM: per slot S (and P), O
+constexpr int kThreads = 640, kStages = 5, kSlots = 2, kItems = 4, kKeys = 128;
+constexpr int kProducer = 0, kIssueS = 1, kIssuePv = 2, kSoftmax = 4;  // warps: producer, issuers, softmax
+constexpr uint32_t kTileBytes = kKeys * 128;
+constexpr uint32_t kColSlot = 256, kColP = 128, kColO = 192;  // TMEM: per slot S, P, O
 // flags of a tile: no more; (per slot) it has the tile; it is its first, its last of the item
-// tiles go to the slots in turn
-constexpr int kTerm = 1, kTurns = 1 << 16, kHas = 2, kBegin = kHas << kSlots, kEnd = kBegin << kSlots;
-constexpr float kMost = 8192.0f;  // sum of 64 exponentials above which the reference is raised
+constexpr int kTerm = 1, kHas = 2, kBegin = kHas << kSlots, kEnd = kBegin << kSlots;
+constexpr float kMost = 8192.0f;  // sum of 16 exponentials above which the reference is raised
 // Lowest reference maximum: finite, so that rows that have seen no key yet give exponentials of 0.
 constexpr float kMinRef = -2147483648.0f;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -49,7 +52,7 @@ struct Item {
   int h, tok;                   // head of K (-1: no more items), first token of the sequence
   int t0, t1, g0;            // tiles; number of the first among all of the CTA's
   int n[kSlots];             // tiles of each 128 rows' keys
-  int parts;                 // 128 rows that the item has, 1..4: slot s takes part s mod `parts` (3: slot 3 idles) and,
+  int parts;                 // 128 rows that the item has, 1 or 2: slot s takes part s mod `parts` and,
   int ways;                  // of that, every `ways`th tile
   int part;                  // slot of partial results, or -1: whole
 };
@@ -59,10 +62,10 @@ struct __align__(1024) Smem {
   uint8_t K[kStages][kTileBytes];
   uint8_t V[kStages][kTileBytes];
   uint64_t kv_full[kStages], kv_empty[kStages];
-  float other[kSlots][2][128];  // maxima and sums of slots that share rows
-  uint64_t other_full[kSlots][4], other_empty[kSlots][4];  // (and their quarters)
-  uint64_t q_full[kSlots], q_empty[kSlots], drain[2];
-  uint64_t s_full[kSlots], p_full[kSlots], o_full[kSlots];
+  float stat[2][kSlots][2][128];  // maxima and sums of the slots' rows, of two items
+  uint64_t stat_full[kSlots][4], other_full[4], other_empty[4];  // (of each quarter)
+  uint64_t q_full[kSlots], q_empty[kSlots], drain[1 + kSlots];
+  uint64_t s_full[kSlots], s_free[kSlots], p_full[kSlots], o_full[kSlots];
   uint64_t it_full[kItems], it_empty[kItems];
   int64_t scratch[34];
   Item item[kItems], next;
@@ -83,7 +86,7 @@ __device__ __forceinline__ int part_tokens(int nq, int tok, int s, int T) { retu
 __device__ __forceinline__ int part_tiles(const DenseArgs& a, const Seq& q, int tok, int s, int T) {
   const int n = part_tokens(q.nq, tok, s, T);
   if (n == 0) return 0;
-  return (max(0, row_limit(a, q, q.d + tok + s * T + n - 1)) + kTile - 1) / kTile;
+  return (max(0, row_limit(a, q, q.d + tok + s * T + n - 1)) + kKeys - 1) / kKeys;
 }
 __device__ __forceinline__ int item_tiles(const DenseArgs& a, const Seq& q, int tok, int T) {
   int n = 0;
@@ -91,7 +94,7 @@ __device__ __forceinline__ int item_tiles(const DenseArgs& a, const Seq& q, int 
   for (int s = 0; s < kSlots; ++s) n = max(n, part_tiles(a, q, tok, s, T));
   return n;
 }
-__device__ __forceinline__ int ways_of(int parts) { return parts == 1 ? 4 : parts == 2 ? 2 : 1; }
+__device__ __forceinline__ int ways_of(int parts) { return parts == 1 ? kSlots : 1; }
 
 }  // namespace
 
@@ -109,23 +112,25 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
       mbar_init(&S.kv_full[s], 1);
-      mbar_init(&S.kv_empty[s], kSlots);
+      mbar_init(&S.kv_empty[s], 1 + kSlots);
     }
     for (int s = 0; s < kSlots; ++s) {
       mbar_init(&S.q_full[s], 1);
       mbar_init(&S.q_empty[s], 1);
       mbar_init(&S.s_full[s], 1);
-      mbar_init(&S.p_full[s], 4);
+      mbar_init(&S.s_free[s], 8);
+      mbar_init(&S.p_full[s], 8);
       mbar_init(&S.o_full[s], 1);
-      for (int q = 0; q < 4; ++q) {
-        mbar_init(&S.other_full[s][q], 1);
-        mbar_init(&S.other_empty[s][q], 1);
-      }
+      for (int q = 0; q < 4; ++q) mbar_init(&S.stat_full[s][q], 2);
     }
-    for (int p = 0; p < 2; ++p) mbar_init(&S.drain[p], 1);
+    for (int i = 0; i < 1 + kSlots; ++i) mbar_init(&S.drain[i], 1);
+    for (int q = 0; q < 4; ++q) {
+      mbar_init(&S.other_full[q], 2);
+      mbar_init(&S.other_empty[q], 2);
+    }
     for (int i = 0; i < kItems; ++i) {
       mbar_init(&S.it_full[i], 1);
-      mbar_init(&S.it_empty[i], 4 * kSlots);
+      mbar_init(&S.it_empty[i], 8 * kSlots);
     }
     S.abort = 0;
     fence_barrier_init();
@@ -133,26 +138,26 @@ __global__ void __launch_bounds__(kThreads, 1)
     prefetch_tensormap(&tmK);
     prefetch_tensormap(&tmV);
   }
-  if (warp == kIssuer) tmem_alloc(&S.tmem_base, 512);
+  if (warp == kIssueS) tmem_alloc(&S.tmem_base, 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = S.tmem_base;
   rows::stream_acquire();
-  auto line_of = [&](const Seq& s) { return row_line(a, s, kSlots * T, [&](int n) { return n > 3 * T ? 8 : n > 2 * T ? 6 : n > T ? 5 : 3; }); };
+  auto line_of = [&](const Seq& s) { return row_line(a, s, kSlots * T, [&](int n) { return n > T ? 8 : 5; }); };
   const Range range = find_range(a, line_of, gridDim.x, blockIdx.x, S.scratch, blockIdx.x == 0 ? a.status : nullptr);
 
   // 640 threads start with 96 registers each; the softmax warps, which hold a row's scores, get 104 of them
   // (512 x 104 + 128 x 64 <= 640 x 96).  A spilled register would go to L2: shared memory leaves next to no L1.
-  if (warp >= kProducer) {
+  if (warp < kSoftmax) {
     regs_dec<64>();
     if (warp == kProducer) {
       // =============================== producer ====================================
       int g = 0, pub = 0;
       uint32_t loads = 0;  // times that each slot's Q was loaded, a byte per slot
       bool failed = false;
-      const int box = a.table ? min(kTile, a.page & -a.page) : kTile;  // the page's power of two
-      const int boxes = kTile / box;
+      const int box = a.table ? min(kKeys, a.page & -a.page) : kKeys;  // the page's power of two
+      const int boxes = kKeys / box;
         // The next item that this share has tiles of, to S.next (h -1: none left).  One lane looks for it, in shared
       // memory: the sequences' arithmetic in 64 bits would otherwise take the registers of the tile loop.
       auto advance = [&](bool first) {
@@ -201,7 +206,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (item.t0 == item.t1) continue;  // rows without keys
           const int h = item.h, nk = item.nk, t0 = item.t0, t1 = item.t1, k0 = item.k0;
           const int32_t* table = a.table ? a.table + item.b * a.table_stride : nullptr;
-          // lanes 0..3: what slot `lane` takes of the item
+          // the first lanes: what slot `lane` takes of the item
           const int parts = item.parts, ways = item.ways, mine_part = lane % parts, way = lane / parts;
           const int last = lane < kSlots && way < ways ? min(t1, item.n[mine_part]) : 0;
           const uint32_t some = __ballot_sync(0xffffffffu, t0 + way < last);
@@ -225,7 +230,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const bool mine = lane < 2 * boxes;
           const int at = (lane < boxes ? lane : lane - boxes) * box;  // its first key in the tile
           auto place = [&](int t, int& row, int& page) {
-            const int key = t * kTile + at;
+            const int key = t * kKeys + at;
             row = k0 + key, page = 0;
             if (!table) return;
             row = key % a.page, page = (int)a.n_pages;  // no such page: TMA fills in zeros
@@ -245,7 +250,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (t + 1 < t1) place(t + 1, next_row, next_page);
             int flags = 0;
             if (t < last && (t - t0) % ways == way) {
-              flags = kHas << lane | (ways > 1 ? kTurns : 0);
+              flags = kHas << lane;
               if (t == t0 + way) flags |= kBegin << lane;
               if (t + ways >= last) flags |= kEnd << lane;
             }
@@ -290,104 +295,144 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int s = 0; s < kSlots; ++s)
           if (loads >> (8 * s) & 0xff) mbar_wait(&S.q_full[s], ((loads >> (8 * s) & 0xff) - 1) & 1, &no_abort, kDrainNs);
       }
-    } else if (warp < kIssuer + 2) {
+    } else {
       // ================================ MMA issuers ==================================
-      const int pair = warp - kIssuer;
       const bool leader = elect_one();
       bool failed = false;
-      constexpr uint32_t kQk = idesc16<kF16>(128, kTile, false), kPv = idesc16<kF16>(128, 64, true);
+      constexpr uint32_t kQk = idesc16<kF16>(128, kKeys, false), kPv = idesc16<kF16>(128, 64, true);
       constexpr uint64_t kStageUnits = kTileBytes >> 4, kQUnits = (128 * 128) >> 4;
-      const uint64_t kd0 = sdesc_sw128(smem_u32(S.K[0])), vd0 = sdesc_sw128(smem_u32(S.V[0]));
-      const uint64_t qd0 = sdesc_sw128(smem_u32(S.Q[2 * pair]));
-      int st = 0;
       uint32_t phase = 0;
-      // of each of the two slots: tiles' P and items' Q so far (parity); stage of the tile whose P V is to come (or -1);
-      // whether that is its item's last, its item's first
-      uint32_t p_phase[2] = {0, 0}, q_phase[2] = {0, 0};
-      int held[2] = {-1, -1};
-      bool ends[2] = {false, false}, begins[2] = {false, false};
-      auto issue_pv = [&](int j) -> bool {
-        const int slot = 2 * pair + j;
-        if (!wait(&S.p_full[slot], p_phase[j], abort)) return false;
-        tc_fence_after();
-        if (leader) {
-          const uint32_t tm = tmem + slot * kColSlot;
-          const uint64_t vd = vd0 + (uint64_t)held[j] * kStageUnits;
-#pragma unroll
-          for (int k = 0; k < 4; ++k) mma_bf16_ts(tm + kColO, tm + 8 * k, vd + 128 * k, kPv, (k > 0 || !begins[j]) ? 1u : 0u);
-          mma_commit(&S.kv_empty[held[j]]);
-          if (ends[j]) mma_commit(&S.o_full[slot]);
-        }
-        __syncwarp();
-        p_phase[j] ^= 1;
-        held[j] = -1;
-        return true;
-      };
-      // Per tile and slot: P V of the slot's tile before, then S.  The last P V of an item does not wait for a tile to
-      // come: the producer may be waiting for the softmax warps to end the item.
-      while (!failed) {
-        if (!wait(&S.kv_full[st], phase, abort)) {
-          failed = true;
-          break;
-        }
-        const int flags = S.flags[st];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int slot = 2 * pair + j;
-          const bool has = flags >> slot & kHas;
-          if (failed) continue;
-          if (has && (flags >> slot & kBegin)) {
-            if (!wait(&S.q_full[slot], q_phase[j], abort)) failed = true;
-            q_phase[j] ^= 1;
-          }
-          if (!failed && held[j] >= 0 && (has || ends[j] || (flags & kTerm) ||
-                                           ((flags & kTurns) && mbar_ready(&S.p_full[slot], p_phase[j]))) &&
-              !issue_pv(j))
+      if (warp == kIssueS) {
+        const uint64_t kd0 = sdesc_sw128(smem_u32(S.K[0])), qd0 = sdesc_sw128(smem_u32(S.Q[0]));
+        uint32_t s_phase[kSlots] = {1, 1}, q_phase[kSlots] = {0, 0};
+        for (int st = 0; !failed;) {
+          if (!wait(&S.kv_full[st], phase, abort)) {
             failed = true;
-          if (failed || (flags & kTerm)) continue;
-          if (has) {
+            break;
+          }
+          const int flags = S.flags[st];
+          if (flags & kTerm) break;
+          const uint64_t kd = kd0 + (uint64_t)st * kStageUnits;
+#pragma unroll
+          for (int s = 0; s < kSlots; ++s) {
+            if (failed || !(flags & kHas << s)) continue;
+            if (flags & kBegin << s) {
+              failed = !wait(&S.q_full[s], q_phase[s], abort);
+              q_phase[s] ^= 1;
+            }
+            // (the first time: at once)
+            if (failed || !wait(&S.s_free[s], s_phase[s], abort)) {
+              failed = true;
+              continue;
+            }
+            s_phase[s] ^= 1;
             tc_fence_after();
             if (leader) {
-              const uint64_t kd = kd0 + (uint64_t)st * kStageUnits, qd = qd0 + j * kQUnits;
+              const uint64_t qd = qd0 + s * kQUnits;
 #pragma unroll
-              for (int k = 0; k < 4; ++k)
-                mma_bf16_ss(tmem + slot * kColSlot, qd + 2 * k, kd + 2 * k, kQk, k > 0 ? 1u : 0u);
-              mma_commit(&S.s_full[slot]);
-              if (flags >> slot & kEnd) mma_commit(&S.q_empty[slot]);
+              for (int k = 0; k < 4; ++k) mma_bf16_ss(tmem + s * kColSlot, qd + 2 * k, kd + 2 * k, kQk, k > 0 ? 1u : 0u);
+              mma_commit(&S.s_full[s]);
+              if (flags & kEnd << s) mma_commit(&S.q_empty[s]);
             }
-            held[j] = st, ends[j] = flags >> slot & kEnd, begins[j] = flags >> slot & kBegin;
+            __syncwarp();
+          }
+          if (lane == 0) mbar_arrive(&S.kv_empty[st]);
+          if (++st == kStages) st = 0, phase ^= 1;
+        }
+      } else {
+        const int slot = warp - kIssuePv;
+        const uint32_t tm = tmem + slot * kColSlot;
+        const uint64_t vd0 = sdesc_sw128(smem_u32(S.V[0]));
+        uint32_t p_phase = 0;
+        for (int st = 0;;) {
+          if (!wait(&S.kv_full[st], phase, abort)) {
+            failed = true;
+            break;
+          }
+          const int flags = S.flags[st];
+          if (flags & kTerm) break;
+          if (flags & kHas << slot) {
+            if (!wait(&S.p_full[slot], p_phase, abort)) {
+              failed = true;
+              break;
+            }
+            p_phase ^= 1;
+            tc_fence_after();
+            if (leader) {
+              const uint64_t vd = vd0 + (uint64_t)st * kStageUnits;
+              mma_bf16_ts(tm + kColO, tm + kColP, vd, kPv, flags & kBegin << slot ? 0u : 1u);
+#pragma unroll
+              for (int k = 1; k < 8; ++k) mma_bf16_ts(tm + kColO, tm + kColP + 8 * k, vd + 128 * k, kPv, 1u);
+              mma_commit(&S.o_full[slot]);
+              mma_commit(&S.kv_empty[st]);
+            }
+            __syncwarp();
           } else if (lane == 0) {
             mbar_arrive(&S.kv_empty[st]);
           }
-          __syncwarp();
-        }
-        if (flags & kTerm) break;
-        if (++st == kStages) st = 0, phase ^= 1;
-        if (!failed && ((held[0] >= 0 && ends[0]) || (held[1] >= 0 && ends[1])) && !mbar_ready(&S.kv_full[st], phase)) {
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-            if (!failed && held[j] >= 0 && ends[j] && !issue_pv(j)) failed = true;
+          if (++st == kStages) st = 0, phase ^= 1;
         }
       }
       if (failed && lane == 0) give_up(S, a.status);
       // wait for every MMA issued so far before TMEM is released
       if (leader) {
-        mma_commit(&S.drain[pair]);
+        mma_commit(&S.drain[warp - kIssueS]);
         volatile int no_abort = 0;
-        mbar_wait(&S.drain[pair], 0, &no_abort, kDrainNs);
+        mbar_wait(&S.drain[warp - kIssueS], 0, &no_abort, kDrainNs);
       }
       __syncwarp();
     }
   } else {
     regs_inc<104>();
     // ================================ softmax =====================================
-    const int slot = warp >> 2, quarter = warp & 3;
-    const int r = quarter * 32 + lane;             // row within the slot
-    const uint32_t tm = tmem + slot * kColSlot + ((uint32_t)(quarter * 32) << 16);
+    const int idx = warp - kSoftmax, slot = idx >> 3, half = idx >> 2 & 1, quarter = warp & 3;
+    const int r0 = quarter * 32 + half * 16 + (lane >> 2), two = 2 * (lane & 3);  // this lane's rows: r0, r0 + 8; columns
+    const uint32_t tq = tmem + slot * kColSlot + ((uint32_t)(quarter * 32) << 16), tm = tq + ((uint32_t)(half * 16) << 16);
     const float kScale = kGen ? 1.0f : kLog2e * 0.125f;
     const float cap = a.cap, in = a.cap > 0.f ? 0.125f / a.cap : 0.125f * kLog2e, out = a.cap * kLog2e;
-    uint32_t c = 0, ended = 0;        // tiles of this slot, and items with any, so far
-    uint32_t turn1 = 0, turn23 = 0;   // items in which slot 1, slots 2 and 3 help another one, so far
+    // p = 2^(x kScale - m) of 64 columns, packed, and their sums
+    auto exps = [&](const float (&x)[32], const float (&m)[2], uint32_t (&w)[16], float (&sum)[2]) {
+      float s[2][2] = {{0.f, 0.f}, {0.f, 0.f}};
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        float t0, t1;
+        fma2(t0, t1, x[2 * e], x[2 * e + 1], kScale, kScale, -m[e & 1], -m[e & 1]);
+        t0 = ex2(t0), t1 = ex2(t1);
+        w[e] = pack2<kF16>(t0, t1);
+        add2(s[e & 1][0], s[e & 1][1], s[e & 1][0], s[e & 1][1], t0, t1);
+      }
+      sum[0] = s[0][0] + s[0][1], sum[1] = s[1][0] + s[1][1];
+    };
+    // the largest score of 64 columns, of each row
+    auto row_max = [&](const float (&x)[32], float (&top)[2]) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        top[i] = fmaxf(x[2 * i], x[2 * i + 1]);
+#pragma unroll
+        for (int j = 1; j < 8; ++j) top[i] = fmax3(top[i], x[4 * j + 2 * i], x[4 * j + 2 * i + 1]);
+        top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
+        top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2)) * kScale;
+      }
+    };
+    // the reference maxima to those of these columns, where they are larger; what was summed up is to be scaled by alpha
+    auto raise = [&](const float (&x)[32], float (&m)[2], float (&alpha)[2]) {
+      float top[2];
+      row_max(x, top);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        top[j] = fmaxf(top[j], m[j]);
+        alpha[j] = ex2(m[j] - top[j]);
+        m[j] = top[j];
+      }
+    };
+    auto scale_o = [&](const float (&alpha)[2]) {
+      uint32_t v[32];
+      RESS_TMEM_LD16X64(tm + kColO, v);
+#pragma unroll
+      for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * alpha[e >> 1 & 1]);
+      RESS_TMEM_ST16X64(tm + kColO, v);
+    };
+    uint32_t c = 0, turn = 0, led = 0;  // tiles of this slot, items of one part, and items that it writes, so far
     bool stop = false;
     for (int pub = 0; !stop; ++pub) {
       const int i = pub % kItems;
@@ -397,206 +442,224 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       const Item& item = S.item[i];
       if (item.h < 0) break;
-      const int parts = item.parts, ways = item.ways, part = slot % parts, way = slot / parts;
-      const int ntok = way < ways ? part_tokens(item.nq, item.tok, part, T) : 0;
-      const int from = item.t0 + way, tiles = way < ways ? max(0, min(item.t1, item.n[part]) - from + ways - 1) / ways : 0;
-      const int tok = item.tok + part * T + r / G;  // of the sequence
-      const bool exists = r / G < ntok;
-      const int pos = item.d + tok;
-      const int lim = !exists ? 0 : a.causal ? min(item.nk, max(item.p, pos + 1)) : item.nk;
-      // rows that do not exist see what the last one does: no tile is masked for them alone
-      const int least = __reduce_min_sync(0xffffffffu, exists ? max(lim, 0) : INT32_MAX);
-      const bool any = __any_sync(0xffffffffu, exists);
-      const int head = item.h * G + r % G;
-      float slope = 0.f;
-      if (kGen && a.slopes && exists) slope = a.slopes[head] * kLog2e;
-      float m = -INFINITY, l = 0.f;  // reference maximum (log2 units), sum of the exponentials against it
+      const int parts = item.parts, ways = item.ways, part = slot % parts, way = slot / parts, nk = item.nk;
+      const int ntok = part_tokens(item.nq, item.tok, part, T), tok0 = item.tok + part * T;
+      const int from = item.t0 + way, tiles = max(0, min(item.t1, item.n[part]) - from + ways - 1) / ways;
+      int pos[2], lim[2];
+      float slope[2];
+      int least = INT32_MAX;
+      bool any = false;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int r = r0 + 8 * j, t = r / G;
+        pos[j] = item.d + tok0 + t;
+        lim[j] = t >= ntok ? 0 : a.causal ? max(0, min(nk, max(item.p, pos[j] + 1))) : nk;
+        // rows that do not exist are masked for nobody's sake
+        if (t < ntok) least = min(least, lim[j]), any = true;
+        slope[j] = kGen && a.slopes && t < ntok ? a.slopes[item.h * G + r % G] * kLog2e : 0.f;
+      }
+      least = __reduce_min_sync(0xffffffffu, least);
+      any = __any_sync(0xffffffffu, any);
+      // scores of the 64 keys from `first` on, as the exponentials take them
+      auto scores = [&](const uint32_t (&v)[32], float (&x)[32], int first) {
+#pragma unroll
+        for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(v[e]);
+        if (kGen) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) x[e] = cap > 0.f ? out * tanh_of(x[e] * in) : x[e] * in;
+          if (a.slopes) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              const int j = e >> 1 & 1;
+              x[e] = fmaf(-slope[j], fabsf((float)(pos[j] - first - two) - (float)(8 * (e >> 2) + (e & 1))), x[e]);
+            }
+          }
+        }
+        if (first + 64 > least) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) x[e] = 8 * (e >> 2) + (e & 1) < lim[e >> 1 & 1] - first - two ? x[e] : -INFINITY;
+        }
+      };
+      float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};  // reference maxima (log2 units), this lane's sums
       for (int k = 0; k < tiles; ++k, ++c) {
-        const int t = from + k * ways, key = t * kTile;
+        const int t = from + k * ways, key = t * kKeys;
         if (!wait(&S.s_full[slot], c & 1, abort)) {
           give_up(S, a.status);
           stop = true;
           break;
         }
         tc_fence_after();
-        if (any) {  // rows of a warp without any are garbage that nothing reads
-          float alpha = 1.f, sum;
-          uint32_t w[32];
-          // Against the reference so far: a sum below kMost says that no exponential is above it, so the maximum is
-          // looked for only in an item's first tile and where that fails.
-          bool looked = k == 0;
-#pragma unroll 1
-          for (;;) {
-            float x[64];
-            {
-              uint32_t v[64];
-              RESS_TMEM_LD64(tm, v);
-#pragma unroll
-              for (int e = 0; e < 64; ++e) x[e] = __uint_as_float(v[e]);
-            }
-            if (kGen) {
-              if (cap > 0.f) {
-#pragma unroll
-                for (int e = 0; e < 64; ++e) x[e] = out * tanh_of(x[e] * in);
-              } else {
-#pragma unroll
-                for (int e = 0; e < 64; ++e) x[e] *= in;
-              }
-              if (a.slopes) {
-                const float dist = (float)(pos - key);
-#pragma unroll
-                for (int e = 0; e < 64; ++e) x[e] = fmaf(-slope, fabsf(dist - (float)e), x[e]);
-              }
-            }
-            if (key + kTile > least) {
-#pragma unroll
-              for (int e = 0; e < 64; ++e) x[e] = key + e < lim ? x[e] : -INFINITY;
-            }
-            if (looked) {
-              float top = x[0];
-#pragma unroll
-              for (int e = 1; e < 63; e += 2) top = fmax3(top, x[e], x[e + 1]);
-              top = fmaxf(top, x[63]) * kScale;
-              if (k == 0) {
-                m = fmaxf(top, kMinRef);
-              } else if (top > m) {
-                alpha = ex2(m - top);
-                m = top;
-              }
-            }
-            const float nm = -m;
-            float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
-#pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              float t0, t1;
-              fma2(t0, t1, x[2 * e], x[2 * e + 1], kScale, kScale, nm, nm);
-              t0 = ex2(t0), t1 = ex2(t1);
-              w[e] = pack2<kF16>(t0, t1);
-              if (e & 1)
-                add2(s2, s3, s2, s3, t0, t1);
-              else
-                add2(s0, s1, s0, s1, t0, t1);
-            }
-            sum = (s0 + s2) + (s1 + s3);
-            if (looked || !__any_sync(0xffffffffu, sum > kMost)) break;
-            looked = true;
+        if (any) {
+          // Two halves of 64 columns.  Against the reference so far: sums below kMost say that no exponential is above
+          // it, so the maximum is looked for only in an item's first columns and where that fails, which is found out
+          // while the next load or the store is on its way.
+          float x[32], sum[2], alpha[2];
+          uint32_t v[32], w[16];
+          RESS_TMEM_LD16X64(tm, v);
+          scores(v, x, key);
+          if (k == 0) {
+            row_max(x, alpha);
+            m[0] = fmaxf(alpha[0], kMinRef), m[1] = fmaxf(alpha[1], kMinRef);
           }
-          l = fmaf(l, alpha, sum);
-          RESS_TMEM_ST32(tm, w);
-          if (looked && k > 0) {  // the P V before this one is done: S of this tile was issued after it
+          exps(x, m, w, sum);
+          // the P V before this one has read P and added to O
+          if (c > 0 && !wait(&S.o_full[slot], (c - 1) & 1, abort)) {
+            give_up(S, a.status);
+            stop = true;
+            break;
+          }
+          tc_fence_after();
+          RESS_TMEM_ST16X32P_NOWAIT(tm + kColP, w);
+          RESS_TMEM_LD16X64_NOWAIT(tm + 64, v);
+          if (__any_sync(0xffffffffu, fmaxf(sum[0], sum[1]) > kMost)) {
+            RESS_TMEM_WAIT_LD32(v);
+            tmem_wait_st();
+            RESS_TMEM_LD16X64(tm, v);
+            scores(v, x, key);
+            raise(x, m, alpha);
+            l[0] *= alpha[0], l[1] *= alpha[1];
+            exps(x, m, w, sum);
+            RESS_TMEM_ST16X32P(tm + kColP, w);
+            if (k > 0) scale_o(alpha);
+            RESS_TMEM_LD16X64_NOWAIT(tm + 64, v);
+          }
+          l[0] += sum[0], l[1] += sum[1];
+          RESS_TMEM_WAIT_LD32(v);
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&S.s_free[slot]);  // S is in registers
+          __syncwarp();
+          scores(v, x, key + 64);
+          exps(x, m, w, sum);
+          RESS_TMEM_ST16X32P_NOWAIT(tm + kColP + 32, w);
+          if (__any_sync(0xffffffffu, fmaxf(sum[0], sum[1]) > kMost)) {
+            tmem_wait_st();
+            raise(x, m, alpha);
+            l[0] *= alpha[0], l[1] *= alpha[1];
+            exps(x, m, w, sum);
+            RESS_TMEM_ST16X32P(tm + kColP + 32, w);
+            RESS_TMEM_LD16X32P(tm + kColP, w);  // the first half's P
 #pragma unroll
-            for (int hc = 0; hc < 2; ++hc) {
-              uint32_t v[32];
-              RESS_TMEM_LD32(tm + kColO + 32 * hc, v);
-#pragma unroll
-              for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * alpha);
-              RESS_TMEM_ST32(tm + kColO + 32 * hc, v);
+            for (int e = 0; e < 16; ++e) {
+              const float2 y = unpack2<kF16>(w[e]);
+              w[e] = pack2<kF16>(y.x * alpha[e & 1], y.y * alpha[e & 1]);
             }
+            RESS_TMEM_ST16X32P(tm + kColP, w);
+            if (k > 0) scale_o(alpha);
+          }
+          l[0] += sum[0], l[1] += sum[1];
+          tmem_wait_st();
+        } else {  // no rows in this warp: P is garbage that nothing reads
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&S.s_free[slot]);
+          __syncwarp();
+          if (c > 0 && !wait(&S.o_full[slot], (c - 1) & 1, abort)) {
+            give_up(S, a.status);
+            stop = true;
+            break;
           }
         }
-        if (key + kTile > item.nk) {  // V's rows behind the last key
+        if (key + kKeys > nk) {  // V's rows behind the last key
           const int g = item.g0 + t - item.t0, st = g % kStages;
           if (!wait(&S.kv_full[st], (g / kStages) & 1, abort)) {
             give_up(S, a.status);
             stop = true;
             break;
           }
-          zero_rows(S.V[st], item.nk - key, r);
+          zero_rows(S.V[st], nk - key, (idx & 7) * 32 + lane);
           fence_proxy_async_smem();
         }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&S.p_full[slot]);
+        __syncwarp();
       }
       if (stop) break;
       if (tiles > 0) {
-        if (!wait(&S.o_full[slot], ended & 1, abort)) {
+        if (!wait(&S.o_full[slot], (c - 1) & 1, abort)) {
           give_up(S, a.status);
           break;
         }
-        ++ended;
         tc_fence_after();
       }
-      // Slots with the same rows: the first of them adds the others' O, which it reads where they are, to its own:
-      // O = sum_s 2^(m_s - m) O_s.
-      const uint32_t turn = (slot == 1 ? turn1 : turn23) & 1;
-      if (way > 0 && way < ways) {
-        S.other[slot][0][r] = l == 0.f ? -INFINITY : m;
-        S.other[slot][1][r] = l;
-        tc_fence_before();
-        __syncwarp();
+      // The rows' maxima and sums, for those that write them: from here on a lane has a whole row of a quarter, of which
+      // this warp writes half of the channels.  Slots with the same rows: the first adds the other's O, which it
+      // reads where it is, to its own, O = sum_s 2^(m_s - m) O_s.
+      float(*stat)[2][128] = S.stat[pub & 1];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        l[j] += __shfl_xor_sync(0xffffffffu, l[j], 1);
+        l[j] += __shfl_xor_sync(0xffffffffu, l[j], 2);
+        if ((lane & 3) == 0) {
+          stat[slot][0][r0 + 8 * j] = l[j] == 0.f ? -INFINITY : m[j];
+          stat[slot][1][r0 + 8 * j] = l[j];
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (way > 0) {
         if (lane == 0) {
-          mbar_arrive(&S.other_full[slot][quarter]);
+          mbar_arrive(&S.other_full[quarter]);
           mbar_arrive(&S.it_empty[i]);
         }
-        if (!wait(&S.other_empty[slot][quarter], turn, abort)) {
+        __syncwarp();
+        if (!wait(&S.other_empty[quarter], turn & 1, abort)) {
           give_up(S, a.status);
           break;
         }
       } else {
-        float by[kSlots] = {1.f, 0.f, 0.f, 0.f};  // weights of this slot and the others
-        if (ways > 1) {
-          float ms[kSlots];
-          ms[0] = l == 0.f ? -INFINITY : m;
-#pragma unroll
-          for (int j = 1; j < kSlots; ++j) {
-            ms[j] = -INFINITY;
-            if (j < ways) {
-              const int s = slot + j * parts;
-              if (!wait(&S.other_full[s][quarter], (s == 1 ? turn1 : turn23) & 1, abort)) stop = true;
-              ms[j] = S.other[s][0][r];
-            }
-          }
-          if (stop) {
-            give_up(S, a.status);
-            break;
-          }
-          tc_fence_after();
-          const float top = fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3]));
-          by[0] = ms[0] == -INFINITY ? 0.f : ex2(ms[0] - top);
-          l *= by[0];
-#pragma unroll
-          for (int j = 1; j < kSlots; ++j)
-            if (ms[j] != -INFINITY) {
-              by[j] = ex2(ms[j] - top);
-              l = fmaf(by[j], S.other[slot + j * parts][1][r], l);
-            }
-          if (top != -INFINITY) m = top;
+        const int r = quarter * 32 + lane, head = item.h * G + r % G;
+        const bool exists = r / G < ntok;
+        if (lane == 0) mbar_arrive(&S.stat_full[slot][quarter]);
+        __syncwarp();
+        if (!wait(&S.stat_full[slot][quarter], led & 1, abort) ||
+            (ways > 1 && !wait(&S.other_full[quarter], turn & 1, abort))) {
+          give_up(S, a.status);
+          break;
         }
-        const float inv = l == 0.f ? 0.f : 1.0f / l;
-        const int64_t q = (int64_t)item.q0 + tok;
-#pragma unroll 1
-        for (int hc = 0; hc < 2 && any; ++hc) {
+        tc_fence_after();
+        float mr = stat[slot][0][r], lr = stat[slot][1][r], by0 = 1.f, by1 = 0.f;
+        if (ways > 1) {
+          const float m1 = stat[slot + 1][0][r], l1 = stat[slot + 1][1][r], top = fmaxf(mr, m1);
+          by0 = mr == -INFINITY ? 0.f : ex2(mr - top);
+          by1 = m1 == -INFINITY ? 0.f : ex2(m1 - top);
+          mr = top;
+          lr = fmaf(lr, by0, l1 * by1);
+        }
+        const int64_t q = (int64_t)item.q0 + tok0 + r / G;
+        if (__any_sync(0xffffffffu, exists)) {
           uint32_t o[32];
           if (tiles > 0) {
-            RESS_TMEM_LD32(tm + kColO + 32 * hc, o);
+            RESS_TMEM_LD32(tq + kColO + 32 * half, o);
           } else {
 #pragma unroll
             for (int e = 0; e < 32; ++e) o[e] = 0u;
           }
           if (ways > 1) {
+            uint32_t v[32];
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * by[0]);
+            for (int e = 0; e < 32; ++e) v[e] = 0u;
+            if (from + 1 < min(item.t1, item.n[part])) RESS_TMEM_LD32(tq + kColSlot + kColO + 32 * half, v);
 #pragma unroll
-            for (int j = 1; j < kSlots; ++j)
-              if (j < ways && from + j < min(item.t1, item.n[part])) {
-                uint32_t v[32];
-                RESS_TMEM_LD32(tm + j * parts * kColSlot + kColO + 32 * hc, v);
-#pragma unroll
-                for (int e = 0; e < 32; ++e)
-                  o[e] = __float_as_uint(fmaf(__uint_as_float(v[e]), by[j], __uint_as_float(o[e])));
-              }
+            for (int e = 0; e < 32; ++e)
+              o[e] = __float_as_uint(fmaf(__uint_as_float(v[e]), by1, __uint_as_float(o[e]) * by0));
           }
-          if (!exists) continue;
-          if (item.part >= 0) {
-            float4* dst = reinterpret_cast<float4*>(a.part + item.part * kPartFloats + (part * 128 + r) * 64 + 32 * hc);
+          if (!exists) {
+          } else if (item.part >= 0) {
+            float* parts_at = a.part + item.part * kPartFloats;
+            float4* dst = reinterpret_cast<float4*>(parts_at + (part * 128 + r) * 64 + 32 * half);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
               dst[e] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]),
                                    __uint_as_float(o[4 * e + 3]));
+            if (half == 0) {
+              parts_at[kRows * 64 + part * 128 + r] = mr;
+              parts_at[kRows * 65 + part * 128 + r] = lr;
+            }
           } else {
+            const float inv = lr == 0.f ? 0.f : 1.0f / lr;
             uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.o.data) + q * a.o.token_stride +
-                                                  head * a.o.head_stride + 32 * hc);
+                                                  head * a.o.head_stride + 32 * half);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               uint32_t w[4];
@@ -605,31 +668,26 @@ __global__ void __launch_bounds__(kThreads, 1)
                 w[f] = pack2<kF16>(__uint_as_float(o[8 * e + 2 * f]) * inv, __uint_as_float(o[8 * e + 2 * f + 1]) * inv);
               dst[e] = make_uint4(w[0], w[1], w[2], w[3]);
             }
+            if (half == 0 && a.lse) a.lse[head * a.rows + q] = lr == 0.f ? -INFINITY : (mr + log2f(lr)) * 0.6931471805599453f;
           }
-        }
-        if (exists && item.part >= 0) {
-          float* rest = a.part + item.part * kPartFloats + kRows * 64 + part * 128 + r;
-          rest[0] = l == 0.f ? -INFINITY : m;
-          rest[kRows] = l;
-        } else if (exists && a.lse) {
-          a.lse[head * a.rows + q] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
         }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
-          for (int j = 1; j < ways; ++j) mbar_arrive(&S.other_empty[slot + j * parts][quarter]);
+          if (ways > 1) mbar_arrive(&S.other_empty[quarter]);
           mbar_arrive(&S.it_empty[i]);
         }
+        __syncwarp();
+        ++led;
       }
-      turn1 += parts == 1;
-      turn23 += parts <= 2;
+      turn += ways > 1;
     }
   }
 
   __syncwarp();
   tc_fence_before();
   __syncthreads();
-  if (warp == kIssuer) {
+  if (warp == kIssueS) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
@@ -645,7 +703,7 @@ __global__ void __launch_bounds__(256) k_flash_join(const __grid_constant__ Dens
   __shared__ int64_t scratch[34];
   rows::stream_acquire();
   const int G = a.group, T = 128 / G;
-  auto line_of = [&](const Seq& s) { return row_line(a, s, kSlots * T, [&](int n) { return n > 3 * T ? 8 : n > 2 * T ? 6 : n > T ? 5 : 3; }); };
+  auto line_of = [&](const Seq& s) { return row_line(a, s, kSlots * T, [&](int n) { return n > T ? 8 : 5; }); };
   const int first = blockIdx.x;
   const Range r = find_range(a, line_of, ctas, first + 1, scratch, nullptr);
   if (first + 1 >= r.active || r.total == 0) return;
@@ -756,7 +814,7 @@ cudaError_t launch_flash(const DenseArgs& a, cudaStream_t st) {
   const int64_t keys = a.table ? a.page : a.keys > 0 ? a.keys : 1, pages = a.table ? a.n_pages : 1;
   ress_heads k = a.k, v = a.v;
   if (!a.table && a.keys == 0) k = v = a.q, k.head_stride = v.head_stride = 64;
-  const int box = a.table && (a.page & -a.page) < kTile ? (a.page & -a.page) : kTile;
+  const int box = a.table && (a.page & -a.page) < kKeys ? (a.page & -a.page) : kKeys;
   if (!make_row_map(&tq, a.q, a.type, a.rows, a.kv_heads, a.group, 128 / a.group) ||
       !make_key_map(&tk, k, a.type, keys, pages, a.k_page_stride, a.kv_heads, box) ||
       !make_key_map(&tv, v, a.type, keys, pages, a.v_page_stride, a.kv_heads, box))
