@@ -116,10 +116,17 @@ struct Range {
   int64_t total, x0, x1, base;
   int b0, active;
 };
-__device__ __forceinline__ int active_ctas(int64_t total, int ctas) {
-  return (int)max((int64_t)1, min((int64_t)ctas, total / kLeast));
+// a / b of numbers that are mostly below 2^32 (a division of 64 bits takes some hundred instructions).
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
 }
-__device__ __forceinline__ int64_t bound(int64_t total, int active, int c) { return total / active * c + total % active * c / active; }
+__device__ __forceinline__ int active_ctas(int64_t total, int ctas) {
+  return (int)max((int64_t)1, min((int64_t)ctas, quotient(total, kLeast)));
+}
+__device__ __forceinline__ int64_t bound(int64_t total, int active, int c) {
+  const int64_t one = quotient(total, active);
+  return one * c + quotient((total - one * active) * c, active);
+}
 
 // All threads of the CTA: share `cta` of `ctas`.  scratch: 34 words of shared memory; status: NULL, or where
 // sequences outside their tensors are told.
@@ -171,6 +178,32 @@ __device__ __forceinline__ Range find_range(const DenseArgs& a, LineOf line_of, 
   return r;
 }
 
+// The same by one warp, for up to 32 sequences.
+template <class LineOf>
+__device__ __forceinline__ Range find_range_warp(const DenseArgs& a, LineOf line_of, int ctas, int cta, uint32_t* status) {
+  const int lane = threadIdx.x & 31;
+  int64_t sum = 0;
+  if (lane < a.n_seqs) {
+    const Line l = line_of(load_seq(a, lane, status));
+    sum = a.kv_heads * l.before(l.n);
+  }
+  int64_t inc = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t v = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += v;
+  }
+  Range r;
+  r.total = __shfl_sync(0xffffffffu, inc, 31);
+  r.active = active_ctas(r.total, ctas);
+  r.x0 = cta < r.active ? bound(r.total, r.active, cta) : r.total;
+  r.x1 = cta < r.active ? bound(r.total, r.active, cta + 1) : r.total;
+  const uint32_t here = __ballot_sync(0xffffffffu, r.x0 >= inc - sum && r.x0 < inc);
+  r.b0 = here ? __ffs(here) - 1 : 0;
+  r.base = __shfl_sync(0xffffffffu, inc - sum, r.b0);
+  return r;
+}
+
 // The items that a share touches, one after another.
 struct Cursor {
   Seq s;
@@ -184,8 +217,8 @@ __device__ __forceinline__ void seek(const DenseArgs& a, LineOf line_of, int64_t
   c.s = load_seq(a, b, nullptr);
   c.l = line_of(c.s);
   const int64_t one = c.l.before(c.l.n), rem = x - base;
-  c.h = (int)(rem / one);
-  const int64_t r = rem % one;
+  c.h = (int)quotient(rem, one);
+  const int64_t r = rem - c.h * one;
   int lo = 0, hi = c.l.n - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) / 2;
@@ -219,8 +252,8 @@ __device__ __forceinline__ bool next(const DenseArgs& a, LineOf line_of, Cursor&
 // Tiles [t0, t1) of an item's n that share [x0, x1) has.
 __device__ __forceinline__ void tiles_of(const Cursor& c, int64_t x0, int64_t x1, int n, int& t0, int& t1) {
   const int64_t lo = max(x0 - c.start, (int64_t)0), hi = min(x1 - c.start, c.weight);
-  t0 = (int)(lo * n / c.weight);
-  t1 = (int)(hi * n / c.weight);
+  t0 = (int)quotient(lo * n, c.weight);
+  t1 = (int)quotient(hi * n, c.weight);
 }
 
 // Bounded wait for a whole warp: every lane tests the barrier, else lane 0 polls and tells the others, so that
@@ -309,6 +342,21 @@ __device__ __forceinline__ void regs_inc() {
       : "memory")
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// Four lanes with four words each: lane i's word j becomes lane j's word i.
+__device__ __forceinline__ void transpose4(uint32_t& w0, uint32_t& w1, uint32_t& w2, uint32_t& w3, int lane) {
+  const bool odd = lane & 1, high = lane & 2;
+  const uint32_t a = __shfl_xor_sync(0xffffffffu, odd ? w0 : w1, 1), b = __shfl_xor_sync(0xffffffffu, odd ? w2 : w3, 1);
+  if (odd)
+    w0 = a, w2 = b;
+  else
+    w1 = a, w3 = b;
+  const uint32_t c = __shfl_xor_sync(0xffffffffu, high ? w0 : w2, 2), d = __shfl_xor_sync(0xffffffffu, high ? w1 : w3, 2);
+  if (high)
+    w0 = c, w1 = d;
+  else
+    w2 = c, w3 = d;
+}
+
 // Whether the phase is complete now, for the whole warp.
 __device__ __forceinline__ bool mbar_ready(uint64_t* bar, uint32_t parity) {
   return __all_sync(0xffffffffu, mbar_try_wait(bar, parity));
@@ -355,13 +403,16 @@ __device__ __forceinline__ void zero_row(uint8_t* tile, int from, int i) {
   }
 }
 
-// tanh.  Near 0, where 1 - 2 / (e^2u + 1) cancels, its series (to u^7: off by 2^-21 of itself at |u| = 1/4,
-// where the other form's rounding is 2^-22).
-__device__ __forceinline__ float tanh_of(float u) {
-  const float e = ex2(u * 2.8853900817779268f), u2 = u * u;
-  const float far = 1.0f - __fdividef(2.0f, e + 1.0f);
-  const float near = u * fmaf(u2, fmaf(u2, fmaf(u2, -17.0f / 315.0f, 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
-  return fabsf(u) < 0.25f ? near : far;
+// (y0, y1) = top tanh(x / cap) of two scores, c = 2 log2(e) / cap: top (1 - 2 / (2^(c x) + 1)), off by 2^-21 top (the
+// rounding near 1; relative to a score near 0 more, but it is an exponent).
+__device__ __forceinline__ void capped2(float& x0, float& x1, float c, float top) {
+  float e0, e1;
+  fma2(e0, e1, x0, x1, c, c, 0.f, 0.f);
+  e0 = ex2(e0), e1 = ex2(e1);
+  add2(e0, e1, e0, e1, 1.f, 1.f);
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(e0));
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(e1));
+  fma2(x0, x1, e0, e1, -2.f * top, -2.f * top, top, top);
 }
 
 }  // namespace work

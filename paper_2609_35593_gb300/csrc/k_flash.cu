@@ -11,8 +11,8 @@
 //               than 2^13 (what P's 16 bits and O's 32 hold easily): O in TMEM is rescaled seldom, and no maximum is
 //               formed otherwise.  Sums are float32, of the exponentials before they are rounded to 16 bits, one for
 //               each lane until the item ends.
-//   warp 0      item and tile producer: TMA of Q, K and V (128-byte swizzle), 5 stages of 32 KB, so that single
-//               tokens, which only stream the cache, keep over 100 KB per SM in flight
+//   warp 0      item and tile producer: TMA of Q, K and V (128-byte swizzle), 4 stages of 32 KB, so that single
+//               tokens, which only stream the cache, keep 100 KB per SM in flight, and Q of the next item
 //   warp 1      issuer of S = Q K^T (M128 N128 K64, both from shared memory)
 //   warps 2, 3  issuers of O += P V (M128 N64 K128, P from TMEM, V MN-major), a slot each.  S and P have columns of their
 //               own: S of the next tile runs while the exponentials of this one are formed.
@@ -34,7 +34,7 @@ using namespace work;
 
 namespace {
 
-constexpr int kThreads = 640, kStages = 5, kSlots = 2, kItems = 4, kKeys = 128;
+constexpr int kThreads = 640, kStages = 4, kSlots = 2, kItems = 4, kKeys = 128;
 constexpr int kProducer = 0, kIssueS = 1, kIssuePv = 2, kSoftmax = 4;  // warps: producer, issuers, softmax
 constexpr uint32_t kTileBytes = kKeys * 128;
 constexpr uint32_t kColSlot = 256, kColP = 128, kColO = 192;  // TMEM: per slot S, P, O
@@ -58,13 +58,13 @@ struct Item {
 };
 
 struct __align__(1024) Smem {
-  uint8_t Q[kSlots][128 * 128];
+  uint8_t Q[2][kSlots][128 * 128];  // of two items of each slot
   uint8_t K[kStages][kTileBytes];
   uint8_t V[kStages][kTileBytes];
   uint64_t kv_full[kStages], kv_empty[kStages];
-  float stat[2][kSlots][2][128];  // maxima and sums of the slots' rows, of two items
-  uint64_t stat_full[kSlots][4], other_full[4], other_empty[4];  // (of each quarter)
-  uint64_t q_full[kSlots], q_empty[kSlots], drain[1 + kSlots];
+  float other[2][128];                     // items of one part: slot 1's maxima and sums
+  uint64_t other_full[8], other_empty[8];  // (of each warp's rows)
+  uint64_t q_full[2][kSlots], q_empty[2][kSlots], drain[1 + kSlots];
   uint64_t s_full[kSlots], s_free[kSlots], p_full[kSlots], o_full[kSlots];
   uint64_t it_full[kItems], it_empty[kItems];
   int64_t scratch[34];
@@ -115,18 +115,19 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&S.kv_empty[s], 1 + kSlots);
     }
     for (int s = 0; s < kSlots; ++s) {
-      mbar_init(&S.q_full[s], 1);
-      mbar_init(&S.q_empty[s], 1);
+      for (int b = 0; b < 2; ++b) {
+        mbar_init(&S.q_full[b][s], 1);
+        mbar_init(&S.q_empty[b][s], 1);
+      }
       mbar_init(&S.s_full[s], 1);
       mbar_init(&S.s_free[s], 8);
       mbar_init(&S.p_full[s], 8);
       mbar_init(&S.o_full[s], 1);
-      for (int q = 0; q < 4; ++q) mbar_init(&S.stat_full[s][q], 2);
     }
     for (int i = 0; i < 1 + kSlots; ++i) mbar_init(&S.drain[i], 1);
-    for (int q = 0; q < 4; ++q) {
-      mbar_init(&S.other_full[q], 2);
-      mbar_init(&S.other_empty[q], 2);
+    for (int q = 0; q < 8; ++q) {
+      mbar_init(&S.other_full[q], 1);
+      mbar_init(&S.other_empty[q], 1);
     }
     for (int i = 0; i < kItems; ++i) {
       mbar_init(&S.it_full[i], 1);
@@ -145,7 +146,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tmem = S.tmem_base;
   rows::stream_acquire();
   auto line_of = [&](const Seq& s) { return row_line(a, s, kSlots * T, [&](int n) { return n > T ? 8 : 5; }); };
-  const Range range = find_range(a, line_of, gridDim.x, blockIdx.x, S.scratch, blockIdx.x == 0 ? a.status : nullptr);
+  Range range;  // (of the producer)
+  if (a.n_seqs > 32) range = find_range(a, line_of, gridDim.x, blockIdx.x, S.scratch, blockIdx.x == 0 ? a.status : nullptr);
 
   // 640 threads start with 96 registers each; the softmax warps, which hold a row's scores, get 104 of them
   // (512 x 104 + 128 x 64 <= 640 x 96).  A spilled register would go to L2: shared memory leaves next to no L1.
@@ -154,6 +156,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (warp == kProducer) {
       // =============================== producer ====================================
       int g = 0, pub = 0;
+      if (a.n_seqs <= 32)
+        range = find_range_warp(a, line_of, gridDim.x, blockIdx.x, blockIdx.x == 0 ? a.status : nullptr);
       uint32_t loads = 0;  // times that each slot's Q was loaded, a byte per slot
       bool failed = false;
       const int box = a.table ? min(kKeys, a.page & -a.page) : kKeys;  // the page's power of two
@@ -212,18 +216,18 @@ __global__ void __launch_bounds__(kThreads, 1)
           const uint32_t some = __ballot_sync(0xffffffffu, t0 + way < last);
           for (int s = 0; s < kSlots; ++s) {
             if (!(some >> s & 1)) continue;
-            const uint32_t times = loads >> (8 * s) & 0xff;
-            if (times > 0 && !wait(&S.q_empty[s], (times - 1) & 1, abort)) {
+            const uint32_t times = loads >> (8 * s) & 0xff, buf = times & 1;
+            if (times > 1 && !wait(&S.q_empty[buf][s], ((times >> 1) - 1) & 1, abort)) {
               failed = true;
               break;
             }
             if (lane == 0) {
-              mbar_arrive_expect_tx(&S.q_full[s], T * G * 128);
-              tma_load_4d(S.Q[s], &tmQ, &S.q_full[s], 0, 0, h, item.q0 + item.tok + s % parts * T);
+              mbar_arrive_expect_tx(&S.q_full[buf][s], T * G * 128);
+              tma_load_4d(S.Q[buf][s], &tmQ, &S.q_full[buf][s], 0, 0, h, item.q0 + item.tok + s % parts * T);
             }
             __syncwarp();
-            // counts to 255 and goes on at 128 + (same parity)
-            loads = (loads & ~(0xffu << (8 * s))) | ((times == 255 ? 128 : times + 1) << (8 * s));
+            // from 252 on at 248, which is the same modulo 4
+            loads = (loads & ~(0xffu << (8 * s))) | ((times == 251 ? 248 : times + 1) << (8 * s));
           }
           if (failed) break;
           // where this lane's box of a tile is: lanes 0..boxes-1 load K, the next ones V
@@ -293,7 +297,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int back = 1; back <= kStages && g - back >= 0; ++back)
           mbar_wait(&S.kv_full[(g - back) % kStages], ((g - back) / kStages) & 1, &no_abort, kDrainNs);
         for (int s = 0; s < kSlots; ++s)
-          if (loads >> (8 * s) & 0xff) mbar_wait(&S.q_full[s], ((loads >> (8 * s) & 0xff) - 1) & 1, &no_abort, kDrainNs);
+          for (int back = 1; back <= 2; ++back) {
+            const int times = (int)(loads >> (8 * s) & 0xff) - back;
+            if (times >= 0) mbar_wait(&S.q_full[times & 1][s], (times >> 1) & 1, &no_abort, kDrainNs);
+          }
       }
     } else {
       // ================================ MMA issuers ==================================
@@ -303,8 +310,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       constexpr uint64_t kStageUnits = kTileBytes >> 4, kQUnits = (128 * 128) >> 4;
       uint32_t phase = 0;
       if (warp == kIssueS) {
-        const uint64_t kd0 = sdesc_sw128(smem_u32(S.K[0])), qd0 = sdesc_sw128(smem_u32(S.Q[0]));
-        uint32_t s_phase[kSlots] = {1, 1}, q_phase[kSlots] = {0, 0};
+        const uint64_t kd0 = sdesc_sw128(smem_u32(S.K[0])), qd0 = sdesc_sw128(smem_u32(S.Q[0][0]));
+        uint32_t s_phase[kSlots] = {1, 1}, q_next[kSlots] = {0, 0}, buf[kSlots] = {0, 0};
         for (int st = 0; !failed;) {
           if (!wait(&S.kv_full[st], phase, abort)) {
             failed = true;
@@ -317,8 +324,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int s = 0; s < kSlots; ++s) {
             if (failed || !(flags & kHas << s)) continue;
             if (flags & kBegin << s) {
-              failed = !wait(&S.q_full[s], q_phase[s], abort);
-              q_phase[s] ^= 1;
+              buf[s] = q_next[s] & 1;
+              failed = !wait(&S.q_full[buf[s]][s], (q_next[s] >> 1) & 1, abort);
+              ++q_next[s];
             }
             // (the first time: at once)
             if (failed || !wait(&S.s_free[s], s_phase[s], abort)) {
@@ -328,11 +336,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             s_phase[s] ^= 1;
             tc_fence_after();
             if (leader) {
-              const uint64_t qd = qd0 + s * kQUnits;
+              const uint64_t qd = qd0 + (kSlots * buf[s] + s) * kQUnits;
 #pragma unroll
               for (int k = 0; k < 4; ++k) mma_bf16_ss(tmem + s * kColSlot, qd + 2 * k, kd + 2 * k, kQk, k > 0 ? 1u : 0u);
               mma_commit(&S.s_full[s]);
-              if (flags & kEnd << s) mma_commit(&S.q_empty[s]);
+              if (flags & kEnd << s) mma_commit(&S.q_empty[buf[s]][s]);
             }
             __syncwarp();
           }
@@ -387,9 +395,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ================================ softmax =====================================
     const int idx = warp - kSoftmax, slot = idx >> 3, half = idx >> 2 & 1, quarter = warp & 3;
     const int r0 = quarter * 32 + half * 16 + (lane >> 2), two = 2 * (lane & 3);  // this lane's rows: r0, r0 + 8; columns
-    const uint32_t tq = tmem + slot * kColSlot + ((uint32_t)(quarter * 32) << 16), tm = tq + ((uint32_t)(half * 16) << 16);
+    const uint32_t tm = tmem + slot * kColSlot + ((uint32_t)(quarter * 32 + half * 16) << 16);
     const float kScale = kGen ? 1.0f : kLog2e * 0.125f;
-    const float cap = a.cap, in = a.cap > 0.f ? 0.125f / a.cap : 0.125f * kLog2e, out = a.cap * kLog2e;
+    const float cap = a.cap, in = a.cap > 0.f ? 0.25f * kLog2e / a.cap : 0.125f * kLog2e, out = a.cap * kLog2e;
     // p = 2^(x kScale - m) of 64 columns, packed, and their sums
     auto exps = [&](const float (&x)[32], const float (&m)[2], uint32_t (&w)[16], float (&sum)[2]) {
       float s[2][2] = {{0.f, 0.f}, {0.f, 0.f}};
@@ -432,7 +440,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * alpha[e >> 1 & 1]);
       RESS_TMEM_ST16X64(tm + kColO, v);
     };
-    uint32_t c = 0, turn = 0, led = 0;  // tiles of this slot, items of one part, and items that it writes, so far
+    uint32_t c = 0, turn = 0;  // tiles of this slot, and items of one part, so far
     bool stop = false;
     for (int pub = 0; !stop; ++pub) {
       const int i = pub % kItems;
@@ -465,8 +473,13 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(v[e]);
         if (kGen) {
+          if (cap > 0.f) {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) x[e] = cap > 0.f ? out * tanh_of(x[e] * in) : x[e] * in;
+            for (int e = 0; e < 32; e += 2) capped2(x[e], x[e + 1], in, out);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) x[e] *= in;
+          }
           if (a.slopes) {
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
@@ -582,103 +595,102 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         tc_fence_after();
       }
-      // The rows' maxima and sums, for those that write them: from here on a lane has a whole row of a quarter, of which
-      // this warp writes half of the channels.  Slots with the same rows: the first adds the other's O, which it
-      // reads where it is, to its own, O = sum_s 2^(m_s - m) O_s.
-      float(*stat)[2][128] = S.stat[pub & 1];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         l[j] += __shfl_xor_sync(0xffffffffu, l[j], 1);
         l[j] += __shfl_xor_sync(0xffffffffu, l[j], 2);
-        if ((lane & 3) == 0) {
-          stat[slot][0][r0 + 8 * j] = l[j] == 0.f ? -INFINITY : m[j];
-          stat[slot][1][r0 + 8 * j] = l[j];
-        }
+        if (l[j] == 0.f) m[j] = -INFINITY;
       }
-      tc_fence_before();
-      __syncwarp();
+      // Slots with the same rows: slot 0 adds the other's O, which it reads where it is, to its own,
+      // O = sum_s 2^(m_s - m) O_s.
       if (way > 0) {
+        if ((lane & 3) == 0) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j) S.other[0][r0 + 8 * j] = m[j], S.other[1][r0 + 8 * j] = l[j];
+        }
+        tc_fence_before();
+        __syncwarp();
         if (lane == 0) {
-          mbar_arrive(&S.other_full[quarter]);
+          mbar_arrive(&S.other_full[idx & 7]);
           mbar_arrive(&S.it_empty[i]);
         }
         __syncwarp();
-        if (!wait(&S.other_empty[quarter], turn & 1, abort)) {
+        if (!wait(&S.other_empty[idx & 7], turn & 1, abort)) {
           give_up(S, a.status);
           break;
         }
       } else {
-        const int r = quarter * 32 + lane, head = item.h * G + r % G;
-        const bool exists = r / G < ntok;
-        if (lane == 0) mbar_arrive(&S.stat_full[slot][quarter]);
-        __syncwarp();
-        if (!wait(&S.stat_full[slot][quarter], led & 1, abort) ||
-            (ways > 1 && !wait(&S.other_full[quarter], turn & 1, abort))) {
-          give_up(S, a.status);
-          break;
-        }
-        tc_fence_after();
-        float mr = stat[slot][0][r], lr = stat[slot][1][r], by0 = 1.f, by1 = 0.f;
+        float by0[2] = {1.f, 1.f}, by1[2] = {0.f, 0.f};
         if (ways > 1) {
-          const float m1 = stat[slot + 1][0][r], l1 = stat[slot + 1][1][r], top = fmaxf(mr, m1);
-          by0 = mr == -INFINITY ? 0.f : ex2(mr - top);
-          by1 = m1 == -INFINITY ? 0.f : ex2(m1 - top);
-          mr = top;
-          lr = fmaf(lr, by0, l1 * by1);
-        }
-        const int64_t q = (int64_t)item.q0 + tok0 + r / G;
-        if (__any_sync(0xffffffffu, exists)) {
-          uint32_t o[32];
-          if (tiles > 0) {
-            RESS_TMEM_LD32(tq + kColO + 32 * half, o);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = 0u;
+          if (!wait(&S.other_full[idx & 7], turn & 1, abort)) {
+            give_up(S, a.status);
+            break;
           }
-          if (ways > 1) {
+          tc_fence_after();
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const float m1 = S.other[0][r0 + 8 * j], l1 = S.other[1][r0 + 8 * j], top = fmaxf(m[j], m1);
+            by0[j] = m[j] == -INFINITY ? 0.f : ex2(m[j] - top);
+            by1[j] = m1 == -INFINITY ? 0.f : ex2(m1 - top);
+            m[j] = top;
+            l[j] = fmaf(l[j], by0[j], l1 * by1[j]);
+          }
+        }
+        if (any) {
+          float o[32];
+          {
             uint32_t v[32];
 #pragma unroll
             for (int e = 0; e < 32; ++e) v[e] = 0u;
-            if (from + 1 < min(item.t1, item.n[part])) RESS_TMEM_LD32(tq + kColSlot + kColO + 32 * half, v);
+            if (tiles > 0) RESS_TMEM_LD16X64(tm + kColO, v);
 #pragma unroll
-            for (int e = 0; e < 32; ++e)
-              o[e] = __float_as_uint(fmaf(__uint_as_float(v[e]), by1, __uint_as_float(o[e]) * by0));
+            for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(v[e]) * by0[e >> 1 & 1];
           }
-          if (!exists) {
-          } else if (item.part >= 0) {
-            float* parts_at = a.part + item.part * kPartFloats;
-            float4* dst = reinterpret_cast<float4*>(parts_at + (part * 128 + r) * 64 + 32 * half);
+          if (ways > 1 && from + 1 < min(item.t1, item.n[part])) {
+            uint32_t v[32];
+            RESS_TMEM_LD16X64(tm + kColSlot + kColO, v);
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              dst[e] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]),
-                                   __uint_as_float(o[4 * e + 3]));
-            if (half == 0) {
-              parts_at[kRows * 64 + part * 128 + r] = mr;
-              parts_at[kRows * 65 + part * 128 + r] = lr;
+            for (int e = 0; e < 32; ++e) o[e] = fmaf(__uint_as_float(v[e]), by1[e >> 1 & 1], o[e]);
+          }
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int r = r0 + 8 * j, t = r / G, head = item.h * G + r % G;
+            const int64_t q = (int64_t)item.q0 + tok0 + t;
+            if (item.part >= 0) {
+              float* to = a.part + item.part * kPartFloats + part * 128 + r;
+              if (t < ntok) {
+                float2* dst = reinterpret_cast<float2*>(a.part + item.part * kPartFloats + (part * 128 + r) * 64 + two);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) dst[4 * e] = make_float2(o[4 * e + 2 * j], o[4 * e + 2 * j + 1]);
+                if ((lane & 3) == 0) to[kRows * 64] = m[j], to[kRows * 65] = l[j];
+              }
+            } else {
+              const float inv = l[j] == 0.f ? 0.f : 1.0f / l[j];
+              uint32_t w[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) w[e] = pack2<kF16>(o[4 * e + 2 * j] * inv, o[4 * e + 2 * j + 1] * inv);
+              // a row's four lanes: from two channels of every eight to eight of every 32
+              transpose4(w[0], w[1], w[2], w[3], lane);
+              transpose4(w[4], w[5], w[6], w[7], lane);
+              if (t < ntok) {
+                uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.o.data) + q * a.o.token_stride +
+                                                      head * a.o.head_stride) + (lane & 3);
+                dst[0] = make_uint4(w[0], w[1], w[2], w[3]);
+                dst[4] = make_uint4(w[4], w[5], w[6], w[7]);
+                if (a.lse && (lane & 3) == 0)
+                  a.lse[head * a.rows + q] = l[j] == 0.f ? -INFINITY : (m[j] + log2f(l[j])) * 0.6931471805599453f;
+              }
             }
-          } else {
-            const float inv = lr == 0.f ? 0.f : 1.0f / lr;
-            uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.o.data) + q * a.o.token_stride +
-                                                  head * a.o.head_stride + 32 * half);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              uint32_t w[4];
-#pragma unroll
-              for (int f = 0; f < 4; ++f)
-                w[f] = pack2<kF16>(__uint_as_float(o[8 * e + 2 * f]) * inv, __uint_as_float(o[8 * e + 2 * f + 1]) * inv);
-              dst[e] = make_uint4(w[0], w[1], w[2], w[3]);
-            }
-            if (half == 0 && a.lse) a.lse[head * a.rows + q] = lr == 0.f ? -INFINITY : (mr + log2f(lr)) * 0.6931471805599453f;
+            __syncwarp();
           }
         }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
-          if (ways > 1) mbar_arrive(&S.other_empty[quarter]);
+          if (ways > 1) mbar_arrive(&S.other_empty[idx & 7]);
           mbar_arrive(&S.it_empty[i]);
         }
         __syncwarp();
-        ++led;
       }
       turn += ways > 1;
     }
@@ -779,7 +791,7 @@ static bool encode(void* map, const void* base, int type, const cuuint64_t (&dim
   return fn && fn(static_cast<CUtensorMap*>(map),
                   type == RESS_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4,
                   const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 

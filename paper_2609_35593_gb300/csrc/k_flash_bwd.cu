@@ -457,7 +457,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int tid = (warp - 2 - 4 * group) * 32 + lane;  // 0..127, for the zeroing
     const uint32_t tm = tmem + ((uint32_t)(quarter * 32) << 16), tS = tm + 128 * group, tP = tS + kColP;
     const float kScale = kLog2e * 0.125f;
-    const float cap = a.cap, in = a.cap > 0.f ? 0.125f / a.cap : 0.125f * kLog2e, out = a.cap * kLog2e;
+    const float cap = a.cap, in = a.cap > 0.f ? 0.25f * kLog2e / a.cap : 0.125f * kLog2e, out = a.cap * kLog2e;
+    const float back = a.cap > 0.f ? 1.0f / out : 0.f;
     const float scale = kF16 ? grad_scale(a.big, a.n_big) : 1.f, f = kF16 ? scale * exp2f(-kPScale) : 1.f;
     const float undo = 0.125f / scale;
     int it = 0;
@@ -518,9 +519,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             float c0 = 1.f, c1 = 1.f;
             if (kGen) {
               if (cap > 0.f) {
-                const float u0 = tanh_of(x0 * in), u1 = tanh_of(x1 * in);
-                c0 = fmaf(-u0, u0, 1.f), c1 = fmaf(-u1, u1, 1.f);
-                x0 = out * u0, x1 = out * u1;
+                capped2(x0, x1, in, out);
+                float u0, u1;
+                mul2(u0, u1, x0, x1, back, back);
+                fma2(c0, c1, -u0, -u1, u0, u1, 1.f, 1.f);
               } else {
                 x0 *= in, x1 *= in;
               }
