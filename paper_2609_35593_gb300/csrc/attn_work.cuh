@@ -5,8 +5,9 @@
 // (of all the heads of Q that share it), or in the gradient of K and V a range of keys.  Lengths are device
 // data, so the host knows only the totals: every CTA adds up all sequences' work itself (a few hundred
 // instructions, sequences over its threads) and takes share c of C of it, wherever that begins and ends.
-// An item that several CTAs have shares of leaves partial results in the workspace, two slots per CTA, which
-// a second kernel adds up in the order of the shares: no atomics, the same bits for the same inputs.
+// An item that several CTAs have shares of leaves partial results in the workspace, two slots per CTA, with a note
+// of what they are of; a second kernel adds them up in the order of the shares: no atomics, the same bits for the
+// same inputs.  (It looked for the shares itself at first, as the CTAs do, and took 20 to 40 us.)
 // With whole items instead, 176 items of 172 tiles on 152 SMs (one image over the keys of 32) would take two
 // rounds where 1.16 do.
 //
@@ -21,7 +22,7 @@ namespace ress {
 namespace work {
 using namespace ptx;
 
-constexpr int kMaxCtas = 192;            // most CTAs that share a call's work (one per SM)
+constexpr int kMaxCtas = kDenseMaxCtas;
 constexpr int kTile = 64;                // columns of a tile
 constexpr int64_t kOver = 8 * 2 * kTile; // an item's loads and epilogue, as work: two tiles
 constexpr int64_t kLeast = 8 * 4 * kTile;  // least share of a CTA: four tiles
@@ -254,6 +255,15 @@ __device__ __forceinline__ void tiles_of(const Cursor& c, int64_t x0, int64_t x1
   const int64_t lo = max(x0 - c.start, (int64_t)0), hi = min(x1 - c.start, c.weight);
   t0 = (int)quotient(lo * n, c.weight);
   t1 = (int)quotient(hi * n, c.weight);
+}
+
+// Slots of the workspace: a CTA's share of an item that began before its own shares, and of one that it is the first of.
+__device__ __forceinline__ int share_slot(const Cursor& c, int64_t x0) { return 2 * (int)blockIdx.x + (c.start >= x0 ? 1 : 0); }
+// The share after `slot` of the same item (shares without tiles have no note).
+__device__ __forceinline__ int next_share(const DenseArgs& a, int slot, int ctas) {
+  for (int c = slot / 2 + 1; c < ctas; ++c)
+    if (a.share[2 * c].n >= 0) return 2 * c;
+  return -1;  // (does not happen: the last share of an item ends it)
 }
 
 // Bounded wait for a whole warp: every lane tests the barrier, else lane 0 polls and tells the others, so that

@@ -162,7 +162,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool failed = false;
       const int box = a.table ? min(kKeys, a.page & -a.page) : kKeys;  // the page's power of two
       const int boxes = kKeys / box;
-        // The next item that this share has tiles of, to S.next (h -1: none left).  One lane looks for it, in shared
+        if (lane == 0) a.share[2 * blockIdx.x].n = a.share[2 * blockIdx.x + 1].n = -1;
+      // The next item that this share has tiles of, to S.next (h -1: none left).  One lane looks for it, in shared
       // memory: the sequences' arithmetic in 64 bits would otherwise take the registers of the tile loop.
       auto advance = [&](bool first) {
         __syncwarp();
@@ -182,7 +183,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int s = 0; s < kSlots; ++s) item.n[s] = part_tiles(a, c.s, tok, s, T);
             item.parts = min(kSlots, (c.s.nq - tok + T - 1) / T);
             item.ways = ways_of(item.parts);
-            item.part = t0 == 0 && t1 == n ? -1 : 2 * (int)blockIdx.x + (c.start >= range.x0 ? 1 : 0);
+            item.part = t0 == 0 && t1 == n ? -1 : share_slot(c, range.x0);
+            if (item.part >= 0)
+              a.share[item.part] = DenseShare{t0, t1, n, c.h, c.s.q0 + tok, min(c.s.nq - tok, kSlots * T), {}};
             break;
           }
         }
@@ -706,63 +709,39 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // ------------------------------------------------------------------------------------
-// Items that several CTAs had shares of: with m the largest of their maxima,
-// O = sum_s 2^(m_s - m) O_s / l and l = sum_s 2^(m_s - m) l_s.  Block (c, y) takes the item that the end of share
-// c is inside of, if no earlier share ends there: 32 of its rows, half a warp per row and step.
+// Items that several CTAs had shares of: with m the largest of their maxima, O = sum_s 2^(m_s - m) O_s / l and
+// l = sum_s 2^(m_s - m) l_s.  Block (s, y) takes the item that slot s has the first share of, if any: 32 of its rows,
+// half a warp per row and step.
 // ------------------------------------------------------------------------------------
 template <bool kF16>
 __global__ void __launch_bounds__(256) k_flash_join(const __grid_constant__ DenseArgs a, int ctas) {
-  __shared__ int64_t scratch[34];
   rows::stream_acquire();
-  const int G = a.group, T = 128 / G;
-  auto line_of = [&](const Seq& s) { return row_line(a, s, kSlots * T, [&](int n) { return n > T ? 8 : 5; }); };
-  const int first = blockIdx.x;
-  const Range r = find_range(a, line_of, ctas, first + 1, scratch, nullptr);
-  if (first + 1 >= r.active || r.total == 0) return;
-  Cursor c;
-  seek(a, line_of, r.x0, r.b0, r.base, c);
-  const int64_t end = c.start + c.weight;
-  if (c.start == r.x0 || (first > 0 && bound(r.total, r.active, first) > c.start)) return;
-  const int tok0 = c.j * kSlots * T;
-  const int n = item_tiles(a, c.s, tok0, T);
-  if (n == 0) return;
-  int parts = 1;  // shares first .. first + parts - 1 touch the item
-  while (first + parts < r.active && bound(r.total, r.active, first + parts) < end) ++parts;
-  auto share = [&](int k, int& t0, int& t1) {
-    tiles_of(c, bound(r.total, r.active, first + k), bound(r.total, r.active, first + k + 1), n, t0, t1);
-  };
-  auto slot_of = [&](int k) -> const float* {
-    return a.part + (2 * (int64_t)(first + k) + (c.start >= bound(r.total, r.active, first + k) ? 1 : 0)) * kPartFloats;
-  };
-  for (int k = 0; k < parts; ++k) {
-    int t0, t1;
-    share(k, t0, t1);
-    if (t0 == 0 && t1 == n) return;  // one of them has it all
-  }
-  const int half = threadIdx.x >> 4, sub = threadIdx.x & 15;
-  for (int i = half; i < 32; i += 16) {
-    const int row = blockIdx.y * 32 + i, slot = row >> 7, rr = row & 127;
-    if (rr / G >= part_tokens(c.s.nq, tok0, slot, T)) continue;
+  const DenseShare item = a.share[blockIdx.x];
+  if (item.n < 0 || item.t0 != 0) return;
+  const int G = a.group, T = 128 / G, sub = threadIdx.x & 15;
+  for (int i = threadIdx.x >> 4; i < 32; i += 16) {
+    const int row = blockIdx.y * 32 + i, tok = (row >> 7) * T + (row & 127) / G;
+    if ((row & 127) >= T * G || tok >= item.count) continue;
     float m = -INFINITY, l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k = 0; k < parts; ++k) {
-      int t0, t1;
-      share(k, t0, t1);
-      if (t0 == t1) continue;
-      const float* p = slot_of(k);
+    for (int s = blockIdx.x, t1 = item.t1;;) {
+      const float* p = a.part + s * kPartFloats;
       const float mk = p[kRows * 64 + row];
-      if (mk == -INFINITY) continue;
-      const float4 v = reinterpret_cast<const float4*>(p + row * 64)[sub];
-      const float lk = p[kRows * 65 + row], top = fmaxf(m, mk);
-      const float wa = m == -INFINITY ? 0.f : ex2(m - top), wb = ex2(mk - top);
-      m = top;
-      l = fmaf(l, wa, lk * wb);
-      o.x = fmaf(o.x, wa, v.x * wb), o.y = fmaf(o.y, wa, v.y * wb);
-      o.z = fmaf(o.z, wa, v.z * wb), o.w = fmaf(o.w, wa, v.w * wb);
+      if (mk != -INFINITY) {
+        const float4 v = reinterpret_cast<const float4*>(p + row * 64)[sub];
+        const float lk = p[kRows * 65 + row], top = fmaxf(m, mk);
+        const float wa = m == -INFINITY ? 0.f : ex2(m - top), wb = ex2(mk - top);
+        m = top;
+        l = fmaf(l, wa, lk * wb);
+        o.x = fmaf(o.x, wa, v.x * wb), o.y = fmaf(o.y, wa, v.y * wb);
+        o.z = fmaf(o.z, wa, v.z * wb), o.w = fmaf(o.w, wa, v.w * wb);
+      }
+      if (t1 >= item.n || (s = next_share(a, s, ctas)) < 0) break;
+      t1 = a.share[s].t1;
     }
     const float inv = l == 0.f ? 0.f : 1.0f / l;
-    const int64_t q = (int64_t)c.s.q0 + tok0 + slot * T + rr / G;
-    const int head = c.h * G + rr % G;
+    const int64_t q = (int64_t)item.first + tok;
+    const int head = item.head * G + (row & 127) % G;
     uint2* dst = reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.o.data) + q * a.o.token_stride + head * a.o.head_stride);
     dst[sub] = make_uint2(pack2<kF16>(o.x * inv, o.y * inv), pack2<kF16>(o.z * inv, o.w * inv));
     if (a.lse && sub == 0) a.lse[head * a.rows + q] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
@@ -839,7 +818,7 @@ cudaError_t launch_flash(const DenseArgs& a, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   if ((e = launch_pdl(kern, ctas, kThreads, smem, st, true, tq, tk, tv, a)) != cudaSuccess) return e;
   if (ctas == 1) return e;
-  return launch_pdl(f16 ? k_flash_join<true> : k_flash_join<false>, dim3(ctas - 1, kRows / 32), 256, 0, st, true, a, ctas);
+  return launch_pdl(f16 ? k_flash_join<true> : k_flash_join<false>, dim3(2 * ctas, kRows / 32), 256, 0, st, true, a, ctas);
 }
 
 }  // namespace ress

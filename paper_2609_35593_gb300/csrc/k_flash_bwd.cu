@@ -229,6 +229,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     int g = 0, it = 0, pub = 0;
     bool failed = false, a_loaded = false;
     const float f = kF16 ? grad_scale(a.big, a.n_big) * exp2f(-kPScale) : 1.f;
+    if (lane == 0) a.share[2 * blockIdx.x].n = a.share[2 * blockIdx.x + 1].n = -1;
+    __syncwarp();
     auto publish = [&](const Item* item) -> bool {
       const int i = pub % kItems, u = pub / kItems;
       if (u > 0 && !wait(&S.it_empty[i], (u - 1) & 1, abort)) return false;
@@ -253,8 +255,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int n = item_tiles<kKeys>(a, c.s, item.at, T, item.from);
         tiles_of(c, range.x0, range.x1, n, item.t0, item.t1);
         item.g0 = g;
-        item.part = item.t0 == 0 && item.t1 == n ? -1 : 2 * (int)blockIdx.x + (c.start >= range.x0 ? 1 : 0);
+        item.part = item.t0 == 0 && item.t1 == n ? -1 : share_slot(c, range.x0);
         if (item.t0 == item.t1 && (n > 0 || c.start < range.x0)) continue;
+        if (item.part >= 0 && lane == 0)
+          a.share[item.part] = DenseShare{item.t0, item.t1, n, c.h, (kKeys ? c.s.k0 : c.s.q0) + item.at,
+                                          min((kKeys ? c.s.nk : c.s.nq) - item.at, kKeys ? 128 : T), {}};
         if (!publish(&item)) {
           failed = true;
           break;
@@ -626,52 +631,28 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // Gradients of items that several CTAs had shares of: the shares' sums, in their order.  Blocks as in k_flash_join: 32
-// rows each, half a warp per row.
+// rows each (of dK, then of dV), half a warp per row.
 template <bool kF16, bool kKeys>
 __global__ void __launch_bounds__(256) k_flash_bwd_join(const __grid_constant__ DenseArgs a, int ctas) {
-  __shared__ int64_t scratch[34];
   rows::stream_acquire();
-  const int G = a.group, T = 128 / G;
-  const Lines<kKeys> line_of{a, T};
-  const int first = blockIdx.x;
-  const Range r = find_range(a, line_of, ctas, first + 1, scratch, nullptr);
-  if (first + 1 >= r.active || r.total == 0) return;
-  Cursor c;
-  seek(a, line_of, r.x0, r.b0, r.base, c);
-  const int64_t end = c.start + c.weight;
-  if (c.start == r.x0 || (first > 0 && bound(r.total, r.active, first) > c.start)) return;
-  const int at = c.j * (kKeys ? 128 : T);
-  int from;
-  const int n = item_tiles<kKeys>(a, c.s, at, T, from);
-  if (n == 0) return;
-  int parts = 1;
-  while (first + parts < r.active && bound(r.total, r.active, first + parts) < end) ++parts;
-  auto share = [&](int k, int& t0, int& t1) {
-    tiles_of(c, bound(r.total, r.active, first + k), bound(r.total, r.active, first + k + 1), n, t0, t1);
-  };
-  for (int k = 0; k < parts; ++k) {
-    int t0, t1;
-    share(k, t0, t1);
-    if (t0 == 0 && t1 == n) return;  // one of them has it all
-  }
+  const DenseShare item = a.share[blockIdx.x];
+  if (item.n < 0 || item.t0 != 0) return;
+  const int G = a.group, T = 128 / G, sub = threadIdx.x & 15;
   const float undo = 0.125f / (kF16 ? grad_scale(a.big, a.n_big) : 1.f);
-  const int half = threadIdx.x >> 4, sub = threadIdx.x & 15;
-  for (int i = half; i < 32; i += 16) {
-    const int row = blockIdx.y * 32 + i, which = row >> 7, rr = row & 127;  // rows of dK, then of dV
-    if (kKeys ? at + rr >= c.s.nk : rr / G >= T || at + rr / G >= c.s.nq) continue;
+  for (int i = threadIdx.x >> 4; i < 32; i += 16) {
+    const int row = blockIdx.y * 32 + i, which = row >> 7, rr = row & 127;
+    if (kKeys ? rr >= item.count : rr >= T * G || rr / G >= item.count) continue;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k = 0; k < parts; ++k) {
-      int t0, t1;
-      share(k, t0, t1);
-      if (t0 == t1) continue;
-      const int64_t slot = 2 * (int64_t)(first + k) + (c.start >= bound(r.total, r.active, first + k) ? 1 : 0);
-      const float4 v = reinterpret_cast<const float4*>(a.part + slot * kPartFloats + row * 64)[sub];
+    for (int s = blockIdx.x, t1 = item.t1;;) {
+      const float4 v = reinterpret_cast<const float4*>(a.part + s * kPartFloats + row * 64)[sub];
       o.x += v.x, o.y += v.y, o.z += v.z, o.w += v.w;
+      if (t1 >= item.n || (s = next_share(a, s, ctas)) < 0) break;
+      t1 = a.share[s].t1;
     }
     const float by = kKeys && which ? (kF16 ? exp2f(-kPScale) : 1.f) : undo;
     const ress_heads& d = kKeys ? (which ? a.dv : a.dk) : a.dq;
-    const int64_t token = kKeys ? (int64_t)c.s.k0 + at + rr : (int64_t)c.s.q0 + at + rr / G;
-    const int head = kKeys ? c.h : c.h * G + rr % G;
+    const int64_t token = (int64_t)item.first + (kKeys ? rr : rr / G);
+    const int head = kKeys ? item.head : item.head * G + rr % G;
     reinterpret_cast<uint2*>(static_cast<uint16_t*>(d.data) + token * d.token_stride + head * d.head_stride)[sub] =
         make_uint2(pack2<kF16>(o.x * by, o.y * by), pack2<kF16>(o.z * by, o.w * by));
   }
@@ -684,7 +665,7 @@ static cudaError_t launch_pass(const DenseArgs& a, const CUtensorMap (&m)[4], in
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   if ((e = launch_pdl(kern, ctas, kThreads, smem, st, true, m[0], m[1], m[2], m[3], a)) != cudaSuccess || ctas == 1) return e;
-  return launch_pdl(k_flash_bwd_join<kF16, kKeys>, dim3(ctas - 1, kKeys ? 8 : 4), 256, 0, st, true, a, ctas);
+  return launch_pdl(k_flash_bwd_join<kF16, kKeys>, dim3(2 * ctas, kKeys ? 8 : 4), 256, 0, st, true, a, ctas);
 }
 
 template <bool kF16>

@@ -968,8 +968,10 @@ int check_tiles(const ress_heads& h, int64_t tokens, int heads, bool output, con
   return RESS_OK;
 }
 
+constexpr int64_t kShareBytes = 2 * ress::kDenseMaxCtas * (int64_t)sizeof(ress::DenseShare);
+
 size_t attn_bytes(int64_t rows, int32_t q_heads, int32_t backward) {
-  const int64_t parts = 256 + ress::align256((int64_t)ress::dense_part_bytes());
+  const int64_t parts = 256 + kShareBytes + ress::align256((int64_t)ress::dense_part_bytes());
   return (size_t)(backward ? parts + ress::align256(rows * q_heads * 8) + ress::kBigParts * 4 : parts);
 }
 
@@ -1040,6 +1042,8 @@ int attn_checks(const ress_attn_args* a, const ress_pages* pg, bool backward, vo
   out->q = a->q, out->k = a->k, out->v = a->v, out->o = a->o, out->lse = a->lse;
   out->status = static_cast<uint32_t*>(ws);
   char* w = static_cast<char*>(ws) + 256;
+  out->share = reinterpret_cast<ress::DenseShare*>(w);
+  w += kShareBytes;
   out->part = reinterpret_cast<float*>(w);
   out->stat = reinterpret_cast<float2*>(w += ress::align256((int64_t)ress::dense_part_bytes()));
   out->big = reinterpret_cast<float*>(w + ress::align256(a->rows * a->q_heads * 8));

@@ -342,10 +342,18 @@ struct DenseArgs {
   float* lse;
   uint32_t* status;
   float* part;   // partial results of items that several CTAs share
+  struct DenseShare* share;  // what each slot of partial results is of
   float2* stat;  // gradient: per row of each head of K, log2 of its sum and o . do
   float* big;    // gradient in f16: largest |do| of each of n_big parts of the rows
   int n_big;
 };
+// A CTA's share of an item that others have shares of too: tiles t0..t1-1 of n (n -1: none).
+struct DenseShare {
+  int32_t t0, t1, n, head;  // head of K
+  int32_t first, count;     // first row or key of the item among all, and how many (in tokens)
+  int32_t pad[2];
+};
+constexpr int kDenseMaxCtas = 192;  // most CTAs that share a call's work (one per SM)
 size_t dense_part_bytes();
 constexpr int kBigParts = 1024;
 cudaError_t launch_flash(const DenseArgs& a, cudaStream_t st);
