@@ -291,6 +291,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         __syncwarp();
         if (lane == 0) S.next.h = -1;
+        __syncwarp();
         if (!failed && !publish()) failed = true;
       }
       if (failed && lane == 0) {

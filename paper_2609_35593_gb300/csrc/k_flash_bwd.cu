@@ -5,15 +5,16 @@
 // streaming past them (dQ: three products a tile), and items of 128 keys with the rows streaming past (dK, dV:
 // four).  One pass with five products would add dQ up from different CTAs: with atomics the bits change from run to
 // run, in order the CTAs wait for one another.  The second pass works on the transposed scores
-// S^T = K Q^T, so that in both what the element-wise warps write (P, dS; 16 bits, in TMEM over the scores they
-// came from) is the A operand of the next product: nothing of the size of the scores touches shared memory.
-// Heads of Q that share a head of K and V are rows of the same item (or columns of the same tile), which adds
-// up their gradients.
+// S^T = K Q^T, so that in both what the element-wise warps write (P, dS; 16 bits, in TMEM) is the A operand of the
+// next product: nothing of the size of the scores touches shared memory.  Heads of Q that share a head of K and V are
+// rows of the same item (or columns of the same tile), which adds up their gradients.
 //
-// Roles (320 threads, one CTA per SM): producer, MMA issuer, and two groups of four warps that take every other
-// tile: S and dP of the next tile are computed while a group works on the last one.  TMEM: S and dP of two tiles (256
-// columns), two accumulators, two A operands (copied there once per item).  Shares of the work, partial results and
-// waits are those of k_flash.cu (attn_work.cuh).
+// Roles (640 threads, one CTA per SM): warp 0 producer, warp 1 issuer of S and dP (M128 N128 K64, operands in shared
+// memory, each as soon as the last one's values are in registers), warps 2 and 3 issuers of the sums over P and over dS, warps 4-19 element-wise: 16 rows x 64 columns of a tile
+// of 128 x 128 each.  S and dP (256 columns of TMEM) are free for the next tile as soon as they are in registers, P and
+// dS (128) have columns of their own, so the products of the next tile run meanwhile; two accumulators (128).  With
+// eight element-wise warps on tiles of 64 columns and one issuer a tile of 128 x 64 took 1,700 cycles, its four
+// products 512 (8 images at once: 2,200 us).  Shares of the work, partial results and waits are those of k_flash.cu.
 //
 // In f16, P is kept times 2^8 and dS times a power of two that brings the largest |dO| to 1..2: probabilities of rows on
 // thousands of keys are below f16's 2^-14, and so may gradients be.  dP is at most 64 max|dO| max|V|, so dS stays
@@ -28,10 +29,10 @@ using namespace work;
 
 namespace {
 
-constexpr int kThreads = 320, kStages = 6, kItems = 4;
-static_assert(kStages % 2 == 0, "a stage is always the same group's");
-constexpr uint32_t kTileBytes = kTile * 128;
-constexpr uint32_t kColP = 64, kColAcc1 = 256, kColAcc2 = 320, kColA1 = 384, kColA2 = 416;  // buffer b: 128 b
+constexpr int kThreads = 640, kStages = 4, kItems = 4, kCols = 128;
+constexpr int kProducer = 0, kIssueS = 1, kIssueP = 2, kIssueDs = 3, kElem = 4;  // warps
+constexpr uint32_t kTileBytes = kCols * 128;
+constexpr uint32_t kColDp = 128, kColP = 256, kColDs = 320, kColAcc1 = 384, kColAcc2 = 448;  // TMEM; S at 0
 constexpr int kFirst = 1, kLast = 2, kTerm = 4, kMask = 8;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int64_t kPartFloats = 256 * 66;  // as k_flash.cu's: 128 rows of one or two gradients
@@ -39,29 +40,30 @@ constexpr float kPScale = 8.0f;            // log2 of P's scale in f16
 
 struct Item {
   int q0, k0, nq, nk, d, p;
-  int h, at;        // head of K; first token or key
+  int h, at;        // head of K (-1: no more items); first token or key
   int from, t0, t1, g0;  // first row of the first tile (dK, dV); tiles; number of the first among all of the CTA's
   int part;
 };
 
-// What the columns of a tile are, where they are rows of Q (two of them next to each other are read together).
+// What the columns of a tile are, where they are rows of Q (two next to each other are read together).
 struct __align__(16) Cols {
-  float lse[kTile], delta[kTile];  // -log2 of the sums, -delta (times the scale)
-  int lim[kTile];                  // keys seen
-  float pos[kTile], slope[kTile];
+  float lse[kCols], delta[kCols];  // -log2 of the sums, -delta (times the scale)
+  int lim[kCols];                  // keys seen
+  float pos[kCols], slope[kCols];
 };
 
 struct __align__(1024) Smem {
-  uint8_t A1[128 * 128], A2[128 * 128];
+  uint8_t A[2][2][128 * 128];  // of two items
   uint8_t B1[kStages][kTileBytes];
   uint8_t B2[kStages][kTileBytes];
   Cols cols[kStages];
   uint64_t kv_full[kStages], kv_empty[kStages];
-  uint64_t q_full, q_empty, drain;
-  uint64_t s_full[2], p_full[2], acc_full, acc_empty;
+  uint64_t a_full[2], a_empty[2], drain[3];
+  uint64_t s_full, s_free, dp_full, dp_free, p_full, p_done, acc_full, acc_empty;
   uint64_t it_full[kItems], it_empty[kItems];
   int64_t scratch[34];
-  Item item[kItems];
+  Item item[kItems], next;
+  Cursor cursor;
   int flags[kStages];
   uint32_t tmem_base;
   int abort;
@@ -102,24 +104,9 @@ __device__ __forceinline__ int item_tiles(const DenseArgs& a, const Seq& s, int 
   from = 0;
   if (kKeys) {
     from = first_row(a, s, at);
-    const int per = kTile / a.group;
-    return (s.nq - from + per - 1) / per;
+    return (s.nq - from + T - 1) / T;
   }
-  return (max(0, row_limit(a, s, s.d + min(s.nq, at + T) - 1)) + kTile - 1) / kTile;
-}
-
-// 64 (or 32) channels of one row, scaled and rounded.
-template <bool kF16, int N>
-__device__ __forceinline__ void store_row(void* dst, const uint32_t (&o)[N], float by) {
-  uint4* p = static_cast<uint4*>(dst);
-#pragma unroll
-  for (int k = 0; k < N / 8; ++k) {
-    uint32_t w[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      w[e] = pack2<kF16>(__uint_as_float(o[8 * k + 2 * e]) * by, __uint_as_float(o[8 * k + 2 * e + 1]) * by);
-    p[k] = make_uint4(w[0], w[1], w[2], w[3]);
-  }
+  return (max(0, row_limit(a, s, s.d + min(s.nq, at + T) - 1)) + kCols - 1) / kCols;
 }
 
 }  // namespace
@@ -183,25 +170,30 @@ __global__ void __launch_bounds__(kThreads, 1)
   Smem& S = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   volatile int* abort = &S.abort;
-  const int G = a.group, T = 128 / G, per = kTile / G;
+  const int G = a.group, T = 128 / G;
+  constexpr int kSums = kKeys ? 2 : 1;  // issuers of sums
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
       mbar_init(&S.kv_full[s], 1);
-      mbar_init(&S.kv_empty[s], 1);
+      mbar_init(&S.kv_empty[s], 1 + kSums);
     }
-    mbar_init(&S.q_full, 1);
-    mbar_init(&S.q_empty, 1);
-    mbar_init(&S.drain, 1);
     for (int b = 0; b < 2; ++b) {
-      mbar_init(&S.s_full[b], 1);
-      mbar_init(&S.p_full[b], 4);
+      mbar_init(&S.a_full[b], 1);
+      mbar_init(&S.a_empty[b], 1);
     }
-    mbar_init(&S.acc_full, 1);
-    mbar_init(&S.acc_empty, 8);
+    for (int i = 0; i < 3; ++i) mbar_init(&S.drain[i], 1);
+    mbar_init(&S.s_full, 1);
+    mbar_init(&S.s_free, 16);
+    mbar_init(&S.dp_full, 1);
+    mbar_init(&S.dp_free, 16);
+    mbar_init(&S.p_full, 16);
+    mbar_init(&S.p_done, kSums);
+    mbar_init(&S.acc_full, kSums);
+    mbar_init(&S.acc_empty, 16);
     for (int i = 0; i < kItems; ++i) {
       mbar_init(&S.it_full[i], 1);
-      mbar_init(&S.it_empty[i], 8);
+      mbar_init(&S.it_empty[i], 16);
     }
     S.abort = 0;
     fence_barrier_init();
@@ -210,263 +202,294 @@ __global__ void __launch_bounds__(kThreads, 1)
     prefetch_tensormap(&tmB1);
     prefetch_tensormap(&tmB2);
   }
-  if (kKeys && per * G < kTile) {  // rows of a tile that no box reaches are summed over, times 0
+  if (kKeys && T * G < kCols) {  // rows of a tile that no box reaches are summed over, times 0
     for (int f = threadIdx.x; f < (int)(2 * kStages * kTileBytes / 16); f += kThreads)
       reinterpret_cast<uint4*>(S.B1)[f] = make_uint4(0u, 0u, 0u, 0u);
     fence_proxy_async_smem();
   }
-  if (warp == 1) tmem_alloc(&S.tmem_base, 512);
+  if (warp == kIssueS) tmem_alloc(&S.tmem_base, 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = S.tmem_base;
   rows::stream_acquire();
   const Lines<kKeys> line_of{a, T};
-  const Range range = find_range(a, line_of, gridDim.x, blockIdx.x, S.scratch, blockIdx.x == 0 ? a.status : nullptr);
+  Range range;  // (of the producer)
+  if (a.n_seqs > 32) range = find_range(a, line_of, gridDim.x, blockIdx.x, S.scratch, blockIdx.x == 0 ? a.status : nullptr);
 
-  if (warp == 0) {
-    // =============================== producer ====================================
-    int g = 0, it = 0, pub = 0;
-    bool failed = false, a_loaded = false;
-    const float f = kF16 ? grad_scale(a.big, a.n_big) * exp2f(-kPScale) : 1.f;
-    if (lane == 0) a.share[2 * blockIdx.x].n = a.share[2 * blockIdx.x + 1].n = -1;
-    __syncwarp();
-    auto publish = [&](const Item* item) -> bool {
-      const int i = pub % kItems, u = pub / kItems;
-      if (u > 0 && !wait(&S.it_empty[i], (u - 1) & 1, abort)) return false;
-      if (lane == 0) {
-        if (item)
-          S.item[i] = *item;
-        else
-          S.item[i].h = -1;
-        mbar_arrive(&S.it_full[i]);
-      }
-      __syncwarp();
-      ++pub;
-      return true;
-    };
-    if (range.x0 < range.x1) {
-      Cursor c;
-      seek(a, line_of, range.x0, range.b0, range.base, c);
-      do {
-        Item item;
-        item.q0 = c.s.q0, item.k0 = c.s.k0, item.nq = c.s.nq, item.nk = c.s.nk, item.d = c.s.d, item.p = c.s.p;
-        item.h = c.h, item.at = c.j * (kKeys ? 128 : T);
-        const int n = item_tiles<kKeys>(a, c.s, item.at, T, item.from);
-        tiles_of(c, range.x0, range.x1, n, item.t0, item.t1);
-        item.g0 = g;
-        item.part = item.t0 == 0 && item.t1 == n ? -1 : share_slot(c, range.x0);
-        if (item.t0 == item.t1 && (n > 0 || c.start < range.x0)) continue;
-        if (item.part >= 0 && lane == 0)
-          a.share[item.part] = DenseShare{item.t0, item.t1, n, c.h, (kKeys ? c.s.k0 : c.s.q0) + item.at,
-                                          min((kKeys ? c.s.nk : c.s.nq) - item.at, kKeys ? 128 : T), {}};
-        if (!publish(&item)) {
-          failed = true;
-          break;
-        }
-        if (n == 0) continue;
-        if (it > 0 && !wait(&S.q_empty, (it - 1) & 1, abort)) {
-          failed = true;
-          break;
-        }
+  // registers as in k_flash
+  if (warp < kElem) {
+    regs_dec<64>();
+    if (warp == kProducer) {
+      // =============================== producer ====================================
+      int g = 0, it = 0, pub = 0;
+      bool failed = false;
+      if (a.n_seqs <= 32)
+        range = find_range_warp(a, line_of, gridDim.x, blockIdx.x, blockIdx.x == 0 ? a.status : nullptr);
+      const float f = kF16 && kKeys ? grad_scale(a.big, a.n_big) * exp2f(-kPScale) : 1.f;
+      if (lane == 0) a.share[2 * blockIdx.x].n = a.share[2 * blockIdx.x + 1].n = -1;
+      int col_tok[4];  // token of this lane's columns lane, lane + 32, .. of a tile of rows (past it: never one)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) col_tok[e] = lane + 32 * e < T * G ? (lane + 32 * e) / G : INT32_MAX / 2;
+      // The next item that this share has tiles of, to S.next (see k_flash).
+      auto advance = [&](bool first) {
+        __syncwarp();
         if (lane == 0) {
-          mbar_arrive_expect_tx(&S.q_full, kKeys ? 2 * 128 * 128 : 2 * T * G * 128);
-          if (kKeys) {
-            tma_load_4d(S.A1, &tmA1, &S.q_full, 0, c.h, item.k0 + item.at, 0);
-            tma_load_4d(S.A2, &tmA2, &S.q_full, 0, c.h, item.k0 + item.at, 0);
-          } else {
-            tma_load_4d(S.A1, &tmA1, &S.q_full, 0, 0, c.h, item.q0 + item.at);
-            tma_load_4d(S.A2, &tmA2, &S.q_full, 0, 0, c.h, item.q0 + item.at);
+          Cursor& c = S.cursor;
+          Item& item = S.next;
+          item.h = -1;
+          if (first) seek(a, line_of, range.x0, range.b0, range.base, c);
+          while (first || (next(a, line_of, c) && c.start < range.x1)) {
+            first = false;
+            int from, t0, t1;
+            const int at = c.j * (kKeys ? 128 : T), n = item_tiles<kKeys>(a, c.s, at, T, from);
+            tiles_of(c, range.x0, range.x1, n, t0, t1);
+            if (t0 == t1 && (n > 0 || c.start < range.x0)) continue;
+            item.q0 = c.s.q0, item.k0 = c.s.k0, item.nq = c.s.nq, item.nk = c.s.nk, item.d = c.s.d, item.p = c.s.p;
+            item.h = c.h, item.at = at, item.from = from, item.t0 = t0, item.t1 = t1;
+            item.part = t0 == 0 && t1 == n ? -1 : share_slot(c, range.x0);
+            if (item.part >= 0)
+              a.share[item.part] = DenseShare{t0, t1, n, c.h, (kKeys ? c.s.k0 : c.s.q0) + at,
+                                              min((kKeys ? c.s.nk : c.s.nq) - at, kKeys ? 128 : T), {}};
+            break;
           }
         }
         __syncwarp();
-        a_loaded = true;
-        // columns lane and lane + 32 of a tile of rows; the next tile's are loaded ahead
-        auto stats = [&](int t, float2 (&x)[2]) {
-          const int tok = item.from + t * per;
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int col = lane + 32 * e;
-            x[e] = make_float2(INFINITY, 0.f);
-            if (col < per * G && tok + col / G < item.nq)
-              x[e] = a.stat[((int64_t)c.h * a.rows + item.q0 + tok) * G + col];
-          }
-        };
-        float2 now[2], ahead[2];
-        if (kKeys) stats(item.t0, now);
-        for (int t = item.t0; t < item.t1; ++t) {
-          const int s = g % kStages, u = g / kStages;
-          if (kKeys && t + 1 < item.t1) stats(t + 1, ahead);
-          if (u > 0 && !wait(&S.kv_empty[s], (u - 1) & 1, abort)) {
+      };
+      auto publish = [&]() -> bool {
+        const int i = pub % kItems, u = pub / kItems;
+        if (u > 0 && !wait(&S.it_empty[i], (u - 1) & 1, abort)) return false;
+        if (lane == 0) {
+          S.next.g0 = g;
+          S.item[i] = S.next;
+          mbar_arrive(&S.it_full[i]);
+        }
+        __syncwarp();
+        ++pub;
+        return true;
+      };
+      if (range.x0 < range.x1) {
+        for (advance(true); S.next.h >= 0 && !failed; advance(false)) {
+          if (!publish()) {
             failed = true;
             break;
           }
-          int flags = (t == item.t0 ? kFirst : 0) | (t == item.t1 - 1 ? kLast : 0);
-          const int tok = item.from + t * per;
-          if (kKeys) {
-            bool whole = true;
+          const Item& item = S.next;
+          if (item.t0 == item.t1) continue;  // nothing to add up
+          const int buf = it & 1, h = item.h, t0 = item.t0, t1 = item.t1;
+          if (it > 1 && !wait(&S.a_empty[buf], ((it >> 1) - 1) & 1, abort)) {
+            failed = true;
+            break;
+          }
+          if (lane == 0) {
+            mbar_arrive_expect_tx(&S.a_full[buf], kKeys ? 2 * 128 * 128 : 2 * T * G * 128);
+            if (kKeys) {
+              tma_load_4d(S.A[buf][0], &tmA1, &S.a_full[buf], 0, h, item.k0 + item.at, 0);
+              tma_load_4d(S.A[buf][1], &tmA2, &S.a_full[buf], 0, h, item.k0 + item.at, 0);
+            } else {
+              tma_load_4d(S.A[buf][0], &tmA1, &S.a_full[buf], 0, 0, h, item.q0 + item.at);
+              tma_load_4d(S.A[buf][1], &tmA2, &S.a_full[buf], 0, 0, h, item.q0 + item.at);
+            }
+          }
+          __syncwarp();
+          ++it;
+          // the next tile's columns are loaded ahead
+          const float2* stat = a.stat + ((int64_t)h * a.rows + item.q0 + item.from) * G + lane;
+          const int left = item.nq - item.from, pos0 = item.d + item.from, base = kKeys ? item.q0 + item.from : item.k0;
+          const int nk = item.nk, p = item.p, last_key = min(nk, item.at + 128);
+          float slope[4] = {0.f, 0.f, 0.f, 0.f};
+          if (kKeys && kGen && a.slopes) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int col = lane + 32 * e, row = tok + col / G, pos = item.d + row;
-              const bool exists = col < per * G && row < item.nq;
-              const int lim = !exists ? 0 : a.causal ? max(0, max(item.p, pos + 1)) : item.nk;
-              whole = whole && lim >= min(item.nk, item.at + 128);
-              S.cols[s].lse[col] = (kF16 ? kPScale : 0.f) - now[e].x;
-              S.cols[s].delta[col] = -now[e].y * f;
-              S.cols[s].lim[col] = lim;
-              if (kGen) {
-                S.cols[s].pos[col] = (float)pos;
-                S.cols[s].slope[col] = a.slopes && exists ? a.slopes[c.h * G + col % G] * kLog2e : 0.f;
+            for (int e = 0; e < 4; ++e) slope[e] = a.slopes[h * G + (lane + 32 * e) % G] * kLog2e;
+          }
+          auto stats = [&](int t, float2 (&x)[4]) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              x[e] = make_float2(INFINITY, 0.f);
+              if (t * T + col_tok[e] < left) x[e] = stat[(int64_t)t * T * G + 32 * e];
+            }
+          };
+          float2 now[4], ahead[4];
+          if (kKeys) stats(t0, now);
+          for (int t = t0; t < t1; ++t) {
+            const int s = g % kStages, u = g / kStages;
+            if (kKeys && t + 1 < t1) stats(t + 1, ahead);
+            if (u > 0 && !wait(&S.kv_empty[s], (u - 1) & 1, abort)) {
+              failed = true;
+              break;
+            }
+            int flags = (t == t0 ? kFirst : 0) | (t == t1 - 1 ? kLast : 0);
+            if (kKeys) {
+              bool whole = true;
+              Cols& cols = S.cols[s];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int col = lane + 32 * e, row = t * T + col_tok[e];
+                const int lim = row >= left ? 0 : a.causal ? max(p, pos0 + row + 1) : nk;
+                whole = whole && lim >= last_key;
+                cols.lse[col] = (kF16 ? kPScale : 0.f) - now[e].x;
+                cols.delta[col] = -now[e].y * f;
+                cols.lim[col] = lim;
+                if (kGen) cols.pos[col] = (float)(pos0 + row), cols.slope[col] = slope[e];
+                now[e] = ahead[e];
+              }
+              if (!__all_sync(0xffffffffu, whole)) flags |= kMask;
+            }
+            __syncwarp();
+            if (lane == 0) {
+              S.flags[s] = flags;
+              mbar_arrive_expect_tx(&S.kv_full[s], kKeys ? 2 * T * G * 128 : 2 * kTileBytes);
+              if (kKeys) {
+                tma_load_4d(S.B1[s], &tmB1, &S.kv_full[s], 0, 0, h, base + t * T);
+                tma_load_4d(S.B2[s], &tmB2, &S.kv_full[s], 0, 0, h, base + t * T);
+              } else {
+                tma_load_4d(S.B1[s], &tmB1, &S.kv_full[s], 0, h, base + t * kCols, 0);
+                tma_load_4d(S.B2[s], &tmB2, &S.kv_full[s], 0, h, base + t * kCols, 0);
               }
             }
-            if (!__all_sync(0xffffffffu, whole)) flags |= kMask;
+            __syncwarp();
+            ++g;
           }
-          __syncwarp();
-          if (lane == 0) {
-            S.flags[s] = flags;
-            mbar_arrive_expect_tx(&S.kv_full[s], kKeys ? 2 * per * G * 128 : 2 * kTileBytes);
-            if (kKeys) {
-              tma_load_4d(S.B1[s], &tmB1, &S.kv_full[s], 0, 0, c.h, item.q0 + tok);
-              tma_load_4d(S.B2[s], &tmB2, &S.kv_full[s], 0, 0, c.h, item.q0 + tok);
-            } else {
-              tma_load_4d(S.B1[s], &tmB1, &S.kv_full[s], 0, c.h, item.k0 + t * kTile, 0);
-              tma_load_4d(S.B2[s], &tmB2, &S.kv_full[s], 0, c.h, item.k0 + t * kTile, 0);
-            }
-          }
-          __syncwarp();
-          now[0] = ahead[0], now[1] = ahead[1];
-          ++g;
         }
-        if (failed) break;
-        ++it;
-        a_loaded = false;
-      } while (next(a, line_of, c) && c.start < range.x1);
-    }
-    rows::stream_release();
-    if (!failed) {
-      const int s = g % kStages, u = g / kStages;
-      if (u > 0 && !wait(&S.kv_empty[s], (u - 1) & 1, abort)) {
-        failed = true;
-      } else if (lane == 0) {
-        S.flags[s] = kTerm;
-        mbar_arrive(&S.kv_full[s]);
       }
-      if (!failed && !publish(nullptr)) failed = true;
-    }
-    if (failed && lane == 0) {
-      give_up(S, a.status);
-      // let every copy already issued land before the CTA's shared memory goes away
-      volatile int no_abort = 0;
-      for (int back = 1; back <= kStages && g - back >= 0; ++back)
-        mbar_wait(&S.kv_full[(g - back) % kStages], ((g - back) / kStages) & 1, &no_abort, kDrainNs);
-      if (a_loaded) mbar_wait(&S.q_full, it & 1, &no_abort, kDrainNs);
-    }
-  } else if (warp == 1) {
-    // ================================ MMA issuer ===================================
-    const bool leader = elect_one();
-    bool failed = false;
-    constexpr uint32_t kRow = idesc16<kF16>(128, kTile, false), kSum = idesc16<kF16>(128, 64, true);
-    constexpr uint64_t kStageUnits = kTileBytes >> 4;
-    const uint64_t b10 = sdesc_sw128(smem_u32(S.B1[0])), b20 = sdesc_sw128(smem_u32(S.B2[0]));
-    int it = 0, sums = 0;  // items whose A operands are in TMEM, and whose sums were begun
-    auto fetch = [&](int t, int& flags) -> bool {
-      if (!wait(&S.kv_full[t % kStages], (t / kStages) & 1, abort)) return false;
-      flags = S.flags[t % kStages];
-      return true;
-    };
-    auto issue_sums = [&](int t, int flags) -> bool {
-      const int st = t % kStages, b = t & 1;
-      if (!wait(&S.p_full[b], (t >> 1) & 1, abort)) return false;
-      if (flags & kFirst) {  // the item before has been read
-        if (sums > 0 && !wait(&S.acc_empty, (sums - 1) & 1, abort)) return false;
-        ++sums;
-      }
-      tc_fence_after();
-      if (leader) {
-        const uint64_t d1 = b10 + (uint64_t)st * kStageUnits, d2 = b20 + (uint64_t)st * kStageUnits;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const uint32_t more = k > 0 || !(flags & kFirst) ? 1u : 0u;
-          if (kKeys) mma_bf16_ts(tmem + kColAcc2, tmem + 128 * b + 8 * k, d2 + 128 * k, kSum, more);
-          mma_bf16_ts(tmem + kColAcc1, tmem + 128 * b + kColP + 8 * k, d1 + 128 * k, kSum, more);
-        }
-        mma_commit(&S.kv_empty[st]);
-        if (flags & kLast) mma_commit(&S.acc_full);
-      }
-      __syncwarp();
-      return true;
-    };
-    // Per tile: S and dP, then the sums over the tile before it.  The last sums of an item do not wait for a tile
-    // to come: the producer may be waiting for the element-wise warps to end the item.
-    int flags = kTerm, held = -1, held_flags = 0;
-    if (!fetch(0, flags)) failed = true;
-    for (int g = 0; !failed && !(flags & kTerm); ++g) {
-      if (flags & kFirst) {
-        if (!wait(&S.q_full, it & 1, abort)) {
+      rows::stream_release();
+      if (!failed) {
+        const int s = g % kStages, u = g / kStages;
+        if (u > 0 && !wait(&S.kv_empty[s], (u - 1) & 1, abort)) {
           failed = true;
-          break;
-        }
-        tc_fence_after();
-        if (leader) {
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            tmem_cp_128x256b(tmem + kColA1 + 8 * k, sdesc_sw128(smem_u32(S.A1) + 32 * k));
-            tmem_cp_128x256b(tmem + kColA2 + 8 * k, sdesc_sw128(smem_u32(S.A2) + 32 * k));
-          }
-          mma_commit(&S.q_empty);
+        } else if (lane == 0) {
+          S.flags[s] = kTerm;
+          mbar_arrive(&S.kv_full[s]);
         }
         __syncwarp();
-        ++it;
+        if (lane == 0) S.next.h = -1;
+        __syncwarp();
+        if (!failed && !publish()) failed = true;
       }
-      const uint64_t at = (uint64_t)(g % kStages) * kStageUnits;
-      const int b = g & 1;
+      if (failed && lane == 0) {
+        give_up(S, a.status);
+        // let every copy already issued land before the CTA's shared memory goes away
+        volatile int no_abort = 0;
+        for (int back = 1; back <= kStages && g - back >= 0; ++back)
+          mbar_wait(&S.kv_full[(g - back) % kStages], ((g - back) / kStages) & 1, &no_abort, kDrainNs);
+        for (int back = 1; back <= 2 && it - back >= 0; ++back)
+          mbar_wait(&S.a_full[(it - back) & 1], ((it - back) >> 1) & 1, &no_abort, kDrainNs);
+      }
+    } else {
+      // ================================ MMA issuers ==================================
+      const bool leader = elect_one();
+      bool failed = false;
+      constexpr uint32_t kRow = idesc16<kF16>(128, kCols, false), kSum = idesc16<kF16>(128, 64, true);
+      constexpr uint64_t kStageUnits = kTileBytes >> 4, kAUnits = (128 * 128) >> 4;
+      uint32_t phase = 0;
+      if (warp == kIssueS) {
+        const uint64_t b1 = sdesc_sw128(smem_u32(S.B1[0])), b2 = sdesc_sw128(smem_u32(S.B2[0]));
+        const uint64_t a0 = sdesc_sw128(smem_u32(S.A[0][0]));
+        uint32_t s_phase = 1, items = 0;
+        for (int st = 0;;) {
+          if (!wait(&S.kv_full[st], phase, abort)) {
+            failed = true;
+            break;
+          }
+          const int flags = S.flags[st];
+          if (flags & kTerm) break;
+          if (flags & kFirst) {
+            if (!wait(&S.a_full[items & 1], (items >> 1) & 1, abort)) {
+              failed = true;
+              break;
+            }
+            ++items;
+          }
+          const uint32_t buf = (items - 1) & 1;
+          const uint64_t ad = a0 + 2 * buf * kAUnits, at = (uint64_t)st * kStageUnits;
+          if (!wait(&S.s_free, s_phase, abort)) {  // (the first time: at once)
+            failed = true;
+            break;
+          }
+          tc_fence_after();
+          if (leader) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) mma_bf16_ss(tmem, ad + 2 * k, b1 + at + 2 * k, kRow, k > 0 ? 1u : 0u);
+            mma_commit(&S.s_full);
+          }
+          __syncwarp();
+          if (!wait(&S.dp_free, s_phase, abort)) {
+            failed = true;
+            break;
+          }
+          s_phase ^= 1;
+          tc_fence_after();
+          if (leader) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              mma_bf16_ss(tmem + kColDp, ad + kAUnits + 2 * k, b2 + at + 2 * k, kRow, k > 0 ? 1u : 0u);
+            mma_commit(&S.dp_full);
+            if (flags & kLast) mma_commit(&S.a_empty[buf]);
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&S.kv_empty[st]);
+          __syncwarp();
+          if (++st == kStages) st = 0, phase ^= 1;
+        }
+      } else if (kKeys || warp == kIssueDs) {
+        // dQ, dK += dS B1; dV += P B2
+        const bool ds = warp == kIssueDs;
+        const uint64_t b0 = sdesc_sw128(smem_u32(ds ? S.B1[0] : S.B2[0]));
+        const uint32_t acc = tmem + (ds ? kColAcc1 : kColAcc2), from = tmem + (ds ? kColDs : kColP);
+        uint32_t p_phase = 0, e_phase = 1;
+        for (int st = 0;;) {
+          if (!wait(&S.kv_full[st], phase, abort)) {
+            failed = true;
+            break;
+          }
+          const int flags = S.flags[st];
+          if (flags & kTerm) break;
+          if (!wait(&S.p_full, p_phase, abort)) {
+            failed = true;
+            break;
+          }
+          p_phase ^= 1;
+          if (flags & kFirst) {  // the item before has been read (the first time: at once)
+            if (!wait(&S.acc_empty, e_phase, abort)) {
+              failed = true;
+              break;
+            }
+            e_phase ^= 1;
+          }
+          tc_fence_after();
+          if (leader) {
+            const uint64_t bd = b0 + (uint64_t)st * kStageUnits;
+            mma_bf16_ts(acc, from, bd, kSum, flags & kFirst ? 0u : 1u);
+#pragma unroll
+            for (int k = 1; k < 8; ++k) mma_bf16_ts(acc, from + 8 * k, bd + 128 * k, kSum, 1u);
+            mma_commit(&S.p_done);
+            mma_commit(&S.kv_empty[st]);
+            if (flags & kLast) mma_commit(&S.acc_full);
+          }
+          __syncwarp();
+          if (++st == kStages) st = 0, phase ^= 1;
+        }
+      }
+      if (failed && lane == 0) give_up(S, a.status);
+      // wait for every MMA issued so far before TMEM is released
       if (leader) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          mma_bf16_ts(tmem + 128 * b, tmem + kColA1 + 8 * k, b10 + at + 2 * k, kRow, k > 0 ? 1u : 0u);
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          mma_bf16_ts(tmem + 128 * b + kColP, tmem + kColA2 + 8 * k, b20 + at + 2 * k, kRow, k > 0 ? 1u : 0u);
-        mma_commit(&S.s_full[b]);
+        mma_commit(&S.drain[warp - kIssueS]);
+        volatile int no_abort = 0;
+        mbar_wait(&S.drain[warp - kIssueS], 0, &no_abort, kDrainNs);
       }
       __syncwarp();
-      if (held >= 0 && !issue_sums(held, held_flags)) {
-        failed = true;
-        break;
-      }
-      held = g, held_flags = flags;
-      if ((flags & kLast) && !mbar_ready(&S.kv_full[(g + 1) % kStages], ((g + 1) / kStages) & 1)) {
-        if (!issue_sums(held, held_flags)) {
-          failed = true;
-          break;
-        }
-        held = -1;
-      }
-      if (!fetch(g + 1, flags) || ((flags & kTerm) && held >= 0 && !issue_sums(held, held_flags))) {
-        failed = true;
-        break;
-      }
     }
-    if (failed && lane == 0) give_up(S, a.status);
-    // wait for every MMA issued so far before TMEM is released
-    if (leader) {
-      mma_commit(&S.drain);
-      volatile int no_abort = 0;
-      mbar_wait(&S.drain, 0, &no_abort, kDrainNs);
-    }
-    __syncwarp();
   } else {
-    // ============================ element-wise groups ==============================
-    const int group = (warp - 2) >> 2, quarter = warp & 3;
-    const int r = quarter * 32 + lane;
-    const int tid = (warp - 2 - 4 * group) * 32 + lane;  // 0..127, for the zeroing
-    const uint32_t tm = tmem + ((uint32_t)(quarter * 32) << 16), tS = tm + 128 * group, tP = tS + kColP;
+    regs_inc<104>();
+    // ============================ element-wise warps ===============================
+    const int idx = warp - kElem, side = idx >> 3, half = idx >> 2 & 1, quarter = warp & 3;  // side: columns 64 side ..
+    const int r0 = quarter * 32 + half * 16 + (lane >> 2), two = 2 * (lane & 3);  // this lane's rows: r0, r0 + 8; columns
+    const uint32_t tm = tmem + ((uint32_t)(quarter * 32 + half * 16) << 16);
     const float kScale = kLog2e * 0.125f;
     const float cap = a.cap, in = a.cap > 0.f ? 0.25f * kLog2e / a.cap : 0.125f * kLog2e, out = a.cap * kLog2e;
     const float back = a.cap > 0.f ? 1.0f / out : 0.f;
     const float scale = kF16 ? grad_scale(a.big, a.n_big) : 1.f, f = kF16 ? scale * exp2f(-kPScale) : 1.f;
-    const float undo = 0.125f / scale;
-    int it = 0;
+    uint32_t c = 0, it = 0;  // tiles, and items with any, so far
     bool stop = false;
     for (int pub = 0; !stop; ++pub) {
       const int i = pub % kItems;
@@ -474,157 +497,211 @@ __global__ void __launch_bounds__(kThreads, 1)
         give_up(S, a.status);
         break;
       }
-      const Item item = S.item[i];
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&S.it_empty[i]);
+      const Item& item = S.item[i];
       if (item.h < 0) break;
-      // this thread's row: a key, or a row of Q
-      const int tok = item.at + (kKeys ? r : r / G);
-      const bool exists = kKeys ? tok < item.nk : r / G < T && tok < item.nq;
-      const int pos = item.d + tok, head = item.h * G + r % G;  // (of a row of Q)
-      float nlse = -INFINITY, ndelta = 0.f, slope = 0.f;
-      int lim = 0, least = 0;
-      if (!kKeys) {
-        if (exists) {
-          const float2 x = a.stat[((int64_t)item.h * a.rows + item.q0 + tok) * G + r % G];
-          nlse = (kF16 ? kPScale : 0.f) - x.x, ndelta = -x.y * f;
-          lim = a.causal ? min(item.nk, max(item.p, pos + 1)) : item.nk;
-          if (kGen && a.slopes) slope = a.slopes[head] * kLog2e;
+      // this lane's rows: keys, or rows of Q
+      const int tiles = item.t1 - item.t0, nk = item.nk;
+      int tok[2], pos[2], lim[2] = {0, 0}, least = INT32_MAX;
+      float nlse[2] = {-INFINITY, -INFINITY}, ndelta[2] = {0.f, 0.f}, slope[2] = {0.f, 0.f};
+      bool exists[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int r = r0 + 8 * j;
+        tok[j] = item.at + (kKeys ? r : r / G);
+        exists[j] = kKeys ? tok[j] < nk : r / G < T && tok[j] < item.nq;
+        pos[j] = item.d + tok[j];
+        if (!kKeys && exists[j]) {
+          const float2 x = a.stat[((int64_t)item.h * a.rows + item.q0 + tok[j]) * G + r % G];
+          nlse[j] = (kF16 ? kPScale : 0.f) - x.x, ndelta[j] = -x.y * f;
+          lim[j] = a.causal ? max(0, min(nk, max(item.p, pos[j] + 1))) : nk;
+          least = min(least, lim[j]);
+          if (kGen && a.slopes) slope[j] = a.slopes[item.h * G + r % G] * kLog2e;
         }
-        least = __reduce_min_sync(0xffffffffu, exists ? max(lim, 0) : INT32_MAX);
       }
-      const int g1 = item.g0 + item.t1 - item.t0;
-      for (int g = item.g0 + ((item.g0 & 1) != group); g < g1; g += 2) {
-        const int st = g % kStages;
-        if (!wait(&S.kv_full[st], (g / kStages) & 1, abort) || !wait(&S.s_full[group], (g >> 1) & 1, abort)) {
+      if (!kKeys) least = __reduce_min_sync(0xffffffffu, least);
+      for (int k = 0; k < tiles; ++k, ++c) {
+        const int g = item.g0 + k, st = g % kStages, t = item.t0 + k, key = t * kCols;
+        if (!wait(&S.kv_full[st], (g / kStages) & 1, abort) || !wait(&S.s_full, c & 1, abort)) {
           give_up(S, a.status);
           stop = true;
           break;
         }
         tc_fence_after();
-        const int t = item.t0 + g - item.g0, key = t * kTile;
         const Cols& cols = S.cols[st];
-        const bool masked = kKeys ? (S.flags[st] & kMask) != 0 : key + kTile > least;
+        const bool masked = kKeys ? (S.flags[st] & kMask) != 0 : key + kCols > least;
+        float x[32];
+        uint32_t w[16];
+        {
+          uint32_t v[32];
+          RESS_TMEM_LD16X64(tm + 64 * side, v);
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          uint32_t s[32], dp[32], w1[16], w2[16];
-          RESS_TMEM_LD32(tS + 32 * hf, s);
-          RESS_TMEM_LD32(tP + 32 * hf, dp);
-#pragma unroll
-          for (int e = 0; e < 32; e += 2) {
-            const int col = 32 * hf + e;
-            float l0 = nlse, l1 = nlse, n0 = ndelta, n1 = ndelta;
-            if (kKeys) {
-              const float2 l = *reinterpret_cast<const float2*>(&cols.lse[col]);
-              const float2 n = *reinterpret_cast<const float2*>(&cols.delta[col]);
-              l0 = l.x, l1 = l.y, n0 = n.x, n1 = n.y;
-            }
-            float x0 = __uint_as_float(s[e]), x1 = __uint_as_float(s[e + 1]);
-            float y0 = __uint_as_float(dp[e]), y1 = __uint_as_float(dp[e + 1]);
-            float c0 = 1.f, c1 = 1.f;
-            if (kGen) {
-              if (cap > 0.f) {
-                capped2(x0, x1, in, out);
-                float u0, u1;
-                mul2(u0, u1, x0, x1, back, back);
-                fma2(c0, c1, -u0, -u1, u0, u1, 1.f, 1.f);
-              } else {
-                x0 *= in, x1 *= in;
-              }
-              if (a.slopes) {
-                if (kKeys) {
-                  const float2 q = *reinterpret_cast<const float2*>(&cols.pos[col]);
-                  const float2 m = *reinterpret_cast<const float2*>(&cols.slope[col]);
-                  x0 = fmaf(-m.x, fabsf(q.x - (float)tok), x0);
-                  x1 = fmaf(-m.y, fabsf(q.y - (float)tok), x1);
-                } else {
-                  x0 = fmaf(-slope, fabsf((float)(pos - key - col)), x0);
-                  x1 = fmaf(-slope, fabsf((float)(pos - key - col - 1)), x1);
-                }
-              }
-              add2(x0, x1, x0, x1, l0, l1);
-            } else {
-              fma2(x0, x1, x0, x1, kScale, kScale, l0, l1);
-            }
-            x0 = ex2(x0), x1 = ex2(x1);
-            if (kF16)
-              fma2(y0, y1, y0, y1, f, f, n0, n1);
-            else
-              add2(y0, y1, y0, y1, n0, n1);
-            if (kGen) mul2(y0, y1, y0, y1, c0, c1);
-            mul2(y0, y1, y0, y1, x0, x1);
-            if (masked) {
-              bool s0, s1;
-              if (kKeys) {
-                const int2 m = *reinterpret_cast<const int2*>(&cols.lim[col]);
-                s0 = tok < m.x, s1 = tok < m.y;
-              } else {
-                s0 = key + col < lim, s1 = key + col + 1 < lim;
-              }
-              x0 = s0 ? x0 : 0.f, x1 = s1 ? x1 : 0.f;
-              y0 = s0 ? y0 : 0.f, y1 = s1 ? y1 : 0.f;
-            }
-            w1[e >> 1] = pack2<kF16>(x0, x1);
-            w2[e >> 1] = pack2<kF16>(y0, y1);
-          }
-          if (kKeys) RESS_TMEM_ST16(tS + 16 * hf, w1);
-          RESS_TMEM_ST16(tP + 16 * hf, w2);
-        }
-        // rows of the tile that are not this sequence's, which the sums run over
-        const int valid = kKeys ? (item.nq - item.from - t * per) * G : item.nk - key;
-        if (valid < (kKeys ? per * G : kTile)) {
-          zero_rows(S.B1[st], valid, tid);
-          if (kKeys) zero_rows(S.B2[st], valid, tid);
-          fence_proxy_async_smem();
+          for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(v[e]);
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&S.p_full[group]);
+        if (lane == 0) mbar_arrive(&S.s_free);  // S is in registers: that of the next tile may come
+        __syncwarp();
+        // P
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) {
+          const int j = e >> 1 & 1, col = 64 * side + 8 * (e >> 2) + two;  // row, columns col and col + 1
+          float l0 = nlse[j], l1 = nlse[j];
+          if (kKeys) {
+            const float2 l = *reinterpret_cast<const float2*>(&cols.lse[col]);
+            l0 = l.x, l1 = l.y;
+          }
+          float x0 = x[e], x1 = x[e + 1];
+          float c0 = 1.f, c1 = 1.f;
+          if (kGen) {
+            if (cap > 0.f) {
+              capped2(x0, x1, in, out);
+              float u0, u1;
+              mul2(u0, u1, x0, x1, back, back);
+              fma2(c0, c1, -u0, -u1, u0, u1, 1.f, 1.f);
+            } else {
+              x0 *= in, x1 *= in;
+            }
+            if (a.slopes) {
+              if (kKeys) {
+                const float2 q = *reinterpret_cast<const float2*>(&cols.pos[col]);
+                const float2 m = *reinterpret_cast<const float2*>(&cols.slope[col]);
+                x0 = fmaf(-m.x, fabsf(q.x - (float)tok[j]), x0);
+                x1 = fmaf(-m.y, fabsf(q.y - (float)tok[j]), x1);
+              } else {
+                x0 = fmaf(-slope[j], fabsf((float)(pos[j] - key - col)), x0);
+                x1 = fmaf(-slope[j], fabsf((float)(pos[j] - key - col - 1)), x1);
+              }
+            }
+            add2(x0, x1, x0, x1, l0, l1);
+          } else {
+            fma2(x0, x1, x0, x1, kScale, kScale, l0, l1);
+          }
+          x0 = ex2(x0), x1 = ex2(x1);
+          if (masked) {
+            bool s0, s1;
+            if (kKeys) {
+              const int2 m = *reinterpret_cast<const int2*>(&cols.lim[col]);
+              s0 = tok[j] < m.x, s1 = tok[j] < m.y;
+            } else {
+              s0 = key + col < lim[j], s1 = key + col + 1 < lim[j];
+            }
+            x0 = s0 ? x0 : 0.f, x1 = s1 ? x1 : 0.f;
+          }
+          if (kKeys) w[e >> 1] = pack2<kF16>(x0, x1);
+          if (kGen) mul2(x0, x1, x0, x1, c0, c1);
+          x[e] = x0, x[e + 1] = x1;  // p, times the cap's slope
+        }
+        // the sums over the tile before this one have read P and dS
+        if ((c > 0 && !wait(&S.p_done, (c - 1) & 1, abort)) || !wait(&S.dp_full, c & 1, abort)) {
+          give_up(S, a.status);
+          stop = true;
+          break;
+        }
+        tc_fence_after();
+        if (kKeys) RESS_TMEM_ST16X32P_NOWAIT(tm + kColP + 32 * side, w);
+        uint32_t v[32];
+        RESS_TMEM_LD16X64(tm + kColDp + 64 * side, v);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&S.dp_free);
+        __syncwarp();
+        // dS; a masked p is 0, and so is its dS whatever dP is
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) {
+          const int j = e >> 1 & 1, col = 64 * side + 8 * (e >> 2) + two;
+          float n0 = ndelta[j], n1 = ndelta[j];
+          if (kKeys) {
+            const float2 n = *reinterpret_cast<const float2*>(&cols.delta[col]);
+            n0 = n.x, n1 = n.y;
+          }
+          float y0 = __uint_as_float(v[e]), y1 = __uint_as_float(v[e + 1]);
+          if (kF16)
+            fma2(y0, y1, y0, y1, f, f, n0, n1);
+          else
+            add2(y0, y1, y0, y1, n0, n1);
+          mul2(y0, y1, y0, y1, x[e], x[e + 1]);
+          if (masked) y0 = x[e] == 0.f ? 0.f : y0, y1 = x[e + 1] == 0.f ? 0.f : y1;
+          w[e >> 1] = pack2<kF16>(y0, y1);
+        }
+        if (kKeys) tmem_wait_st();
+        RESS_TMEM_ST16X32P_NOWAIT(tm + kColDs + 32 * side, w);
+        // rows of the tile that are not this sequence's, which the sums run over
+        const int valid = kKeys ? (item.nq - item.from - t * T) * G : nk - key;
+        if (valid < (kKeys ? T * G : kCols)) {
+          if (side == 0)
+            zero_rows(S.B1[st], valid, (idx & 7) * 32 + lane);
+          else if (kKeys)
+            zero_rows(S.B2[st], valid, (idx & 7) * 32 + lane);
+          fence_proxy_async_smem();
+        }
+        __syncwarp();
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&S.p_full);
+        __syncwarp();
       }
       if (stop) break;
-      // group 0 takes dK, or half of the channels of dQ; group 1 dV, or the other half
-      constexpr int N = kKeys ? 64 : 32;
-      uint32_t o[N];
-      if (item.t1 > item.t0) {
+      // side 0 takes dK or dQ, side 1 dV
+      float o[32];
+#pragma unroll
+      for (int e = 0; e < 32; ++e) o[e] = 0.f;
+      if (tiles > 0) {
         if (!wait(&S.acc_full, it & 1, abort)) {
           give_up(S, a.status);
           break;
         }
         ++it;
         tc_fence_after();
-        if constexpr (kKeys)
-          RESS_TMEM_LD64(tm + (group ? kColAcc2 : kColAcc1), o);
-        else
-          RESS_TMEM_LD32(tm + kColAcc1 + 32 * group, o);
+        uint32_t v[32];
+        RESS_TMEM_LD16X64(tm + (kKeys && side ? kColAcc2 : kColAcc1), v);
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&S.acc_empty);
-      } else {
+        __syncwarp();
 #pragma unroll
-        for (int e = 0; e < N; ++e) o[e] = 0u;
+        for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(v[e]);
       }
-      if (!exists) continue;
-      const float by = kKeys && group ? (kF16 ? exp2f(-kPScale) : 1.f) : undo;
-      if (item.part >= 0) {
-        float4* dst = reinterpret_cast<float4*>(a.part + item.part * kPartFloats + (kKeys ? (group * 128 + r) * 64 : r * 64 + 32 * group));
+      const float by = kKeys && side ? (kF16 ? exp2f(-kPScale) : 1.f) : 0.125f / scale;
+      const ress_heads& to = kKeys ? (side ? a.dv : a.dk) : a.dq;
 #pragma unroll
-        for (int e = 0; e < N / 4; ++e)
-          dst[e] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]),
-                               __uint_as_float(o[4 * e + 3]));
-      } else if (kKeys) {
-        const ress_heads& d = group ? a.dv : a.dk;
-        store_row<kF16>(static_cast<uint16_t*>(d.data) + ((int64_t)item.k0 + tok) * d.token_stride + item.h * d.head_stride, o, by);
-      } else {
-        store_row<kF16>(static_cast<uint16_t*>(a.dq.data) + ((int64_t)item.q0 + tok) * a.dq.token_stride +
-                            head * a.dq.head_stride + 32 * group, o, by);
+      for (int j = 0; j < 2; ++j) {
+        const int r = r0 + 8 * j;
+        if (!kKeys && side) break;
+        if (item.part >= 0) {
+          float2* dst = reinterpret_cast<float2*>(a.part + item.part * kPartFloats + (side * 128 + r) * 64 + two);
+          if (exists[j]) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dst[4 * e] = make_float2(o[4 * e + 2 * j], o[4 * e + 2 * j + 1]);
+          }
+        } else {
+          uint32_t w[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) w[e] = pack2<kF16>(o[4 * e + 2 * j] * by, o[4 * e + 2 * j + 1] * by);
+          // a row's four lanes: from two channels of every eight to eight of every 32
+          transpose4(w[0], w[1], w[2], w[3], lane);
+          transpose4(w[4], w[5], w[6], w[7], lane);
+          if (exists[j]) {
+            const int64_t token = (int64_t)(kKeys ? item.k0 : item.q0) + tok[j];
+            const int head = kKeys ? item.h : item.h * G + r % G;
+            uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(to.data) + token * to.token_stride +
+                                                  head * to.head_stride) + (lane & 3);
+            dst[0] = make_uint4(w[0], w[1], w[2], w[3]);
+            dst[4] = make_uint4(w[4], w[5], w[6], w[7]);
+          }
+        }
+        __syncwarp();
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&S.it_empty[i]);
+      __syncwarp();
     }
   }
 
   __syncwarp();
   tc_fence_before();
   __syncthreads();
-  if (warp == 1) {
+  if (warp == kIssueS) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
@@ -685,7 +762,7 @@ static cudaError_t launch_type(DenseArgs a, cudaStream_t st) {
   const int64_t rows = a.rows > 0 ? a.rows : 1, keys = a.keys > 0 ? a.keys : 1;
   CUtensorMap m[4];
   if (a.keys > 0) {
-    const int per = kTile / a.group;
+    const int per = 128 / a.group;
     if (!make_key_map(&m[0], k, a.type, keys, 1, 0, a.kv_heads, 128) || !make_key_map(&m[1], v, a.type, keys, 1, 0, a.kv_heads, 128) ||
         !make_row_map(&m[2], q, a.type, rows, a.kv_heads, a.group, per) ||
         !make_row_map(&m[3], g, a.type, rows, a.kv_heads, a.group, per))
@@ -696,7 +773,7 @@ static cudaError_t launch_type(DenseArgs a, cudaStream_t st) {
   if (a.rows > 0) {
     const int T = 128 / a.group;
     if (!make_row_map(&m[0], q, a.type, rows, a.kv_heads, a.group, T) || !make_row_map(&m[1], g, a.type, rows, a.kv_heads, a.group, T) ||
-        !make_key_map(&m[2], k, a.type, keys, 1, 0, a.kv_heads, kTile) || !make_key_map(&m[3], v, a.type, keys, 1, 0, a.kv_heads, kTile))
+        !make_key_map(&m[2], k, a.type, keys, 1, 0, a.kv_heads, kCols) || !make_key_map(&m[3], v, a.type, keys, 1, 0, a.kv_heads, kCols))
       return cudaErrorInvalidValue;
     if ((e = gen ? launch_pass<kF16, true, false>(a, m, ctas, st) : launch_pass<kF16, false, false>(a, m, ctas, st)) != cudaSuccess)
       return e;
