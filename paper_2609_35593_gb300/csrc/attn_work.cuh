@@ -352,6 +352,12 @@ __device__ __forceinline__ void regs_inc() {
       : "memory")
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+__device__ __forceinline__ float lg2(float x) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // Four lanes with four words each: lane i's word j becomes lane j's word i.
 __device__ __forceinline__ void transpose4(uint32_t& w0, uint32_t& w1, uint32_t& w2, uint32_t& w3, int lane) {
   const bool odd = lane & 1, high = lane & 2;
@@ -423,6 +429,50 @@ __device__ __forceinline__ void capped2(float& x0, float& x1, float c, float top
   asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(e0));
   asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(e1));
   fma2(x0, x1, e0, e1, -2.f * top, -2.f * top, top, top);
+}
+
+__device__ __forceinline__ void mul2(float& d0, float& d1, float a0, float a1, float b0, float b1) {
+  asm("{\n\t.reg .b64 ra, rb, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\t"
+      "mul.rn.f32x2 rd, ra, rb;\n\tmov.b64 {%0, %1}, rd;\n\t}"
+      : "=f"(d0), "=f"(d1)
+      : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
+}
+
+// Products q.k to capped scores in log2 units, a warp's 16 rows x 64 columns.  Where none of them is above half of the cap,
+// x times a polynomial in x^2 (set_cap): five packed instructions a pair on the FMA pipe, next to which the SFU forms the
+// exponentials; else capped2, whose four SFU operations a pair are twice what the exponentials take (packed documents,
+// cap 30: 251 us with capped2 alone).
+__device__ __forceinline__ void cap_scores(float (&x)[32], const DenseArgs& a, float in, float out) {
+  float z[32], top = 0.f;
+#pragma unroll
+  for (int e = 0; e < 32; e += 2) {
+    mul2(z[e], z[e + 1], x[e], x[e + 1], x[e], x[e + 1]);
+    top = fmax3(top, z[e], z[e + 1]);
+  }
+  if (!__any_sync(0xffffffffu, !(top <= a.cap_square))) {
+#pragma unroll
+    for (int e = 0; e < 32; e += 2) {
+      float p0, p1;
+      fma2(p0, p1, z[e], z[e + 1], a.cap_poly[3], a.cap_poly[3], a.cap_poly[2], a.cap_poly[2]);
+      fma2(p0, p1, z[e], z[e + 1], p0, p1, a.cap_poly[1], a.cap_poly[1]);
+      fma2(p0, p1, z[e], z[e + 1], p0, p1, a.cap_poly[0], a.cap_poly[0]);
+      mul2(x[e], x[e + 1], x[e], x[e + 1], p0, p1);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 32; e += 2) capped2(x[e], x[e + 1], in, out);
+  }
+}
+
+// tanh(u) / u for u^2 = z up to 1/4: a polynomial fitted to it at Chebyshev points by reweighted least squares, off by
+// 2^-20.8 of itself; its coefficients times what makes x = q.k out of u = x / (8 cap), and log2(e) cap u of tanh(u).
+inline void set_cap(DenseArgs& a) {
+  constexpr double kFit[4] = {0.999999463558197, -0.33326318860054016, 0.13190296292304993, -0.04440222308039665};
+  const double u = 0.125 / a.cap;
+  double scale = 0.125 * 1.4426950408889634;
+  for (int k = 0; k < 4; ++k, scale *= u * u) a.cap_poly[k] = (float)(kFit[k] * scale);
+  // (caps so small that the coefficients are beyond float32 have no such products)
+  a.cap_square = a.cap > 1e-3f ? (float)(0.25 / (u * u)) : -1.f;
 }
 
 }  // namespace work

@@ -62,6 +62,7 @@ struct __align__(1024) Smem {
   uint8_t K[kStages][kTileBytes];
   uint8_t V[kStages][kTileBytes];
   uint64_t kv_full[kStages], kv_empty[kStages];
+  uint8_t row_token[128], row_head[128];   // of the 128 rows of a part
   float other[2][128];                     // items of one part: slot 1's maxima and sums
   uint64_t other_full[8], other_empty[8];  // (of each warp's rows)
   uint64_t q_full[2][kSlots], q_empty[2][kSlots], drain[1 + kSlots];
@@ -139,6 +140,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     prefetch_tensormap(&tmK);
     prefetch_tensormap(&tmV);
   }
+  if (const int r = (int)threadIdx.x - 512; r >= 0) S.row_token[r] = r / G, S.row_head[r] = r % G;
   if (warp == kIssueS) tmem_alloc(&S.tmem_base, 512);
   tc_fence_before();
   __syncthreads();
@@ -204,19 +206,25 @@ __global__ void __launch_bounds__(kThreads, 1)
         return true;
       };
       if (range.x0 < range.x1) {
-        for (advance(true); S.next.h >= 0 && !failed; advance(false)) {
+        advance(true);
+        while (S.next.h >= 0 && !failed) {
           if (!publish()) {
             failed = true;
             break;
           }
           const Item& item = S.next;
-          if (item.t0 == item.t1) continue;  // rows without keys
+          if (item.t0 == item.t1) {  // rows without keys
+            advance(false);
+            continue;
+          }
           const int h = item.h, nk = item.nk, t0 = item.t0, t1 = item.t1, k0 = item.k0;
           const int32_t* table = a.table ? a.table + item.b * a.table_stride : nullptr;
           // the first lanes: what slot `lane` takes of the item
           const int parts = item.parts, ways = item.ways, mine_part = lane % parts, way = lane / parts;
           const int last = lane < kSlots && way < ways ? min(t1, item.n[mine_part]) : 0;
           const uint32_t some = __ballot_sync(0xffffffffu, t0 + way < last);
+          // slopes: the nearest keys of a causal row first, or the reference would be raised from tile to tile
+          const int step = a.slopes ? -1 : 1, begin = a.slopes ? t1 - 1 : t0;
           for (int s = 0; s < kSlots; ++s) {
             if (!(some >> s & 1)) continue;
             const uint32_t times = loads >> (8 * s) & 0xff, buf = times & 1;
@@ -250,16 +258,17 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           };
           int row, page;
-          place(t0, row, page);
-          for (int t = t0; t < t1; ++t) {
-            const int s = g % kStages, u = g / kStages;
+          place(begin, row, page);
+          for (int i = 0; i < t1 - t0; ++i) {
+            const int s = g % kStages, u = g / kStages, t = begin + step * i;
             int next_row = 0, next_page = 0;
-            if (t + 1 < t1) place(t + 1, next_row, next_page);
+            if (i + 1 < t1 - t0) place(t + step, next_row, next_page);
             int flags = 0;
-            if (t < last && (t - t0) % ways == way) {
+            if (ways > 1 ? lane < kSlots && i % kSlots == lane : t < last) {
               flags = kHas << lane;
-              if (t == t0 + way) flags |= kBegin << lane;
-              if (t + ways >= last) flags |= kEnd << lane;
+              const bool is_low = t == t0, is_high = t == last - 1;
+              if (ways > 1 ? i == lane : a.slopes ? is_high : is_low) flags |= kBegin << lane;
+              if (ways > 1 ? i + kSlots >= t1 - t0 : a.slopes ? is_low : is_high) flags |= kEnd << lane;
             }
             flags = __reduce_or_sync(0xffffffffu, flags);
             if (u > 0 && !wait(&S.kv_empty[s], (u - 1) & 1, abort)) {
@@ -277,6 +286,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             __syncwarp();
             row = next_row, page = next_page;
             ++g;
+            // the next item is looked for while the first tiles are worked on
+            if (i == min(kStages, t1 - t0) - 1) advance(false);
           }
         }
       }
@@ -456,19 +467,22 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (item.h < 0) break;
       const int parts = item.parts, ways = item.ways, part = slot % parts, way = slot / parts, nk = item.nk;
       const int ntok = part_tokens(item.nq, item.tok, part, T), tok0 = item.tok + part * T;
-      const int from = item.t0 + way, tiles = max(0, min(item.t1, item.n[part]) - from + ways - 1) / ways;
+      const int last = min(item.t1, item.n[part]), tiles = max(0, last - item.t0 - way + ways - 1) / ways;
+      // tile k of this slot is the (first + ways k)-th that comes, tile from + step k
+      const int first_tile = ways > 1 ? way : a.slopes ? item.t1 - last : 0, step = a.slopes ? -ways : ways;
+      const int from = a.slopes ? item.t1 - 1 - first_tile : item.t0 + first_tile;
       int pos[2], lim[2];
       float slope[2];
       int least = INT32_MAX;
       bool any = false;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const int r = r0 + 8 * j, t = r / G;
+        const int r = r0 + 8 * j, t = S.row_token[r];
         pos[j] = item.d + tok0 + t;
         lim[j] = t >= ntok ? 0 : a.causal ? max(0, min(nk, max(item.p, pos[j] + 1))) : nk;
         // rows that do not exist are masked for nobody's sake
         if (t < ntok) least = min(least, lim[j]), any = true;
-        slope[j] = kGen && a.slopes && t < ntok ? a.slopes[item.h * G + r % G] * kLog2e : 0.f;
+        slope[j] = kGen && a.slopes && t < ntok ? a.slopes[item.h * G + S.row_head[r]] * kLog2e : 0.f;
       }
       least = __reduce_min_sync(0xffffffffu, least);
       any = __any_sync(0xffffffffu, any);
@@ -478,8 +492,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(v[e]);
         if (kGen) {
           if (cap > 0.f) {
-#pragma unroll
-            for (int e = 0; e < 32; e += 2) capped2(x[e], x[e + 1], in, out);
+            cap_scores(x, a, in, out);
           } else {
 #pragma unroll
             for (int e = 0; e < 32; ++e) x[e] *= in;
@@ -499,7 +512,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       };
       float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};  // reference maxima (log2 units), this lane's sums
       for (int k = 0; k < tiles; ++k, ++c) {
-        const int t = from + k * ways, key = t * kKeys;
+        const int t = from + k * step, key = t * kKeys;
         if (!wait(&S.s_full[slot], c & 1, abort)) {
           give_up(S, a.status);
           stop = true;
@@ -577,7 +590,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
         if (key + kKeys > nk) {  // V's rows behind the last key
-          const int g = item.g0 + t - item.t0, st = g % kStages;
+          const int g = item.g0 + first_tile + k * ways, st = g % kStages;
           if (!wait(&S.kv_full[st], (g / kStages) & 1, abort)) {
             give_up(S, a.status);
             stop = true;
@@ -650,7 +663,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(v[e]) * by0[e >> 1 & 1];
           }
-          if (ways > 1 && from + 1 < min(item.t1, item.n[part])) {
+          if (ways > 1 && item.t0 + 1 < last) {
             uint32_t v[32];
             RESS_TMEM_LD16X64(tm + kColSlot + kColO, v);
 #pragma unroll
@@ -658,7 +671,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            const int r = r0 + 8 * j, t = r / G, head = item.h * G + r % G;
+            const int r = r0 + 8 * j, t = S.row_token[r], head = item.h * G + S.row_head[r];
             const int64_t q = (int64_t)item.q0 + tok0 + t;
             if (item.part >= 0) {
               float* to = a.part + item.part * kPartFloats + part * 128 + r;
@@ -669,7 +682,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if ((lane & 3) == 0) to[kRows * 64] = m[j], to[kRows * 65] = l[j];
               }
             } else {
-              const float inv = l[j] == 0.f ? 0.f : 1.0f / l[j];
+              const float inv = l[j] == 0.f ? 0.f : __fdividef(1.0f, l[j]);
               uint32_t w[8];
 #pragma unroll
               for (int e = 0; e < 8; ++e) w[e] = pack2<kF16>(o[4 * e + 2 * j] * inv, o[4 * e + 2 * j + 1] * inv);
@@ -682,7 +695,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 dst[0] = make_uint4(w[0], w[1], w[2], w[3]);
                 dst[4] = make_uint4(w[4], w[5], w[6], w[7]);
                 if (a.lse && (lane & 3) == 0)
-                  a.lse[head * a.rows + q] = l[j] == 0.f ? -INFINITY : (m[j] + log2f(l[j])) * 0.6931471805599453f;
+                  a.lse[head * a.rows + q] = l[j] == 0.f ? -INFINITY : (m[j] + lg2(l[j])) * 0.6931471805599453f;
               }
             }
             __syncwarp();
@@ -745,7 +758,7 @@ __global__ void __launch_bounds__(256) k_flash_join(const __grid_constant__ Dens
     const int head = item.head * G + (row & 127) % G;
     uint2* dst = reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.o.data) + q * a.o.token_stride + head * a.o.head_stride);
     dst[sub] = make_uint2(pack2<kF16>(o.x * inv, o.y * inv), pack2<kF16>(o.z * inv, o.w * inv));
-    if (a.lse && sub == 0) a.lse[head * a.rows + q] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+    if (a.lse && sub == 0) a.lse[head * a.rows + q] = l == 0.f ? -INFINITY : (m + lg2(l)) * 0.6931471805599453f;
   }
 }
 
@@ -800,7 +813,9 @@ int dense_ctas() {
 
 size_t dense_part_bytes() { return (size_t)kMaxCtas * 2 * kPartFloats * 4; }
 
-cudaError_t launch_flash(const DenseArgs& a, cudaStream_t st) {
+cudaError_t launch_flash(const DenseArgs& args, cudaStream_t st) {
+  DenseArgs a = args;
+  if (a.cap > 0.f) set_cap(a);
   CUtensorMap tq, tk, tv;
   // a tensor without keys is not read, but needs a map
   const int64_t keys = a.table ? a.page : a.keys > 0 ? a.keys : 1, pages = a.table ? a.n_pages : 1;

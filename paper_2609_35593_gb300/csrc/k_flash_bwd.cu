@@ -75,13 +75,6 @@ __device__ __forceinline__ void give_up(Smem& S, uint32_t* status) {
   *reinterpret_cast<volatile int*>(&S.abort) = 1;
 }
 
-__device__ __forceinline__ void mul2(float& d0, float& d1, float a0, float a1, float b0, float b1) {
-  asm("{\n\t.reg .b64 ra, rb, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\t"
-      "mul.rn.f32x2 rd, ra, rb;\n\tmov.b64 {%0, %1}, rd;\n\t}"
-      : "=f"(d0), "=f"(d1)
-      : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
-}
-
 // The power of two that brings the largest |dO| to 1..2 (1 where there is none, or it is not finite).
 __device__ __forceinline__ float grad_scale(const float* big, int n) {
   float m = 0.f;
@@ -521,7 +514,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!kKeys) least = __reduce_min_sync(0xffffffffu, least);
       for (int k = 0; k < tiles; ++k, ++c) {
         const int g = item.g0 + k, st = g % kStages, t = item.t0 + k, key = t * kCols;
-        if (!wait(&S.kv_full[st], (g / kStages) & 1, abort) || !wait(&S.s_full, c & 1, abort)) {
+        // (the columns' numbers are there, and in the other pass nothing but S is looked at before the tail)
+        if ((kKeys && !wait(&S.kv_full[st], (g / kStages) & 1, abort)) || !wait(&S.s_full, c & 1, abort)) {
           give_up(S, a.status);
           stop = true;
           break;
@@ -542,6 +536,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane == 0) mbar_arrive(&S.s_free);  // S is in registers: that of the next tile may come
         __syncwarp();
         // P
+        if (kGen && cap > 0.f) cap_scores(x, a, in, out);
 #pragma unroll
         for (int e = 0; e < 32; e += 2) {
           const int j = e >> 1 & 1, col = 64 * side + 8 * (e >> 2) + two;  // row, columns col and col + 1
@@ -554,7 +549,6 @@ __global__ void __launch_bounds__(kThreads, 1)
           float c0 = 1.f, c1 = 1.f;
           if (kGen) {
             if (cap > 0.f) {
-              capped2(x0, x1, in, out);
               float u0, u1;
               mul2(u0, u1, x0, x1, back, back);
               fma2(c0, c1, -u0, -u1, u0, u1, 1.f, 1.f);
@@ -628,6 +622,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         // rows of the tile that are not this sequence's, which the sums run over
         const int valid = kKeys ? (item.nq - item.from - t * T) * G : nk - key;
         if (valid < (kKeys ? T * G : kCols)) {
+          if (!kKeys && !wait(&S.kv_full[st], (g / kStages) & 1, abort)) {
+            give_up(S, a.status);
+            stop = true;
+            break;
+          }
           if (side == 0)
             zero_rows(S.B1[st], valid, (idx & 7) * 32 + lane);
           else if (kKeys)
@@ -755,6 +754,7 @@ static cudaError_t launch_type(DenseArgs a, cudaStream_t st) {
     if ((e = launch_pdl(k_flash_rows<kF16>, dim3(a.n_big), 256, 0, st, true, a)) != cudaSuccess) return e;
   }
   const bool gen = a.cap > 0.f || a.slopes;
+  if (a.cap > 0.f) set_cap(a);
   // a tensor without rows or keys is not read, but its map needs some memory
   ress_heads q = a.q, g = a.d_o, k = a.k, v = a.v;
   if (a.rows == 0) q = g = k, q.head_stride = g.head_stride = 64;
