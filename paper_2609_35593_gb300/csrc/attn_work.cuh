@@ -24,7 +24,7 @@ using namespace ptx;
 
 constexpr int kMaxCtas = kDenseMaxCtas;
 constexpr int kTile = 64;                // columns of a tile
-constexpr int64_t kOver = 8 * 2 * kTile; // an item's loads and epilogue, as work: two tiles
+constexpr int64_t kOver = 8 * 6 * kTile; // an item's loads and epilogue, as work: three tiles of 128 keys
 constexpr int64_t kLeast = 8 * 4 * kTile;  // least share of a CTA: four tiles
 constexpr uint64_t kWaitNs = 2000000000ull;  // 2 s per wait
 constexpr uint64_t kDrainNs = 200000000ull;  // 0.2 s to drain after an abort

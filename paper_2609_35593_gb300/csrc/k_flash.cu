@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = S.tmem_base;
   rows::stream_acquire();
-  auto line_of = [&](const Seq& s) { return row_line(a, s, kSlots * T, [&](int n) { return n > T ? 8 : 5; }); };
+  auto line_of = [&](const Seq& s) { return row_line(a, s, kSlots * T, [&](int n) { return n > T ? 8 : 6; }); };
   Range range;  // (of the producer)
   if (a.n_seqs > 32) range = find_range(a, line_of, gridDim.x, blockIdx.x, S.scratch, blockIdx.x == 0 ? a.status : nullptr);
 

@@ -30,7 +30,7 @@ using namespace work;
 namespace {
 
 constexpr int kThreads = 640, kStages = 4, kItems = 4, kCols = 128;
-constexpr int kProducer = 0, kIssueS = 1, kIssueP = 2, kIssueDs = 3, kElem = 4;  // warps
+constexpr int kProducer = 0, kIssueS = 1, kIssueDs = 3, kElem = 4;  // warps (2: issuer of the sums over P)
 constexpr uint32_t kTileBytes = kCols * 128;
 constexpr uint32_t kColDp = 128, kColP = 256, kColDs = 320, kColAcc1 = 384, kColAcc2 = 448;  // TMEM; S at 0
 constexpr int kFirst = 1, kLast = 2, kTerm = 4, kMask = 8;

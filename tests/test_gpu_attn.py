@@ -256,6 +256,44 @@ def test_bad_pages_are_told():
     assert (o[2:] == 0).all() and (o[:2] != 0).any()
 
 
+def test_a_cache_past_32_bit_offsets():
+    """2.1 million rows of 16 heads: 2^31 elements and more, pages of the sequences at both ends; and K, V written there."""
+    page, kv, pages = 256, 16, 8300
+    kp, vp = (torch.zeros(pages, page, kv, 64, dtype=BF16, device="cuda") for _ in range(2))
+    assert kp.numel() > 2 ** 31
+    lens = ([3, 70], [600, 300])
+    q, k, v = problem(*lens, 16, kv)
+    table = ints([pages - 1, 0, pages - 3, 1, pages - 2, 2]).view(2, 3)
+    at = torch.cat([table[b, torch.arange(n, device="cuda") // page] * page + torch.arange(n, device="cuda") % page
+                    for b, n in enumerate(lens[1])]).int()
+    ws, ws2 = workspace(73, 16), torch.zeros(256, dtype=torch.uint8, device="cuda")
+    ress.cache_write(k, v, at, kp, vp, ws2)
+    ress.status(ws2)
+    assert torch.equal(kp.view(-1, kv, 64)[at.long()], k) and torch.equal(vp.view(-1, kv, 64)[at.long()], v)
+    o, lse = torch.empty_like(q), torch.empty(16, 73, device="cuda")
+    ress.paged_attn(q, kp, vp, table, ints(lens[1]), o, ws, R.starts(lens[0]), lse=lse, causal=True)
+    ress.status(ws)
+    check(q, k, v, *lens, (o, lse), causal=True)
+
+
+def test_packed_rows_past_32_bit_offsets():
+    """Two sequences at the ends of tensors of more than 2^31 elements."""
+    n, heads = (1 << 25) + 300, 1
+    q, k, v, o = (torch.zeros(n, heads, 64, dtype=BF16, device="cuda") for _ in range(4))
+    a, b = 130, n - 170
+    for i, t in enumerate((q, k, v)):
+        t[:a], t[b:] = normal(i, a, heads, 64), normal(9 + i, n - b, heads, 64)
+    # between them keys without rows, and rows without keys
+    starts, k_starts = ints([0, a, a, b, n]), ints([0, a, b, b, n])
+    lse, ws = torch.zeros(heads, n, device="cuda"), workspace(n, heads)
+    ress.attn(q, k, v, o, ws, starts, k_starts, lse=lse)
+    ress.status(ws)
+    for part in (slice(0, a), slice(b, n)):
+        m = part.stop - part.start
+        check(q[part], k[part], v[part], [m], [m], (o[part], lse[:, part]))
+    assert (o[a:b] == 0).all()
+
+
 def tables_of(have, add, free, taken, table, page):
     """What cache_tables is to give, one token after another."""
     table, slots, pos, starts = table.tolist(), [], [], [0]
