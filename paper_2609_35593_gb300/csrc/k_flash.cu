@@ -505,7 +505,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
         }
-        if (first + 64 > least) {
+        if (__any_sync(0xffffffffu, first + 64 > least)) {  // (the vote keeps this a branch, not selects)
 #pragma unroll
           for (int e = 0; e < 32; ++e) x[e] = 8 * (e >> 2) + (e & 1) < lim[e >> 1 & 1] - first - two ? x[e] : -INFINITY;
         }
