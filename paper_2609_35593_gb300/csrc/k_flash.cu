@@ -52,8 +52,7 @@ struct Item {
   int h, tok;                   // head of K (-1: no more items), first token of the sequence
   int t0, t1, g0;            // tiles; number of the first among all of the CTA's
   int n[kSlots];             // tiles of each 128 rows' keys
-  int parts;                 // 128 rows that the item has, 1 or 2: slot s takes part s mod `parts` and,
-  int ways;                  // of that, every `ways`th tile
+  int ways;                  // 1: slot s takes 128 rows s; 2: there are only 128 rows, of which the slots take tiles in turn
   int part;                  // slot of partial results, or -1: whole
 };
 
@@ -95,7 +94,6 @@ __device__ __forceinline__ int item_tiles(const DenseArgs& a, const Seq& q, int 
   for (int s = 0; s < kSlots; ++s) n = max(n, part_tiles(a, q, tok, s, T));
   return n;
 }
-__device__ __forceinline__ int ways_of(int parts) { return parts == 1 ? kSlots : 1; }
 
 }  // namespace
 
@@ -183,8 +181,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             item.q0 = c.s.q0, item.nq = c.s.nq, item.k0 = c.s.k0, item.nk = c.s.nk, item.d = c.s.d, item.p = c.s.p;
             item.h = c.h, item.b = c.b, item.tok = tok, item.t0 = t0, item.t1 = t1;
             for (int s = 0; s < kSlots; ++s) item.n[s] = part_tiles(a, c.s, tok, s, T);
-            item.parts = min(kSlots, (c.s.nq - tok + T - 1) / T);
-            item.ways = ways_of(item.parts);
+            item.ways = c.s.nq - tok > T ? 1 : kSlots;
             item.part = t0 == 0 && t1 == n ? -1 : share_slot(c, range.x0);
             if (item.part >= 0)
               a.share[item.part] = DenseShare{t0, t1, n, c.h, c.s.q0 + tok, min(c.s.nq - tok, kSlots * T), {}};
@@ -220,8 +217,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int h = item.h, nk = item.nk, t0 = item.t0, t1 = item.t1, k0 = item.k0;
           const int32_t* table = a.table ? a.table + item.b * a.table_stride : nullptr;
           // the first lanes: what slot `lane` takes of the item
-          const int parts = item.parts, ways = item.ways, mine_part = lane % parts, way = lane / parts;
-          const int last = lane < kSlots && way < ways ? min(t1, item.n[mine_part]) : 0;
+          const int ways = item.ways, mine_part = ways > 1 ? 0 : lane, way = ways > 1 ? lane : 0;
+          const int last = lane < kSlots ? min(t1, item.n[mine_part]) : 0;
           const uint32_t some = __ballot_sync(0xffffffffu, t0 + way < last);
           // slopes: the nearest keys of a causal row first, or the reference would be raised from tile to tile
           const int step = a.slopes ? -1 : 1, begin = a.slopes ? t1 - 1 : t0;
@@ -234,7 +231,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             if (lane == 0) {
               mbar_arrive_expect_tx(&S.q_full[buf][s], T * G * 128);
-              tma_load_4d(S.Q[buf][s], &tmQ, &S.q_full[buf][s], 0, 0, h, item.q0 + item.tok + s % parts * T);
+              tma_load_4d(S.Q[buf][s], &tmQ, &S.q_full[buf][s], 0, 0, h, item.q0 + item.tok + (ways > 1 ? 0 : s * T));
             }
             __syncwarp();
             // from 252 on at 248, which is the same modulo 4
@@ -465,9 +462,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       const Item& item = S.item[i];
       if (item.h < 0) break;
-      const int parts = item.parts, ways = item.ways, part = slot % parts, way = slot / parts, nk = item.nk;
+      const int ways = item.ways, part = ways > 1 ? 0 : slot, way = ways > 1 ? slot : 0, nk = item.nk;
       const int ntok = part_tokens(item.nq, item.tok, part, T), tok0 = item.tok + part * T;
-      const int last = min(item.t1, item.n[part]), tiles = max(0, last - item.t0 - way + ways - 1) / ways;
+      const int last = min(item.t1, item.n[part]), tiles = ways > 1 ? max(0, last - item.t0 - way + 1) >> 1 : max(0, last - item.t0);
+      static_assert(kSlots == 2, "two slots take turns");
       // tile k of this slot is the (first + ways k)-th that comes, tile from + step k
       const int first_tile = ways > 1 ? way : a.slopes ? item.t1 - last : 0, step = a.slopes ? -ways : ways;
       const int from = a.slopes ? item.t1 - 1 - first_tile : item.t0 + first_tile;
@@ -637,7 +635,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           break;
         }
       } else {
-        float by0[2] = {1.f, 1.f}, by1[2] = {0.f, 0.f};
+        float by0[2], by1[2];
         if (ways > 1) {
           if (!wait(&S.other_full[idx & 7], turn & 1, abort)) {
             give_up(S, a.status);
@@ -661,13 +659,16 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int e = 0; e < 32; ++e) v[e] = 0u;
             if (tiles > 0) RESS_TMEM_LD16X64(tm + kColO, v);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(v[e]) * by0[e >> 1 & 1];
+            for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(v[e]);
           }
-          if (ways > 1 && item.t0 + 1 < last) {
+          if (ways > 1) {
             uint32_t v[32];
-            RESS_TMEM_LD16X64(tm + kColSlot + kColO, v);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = fmaf(__uint_as_float(v[e]), by1[e >> 1 & 1], o[e]);
+            for (int e = 0; e < 32; ++e) v[e] = 0u;
+            if (item.t0 + 1 < last) RESS_TMEM_LD16X64(tm + kColSlot + kColO, v);
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              o[e] = fmaf(__uint_as_float(v[e]), by1[e >> 1 & 1], o[e] * by0[e >> 1 & 1]);
           }
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
