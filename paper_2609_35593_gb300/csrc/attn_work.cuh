@@ -220,17 +220,22 @@ __device__ __forceinline__ void seek(const DenseArgs& a, LineOf line_of, int64_t
   const int64_t one = c.l.before(c.l.n), rem = x - base;
   c.h = (int)quotient(rem, one);
   const int64_t r = rem - c.h * one;
-  int lo = 0, hi = c.l.n - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) / 2;
-    if (c.l.before(mid) <= r)
-      lo = mid;
-    else
-      hi = mid - 1;
+  // The item that holds r: by the line's formula in float, put right by the exact sums.
+  int j;
+  const float each = (float)(kOver + 8 * c.l.a);
+  if ((float)r < each * (float)c.l.cnt || c.l.step == 0) {
+    j = (int)((float)r / each);
+  } else {  // each cnt + (m - cnt) (kOver + 8 b) + 4 step (m (m - 1) - cnt (cnt - 1)) = r
+    const float n = (float)c.l.cnt, s4 = 4.f * (float)c.l.step, lin = (float)(kOver + 8 * c.l.b) - s4;
+    const float rest = each * n - n * (float)(kOver + 8 * c.l.b) - s4 * n * (n - 1.f) - (float)r;
+    j = (int)((-lin + sqrtf(fmaxf(lin * lin - 4.f * s4 * rest, 0.f))) / (2.f * s4));
   }
-  c.j = lo;
-  c.start = base + c.h * one + c.l.before(lo);
-  c.weight = c.l.before(lo + 1) - c.l.before(lo);
+  j = max(0, min(j, c.l.n - 1));
+  while (j > 0 && c.l.before(j) > r) --j;
+  while (j < c.l.n - 1 && c.l.before(j + 1) <= r) ++j;
+  c.j = j;
+  c.start = base + c.h * one + c.l.before(j);
+  c.weight = c.l.before(j + 1) - c.l.before(j);
 }
 // The next item (false: there is none).
 template <class LineOf>

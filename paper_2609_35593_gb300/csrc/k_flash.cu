@@ -161,7 +161,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t loads = 0;  // times that each slot's Q was loaded, a byte per slot
       bool failed = false;
       const int box = a.table ? min(kKeys, a.page & -a.page) : kKeys;  // the page's power of two
-      const int boxes = kKeys / box;
+      const int boxes = kKeys / box, page_shift = (a.page & (a.page - 1)) == 0 ? __ffs(a.page) - 1 : -1;
         if (lane == 0) a.share[2 * blockIdx.x].n = a.share[2 * blockIdx.x + 1].n = -1;
       // The next item that this share has tiles of, to S.next (h -1: none left).  One lane looks for it, in shared
       // memory: the sequences' arithmetic in 64 bits would otherwise take the registers of the tile loop.
@@ -245,9 +245,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int key = t * kKeys + at;
             row = k0 + key, page = 0;
             if (!table) return;
-            row = key % a.page, page = (int)a.n_pages;  // no such page: TMA fills in zeros
+            const int col = page_shift >= 0 ? key >> page_shift : key / a.page;
+            row = key - col * a.page, page = (int)a.n_pages;  // no such page: TMA fills in zeros
             if (mine && key < nk) {
-              const int id = table[key / a.page];
+              const int id = table[col];
               if (id >= 0 && id < a.n_pages)
                 page = id;
               else

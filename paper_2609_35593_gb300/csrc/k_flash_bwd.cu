@@ -57,6 +57,7 @@ struct __align__(1024) Smem {
   uint8_t B1[kStages][kTileBytes];
   uint8_t B2[kStages][kTileBytes];
   Cols cols[kStages];
+  uint8_t row_token[128], row_head[128];  // of 128 rows of Q
   uint64_t kv_full[kStages], kv_empty[kStages];
   uint64_t a_full[2], a_empty[2], drain[3];
   uint64_t s_full, s_free, dp_full, dp_free, p_full, p_done, acc_full, acc_empty;
@@ -200,6 +201,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       reinterpret_cast<uint4*>(S.B1)[f] = make_uint4(0u, 0u, 0u, 0u);
     fence_proxy_async_smem();
   }
+  if (const int r = (int)threadIdx.x - 512; r >= 0) S.row_token[r] = r / G, S.row_head[r] = r % G;
   if (warp == kIssueS) tmem_alloc(&S.tmem_base, 512);
   tc_fence_before();
   __syncthreads();
@@ -500,15 +502,15 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const int r = r0 + 8 * j;
-        tok[j] = item.at + (kKeys ? r : r / G);
-        exists[j] = kKeys ? tok[j] < nk : r / G < T && tok[j] < item.nq;
+        tok[j] = item.at + (kKeys ? r : S.row_token[r]);
+        exists[j] = kKeys ? tok[j] < nk : S.row_token[r] < T && tok[j] < item.nq;
         pos[j] = item.d + tok[j];
         if (!kKeys && exists[j]) {
-          const float2 x = a.stat[((int64_t)item.h * a.rows + item.q0 + tok[j]) * G + r % G];
+          const float2 x = a.stat[((int64_t)item.h * a.rows + item.q0 + tok[j]) * G + S.row_head[r]];
           nlse[j] = (kF16 ? kPScale : 0.f) - x.x, ndelta[j] = -x.y * f;
           lim[j] = a.causal ? max(0, min(nk, max(item.p, pos[j] + 1))) : nk;
           least = min(least, lim[j]);
-          if (kGen && a.slopes) slope[j] = a.slopes[item.h * G + r % G] * kLog2e;
+          if (kGen && a.slopes) slope[j] = a.slopes[item.h * G + S.row_head[r]] * kLog2e;
         }
       }
       if (!kKeys) least = __reduce_min_sync(0xffffffffu, least);
@@ -692,7 +694,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           transpose4(w[4], w[5], w[6], w[7], lane);
           if (exists[j]) {
             const int64_t token = (int64_t)(kKeys ? item.k0 : item.q0) + tok[j];
-            const int head = kKeys ? item.h : item.h * G + r % G;
+            const int head = kKeys ? item.h : item.h * G + S.row_head[r];
             uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(to.data) + token * to.token_stride +
                                                   head * to.head_stride) + (lane & 3);
             dst[0] = make_uint4(w[0], w[1], w[2], w[3]);

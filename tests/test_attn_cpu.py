@@ -1,5 +1,4 @@
-"""Refusals of the dense attention and of the cache, at the C ABI and in the binding: nothing is launched.  And the closed
-forms by which the attention shares its work."""
+"""Refusals of the dense attention and of the cache, at the C ABI and in the binding: nothing is launched."""
 import ctypes
 
 import pytest
