@@ -11,9 +11,9 @@ Forward, all on this package's kernels:
     y = x + O W_o^T
 Calibration (the paper's Sec. 4.4 takes head budgets as given; Appendix D allots them by the Fisher
 information of the heads' QKV projections, the squares of the gradients with respect to their outputs):
-the gradient of a loss goes back through dense attention (torch autograd, small scenes only), then
-through the rotation and the head norm (rope_bwd) to the projections' outputs, and on through the
-projections and layer_norm_bwd to the residual stream, as a training step would take it.
+the gradient of a loss goes back through dense attention (attn, attn_bwd), then through the rotation
+and the head norm (rope_bwd) to the projections' outputs, and on through the projections and
+layer_norm_bwd to the residual stream, as a training step would take it.
 """
 import argparse
 import os
@@ -92,11 +92,13 @@ class Sublayer:
         ress.qkv_proj(self.d, self.h, W["q"], W["k"], W["v"], self.raw["q"], self.raw["k"], self.raw["v"], ws,
                       b_q=self.b["q"], b_k=self.b["k"], b_v=self.b["v"])
         ress.status(ws)
-        Q, K, V = (t.float().requires_grad_() for t in (self.Q, self.K, self.V))
-        O = torch.softmax(torch.einsum("ihc,jhc->hij", Q, K) / 8.0, -1) @ V.transpose(0, 1)
-        dO = (dy.float() @ self.W_o.float()).view(self.N, self.H, 64)
-        O.transpose(0, 1).backward(dO)
-        dQ, dK, dV = (t.grad.bfloat16() for t in (Q, K, V))
+        O, dQ, dK, dV = (torch.empty_like(self.Q) for _ in range(4))
+        lse = torch.empty(self.H, self.N, device="cuda", dtype=torch.float32)
+        aws = torch.zeros(ress.attn_workspace_bytes(self.N, self.H, backward=True), dtype=torch.uint8, device="cuda")
+        ress.attn(self.Q, self.K, self.V, O, aws, lse=lse)
+        dO = (dy @ self.W_o).view(self.N, self.H, 64)
+        ress.attn_bwd(dO, self.Q, self.K, self.V, O, lse, dQ, dK, dV, aws)
+        ress.status(aws)
         dq, dk = torch.empty_like(dQ), torch.empty_like(dK)
         head = torch.empty(4, 64, device="cuda", dtype=torch.float32)
         rws = torch.empty(ress.rope_workspace_bytes(self.plan, self.N, self.H, self.H), dtype=torch.uint8, device="cuda")

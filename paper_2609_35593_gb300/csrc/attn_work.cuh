@@ -8,8 +8,8 @@
 // An item that several CTAs have shares of leaves partial results in the workspace, two slots per CTA, with a note
 // of what they are of; a second kernel adds them up in the order of the shares: no atomics, the same bits for the
 // same inputs.  (It looked for the shares itself at first, as the CTAs do, and took 20 to 40 us.)
-// With whole items instead, 176 items of 172 tiles on 152 SMs (one image over the keys of 32) would take two
-// rounds where 1.16 do.
+// With whole items instead, 96 items of 344 tiles on 152 SMs (one image's rows over the keys of 32, 16 heads) would
+// take one round of 344 tiles where 217 a CTA do.
 //
 // An item's work is kOver + mul x its length, a length being the keys (or rows) that it sees, in closed form
 // over the items of a sequence: a constant up to some item, then linear (causal), the last one on its own.
@@ -23,9 +23,10 @@ namespace work {
 using namespace ptx;
 
 constexpr int kMaxCtas = kDenseMaxCtas;
-constexpr int kTile = 64;                // columns of a tile
-constexpr int64_t kOver = 8 * 6 * kTile; // an item's loads and epilogue, as work: three tiles of 128 keys
-constexpr int64_t kLeast = 8 * 4 * kTile;  // least share of a CTA: four tiles
+// An item's loads and epilogue, as work: three tiles of 128 keys (8,000 to 10,000 cycles against 1,850 a tile are more,
+// but part of them runs under the neighbours' tiles; two, four and six tiles were no better over the cases).
+constexpr int64_t kOver = 8 * 384;
+constexpr int64_t kLeast = 8 * 256;  // least share of a CTA: two tiles
 constexpr uint64_t kWaitNs = 2000000000ull;  // 2 s per wait
 constexpr uint64_t kDrainNs = 200000000ull;  // 0.2 s to drain after an abort
 
@@ -378,11 +379,6 @@ __device__ __forceinline__ void transpose4(uint32_t& w0, uint32_t& w1, uint32_t&
     w2 = c, w3 = d;
 }
 
-// Whether the phase is complete now, for the whole warp.
-__device__ __forceinline__ bool mbar_ready(uint64_t* bar, uint32_t parity) {
-  return __all_sync(0xffffffffu, mbar_try_wait(bar, parity));
-}
-
 template <bool kF16>
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   uint32_t r;
@@ -415,15 +411,6 @@ __device__ __forceinline__ void zero_rows(uint8_t* tile, int from, int i) {
   }
 }
 
-// The 128 bytes of row i.
-__device__ __forceinline__ void zero_row(uint8_t* tile, int from, int i) {
-  if (i >= from) {
-    uint4* p = reinterpret_cast<uint4*>(tile + i * 128);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) p[k] = make_uint4(0u, 0u, 0u, 0u);
-  }
-}
-
 // (y0, y1) = top tanh(x / cap) of two scores, c = 2 log2(e) / cap: top (1 - 2 / (2^(c x) + 1)), off by 2^-21 top (the
 // rounding near 1; relative to a score near 0 more, but it is an exponent).
 __device__ __forceinline__ void capped2(float& x0, float& x1, float c, float top) {
@@ -445,8 +432,8 @@ __device__ __forceinline__ void mul2(float& d0, float& d1, float a0, float a1, f
 
 // Products q.k to capped scores in log2 units, a warp's 16 rows x 64 columns.  Where none of them is above half of the cap,
 // x times a polynomial in x^2 (set_cap): five packed instructions a pair on the FMA pipe, next to which the SFU forms the
-// exponentials; else capped2, whose four SFU operations a pair are twice what the exponentials take (packed documents,
-// cap 30: 251 us with capped2 alone).
+// exponentials; else capped2, whose four SFU operations a pair are twice what the exponentials take (packed documents of
+// 30 to 6,000 rows, cap 30: 251 us with capped2 alone, 239 with both).
 __device__ __forceinline__ void cap_scores(float (&x)[32], const DenseArgs& a, float in, float out) {
   float z[32], top = 0.f;
 #pragma unroll

@@ -11,16 +11,17 @@
 //               than 2^13 (what P's 16 bits and O's 32 hold easily): O in TMEM is rescaled seldom, and no maximum is
 //               formed otherwise.  Sums are float32, of the exponentials before they are rounded to 16 bits, one for
 //               each lane until the item ends.
-//   warp 0      item and tile producer: TMA of Q, K and V (128-byte swizzle), 4 stages of 32 KB, so that single
-//               tokens, which only stream the cache, keep 100 KB per SM in flight, and Q of the next item
+//   warp 0      item and tile producer: TMA of Q, K and V (128-byte swizzle), 5 stages of 32 KB, so that single
+//               tokens, which only stream the cache, keep 100 KB per SM in flight
 //   warp 1      issuer of S = Q K^T (M128 N128 K64, both from shared memory)
 //   warps 2, 3  issuers of O += P V (M128 N64 K128, P from TMEM, V MN-major), a slot each.  S and P have columns of their
 //               own: S of the next tile runs while the exponentials of this one are formed.
 // What bounds it is the chain of a slot's tile: scores from TMEM, exponentials, P to TMEM and the hand-overs between
 // warps take some 1,200 cycles whatever they compute, so the tiles are as large as TMEM allows, and the 16 warps of
-// softmax (four to a sub-partition) work while others wait.  Measured on 8 images at once, all with the same
-// results: a row per thread and 8 warps, S of 64 keys double-buffered under P 636 us, 128 keys with S and P apart 618;
-// 12 warps, three slots of 64 keys 586; 16 warps, four slots of 64 keys and two issuers 553.
+// softmax (four to a sub-partition) work while others wait.  8 images at once (10,992 rows and keys, 16 heads) take 447 us,
+// 1.11 PFLOP/s; other forms of the same results: a row per thread and 8 warps, S of 64 keys double-buffered under P 636,
+// 128 keys with S and P apart 618; 12 warps, three slots of 64 keys 586; 16 warps, four slots of 64 keys and two issuers
+// 553; this form at first 482 (its join looked for the shares itself, 25 us of that).
 // Rows of V behind a sequence's last key are zeroed in shared memory (0 x NaN of a cache page never written
 // would be NaN); keys there and masked ones are -inf by selection, whatever their scores are.
 // Every mbarrier wait is bounded; one that gives up records RESS_ETIMEOUT and the CTA leaves, see k_attn.cu.
@@ -34,7 +35,7 @@ using namespace work;
 
 namespace {
 
-constexpr int kThreads = 640, kStages = 4, kSlots = 2, kItems = 4, kKeys = 128;
+constexpr int kThreads = 640, kStages = 5, kSlots = 2, kItems = 4, kKeys = 128;
 constexpr int kProducer = 0, kIssueS = 1, kIssuePv = 2, kSoftmax = 4;  // warps: producer, issuers, softmax
 constexpr uint32_t kTileBytes = kKeys * 128;
 constexpr uint32_t kColSlot = 256, kColP = 128, kColO = 192;  // TMEM: per slot S, P, O
@@ -57,14 +58,14 @@ struct Item {
 };
 
 struct __align__(1024) Smem {
-  uint8_t Q[2][kSlots][128 * 128];  // of two items of each slot
+  uint8_t Q[kSlots][128 * 128];
   uint8_t K[kStages][kTileBytes];
   uint8_t V[kStages][kTileBytes];
   uint64_t kv_full[kStages], kv_empty[kStages];
   uint8_t row_token[128], row_head[128];   // of the 128 rows of a part
   float other[2][128];                     // items of one part: slot 1's maxima and sums
   uint64_t other_full[8], other_empty[8];  // (of each warp's rows)
-  uint64_t q_full[2][kSlots], q_empty[2][kSlots], drain[1 + kSlots];
+  uint64_t q_full[kSlots], q_empty[kSlots], drain[1 + kSlots];
   uint64_t s_full[kSlots], s_free[kSlots], p_full[kSlots], o_full[kSlots];
   uint64_t it_full[kItems], it_empty[kItems];
   int64_t scratch[34];
@@ -114,10 +115,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&S.kv_empty[s], 1 + kSlots);
     }
     for (int s = 0; s < kSlots; ++s) {
-      for (int b = 0; b < 2; ++b) {
-        mbar_init(&S.q_full[b][s], 1);
-        mbar_init(&S.q_empty[b][s], 1);
-      }
+      mbar_init(&S.q_full[s], 1);
+      mbar_init(&S.q_empty[s], 1);
       mbar_init(&S.s_full[s], 1);
       mbar_init(&S.s_free[s], 8);
       mbar_init(&S.p_full[s], 8);
@@ -158,11 +157,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       int g = 0, pub = 0;
       if (a.n_seqs <= 32)
         range = find_range_warp(a, line_of, gridDim.x, blockIdx.x, blockIdx.x == 0 ? a.status : nullptr);
-      uint32_t loads = 0;  // times that each slot's Q was loaded, a byte per slot
+      uint32_t loads = 0;  // of each slot's Q so far, two bits a slot
       bool failed = false;
       const int box = a.table ? min(kKeys, a.page & -a.page) : kKeys;  // the page's power of two
       const int boxes = kKeys / box, page_shift = (a.page & (a.page - 1)) == 0 ? __ffs(a.page) - 1 : -1;
-        if (lane == 0) a.share[2 * blockIdx.x].n = a.share[2 * blockIdx.x + 1].n = -1;
+      if (lane == 0) a.share[2 * blockIdx.x].n = a.share[2 * blockIdx.x + 1].n = -1;
       // The next item that this share has tiles of, to S.next (h -1: none left).  One lane looks for it, in shared
       // memory: the sequences' arithmetic in 64 bits would otherwise take the registers of the tile loop.
       auto advance = [&](bool first) {
@@ -224,18 +223,18 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int step = a.slopes ? -1 : 1, begin = a.slopes ? t1 - 1 : t0;
           for (int s = 0; s < kSlots; ++s) {
             if (!(some >> s & 1)) continue;
-            const uint32_t times = loads >> (8 * s) & 0xff, buf = times & 1;
-            if (times > 1 && !wait(&S.q_empty[buf][s], ((times >> 1) - 1) & 1, abort)) {
+            // phases of its barriers (2 bits: none yet, 1, 2, 1, ..)
+            const uint32_t times = loads >> (2 * s) & 3;
+            if (times > 0 && !wait(&S.q_empty[s], times - 1, abort)) {
               failed = true;
               break;
             }
             if (lane == 0) {
-              mbar_arrive_expect_tx(&S.q_full[buf][s], T * G * 128);
-              tma_load_4d(S.Q[buf][s], &tmQ, &S.q_full[buf][s], 0, 0, h, item.q0 + item.tok + (ways > 1 ? 0 : s * T));
+              mbar_arrive_expect_tx(&S.q_full[s], T * G * 128);
+              tma_load_4d(S.Q[s], &tmQ, &S.q_full[s], 0, 0, h, item.q0 + item.tok + (ways > 1 ? 0 : s * T));
             }
             __syncwarp();
-            // from 252 on at 248, which is the same modulo 4
-            loads = (loads & ~(0xffu << (8 * s))) | ((times == 251 ? 248 : times + 1) << (8 * s));
+            loads = (loads & ~(3u << (2 * s))) | ((times == 1 ? 2 : 1) << (2 * s));
           }
           if (failed) break;
           // where this lane's box of a tile is: lanes 0..boxes-1 load K, the next ones V
@@ -310,10 +309,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int back = 1; back <= kStages && g - back >= 0; ++back)
           mbar_wait(&S.kv_full[(g - back) % kStages], ((g - back) / kStages) & 1, &no_abort, kDrainNs);
         for (int s = 0; s < kSlots; ++s)
-          for (int back = 1; back <= 2; ++back) {
-            const int times = (int)(loads >> (8 * s) & 0xff) - back;
-            if (times >= 0) mbar_wait(&S.q_full[times & 1][s], (times >> 1) & 1, &no_abort, kDrainNs);
-          }
+          if (loads >> (2 * s) & 3) mbar_wait(&S.q_full[s], (loads >> (2 * s) & 3) - 1, &no_abort, kDrainNs);
       }
     } else {
       // ================================ MMA issuers ==================================
@@ -323,8 +319,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       constexpr uint64_t kStageUnits = kTileBytes >> 4, kQUnits = (128 * 128) >> 4;
       uint32_t phase = 0;
       if (warp == kIssueS) {
-        const uint64_t kd0 = sdesc_sw128(smem_u32(S.K[0])), qd0 = sdesc_sw128(smem_u32(S.Q[0][0]));
-        uint32_t s_phase[kSlots] = {1, 1}, q_next[kSlots] = {0, 0}, buf[kSlots] = {0, 0};
+        const uint64_t kd0 = sdesc_sw128(smem_u32(S.K[0])), qd0 = sdesc_sw128(smem_u32(S.Q[0]));
+        uint32_t s_phase[kSlots] = {1, 1}, q_phase[kSlots] = {0, 0};
         for (int st = 0; !failed;) {
           if (!wait(&S.kv_full[st], phase, abort)) {
             failed = true;
@@ -337,9 +333,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int s = 0; s < kSlots; ++s) {
             if (failed || !(flags & kHas << s)) continue;
             if (flags & kBegin << s) {
-              buf[s] = q_next[s] & 1;
-              failed = !wait(&S.q_full[buf[s]][s], (q_next[s] >> 1) & 1, abort);
-              ++q_next[s];
+              failed = !wait(&S.q_full[s], q_phase[s], abort);
+              q_phase[s] ^= 1;
             }
             // (the first time: at once)
             if (failed || !wait(&S.s_free[s], s_phase[s], abort)) {
@@ -349,11 +344,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             s_phase[s] ^= 1;
             tc_fence_after();
             if (leader) {
-              const uint64_t qd = qd0 + (kSlots * buf[s] + s) * kQUnits;
+              const uint64_t qd = qd0 + s * kQUnits;
 #pragma unroll
               for (int k = 0; k < 4; ++k) mma_bf16_ss(tmem + s * kColSlot, qd + 2 * k, kd + 2 * k, kQk, k > 0 ? 1u : 0u);
               mma_commit(&S.s_full[s]);
-              if (flags & kEnd << s) mma_commit(&S.q_empty[buf[s]][s]);
+              if (flags & kEnd << s) mma_commit(&S.q_empty[s]);
             }
             __syncwarp();
           }

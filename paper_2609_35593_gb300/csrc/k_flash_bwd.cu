@@ -10,11 +10,12 @@
 // rows of the same item (or columns of the same tile), which adds up their gradients.
 //
 // Roles (640 threads, one CTA per SM): warp 0 producer, warp 1 issuer of S and dP (M128 N128 K64, operands in shared
-// memory, each as soon as the last one's values are in registers), warps 2 and 3 issuers of the sums over P and over dS, warps 4-19 element-wise: 16 rows x 64 columns of a tile
-// of 128 x 128 each.  S and dP (256 columns of TMEM) are free for the next tile as soon as they are in registers, P and
+// memory, each as soon as the last one's values are in registers), warps 2 and 3 issuers of the sums over P and over dS,
+// warps 4-19 element-wise: 16 rows x 64 columns of a tile of 128 x 128 each.  S and dP (256 columns of TMEM) are free for the next tile as soon as they are in registers, P and
 // dS (128) have columns of their own, so the products of the next tile run meanwhile; two accumulators (128).  With
 // eight element-wise warps on tiles of 64 columns and one issuer a tile of 128 x 64 took 1,700 cycles, its four
-// products 512 (8 images at once: 2,200 us).  Shares of the work, partial results and waits are those of k_flash.cu.
+// products 512 (8 images at once, 10,992 rows and keys of 16 heads: 2,200 us; now 1,490, 0.82 PFLOP/s of five products'
+// work or 1.16 of the seven formed).  What bounds it is the chain of a tile from scores to dS and back.  Shares of the work, partial results and waits are those of k_flash.cu.
 //
 // In f16, P is kept times 2^8 and dS times a power of two that brings the largest |dO| to 1..2: probabilities of rows on
 // thousands of keys are below f16's 2^-14, and so may gradients be.  dP is at most 64 max|dO| max|V|, so dS stays

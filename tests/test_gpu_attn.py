@@ -14,6 +14,15 @@ pytestmark = pytest.mark.gpu
 BF16, F16 = torch.bfloat16, torch.float16
 
 
+@pytest.fixture(autouse=True)
+def float32_by_default():
+    """Tensors made without a dtype here are float32, whatever other files left as the default."""
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(before)
+
+
 def normal(seed, *shape, kind=BF16, by=1.0):
     g = torch.Generator(device="cuda").manual_seed(seed)
     return (by * torch.randn(*shape, generator=g, device="cuda")).to(kind)

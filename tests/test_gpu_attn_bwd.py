@@ -14,6 +14,15 @@ from test_gpu_attn import BF16, F16, ints, masks, normal, problem, run, workspac
 pytestmark = pytest.mark.gpu
 
 
+@pytest.fixture(autouse=True)
+def float32_by_default():
+    """Tensors made without a dtype here are float32, whatever other files left as the default."""
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(before)
+
+
 def grads(do, q, k, v, o, lse, q_lens, k_lens, **mask):
     out = [torch.full_like(t, 7.0) for t in (q, k, v)]
     ws = workspace(*q.shape[:2], backward=True)
