@@ -15,6 +15,8 @@
 // over the items of a sequence: a constant up to some item, then linear (causal), the last one on its own.
 #pragma once
 
+#include <cfloat>
+
 #include "row_ops.cuh"
 #include "sm100_ptx.cuh"
 
@@ -435,19 +437,17 @@ __device__ __forceinline__ void mul2(float& d0, float& d1, float a0, float a1, f
 // exponentials; else capped2, whose four SFU operations a pair are twice what the exponentials take (packed documents of
 // 30 to 6,000 rows, cap 30: 251 us with capped2 alone, 239 with both).
 __device__ __forceinline__ void cap_scores(float (&x)[32], const DenseArgs& a, float in, float out) {
-  float z[32], top = 0.f;
+  float top = 0.f;
 #pragma unroll
-  for (int e = 0; e < 32; e += 2) {
-    mul2(z[e], z[e + 1], x[e], x[e + 1], x[e], x[e + 1]);
-    top = fmax3(top, z[e], z[e + 1]);
-  }
-  if (!__any_sync(0xffffffffu, !(top <= a.cap_square))) {
+  for (int e = 0; e < 32; e += 2) top = fmax3(top, fabsf(x[e]), fabsf(x[e + 1]));
+  if (!__any_sync(0xffffffffu, !(top <= a.cap_small))) {
 #pragma unroll
     for (int e = 0; e < 32; e += 2) {
-      float p0, p1;
-      fma2(p0, p1, z[e], z[e + 1], a.cap_poly[3], a.cap_poly[3], a.cap_poly[2], a.cap_poly[2]);
-      fma2(p0, p1, z[e], z[e + 1], p0, p1, a.cap_poly[1], a.cap_poly[1]);
-      fma2(p0, p1, z[e], z[e + 1], p0, p1, a.cap_poly[0], a.cap_poly[0]);
+      float z0, z1, p0, p1;
+      mul2(z0, z1, x[e], x[e + 1], x[e], x[e + 1]);
+      fma2(p0, p1, z0, z1, a.cap_poly[3], a.cap_poly[3], a.cap_poly[2], a.cap_poly[2]);
+      fma2(p0, p1, z0, z1, p0, p1, a.cap_poly[1], a.cap_poly[1]);
+      fma2(p0, p1, z0, z1, p0, p1, a.cap_poly[0], a.cap_poly[0]);
       mul2(x[e], x[e + 1], x[e], x[e + 1], p0, p1);
     }
   } else {
@@ -464,7 +464,7 @@ inline void set_cap(DenseArgs& a) {
   double scale = 0.125 * 1.4426950408889634;
   for (int k = 0; k < 4; ++k, scale *= u * u) a.cap_poly[k] = (float)(kFit[k] * scale);
   // (caps so small that the coefficients are beyond float32 have no such products)
-  a.cap_square = a.cap > 1e-3f ? (float)(0.25 / (u * u)) : -1.f;
+  a.cap_small = a.cap > 1e-3f ? (float)fmin(0.5 / u, (double)FLT_MAX) : -1.f;
 }
 
 }  // namespace work

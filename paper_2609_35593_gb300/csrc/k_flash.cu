@@ -137,7 +137,15 @@ __global__ void __launch_bounds__(kThreads, 1)
     prefetch_tensormap(&tmK);
     prefetch_tensormap(&tmV);
   }
-  if (const int r = (int)threadIdx.x - 512; r >= 0) S.row_token[r] = r / G, S.row_head[r] = r % G;
+  if (const int r = (int)threadIdx.x - 512; r >= 0) {
+    S.row_token[r] = r / G, S.row_head[r] = r % G;
+    // rows that no token fills stay 0: what was there before might be scores too large for the short way to cap them
+    if (r >= T * G) {
+#pragma unroll 1
+      for (int i = 0; i < kSlots * 8; ++i) reinterpret_cast<uint4*>(S.Q[i >> 3] + r * 128)[i & 7] = make_uint4(0u, 0u, 0u, 0u);
+      fence_proxy_async_smem();
+    }
+  }
   if (warp == kIssueS) tmem_alloc(&S.tmem_base, 512);
   tc_fence_before();
   __syncthreads();
@@ -456,24 +464,27 @@ __global__ void __launch_bounds__(kThreads, 1)
         give_up(S, a.status);
         break;
       }
+      // (Read again where it is needed after the tiles: what is kept over them in registers would be spilled.)
       const Item& item = S.item[i];
       if (item.h < 0) break;
-      const int ways = item.ways, part = ways > 1 ? 0 : slot, way = ways > 1 ? slot : 0, nk = item.nk;
-      const int ntok = part_tokens(item.nq, item.tok, part, T), tok0 = item.tok + part * T;
-      const int last = min(item.t1, item.n[part]), tiles = ways > 1 ? max(0, last - item.t0 - way + 1) >> 1 : max(0, last - item.t0);
-      static_assert(kSlots == 2, "two slots take turns");
-      // tile k of this slot is the (first + ways k)-th that comes, tile from + step k
-      const int first_tile = ways > 1 ? way : a.slopes ? item.t1 - last : 0, step = a.slopes ? -ways : ways;
-      const int from = a.slopes ? item.t1 - 1 - first_tile : item.t0 + first_tile;
+      auto part_of = [&]() { return item.ways > 1 ? 0 : slot; };
+      int tiles, key, dkey;  // this slot's tiles, the first key of the first, from one to the next
+      {
+        const int ways = item.ways, way = ways > 1 ? slot : 0, last = min(item.t1, item.n[part_of()]);
+        tiles = ways > 1 ? max(0, last - item.t0 - way + 1) >> 1 : max(0, last - item.t0);
+        static_assert(kSlots == 2, "two slots take turns");
+        key = (a.slopes ? (ways > 1 ? item.t1 - way : last) - 1 : item.t0 + way) * kKeys;
+        dkey = a.slopes ? -ways * kKeys : ways * kKeys;
+      }
       int pos[2], lim[2];
       float slope[2];
-      int least = INT32_MAX;
+      int least = item.nk;
       bool any = false;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const int r = r0 + 8 * j, t = S.row_token[r];
-        pos[j] = item.d + tok0 + t;
-        lim[j] = t >= ntok ? 0 : a.causal ? max(0, min(nk, max(item.p, pos[j] + 1))) : nk;
+        const int r = r0 + 8 * j, t = S.row_token[r], part = part_of(), ntok = part_tokens(item.nq, item.tok, part, T);
+        pos[j] = item.d + item.tok + part * T + t;
+        lim[j] = t >= ntok ? 0 : a.causal ? max(0, min(item.nk, max(item.p, pos[j] + 1))) : item.nk;
         // rows that do not exist are masked for nobody's sake
         if (t < ntok) least = min(least, lim[j]), any = true;
         slope[j] = kGen && a.slopes && t < ntok ? a.slopes[item.h * G + S.row_head[r]] * kLog2e : 0.f;
@@ -505,8 +516,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       };
       float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};  // reference maxima (log2 units), this lane's sums
-      for (int k = 0; k < tiles; ++k, ++c) {
-        const int t = from + k * step, key = t * kKeys;
+      for (int k = 0; k < tiles; ++k, ++c, key += dkey) {
         if (!wait(&S.s_full[slot], c & 1, abort)) {
           give_up(S, a.status);
           stop = true;
@@ -583,8 +593,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             break;
           }
         }
-        if (key + kKeys > nk) {  // V's rows behind the last key
-          const int g = item.g0 + first_tile + k * ways, st = g % kStages;
+        if (const int nk = key + kKeys > least ? item.nk : INT32_MAX; key + kKeys > nk) {  // V's rows behind the last key
+          const int t = key / kKeys, g = item.g0 + (a.slopes ? item.t1 - 1 - t : t - item.t0), st = g % kStages;
           if (!wait(&S.kv_full[st], (g / kStages) & 1, abort)) {
             give_up(S, a.status);
             stop = true;
@@ -599,18 +609,49 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
       }
       if (stop) break;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        l[j] += __shfl_xor_sync(0xffffffffu, l[j], 1);
+        l[j] += __shfl_xor_sync(0xffffffffu, l[j], 2);
+        if (l[j] == 0.f) m[j] = -INFINITY;
+      }
+      // What does not take O is done before it is waited for: where the rows go (null: nowhere), and what is told of
+      // their sums.
+      const int ways = item.ways, way = ways > 1 ? slot : 0, whole = item.part < 0;
+      char* dst[2];
+      {
+        const int part = part_of(), tok0 = item.tok + part * T, ntok = part_tokens(item.nq, item.tok, part, T);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int r = r0 + 8 * j, t = S.row_token[r], head = item.h * G + S.row_head[r];
+          const int64_t q = (int64_t)item.q0 + tok0 + t;
+          if (whole)
+            dst[j] = reinterpret_cast<char*>(static_cast<uint16_t*>(a.o.data) + q * a.o.token_stride + head * a.o.head_stride) +
+                     16 * (lane & 3);
+          else
+            dst[j] = reinterpret_cast<char*>(a.part + item.part * kPartFloats + (part * 128 + r) * 64) + 8 * (lane & 3);
+          if (t >= ntok || way > 0) dst[j] = nullptr;
+        }
+      }
+      auto tell = [&](int j) {
+        if (!dst[j] || (lane & 3) != 0) return;
+        const int r = r0 + 8 * j;
+        if (!whole) {
+          float* to = a.part + item.part * kPartFloats + part_of() * 128 + r;
+          to[kRows * 64] = m[j], to[kRows * 65] = l[j];
+        } else if (a.lse) {
+          a.lse[(item.h * G + S.row_head[r]) * a.rows + item.q0 + item.tok + part_of() * T + S.row_token[r]] =
+              l[j] == 0.f ? -INFINITY : (m[j] + lg2(l[j])) * 0.6931471805599453f;
+        }
+      };
+      if (ways == 1) tell(0), tell(1);
+      __syncwarp();
       if (tiles > 0) {
         if (!wait(&S.o_full[slot], (c - 1) & 1, abort)) {
           give_up(S, a.status);
           break;
         }
         tc_fence_after();
-      }
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        l[j] += __shfl_xor_sync(0xffffffffu, l[j], 1);
-        l[j] += __shfl_xor_sync(0xffffffffu, l[j], 2);
-        if (l[j] == 0.f) m[j] = -INFINITY;
       }
       // Slots with the same rows: slot 0 adds the other's O, which it reads where it is, to its own,
       // O = sum_s 2^(m_s - m) O_s.
@@ -645,7 +686,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             by1[j] = m1 == -INFINITY ? 0.f : ex2(m1 - top);
             m[j] = top;
             l[j] = fmaf(l[j], by0[j], l1 * by1[j]);
+            tell(j);
           }
+          __syncwarp();
         }
         if (any) {
           float o[32];
@@ -661,24 +704,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             uint32_t v[32];
 #pragma unroll
             for (int e = 0; e < 32; ++e) v[e] = 0u;
-            if (item.t0 + 1 < last) RESS_TMEM_LD16X64(tm + kColSlot + kColO, v);
+            if (item.t0 + 1 < min(item.t1, item.n[0])) RESS_TMEM_LD16X64(tm + kColSlot + kColO, v);
 #pragma unroll
             for (int e = 0; e < 32; ++e)
               o[e] = fmaf(__uint_as_float(v[e]), by1[e >> 1 & 1], o[e] * by0[e >> 1 & 1]);
           }
+          if (whole) {
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const int r = r0 + 8 * j, t = S.row_token[r], head = item.h * G + S.row_head[r];
-            const int64_t q = (int64_t)item.q0 + tok0 + t;
-            if (item.part >= 0) {
-              float* to = a.part + item.part * kPartFloats + part * 128 + r;
-              if (t < ntok) {
-                float2* dst = reinterpret_cast<float2*>(a.part + item.part * kPartFloats + (part * 128 + r) * 64 + two);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) dst[4 * e] = make_float2(o[4 * e + 2 * j], o[4 * e + 2 * j + 1]);
-                if ((lane & 3) == 0) to[kRows * 64] = m[j], to[kRows * 65] = l[j];
-              }
-            } else {
+            for (int j = 0; j < 2; ++j) {
               const float inv = l[j] == 0.f ? 0.f : __fdividef(1.0f, l[j]);
               uint32_t w[8];
 #pragma unroll
@@ -686,17 +719,21 @@ __global__ void __launch_bounds__(kThreads, 1)
               // a row's four lanes: from two channels of every eight to eight of every 32
               transpose4(w[0], w[1], w[2], w[3], lane);
               transpose4(w[4], w[5], w[6], w[7], lane);
-              if (t < ntok) {
-                uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.o.data) + q * a.o.token_stride +
-                                                      head * a.o.head_stride) + (lane & 3);
-                dst[0] = make_uint4(w[0], w[1], w[2], w[3]);
-                dst[4] = make_uint4(w[4], w[5], w[6], w[7]);
-                if (a.lse && (lane & 3) == 0)
-                  a.lse[head * a.rows + q] = l[j] == 0.f ? -INFINITY : (m[j] + lg2(l[j])) * 0.6931471805599453f;
+              if (dst[j]) {
+                reinterpret_cast<uint4*>(dst[j])[0] = make_uint4(w[0], w[1], w[2], w[3]);
+                reinterpret_cast<uint4*>(dst[j])[4] = make_uint4(w[4], w[5], w[6], w[7]);
               }
             }
-            __syncwarp();
+          } else {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              if (!dst[j]) continue;
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                reinterpret_cast<float2*>(dst[j])[4 * e] = make_float2(o[4 * e + 2 * j], o[4 * e + 2 * j + 1]);
+            }
           }
+          __syncwarp();
         }
         tc_fence_before();
         __syncwarp();

@@ -330,7 +330,7 @@ struct DenseArgs {
   int type, n_seqs, kv_heads, group;  // group: heads of Q per head of K and V
   int causal;
   float cap;
-  float cap_poly[4], cap_square;  // for products whose square is at most cap_square (see set_cap)
+  float cap_poly[4], cap_small;  // for products of at most cap_small (see set_cap)
   int64_t rows, keys;
   const int32_t *q_start, *k_start, *prefix;
   const float* slopes;
