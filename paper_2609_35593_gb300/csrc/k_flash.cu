@@ -98,8 +98,8 @@ __device__ __forceinline__ int item_tiles(const DenseArgs& a, const Seq& q, int 
 
 }  // namespace
 
-// kGen: scores with a cap or slopes.
-template <bool kF16, bool kGen>
+// kGen: 1, capped scores; 2, scores with slopes, capped or not; 0, neither.
+template <bool kF16, int kGen>
 __global__ void __launch_bounds__(kThreads, 1)
     k_flash(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
             const __grid_constant__ CUtensorMap tmV, const __grid_constant__ DenseArgs a) {
@@ -108,6 +108,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   volatile int* abort = &S.abort;
   const int G = a.group, T = 128 / G;
+  constexpr bool kSlopes = kGen == 2;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -228,7 +229,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int last = lane < kSlots ? min(t1, item.n[mine_part]) : 0;
           const uint32_t some = __ballot_sync(0xffffffffu, t0 + way < last);
           // slopes: the nearest keys of a causal row first, or the reference would be raised from tile to tile
-          const int step = a.slopes ? -1 : 1, begin = a.slopes ? t1 - 1 : t0;
+          const int step = kSlopes ? -1 : 1, begin = kSlopes ? t1 - 1 : t0;
           for (int s = 0; s < kSlots; ++s) {
             if (!(some >> s & 1)) continue;
             // phases of its barriers (2 bits: none yet, 1, 2, 1, ..)
@@ -272,8 +273,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (ways > 1 ? lane < kSlots && i % kSlots == lane : t < last) {
               flags = kHas << lane;
               const bool is_low = t == t0, is_high = t == last - 1;
-              if (ways > 1 ? i == lane : a.slopes ? is_high : is_low) flags |= kBegin << lane;
-              if (ways > 1 ? i + kSlots >= t1 - t0 : a.slopes ? is_low : is_high) flags |= kEnd << lane;
+              if (ways > 1 ? i == lane : kSlopes ? is_high : is_low) flags |= kBegin << lane;
+              if (ways > 1 ? i + kSlots >= t1 - t0 : kSlopes ? is_low : is_high) flags |= kEnd << lane;
             }
             flags = __reduce_or_sync(0xffffffffu, flags);
             if (u > 0 && !wait(&S.kv_empty[s], (u - 1) & 1, abort)) {
@@ -473,8 +474,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int ways = item.ways, way = ways > 1 ? slot : 0, last = min(item.t1, item.n[part_of()]);
         tiles = ways > 1 ? max(0, last - item.t0 - way + 1) >> 1 : max(0, last - item.t0);
         static_assert(kSlots == 2, "two slots take turns");
-        key = (a.slopes ? (ways > 1 ? item.t1 - way : last) - 1 : item.t0 + way) * kKeys;
-        dkey = a.slopes ? -ways * kKeys : ways * kKeys;
+        key = (kSlopes ? (ways > 1 ? item.t1 - way : last) - 1 : item.t0 + way) * kKeys;
+        dkey = kSlopes ? -ways * kKeys : ways * kKeys;
       }
       int pos[2], lim[2];
       float slope[2];
@@ -487,7 +488,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         lim[j] = t >= ntok ? 0 : a.causal ? max(0, min(item.nk, max(item.p, pos[j] + 1))) : item.nk;
         // rows that do not exist are masked for nobody's sake
         if (t < ntok) least = min(least, lim[j]), any = true;
-        slope[j] = kGen && a.slopes && t < ntok ? a.slopes[item.h * G + S.row_head[r]] * kLog2e : 0.f;
+        slope[j] = kSlopes && t < ntok ? a.slopes[item.h * G + S.row_head[r]] * kLog2e : 0.f;
       }
       least = __reduce_min_sync(0xffffffffu, least);
       any = __any_sync(0xffffffffu, any);
@@ -496,13 +497,13 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(v[e]);
         if (kGen) {
-          if (cap > 0.f) {
+          if (!kSlopes || cap > 0.f) {
             cap_scores(x, a, in, out);
           } else {
 #pragma unroll
             for (int e = 0; e < 32; ++e) x[e] *= in;
           }
-          if (a.slopes) {
+          if (kSlopes) {
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
               const int j = e >> 1 & 1;
@@ -594,7 +595,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
         if (const int nk = key + kKeys > least ? item.nk : INT32_MAX; key + kKeys > nk) {  // V's rows behind the last key
-          const int t = key / kKeys, g = item.g0 + (a.slopes ? item.t1 - 1 - t : t - item.t0), st = g % kStages;
+          const int t = key / kKeys, g = item.g0 + (kSlopes ? item.t1 - 1 - t : t - item.t0), st = g % kStages;
           if (!wait(&S.kv_full[st], (g / kStages) & 1, abort)) {
             give_up(S, a.status);
             stop = true;
@@ -715,7 +716,11 @@ __global__ void __launch_bounds__(kThreads, 1)
               const float inv = l[j] == 0.f ? 0.f : __fdividef(1.0f, l[j]);
               uint32_t w[8];
 #pragma unroll
-              for (int e = 0; e < 8; ++e) w[e] = pack2<kF16>(o[4 * e + 2 * j] * inv, o[4 * e + 2 * j + 1] * inv);
+              for (int e = 0; e < 8; ++e) {
+                float y0, y1;
+                mul2(y0, y1, o[4 * e + 2 * j], o[4 * e + 2 * j + 1], inv, inv);
+                w[e] = pack2<kF16>(y0, y1);
+              }
               // a row's four lanes: from two channels of every eight to eight of every 32
               transpose4(w[0], w[1], w[2], w[3], lane);
               transpose4(w[4], w[5], w[6], w[7], lane);
@@ -860,8 +865,10 @@ cudaError_t launch_flash(const DenseArgs& args, cudaStream_t st) {
       !make_key_map(&tk, k, a.type, keys, pages, a.k_page_stride, a.kv_heads, box) ||
       !make_key_map(&tv, v, a.type, keys, pages, a.v_page_stride, a.kv_heads, box))
     return cudaErrorInvalidValue;
-  const bool f16 = a.type == RESS_F16, gen = a.cap > 0.f || a.slopes;
-  auto kern = f16 ? (gen ? k_flash<true, true> : k_flash<true, false>) : gen ? k_flash<false, true> : k_flash<false, false>;
+  const bool f16 = a.type == RESS_F16;
+  auto kern = a.slopes     ? (f16 ? k_flash<true, 2> : k_flash<false, 2>)
+              : a.cap > 0.f ? (f16 ? k_flash<true, 1> : k_flash<false, 1>)
+                            : (f16 ? k_flash<true, 0> : k_flash<false, 0>);
   const size_t smem = sizeof(Smem) + 1024;
   const int ctas = dense_ctas();
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
