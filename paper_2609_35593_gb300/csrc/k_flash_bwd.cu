@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(256) k_flash_rows(const __grid_constant__ Dens
 }
 
 // kKeys: items of keys (dK, dV); else of rows (dQ).
-template <bool kF16, bool kGen, bool kKeys>
+template <bool kF16, int kGen, bool kKeys>
 __global__ void __launch_bounds__(kThreads, 1)
     k_flash_bwd(const __grid_constant__ CUtensorMap tmA1, const __grid_constant__ CUtensorMap tmA2,
                 const __grid_constant__ CUtensorMap tmB1, const __grid_constant__ CUtensorMap tmB2,
@@ -167,6 +167,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   volatile int* abort = &S.abort;
   const int G = a.group, T = 128 / G;
   constexpr int kSums = kKeys ? 2 : 1;  // issuers of sums
+  constexpr bool kSlopes = kGen == 2;   // (kGen as in k_flash)
+  static_assert(offsetof(Smem, B2) == offsetof(Smem, B1) + kStages * kTileBytes && kTileBytes == sizeof S.A[0][0], "tiles one after another");
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -202,7 +204,16 @@ __global__ void __launch_bounds__(kThreads, 1)
       reinterpret_cast<uint4*>(S.B1)[f] = make_uint4(0u, 0u, 0u, 0u);
     fence_proxy_async_smem();
   }
-  if (const int r = (int)threadIdx.x - 512; r >= 0) S.row_token[r] = r / G, S.row_head[r] = r % G;
+  if (const int r = (int)threadIdx.x - 512; r >= 0) {
+    S.row_token[r] = r / G, S.row_head[r] = r % G;
+    // rows that no token fills stay 0, as in k_flash
+    if (r >= T * G) {
+#pragma unroll 1
+      for (int i = 0; i < (kKeys ? 2 * kStages : 4) * 8; ++i)
+        reinterpret_cast<uint4*>((kKeys ? S.B1[0] : S.A[0][0]) + (i >> 3) * kTileBytes + r * 128)[i & 7] = make_uint4(0u, 0u, 0u, 0u);
+      fence_proxy_async_smem();
+    }
+  }
   if (warp == kIssueS) tmem_alloc(&S.tmem_base, 512);
   tc_fence_before();
   __syncthreads();
@@ -294,7 +305,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int left = item.nq - item.from, pos0 = item.d + item.from, base = kKeys ? item.q0 + item.from : item.k0;
           const int nk = item.nk, p = item.p, last_key = min(nk, item.at + 128);
           float slope[4] = {0.f, 0.f, 0.f, 0.f};
-          if (kKeys && kGen && a.slopes) {
+          if (kKeys && kSlopes) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) slope[e] = a.slopes[h * G + (lane + 32 * e) % G] * kLog2e;
           }
@@ -326,7 +337,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 cols.lse[col] = (kF16 ? kPScale : 0.f) - now[e].x;
                 cols.delta[col] = -now[e].y * f;
                 cols.lim[col] = lim;
-                if (kGen) cols.pos[col] = (float)(pos0 + row), cols.slope[col] = slope[e];
+                if (kSlopes) cols.pos[col] = (float)(pos0 + row), cols.slope[col] = slope[e];
                 now[e] = ahead[e];
               }
               if (!__all_sync(0xffffffffu, whole)) flags |= kMask;
@@ -496,22 +507,24 @@ __global__ void __launch_bounds__(kThreads, 1)
       const Item& item = S.item[i];
       if (item.h < 0) break;
       // this lane's rows: keys, or rows of Q
-      const int tiles = item.t1 - item.t0, nk = item.nk;
-      int tok[2], pos[2], lim[2] = {0, 0}, least = INT32_MAX;
+      const int tiles = item.t1 - item.t0;
+      auto token_of = [&](int j) { return item.at + (kKeys ? r0 + 8 * j : S.row_token[r0 + 8 * j]); };
+      auto exists = [&](int j) {
+        return kKeys ? token_of(j) < item.nk : S.row_token[r0 + 8 * j] < T && token_of(j) < item.nq;
+      };
+      int tok[2], pos[2], lim[2] = {0, 0}, least = item.nk;
       float nlse[2] = {-INFINITY, -INFINITY}, ndelta[2] = {0.f, 0.f}, slope[2] = {0.f, 0.f};
-      bool exists[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const int r = r0 + 8 * j;
-        tok[j] = item.at + (kKeys ? r : S.row_token[r]);
-        exists[j] = kKeys ? tok[j] < nk : S.row_token[r] < T && tok[j] < item.nq;
+        tok[j] = token_of(j);
         pos[j] = item.d + tok[j];
-        if (!kKeys && exists[j]) {
+        if (!kKeys && exists(j)) {
           const float2 x = a.stat[((int64_t)item.h * a.rows + item.q0 + tok[j]) * G + S.row_head[r]];
           nlse[j] = (kF16 ? kPScale : 0.f) - x.x, ndelta[j] = -x.y * f;
-          lim[j] = a.causal ? max(0, min(nk, max(item.p, pos[j] + 1))) : nk;
+          lim[j] = a.causal ? max(0, min(item.nk, max(item.p, pos[j] + 1))) : item.nk;
           least = min(least, lim[j]);
-          if (kGen && a.slopes) slope[j] = a.slopes[item.h * G + S.row_head[r]] * kLog2e;
+          if (kSlopes) slope[j] = a.slopes[item.h * G + S.row_head[r]] * kLog2e;
         }
       }
       if (!kKeys) least = __reduce_min_sync(0xffffffffu, least);
@@ -525,7 +538,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         tc_fence_after();
         const Cols& cols = S.cols[st];
-        const bool masked = kKeys ? (S.flags[st] & kMask) != 0 : key + kCols > least;
+        const bool masked = kKeys ? (S.flags[st] & kMask) != 0 : key + kCols > least;  // (warp's rows: at least at the last key)
         float x[32];
         uint32_t w[16];
         {
@@ -555,7 +568,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         };
         // P
-        if (kGen && cap > 0.f) cap_scores(x, a, in, out);
+        if (kGen == 1 || (kSlopes && cap > 0.f)) cap_scores(x, a, in, out);
 #pragma unroll
         for (int e = 0; e < 32; e += 2) {
           const int j = e >> 1 & 1, col = 64 * side + 8 * (e >> 2) + two;  // row, columns col and col + 1
@@ -567,14 +580,14 @@ __global__ void __launch_bounds__(kThreads, 1)
           float x0 = x[e], x1 = x[e + 1];
           float c0 = 1.f, c1 = 1.f;
           if (kGen) {
-            if (cap > 0.f) {
+            if (!kSlopes || cap > 0.f) {
               float u0, u1;
               mul2(u0, u1, x0, x1, back, back);
               fma2(c0, c1, -u0, -u1, u0, u1, 1.f, 1.f);
             } else {
               x0 *= in, x1 *= in;
             }
-            if (a.slopes) {
+            if (kSlopes) {
               if (kKeys) {
                 const float2 q = *reinterpret_cast<const float2*>(&cols.pos[col]);
                 const float2 m = *reinterpret_cast<const float2*>(&cols.slope[col]);
@@ -633,7 +646,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (kKeys) tmem_wait_st();
         RESS_TMEM_ST16X32P_NOWAIT(tm + kColDs + 32 * side, w);
         // rows of the tile that are not this sequence's, which the sums run over
-        const int valid = kKeys ? (item.nq - item.from - t * T) * G : nk - key;
+        const int valid = kKeys ? (item.nq - item.from - t * T) * G : masked ? item.nk - key : kCols;
         if (valid < (kKeys ? T * G : kCols)) {
           if (!kKeys && !wait(&S.kv_full[st], (g / kStages) & 1, abort)) {
             give_up(S, a.status);
@@ -682,19 +695,23 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!kKeys && side) break;
         if (item.part >= 0) {
           float2* dst = reinterpret_cast<float2*>(a.part + item.part * kPartFloats + (side * 128 + r) * 64 + two);
-          if (exists[j]) {
+          if (exists(j)) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) dst[4 * e] = make_float2(o[4 * e + 2 * j], o[4 * e + 2 * j + 1]);
           }
         } else {
           uint32_t w[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) w[e] = pack2<kF16>(o[4 * e + 2 * j] * by, o[4 * e + 2 * j + 1] * by);
+          for (int e = 0; e < 8; ++e) {
+            float y0, y1;
+            mul2(y0, y1, o[4 * e + 2 * j], o[4 * e + 2 * j + 1], by, by);
+            w[e] = pack2<kF16>(y0, y1);
+          }
           // a row's four lanes: from two channels of every eight to eight of every 32
           transpose4(w[0], w[1], w[2], w[3], lane);
           transpose4(w[4], w[5], w[6], w[7], lane);
-          if (exists[j]) {
-            const int64_t token = (int64_t)(kKeys ? item.k0 : item.q0) + tok[j];
+          if (exists(j)) {
+            const int64_t token = (int64_t)(kKeys ? item.k0 : item.q0) + token_of(j);
             const int head = kKeys ? item.h : item.h * G + S.row_head[r];
             uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(to.data) + token * to.token_stride +
                                                   head * to.head_stride) + (lane & 3);
@@ -747,7 +764,7 @@ __global__ void __launch_bounds__(256) k_flash_bwd_join(const __grid_constant__ 
   }
 }
 
-template <bool kF16, bool kGen, bool kKeys>
+template <bool kF16, int kGen, bool kKeys>
 static cudaError_t launch_pass(const DenseArgs& a, const CUtensorMap (&m)[4], int ctas, cudaStream_t st) {
   auto kern = k_flash_bwd<kF16, kGen, kKeys>;
   const size_t smem = sizeof(Smem) + 1024;
@@ -766,7 +783,6 @@ static cudaError_t launch_type(DenseArgs a, cudaStream_t st) {
     a.n_big = (int)(rows / 32 < kBigParts ? (rows + 31) / 32 : kBigParts);
     if ((e = launch_pdl(k_flash_rows<kF16>, dim3(a.n_big), 256, 0, st, true, a)) != cudaSuccess) return e;
   }
-  const bool gen = a.cap > 0.f || a.slopes;
   if (a.cap > 0.f) set_cap(a);
   // a tensor without rows or keys is not read, but its map needs some memory
   ress_heads q = a.q, g = a.d_o, k = a.k, v = a.v;
@@ -780,16 +796,20 @@ static cudaError_t launch_type(DenseArgs a, cudaStream_t st) {
         !make_row_map(&m[2], q, a.type, rows, a.kv_heads, a.group, per) ||
         !make_row_map(&m[3], g, a.type, rows, a.kv_heads, a.group, per))
       return cudaErrorInvalidValue;
-    if ((e = gen ? launch_pass<kF16, true, true>(a, m, ctas, st) : launch_pass<kF16, false, true>(a, m, ctas, st)) != cudaSuccess)
-      return e;
+    e = a.slopes ? launch_pass<kF16, 2, true>(a, m, ctas, st)
+        : a.cap > 0.f ? launch_pass<kF16, 1, true>(a, m, ctas, st)
+                      : launch_pass<kF16, 0, true>(a, m, ctas, st);
+    if (e != cudaSuccess) return e;
   }
   if (a.rows > 0) {
     const int T = 128 / a.group;
     if (!make_row_map(&m[0], q, a.type, rows, a.kv_heads, a.group, T) || !make_row_map(&m[1], g, a.type, rows, a.kv_heads, a.group, T) ||
         !make_key_map(&m[2], k, a.type, keys, 1, 0, a.kv_heads, kCols) || !make_key_map(&m[3], v, a.type, keys, 1, 0, a.kv_heads, kCols))
       return cudaErrorInvalidValue;
-    if ((e = gen ? launch_pass<kF16, true, false>(a, m, ctas, st) : launch_pass<kF16, false, false>(a, m, ctas, st)) != cudaSuccess)
-      return e;
+    e = a.slopes ? launch_pass<kF16, 2, false>(a, m, ctas, st)
+        : a.cap > 0.f ? launch_pass<kF16, 1, false>(a, m, ctas, st)
+                      : launch_pass<kF16, 0, false>(a, m, ctas, st);
+    if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
 }
