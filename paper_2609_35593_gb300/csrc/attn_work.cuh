@@ -25,8 +25,8 @@ namespace work {
 using namespace ptx;
 
 constexpr int kMaxCtas = kDenseMaxCtas;
-// An item's loads and epilogue, as work: three tiles of 128 keys (8,000 to 10,000 cycles against 1,850 a tile are more,
-// but part of them runs under the neighbours' tiles; two, four and six tiles were no better over the cases).
+// An item's loads and epilogue, as work: three tiles of 128 keys (packed documents of 30 to 6,000 rows 185 us; counted as
+// two tiles 192, as four 198; long sequences the same).
 constexpr int64_t kOver = 8 * 384;
 constexpr int64_t kLeast = 8 * 256;  // least share of a CTA: two tiles
 constexpr uint64_t kWaitNs = 2000000000ull;  // 2 s per wait
@@ -434,8 +434,8 @@ __device__ __forceinline__ void mul2(float& d0, float& d1, float a0, float a1, f
 
 // Products q.k to capped scores in log2 units, a warp's 16 rows x 64 columns.  Where none of them is above half of the cap,
 // x times a polynomial in x^2 (set_cap): five packed instructions a pair on the FMA pipe, next to which the SFU forms the
-// exponentials; else capped2, whose four SFU operations a pair are twice what the exponentials take (packed documents of
-// 30 to 6,000 rows, cap 30: 251 us with capped2 alone, 239 with both).
+// exponentials; else capped2, whose four SFU operations a pair are twice what the exponentials take (with capped2 alone packed
+// documents, cap 30, took 251 us where 239 with both).  A polynomial of one term less up to a quarter of the cap gains nothing.
 __device__ __forceinline__ void cap_scores(float (&x)[32], const DenseArgs& a, float in, float out) {
   float top = 0.f;
 #pragma unroll

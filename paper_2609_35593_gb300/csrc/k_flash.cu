@@ -17,9 +17,9 @@
 //   warps 2, 3  issuers of O += P V (M128 N64 K128, P from TMEM, V MN-major), a slot each.  S and P have columns of their
 //               own: S of the next tile runs while the exponentials of this one are formed.
 // What bounds it is the chain of a slot's tile: scores from TMEM, exponentials, P to TMEM and the hand-overs between
-// warps take some 1,200 cycles whatever they compute, so the tiles are as large as TMEM allows, and the 16 warps of
-// softmax (four to a sub-partition) work while others wait.  8 images at once (10,992 rows and keys, 16 heads) take 447 us,
-// 1.11 PFLOP/s; other forms of the same results: a row per thread and 8 warps, S of 64 keys double-buffered under P 636,
+// warps, some 2,200 cycles of which the MMAs take 1,024, so the tiles are as large as TMEM allows, and the 16 warps of
+// softmax (four to a sub-partition) work while others wait.  8 images at once (10,992 rows and keys, 16 heads) take 437 us,
+// 1.13 PFLOP/s; other forms of the same results: a row per thread and 8 warps, S of 64 keys double-buffered under P 636,
 // 128 keys with S and P apart 618; 12 warps, three slots of 64 keys 586; 16 warps, four slots of 64 keys and two issuers
 // 553; this form at first 482 (its join looked for the shares itself, 25 us of that).
 // Rows of V behind a sequence's last key are zeroed in shared memory (0 x NaN of a cache page never written
@@ -98,7 +98,8 @@ __device__ __forceinline__ int item_tiles(const DenseArgs& a, const Seq& q, int 
 
 }  // namespace
 
-// kGen: 1, capped scores; 2, scores with slopes, capped or not; 0, neither.
+// kGen: 1, capped scores; 2, scores with slopes, capped or not; 0, neither.  (One kernel for 1 and 2 keeps slopes in
+// registers and spills others: packed documents with a cap 218 us where 186.)
 template <bool kF16, int kGen>
 __global__ void __launch_bounds__(kThreads, 1)
     k_flash(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
@@ -465,7 +466,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         give_up(S, a.status);
         break;
       }
-      // (Read again where it is needed after the tiles: what is kept over them in registers would be spilled.)
+      // (Read again where it is needed after the tiles: what is kept over them in registers would be spilled, 447 us
+      // where 438 on 8 images at once.)
       const Item& item = S.item[i];
       if (item.h < 0) break;
       auto part_of = [&]() { return item.ways > 1 ? 0 : slot; };

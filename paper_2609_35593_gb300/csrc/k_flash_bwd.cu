@@ -14,8 +14,8 @@
 // warps 4-19 element-wise: 16 rows x 64 columns of a tile of 128 x 128 each.  S and dP (256 columns of TMEM) are free for the next tile as soon as they are in registers, P and
 // dS (128) have columns of their own, so the products of the next tile run meanwhile; two accumulators (128).  With
 // eight element-wise warps on tiles of 64 columns and one issuer a tile of 128 x 64 took 1,700 cycles, its four
-// products 512 (8 images at once, 10,992 rows and keys of 16 heads: 2,200 us; now 1,490, 0.82 PFLOP/s of five products'
-// work or 1.16 of the seven formed).  What bounds it is the chain of a tile from scores to dS and back.  Shares of the work, partial results and waits are those of k_flash.cu.
+// products 512 (8 images at once, 10,992 rows and keys of 16 heads: 2,200 us; now 1,394, 0.89 PFLOP/s of five products'
+// work or 1.24 of the seven formed).  What bounds it is the chain of a tile from scores to dS and back.  Shares of the work, partial results and waits are those of k_flash.cu.
 //
 // In f16, P is kept times 2^8 and dS times a power of two that brings the largest |dO| to 1..2: probabilities of rows on
 // thousands of keys are below f16's 2^-14, and so may gradients be.  dP is at most 64 max|dO| max|V|, so dS stays
@@ -528,8 +528,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       if (!kKeys) least = __reduce_min_sync(0xffffffffu, least);
-      for (int k = 0; k < tiles; ++k, ++c) {
-        const int g = item.g0 + k, st = g % kStages, t = item.t0 + k, key = t * kCols;
+      // (In registers: read from the item in shared memory in every tile they cost 40 of 1,434 us on 8 images at once.)
+      const int full = kKeys ? T * G : kCols;  // rows of a tile
+      int g = item.g0, key = kKeys ? 0 : item.t0 * kCols, left = kKeys ? (item.nq - item.from - item.t0 * T) * G : 0;
+      for (int n = tiles; n > 0; --n, ++c, ++g, key += kCols, left -= full) {
+        const int st = g % kStages;
         // (the columns' numbers are there, and in the other pass nothing but S is looked at before the tail)
         if ((kKeys && !wait(&S.kv_full[st], (g / kStages) & 1, abort)) || !wait(&S.s_full, c & 1, abort)) {
           give_up(S, a.status);
@@ -646,8 +649,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (kKeys) tmem_wait_st();
         RESS_TMEM_ST16X32P_NOWAIT(tm + kColDs + 32 * side, w);
         // rows of the tile that are not this sequence's, which the sums run over
-        const int valid = kKeys ? (item.nq - item.from - t * T) * G : masked ? item.nk - key : kCols;
-        if (valid < (kKeys ? T * G : kCols)) {
+        const int valid = kKeys ? left : masked ? item.nk - key : kCols;
+        if (valid < full) {
           if (!kKeys && !wait(&S.kv_full[st], (g / kStages) & 1, abort)) {
             give_up(S, a.status);
             stop = true;
