@@ -443,6 +443,7 @@ int ress_qkv_proj(const ress_dims* dims, const uint16_t* x, const uint16_t* W_q,
  * Calls on one workspace must not overlap. */
 #define RESS_MAX_GROUP 64
 #define RESS_MAX_SEQS 8192 /* of ress_cache_tables */
+#define RESS_MAX_KEYS 2147483392 /* 2^31 - 256: of k and v, and table_cols * page */
 typedef struct {
   int32_t type;     /* RESS_BF16 or RESS_F16: of all heads                                    */
   int32_t n_seqs;   /* >= 0                                                                   */
@@ -450,7 +451,7 @@ typedef struct {
   int32_t causal;   /* 0 or 1                                                                 */
   float cap;        /* > 0, or 0 for none                                                     */
   int64_t rows;     /* of q, o (and their gradients), lse: below 2^31                         */
-  int64_t keys;     /* of k, v (and their gradients); not for paged calls                     */
+  int64_t keys;     /* of k, v (and their gradients), at most RESS_MAX_KEYS; not for paged calls */
   const int32_t* q_start; /* device int32 [n_seqs + 1]; NULL: one sequence of all rows        */
   const int32_t* k_start; /* device int32 [n_seqs + 1]; NULL: one sequence of all keys        */
   const int32_t* prefix;  /* device int32 [n_seqs], only with causal; NULL: none              */

@@ -25,7 +25,7 @@ namespace work {
 using namespace ptx;
 
 constexpr int kMaxCtas = kDenseMaxCtas;
-// An item's loads and epilogue, as work: three tiles of 128 keys (packed documents of 30 to 6,000 rows 185 us; counted as
+// An item's loads and epilogue, as work: three tiles of 128 keys (packed documents of 52 to 2531 rows 185 us; counted as
 // two tiles 192, as four 198; long sequences the same).
 constexpr int64_t kOver = 8 * 384;
 constexpr int64_t kLeast = 8 * 256;  // least share of a CTA: two tiles

@@ -50,7 +50,7 @@ struct Item {
 struct __align__(16) Cols {
   float lse[kCols], delta[kCols];  // -log2 of the sums, -delta (times the scale)
   int lim[kCols];                  // keys seen
-  float pos[kCols], slope[kCols];
+  float pos[kCols], slope[kCols];  // position after the item's first key (exact where it matters, however long the sequence)
 };
 
 struct __align__(1024) Smem {
@@ -337,7 +337,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 cols.lse[col] = (kF16 ? kPScale : 0.f) - now[e].x;
                 cols.delta[col] = -now[e].y * f;
                 cols.lim[col] = lim;
-                if (kSlopes) cols.pos[col] = (float)(pos0 + row), cols.slope[col] = slope[e];
+                if (kSlopes) cols.pos[col] = (float)(pos0 + row - item.at), cols.slope[col] = slope[e];
                 now[e] = ahead[e];
               }
               if (!__all_sync(0xffffffffu, whole)) flags |= kMask;
@@ -594,8 +594,8 @@ __global__ void __launch_bounds__(kThreads, 1)
               if (kKeys) {
                 const float2 q = *reinterpret_cast<const float2*>(&cols.pos[col]);
                 const float2 m = *reinterpret_cast<const float2*>(&cols.slope[col]);
-                x0 = fmaf(-m.x, fabsf(q.x - (float)tok[j]), x0);
-                x1 = fmaf(-m.y, fabsf(q.y - (float)tok[j]), x1);
+                x0 = fmaf(-m.x, fabsf(q.x - (float)(r0 + 8 * j)), x0);
+                x1 = fmaf(-m.y, fabsf(q.y - (float)(r0 + 8 * j)), x1);
               } else {
                 x0 = fmaf(-slope[j], fabsf((float)(pos[j] - key - col)), x0);
                 x1 = fmaf(-slope[j], fabsf((float)(pos[j] - key - col - 1)), x1);

@@ -1012,7 +1012,7 @@ int attn_checks(const ress_attn_args* a, const ress_pages* pg, bool backward, vo
     if (pg->page < 8 || pg->page % 8) return fail(RESS_EUNSUPPORTED, "page %d is not a multiple of 8", pg->page);
     if (pg->n_pages < 0 || pg->n_pages > INT32_MAX / pg->page)
       return fail(RESS_EINVAL, "%lld pages of %d outside 0..2^31-1 rows", (long long)pg->n_pages, pg->page);
-    if (pg->table_cols < 0 || pg->table_cols > INT32_MAX / pg->page ||
+    if (pg->table_cols < 0 || pg->table_cols > RESS_MAX_KEYS / pg->page ||
         (a->n_seqs > 1 && (pg->table_stride < 0 || pg->table_stride > INT64_MAX / 8 / a->n_seqs)))
       return fail(RESS_EINVAL, "table of %d columns, %lld apart", pg->table_cols, (long long)pg->table_stride);
     if (a->n_seqs > 0 && a->rows > 0) {
@@ -1029,7 +1029,7 @@ int attn_checks(const ress_attn_args* a, const ress_pages* pg, bool backward, vo
     out->table_cols = pg->table_cols, out->page = pg->page;
     out->k_page_stride = pg->k_page_stride, out->v_page_stride = pg->v_page_stride;
   } else {
-    if (a->keys < 0 || a->keys > INT32_MAX) return fail(RESS_EINVAL, "keys %lld outside 0..2^31-1", (long long)a->keys);
+    if (a->keys < 0 || a->keys > RESS_MAX_KEYS) return fail(RESS_EINVAL, "keys %lld outside 0..2^31-256", (long long)a->keys);
     if (a->keys > 0 && ((e = check_tiles(a->k, a->keys, a->kv_heads, false, "k")) ||
                         (e = check_tiles(a->v, a->keys, a->kv_heads, false, "v"))))
       return e;

@@ -66,7 +66,7 @@ BAD = [("type", 2, EUNSUPPORTED), ("type", -1, EUNSUPPORTED), ("q_heads", 0, EUN
        ("o", Heads(AT, 128, 64), EINVAL), ("o", Heads(AT, 256, 32), EINVAL)]
 
 
-@pytest.mark.parametrize("field,value,code", BAD + [("keys", -1, EINVAL), ("keys", 1 << 31, EINVAL), ("k_start", None, EINVAL)])
+@pytest.mark.parametrize("field,value,code", BAD + [("keys", -1, EINVAL), ("keys", 1 << 31, EINVAL), ("keys", (1 << 31) - 255, EINVAL), ("k_start", None, EINVAL)])
 def test_attention_refuses(field, value, code):
     assert call("ress_attn", args(**{field: value})) == code
     assert ress._lib.ress_last_error()
@@ -87,6 +87,7 @@ def test_a_prefix_needs_the_causal_mask():
 
 @pytest.mark.parametrize("field,value,code", [("page", 4, EUNSUPPORTED), ("page", 12, EUNSUPPORTED), ("page", 0, EUNSUPPORTED),
                                               ("n_pages", 0, EINVAL), ("n_pages", 1 << 26, EINVAL), ("table_cols", -1, EINVAL),
+                                              ("table_cols", (1 << 25) - 3, EINVAL),
                                               ("table", None, EINVAL), ("lens", None, EINVAL), ("lens", AT + 2, EINVAL),
                                               ("k_page_stride", 12, EINVAL), ("v_page_stride", 0, EINVAL),
                                               ("table_stride", -1, EINVAL)])

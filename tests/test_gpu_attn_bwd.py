@@ -71,6 +71,22 @@ def test_long_sequences_split_over_ctas():
     check([2500, 2, 1000], [2700, 3000, 1000], 4, 2, causal=True)
 
 
+def test_slopes_at_positions_past_float32():
+    """Distances are those of integers also where a position has more than 24 bits.  Keys 2,000 back and more weigh e^-2000."""
+    n, near, rows = (1 << 24) + 2001, 2000, 150
+    q, k, v = problem([rows], [near], 2, 1)
+    do = normal(9, *q.shape, by=0.1)
+    mask = {"causal": True, "slopes": torch.ones(2, device="cuda")}
+    far = [torch.zeros(n, 1, 64, dtype=BF16, device="cuda") for _ in range(2)]
+    far[0][-near:], far[1][-near:] = k, v
+    o, lse = run(q, *far, [rows], [n], **mask)
+    want, off = R.gradients(do, q, k, v, o, lse, [rows], [near], **mask)
+    dq, dk, dv = grads(do, q, *far, o, lse, [rows], [n], **mask)
+    for g, w, f, name in zip((dq, dk[-near:], dv[-near:]), want, off, ("dq", "dk", "dv")):
+        R.close(g, w, f, name)
+    assert (dk[:-near] == 0).all() and (dv[:-near] == 0).all()
+
+
 def test_rows_and_keys_behind_the_last_sequence():
     """A padded batch: what is behind is neither read into results nor written."""
     lens, pad = ([130, 70], [130, 70]), 41
