@@ -443,10 +443,11 @@ int ress_qkv_proj(const ress_dims* dims, const uint16_t* x, const uint16_t* W_q,
  * Calls on one workspace must not overlap. */
 #define RESS_MAX_GROUP 64
 #define RESS_MAX_SEQS 8192 /* of ress_cache_tables */
+#define RESS_MAX_PACKED 1048576 /* sequences of a call */
 #define RESS_MAX_KEYS 2147483392 /* 2^31 - 256: of k and v, and table_cols * page */
 typedef struct {
   int32_t type;     /* RESS_BF16 or RESS_F16: of all heads                                    */
-  int32_t n_seqs;   /* >= 0                                                                   */
+  int32_t n_seqs;   /* 0..RESS_MAX_PACKED                                                     */
   int32_t q_heads, kv_heads;
   int32_t causal;   /* 0 or 1                                                                 */
   float cap;        /* > 0, or 0 for none                                                     */

@@ -8,6 +8,7 @@
 #include <string.h>
 
 #include <atomic>
+#include <initializer_list>
 #include <mutex>
 
 #include "ress_internal.cuh"
@@ -992,7 +993,8 @@ int attn_checks(const ress_attn_args* a, const ress_pages* pg, bool backward, vo
   if (a->kv_heads < 1 || a->q_heads % a->kv_heads || a->q_heads / a->kv_heads > RESS_MAX_GROUP)
     return fail(RESS_EUNSUPPORTED, "%d heads of Q over %d of K (a multiple, at most %d times)", a->q_heads, a->kv_heads,
                 RESS_MAX_GROUP);
-  if (a->n_seqs < 0 || a->n_seqs > INT32_MAX / 2) return fail(RESS_EINVAL, "n_seqs %d out of range", a->n_seqs);
+  if (a->n_seqs < 0 || a->n_seqs > RESS_MAX_PACKED)  // (a CTA passes over empty ones, while others wait for 2 s at most)
+    return fail(RESS_EINVAL, "n_seqs %d outside 0..%d", a->n_seqs, RESS_MAX_PACKED);
   if (a->causal != 0 && a->causal != 1) return fail(RESS_EINVAL, "causal is %d, not 0 or 1", a->causal);
   if (!(a->cap >= 0.0f && a->cap <= FLT_MAX) || (a->cap > 0.0f && a->cap < 1e-30f))
     return fail(RESS_EINVAL, "cap %g is neither 0 nor a number in 1e-30..", (double)a->cap);
@@ -1050,6 +1052,13 @@ int attn_checks(const ress_attn_args* a, const ress_pages* pg, bool backward, vo
   return RESS_OK;
 }
 
+// Outputs are written while other CTAs still read the inputs.
+int check_apart(const ress_heads& out, const char* name, std::initializer_list<const void*> ins) {
+  for (const void* p : ins)
+    if (out.data == p) return fail(RESS_EINVAL, "%s must not be an input", name);
+  return RESS_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1063,6 +1072,7 @@ int ress_attn(const ress_attn_args* args, void* ws, size_t ws_bytes, void* strea
   int e = attn_checks(args, nullptr, false, ws, ws_bytes, &a);
   if (e) return e;
   if (a.rows == 0 || a.n_seqs == 0) return ok();
+  if ((e = check_apart(a.o, "o", {a.q.data, a.k.data, a.v.data}))) return e;
   cudaError_t ce = ress::launch_flash(a, static_cast<cudaStream_t>(stream));
   if (ce != cudaSuccess) return cuda_fail(ce, "ress_attn");
   return ok();
@@ -1080,6 +1090,10 @@ int ress_attn_bwd(const ress_attn_args* args, const ress_attn_grads* g, void* ws
                      (e = check_tiles(g->dv, a.keys, a.kv_heads, true, "dv"))))
     return e;
   if ((a.rows == 0 && a.keys == 0) || a.n_seqs == 0) return ok();
+  const std::initializer_list<const void*> ins = {a.q.data, a.k.data, a.v.data, a.o.data, g->d_o.data};
+  if ((a.rows > 0 && (e = check_apart(g->dq, "dq", ins))) ||
+      (a.keys > 0 && ((e = check_apart(g->dk, "dk", ins)) || (e = check_apart(g->dv, "dv", ins)))))
+    return e;
   a.d_o = g->d_o, a.dq = g->dq, a.dk = g->dk, a.dv = g->dv;
   cudaError_t ce = ress::launch_flash_bwd(a, static_cast<cudaStream_t>(stream));
   if (ce != cudaSuccess) return cuda_fail(ce, "ress_attn_bwd");
@@ -1092,6 +1106,7 @@ int ress_paged_attn(const ress_attn_args* args, const ress_pages* pages, void* w
   int e = attn_checks(args, pages, false, ws, ws_bytes, &a);
   if (e) return e;
   if (a.rows == 0 || a.n_seqs == 0) return ok();
+  if ((e = check_apart(a.o, "o", {a.q.data, a.k.data, a.v.data}))) return e;
   cudaError_t ce = ress::launch_flash(a, static_cast<cudaStream_t>(stream));
   if (ce != cudaSuccess) return cuda_fail(ce, "ress_paged_attn");
   return ok();

@@ -57,7 +57,7 @@ def call(name, *a, ws=WS, size=1 << 40):
 
 
 BAD = [("type", 2, EUNSUPPORTED), ("type", -1, EUNSUPPORTED), ("q_heads", 0, EUNSUPPORTED), ("q_heads", 5, EUNSUPPORTED),
-       ("q_heads", 130, EUNSUPPORTED), ("kv_heads", 0, EUNSUPPORTED), ("n_seqs", -1, EINVAL), ("causal", 2, EINVAL),
+       ("q_heads", 130, EUNSUPPORTED), ("kv_heads", 0, EUNSUPPORTED), ("n_seqs", -1, EINVAL), ("n_seqs", (1 << 20) + 1, EINVAL), ("causal", 2, EINVAL),
        ("cap", -1.0, EINVAL), ("cap", float("nan"), EINVAL), ("cap", float("inf"), EINVAL), ("cap", 1e-31, EINVAL),
        ("rows", -1, EINVAL), ("rows", 1 << 31, EINVAL), ("q_start", None, EINVAL), ("q_start", AT + 2, EINVAL),
        ("prefix", AT + 1, EINVAL), ("slopes", AT + 1, EINVAL), ("lse", AT + 2, EINVAL), ("q", Heads(None, 256, 64), EINVAL),
@@ -117,6 +117,17 @@ def test_workspaces():
     for rows, heads_ in ((-1, 4), (1 << 31, 4), (5, 0)):
         with pytest.raises(ress.RessError):
             ress.attn_workspace_bytes(rows, heads_)
+
+
+def test_outputs_are_not_inputs():
+    assert call("ress_attn", args()) == EINVAL
+    assert call("ress_paged_attn", args(), Pages(AT, AT, 8, 8, 64, 100, 64 * 128, 64 * 128)) == EINVAL
+    assert b"o must not be an input" in ress._lib.ress_last_error()
+    for name in ("dq", "dk", "dv"):
+        g = Grads(heads(4), *(heads(n, AT + (i << 24)) for i, n in ((1, 4), (2, 2), (3, 2))))
+        setattr(g, name, heads(4 if name == "dq" else 2))
+        assert call("ress_attn_bwd", args(), g) == EINVAL
+        assert name.encode() + b" must not be an input" in ress._lib.ress_last_error()
 
 
 def test_nothing_to_do_launches_nothing():
