@@ -670,6 +670,14 @@ def _on_current_device(t):
         raise ValueError(f"tensors on {t.device}, which is not the current CUDA device")
 
 
+def _scratch_beside(ws, t):
+    """As _scratch, of a workspace on t's device."""
+    s = _scratch(ws)
+    if ws is not None and ws.get_device() != t.get_device():
+        raise ValueError(f"ws is on {ws.device}, the tensors on {t.device}")
+    return s
+
+
 def _attn_args(q, k, v, o, lse, q_start, k_start, prefix, slopes, causal, cap, paged):
     args = _t.attn_args(q, k, v, o, lse, q_start, k_start, prefix, slopes, bool(causal), cap, paged)
     if args is None:
@@ -729,7 +737,7 @@ def attn(q, k, v, o, ws, q_start=None, k_start=None, lse=None, causal: bool = Fa
     sequence).  causal, prefix (int32 per sequence), cap, slopes (float32 per head of q): see include/ress.h.
     lse: float32 [q_heads, rows] output, or None."""
     a = _attn_args(q, k, v, o, lse, q_start, k_start, prefix, slopes, causal, cap, False)
-    _check(_lib.ress_attn(a, *_scratch(ws), _stream(stream)))
+    _check(_lib.ress_attn(a, *_scratch_beside(ws, q), _stream(stream)))
 
 
 def attn_bwd(do, q, k, v, o, lse, dq, dk, dv, ws, q_start=None, k_start=None, causal: bool = False, prefix=None,
@@ -743,7 +751,7 @@ def attn_bwd(do, q, k, v, o, lse, dq, dk, dv, ws, q_start=None, k_start=None, ca
     if g is None:
         for t, name, like in ((do, "do", q), (dq, "dq", q), (dk, "dk", k), (dv, "dv", k)):
             _refuse_tiles(t, name, q, tuple(like.shape))
-    _check(_lib.ress_attn_bwd(a, g, *_scratch(ws), _stream(stream)))
+    _check(_lib.ress_attn_bwd(a, g, *_scratch_beside(ws, q), _stream(stream)))
 
 
 def paged_attn(q, k_pages, v_pages, table, lens, o, ws, q_start=None, lse=None, causal: bool = False, prefix=None,
@@ -757,7 +765,7 @@ def paged_attn(q, k_pages, v_pages, table, lens, o, ws, q_start=None, lse=None, 
         _refuse_numbers(lens, "lens", q, seqs)
         _refuse_table(table, seqs)
         raise ValueError("lens and table are needed, on q's device")
-    _check(_lib.ress_paged_attn(a, p, *_scratch(ws), _stream(stream)))
+    _check(_lib.ress_paged_attn(a, p, *_scratch_beside(ws, q), _stream(stream)))
 
 
 def _refuse_table(table, seqs=None):
@@ -785,7 +793,7 @@ def cache_tables(have, add, free, taken, table, page: int, lens, q_start, slots,
             _refuse_numbers(t, name, table, size)
         raise ValueError(f"page {page} out of range, or slots and pos of different sizes")
     _on_current_device(table)
-    _check(_lib.ress_cache_tables(a, *_scratch(ws), _stream(stream)))
+    _check(_lib.ress_cache_tables(a, *_scratch_beside(ws, table), _stream(stream)))
 
 
 def cache_write(k, v, slots, k_pages, v_pages, ws, stream=None):
@@ -800,7 +808,7 @@ def cache_write(k, v, slots, k_pages, v_pages, ws, stream=None):
         _refuse_numbers(slots, "slots", k, k.shape[0])
         raise ValueError(f"k has {k.shape[1]} heads, the pages {k_pages.shape[2]}, or slots are missing")
     _on_current_device(k)
-    _check(_lib.ress_cache_write(*a, *_scratch(ws), _stream(stream)))
+    _check(_lib.ress_cache_write(*a, *_scratch_beside(ws, k), _stream(stream)))
 
 
 class Buffers:

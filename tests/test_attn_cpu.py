@@ -119,6 +119,18 @@ def test_workspaces():
             ress.attn_workspace_bytes(rows, heads_)
 
 
+def test_a_workspace_of_another_device(monkeypatch):
+    class On:
+        def __init__(self, n):
+            self.device = f"cuda:{n}"
+            self.get_device = lambda: n
+
+    monkeypatch.setattr(ress, "_scratch", lambda ws: (0, 0))
+    assert ress._scratch_beside(On(0), On(0)) == (0, 0) == ress._scratch_beside(None, On(1))
+    with pytest.raises(ValueError, match="cuda:1"):
+        ress._scratch_beside(On(1), On(0))
+
+
 def test_outputs_are_not_inputs():
     assert call("ress_attn", args()) == EINVAL
     assert call("ress_paged_attn", args(), Pages(AT, AT, 8, 8, 64, 100, 64 * 128, 64 * 128)) == EINVAL
