@@ -432,27 +432,41 @@ __device__ __forceinline__ void mul2(float& d0, float& d1, float a0, float a1, f
       : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
 }
 
-// Products q.k to capped scores in log2 units, a warp's 16 rows x 64 columns.  Where none of them is above half of the cap,
-// x times a polynomial in x^2 (set_cap): five packed instructions a pair on the FMA pipe, next to which the SFU forms the
-// exponentials; else capped2, whose four SFU operations a pair are twice what the exponentials take (with capped2 alone packed
-// documents, cap 30, took 251 us where 239 with both).  A polynomial of one term less up to a quarter of the cap gains nothing.
+// Products q.k to capped scores in log2 units: up to half of the cap x times a polynomial in x^2 (set_cap), five packed
+// instructions a pair on the FMA pipe, next to which the SFU forms the exponentials; above it capped2, whose four SFU operations a
+// pair are twice what the exponentials take (with capped2 alone packed documents, cap 30, took 251 us where 239 with both).  A
+// polynomial of one term less up to a quarter of the cap gains nothing.
+__device__ __forceinline__ void cap_small2(float& x0, float& x1, const DenseArgs& a) {
+  float z0, z1, p0, p1;
+  mul2(z0, z1, x0, x1, x0, x1);
+  fma2(p0, p1, z0, z1, a.cap_poly[3], a.cap_poly[3], a.cap_poly[2], a.cap_poly[2]);
+  fma2(p0, p1, z0, z1, p0, p1, a.cap_poly[1], a.cap_poly[1]);
+  fma2(p0, p1, z0, z1, p0, p1, a.cap_poly[0], a.cap_poly[0]);
+  mul2(x0, x1, x0, x1, p0, p1);
+}
+
+// The same of a warp's 16 rows x 64 columns.  The two forms differ in their last bits, so each product's own size chooses
+// between them: what is not seen (stale rows of a page, a batch's neighbours) changes no bit, and the warp only leaves capped2
+// out where no product needs it.  Measured on f16 documents, cap 30 with no product above half of it, and cap 2 with most of them
+// above: this 179 and 250 us; the warp's largest product choosing for all (what is not seen among them) 179 and 199; the same with zeros
+// for what is not seen 208 and 223, of which most is the code (the loop of the softmax warps is near what the instruction
+// cache holds); capped2 in all tiles with a mask 190 and 205.
 __device__ __forceinline__ void cap_scores(float (&x)[32], const DenseArgs& a, float in, float out) {
   float top = 0.f;
 #pragma unroll
   for (int e = 0; e < 32; e += 2) top = fmax3(top, fabsf(x[e]), fabsf(x[e + 1]));
   if (!__any_sync(0xffffffffu, !(top <= a.cap_small))) {
 #pragma unroll
-    for (int e = 0; e < 32; e += 2) {
-      float z0, z1, p0, p1;
-      mul2(z0, z1, x[e], x[e + 1], x[e], x[e + 1]);
-      fma2(p0, p1, z0, z1, a.cap_poly[3], a.cap_poly[3], a.cap_poly[2], a.cap_poly[2]);
-      fma2(p0, p1, z0, z1, p0, p1, a.cap_poly[1], a.cap_poly[1]);
-      fma2(p0, p1, z0, z1, p0, p1, a.cap_poly[0], a.cap_poly[0]);
-      mul2(x[e], x[e + 1], x[e], x[e + 1], p0, p1);
-    }
+    for (int e = 0; e < 32; e += 2) cap_small2(x[e], x[e + 1], a);
   } else {
 #pragma unroll
-    for (int e = 0; e < 32; e += 2) capped2(x[e], x[e + 1], in, out);
+    for (int e = 0; e < 32; e += 2) {
+      float y0 = x[e], y1 = x[e + 1];
+      const bool s0 = fabsf(y0) <= a.cap_small, s1 = fabsf(y1) <= a.cap_small;
+      cap_small2(y0, y1, a);
+      capped2(x[e], x[e + 1], in, out);
+      x[e] = s0 ? y0 : x[e], x[e + 1] = s1 ? y1 : x[e + 1];
+    }
   }
 }
 
