@@ -113,14 +113,24 @@ __global__ void __launch_bounds__(256) k_flash_rows(const __grid_constant__ Dens
   __shared__ float tops[8];
   rows::stream_acquire();
   const int sub = threadIdx.x & 7, heads = a.kv_heads * a.group;
-  // rows of no sequence do not count
-  const int64_t lo = a.q_start ? max(0, a.q_start[0]) : 0;
-  const int64_t hi = a.q_start ? min(a.rows, (int64_t)a.q_start[a.n_seqs]) : a.rows;
+  // Rows behind the last sequence are left out: those from the largest start on (the last one, unless some are bad: the sequences
+  // around a bad one are as ever).
+  int64_t hi = a.rows;
+  if (a.q_start) {
+    __shared__ int ends[8];
+    int end = 0;
+    for (int b = threadIdx.x; b <= a.n_seqs; b += 256) end = max(end, a.q_start[b]);
+    end = __reduce_max_sync(0xffffffffu, end);
+    if ((threadIdx.x & 31) == 0) ends[threadIdx.x >> 5] = end;
+    __syncthreads();
+    for (int w = 0; w < 8; ++w) end = max(end, ends[w]);
+    hi = min(hi, (int64_t)end);
+  }
   float top = 0.f;
   for (int64_t i = (int64_t)blockIdx.x * 32 + (threadIdx.x >> 3); i < a.rows * heads; i += (int64_t)gridDim.x * 32) {
     const int64_t t = i / heads;
     const int head = (int)(i - t * heads);
-    if (t < lo || t >= hi) continue;  // (all eight lanes)
+    if (t >= hi) continue;  // (all eight lanes)
     const uint4 o = ld_stream(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.o.data) + t * a.o.token_stride +
                                                               head * a.o.head_stride) + sub);
     const uint4 g = ld_stream(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.d_o.data) +
