@@ -466,8 +466,9 @@ int ress_attn(const ress_attn_args* a, void* ws, size_t ws_bytes, void* stream);
 /* Gradients of ress_attn with respect to q, k and v from that of o (d_o): a->o and a->lse as the call
  * wrote them (lse is needed here).  The gradients of heads of K and V that several heads of Q use are
  * added up in float32, in a fixed order.  p and the gradients of the scores are rounded to the
- * tensors' type for their products (in f16 after scaling by a power of two: finite for |v| up to 250 whatever d_o
- * is).  dq, dk, dv are written for the rows and keys of every sequence, and must not overlap inputs.  ws: the workspace of backward = 1. */
+ * tensors' type for their products; in f16 after scaling by powers of two, so that they stay finite whatever v and d_o
+ * are, and of a gradient of a score what is lost is below 2^-39 of 2 |d_o| max|v| (norms over channels, of its sequence; for dq
+ * |d_o| of the row).  dq, dk, dv are written for the rows and keys of every sequence, and must not overlap inputs.  ws: the workspace of backward = 1. */
 typedef struct {
   ress_heads d_o, dq; /* as q */
   ress_heads dk, dv;  /* as k */

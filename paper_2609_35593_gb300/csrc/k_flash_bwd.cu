@@ -17,9 +17,13 @@
 // products 512 (8 images at once, 10,992 rows and keys of 16 heads: 2,200 us; now 1,394, 0.89 PFLOP/s of five products'
 // work or 1.24 of the seven formed).  What bounds it is the chain of a tile from scores to dS and back.  Shares of the work, partial results and waits are those of k_flash.cu.
 //
-// In f16, P is kept times 2^8 and dS times a power of two that brings the largest |dO| to 1..2: probabilities of rows on
-// thousands of keys are below f16's 2^-14, and so may gradients be.  dP is at most 64 max|dO| max|V|, so dS stays
-// finite for |V| up to 250 whatever the values, and is taken back to scale in float32.
+// In f16, P is kept times 2^8 and dS times a power of two: probabilities of rows on thousands of keys are below f16's 2^-14,
+// and so may gradients be.  |dP - delta| is at most 2 |dO| max|V| over the sequence's keys (norms over channels: O is a mean of
+// rows of V), so the power that brings this to 2^14..2^15 keeps dS finite whatever the values are, and what is lost of it below
+// 2^-39 of that bound.  |dO| is that of the row where rows are the accumulators' rows (dQ), and the sequence's largest where the rows are
+// summed over (dK): no row and no sequence takes digits from others.  The largest come from chunks of 16 rows or keys that
+// k_flash_rows leaves, once per sequence and head (k_flash_steps: a launch of some 4 us; looked up by the producers instead,
+// f16 documents took 255 us where 230, 32 images 1,148 where 1,005).  Gradients are taken back to scale in float32.
 #include <cudaTypedefs.h>
 
 #include "attn_work.cuh"
@@ -44,6 +48,7 @@ struct Item {
   int h, at;        // head of K (-1: no more items); first token or key
   int from, t0, t1, g0;  // first row of the first tile (dK, dV); tiles; number of the first among all of the CTA's
   int part;
+  float step;  // f16: the power of two of dS (dK), the largest |V|^2 (dQ)
 };
 
 // What the columns of a tile are, where they are rows of Q (two next to each other are read together).
@@ -77,14 +82,41 @@ __device__ __forceinline__ void give_up(Smem& S, uint32_t* status) {
   *reinterpret_cast<volatile int*>(&S.abort) = 1;
 }
 
-// The power of two that brings the largest |dO| to 1..2 (1 where there is none, or it is not finite).
-__device__ __forceinline__ float grad_scale(const float* big, int n) {
-  float m = 0.f;
-  for (int i = threadIdx.x & 31; i < n; i += 32) m = fmaxf(m, big[i]);
+// The power of two that brings 2 |dO| |V|, by their squares, to 2^14..2^15 (1 where there is none, or they are not finite).
+__device__ __forceinline__ float step_scale(float do2, float v2) {
+  const float b = do2 * v2;
+  if (!(b > 0.f && b < 3e38f)) return 1.f;
+  const int e = (__float_as_int(b) >> 23) - 127;  // sqrt(b) is below 2^((e + 1) / 2)
+  return __int_as_float((127 + 14 - ((e + 2) >> 1)) << 23);
+}
+__device__ __forceinline__ float inverse2(float p) { return __int_as_float((254 << 23) - __float_as_int(p)); }  // of a power of two
+
+__device__ __forceinline__ float square8(uint4 v) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  float s = 0.f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float2 x = unpack2<true>(w[e]);
+    s = fmaf(x.x, x.x, fmaf(x.y, x.y, s));
+  }
+  return s;
+}
+__device__ __forceinline__ const uint4* row_at(const ress_heads& h, int64_t token, int head, int chunk) {
+  return reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(h.data) + token * h.token_stride + head * h.head_stride) + chunk;
+}
+
+// Rows [lo, hi) of a head as whole chunks [c0, c1) and what is left of them at both ends: [lo, e0) and [e1, hi).
+struct Chunks {
+  int c0, c1, e0, e1;
+  __device__ Chunks(int lo, int hi, int chunk) {
+    c0 = (int)(((int64_t)lo + chunk - 1) / chunk), c1 = hi / chunk;
+    e0 = c0 < c1 ? c0 * chunk : hi, e1 = c0 < c1 ? c1 * chunk : hi;
+  }
+};
+__device__ __forceinline__ float warp_max(float m) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  if (!(m > 0.f) || m > 3e38f) return 1.f;
-  return exp2f((float)-ilogbf(fmaxf(m, 1e-30f)));
+  return m;
 }
 
 // Items and the tiles of each.
@@ -107,12 +139,12 @@ __device__ __forceinline__ int item_tiles(const DenseArgs& a, const Seq& s, int 
 }  // namespace
 
 // Per row: log2 of its sum and delta = O . dO, laid out as the tiles of rows read them ([kv_heads, rows, group]), and
-// in f16 the largest |dO| of each CTA's rows.  Eight lanes a row; bound by HBM (O and dO once).
+// in f16 |dO|^2 and the largest of it, and of |V|^2, in chunks.  A chunk of a head per warp, eight lanes a row; bound by HBM
+// (O and dO once; in f16 V too).
 template <bool kF16>
 __global__ void __launch_bounds__(256) k_flash_rows(const __grid_constant__ DenseArgs a) {
-  __shared__ float tops[8];
   rows::stream_acquire();
-  const int sub = threadIdx.x & 7, heads = a.kv_heads * a.group;
+  const int lane = threadIdx.x & 31, sub = lane & 7;
   // Rows behind the last sequence are left out: those from the largest start on (the last one, unless some are bad: the sequences
   // around a bad one are as ever).
   int64_t hi = a.rows;
@@ -121,47 +153,125 @@ __global__ void __launch_bounds__(256) k_flash_rows(const __grid_constant__ Dens
     int end = 0;
     for (int b = threadIdx.x; b <= a.n_seqs; b += 256) end = max(end, a.q_start[b]);
     end = __reduce_max_sync(0xffffffffu, end);
-    if ((threadIdx.x & 31) == 0) ends[threadIdx.x >> 5] = end;
+    if (lane == 0) ends[threadIdx.x >> 5] = end;
     __syncthreads();
     for (int w = 0; w < 8; ++w) end = max(end, ends[w]);
     hi = min(hi, (int64_t)end);
   }
-  float top = 0.f;
-  for (int64_t i = (int64_t)blockIdx.x * 32 + (threadIdx.x >> 3); i < a.rows * heads; i += (int64_t)gridDim.x * 32) {
-    const int64_t t = i / heads;
-    const int head = (int)(i - t * heads);
-    if (t >= hi) continue;  // (all eight lanes)
-    const uint4 o = ld_stream(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.o.data) + t * a.o.token_stride +
-                                                              head * a.o.head_stride) + sub);
-    const uint4 g = ld_stream(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.d_o.data) +
-                                                              t * a.d_o.token_stride + head * a.d_o.head_stride) + sub);
-    const uint32_t ow[4] = {o.x, o.y, o.z, o.w}, gw[4] = {g.x, g.y, g.z, g.w};
-    float sum = 0.f;
+  auto total = [](float x) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float2 x = unpack2<kF16>(ow[e]), y = unpack2<kF16>(gw[e]);
-      sum = fmaf(x.x, y.x, fmaf(x.y, y.y, sum));
-      if (kF16) top = fmaxf(top, fmaxf(fabsf(y.x), fabsf(y.y)));
-    }
-    const uint32_t lanes = 0xffu << (threadIdx.x & 24);
+    for (int s = 4; s > 0; s >>= 1) x += __shfl_xor_sync(0xffffffffu, x, s);
+    return x;
+  };
+  constexpr int kAtOnce = kTopRows / 4;
+  const int heads = a.kv_heads * a.group;
+  const int64_t q_chunks = (a.rows + kTopRows - 1) / kTopRows, v_chunks = kF16 ? (a.keys + a.v_chunk - 1) / a.v_chunk : 0;
+  const int64_t q_units = q_chunks * heads, units = q_units + v_chunks * a.kv_heads;
+  for (int64_t u = blockIdx.x * 8 + (threadIdx.x >> 5); u < units; u += gridDim.x * 8) {
+    // the heads of a chunk next to each other, as they are in memory
+    float top = 0.f;
+    if (u < q_units) {
+      const int64_t c = quotient(u, heads), t0 = c * kTopRows + (lane >> 3);
+      const int head = (int)(u - c * heads), h = head / a.group, g = head - h * a.group;
+      uint4 o[kAtOnce], d[kAtOnce];
 #pragma unroll
-    for (int s = 4; s > 0; s >>= 1) sum += __shfl_xor_sync(lanes, sum, s);
-    if (sub == 0) {
-      const float lse = a.lse[head * a.rows + t];
-      // a row that sees nothing: 2^(s - inf) = 0
-      a.stat[((int64_t)(head / a.group) * a.rows + t) * a.group + head % a.group] =
-          make_float2(lse == -INFINITY ? INFINITY : lse * kLog2e, sum);
+      for (int i = 0; i < kAtOnce; ++i) {
+        o[i] = d[i] = make_uint4(0u, 0u, 0u, 0u);
+        const int64_t t = t0 + 4 * i;
+        if (t < hi) o[i] = ld_stream(row_at(a.o, t, head, sub)), d[i] = ld_stream(row_at(a.d_o, t, head, sub));
+      }
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const uint32_t ow[4] = {o[i].x, o[i].y, o[i].z, o[i].w}, dw[4] = {d[i].x, d[i].y, d[i].z, d[i].w};
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float2 x = unpack2<kF16>(ow[e]), y = unpack2<kF16>(dw[e]);
+          sum = fmaf(x.x, y.x, fmaf(x.y, y.y, sum));
+        }
+        sum = total(sum);
+        const float square = kF16 ? total(square8(d[i])) : 0.f;
+        top = fmaxf(top, square);
+        const int64_t t = t0 + 4 * i;
+        if (sub == 0 && t < hi) {
+          const float lse = a.lse[head * a.rows + t];
+          const int64_t at = ((int64_t)h * a.rows + t) * a.group + g;
+          // a row that sees nothing: 2^(s - inf) = 0
+          a.stat[at] = make_float2(lse == -INFINITY ? INFINITY : lse * kLog2e, sum);
+          if (kF16) a.norm[at] = square;
+        }
+      }
+      if (kF16) {
+        top = warp_max(top);
+        if (lane == 0) a.q_top[head * q_chunks + c] = top;
+      }
+    } else {
+      const int64_t c = quotient(u - q_units, a.kv_heads), k1 = min(a.keys, (c + 1) * a.v_chunk);
+      const int h = (int)(u - q_units - c * a.kv_heads);
+#pragma unroll 1
+      for (int64_t k0 = c * a.v_chunk + (lane >> 3); k0 - (lane >> 3) < k1; k0 += 4 * kAtOnce) {
+        uint4 v[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+          v[i] = make_uint4(0u, 0u, 0u, 0u);
+          if (k0 + 4 * i < k1) v[i] = ld_stream(row_at(a.v, k0 + 4 * i, h, sub));
+        }
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) top = fmaxf(top, total(square8(v[i])));
+      }
+      top = warp_max(top);
+      if (lane == 0) a.v_top[h * v_chunks + c] = top;
     }
   }
-  if (kF16) {
+}
+
+// In f16, of each sequence and head of K, laid out by the sequence's first row ([kv_heads, rows]): the largest |V|^2 of its keys,
+// and the power of two of dS with the largest |dO|^2 of its rows.  A CTA each; bound by latency (two rounds of loads for
+// sequences of some thousand rows).
+constexpr int kStepThreads = 128;
+__global__ void __launch_bounds__(kStepThreads) k_flash_steps(const __grid_constant__ DenseArgs a) {
+  __shared__ float tops[2][kStepThreads / 32];
+  rows::stream_acquire();
+  const int tid = threadIdx.x, G = a.group;
+  const int64_t q_chunks = (a.rows + kTopRows - 1) / kTopRows, v_chunks = (a.keys + a.v_chunk - 1) / a.v_chunk;
+  for (int64_t u = blockIdx.x; u < (int64_t)a.n_seqs * a.kv_heads; u += gridDim.x) {
+    const int b = (int)(u / a.kv_heads), h = (int)(u - (int64_t)b * a.kv_heads);
+    const Seq s = load_seq(a, b, nullptr);
+    if (s.nq == 0) continue;
+    float v2 = 0.f, d2 = 0.f;
+    {
+      const Chunks r(s.k0, s.k0 + s.nk, a.v_chunk);
+#pragma unroll 8
+      for (int c = r.c0 + tid; c < r.c1; c += kStepThreads) v2 = fmaxf(v2, a.v_top[h * v_chunks + c]);
+      const int first = r.e0 - s.k0, n = first + s.k0 + s.nk - r.e1;
+#pragma unroll 4
+      for (int i = 0; i < n; i += kStepThreads / 8) {  // eight lanes a row
+        const int k = i + (tid >> 3);
+        float x = k < n ? square8(*row_at(a.v, k < first ? s.k0 + k : r.e1 + k - first, h, tid & 7)) : 0.f;
 #pragma unroll
-    for (int s = 16; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
-    if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = top;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      for (int w = 1; w < 8; ++w) top = fmaxf(top, tops[w]);
-      a.big[blockIdx.x] = top;
+        for (int o = 4; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+        v2 = fmaxf(v2, x);
+      }
     }
+    {
+      const Chunks r(s.q0, s.q0 + s.nq, kTopRows);
+      for (int c = r.c0 + tid; c < r.c1; c += kStepThreads)
+#pragma unroll 4
+        for (int g = 0; g < G; ++g) d2 = fmaxf(d2, a.q_top[((int64_t)h * G + g) * q_chunks + c]);
+      const float* norm = a.norm + (int64_t)h * a.rows * G;
+      const int first = (r.e0 - s.q0) * G, n = first + (s.q0 + s.nq - r.e1) * G;
+#pragma unroll 4
+      for (int i = tid; i < n; i += kStepThreads)
+        d2 = fmaxf(d2, norm[i < first ? (int64_t)s.q0 * G + i : (int64_t)r.e1 * G + i - first]);
+    }
+    v2 = warp_max(v2), d2 = warp_max(d2);
+    if ((tid & 31) == 0) tops[0][tid >> 5] = v2, tops[1][tid >> 5] = d2;
+    __syncthreads();
+    if (tid == 0) {
+      for (int w = 1; w < kStepThreads / 32; ++w) v2 = fmaxf(v2, tops[0][w]), d2 = fmaxf(d2, tops[1][w]);
+      a.steps[(int64_t)h * a.rows + s.q0] = make_float2(v2, step_scale(d2, v2));
+    }
+    __syncthreads();
   }
 }
 
@@ -243,7 +353,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool failed = false;
       if (a.n_seqs <= 32)
         range = find_range_warp(a, line_of, gridDim.x, blockIdx.x, blockIdx.x == 0 ? a.status : nullptr);
-      const float f = kF16 && kKeys ? grad_scale(a.big, a.n_big) * exp2f(-kPScale) : 1.f;
       if (lane == 0) a.share[2 * blockIdx.x].n = a.share[2 * blockIdx.x + 1].n = -1;
       int col_tok[4];  // token of this lane's columns lane, lane + 32, .. of a tile of rows (past it: never one)
 #pragma unroll
@@ -265,6 +374,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             item.q0 = c.s.q0, item.k0 = c.s.k0, item.nq = c.s.nq, item.nk = c.s.nk, item.d = c.s.d, item.p = c.s.p;
             item.h = c.h, item.at = at, item.from = from, item.t0 = t0, item.t1 = t1;
             item.part = t0 == 0 && t1 == n ? -1 : share_slot(c, range.x0);
+            if (kF16) {
+              item.step = 1.f;
+              if (t0 < t1) item.step = reinterpret_cast<const float*>(a.steps + (int64_t)c.h * a.rows + c.s.q0)[kKeys];
+            }
             if (item.part >= 0)
               a.share[item.part] = DenseShare{t0, t1, n, c.h, (kKeys ? c.s.k0 : c.s.q0) + at,
                                               min((kKeys ? c.s.nk : c.s.nq) - at, kKeys ? 128 : T), {}};
@@ -314,6 +427,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const float2* stat = a.stat + ((int64_t)h * a.rows + item.q0 + item.from) * G + lane;
           const int left = item.nq - item.from, pos0 = item.d + item.from, base = kKeys ? item.q0 + item.from : item.k0;
           const int nk = item.nk, p = item.p, last_key = min(nk, item.at + 128);
+          const float f = kF16 && kKeys ? item.step * exp2f(-kPScale) : 1.f;
           float slope[4] = {0.f, 0.f, 0.f, 0.f};
           if (kKeys && kSlopes) {
 #pragma unroll
@@ -505,7 +619,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     const float kScale = kLog2e * 0.125f;
     const float cap = a.cap, in = a.cap > 0.f ? 0.25f * kLog2e / a.cap : 0.125f * kLog2e, out = a.cap * kLog2e;
     const float back = a.cap > 0.f ? 1.0f / out : 0.f;
-    const float scale = kF16 ? grad_scale(a.big, a.n_big) : 1.f, f = kF16 ? scale * exp2f(-kPScale) : 1.f;
     uint32_t c = 0, it = 0;  // tiles, and items with any, so far
     bool stop = false;
     for (int pub = 0; !stop; ++pub) {
@@ -524,14 +637,18 @@ __global__ void __launch_bounds__(kThreads, 1)
       };
       int tok[2], pos[2], lim[2] = {0, 0}, least = item.nk;
       float nlse[2] = {-INFINITY, -INFINITY}, ndelta[2] = {0.f, 0.f}, slope[2] = {0.f, 0.f};
+      float f[2];  // dS's power of two, over that of P (of both rows the same in the pass over keys)
+      f[0] = f[1] = kF16 && kKeys ? item.step * exp2f(-kPScale) : 1.f;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const int r = r0 + 8 * j;
         tok[j] = token_of(j);
         pos[j] = item.d + tok[j];
         if (!kKeys && exists(j)) {
-          const float2 x = a.stat[((int64_t)item.h * a.rows + item.q0 + tok[j]) * G + S.row_head[r]];
-          nlse[j] = (kF16 ? kPScale : 0.f) - x.x, ndelta[j] = -x.y * f;
+          const int64_t at = ((int64_t)item.h * a.rows + item.q0 + tok[j]) * G + S.row_head[r];
+          const float2 x = a.stat[at];
+          if (kF16) f[j] = step_scale(a.norm[at], item.step) * exp2f(-kPScale);
+          nlse[j] = (kF16 ? kPScale : 0.f) - x.x, ndelta[j] = -x.y * f[j];
           lim[j] = a.causal ? max(0, min(item.nk, max(item.p, pos[j] + 1))) : item.nk;
           least = min(least, lim[j]);
           if (kSlopes) slope[j] = a.slopes[item.h * G + S.row_head[r]] * kLog2e;
@@ -650,7 +767,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           float y0 = __uint_as_float(v[e]), y1 = __uint_as_float(v[e + 1]);
           if (kF16)
-            fma2(y0, y1, y0, y1, f, f, n0, n1);
+            fma2(y0, y1, y0, y1, f[j], f[j], n0, n1);
           else
             add2(y0, y1, y0, y1, n0, n1);
           mul2(y0, y1, y0, y1, x[e], x[e + 1]);
@@ -700,17 +817,17 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(v[e]);
       }
-      const float by = kKeys && side ? (kF16 ? exp2f(-kPScale) : 1.f) : 0.125f / scale;
       const ress_heads& to = kKeys ? (side ? a.dv : a.dk) : a.dq;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const int r = r0 + 8 * j;
         if (!kKeys && side) break;
+        const float by = (kKeys && side ? 1.f : kF16 ? 0.125f * inverse2(f[j]) : 0.125f) * (kF16 ? exp2f(-kPScale) : 1.f);
         if (item.part >= 0) {
           float2* dst = reinterpret_cast<float2*>(a.part + item.part * kPartFloats + (side * 128 + r) * 64 + two);
           if (exists(j)) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) dst[4 * e] = make_float2(o[4 * e + 2 * j], o[4 * e + 2 * j + 1]);
+            for (int e = 0; e < 8; ++e) dst[4 * e] = make_float2(o[4 * e + 2 * j] * by, o[4 * e + 2 * j + 1] * by);
           }
         } else {
           uint32_t w[8];
@@ -757,7 +874,6 @@ __global__ void __launch_bounds__(256) k_flash_bwd_join(const __grid_constant__ 
   const DenseShare item = a.share[blockIdx.x];
   if (item.n < 0 || item.t0 != 0) return;
   const int G = a.group, T = 128 / G, sub = threadIdx.x & 15;
-  const float undo = 0.125f / (kF16 ? grad_scale(a.big, a.n_big) : 1.f);
   for (int i = threadIdx.x >> 4; i < 32; i += 16) {
     const int row = blockIdx.y * 32 + i, which = row >> 7, rr = row & 127;
     if (kKeys ? rr >= item.count : rr >= T * G || rr / G >= item.count) continue;
@@ -768,12 +884,11 @@ __global__ void __launch_bounds__(256) k_flash_bwd_join(const __grid_constant__ 
       if (t1 >= item.n || (s = next_share(a, s, ctas)) < 0) break;
       t1 = a.share[s].t1;
     }
-    const float by = kKeys && which ? (kF16 ? exp2f(-kPScale) : 1.f) : undo;
     const ress_heads& d = kKeys ? (which ? a.dv : a.dk) : a.dq;
     const int64_t token = (int64_t)item.first + (kKeys ? rr : rr / G);
     const int head = kKeys ? item.head : item.head * G + rr % G;
     reinterpret_cast<uint2*>(static_cast<uint16_t*>(d.data) + token * d.token_stride + head * d.head_stride)[sub] =
-        make_uint2(pack2<kF16>(o.x * by, o.y * by), pack2<kF16>(o.z * by, o.w * by));
+        make_uint2(pack2<kF16>(o.x, o.y), pack2<kF16>(o.z, o.w));
   }
 }
 
@@ -791,10 +906,17 @@ template <bool kF16>
 static cudaError_t launch_type(DenseArgs a, cudaStream_t st) {
   const int ctas = dense_ctas();
   cudaError_t e;
+  a.v_chunk = kTopRows;
+  const auto v_chunks = [&] { return (a.keys + a.v_chunk - 1) / a.v_chunk; };
+  while (v_chunks() > kHeadTops || v_chunks() * a.kv_heads > kVTops) a.v_chunk *= 2;
   if (a.rows > 0) {
-    const int64_t rows = a.rows * a.kv_heads * a.group;
-    a.n_big = (int)(rows / 32 < kBigParts ? (rows + 31) / 32 : kBigParts);
-    if ((e = launch_pdl(k_flash_rows<kF16>, dim3(a.n_big), 256, 0, st, true, a)) != cudaSuccess) return e;
+    const int64_t chunks = a.kv_heads * ((a.rows + kTopRows - 1) / kTopRows * a.group + (kF16 ? v_chunks() : 0));
+    const int64_t units = (chunks + 7) / 8, full = 8 * (int64_t)ctas;
+    if ((e = launch_pdl(k_flash_rows<kF16>, dim3((unsigned)(units < full ? units : full)), 256, 0, st, true, a)) != cudaSuccess)
+      return e;
+    const int64_t pairs = (int64_t)a.n_seqs * a.kv_heads, most = 16 * (int64_t)ctas;
+    if (kF16 && (e = launch_pdl(k_flash_steps, dim3((unsigned)(pairs < most ? pairs : most)), kStepThreads, 0, st, true, a)) != cudaSuccess)
+      return e;
   }
   if (a.cap > 0.f) set_cap(a);
   // a tensor without rows or keys is not read, but its map needs some memory

@@ -973,7 +973,10 @@ constexpr int64_t kShareBytes = 2 * ress::kDenseMaxCtas * (int64_t)sizeof(ress::
 
 size_t attn_bytes(int64_t rows, int32_t q_heads, int32_t backward) {
   const int64_t parts = 256 + kShareBytes + ress::align256((int64_t)ress::dense_part_bytes());
-  return (size_t)(backward ? parts + ress::align256(rows * q_heads * 8) + ress::kBigParts * 4 : parts);
+  if (!backward) return (size_t)parts;
+  const int64_t tops = (rows + ress::kTopRows - 1) / ress::kTopRows * q_heads;
+  return (size_t)(parts + 2 * ress::align256(rows * q_heads * 8) + ress::align256(rows * q_heads * 4) + ress::align256(tops * 4) +
+                  ress::kVTops * 4);
 }
 
 int check_rows(int64_t rows, int32_t q_heads) {
@@ -1048,7 +1051,10 @@ int attn_checks(const ress_attn_args* a, const ress_pages* pg, bool backward, vo
   w += kShareBytes;
   out->part = reinterpret_cast<float*>(w);
   out->stat = reinterpret_cast<float2*>(w += ress::align256((int64_t)ress::dense_part_bytes()));
-  out->big = reinterpret_cast<float*>(w + ress::align256(a->rows * a->q_heads * 8));
+  out->steps = reinterpret_cast<float2*>(w += ress::align256(a->rows * a->q_heads * 8));
+  out->norm = reinterpret_cast<float*>(w += ress::align256(a->rows * a->q_heads * 8));
+  out->v_top = reinterpret_cast<float*>(w += ress::align256(a->rows * a->q_heads * 4));
+  out->q_top = out->v_top + ress::kVTops;
   return RESS_OK;
 }
 

@@ -345,8 +345,11 @@ struct DenseArgs {
   float* part;   // partial results of items that several CTAs share
   struct DenseShare* share;  // what each slot of partial results is of
   float2* stat;  // gradient: per row of each head of K, log2 of its sum and o . do
-  float* big;    // gradient in f16: largest |do| of each of n_big parts of the rows
-  int n_big;
+  // gradient in f16: |do|^2 of each row (laid out as stat); the largest |do|^2 and |v|^2 of each head in chunks of
+  // kTopRows rows and v_chunk keys; and what k_flash_steps makes of them
+  float *norm, *q_top, *v_top;
+  float2* steps;
+  int v_chunk;
 };
 // A CTA's share of an item that others have shares of too: tiles t0..t1-1 of n (n -1: none).
 struct DenseShare {
@@ -356,7 +359,8 @@ struct DenseShare {
 };
 constexpr int kDenseMaxCtas = 192;  // most CTAs that share a call's work (one per SM)
 size_t dense_part_bytes();
-constexpr int kBigParts = 1024;
+// v_chunk: kTopRows, and twice as many until there are at most kHeadTops chunks of a head and kVTops in all.
+constexpr int kTopRows = 16, kHeadTops = 4096, kVTops = 1 << 18;
 cudaError_t launch_flash(const DenseArgs& a, cudaStream_t st);
 cudaError_t launch_flash_bwd(const DenseArgs& a, cudaStream_t st);
 // Tensor maps of the dense attention: heads of Q of one head of K, `tokens` tokens of them per box; and heads
