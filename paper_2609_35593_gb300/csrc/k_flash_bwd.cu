@@ -26,6 +26,8 @@
 // f16 documents took 255 us where 230, 32 images 1,148 where 1,005).  Gradients are taken back to scale in float32.
 #include <cudaTypedefs.h>
 
+#include <type_traits>
+
 #include "attn_work.cuh"
 
 namespace ress {
@@ -697,46 +699,51 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
         };
-        // P
-        if (kGen == 1 || (kSlopes && cap > 0.f)) cap_scores(x, a, in, out);
+        // P; kCap: 0, no cap; 1, no product above half of it; 2, any
+        auto probabilities = [&](auto cap_form) {
+          constexpr int kCap = decltype(cap_form)::value;
 #pragma unroll
-        for (int e = 0; e < 32; e += 2) {
-          const int j = e >> 1 & 1, col = 64 * side + 8 * (e >> 2) + two;  // row, columns col and col + 1
-          float l0 = nlse[j], l1 = nlse[j];
-          if (kKeys) {
-            const float2 l = *reinterpret_cast<const float2*>(&cols.lse[col]);
-            l0 = l.x, l1 = l.y;
-          }
-          float x0 = x[e], x1 = x[e + 1];
-          float c0 = 1.f, c1 = 1.f;
-          if (kGen) {
-            if (!kSlopes || cap > 0.f) {
-              float u0, u1;
-              mul2(u0, u1, x0, x1, back, back);
-              fma2(c0, c1, -u0, -u1, u0, u1, 1.f, 1.f);
-            } else {
-              x0 *= in, x1 *= in;
+          for (int e = 0; e < 32; e += 2) {
+            const int j = e >> 1 & 1, col = 64 * side + 8 * (e >> 2) + two;  // row, columns col and col + 1
+            float l0 = nlse[j], l1 = nlse[j];
+            if (kKeys) {
+              const float2 l = *reinterpret_cast<const float2*>(&cols.lse[col]);
+              l0 = l.x, l1 = l.y;
             }
-            if (kSlopes) {
-              if (kKeys) {
-                const float2 q = *reinterpret_cast<const float2*>(&cols.pos[col]);
-                const float2 m = *reinterpret_cast<const float2*>(&cols.slope[col]);
-                x0 = fmaf(-m.x, fabsf(q.x - (float)(r0 + 8 * j)), x0);
-                x1 = fmaf(-m.y, fabsf(q.y - (float)(r0 + 8 * j)), x1);
-              } else {
-                x0 = fmaf(-slope[j], fabsf((float)(pos[j] - key - col)), x0);
-                x1 = fmaf(-slope[j], fabsf((float)(pos[j] - key - col - 1)), x1);
+            float x0 = x[e], x1 = x[e + 1];
+            float c0 = 1.f, c1 = 1.f;
+            if (kGen) {
+              if (kCap)
+                cap_slope2<kCap == 2>(x0, x1, c0, c1, a, in, out, back);
+              else
+                x0 *= in, x1 *= in;
+              if (kSlopes) {
+                if (kKeys) {
+                  const float2 q = *reinterpret_cast<const float2*>(&cols.pos[col]);
+                  const float2 m = *reinterpret_cast<const float2*>(&cols.slope[col]);
+                  x0 = fmaf(-m.x, fabsf(q.x - (float)(r0 + 8 * j)), x0);
+                  x1 = fmaf(-m.y, fabsf(q.y - (float)(r0 + 8 * j)), x1);
+                } else {
+                  x0 = fmaf(-slope[j], fabsf((float)(pos[j] - key - col)), x0);
+                  x1 = fmaf(-slope[j], fabsf((float)(pos[j] - key - col - 1)), x1);
+                }
               }
+              add2(x0, x1, x0, x1, l0, l1);
+            } else {
+              fma2(x0, x1, x0, x1, kScale, kScale, l0, l1);
             }
-            add2(x0, x1, x0, x1, l0, l1);
-          } else {
-            fma2(x0, x1, x0, x1, kScale, kScale, l0, l1);
+            x0 = ex2(x0), x1 = ex2(x1);
+            if (kKeys) w[e >> 1] = pack2<kF16>(x0, x1);
+            if (kCap) mul2(x0, x1, x0, x1, c0, c1);
+            x[e] = x0, x[e + 1] = x1;  // p, times the cap's slope
           }
-          x0 = ex2(x0), x1 = ex2(x1);
-          if (kKeys) w[e >> 1] = pack2<kF16>(x0, x1);
-          if (kGen) mul2(x0, x1, x0, x1, c0, c1);
-          x[e] = x0, x[e + 1] = x1;  // p, times the cap's slope
-        }
+        };
+        if (kGen == 0 || (kSlopes && cap == 0.f))
+          probabilities(std::integral_constant<int, 0>());
+        else if (!any_above_cap(x, a))
+          probabilities(std::integral_constant<int, kGen == 0 ? 0 : 1>());
+        else
+          probabilities(std::integral_constant<int, kGen == 0 ? 0 : 2>());
         masks([&](int e, bool seen) {
           x[e] = seen ? x[e] : 0.f;
           w[e >> 1] &= seen ? 0xffffffffu : e & 1 ? 0x0000ffffu : 0xffff0000u;
