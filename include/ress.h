@@ -436,7 +436,7 @@ int ress_qkv_proj(const ress_dims* dims, const uint16_t* x, const uint16_t* W_q,
  * there is one head or one token), data 16-byte aligned.  Heads h g .. h g + g - 1 of Q use head h
  * of K and V, g = q_heads / kv_heads at most RESS_MAX_GROUP.  The starts of the sequences are device
  * data, so that a captured graph serves other lengths: q_start[n_seqs + 1] ascending; rows behind the last
- * sequence change nothing and are not written.  o and lse must not overlap inputs.  A start or a length
+ * sequence change nothing and are not written.  o and lse must not share memory with inputs or one another.  A start or a length
  * outside its tensor is recorded in the status word (RESS_EDEVICE); that sequence then has no rows
  * (or keys).  ws: 256-byte aligned, ress_attn_workspace_bytes(rows, q_heads, backward) bytes, a status
  * word first (zero before the first call, read by ress_status); the rest needs no initialisation.
@@ -468,7 +468,7 @@ int ress_attn(const ress_attn_args* a, void* ws, size_t ws_bytes, void* stream);
  * added up in float32, in a fixed order.  p and the gradients of the scores are rounded to the
  * tensors' type for their products; in f16 after scaling by powers of two, so that they stay finite whatever v and d_o
  * are, and of a gradient of a score what is lost is below 2^-39 of 2 |d_o| max|v| (norms over channels, of its sequence; for dq
- * |d_o| of the row).  dq, dk, dv are written for the rows and keys of every sequence, and must not overlap inputs.  ws: the workspace of backward = 1. */
+ * |d_o| of the row).  dq, dk, dv are written for the rows and keys of every sequence, and must not share memory with inputs or one another.  ws: the workspace of backward = 1. */
 typedef struct {
   ress_heads d_o, dq; /* as q */
   ress_heads dk, dv;  /* as k */
@@ -499,8 +499,8 @@ int ress_paged_attn(const ress_attn_args* a, const ress_pages* pages, void* ws, 
  * among all of them; slots, pos [n_slots]: each new token's row in the cache (page x page size +
  * row) and its position in its sequence, -1 behind the last token; taken_out[0], the free pages used
  * so far.  Where pages, table columns or slots do not suffice, or a length is negative, the status word says so,
- * and tokens without a place get slot -1.  All device int32; outputs must not be inputs, but for
- * the table.  ws: 256 bytes, a status word as above. */
+ * and tokens without a place get slot -1.  All device int32; outputs must not share memory with inputs or one
+ * another (entries of the table that are held already are read).  ws: 256 bytes, a status word as above. */
 typedef struct {
   int32_t n_seqs;  /* 0..RESS_MAX_SEQS                  */
   int32_t page;    /* tokens of a page, >= 1            */
@@ -513,7 +513,8 @@ int ress_cache_tables(const ress_tables* t, void* ws, size_t ws_bytes, void* str
 
 /* Writes K and V of `tokens` tokens (heads as in ress_attn, any 16-bit type) to rows slots[i] of the
  * pages (kc, vc: as k and v of ress_paged_attn); a slot of -1 is passed over, another one outside the
- * pages is recorded in the status word.  Slots must differ.  ws: 256 bytes, a status word as above. */
+ * pages is recorded in the status word.  Slots must differ, and kc and vc must not share memory; k and v may be rows of
+ * the pages that no slot names.  ws: 256 bytes, a status word as above. */
 int ress_cache_write(int64_t tokens, int32_t kv_heads, const ress_heads* k, const ress_heads* v,
                      const int32_t* slots, const ress_heads* kc, const ress_heads* vc,
                      int64_t k_page_stride, int64_t v_page_stride, int32_t page, int64_t n_pages,

@@ -8,6 +8,7 @@
 #include <string.h>
 
 #include <atomic>
+#include <algorithm>
 #include <initializer_list>
 #include <mutex>
 
@@ -1058,10 +1059,70 @@ int attn_checks(const ress_attn_args* a, const ress_pages* pg, bool backward, vo
   return RESS_OK;
 }
 
-// Outputs are written while other CTAs still read the inputs.
-int check_apart(const ress_heads& out, const char* name, std::initializer_list<const void*> ins) {
-  for (const void* p : ins)
-    if (out.data == p) return fail(RESS_EINVAL, "%s must not be an input", name);
+// Bytes that a tensor holds: runs of `width`, count[k] of them `step[k]` apart in each dimension.
+struct Runs {
+  const void* at;
+  int64_t width;
+  struct { int64_t count, step; } dims[3];
+};
+Runs run_of(const void* p, int64_t bytes) { return {p, p ? bytes : 0, {{1, 0}, {1, 0}, {1, 0}}}; }
+Runs runs_of(const ress_heads& h, int64_t tokens, int heads, int64_t pages = 1, int64_t page_stride = 0) {
+  return {h.data, 128, {{pages, 2 * page_stride}, {tokens, 2 * h.token_stride}, {heads, 2 * h.head_stride}}};
+}
+
+// Whether dims[k..] with factors in lo..hi each take d into (-w_b, w_a).  steps is descending; `tries` bounds the search
+// (false where it ends: such strides are not refused).
+struct Factor {
+  int64_t lo, hi, step;
+};
+bool reaches(const Factor* f, int n, int64_t d, int64_t w_a, int64_t w_b, int& tries) {
+  if (n == 0) return d > -w_b && d < w_a;
+  int64_t low = 0, high = 0;  // what the dimensions after this one add
+  for (int k = 1; k < n; ++k) low += f[k].lo * f[k].step, high += f[k].hi * f[k].step;
+  // -w_b - high < d + m step < w_a - low
+  const auto below = [](int64_t a, int64_t b) { return a / b - (a % b < 0); };  // floor
+  const int64_t from = std::max(f->lo, below(-w_b - high - d, f->step) + 1), to = std::min(f->hi, -below(-(w_a - low - d), f->step) - 1);
+  for (int64_t m = from; m <= to && tries > 0; ++m, --tries)
+    if (reaches(f + 1, n - 1, d + m * f->step, w_a, w_b, tries)) return true;
+  return false;
+}
+// Whether two tensors share a byte.  Views that lie between one another (heads of one tensor of projections) do not.
+bool meet(const Runs& a, const Runs& b) {
+  int64_t span_a = a.width, span_b = b.width;
+  if (!a.width || !b.width) return false;
+  Factor f[6];
+  int n = 0;
+  for (int k = 0; k < 3; ++k) {
+    const auto &x = a.dims[k], &y = b.dims[k];
+    if (x.count < 1 || y.count < 1) return false;
+    span_a += (x.count - 1) * x.step * (x.count > 1), span_b += (y.count - 1) * y.step * (y.count > 1);
+    if (x.count > 1 && y.count > 1 && x.step == y.step)
+      f[n++] = {1 - x.count, y.count - 1, x.step};
+    else {
+      if (x.count > 1) f[n++] = {1 - x.count, 0, x.step};
+      if (y.count > 1) f[n++] = {0, y.count - 1, y.step};
+    }
+  }
+  const int64_t d = static_cast<int64_t>(reinterpret_cast<uintptr_t>(b.at) - reinterpret_cast<uintptr_t>(a.at));
+  if (d == 0) return true;
+  if (d >= span_a || d <= -span_b) return false;
+  std::sort(f, f + n, [](const Factor& x, const Factor& y) { return x.step > y.step; });
+  int tries = 10000;
+  return reaches(f, n, d, a.width, b.width, tries);
+}
+
+// Outputs are written while other CTAs still read the inputs, and by several warps at once.
+struct Named {
+  Runs runs;
+  const char* name;
+};
+int check_apart(std::initializer_list<Named> outs, std::initializer_list<Runs> ins) {
+  for (const Named* o = outs.begin(); o != outs.end(); ++o) {
+    for (const Runs& i : ins)
+      if (meet(o->runs, i)) return fail(RESS_EINVAL, "%s must not be an input or share memory with one", o->name);
+    for (const Named* p = outs.begin(); p != o; ++p)
+      if (meet(o->runs, p->runs)) return fail(RESS_EINVAL, "%s must not share memory with %s", o->name, p->name);
+  }
   return RESS_OK;
 }
 
@@ -1078,7 +1139,9 @@ int ress_attn(const ress_attn_args* args, void* ws, size_t ws_bytes, void* strea
   int e = attn_checks(args, nullptr, false, ws, ws_bytes, &a);
   if (e) return e;
   if (a.rows == 0 || a.n_seqs == 0) return ok();
-  if ((e = check_apart(a.o, "o", {a.q.data, a.k.data, a.v.data}))) return e;
+  if ((e = check_apart({{runs_of(a.o, a.rows, args->q_heads), "o"}, {run_of(a.lse, a.rows * args->q_heads * 4), "lse"}},
+                       {runs_of(a.q, a.rows, args->q_heads), runs_of(a.k, a.keys, a.kv_heads), runs_of(a.v, a.keys, a.kv_heads)})))
+    return e;
   cudaError_t ce = ress::launch_flash(a, static_cast<cudaStream_t>(stream));
   if (ce != cudaSuccess) return cuda_fail(ce, "ress_attn");
   return ok();
@@ -1096,9 +1159,10 @@ int ress_attn_bwd(const ress_attn_args* args, const ress_attn_grads* g, void* ws
                      (e = check_tiles(g->dv, a.keys, a.kv_heads, true, "dv"))))
     return e;
   if ((a.rows == 0 && a.keys == 0) || a.n_seqs == 0) return ok();
-  const std::initializer_list<const void*> ins = {a.q.data, a.k.data, a.v.data, a.o.data, g->d_o.data};
-  if ((a.rows > 0 && (e = check_apart(g->dq, "dq", ins))) ||
-      (a.keys > 0 && ((e = check_apart(g->dk, "dk", ins)) || (e = check_apart(g->dv, "dv", ins)))))
+  const auto rows = [&](const ress_heads& h) { return runs_of(h, a.rows, args->q_heads); };
+  const auto keys = [&](const ress_heads& h) { return runs_of(h, a.keys, a.kv_heads); };
+  if ((e = check_apart({{rows(g->dq), "dq"}, {keys(g->dk), "dk"}, {keys(g->dv), "dv"}},
+                       {rows(a.q), keys(a.k), keys(a.v), rows(a.o), rows(g->d_o), run_of(a.lse, a.rows * args->q_heads * 4)})))
     return e;
   a.d_o = g->d_o, a.dq = g->dq, a.dk = g->dk, a.dv = g->dv;
   cudaError_t ce = ress::launch_flash_bwd(a, static_cast<cudaStream_t>(stream));
@@ -1112,7 +1176,10 @@ int ress_paged_attn(const ress_attn_args* args, const ress_pages* pages, void* w
   int e = attn_checks(args, pages, false, ws, ws_bytes, &a);
   if (e) return e;
   if (a.rows == 0 || a.n_seqs == 0) return ok();
-  if ((e = check_apart(a.o, "o", {a.q.data, a.k.data, a.v.data}))) return e;
+  if ((e = check_apart({{runs_of(a.o, a.rows, args->q_heads), "o"}, {run_of(a.lse, a.rows * args->q_heads * 4), "lse"}},
+                       {runs_of(a.q, a.rows, args->q_heads), runs_of(a.k, a.page, a.kv_heads, a.n_pages, a.k_page_stride),
+                        runs_of(a.v, a.page, a.kv_heads, a.n_pages, a.v_page_stride)})))
+    return e;
   cudaError_t ce = ress::launch_flash(a, static_cast<cudaStream_t>(stream));
   if (ce != cudaSuccess) return cuda_fail(ce, "ress_paged_attn");
   return ok();
@@ -1128,17 +1195,19 @@ int ress_cache_tables(const ress_tables* t, void* ws, size_t ws_bytes, void* str
       t->n_free < 0 || t->n_free > INT32_MAX || t->n_slots < 0 || t->n_slots > INT32_MAX)
     return fail(RESS_EINVAL, "table of %d columns, %lld apart, %lld free pages, %lld slots: out of range", t->table_cols,
                 (long long)t->table_stride, (long long)t->n_free, (long long)t->n_slots);
-  const struct { const int32_t* p; bool needed; const char* name; } ins[] = {
-      {t->have, t->n_seqs > 0, "have"}, {t->add, t->n_seqs > 0, "add"}, {t->free, t->n_free > 0, "free"}, {t->taken, true, "taken"}},
-      outs[] = {{t->table, t->n_seqs > 0 && t->table_cols > 0, "table"}, {t->lens, t->n_seqs > 0, "lens"},
-                {t->q_start, true, "q_start"}, {t->slots, t->n_slots > 0, "slots"}, {t->pos, t->n_slots > 0, "pos"},
-                {t->taken_out, true, "taken_out"}};
-  for (const auto& i : ins)
-    if (i.needed && (e = check_ptr(i.p, 4, i.name))) return e;
-  for (const auto& o : outs) {
-    if (o.needed && (e = check_ptr(o.p, 4, o.name))) return e;
-    for (const auto& i : ins)
-      if (o.needed && i.needed && o.p == i.p) return fail(RESS_EINVAL, "%s must not be %s", o.name, i.name);
+  // (the table is read as well, by the tokens that do not begin a page)
+  struct { const int32_t* p; int64_t n; const char* name; } all[] = {
+      {t->have, t->n_seqs, "have"}, {t->add, t->n_seqs, "add"}, {t->free, t->n_free, "free"}, {t->taken, 1, "taken"},
+      {t->table, t->n_seqs > 0 ? t->table_cols : 0, "table"}, {t->lens, t->n_seqs, "lens"}, {t->q_start, t->n_seqs + 1, "q_start"},
+      {t->slots, t->n_slots, "slots"}, {t->pos, t->n_slots, "pos"}, {t->taken_out, 1, "taken_out"}};
+  constexpr int kIns = 4, kAll = 10, kTable = 4;
+  Runs runs[kAll];
+  for (int i = 0; i < kAll; ++i) {
+    if (all[i].n > 0 && (e = check_ptr(all[i].p, 4, all[i].name))) return e;
+    runs[i] = run_of(all[i].p, all[i].n * 4);
+    if (i == kTable && t->n_seqs > 0) runs[i].dims[0] = {t->n_seqs, 4 * t->table_stride};
+    for (int k = 0; k < i && i >= kIns; ++k)
+      if (meet(runs[i], runs[k])) return fail(RESS_EINVAL, "%s must not share memory with %s", all[i].name, all[k].name);
   }
   if ((e = check_scratch(ws, ws_bytes, 256))) return e;
   ress::CacheTablesArgs a{t->n_seqs, t->page, t->table_cols, t->n_free, t->n_slots, t->table_stride, t->have, t->add,
@@ -1168,6 +1237,10 @@ int ress_cache_write(int64_t tokens, int32_t kv_heads, const ress_heads* k, cons
   for (int64_t s : {k_page_stride, v_page_stride})
     if (n_pages > 1 && (s < 64 || s % 8 || s > INT64_MAX / 16 / n_pages))
       return fail(RESS_EINVAL, "page stride %lld is not a multiple of 8 in range", (long long)s);
+  // (k and v may be rows of the pages that no slot names)
+  if ((e = check_apart({{runs_of(*kc, page, kv_heads, n_pages, k_page_stride), "kc"}, {runs_of(*vc, page, kv_heads, n_pages, v_page_stride), "vc"}},
+                       {})))
+    return e;
   ress::CacheWriteArgs a{tokens, n_pages, kv_heads, page, *k, *v, *kc, *vc, k_page_stride, v_page_stride, slots,
                          static_cast<uint32_t*>(ws)};
   cudaError_t ce = ress::launch_cache_write(a, static_cast<cudaStream_t>(stream));
