@@ -11,9 +11,10 @@ Forward, all on this package's kernels:
     y = x + O W_o^T
 Calibration (the paper's Sec. 4.4 takes head budgets as given; Appendix D allots them by the Fisher
 information of the heads' QKV projections, the squares of the gradients with respect to their outputs):
-the gradient of a loss goes back through dense attention (attn, attn_bwd), then through the rotation
-and the head norm (rope_bwd) to the projections' outputs, and on through the projections and
-layer_norm_bwd to the residual stream, as a training step would take it.
+the gradient of a loss goes back through dense attention (attn, attn_bwd: O, its gradient and the
+probabilities in bf16, as the sublayer itself holds them, sums in float32), then through the rotation and the
+head norm (rope_bwd) to the projections' outputs, and on through the projections and layer_norm_bwd to the
+residual stream, bf16 or float32, as a training step would take it.
 """
 import argparse
 import os
@@ -96,7 +97,7 @@ class Sublayer:
         lse = torch.empty(self.H, self.N, device="cuda", dtype=torch.float32)
         aws = torch.zeros(ress.attn_workspace_bytes(self.N, self.H, backward=True), dtype=torch.uint8, device="cuda")
         ress.attn(self.Q, self.K, self.V, O, aws, lse=lse)
-        dO = (dy @ self.W_o).view(self.N, self.H, 64)
+        dO = (dy.float() @ self.W_o.float()).to(O.dtype).view(self.N, self.H, 64)
         ress.attn_bwd(dO, self.Q, self.K, self.V, O, lse, dQ, dK, dV, aws)
         ress.status(aws)
         dq, dk = torch.empty_like(dQ), torch.empty_like(dK)
