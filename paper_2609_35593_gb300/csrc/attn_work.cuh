@@ -504,6 +504,9 @@ __device__ __forceinline__ void cap_slope2(float& x0, float& x1, float& c0, floa
   }
 }
 
+// Which kernel: 1, with a cap; 2, with slopes; 3, both.
+inline int dense_gen(const DenseArgs& a) { return (a.cap > 0.f ? 1 : 0) + (a.slopes ? 2 : 0); }
+
 // tanh(u) / u for u^2 = z up to 1/4: a polynomial fitted to it at Chebyshev points by reweighted least squares, off by
 // 2^-20.8 of itself; its coefficients times what makes x = q.k out of u = x / (8 cap), and log2(e) cap u of tanh(u).
 inline void set_cap(DenseArgs& a) {

@@ -98,8 +98,8 @@ __device__ __forceinline__ int item_tiles(const DenseArgs& a, const Seq& q, int 
 
 }  // namespace
 
-// kGen: 1, capped scores; 2, scores with slopes, capped or not; 0, neither.  (One kernel for 1 and 2 keeps slopes in
-// registers and spills others: packed documents with a cap 218 us where 186.)
+// kGen: 1, capped scores; 2, scores with slopes; 3, both; 0, neither.  (One kernel for caps and slopes keeps slopes in registers and
+// spills others: packed documents with a cap 218 us where 186; one for 2 and 3 takes 406 us where 346 on 10,992 causal rows.)
 template <bool kF16, int kGen>
 __global__ void __launch_bounds__(kThreads, 1)
     k_flash(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   volatile int* abort = &S.abort;
   const int G = a.group, T = 128 / G;
-  constexpr bool kSlopes = kGen == 2;
+  constexpr bool kSlopes = kGen >= 2, kCap = kGen & 1;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -415,7 +415,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int r0 = quarter * 32 + half * 16 + (lane >> 2), two = 2 * (lane & 3);  // this lane's rows: r0, r0 + 8; columns
     const uint32_t tm = tmem + slot * kColSlot + ((uint32_t)(quarter * 32 + half * 16) << 16);
     const float kScale = kGen ? 1.0f : kLog2e * 0.125f;
-    const float cap = a.cap, in = a.cap > 0.f ? 0.25f * kLog2e / a.cap : 0.125f * kLog2e, out = a.cap * kLog2e;
+    const float in = kCap ? 0.25f * kLog2e / a.cap : 0.125f * kLog2e, out = a.cap * kLog2e;
     // p = 2^(x kScale - m) of 64 columns, packed, and their sums
     auto exps = [&](const float (&x)[32], const float (&m)[2], uint32_t (&w)[16], float (&sum)[2]) {
       float s[2][2] = {{0.f, 0.f}, {0.f, 0.f}};
@@ -499,7 +499,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(v[e]);
         if (kGen) {
-          if (!kSlopes || cap > 0.f) {
+          if (kCap) {
             cap_scores(x, a, in, out);
           } else {
 #pragma unroll
@@ -868,9 +868,9 @@ cudaError_t launch_flash(const DenseArgs& args, cudaStream_t st) {
       !make_key_map(&tv, v, a.type, keys, pages, a.v_page_stride, a.kv_heads, box))
     return cudaErrorInvalidValue;
   const bool f16 = a.type == RESS_F16;
-  auto kern = a.slopes     ? (f16 ? k_flash<true, 2> : k_flash<false, 2>)
-              : a.cap > 0.f ? (f16 ? k_flash<true, 1> : k_flash<false, 1>)
-                            : (f16 ? k_flash<true, 0> : k_flash<false, 0>);
+  decltype(&k_flash<false, 0>) const kernels[4][2] = {{k_flash<false, 0>, k_flash<true, 0>}, {k_flash<false, 1>, k_flash<true, 1>},
+                                                       {k_flash<false, 2>, k_flash<true, 2>}, {k_flash<false, 3>, k_flash<true, 3>}};
+  const auto kern = kernels[dense_gen(a)][f16];
   const size_t smem = sizeof(Smem) + 1024;
   const int ctas = dense_ctas();
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);

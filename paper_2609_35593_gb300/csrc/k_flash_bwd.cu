@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   volatile int* abort = &S.abort;
   const int G = a.group, T = 128 / G;
   constexpr int kSums = kKeys ? 2 : 1;  // issuers of sums
-  constexpr bool kSlopes = kGen == 2;   // (kGen as in k_flash)
+  constexpr bool kSlopes = kGen >= 2, kCap = kGen & 1;  // (kGen as in k_flash)
   static_assert(offsetof(Smem, B2) == offsetof(Smem, B1) + kStages * kTileBytes && kTileBytes == sizeof S.A[0][0], "tiles one after another");
 
   if (threadIdx.x == 0) {
@@ -619,8 +619,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int r0 = quarter * 32 + half * 16 + (lane >> 2), two = 2 * (lane & 3);  // this lane's rows: r0, r0 + 8; columns
     const uint32_t tm = tmem + ((uint32_t)(quarter * 32 + half * 16) << 16);
     const float kScale = kLog2e * 0.125f;
-    const float cap = a.cap, in = a.cap > 0.f ? 0.25f * kLog2e / a.cap : 0.125f * kLog2e, out = a.cap * kLog2e;
-    const float back = a.cap > 0.f ? 1.0f / out : 0.f;
+    const float in = kCap ? 0.25f * kLog2e / a.cap : 0.125f * kLog2e, out = a.cap * kLog2e;
+    const float back = kCap ? 1.0f / out : 0.f;
     uint32_t c = 0, it = 0;  // tiles, and items with any, so far
     bool stop = false;
     for (int pub = 0; !stop; ++pub) {
@@ -699,9 +699,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
         };
-        // P; kCap: 0, no cap; 1, no product above half of it; 2, any
-        auto probabilities = [&](auto cap_form) {
-          constexpr int kCap = decltype(cap_form)::value;
+        // P; kLarge: a product may be above half of the cap
+        auto probabilities = [&](auto large) {
+          constexpr bool kLarge = decltype(large)::value;
 #pragma unroll
           for (int e = 0; e < 32; e += 2) {
             const int j = e >> 1 & 1, col = 64 * side + 8 * (e >> 2) + two;  // row, columns col and col + 1
@@ -714,7 +714,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             float c0 = 1.f, c1 = 1.f;
             if (kGen) {
               if (kCap)
-                cap_slope2<kCap == 2>(x0, x1, c0, c1, a, in, out, back);
+                cap_slope2<kLarge>(x0, x1, c0, c1, a, in, out, back);
               else
                 x0 *= in, x1 *= in;
               if (kSlopes) {
@@ -738,12 +738,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             x[e] = x0, x[e + 1] = x1;  // p, times the cap's slope
           }
         };
-        if (kGen == 0 || (kSlopes && cap == 0.f))
-          probabilities(std::integral_constant<int, 0>());
-        else if (!any_above_cap(x, a))
-          probabilities(std::integral_constant<int, kGen == 0 ? 0 : 1>());
+        if (!kCap || !any_above_cap(x, a))
+          probabilities(std::false_type());
         else
-          probabilities(std::integral_constant<int, kGen == 0 ? 0 : 2>());
+          probabilities(std::integral_constant<bool, kCap>());
         masks([&](int e, bool seen) {
           x[e] = seen ? x[e] : 0.f;
           w[e >> 1] &= seen ? 0xffffffffu : e & 1 ? 0x0000ffffu : 0xffff0000u;
@@ -909,6 +907,16 @@ static cudaError_t launch_pass(const DenseArgs& a, const CUtensorMap (&m)[4], in
   return launch_pdl(k_flash_bwd_join<kF16, kKeys>, dim3(2 * ctas, kKeys ? 8 : 4), 256, 0, st, true, a, ctas);
 }
 
+template <bool kF16, bool kKeys>
+static cudaError_t launch_gen(const DenseArgs& a, const CUtensorMap (&m)[4], int ctas, cudaStream_t st) {
+  switch (dense_gen(a)) {
+    case 0: return launch_pass<kF16, 0, kKeys>(a, m, ctas, st);
+    case 1: return launch_pass<kF16, 1, kKeys>(a, m, ctas, st);
+    case 2: return launch_pass<kF16, 2, kKeys>(a, m, ctas, st);
+    default: return launch_pass<kF16, 3, kKeys>(a, m, ctas, st);
+  }
+}
+
 template <bool kF16>
 static cudaError_t launch_type(DenseArgs a, cudaStream_t st) {
   const int ctas = dense_ctas();
@@ -938,9 +946,7 @@ static cudaError_t launch_type(DenseArgs a, cudaStream_t st) {
         !make_row_map(&m[2], q, a.type, rows, a.kv_heads, a.group, per) ||
         !make_row_map(&m[3], g, a.type, rows, a.kv_heads, a.group, per))
       return cudaErrorInvalidValue;
-    e = a.slopes ? launch_pass<kF16, 2, true>(a, m, ctas, st)
-        : a.cap > 0.f ? launch_pass<kF16, 1, true>(a, m, ctas, st)
-                      : launch_pass<kF16, 0, true>(a, m, ctas, st);
+    e = launch_gen<kF16, true>(a, m, ctas, st);
     if (e != cudaSuccess) return e;
   }
   if (a.rows > 0) {
@@ -948,9 +954,7 @@ static cudaError_t launch_type(DenseArgs a, cudaStream_t st) {
     if (!make_row_map(&m[0], q, a.type, rows, a.kv_heads, a.group, T) || !make_row_map(&m[1], g, a.type, rows, a.kv_heads, a.group, T) ||
         !make_key_map(&m[2], k, a.type, keys, 1, 0, a.kv_heads, kCols) || !make_key_map(&m[3], v, a.type, keys, 1, 0, a.kv_heads, kCols))
       return cudaErrorInvalidValue;
-    e = a.slopes ? launch_pass<kF16, 2, false>(a, m, ctas, st)
-        : a.cap > 0.f ? launch_pass<kF16, 1, false>(a, m, ctas, st)
-                      : launch_pass<kF16, 0, false>(a, m, ctas, st);
+    e = launch_gen<kF16, false>(a, m, ctas, st);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
