@@ -430,7 +430,8 @@ int ress_qkv_proj(const ress_dims* dims, const uint16_t* x, const uint16_t* W_q,
  * lse = -infinity.  Keys outside a sequence and pages' unused rows change nothing, whatever they
  * hold; K and V of a sequence's own keys should be finite (a masked key's infinity in V still
  * reaches rows by 0 x infinity).  Products are exact and summed in float32; the exponentials are
- * rounded to the tensors' type for their product with V, their sums are not.
+ * rounded to the tensors' type for their product with V (in f16 what is below 2^-25 of a row's largest counts as 0 there),
+ * their sums are not.
  *
  * Heads are [tokens, heads, 64] with strides in elements, multiples of 8 above 0 (any stride where
  * there is one head or one token), data 16-byte aligned.  Heads h g .. h g + g - 1 of Q use head h

@@ -404,7 +404,7 @@ __host__ __device__ constexpr uint32_t idesc16(int M, int N, bool b_mn_major) {
   return kF16 ? idesc_bf16_f32(M, N, b_mn_major) & ~((1u << 7) | (1u << 10)) : idesc_bf16_f32(M, N, b_mn_major);
 }
 
-// 64 bytes of a 128-byte row of a swizzled 64-row tile become 0; thread i of 128 takes half of row i / 2.
+// The rows of a 128-row tile from `from` on become 0; thread i of 256 takes 64 of the 128 bytes of row i / 2.
 __device__ __forceinline__ void zero_rows(uint8_t* tile, int from, int i) {
   if (i / 2 >= from) {
     uint4* p = reinterpret_cast<uint4*>(tile + (i / 2) * 128 + (i & 1) * 64);

@@ -321,14 +321,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     prefetch_tensormap(&tmB1);
     prefetch_tensormap(&tmB2);
   }
-  if (kKeys && T * G < kCols) {  // rows of a tile that no box reaches are summed over, times 0
-    for (int f = threadIdx.x; f < (int)(2 * kStages * kTileBytes / 16); f += kThreads)
-      reinterpret_cast<uint4*>(S.B1)[f] = make_uint4(0u, 0u, 0u, 0u);
-    fence_proxy_async_smem();
-  }
   if (const int r = (int)threadIdx.x - 512; r >= 0) {
     S.row_token[r] = r / G, S.row_head[r] = r % G;
-    // rows that no token fills stay 0, as in k_flash
+    // rows that no token fills stay 0, as in k_flash (where they are rows of a streamed tile they are summed over, times 0)
     if (r >= T * G) {
 #pragma unroll 1
       for (int i = 0; i < (kKeys ? 2 * kStages : 4) * 8; ++i)
