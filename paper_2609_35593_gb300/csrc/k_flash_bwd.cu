@@ -14,8 +14,8 @@
 // warps 4-19 element-wise: 16 rows x 64 columns of a tile of 128 x 128 each.  S and dP (256 columns of TMEM) are free for the next tile as soon as they are in registers, P and
 // dS (128) have columns of their own, so the products of the next tile run meanwhile; two accumulators (128).  With
 // eight element-wise warps on tiles of 64 columns and one issuer a tile of 128 x 64 took 1,700 cycles, its four
-// products 512 (8 images at once, 10,992 rows and keys of 16 heads: 2,200 us; now 1,394, 0.89 PFLOP/s of five products'
-// work or 1.24 of the seven formed).  What bounds it is the chain of a tile from scores to dS and back.  Shares of the work, partial results and waits are those of k_flash.cu.
+// products 512 (8 images at once, 10,992 rows and keys of 16 heads: 2,200 us; now 1,405 to 1,497, 0.83 to 0.88 PFLOP/s of five products'
+// work or 1.16 to 1.23 of the seven formed).  What bounds it is the chain of a tile from scores to dS and back.  Shares of the work, partial results and waits are those of k_flash.cu.
 //
 // In f16, P is kept times 2^8 and dS times a power of two: probabilities of rows on thousands of keys are below f16's 2^-14,
 // and so may gradients be.  |dP - delta| is at most 2 |dO| max|V| over the sequence's keys (norms over channels: O is a mean of
@@ -176,11 +176,16 @@ __global__ void __launch_bounds__(256) k_flash_rows(const __grid_constant__ Dens
       const int64_t c = quotient(u, heads), t0 = c * kTopRows + (lane >> 3);
       const int head = (int)(u - c * heads), h = head / a.group, g = head - h * a.group;
       uint4 o[kAtOnce], d[kAtOnce];
+      float lse[kAtOnce];
 #pragma unroll
       for (int i = 0; i < kAtOnce; ++i) {
         o[i] = d[i] = make_uint4(0u, 0u, 0u, 0u);
+        lse[i] = 0.f;
         const int64_t t = t0 + 4 * i;
-        if (t < hi) o[i] = ld_stream(row_at(a.o, t, head, sub)), d[i] = ld_stream(row_at(a.d_o, t, head, sub));
+        if (t < hi) {
+          o[i] = ld_stream(row_at(a.o, t, head, sub)), d[i] = ld_stream(row_at(a.d_o, t, head, sub));
+          lse[i] = a.lse[head * a.rows + t];
+        }
       }
 #pragma unroll
       for (int i = 0; i < kAtOnce; ++i) {
@@ -196,10 +201,9 @@ __global__ void __launch_bounds__(256) k_flash_rows(const __grid_constant__ Dens
         top = fmaxf(top, square);
         const int64_t t = t0 + 4 * i;
         if (sub == 0 && t < hi) {
-          const float lse = a.lse[head * a.rows + t];
           const int64_t at = ((int64_t)h * a.rows + t) * a.group + g;
           // a row that sees nothing: 2^(s - inf) = 0
-          a.stat[at] = make_float2(lse == -INFINITY ? INFINITY : lse * kLog2e, sum);
+          a.stat[at] = make_float2(lse[i] == -INFINITY ? INFINITY : lse[i] * kLog2e, sum);
           if (kF16) a.norm[at] = square;
         }
       }

@@ -8,8 +8,9 @@ torch = pytest.importorskip("torch")
 if not torch.cuda.is_available():
     pytest.skip("no CUDA device", allow_module_level=True)
 
+import paper_2609_35593_gb300 as ress  # noqa: E402
 from gradients64 import gradients  # noqa: E402
-from test_gpu_attn import F16, R, float32_by_default, normal, problem, run  # noqa: E402,F401
+from test_gpu_attn import F16, R, float32_by_default, normal, problem, run, workspace  # noqa: E402,F401
 from test_gpu_attn_bwd import grads  # noqa: E402
 
 pytestmark = pytest.mark.gpu
@@ -94,3 +95,26 @@ def test_neighbours_of_any_size(bad, causal):
         assert torch.equal(got[1][keys], want[1][keys]) and torch.equal(got[2][keys], want[2][keys])
 
 
+
+
+def test_captured_with_other_lengths():
+    """A replayed graph finds the powers of the sequences that it has then."""
+    heads, n = 4, 500
+    q, k, v = problem([n], [n], heads, 2, F16)
+    do = normal(9, *q.shape, kind=F16, by=0.1)
+    do[n // 2:] *= 2.0 ** -12
+    o, lse, out = torch.zeros_like(q), torch.zeros(heads, n, device="cuda"), [torch.zeros_like(t) for t in (q, k, v)]
+    starts, ws = R.starts([n, 0]), workspace(n, heads, True)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ress.attn(q, k, v, o, ws, starts, starts, lse=lse, causal=True)
+        ress.attn_bwd(do, q, k, v, o, lse, *out, ws, starts, starts, causal=True)
+    for lens in ([500, 0], [250, 250], [77, 423], [0, 500]):
+        starts.copy_(R.starts(lens))
+        graph.replay()
+        ress.status(ws)
+        for a, b in zip(grads(do, q, k, v, *run(q, k, v, lens, lens, causal=True), lens, lens, causal=True), out):
+            assert torch.equal(a, b)
+        want, off = gradients(do, q, k, v, o, lse, lens, lens, causal=True)
+        for g, w, f in zip(out, want, off):
+            R.close(g, w, f)
