@@ -18,8 +18,8 @@
 //               own: S of the next tile runs while the exponentials of this one are formed.
 // What bounds it is the chain of a slot's tile: scores from TMEM, exponentials, P to TMEM and the hand-overs between
 // warps, some 2,200 cycles of which the MMAs take 1,024, so the tiles are as large as TMEM allows, and the 16 warps of
-// softmax (four to a sub-partition) work while others wait.  8 images at once (10,992 rows and keys, 16 heads) take 437 us,
-// 1.13 PFLOP/s; other forms of the same results: a row per thread and 8 warps, S of 64 keys double-buffered under P 636,
+// softmax (four to a sub-partition) work while others wait.  8 images at once (10,992 rows and keys, 16 heads) take 440 to 456 us,
+// 1.1 PFLOP/s; other forms of the same results: a row per thread and 8 warps, S of 64 keys double-buffered under P 636,
 // 128 keys with S and P apart 618; 12 warps, three slots of 64 keys 586; 16 warps, four slots of 64 keys and two issuers
 // 553; this form at first 482 (its join looked for the shares itself, 25 us of that).
 // Rows of V behind a sequence's last key are zeroed in shared memory (0 x NaN of a cache page never written
@@ -159,7 +159,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (a.n_seqs > 32) range = find_range(a, line_of, gridDim.x, blockIdx.x, S.scratch, blockIdx.x == 0 ? a.status : nullptr);
 
   // 640 threads start with 96 registers each; the softmax warps, which hold a row's scores, get 104 of them
-  // (512 x 104 + 128 x 64 <= 640 x 96).  A spilled register would go to L2: shared memory leaves next to no L1.
+  // (512 x 104 + 128 x 64 <= 640 x 96).  A spilled register goes to L2, as shared memory leaves next to no L1
+  // (4 to 20 bytes are, see -Xptxas -v).
   if (warp < kSoftmax) {
     regs_dec<64>();
     if (warp == kProducer) {
