@@ -437,9 +437,9 @@ int ress_qkv_proj(const ress_dims* dims, const uint16_t* x, const uint16_t* W_q,
  * there is one head or one token), data 16-byte aligned.  Heads h g .. h g + g - 1 of Q use head h
  * of K and V, g = q_heads / kv_heads at most RESS_MAX_GROUP.  The starts of the sequences are device
  * data, so that a captured graph serves other lengths: q_start[n_seqs + 1] ascending; rows behind the last
- * sequence change nothing and are not written.  o and lse must not share memory with inputs or one another.  A start or a length
- * outside its tensor is recorded in the status word (RESS_EDEVICE); that sequence then has no rows
- * (or keys).  ws: 256-byte aligned, ress_attn_workspace_bytes(rows, q_heads, backward) bytes, a status
+ * sequence change nothing and are not written.  o and lse must not share memory with inputs or one
+ * another.  A start or a length outside its tensor is recorded in the status word (RESS_EDEVICE); that
+ * sequence then has no rows (or keys).  ws: 256-byte aligned, ress_attn_workspace_bytes(rows, q_heads, backward) bytes, a status
  * word first (zero before the first call, read by ress_status); the rest needs no initialisation.
  * Calls on one workspace must not overlap. */
 #define RESS_MAX_GROUP 64
@@ -467,9 +467,11 @@ int ress_attn(const ress_attn_args* a, void* ws, size_t ws_bytes, void* stream);
 /* Gradients of ress_attn with respect to q, k and v from that of o (d_o): a->o and a->lse as the call
  * wrote them (lse is needed here).  The gradients of heads of K and V that several heads of Q use are
  * added up in float32, in a fixed order.  p and the gradients of the scores are rounded to the
- * tensors' type for their products; in f16 after scaling by powers of two, so that they stay finite whatever v and d_o
- * are, and of a gradient of a score what is lost is below 2^-39 of 2 |d_o| max|v| (norms over channels, of its sequence; for dq
- * |d_o| of the row).  dq, dk, dv are written for the rows and keys of every sequence, and must not share memory with inputs or one another.  ws: the workspace of backward = 1. */
+ * tensors' type for their products; in f16 after scaling by powers of two, so that they stay finite
+ * whatever v and d_o are, and what is lost of a score's gradient is below 2^-39 of 2 |d_o| max|v| (norms
+ * over channels, the largest of its sequence; for dq |d_o| of the row).  dq, dk, dv are written for the
+ * rows and keys of every sequence, and must not share memory with inputs or one another.  ws: the
+ * workspace of backward = 1. */
 typedef struct {
   ress_heads d_o, dq; /* as q */
   ress_heads dk, dv;  /* as k */

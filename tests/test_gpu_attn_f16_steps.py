@@ -79,6 +79,13 @@ def test_gradients_of_nothing():
     check(q, k, v, do, ([50, 60], [50, 60]))
 
 
+def test_no_rows_or_no_keys():
+    """Alone, and between sequences that have both."""
+    for lens in (([0], [70]), ([70], [0]), ([40, 0, 30, 20], [50, 60, 0, 20])):
+        q, k, v = problem(*lens, 4, 2, F16)
+        check(q, k, v, normal(9, *q.shape, kind=F16), lens)
+
+
 @pytest.mark.parametrize("bad", [30000.0, -30000.0, math.inf, -math.inf, math.nan])
 @pytest.mark.parametrize("causal", [False, True])
 def test_neighbours_of_any_size(bad, causal):
